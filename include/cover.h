@@ -24,7 +24,8 @@
  *  - Kernels never trap. A kernel that gives up on an internal wait (bounded at
  *    about one second) records COVER_ERR_DEVICE_TIMEOUT in a per-device status
  *    word; read and clear it with cover_device_status().
- *  - Tensors are dense and contiguous (row-major, last index fastest).
+ *  - Tensors are dense and contiguous (row-major, last index fastest), but where an
+ *    entry point takes strides.
  */
 #ifndef COVER_H_
 #define COVER_H_
@@ -248,6 +249,95 @@ int cover_seed_kv_gather(const void* k, const void* v, const int32_t* seed_idx, 
 int cover_seed_kv_override(void* k, void* v, const int32_t* seed_idx, int n_seeds,
                            int B, int Hkv, int L, int D, int elem_bytes,
                            void* k_cache, void* v_cache, void* stream);
+
+/*
+ * Rotary positions of a layer's queries and keys, before the attention or the
+ * memory takes them (the paper's models rotate q and k; it gives no formula).
+ * Column pair i (0 <= i < R / 2) of a row at position t turns by t * inv_freq[i]
+ * radians:
+ *   y_a = mscale (x_a cos - x_b sin),  y_b = mscale (x_a sin + x_b cos),
+ * (a, b) = (2i, 2i + 1) if interleaved != 0, else (i, i + R / 2); with
+ * inverse != 0 by the opposite angle. That is the gradient too: d loss / d x is
+ * the inverse rotation (same mscale) of d loss / d y. Columns R .. D - 1 are
+ * copied. Contexts are stretched by the frequencies and mscale.
+ *
+ *   q, q_out [B, Hq, L, D], k, k_out [B, Hkv, L, D]: elements of elem_bytes (2: bf16, 4: fp32)
+ *   strides  HOST int64 [12]: strides in elements of (B, H, L) of q, k, q_out, k_out (the
+ *            last dimension is dense); read before the call returns. Rows laid out as a
+ *            projection leaves them ([B, L, H, D] in memory) need no transposition.
+ *   inv_freq [R / 2] fp64; the angle is reduced exactly modulo a turn, so positions
+ *            far out lose nothing
+ *   pos      [B, L] int32 position of every row (any value), or NULL: row l is at pos0 + l
+ * k is NULL and Hkv is 0 where only q is wanted. q_out may be q with the same
+ * strides (in place), likewise k; outputs that overlap an input in another way, or
+ * rows of one output that overlap, give unspecified results. L = 0 is a no-op.
+ * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B or Hq < 1, Hkv or
+ * L < 0, D < 1, R odd, negative or above D, elem_bytes not 2 or 4, a pointer that
+ * is not aligned to its elements; COVER_ERR_UNSUPPORTED for D > 4096;
+ * COVER_ERR_CUDA for a launch failure. Rows that are all 16-byte aligned (and R
+ * and D that split into 16-byte vectors) run on 16-byte accesses.
+ */
+int cover_rope_fwd(const void* q, const void* k, void* q_out, void* k_out, const int64_t* strides,
+                   int B, int Hq, int Hkv, int L, int D, int R,
+                   const double* inv_freq, const int32_t* pos, int pos0,
+                   int interleaved, float mscale, int inverse, int elem_bytes, void* stream);
+
+/*
+ * An 8-bit key/value memory (the prefix cache of Section 6.6 in half the bytes), per layer:
+ *   k8, v8       [B, Hkv, L, D] e4m3 codes
+ *   k_exp, v_exp [B, Hkv, L]    e8m0 exponent bytes, one a row
+ * A row's values are code * 2^(x - 127), x its byte; x = 255: the row reads as NaN. A power of two
+ * scales without rounding: every value is exact in bf16 and fp32.
+ *
+ * cover_kv8_write quantises rows as they are written: x is the smallest byte with
+ *   max |row| <= 448 * 2^(x - 127), held to 17 .. 246 (127 for a row of zeros); the codes are the nearest
+ *   e4m3 values of row * 2^(127 - x), ties to even, saturating. A row with an element
+ *   that is not finite is stored as NaN (x = 255, codes 0). k, v [B, Hkv, n, D] are bf16 (elem_bytes
+ *   2) or fp32 (4); strides: HOST int64 [6], strides in elements of (B, H, n) of k, v, the last
+ *   dimension dense. Slot s goes to position pos0 + s, or to pos[b, s] (int32 [B, n]) where pos is not
+ *   NULL: a listed position outside [0, L) is left out, and where a position is listed again
+ *   the lowest slot is taken (as in cover_attn_fwd). Every other row of the memory is left as it
+ *   was. With pos = seed_idx this overrides the memory at the seeds with their cached states.
+ * cover_kv8_read reads rows back into k, v [B, Hkv, n, D] (dense, bf16 or fp32): row s from
+ *   position pos0 + s or pos[b, s]; a listed position outside [0, L) reads as zeros.
+ *
+ * n = 0 is a no-op. Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hkv, L or D < 1, n < 0,
+ * elem_bytes not 2 or 4, pos0 < 0 or pos0 + n > L without a list, k, v, k8 or v8 not 16-byte
+ * aligned, a stride (of a dimension longer than 1) that is not a multiple of 16 bytes;
+ * COVER_ERR_UNSUPPORTED for D other than 64 and 128, or B > 65535; COVER_ERR_CUDA for a launch failure.
+ */
+int cover_kv8_write(const void* k, const void* v, const int64_t* strides,
+                    const int32_t* pos, int pos0, int n, int B, int Hkv, int L, int D, int elem_bytes,
+                    void* k8, void* v8, uint8_t* k_exp, uint8_t* v_exp, void* stream);
+int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const uint8_t* v_exp,
+                   const int32_t* pos, int pos0, int n, int B, int Hkv, int L, int D, int elem_bytes,
+                   void* k, void* v, void* stream);
+
+/*
+ * cover_attn_fwd_prefix over an 8-bit memory (k8, v8, k_exp, v_exp as above, Lk positions; D = 128): bf16
+ * queries q [B, Hq, Lq, D] at memory positions q0 + r, bf16 out, fp32 lse (NULL = skip), and the seeds'
+ * masked-input pairs k_seedmask, v_seedmask [B, Hkv, n_seeds, D] in bf16. In addition:
+ *   key_lo, key_hi [B, Lq] int32 or NULL (0, Lk): row r of batch row b sees the keys key_lo <= j < key_hi
+ *     only (held to 0 .. Lk): a padded batch's lengths, a prefix, blocks that see themselves and
+ *     those before, documents. A row that sees no key gets out = 0, lse = -inf.
+ *     A seed row's own pair is seen where its position is.
+ *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c).
+ * What a row does not see does not reach it, NaN included; a row that sees a key with
+ * k_exp or v_exp 255 gets NaN in out and lse.
+ * workspace: cover_attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) bytes, 16-byte aligned, no initialisation
+ * needed (NULL if that is 0). It is scratch of the call alone: calls that share one must not
+ * run concurrently on the GPU.
+ * Errors as cover_attn_fwd_prefix, plus COVER_ERR_INVALID_ARG for NULL k_exp or v_exp, a missing
+ * workspace, and a softcap that is negative or not finite.
+ */
+size_t cover_attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk);
+int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8,
+                           const uint8_t* k_exp, const uint8_t* v_exp,
+                           const void* k_seedmask, const void* v_seedmask,
+                           const int32_t* seed_idx, int n_seeds,
+                           int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D,
+                           const int32_t* key_lo, const int32_t* key_hi, float softcap,
+                           void* out, float* lse, void* workspace, void* stream);
 
 /*
  * One decoding step's decisions, fused behind the scoring pass

@@ -21,7 +21,8 @@ _native = None
 # the entry points that the native marshalling (_binding) calls, in the order it binds them
 _BOUND = ("cover_attn_fwd", "cover_attn_fwd_f32", "cover_attn_fwd_prefix", "cover_attn_fwd_prefix_f32",
           "cover_score_fwd", "cover_score_decide_fwd", "cover_attn_mass_fwd", "cover_seed_kv_gather",
-          "cover_seed_kv_override")
+          "cover_seed_kv_override", "cover_rope_fwd", "cover_kv8_write", "cover_kv8_read",
+          "cover_attn_prefix8_workspace_bytes", "cover_attn_fwd_prefix8")
 
 # name -> (restype, argtypes)
 _SIGNATURES = {
@@ -36,6 +37,12 @@ _SIGNATURES = {
     "cover_score_fwd_noalloc": (_I, [_P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P]),
     "cover_seed_kv_gather": (_I, [_P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P]),
     "cover_seed_kv_override": (_I, [_P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P]),
+    "cover_rope_fwd": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _I, _I, ctypes.c_float, _I, _I, _P]),
+    "cover_kv8_write": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P]),
+    "cover_kv8_read": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P]),
+    "cover_attn_prefix8_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I, _I]),
+    "cover_attn_fwd_prefix8": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P,
+                                    ctypes.c_float, _P, _P, _P, _P]),
     "cover_decide_workspace_bytes": (ctypes.c_size_t, [_I, _I]),
     "cover_score_decide_fwd": (_I, [_P, _I, _I, _I, _P, _P, _P, ctypes.c_float, _I, _I, _I, _I, _I, _I, _I,
                                     _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
@@ -91,7 +98,7 @@ class _Declines:
     def attn(*args):
         return None
 
-    score = decide = mass = kv = attn
+    score = decide = mass = kv = rope = kv8_write = kv8_read = attn8 = attn
 
 
 def native():

@@ -9,6 +9,7 @@ Python path behind it takes every other form and raises the errors.
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional
 
 import torch
@@ -327,6 +328,298 @@ def cover_seed_kv_override(k, v, seed_idx, k_cache, v_cache, *, stream=None):
     if seed_idx is not None and seed_idx.shape[1] > 0 and (k_cache is None or v_cache is None):
         raise ValueError("k_cache and v_cache are required")
     return _seed_kv("cover_seed_kv_override", k, v, seed_idx, k_cache, v_cache, stream)
+
+
+def _rows_need(t, name: str, dtypes, device=None):
+    """A [B, H, L, D] tensor of rows whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have 4 dims, got {tuple(t.shape)}")
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} must be on {device}, got {t.device}")
+
+
+def _strides(*tensors):
+    """Their strides of the first three dimensions, in elements, 0 where a dimension has one entry."""
+    vals = [t.stride(i) if t.shape[i] > 1 else 0 for t in tensors for i in range(3)]
+    return (ctypes.c_int64 * len(vals))(*vals)
+
+
+def _launch(fn_name, device, stream, args, made=()):
+    """Calls the entry point on the tensors' device. Tensors made for the call are not handed out again by the
+    allocator before another stream that was given is done with them."""
+    with torch.cuda.device(device):
+        s = _stream(stream)
+        if stream is not None and s != torch.cuda.current_stream().cuda_stream:
+            on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(s, device=device)
+            for t in made:
+                t.record_stream(on)
+        code = getattr(_lib.load(), fn_name)(*args, s)
+    _lib.check(fn_name, code)
+
+
+_ROWS = (torch.bfloat16, torch.float32)
+
+
+def _span(t):
+    """The bytes that a tensor's elements lie in, as (first, end)."""
+    if t.numel() == 0:
+        return 0, 0
+    lo = t.data_ptr() + t.element_size() * sum(min(0, (n - 1) * st) for n, st in zip(t.shape, t.stride()))
+    hi = t.data_ptr() + t.element_size() * (1 + sum(max(0, (n - 1) * st) for n, st in zip(t.shape, t.stride())))
+    return lo, hi
+
+
+def _overlap(a, b):
+    (a0, a1), (b0, b1) = _span(a), _span(b)
+    return a0 < b1 and b0 < a1
+
+
+def _rope_out(x, out, name, others):
+    """The output for x: a new dense tensor, x itself (in place), or one that overlaps none of ``others``."""
+    if out is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _rows_need(out, name, (x.dtype,), x.device)
+    if out.shape != x.shape:
+        raise ValueError(f"{name} must have the shape {tuple(x.shape)}")
+    if any(n > 1 and st == 0 for n, st in zip(out.shape, out.stride())):
+        raise ValueError(f"{name} must not be expanded")
+    in_place = out.data_ptr() == x.data_ptr() and out.stride() == x.stride()
+    if not in_place and any(_overlap(out, t) for t in others if t is not None):
+        raise ValueError(f"{name} must be its input or overlap none of the tensors")
+    return out
+
+
+def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool = False, mscale: float = 1.0,
+                   inverse: bool = False, out_q=None, out_k=None, stream=None):
+    """Rotary positions of queries and keys. Returns (q, k) turned, dense unless out_q / out_k are given (which may be
+    q / k themselves: in place).
+
+    q [B, Hq, L, D], k [B, Hkv, L, D] (or None): bf16 or fp32, dense in the last dimension only (a projection's
+    [B, L, H, D] transposed will do). inv_freq: fp64 [R / 2], radians per position (rope_frequencies); the first
+    R columns turn, in pairs (2i, 2i + 1) if ``interleaved``, else (i, i + R / 2). pos: int32 [B, L], or row l is
+    at pos0 + l. ``inverse`` turns back, which is the gradient with respect to q and k too.
+    """
+    if stream is None and out_q is None and out_k is None and type(mscale) is float:
+        r = (_nat or _native()).rope(q, k, inv_freq, pos, pos0, interleaved, mscale, inverse)
+        if r is not None:
+            return _done("cover_rope_fwd", r)
+    _rows_need(q, "q", _ROWS)
+    B, Hq, L, D = q.shape
+    dev = q.device
+    if k is not None:
+        _rows_need(k, "k", (q.dtype,), dev)
+        if k.shape[0] != B or tuple(k.shape[2:]) != (L, D):
+            raise ValueError("k must be [B, Hkv, L, D] matching q")
+    _need(inv_freq, "inv_freq", torch.float64, 1)
+    if pos is not None:
+        _need(pos, "pos", torch.int32, 2)
+        if tuple(pos.shape) != (B, L):
+            raise ValueError("pos must be [B, L]")
+    _same_device(dev, inv_freq=inv_freq, pos=pos)
+    if 2 * inv_freq.shape[0] > D:
+        raise ValueError("inv_freq must have at most D / 2 entries")
+    oq = _rope_out(q, out_q, "out_q", (q, k, out_k))
+    ok = None if k is None else _rope_out(k, out_k, "out_k", (q, k, oq))
+    has_k = k is not None and k.shape[1] > 0
+    st = _strides(q, k if has_k else q, oq, ok if has_k else oq)
+    _launch("cover_rope_fwd", dev, stream,
+            (_ptr(q), _ptr(k) if has_k else None, _ptr(oq), _ptr(ok) if has_k else None, ctypes.addressof(st), B, Hq,
+             k.shape[1] if has_k else 0, L, D, 2 * inv_freq.shape[0], _ptr(inv_freq) or None, _ptr(pos), int(pos0),
+             1 if interleaved else 0, float(mscale), 1 if inverse else 0, q.element_size()),
+            [t for t, given in ((oq, out_q), (ok, out_k)) if t is not None and given is None])
+    return oq, ok
+
+
+def rope_frequencies(R: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
+                     trained: int = 4096, slow: float = 1.0, fast: float = 32.0, device=None):
+    """(inv_freq, mscale) for cover_rope_fwd: R / 2 frequencies base^(-2i / R) in fp64, stretched by ``factor`` for
+    contexts longer than the ``trained`` one.
+
+    scaling: "none"; "linear": every frequency divided by the factor; "ntk": the base raised so that the slowest
+    frequency is divided by it and the fastest kept; "yarn": pairs that turn at most ``slow`` times in the trained
+    context are divided, those that turn ``fast`` times or more are kept, with a ramp between, and mscale =
+    0.1 ln(factor) + 1.
+    """
+    if R < 2 or R % 2:
+        raise ValueError("R must be even and at least 2")
+    if not factor >= 1.0:
+        raise ValueError("factor must be at least 1")
+    i = torch.arange(R // 2, dtype=torch.float64)
+    mscale = 1.0
+    if scaling == "ntk" and R > 2:
+        base = base * factor ** (R / (R - 2))
+    f = base ** (-2.0 * i / R)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        if not fast > slow:
+            raise ValueError("fast must be above slow")
+        keep = ((trained * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+        mscale = 0.1 * math.log(factor) + 1.0
+    elif scaling not in ("none", "ntk"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.to(device or "cuda"), mscale
+
+
+def kv8_memory(B: int, Hkv: int, L: int, D: int = 128, device=None):
+    """An 8-bit key/value memory of zeros: (k8, v8, k_exp, v_exp), e4m3 codes [B, Hkv, L, D] and e8m0 bytes
+    [B, Hkv, L]."""
+    codes = [torch.zeros((B, Hkv, L, D), dtype=torch.uint8, device=device or "cuda").view(torch.float8_e4m3fn)
+             for _ in range(2)]
+    exps = [torch.full((B, Hkv, L), 127, dtype=torch.uint8, device=device or "cuda") for _ in range(2)]
+    return codes[0], codes[1], exps[0], exps[1]
+
+
+def _kv8_need(k8, v8, k_exp, v_exp):
+    _need(k8, "k8", torch.float8_e4m3fn, 4)
+    _need(v8, "v8", torch.float8_e4m3fn, 4)
+    _need(k_exp, "k_exp", torch.uint8, 3)
+    _need(v_exp, "v_exp", torch.uint8, 3)
+    if v8.shape != k8.shape or k_exp.shape != k8.shape[:3] or v_exp.shape != k8.shape[:3]:
+        raise ValueError("v8 must match k8 [B, Hkv, L, D], and k_exp, v_exp be [B, Hkv, L]")
+    _same_device(k8.device, v8=v8, k_exp=k_exp, v_exp=v_exp)
+
+
+def _kv8_pos(pos, B, n, device):
+    if pos is None:
+        return
+    _need(pos, "pos", torch.int32, 2)
+    if tuple(pos.shape) != (B, n):
+        raise ValueError("pos must be [B, n]")
+    _same_device(device, pos=pos)
+
+
+def cover_kv8_write(k, v, k8, v8, k_exp, v_exp, *, pos=None, pos0: int = 0, stream=None) -> None:
+    """Quantise rows k, v [B, Hkv, n, D] (bf16 or fp32, rows 16-byte aligned, in any layout that is dense in the last
+    dimension) into the memory, in place: slot s at position pos0 + s, or at pos[b, s] (int32 [B, n]; entries
+    outside the memory are left out, of those that name one position the lowest slot is taken)."""
+    if stream is None:
+        r = (_nat or _native()).kv8_write(k, v, k8, v8, k_exp, v_exp, pos, pos0)
+        if r is not None:
+            return None if r is True else _done("cover_kv8_write", r)
+    _kv8_need(k8, v8, k_exp, v_exp)
+    B, Hkv, L, D = k8.shape
+    _rows_need(k, "k", _ROWS, k8.device)
+    _rows_need(v, "v", (k.dtype,), k8.device)
+    n = k.shape[2]
+    if tuple(k.shape) != (B, Hkv, n, D) or v.shape != k.shape:
+        raise ValueError("k and v must be [B, Hkv, n, D] matching the memory")
+    _kv8_pos(pos, B, n, k8.device)
+    st = _strides(k, v)
+    _launch("cover_kv8_write", k8.device, stream,
+            (_ptr(k), _ptr(v), ctypes.addressof(st), _ptr(pos) if n else None, int(pos0), n, B, Hkv, L, D, k.element_size(),
+             _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp)))
+
+
+def cover_kv8_read(k8, v8, k_exp, v_exp, *, pos=None, pos0: int = 0, n: Optional[int] = None, dtype=torch.bfloat16,
+                   stream=None):
+    """Read rows of the memory back: (k, v) [B, Hkv, n, D] in bf16 or fp32, exactly. Row s comes from position pos0 + s
+    (n rows; to the end of the memory if None) or pos[b, s] (int32 [B, n]; zeros for entries outside it)."""
+    if stream is None and dtype in _ROWS:
+        r = (_nat or _native()).kv8_read(k8, v8, k_exp, v_exp, pos, pos0, n, dtype is torch.float32)
+        if r is not None:
+            return _done("cover_kv8_read", r)
+    _kv8_need(k8, v8, k_exp, v_exp)
+    if dtype not in _ROWS:
+        raise TypeError(f"dtype must be torch.bfloat16 or torch.float32, got {dtype}")
+    B, Hkv, L, D = k8.shape
+    if n is None:
+        n = int(pos.shape[1]) if pos is not None else max(0, L - int(pos0))
+    if n < 0:
+        raise ValueError("n must not be negative")
+    _kv8_pos(pos, B, n, k8.device)
+    k = torch.empty((B, Hkv, n, D), dtype=dtype, device=k8.device)
+    v = torch.empty_like(k)
+    _launch("cover_kv8_read", k8.device, stream,
+            (_ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(pos) if n else None, int(pos0), n, B, Hkv, L, D,
+             k.element_size(), _ptr(k) if n else None, _ptr(v) if n else None), (k, v))
+    return k, v
+
+
+def cover_attn_prefix8_workspace_bytes(B: int, Hq: int, Hkv: int, Lq: int, Lk: int) -> int:
+    return int(_lib.load().cover_attn_prefix8_workspace_bytes(int(B), int(Hq), int(Hkv), int(Lq), int(Lk)))
+
+
+def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0: int,
+                           key_lo=None, key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True,
+                           workspace=None, stream=None):
+    """cover_attn_fwd_prefix over an 8-bit memory. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
+
+    key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees (all where None; none: out 0, lse -inf).
+    softcap c > 0: scores become c tanh(score / c). workspace: uint8, at least cover_attn_prefix8_workspace_bytes,
+    scratch of the call; allocated where None.
+    """
+    if stream is None and type(softcap) is float:
+        r = (_nat or _native()).attn8(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
+                                      softcap, out, lse, want_lse, workspace)
+        if r is not None:
+            return _done("cover_attn_fwd_prefix8", r)
+    _need(q, "q", torch.bfloat16, 4)
+    _kv8_need(k8, v8, k_exp, v_exp)
+    B, Hq, Lq, D = q.shape
+    Hkv, Lk = k8.shape[1], k8.shape[2]
+    dev = q.device
+    if tuple(k8.shape) != (B, Hkv, Lk, D):
+        raise ValueError("the memory must be [B, Hkv, Lk, D] matching q")
+    S = 0 if seed_idx is None else int(seed_idx.shape[1])
+    if S > 0:
+        _need(seed_idx, "seed_idx", torch.int32, 2)
+        _need(k_seedmask, "k_seedmask", torch.bfloat16, 4)
+        _need(v_seedmask, "v_seedmask", torch.bfloat16, 4)
+        if tuple(seed_idx.shape) != (B, S):
+            raise ValueError("seed_idx must be [B, S]")
+        if tuple(k_seedmask.shape) != (B, Hkv, S, D) or tuple(v_seedmask.shape) != (B, Hkv, S, D):
+            raise ValueError("k_seedmask / v_seedmask must be [B, Hkv, S, D]")
+        _same_device(dev, seed_idx=seed_idx, k_seedmask=k_seedmask, v_seedmask=v_seedmask)
+    for name, t in (("key_lo", key_lo), ("key_hi", key_hi)):
+        if t is not None:
+            _need(t, name, torch.int32, 2)
+            if tuple(t.shape) != (B, Lq):
+                raise ValueError(f"{name} must be [B, Lq]")
+    made = []
+    if out is None:
+        out = torch.empty_like(q)
+        made.append(out)
+    else:
+        _need(out, "out", torch.bfloat16, 4)
+        if out.shape != q.shape:
+            raise ValueError("out must match q")
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=dev)
+        made.append(lse)
+    elif lse is not None:
+        _need(lse, "lse", torch.float32, 3)
+        if tuple(lse.shape) != (B, Hq, Lq):
+            raise ValueError("lse must be [B, Hq, Lq]")
+    nbytes = cover_attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, 1)
+        if workspace.numel() < nbytes:
+            raise ValueError(f"workspace must have at least {nbytes} bytes")
+    elif nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        made.append(workspace)
+    _same_device(dev, k8=k8, key_lo=key_lo, key_hi=key_hi, out=out, lse=lse, workspace=workspace)
+    _launch("cover_attn_fwd_prefix8", dev, stream,
+            (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
+             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, int(q0), D,
+             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(workspace) if nbytes else None), made)
+    return out, lse
 
 
 def cover_decide_workspace_bytes(N: int, n_seq: int) -> int:

@@ -37,6 +37,11 @@ decltype(&cover_score_decide_fwd) f_decide;
 decltype(&cover_attn_mass_fwd) f_mass;
 decltype(&cover_seed_kv_gather) f_gather;
 decltype(&cover_seed_kv_override) f_override;
+decltype(&cover_rope_fwd) f_rope;
+decltype(&cover_kv8_write) f_kv8_write;
+decltype(&cover_kv8_read) f_kv8_read;
+decltype(&cover_attn_prefix8_workspace_bytes) f_attn8_bytes;
+decltype(&cover_attn_fwd_prefix8) f_attn8;
 
 bool none(PyObject* o) { return o == Py_None; }
 
@@ -69,6 +74,26 @@ struct Args {
     for (const int64_t n : t.sizes()) need(n <= INT_MAX);
     return t;
   }
+
+  // A [B, H, L, D] tensor of bf16 or fp32 rows on the current device that is dense in its last dimension.
+  const Tensor& rows(PyObject* o) {
+    const Tensor& t = any_tensor(o);
+    if (!ok) return t;
+    need((t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat) && t.is_cuda() && t.dim() == 4);
+    if (!ok) return t;
+    need(t.size(3) <= 1 || t.stride(3) == 1);
+    for (const int64_t n : t.sizes()) need(n <= INT_MAX);
+    here(t);
+    return t;
+  }
+
+  // A contiguous tensor on the current device.
+  const Tensor& local(PyObject* o, at::ScalarType dtype, int dims) {
+    const Tensor& t = tensor(o, dtype, dims);
+    if (ok) here(t);
+    return t;
+  }
+  void here(const Tensor& t) { need(t.get_device() == c10::cuda::current_device()); }
 
   template <typename T>
   T* pointer(PyObject* o, at::ScalarType dtype, int dims) {
@@ -371,17 +396,217 @@ PyObject* kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The strides of t's first three dimensions, 0 where a dimension has one entry.
+void strides_of(const Tensor& t, int64_t* s) {
+  for (int i = 0; i < 3; ++i) s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+}
+
+// rope(q, k, inv_freq, pos, pos0, interleaved, mscale, inverse)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor &q = in.rows(a[0]), &f = in.local(a[2], at::kDouble, 1);
+    if (!in.ok) return nullptr;
+    const bool has_k = !none(a[1]);
+    const Tensor& k = has_k ? in.rows(a[1]) : q;
+    if (!in.ok) return nullptr;
+    const int B = dim(q, 0), Hq = dim(q, 1), L = dim(q, 2), D = dim(q, 3), Hkv = has_k ? dim(k, 1) : 0;
+    in.need(k.scalar_type() == q.scalar_type() && dim(k, 0) == B && dim(k, 2) == L && dim(k, 3) == D &&
+            2 * f.size(0) <= D && q.numel() > 0 && f.numel() > 0 && (!has_k || Hkv > 0));
+    const int32_t* pos = nullptr;
+    if (in.ok && !none(a[3])) {
+      const Tensor& t = in.local(a[3], at::kInt, 2);
+      in.need(in.ok && t.size(0) == B && t.size(1) == L);
+      if (in.ok) pos = ptr<int32_t>(t);
+    }
+    const int pos0 = in.integer(a[4]), inter = in.truth(a[5]) ? 1 : 0, inverse = in.truth(a[7]) ? 1 : 0;
+    const float mscale = static_cast<float>(in.real(a[6]));
+    if (!in.ok) return nullptr;
+    Tensor oq = empty(q.sizes(), q.scalar_type(), q), ok;
+    if (has_k) ok = empty(k.sizes(), k.scalar_type(), k);
+    int64_t st[12];
+    strides_of(q, st);
+    strides_of(k, st + 3);
+    strides_of(oq, st + 6);
+    strides_of(has_k ? ok : oq, st + 9);
+    const void *pq = ptr<void>(q), *pk = has_k ? ptr<void>(k) : nullptr;
+    void *po = ptr<void>(oq), *pok = has_k ? ptr<void>(ok) : nullptr, *stream = c10::cuda::getCurrentCUDAStream().stream();
+    const double* pf = ptr<double>(f);
+    const int R = 2 * dim(f, 0), elem = static_cast<int>(q.element_size());
+    const int rc = call(launched, [&] {
+      return f_rope(pq, pk, po, pok, st, B, Hq, Hkv, L, D, R, pf, pos, pos0, inter, mscale, inverse, elem, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return pair(Py_None, std::move(oq), Py_None, std::move(ok));
+  });
+}
+
+// An 8-bit memory: a[0 .. 3] = k8, v8, k_exp, v_exp.
+struct Memory8 {
+  void *k8, *v8;
+  uint8_t *k_exp, *v_exp;
+  int B, Hkv, L, D;
+  Memory8(Args& in, PyObject* const* a) {
+    const Tensor &k = in.local(a[0], at::kFloat8_e4m3fn, 4), &v = in.local(a[1], at::kFloat8_e4m3fn, 4);
+    const Tensor &ke = in.local(a[2], at::kByte, 3), &ve = in.local(a[3], at::kByte, 3);
+    if (!in.ok) return;
+    in.need(v.sizes() == k.sizes() && ke.sizes() == k.sizes().slice(0, 3) && ve.sizes() == ke.sizes());
+    B = dim(k, 0), Hkv = dim(k, 1), L = dim(k, 2), D = dim(k, 3);
+    k8 = ptr<void>(k), v8 = ptr<void>(v), k_exp = ptr<uint8_t>(ke), v_exp = ptr<uint8_t>(ve);
+  }
+};
+
+// kv8_write(k, v, k8, v8, k_exp, v_exp, pos, pos0): True once it is launched
+PyObject* kv8_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor &k = in.rows(a[0]), &v = in.rows(a[1]);
+    if (!in.ok) return nullptr;
+    const Memory8 m(in, a + 2);
+    if (!in.ok) return nullptr;
+    const int rows = dim(k, 2);
+    in.need(v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes() && dim(k, 0) == m.B && dim(k, 1) == m.Hkv &&
+            dim(k, 3) == m.D && rows > 0);
+    const int32_t* pos = nullptr;
+    if (in.ok && !none(a[6])) {
+      const Tensor& t = in.local(a[6], at::kInt, 2);
+      in.need(in.ok && t.size(0) == m.B && t.size(1) == rows);
+      if (in.ok) pos = ptr<int32_t>(t);
+    }
+    const int pos0 = in.integer(a[7]);
+    if (!in.ok) return nullptr;
+    int64_t st[6];
+    strides_of(k, st);
+    strides_of(v, st + 3);
+    const void *pk = ptr<void>(k), *pv = ptr<void>(v);
+    const int elem = static_cast<int>(k.element_size());
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] {
+      return f_kv8_write(pk, pv, st, pos, pos0, rows, m.B, m.Hkv, m.L, m.D, elem, m.k8, m.v8, m.k_exp, m.v_exp, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+  });
+}
+
+// kv8_read(k8, v8, k_exp, v_exp, pos, pos0, n, f32)
+PyObject* kv8_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&](Args& in, bool& launched) -> PyObject* {
+    const Memory8 m(in, a);
+    if (!in.ok) return nullptr;
+    const int pos0 = in.integer(a[5]);
+    const int32_t* pos = nullptr;
+    int rows = m.L - pos0;
+    if (!none(a[4])) {
+      const Tensor& t = in.local(a[4], at::kInt, 2);
+      if (!in.ok) return nullptr;
+      rows = dim(t, 1);
+      in.need(t.size(0) == m.B);
+      pos = ptr<int32_t>(t);
+    }
+    if (!none(a[6])) {
+      const int given = in.integer(a[6]);
+      in.need(pos == nullptr || given == rows);
+      rows = given;
+    }
+    const at::ScalarType dt = in.truth(a[7]) ? at::kFloat : at::kBFloat16;
+    in.need(pos0 >= 0 && rows > 0);
+    if (!in.ok) return nullptr;
+    const Tensor& like = THPVariable_Unpack(a[0]);
+    Tensor k = empty({m.B, m.Hkv, rows, m.D}, dt, like), v = empty({m.B, m.Hkv, rows, m.D}, dt, like);
+    void *pk = ptr<void>(k), *pv = ptr<void>(v), *stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int elem = dt == at::kFloat ? 4 : 2;
+    const int rc = call(launched, [&] {
+      return f_kv8_read(m.k8, m.v8, m.k_exp, m.v_exp, pos, pos0, rows, m.B, m.Hkv, m.L, m.D, elem, pk, pv, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return pair(Py_None, std::move(k), Py_None, std::move(v));
+  });
+}
+
+// attn8(q, k8, v8, k_exp, v_exp, km, vm, seed_idx, q0, key_lo, key_hi, softcap, out, lse, want_lse, workspace)
+PyObject* attn8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor& q = in.local(a[0], at::kBFloat16, 4);
+    if (!in.ok) return nullptr;
+    const Memory8 m(in, a + 1);
+    if (!in.ok) return nullptr;
+    const int B = dim(q, 0), Hq = dim(q, 1), Lq = dim(q, 2);
+    in.need(m.B == B && m.D == dim(q, 3) && q.numel() > 0 && m.L > 0 && m.Hkv > 0);
+    int S = 0;
+    const void *km = nullptr, *vm = nullptr;
+    const int32_t* idx = nullptr;
+    if (!none(a[7])) {
+      const Tensor& seeds = in.any_tensor(a[7]);
+      if (!in.ok || seeds.dim() != 2) return nullptr;
+      if (seeds.size(1) > 0) {
+        const Tensor &si = in.local(a[7], at::kInt, 2), &tk = in.local(a[5], at::kBFloat16, 4),
+                     &tv = in.local(a[6], at::kBFloat16, 4);
+        if (!in.ok) return nullptr;
+        S = dim(si, 1);
+        in.need(dim(si, 0) == B && dim(tk, 0) == B && dim(tk, 1) == m.Hkv && dim(tk, 2) == S && dim(tk, 3) == m.D &&
+                tv.sizes() == tk.sizes());
+        km = ptr<void>(tk), vm = ptr<void>(tv), idx = ptr<int32_t>(si);
+      }
+    }
+    const int32_t* range[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2; ++i) {
+      if (none(a[9 + i])) continue;
+      const Tensor& t = in.local(a[9 + i], at::kInt, 2);
+      in.need(in.ok && t.size(0) == B && t.size(1) == Lq);
+      if (!in.ok) return nullptr;
+      range[i] = ptr<int32_t>(t);
+    }
+    const int q0 = in.integer(a[8]);
+    const float cap = static_cast<float>(in.real(a[11]));
+    void* out = nullptr;
+    float* lse = nullptr;
+    if (!none(a[12])) {
+      const Tensor& t = in.local(a[12], at::kBFloat16, 4);
+      in.need(in.ok && t.sizes() == q.sizes());
+      if (in.ok) out = ptr<void>(t);
+    }
+    if (!none(a[13])) {
+      const Tensor& t = in.local(a[13], at::kFloat, 3);
+      in.need(in.ok && t.sizes() == q.sizes().slice(0, 3));
+      if (in.ok) lse = ptr<float>(t);
+    }
+    const bool make_lse = none(a[13]) && in.truth(a[14]);
+    if (!in.ok) return nullptr;
+    const size_t bytes = f_attn8_bytes(B, Hq, m.Hkv, Lq, m.L);
+    void* ws = nullptr;
+    Tensor new_out, new_lse, new_ws;
+    if (!none(a[15])) {
+      const Tensor& t = in.local(a[15], at::kByte, 1);
+      in.need(in.ok && static_cast<size_t>(t.numel()) >= bytes);
+      if (!in.ok) return nullptr;
+      ws = bytes > 0 ? ptr<void>(t) : nullptr;
+    } else if (bytes > 0) {
+      ws = ptr<void>(new_ws = empty({static_cast<int64_t>(bytes)}, at::kByte, q));
+    }
+    if (out == nullptr) out = ptr<void>(new_out = empty(q.sizes(), at::kBFloat16, q));
+    if (make_lse) lse = ptr<float>(new_lse = empty(q.sizes().slice(0, 3), at::kFloat, q));
+    const void* pq = ptr<void>(q);
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] {
+      return f_attn8(pq, m.k8, m.v8, m.k_exp, m.v_exp, km, vm, idx, S, B, Hq, m.Hkv, Lq, m.L, q0, m.D, range[0], range[1],
+                     cap, out, lse, ws, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return pair(a[12], std::move(new_out), a[13], std::move(new_lse));
+  });
+}
+
 // bind(addresses): the entry points' addresses, in the order below
 PyObject* bind(PyObject*, PyObject* list) {
-  unsigned long long p[9];
+  constexpr int kBound = 14;
+  unsigned long long p[kBound];
   PyObject* t = PySequence_Tuple(list);
   if (t == nullptr) return nullptr;
-  if (PyTuple_GET_SIZE(t) != 9) {
+  if (PyTuple_GET_SIZE(t) != kBound) {
     Py_DECREF(t);
-    PyErr_SetString(PyExc_ValueError, "nine addresses are expected");
+    PyErr_SetString(PyExc_ValueError, "fourteen addresses are expected");
     return nullptr;
   }
-  for (int i = 0; i < 9; ++i) p[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(t, i));
+  for (int i = 0; i < kBound; ++i) p[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(t, i));
   Py_DECREF(t);
   if (PyErr_Occurred()) return nullptr;
   const auto at = [&](int i) { return reinterpret_cast<void*>(static_cast<uintptr_t>(p[i])); };
@@ -394,6 +619,11 @@ PyObject* bind(PyObject*, PyObject* list) {
   f_mass = reinterpret_cast<decltype(f_mass)>(at(6));
   f_gather = reinterpret_cast<decltype(f_gather)>(at(7));
   f_override = reinterpret_cast<decltype(f_override)>(at(8));
+  f_rope = reinterpret_cast<decltype(f_rope)>(at(9));
+  f_kv8_write = reinterpret_cast<decltype(f_kv8_write)>(at(10));
+  f_kv8_read = reinterpret_cast<decltype(f_kv8_read)>(at(11));
+  f_attn8_bytes = reinterpret_cast<decltype(f_attn8_bytes)>(at(12));
+  f_attn8 = reinterpret_cast<decltype(f_attn8)>(at(13));
   Py_RETURN_NONE;
 }
 
@@ -403,6 +633,10 @@ PyMethodDef methods[] = {
     {"decide", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decide)), METH_FASTCALL, nullptr},
     {"mass", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mass)), METH_FASTCALL, nullptr},
     {"kv", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv)), METH_FASTCALL, nullptr},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope)), METH_FASTCALL, nullptr},
+    {"kv8_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv8_write)), METH_FASTCALL, nullptr},
+    {"kv8_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv8_read)), METH_FASTCALL, nullptr},
+    {"attn8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn8)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -205,6 +205,87 @@ int cover_seed_kv_override(void* k, void* v, const int32_t* seed_idx, int n_seed
   return seed_kv_call(true, k, v, seed_idx, n_seeds, B, Hkv, L, D, elem_bytes, k_cache, v_cache, stream);
 }
 
+int cover_rope_fwd(const void* q, const void* k, void* q_out, void* k_out, const int64_t* strides, int B, int Hq,
+                   int Hkv, int L, int D, int R, const double* inv_freq, const int32_t* pos, int pos0,
+                   int interleaved, float mscale, int inverse, int elem_bytes, void* stream) {
+  if (B < 1 || Hq < 1 || Hkv < 0 || L < 0 || D < 1 || R < 0 || R % 2 != 0 || R > D) return COVER_ERR_INVALID_ARG;
+  if (elem_bytes != 2 && elem_bytes != 4) return COVER_ERR_INVALID_ARG;
+  if (L == 0) return COVER_OK;
+  if (q == nullptr || q_out == nullptr || strides == nullptr || (R > 0 && inv_freq == nullptr))
+    return COVER_ERR_INVALID_ARG;
+  if (Hkv > 0 && (k == nullptr || k_out == nullptr)) return COVER_ERR_INVALID_ARG;
+  const size_t e = static_cast<size_t>(elem_bytes);
+  if (!aligned(q, e) || !aligned(q_out, e) || !aligned(inv_freq, 8) || !aligned(pos, 4)) return COVER_ERR_INVALID_ARG;
+  if (Hkv > 0 && (!aligned(k, e) || !aligned(k_out, e))) return COVER_ERR_INVALID_ARG;
+  if (D > 4096) return COVER_ERR_UNSUPPORTED;
+  const cover::RopeArgs a{q,        k,   q_out, k_out,       strides, B,       Hq,        Hkv, L, D, R,
+                          inv_freq, pos, pos0,  interleaved, mscale,  inverse, elem_bytes};
+  return cover::launch_rope(a, static_cast<cudaStream_t>(stream));
+}
+
+// What cover_kv8_write and cover_kv8_read have in common.
+static int check_kv8(const void* k, const void* v, const int32_t* pos, int pos0, int n, int B, int Hkv, int L, int D,
+                     int elem_bytes, const void* k8, const void* v8, const void* k_exp, const void* v_exp) {
+  if (B < 1 || Hkv < 1 || L < 1 || D < 1 || n < 0) return COVER_ERR_INVALID_ARG;
+  if (elem_bytes != 2 && elem_bytes != 4) return COVER_ERR_INVALID_ARG;
+  if (pos == nullptr && (pos0 < 0 || static_cast<long long>(pos0) + n > L)) return COVER_ERR_INVALID_ARG;
+  if (k8 == nullptr || v8 == nullptr || k_exp == nullptr || v_exp == nullptr) return COVER_ERR_INVALID_ARG;
+  if (n > 0 && (k == nullptr || v == nullptr)) return COVER_ERR_INVALID_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k8, 16) || !aligned(v8, 16) || !aligned(pos, 4))
+    return COVER_ERR_INVALID_ARG;
+  return D == 64 || D == 128 ? COVER_OK : COVER_ERR_UNSUPPORTED;
+}
+
+int cover_kv8_write(const void* k, const void* v, const int64_t* strides, const int32_t* pos, int pos0, int n, int B,
+                    int Hkv, int L, int D, int elem_bytes, void* k8, void* v8, uint8_t* k_exp, uint8_t* v_exp,
+                    void* stream) {
+  const int rc = check_kv8(k, v, pos, pos0, n, B, Hkv, L, D, elem_bytes, k8, v8, k_exp, v_exp);
+  if (rc != COVER_OK) return rc;
+  if (n == 0) return COVER_OK;
+  if (strides == nullptr) return COVER_ERR_INVALID_ARG;
+  const int sizes[3] = {B, Hkv, n};
+  for (int i = 0; i < 6; ++i)
+    if (sizes[i % 3] > 1 && strides[i] * elem_bytes % 16 != 0) return COVER_ERR_INVALID_ARG;
+  const cover::Kv8Args a{const_cast<void*>(k), const_cast<void*>(v), strides, pos, pos0, n, B, Hkv, L, D, elem_bytes,
+                         k8, v8, k_exp, v_exp};
+  return cover::launch_kv8(a, true, static_cast<cudaStream_t>(stream));
+}
+
+int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const uint8_t* v_exp, const int32_t* pos,
+                   int pos0, int n, int B, int Hkv, int L, int D, int elem_bytes, void* k, void* v, void* stream) {
+  const int rc = check_kv8(k, v, pos, pos0, n, B, Hkv, L, D, elem_bytes, k8, v8, k_exp, v_exp);
+  if (rc != COVER_OK) return rc;
+  const cover::Kv8Args a{k, v, nullptr, pos, pos0, n, B, Hkv, L, D, elem_bytes, const_cast<void*>(k8),
+                         const_cast<void*>(v8), const_cast<uint8_t*>(k_exp), const_cast<uint8_t*>(v_exp)};
+  return cover::launch_kv8(a, false, static_cast<cudaStream_t>(stream));
+}
+
+size_t cover_attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Lq < 1 || Lk < 1) return 0;
+  return cover::attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk);
+}
+
+int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8, const uint8_t* k_exp, const uint8_t* v_exp,
+                           const void* k_seedmask, const void* v_seedmask, const int32_t* seed_idx, int n_seeds,
+                           int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D, const int32_t* key_lo,
+                           const int32_t* key_hi, float softcap, void* out, float* lse, void* workspace,
+                           void* stream) {
+  int rc = check_window(Lq, Lk, q0);
+  if (rc != COVER_OK) return rc;
+  rc = check_attn_args(q, k8, v8, k_seedmask, v_seedmask, seed_idx, n_seeds, B, Hq, Hkv, Lk, D, out, lse, 16);
+  if (rc != COVER_OK) return rc;
+  if (k_exp == nullptr || v_exp == nullptr || !aligned(key_lo, 4) || !aligned(key_hi, 4) || !aligned(workspace, 16))
+    return COVER_ERR_INVALID_ARG;
+  if (!(softcap >= 0.0f) || softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
+  if (D != 128) return COVER_ERR_UNSUPPORTED;
+  if (workspace == nullptr && cover::attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) > 0) return COVER_ERR_INVALID_ARG;
+  int* st = status_block();
+  if (st == nullptr) return COVER_ERR_CUDA;
+  const cover::Attn8Args a{q,  k8,  v8,  k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,        Hq, Hkv,
+                           Lq, Lk,  q0,  key_lo, key_hi, softcap,  out,        lse,      workspace};
+  return cover::launch_attn_prefix8(a, st, static_cast<cudaStream_t>(stream));
+}
+
 size_t cover_decide_workspace_bytes(int N, int n_seq) {
   if (N < 1 || n_seq < 1) return 0;
   // per-segment counters, then u and ln Z per row

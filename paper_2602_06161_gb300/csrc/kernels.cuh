@@ -139,6 +139,60 @@ int launch_attn_mass(const MassArgs& a, int* status, cudaStream_t stream);
 int launch_seed_kv(bool override_swap, void* k, void* v, const int32_t* seed_idx, int n_seeds, int B, int Hkv, int L,
                    int row_bytes, void* k_cache, void* v_cache, cudaStream_t stream);
 
+// Rotary positions of q and k (rope_kernel.cu). strides: (b, h, l) in elements of q, k, q_out, k_out; Hkv = 0
+// without k.
+struct RopeArgs {
+  const void* q;
+  const void* k;
+  void* q_out;
+  void* k_out;
+  const int64_t* strides;
+  int B, Hq, Hkv, L, D, R;
+  const double* inv_freq;
+  const int32_t* pos;
+  int pos0, interleaved;
+  float mscale;
+  int inverse, elem_bytes;
+};
+int launch_rope(const RopeArgs& a, cudaStream_t stream);
+
+// Rows of an 8-bit memory (kv8_kernel.cu). strides: (b, h, s) in elements of k, v (write only; rows read back
+// are dense).
+struct Kv8Args {
+  void* k;
+  void* v;
+  const int64_t* strides;
+  const int32_t* pos;
+  int pos0, n, B, Hkv, L, D, elem_bytes;
+  void* k8;
+  void* v8;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+};
+int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream);
+
+// Window attention over an 8-bit memory (attn_prefix8.cu).
+struct Attn8Args {
+  const void* q;
+  const void* k8;
+  const void* v8;
+  const uint8_t* k_exp;
+  const uint8_t* v_exp;
+  const void* k_seedmask;
+  const void* v_seedmask;
+  const int32_t* seed_idx;
+  int n_seeds;
+  int B, Hq, Hkv, Lq, L, q0;
+  const int32_t* key_lo;
+  const int32_t* key_hi;
+  float softcap;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L);
+int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream);
+
 int launch_umma_tile(const void* a, const void* b, const void* p, const void* v, float* c1, float* c2, int* status,
                      cudaStream_t stream);
 int launch_wait_timeout(uint64_t limit_ns, int* status, cudaStream_t stream);

@@ -1,0 +1,253 @@
+// kv8_kernel.cu - rows of keys and values into an 8-bit memory and back.
+//
+// The memory of a layer is k8, v8 [B, Hkv, L, D] e4m3 codes and k_exp, v_exp [B, Hkv, L] exponent bytes
+// (e4m3.cuh). Slot s of a batch row stands for position pos0 + s, or pos[b, s] where a list is given.
+//   write: x = the smallest byte with max |row| <= 448 * 2^(x - 127); code = the nearest e4m3 value of
+//          row * 2^(127 - x). A listed position out of [0, L), or named by a lower slot of the same batch row
+//          already, is left out (the lowest slot wins, as in the attention kernels' routing).
+//   read:  row = code * 2^(x - 127); a position out of [0, L) gives zeros.
+//
+// Bound by memory: each row is read and written once. D / N lanes hold a row (N elements of 16 bytes on the wide
+// side), and a thread has the K and V vectors of kTok consecutive slots in flight (128 bytes), so that
+// the exponent bytes of consecutive positions leave in one request too.
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "e4m3.cuh"
+#include "kernels.cuh"
+#include "ptx.cuh"
+
+namespace cover {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTok = 4;   // slots of a lane group
+
+struct Kv8Params {
+  const uint8_t* src[2];     // k, v rows (write) or codes (read)
+  uint8_t* dst[2];           // codes (write) or rows (read)
+  uint8_t* exps[2];
+  long long sb[2], sh[2], sl[2];   // strides of k, v in elements (write)
+  const int32_t* pos;        // [B, n] or null
+  int pos0, n, L, Hkv;
+  int heads;                 // heads of a CTA
+};
+
+template <typename T>
+struct Wide;
+template <>
+struct Wide<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                      pack_bf16x2(x[6], x[7]));
+  }
+};
+template <>
+struct Wide<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+    x[0] = __uint_as_float(r.x), x[1] = __uint_as_float(r.y), x[2] = __uint_as_float(r.z), x[3] = __uint_as_float(r.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+
+template <int N>
+struct Codes;   // N codes in a register or two
+template <>
+struct Codes<8> {
+  using type = uint2;
+  static __device__ __forceinline__ uint2 encode(const float (&x)[8], float inv) {
+    return make_uint2(e4m3x2(x[0] * inv, x[1] * inv) | (e4m3x2(x[2] * inv, x[3] * inv) << 16),
+                      e4m3x2(x[4] * inv, x[5] * inv) | (e4m3x2(x[6] * inv, x[7] * inv) << 16));
+  }
+  static __device__ __forceinline__ void decode(const uint2& c, float scale, float (&x)[8]) {
+    const uint32_t w[4] = {c.x, c.x >> 16, c.y, c.y >> 16};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = e4m3x2_values(w[i]);
+      x[2 * i] = v.x * scale, x[2 * i + 1] = v.y * scale;
+    }
+  }
+};
+template <>
+struct Codes<4> {
+  using type = uint32_t;
+  static __device__ __forceinline__ uint32_t encode(const float (&x)[4], float inv) {
+    return e4m3x2(x[0] * inv, x[1] * inv) | (e4m3x2(x[2] * inv, x[3] * inv) << 16);
+  }
+  static __device__ __forceinline__ void decode(uint32_t c, float scale, float (&x)[4]) {
+    const float2 a = e4m3x2_values(c), b = e4m3x2_values(c >> 16);
+    x[0] = a.x * scale, x[1] = a.y * scale, x[2] = b.x * scale, x[3] = b.y * scale;
+  }
+};
+
+// CTA (slot tile, head group, b): T slots, of p.heads heads one after the other.
+template <typename T, int D, bool kWrite>
+__global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ Kv8Params p) {
+  using W = Wide<T>;
+  constexpr int N = W::kN;
+  constexpr int kLanes = D / N;                      // lanes of a row
+  constexpr int kSlots = kThreads / kLanes * kTok;   // slots of a CTA
+  using C = typename Codes<N>::type;
+  __shared__ int s_pos[kSlots];
+  griddep_wait();
+  griddep_launch_dependents();
+  const int tid = threadIdx.x;
+  const int b = blockIdx.z;
+  const int slot0 = blockIdx.x * kSlots;
+  const int32_t* list = p.pos == nullptr ? nullptr : p.pos + static_cast<size_t>(b) * p.n;
+  for (int i = tid; i < kSlots; i += kThreads) {
+    const int s = slot0 + i;
+    int at = -1;
+    if (s < p.n) at = list != nullptr ? list[s] : p.pos0 + s;
+    s_pos[i] = at >= 0 && at < p.L ? at : -1;
+  }
+  __syncthreads();
+  if (kWrite && list != nullptr) {
+    // a slot whose position a lower slot names does not write it
+    __shared__ uint8_t s_dup[kSlots];
+    for (int i = tid; i < kSlots; i += kThreads) s_dup[i] = 0;
+    __syncthreads();
+    const int live = min(kSlots, p.n - slot0);
+    // one warp per slot in turn, its lanes over the lower slots
+    for (int i = tid >> 5; i < live; i += kThreads / 32) {
+      const int at = s_pos[i];
+      if (at < 0) continue;
+      bool hit = false;
+      for (int o = tid & 31; o < slot0 + i; o += 32) hit |= __ldg(list + o) == at;
+      if (hit) s_dup[i] = 1;
+    }
+    __syncthreads();
+    for (int i = tid; i < kSlots; i += kThreads)
+      if (s_dup[i]) s_pos[i] = -1;
+    __syncthreads();
+  }
+  const int lane = tid % kLanes, group = tid / kLanes;
+  int at[kTok];
+#pragma unroll
+  for (int j = 0; j < kTok; ++j) at[j] = s_pos[group * kTok + j];
+  const int h1 = min(p.Hkv, static_cast<int>(blockIdx.y + 1) * p.heads);
+  for (int h = blockIdx.y * p.heads; h < h1; ++h) {
+    const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + h) * p.L;   // the head's first memory row
+    if (kWrite) {
+      uint4 r[2][kTok];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const T* x = reinterpret_cast<const T*>(p.src[w]) + b * p.sb[w] + h * p.sh[w] + lane * N;
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+          r[w][j] = make_uint4(0, 0, 0, 0);
+          if (at[j] >= 0) r[w][j] = __ldcs(reinterpret_cast<const uint4*>(x + (slot0 + group * kTok + j) * p.sl[w]));
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+          float x[N];
+          W::unpack(r[w][j], x);
+          // the largest magnitude by its bits: NaN is above infinity, infinity above every number
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+          for (int o = kLanes / 2; o >= 1; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int e = e4m3_row_exponent(__uint_as_float(top));
+          const float inv = e4m3_inverse_scale(e);
+          if (e == kExpNan) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = 0.0f;
+          }
+          const C code = Codes<N>::encode(x, inv);
+          if (at[j] >= 0) {
+            *reinterpret_cast<C*>(p.dst[w] + (mem0 + at[j]) * D + lane * N) = code;
+            if (lane == 0) p.exps[w][mem0 + at[j]] = static_cast<uint8_t>(e);
+          }
+        }
+      }
+    } else {
+      C c[2][kTok];
+      uint8_t e[2][kTok];
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+          c[w][j] = C{};
+          e[w][j] = kExpZero;
+          if (at[j] >= 0) {
+            c[w][j] = __ldcs(reinterpret_cast<const C*>(p.src[w] + (mem0 + at[j]) * D + lane * N));
+            e[w][j] = __ldg(p.exps[w] + mem0 + at[j]);
+          }
+        }
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+          const int s = slot0 + group * kTok + j;
+          if (s >= p.n) continue;
+          float x[N];
+          Codes<N>::decode(c[w][j], e4m3_scale(e[w][j]), x);
+          T* out = reinterpret_cast<T*>(p.dst[w]) + ((static_cast<size_t>(b) * p.Hkv + h) * p.n + s) * D + lane * N;
+          *reinterpret_cast<uint4*>(out) = W::pack(x);
+        }
+    }
+  }
+}
+
+template <typename T, int D>
+int launch(Kv8Params p, int B, bool write, cudaStream_t stream) {
+  constexpr int kSlots = kThreads / (D / Wide<T>::kN) * kTok;
+  const long long tiles = (p.n + kSlots - 1) / kSlots;
+  if (B > 65535) return -2;
+  // A CTA takes one head; with a list to search for repeats, as many as leave the GPU about two waves
+  // of CTAs, so that the search is not made again for each head.
+  long long groups = p.Hkv;
+  if (write && p.pos != nullptr) groups = std::min<long long>(p.Hkv, std::max<long long>(1, 2 * 152 * 4 / (tiles * B)));
+  p.heads = static_cast<int>((p.Hkv + groups - 1) / groups);
+  groups = (p.Hkv + p.heads - 1) / p.heads;
+  if (groups > 65535) return -2;
+  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(groups), static_cast<unsigned>(B));
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = pdl_config(grid, dim3(kThreads), 0, stream, attr);
+  const cudaError_t e = write ? cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, true>, p)
+                              : cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, false>, p);
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
+}
+
+}  // namespace
+
+int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
+  if (a.n == 0) return 0;
+  Kv8Params p{};
+  for (int w = 0; w < 2; ++w) {
+    uint8_t* codes = static_cast<uint8_t*>(w ? a.v8 : a.k8);
+    uint8_t* rows = static_cast<uint8_t*>(w ? a.v : a.k);
+    p.src[w] = write ? rows : codes;
+    p.dst[w] = write ? codes : rows;
+    p.exps[w] = w ? a.v_exp : a.k_exp;
+    if (write) p.sb[w] = a.strides[3 * w], p.sh[w] = a.strides[3 * w + 1], p.sl[w] = a.strides[3 * w + 2];
+  }
+  p.pos = a.pos;
+  p.pos0 = a.pos0;
+  p.n = a.n;
+  p.L = a.L;
+  p.Hkv = a.Hkv;
+  using bf16 = __nv_bfloat16;
+  if (a.elem_bytes == 2) return a.D == 64 ? launch<bf16, 64>(p, a.B, write, stream) : launch<bf16, 128>(p, a.B, write, stream);
+  return a.D == 64 ? launch<float, 64>(p, a.B, write, stream) : launch<float, 128>(p, a.B, write, stream);
+}
+
+}  // namespace cover

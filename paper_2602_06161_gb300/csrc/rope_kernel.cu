@@ -1,0 +1,219 @@
+// rope_kernel.cu - rotary positions of a layer's queries and keys.
+//
+// Column pair i of a row at position t turns by the angle t f_i:
+//   y_a = m (x_a cos - x_b sin),  y_b = m (x_a sin + x_b cos)
+// with (a, b) = (2i, 2i + 1) or (i, i + R / 2), m the factor of a stretched context, and the
+// opposite angle for the inverse, which (the rotation being orthogonal) is the gradient as well.
+// Columns R .. D - 1 are copied.
+//
+// The angle. t f_i reaches 1e5 radians and more, where a product in fp32 is off by 1e-2. The frequency
+// is taken as a fraction of a turn in 64-bit fixed point, f_i / 2 pi mod 1: the product with the
+// position wraps modulo one turn by itself, exactly, and its upper 32 bits are the reduced angle (off
+// by t 2^-53 turns from the fp64 frequency and 2^-26 turns from the conversion to fp32).
+//
+// Bound by memory: each row is read and written once. A thread holds one 16-byte vector column (two, R / 2
+// apart, in the layout of halves) of one token and walks over heads, so that its sines and cosines
+// serve all of them; the next kHeadsInFlight heads' loads are in flight together.
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "kernels.cuh"
+#include "ptx.cuh"
+
+namespace cover {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kHeadsInFlight = 4;
+
+struct RopeTensor {
+  const uint8_t* in;
+  uint8_t* out;
+  long long in_b, in_h, in_l, out_b, out_h, out_l;   // strides in elements
+  int heads;
+};
+
+struct RopeParams {
+  RopeTensor t[2];         // q, k
+  const double* inv_freq;  // [R / 2] radians per position
+  const int32_t* pos;      // [B, L] or null: pos0 + l
+  int pos0, L, D, R;
+  int units;               // a row's work items: one a thread
+  int turn_units;          // of them, those that turn (the rest copy columns R .. D - 1)
+  int chunk;               // heads a thread walks over
+  int chunks0, chunks;     // chunks of q, and of q and k
+  long long items;         // B * L * chunks * units
+  float mscale;
+  int inverse;
+};
+
+template <typename T>
+__device__ __forceinline__ float to_f(T x);
+template <>
+__device__ __forceinline__ float to_f(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) {
+  return __bfloat162float(x);
+}
+template <typename T>
+__device__ __forceinline__ T from_f(float x);
+template <>
+__device__ __forceinline__ float from_f(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f(float x) {
+  return __float2bfloat16_rn(x);
+}
+
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Vec {
+  T v[N];
+};
+
+// T: element; N: elements of a thread's vector (16 bytes, or one element where a size, a stride or
+// a pointer does not allow more); kInter: pairs of neighbours (a vector of N >= 2 holds N / 2 pairs).
+template <typename T, int N, bool kInter>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p) {
+  extern __shared__ uint64_t turns[];   // [R / 2] fractions of a turn per position, 2^64 = one turn
+  griddep_wait();
+  griddep_launch_dependents();
+  for (int i = threadIdx.x; i < p.R / 2; i += kThreads) {
+    const double t = p.inv_freq[i] * 0.15915494309189535;   // / 2 pi
+    turns[i] = __double2ull_rn((t - floor(t)) * 18446744073709551616.0);
+  }
+  __syncthreads();
+  const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+  if (item >= p.items) return;
+  const int u = static_cast<int>(item % p.units);
+  long long rest = item / p.units;
+  const int c = static_cast<int>(rest % p.chunks);
+  rest /= p.chunks;                                          // token b * L + l
+  const long long b = rest / p.L;
+  const int l = static_cast<int>(rest - b * p.L);
+  const bool turn = u < p.turn_units;
+  constexpr int kHalf = kInter ? (N >= 2 ? N / 2 : 1) : N;   // pairs of a work item
+  constexpr int kVecs = kInter && N >= 2 ? 1 : 2;            // vectors of a turning work item
+  // columns of the work item's vectors
+  int col0, col1 = 0;
+  if (turn) {
+    col0 = kInter ? u * (N >= 2 ? N : 2) : u * N;
+    col1 = kInter ? col0 + 1 : col0 + p.R / 2;
+  } else {
+    col0 = p.R + (u - p.turn_units) * N;
+  }
+  float cs[kHalf], sn[kHalf];
+  if (turn) {
+    const int32_t at = p.pos != nullptr ? p.pos[rest] : static_cast<int32_t>(static_cast<uint32_t>(p.pos0) + l);
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) {
+      const uint64_t a = static_cast<uint64_t>(static_cast<int64_t>(at)) * turns[u * kHalf + i];
+      // the nearest of 2^-32 turns, in units of pi: [-1, 1]
+      const float x = static_cast<float>(static_cast<int32_t>((a + 0x80000000ull) >> 32)) * 4.656612873077393e-10f;
+      float s, co;
+      sincospif(x, &s, &co);
+      cs[i] = co * p.mscale;
+      sn[i] = (p.inverse ? -s : s) * p.mscale;
+    }
+  }
+  const int which = c >= p.chunks0 ? 1 : 0;
+  const RopeTensor& t = p.t[which];
+  const int h0 = (which ? c - p.chunks0 : c) * p.chunk;
+  const int h1 = min(h0 + p.chunk, t.heads);
+  const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + l * t.in_l;
+  T* out = reinterpret_cast<T*>(t.out) + b * t.out_b + l * t.out_l;
+  using V = Vec<T, N>;
+  for (int h = h0; h < h1; h += kHeadsInFlight) {
+    V x[kHeadsInFlight][2];
+#pragma unroll
+    for (int j = 0; j < kHeadsInFlight; ++j) {
+      if (h + j >= h1) break;
+      x[j][0] = *reinterpret_cast<const V*>(in + (h + j) * t.in_h + col0);
+      if (kVecs == 2 && turn) x[j][1] = *reinterpret_cast<const V*>(in + (h + j) * t.in_h + col1);
+    }
+#pragma unroll
+    for (int j = 0; j < kHeadsInFlight; ++j) {
+      if (h + j >= h1) break;
+      if (turn) {
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          T& xa = kVecs == 1 ? x[j][0].v[(2 * i) % N] : x[j][0].v[i % N];
+          T& xb = kVecs == 1 ? x[j][0].v[(2 * i + 1) % N] : x[j][1].v[i % N];
+          const float a = to_f(xa), d = to_f(xb);
+          xa = from_f<T>(a * cs[i] - d * sn[i]);
+          xb = from_f<T>(a * sn[i] + d * cs[i]);
+        }
+      }
+      *reinterpret_cast<V*>(out + (h + j) * t.out_h + col0) = x[j][0];
+      if (kVecs == 2 && turn) *reinterpret_cast<V*>(out + (h + j) * t.out_h + col1) = x[j][1];
+    }
+  }
+}
+
+// Whether every row of the tensor starts on a vector of n elements of e bytes.
+bool vectors_fit(const RopeTensor& t, int n, int e) {
+  if (t.heads == 0) return true;
+  const auto fits = [&](const void* p) { return reinterpret_cast<uintptr_t>(p) % (static_cast<size_t>(n) * e) == 0; };
+  return fits(t.in) && fits(t.out) && t.in_b % n == 0 && t.in_h % n == 0 && t.in_l % n == 0 && t.out_b % n == 0 &&
+         t.out_h % n == 0 && t.out_l % n == 0;
+}
+
+}  // namespace
+
+int launch_rope(const RopeArgs& a, cudaStream_t stream) {
+  RopeParams p{};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t* s = a.strides + 3 * i;
+    p.t[i] = RopeTensor{static_cast<const uint8_t*>(i ? a.k : a.q), static_cast<uint8_t*>(i ? a.k_out : a.q_out),
+                        s[0], s[1], s[2], s[6], s[7], s[8], i ? a.Hkv : a.Hq};
+  }
+  p.inv_freq = a.inv_freq;
+  p.pos = a.pos;
+  p.pos0 = a.pos0;
+  p.L = a.L;
+  p.D = a.D;
+  p.R = a.R;
+  p.mscale = a.mscale;
+  p.inverse = a.inverse;
+  const int e = a.elem_bytes;
+  int n = 16 / e;
+  const bool wide = vectors_fit(p.t[0], n, e) && vectors_fit(p.t[1], n, e) && a.D % n == 0 &&
+                    (a.interleaved ? a.R % n == 0 : (a.R / 2) % n == 0);
+  if (!wide) n = 1;
+  const int per_unit = a.interleaved ? (n >= 2 ? n / 2 : 1) : n;   // pairs of a work item
+  p.turn_units = a.R / 2 / per_unit;
+  p.units = p.turn_units + (a.D - a.R) / n;
+  // Heads a thread walks over: all work items of a small call are spread over the GPU (one head each), a
+  // large call's threads share their sines and cosines between eight heads.
+  const long long tokens = static_cast<long long>(a.B) * a.L;
+  const long long all = tokens * p.units * (a.Hq + a.Hkv);
+  p.chunk = static_cast<int>(std::min<long long>(8, std::max<long long>(1, all / (152 * 2048))));
+  p.chunks0 = (a.Hq + p.chunk - 1) / p.chunk;
+  p.chunks = p.chunks0 + (a.Hkv + p.chunk - 1) / p.chunk;
+  p.items = tokens * p.chunks * p.units;
+  const long long grid = (p.items + kThreads - 1) / kThreads;
+  if (grid > 0x7fffffffLL) return -2;
+  if (grid == 0) return 0;
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads),
+                                            static_cast<size_t>(a.R / 2) * 8, stream, attr);
+  using bf16 = __nv_bfloat16;
+  cudaError_t r;
+  if (e == 2)
+    r = wide ? (a.interleaved ? cudaLaunchKernelEx(&cfg, rope_kernel<bf16, 8, true>, p)
+                              : cudaLaunchKernelEx(&cfg, rope_kernel<bf16, 8, false>, p))
+             : (a.interleaved ? cudaLaunchKernelEx(&cfg, rope_kernel<bf16, 1, true>, p)
+                              : cudaLaunchKernelEx(&cfg, rope_kernel<bf16, 1, false>, p));
+  else
+    r = wide ? (a.interleaved ? cudaLaunchKernelEx(&cfg, rope_kernel<float, 4, true>, p)
+                              : cudaLaunchKernelEx(&cfg, rope_kernel<float, 4, false>, p))
+             : (a.interleaved ? cudaLaunchKernelEx(&cfg, rope_kernel<float, 1, true>, p)
+                              : cudaLaunchKernelEx(&cfg, rope_kernel<float, 1, false>, p));
+  return r == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
+}
+
+}  // namespace cover
