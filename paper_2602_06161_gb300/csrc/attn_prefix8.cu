@@ -10,7 +10,7 @@
 // The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r
 // of head hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view, cut into Q tiles of 128.
 // A CTA takes one or two Q tiles against the KV tiles (128 keys) of one of nsplit parts of what its rows
-// see. Codes arrive by bulk copies (a KV tile's 128 rows are 16 KB in one piece), four warps decode them to bf16
+// see. Codes arrive by bulk copies (64 rows are 8 KB in one piece); one warpgroup decodes K and one V to bf16
 // (exact: a row's scale is a power of two) into the swizzled layout that the tensor cores read, and S = Q K^T, O += P V
 // run as tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each:
 //   shared Q (kPair = false): both streams are the same Q tile, on the even and the odd KV tiles, with sums and an
@@ -19,9 +19,9 @@
 //   pair (kPair = true): the streams are two Q tiles that read each decoded KV tile together.
 // With nsplit > 1 the parts leave (m, l, O) in fp32 in the workspace and a second kernel combines them.
 //
-// Roles (512 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode (thread = key
-// row); 12 issues the products; 13 issues the copies.
-// Shared memory: Q (32 or 64 KB) | codes ring of 16 KB entries, K and V in turn (4 or 2) | K, V in bf16 (2 x 32 KB each).
+// Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16
+// issues the products; 17 and 18 issue the copies of K and V.
+// Shared memory: Q (32 or 64 KB) | rings of 8 KB entries of codes, K and V (4 or 2 each) | K, V in bf16 (2 x 32 KB each).
 // Tensor memory: S0 | S1 (P overwrites their first 64 columns) | O0 | O1, 128 columns each.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -44,21 +44,22 @@ constexpr int kBM = 128;                   // rows per Q tile
 constexpr int kBN = 128;                   // keys per KV tile
 constexpr int kTileBytes = kBM * kD * 2;   // 32 KB
 constexpr int kBoxBytes = kTileBytes / 2;  // one 64-column, 128-byte-swizzled box
-constexpr int kCodeBytes = kBN * kD;       // 16 KB of codes
-constexpr int kThreads = 512;
-constexpr int kDecodeWarp = 8, kMmaWarp = 12, kLoadWarp = 13;
-constexpr int kLaunchRegs = 128;           // registers per thread at launch (65536 / 512)
-constexpr int kSoftmaxRegs = 192, kDecodeRegs = 80, kIssueRegs = 40;
-static_assert(2 * 128 * kSoftmaxRegs + 128 * kDecodeRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "register split");
+constexpr int kHalf = kBN / 2;             // key rows of a ring entry
+constexpr int kCodeBytes = kHalf * kD;     // 8 KB of codes
+constexpr int kThreads = 640;
+constexpr int kDecodeWarp = 8, kMmaWarp = 16, kLoadWarp = 17;
+constexpr int kLaunchRegs = 96;            // registers per thread at launch (65536 / 640, rounded down to 8)
+constexpr int kSoftmaxRegs = 160, kDecodeRegs = 56, kIssueRegs = 40;
+static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
 
 struct Smem {
-  uint8_t q_and_ring[3 * kTileBytes];   // Q | codes ring
+  uint8_t q_and_ring[3 * kTileBytes];   // Q | rings of K codes and of V codes
   uint8_t k[2][kTileBytes];
   uint8_t v[2][kTileBytes];
   uint64_t q_full;
-  uint64_t c_full[4], c_empty[4];       // codes ring
+  uint64_t c_full[2][4], c_empty[2][4]; // rings of K and V codes
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t s_full[2], p_full[2];        // per stream
   uint64_t o_full, drain;
@@ -125,6 +126,16 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
+// Shared memory by its 32-bit address.
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
 // Bytes of x by the selector's nibbles; a nibble with its top bit set gives eight copies of that byte's sign.
 template <uint32_t kSel>
 __device__ __forceinline__ uint32_t prmt(uint32_t x) {
@@ -140,17 +151,20 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap_log2) {
   return fmaf(-2.0f * cap_log2, rcp_approx(1.0f + t), cap_log2);
 }
 
-// Decodes one row of 128 codes from the ring into row `row` of a bf16 tile (two 64-column boxes, 16-byte
-// chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are the bf16
-// number code * 2^-120 (subnormal codes included), and one multiplication by m1 = 2^(120 + x - 127) gives the
-// value; where that is above bf16's range, m1 = 2^120 and two says to multiply by m2 = 2^(x - 127) too. Both are exact.
-// Lanes take their eight 16-byte pieces in an order of their own, so that reads and writes meet every bank.
+// Decodes half a row of codes: every other one of the eight 16-byte pieces of a row, into its row of a bf16 tile (two
+// 64-column boxes, 16-byte chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are
+// the bf16 number code * 2^-120 (subnormal codes included), and one multiplication by m1 = 2^(120 + x - 127) gives the
+// value; where that is above bf16's range, m1 = 2^120 and kTwo says to multiply by m2 = 2^(x - 127) too. Both are
+// exact. The thread's pieces are u0 ^ 0, 2, 4, 6 with u0 the row's low bits (its partner's: u0 ^ 1), so that the reads
+// and writes of eight lanes meet every bank. src: address of piece u0; d0, d1: of its first chunk, in its box and
+// in the other one.
 template <bool kTwo>
-__device__ __forceinline__ void decode_row(const uint8_t* codes, uint8_t* tile, int row, uint32_t m1, uint32_t m2) {
+__device__ __forceinline__ void decode_half_row(uint32_t src, uint32_t d0, uint32_t d1, uint32_t m1, uint32_t m2) {
+  uint4 next = lds128(src);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int u = (i + row) & 7;
-    const uint4 c = *reinterpret_cast<const uint4*>(codes + row * kD + u * 16);
+  for (int i = 0; i < 4; ++i) {
+    const uint4 c = next;
+    if (i < 3) next = lds128(src ^ (32u * (i + 1)));
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
     uint32_t o[8];
 #pragma unroll
@@ -165,14 +179,13 @@ __device__ __forceinline__ void decode_row(const uint8_t* codes, uint8_t* tile, 
         o[2 * e + 1] = mul_bf16x2(o[2 * e + 1], m2);
       }
     }
-    uint8_t* dst = tile + (u >> 2) * kBoxBytes + row * 128;
-    const int ch = (u & 3) * 2;
-    *reinterpret_cast<uint4*>(dst + ((ch ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-    *reinterpret_cast<uint4*>(dst + (((ch + 1) ^ (row & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+    const uint32_t d = (i & 2 ? d1 : d0) ^ (i & 1 ? 64u : 0u);
+    sts128(d, o[0], o[1], o[2], o[3]);
+    sts128(d ^ 16u, o[4], o[5], o[6], o[7]);
   }
 }
 
-__device__ __forceinline__ void decode(const uint8_t* codes, uint8_t* tile, int row, int x, bool zero) {
+__device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, int x, bool zero) {
   // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
   const bool two = x > 134 && x <= kExpMax;
   uint32_t m1 = two ? 247u << 7 : static_cast<uint32_t>(x + 120) << 7;
@@ -181,9 +194,22 @@ __device__ __forceinline__ void decode(const uint8_t* codes, uint8_t* tile, int 
   if (zero) m1 = 0;
   m1 |= m1 << 16;
   m2 |= m2 << 16;
-  if (__any_sync(0xffffffffu, two)) decode_row<true>(codes, tile, row, m1, m2);
-  else decode_row<false>(codes, tile, row, m1, m2);
+  if (__any_sync(0xffffffffu, two)) decode_half_row<true>(src, d0, d1, m1, m2);
+  else decode_half_row<false>(src, d0, d1, m1, m2);
 }
+
+// The exponent bytes of row lrow of four half tiles from half h on (zero from row `left` on).
+struct FourBytes {
+  uint32_t v[4];
+  __device__ __forceinline__ void load(const uint8_t* exps, int h, int lrow, int left) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = (h + i) * kHalf + lrow;
+      v[i] = row < left ? __ldg(exps + row) : 0u;
+    }
+  }
+  __device__ __forceinline__ uint32_t packed() const { return v[0] | (v[1] << 8) | (v[2] << 16) | (v[3] << 24); }
+};
 
 template <bool kPair, bool kCap>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -191,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr int kQTiles = kPair ? 2 : 1;
-  constexpr int kRing = kPair ? 2 : 4;
+  constexpr int kRing = kPair ? 2 : 4;   // entries of each ring
   uint8_t* const sm_q = sm.q_and_ring;
   uint8_t* const ring = sm.q_and_ring + kQTiles * kTileBytes;
 
@@ -211,14 +237,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kMmaWarp) {
     if (lane == 0) {
       mbar_init(&sm.q_full, 1);
-      for (int i = 0; i < 4; ++i) {
-        mbar_init(&sm.c_full[i], 1);
-        mbar_init(&sm.c_empty[i], kBN);
-      }
+      for (int i = 0; i < 4; ++i)
+        for (int w = 0; w < 2; ++w) {
+          mbar_init(&sm.c_full[w][i], 1);
+          mbar_init(&sm.c_empty[w][i], 128);
+        }
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&sm.k_full[i], kBN);
+        mbar_init(&sm.k_full[i], 128);
         mbar_init(&sm.k_empty[i], 1);
-        mbar_init(&sm.v_full[i], kBN);
+        mbar_init(&sm.v_full[i], 128);
         mbar_init(&sm.v_empty[i], 1);
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], kBM);
@@ -277,31 +304,38 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp >= kMmaWarp) {
     setmaxnreg_dec<kIssueRegs>();
-    if (warp == kLoadWarp && lane == 0 && nt > 0) {
+    const int which = warp - kLoadWarp;   // 0: K (and Q), 1: V
+    if ((which == 0 || which == 1) && lane == 0 && nt > 0) {
       // ---------------- copies ----------------
-      mbar_arrive_expect_tx(&sm.q_full, kQTiles * kTileBytes);
-      for (int t = 0; t < kQTiles; ++t)
-        for (int h = 0; h < 2; ++h)
-          tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &sm.q_full, 64 * h,
-                      static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
+      if (which == 0) {
+        mbar_arrive_expect_tx(&sm.q_full, kQTiles * kTileBytes);
+        for (int t = 0; t < kQTiles; ++t)
+          for (int h = 0; h < 2; ++h)
+            tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &sm.q_full, 64 * h,
+                        static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
+      }
+      const uint8_t* src = (which ? p.v8 : p.k8) + mem0 * kD;
+      uint8_t* const dst = ring + which * kRing * kCodeBytes;
+      // half tiles with a key of the memory
+      const int halves = min(2 * nt, (p.Lk - j0 * kBN + kHalf - 1) / kHalf);
       int e = 0;
       bool ok = true;
-      for (; e < 2 * nt; ++e) {   // entry e: K (even) or V (odd) of tile e / 2
+      for (; e < halves; ++e) {
         const int st = e % kRing;
-        if (e >= kRing) ok = mbar_wait(&sm.c_empty[st], (e / kRing - 1) & 1, &sm.abort);
+        if (e >= kRing) ok = mbar_wait(&sm.c_empty[which][st], (e / kRing - 1) & 1, &sm.abort);
         if (!ok) break;
-        const int key0 = (j0 + (e >> 1)) * kBN;
-        const uint32_t bytes = static_cast<uint32_t>(min(kBN, p.Lk - key0)) * kD;
-        mbar_arrive_expect_tx(&sm.c_full[st], bytes);
-        bulk_load(smem_u32(ring + st * kCodeBytes), ((e & 1) ? p.v8 : p.k8) + (mem0 + key0) * kD, bytes, &sm.c_full[st]);
+        const int key0 = j0 * kBN + e * kHalf;
+        const uint32_t bytes = static_cast<uint32_t>(min(kHalf, p.Lk - key0)) * kD;
+        mbar_arrive_expect_tx(&sm.c_full[which][st], bytes);
+        bulk_load(smem_u32(dst + st * kCodeBytes), src + static_cast<size_t>(key0) * kD, bytes, &sm.c_full[which][st]);
       }
       if (!ok) {
         if (!sm.abort) report_status(p.status, kStatusTimeout, 70);
         sm.abort = 1;
       }
       // every copy lands before the CTA's shared memory is released, whatever the other roles did
-      mbar_wait(&sm.q_full, 0, nullptr);
-      for (int f = max(0, e - kRing); f < e; ++f) mbar_wait(&sm.c_full[f % kRing], (f / kRing) & 1, nullptr);
+      if (which == 0) mbar_wait(&sm.q_full, 0, nullptr);
+      for (int f = max(0, e - kRing); f < e; ++f) mbar_wait(&sm.c_full[which][f % kRing], (f / kRing) & 1, nullptr);
     } else if (warp == kMmaWarp && lane == 0 && nt > 0) {
       // ---------------- products ----------------
       constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
@@ -312,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
       // S[s] = Q . K(stage)^T
       auto issue_s = [&](int s, int st) {
-        const uint64_t a = dq + (kPair ? s * kTileDesc : 0), kb = dk + st * kTileDesc;
+        uint64_t a = dq + (kPair ? s * kTileDesc : 0), kb = dk + st * kTileDesc;
+        asm volatile("" : "+l"(a), "+l"(kb));   // descriptors are added up here, not kept in registers
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
           const uint64_t off = static_cast<uint64_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
@@ -322,10 +357,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       // O[s] (+)= P[s] . V(stage)
       auto issue_pv = [&](int s, int st, bool acc) {
+        uint64_t vb = dv + st * kTileDesc;
+        asm volatile("" : "+l"(vb));
 #pragma unroll
         for (int kk = 0; kk < kBN / 16; ++kk)
           umma_ts(tbase + 2 * kBN + s * kD, tbase + s * kBN + 8 * kk,
-                  dv + st * kTileDesc + static_cast<uint64_t>((kk * 2048) >> 4), id_pv, (acc || kk > 0) ? 1u : 0u);
+                  vb + static_cast<uint64_t>((kk * 2048) >> 4), id_pv, (acc || kk > 0) ? 1u : 0u);
       };
       auto wait = [&](uint64_t* bar, int phase) {
         const bool ok = mbar_wait(bar, phase & 1, &sm.abort);
@@ -393,43 +430,55 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp >= kDecodeWarp) {
-    // ---------------- decoding (thread = key row) ----------------
+    // ---------------- decoding ----------------
     setmaxnreg_dec<kDecodeRegs>();
-    const int row = tid - kDecodeWarp * 32;
-    const uint8_t* kx = p.k_exp + mem0;
-    const uint8_t* vx = p.v_exp + mem0;
-    int key = j0 * kBN + row;
-    int k_next = 0, v_next = 0;
-    if (nt > 0 && key < p.Lk) k_next = __ldg(kx + key), v_next = __ldg(vx + key);
+    const int which = (warp - kDecodeWarp) >> 2;   // 0: K, 1: V
+    const int t = tid & 127;
+    const int lrow = t & (kHalf - 1);              // two threads a row of a half tile
+    const uint32_t u0 = static_cast<uint32_t>((lrow ^ (t >> 6)) & 7);
+    const uint32_t codes = smem_u32(ring + which * kRing * kCodeBytes + lrow * kD) + u0 * 16;
+    const uint32_t tile = smem_u32(which ? sm.v[0] : sm.k[0]) + lrow * 128 + (((u0 & 3) << 5) ^ ((lrow & 7) << 4));
+    const uint32_t box = (u0 >> 2) * kBoxBytes;
+    const int first = j0 * kBN;                    // this part's first key
+    const int left = min(p.Lk - first, nt * kBN);  // keys of this part
+    // exponent bytes are fetched four half tiles at a time, four to eight ahead of their use
+    const uint8_t* exps = (which ? p.v_exp : p.k_exp) + mem0 + first;
+    const uint8_t* v_exps = p.v_exp + mem0 + first;
+    FourBytes x_next, v_next;
+    x_next.load(exps, 0, lrow, left);
+    v_next.load(v_exps, 0, lrow, left);
+    uint32_t xs = 0, vs = 0;
     bool ok = true;
-    for (int j = 0; j < nt; ++j) {
-      const int st = j & 1;
-      const bool zero = key >= p.Lk;
-      const int k_byte = k_next, v_byte = v_next;
-      key += kBN;
-      if (j + 1 < nt && key < p.Lk) k_next = __ldg(kx + key), v_next = __ldg(vx + key);
-      const bool v_nan = !zero && v_byte > kExpMax;
+    for (int h = 0; h < 2 * nt; ++h) {   // half h & 1 of tile h / 2
+      const int j = h >> 1, st = j & 1;
+      if ((h & 3) == 0) {
+        xs = x_next.packed();
+        x_next.load(exps, h + 4, lrow, left);
+        if (which == 0) {
+          vs = v_next.packed();
+          v_next.load(v_exps, h + 4, lrow, left);
+        }
+      }
+      const bool zero = h * kHalf + lrow >= left;
+      const int x = (xs >> (8 * (h & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (h & 3))) & 255);
+      const bool v_nan = xv > kExpMax;
       const uint32_t nans = __ballot_sync(0xffffffffu, v_nan);
-      int e = 2 * j;
-      ok = (j < 2 || warp_wait(&sm.k_empty[st], ((j >> 1) - 1) & 1, &sm.abort)) &&
-           warp_wait(&sm.c_full[e % kRing], (e / kRing) & 1, &sm.abort);
+      if ((h & 1) == 0 && j >= 2) ok = warp_wait(which ? &sm.v_empty[st] : &sm.k_empty[st], ((j >> 1) - 1) & 1, &sm.abort);
+      const bool copied = h * kHalf < left;        // a half past the memory is not copied
+      ok = ok && (!copied || warp_wait(&sm.c_full[which][h % kRing], (h / kRing) & 1, &sm.abort));
       if (!ok) break;
       // tile j - 4 has passed its softmax: S of tile j - 2 came after it
-      if (lane == 0) reinterpret_cast<uint32_t*>(&sm.nan_keys[j & 3])[row >> 5] = nans;
-      decode(ring + (e % kRing) * kCodeBytes, sm.k[st], row, k_byte, zero);
-      mbar_arrive(&sm.c_empty[e % kRing]);
-      fence_proxy_async_smem();
-      mbar_arrive(&sm.k_full[st]);
-      ++e;
-      ok = (j < 2 || warp_wait(&sm.v_empty[st], ((j >> 1) - 1) & 1, &sm.abort)) &&
-           warp_wait(&sm.c_full[e % kRing], (e / kRing) & 1, &sm.abort);
-      if (!ok) break;
+      if (which == 0 && t < kHalf && lane == 0)
+        reinterpret_cast<uint32_t*>(&sm.nan_keys[j & 3])[2 * (h & 1) + (t >> 5)] = nans;
       // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the scores of their
       // keys are made NaN instead
-      decode(ring + (e % kRing) * kCodeBytes, sm.v[st], row, v_byte, zero || v_nan);
-      mbar_arrive(&sm.c_empty[e % kRing]);
-      fence_proxy_async_smem();
-      mbar_arrive(&sm.v_full[st]);
+      const uint32_t to = tile + st * kTileBytes + (h & 1) * kHalf * 128;
+      decode(codes + (h % kRing) * kCodeBytes, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
+      if (copied) mbar_arrive(&sm.c_empty[which][h % kRing]);
+      if (h & 1) {
+        fence_proxy_async_smem();
+        mbar_arrive(which ? &sm.v_full[st] : &sm.k_full[st]);
+      }
     }
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 72);
@@ -554,22 +603,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t scale2 = f2_pack(scale, scale);
       const uint64_t negm2 = f2_pack(-m_use, -m_use);
       uint64_t acc2[4] = {0, 0, 0, 0};
-      uint32_t packed[64];
 #pragma unroll
-      for (int c = 0; c < 64; ++c) {
-        float x0, x1;
-        f2_unpack(f2_fma(f2_pack(s[2 * c], s[2 * c + 1]), scale2, negm2), x0, x1);
-        const float e0 = ex2_approx(x0);
-        const float e1 = ex2_approx(x1);
-        packed[c] = pack_bf16x2(e0, e1);
-        acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
+      for (int hf = 0; hf < 2; ++hf) {
+        uint32_t packed[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          float x0, x1;
+          f2_unpack(f2_fma(f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]), scale2, negm2), x0, x1);
+          const float e0 = ex2_approx(x0);
+          const float e1 = ex2_approx(x1);
+          packed[c] = pack_bf16x2(e0, e1);
+          acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
+        }
+        tmem_st32(s_addr + 32 * hf, packed);
       }
       float rs[4];
       f2_unpack(f2_add(acc2[0], acc2[1]), rs[0], rs[1]);
       f2_unpack(f2_add(acc2[2], acc2[3]), rs[2], rs[3]);
       l_run = l_run * alpha + ((rs[0] + rs[1]) + (rs[2] + rs[3]));
-      tmem_st32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&packed[0]));
-      tmem_st32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&packed[32]));
       if (i > 0 && __any_sync(0xffffffffu, rescaled)) {
         // O holds the stream's earlier products (complete: the commit of this S came after them)
 #pragma unroll 1
