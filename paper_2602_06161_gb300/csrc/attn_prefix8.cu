@@ -10,7 +10,7 @@
 // The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r
 // of head hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view, cut into Q tiles of 128.
 // A CTA takes one or two Q tiles against the KV tiles (128 keys) of one of nsplit parts of what its rows
-// see. Codes arrive by bulk copies (64 rows are 8 KB in one piece); one warpgroup decodes K and one V to bf16
+// see. Codes arrive by bulk copies (128 rows are 16 KB in one piece); one warpgroup decodes K and one V to bf16
 // (exact: a row's scale is a power of two) into the swizzled layout that the tensor cores read, and S = Q K^T, O += P V
 // run as tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each:
 //   shared Q (kPair = false): both streams are the same Q tile, on the even and the odd KV tiles, with sums and an
@@ -21,7 +21,8 @@
 //
 // Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16
 // issues the products; 17 and 18 issue the copies of K and V.
-// Shared memory: Q (32 or 64 KB) | rings of 8 KB entries of codes, K and V (4 or 2 each) | K, V in bf16 (2 x 32 KB each).
+// Shared memory: Q (32 or 64 KB) | rings of two entries of K and of V codes, 128 or 64 rows each | K, V in bf16 (2 x 32 KB
+// each).
 // Tensor memory: S0 | S1 (P overwrites their first 64 columns) | O0 | O1, 128 columns each.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -44,22 +45,21 @@ constexpr int kBM = 128;                   // rows per Q tile
 constexpr int kBN = 128;                   // keys per KV tile
 constexpr int kTileBytes = kBM * kD * 2;   // 32 KB
 constexpr int kBoxBytes = kTileBytes / 2;  // one 64-column, 128-byte-swizzled box
-constexpr int kHalf = kBN / 2;             // key rows of a ring entry
-constexpr int kCodeBytes = kHalf * kD;     // 8 KB of codes
 constexpr int kThreads = 640;
 constexpr int kDecodeWarp = 8, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kLaunchRegs = 96;            // registers per thread at launch (65536 / 640, rounded down to 8)
+// registers of the softmax, decode and issuing threads: a Q tile's softmax threads hold 128 scores each
 constexpr int kSoftmaxRegs = 160, kDecodeRegs = 56, kIssueRegs = 40;
 static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "register split");
+// setmaxnreg.inc takes no count below the thread's own, .dec none above it
+static_assert(kSoftmaxRegs >= kLaunchRegs && kDecodeRegs <= kLaunchRegs && kIssueRegs <= kLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
 
-struct Smem {
-  uint8_t q_and_ring[3 * kTileBytes];   // Q | rings of K codes and of V codes
-  uint8_t k[2][kTileBytes];
-  uint8_t v[2][kTileBytes];
+// Barriers and tables of a CTA.
+struct Ctl {
   uint64_t q_full;
-  uint64_t c_full[2][4], c_empty[2][4]; // rings of K and V codes
+  uint64_t c_full[2][2], c_empty[2][2]; // rings of K and V codes
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t s_full[2], p_full[2];        // per stream
   uint64_t o_full, drain;
@@ -67,6 +67,13 @@ struct Smem {
   int abort;
   int lo, hi;                           // keys that some row of the CTA sees
   uint4 nan_keys[4];                    // per KV tile in turn: keys with a V row of NaN
+};
+
+struct Smem {
+  uint8_t q_and_ring[3 * kTileBytes];   // Q | rings of K codes and of V codes
+  uint8_t k[2][kTileBytes];
+  uint8_t v[2][kTileBytes];
+  Ctl ctl;
   int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
 };
 constexpr size_t kSmemBytes = sizeof(Smem) + 1024;
@@ -105,7 +112,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   const bool ok = mbar_wait(bar, parity, abort);
   return __all_sync(0xffffffffu, ok);
 }
-
 // All 256 threads of the two softmax warpgroups.
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -151,40 +157,46 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap_log2) {
   return fmaf(-2.0f * cap_log2, rcp_approx(1.0f + t), cap_log2);
 }
 
-// Decodes half a row of codes: every other one of the eight 16-byte pieces of a row, into its row of a bf16 tile (two
+// Decodes a row of codes, or every other one of its eight 16-byte pieces (kPieces = 4), into its row of a bf16 tile (two
 // 64-column boxes, 16-byte chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are
 // the bf16 number code * 2^-120 (subnormal codes included), and one multiplication by m1 = 2^(120 + x - 127) gives the
 // value; where that is above bf16's range, m1 = 2^120 and kTwo says to multiply by m2 = 2^(x - 127) too. Both are
-// exact. The thread's pieces are u0 ^ 0, 2, 4, 6 with u0 the row's low bits (its partner's: u0 ^ 1), so that the reads
-// and writes of eight lanes meet every bank. src: address of piece u0; d0, d1: of its first chunk, in its box and
-// in the other one.
-template <bool kTwo>
-__device__ __forceinline__ void decode_half_row(uint32_t src, uint32_t d0, uint32_t d1, uint32_t m1, uint32_t m2) {
-  uint4 next = lds128(src);
+// exact. A row's pieces are taken in the order u0 ^ 0, 1, ... (u0 ^ 0, 2, ... of the half) with u0 the row's low bits, so
+// that the reads and writes of eight lanes meet every bank. src: address of piece u0; d0, d1: of its first chunk, in
+// its box and in the other one.
+template <int kPieces, bool kTwo>
+__device__ __forceinline__ void decode_row(uint32_t src, uint32_t d0, uint32_t d1, uint32_t m1, uint32_t m2) {
+  constexpr int kStep = 8 / kPieces;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 c = next;
-    if (i < 3) next = lds128(src ^ (32u * (i + 1)));
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t o[8];
+  for (int i0 = 0; i0 < kPieces; i0 += 4) {
+    uint4 c[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // bytes 0, 1 (2, 3) sign-extended to 16 bits, moved up by four bits
-      const uint32_t lo = (prmt<0x9180>(w[e]) << 4) & 0x87f087f0u;
-      const uint32_t hi = (prmt<0xb3a2>(w[e]) << 4) & 0x87f087f0u;
-      o[2 * e] = mul_bf16x2(lo, m1);
-      o[2 * e + 1] = mul_bf16x2(hi, m1);
-      if (kTwo) {
-        o[2 * e] = mul_bf16x2(o[2 * e], m2);
-        o[2 * e + 1] = mul_bf16x2(o[2 * e + 1], m2);
+    for (int i = 0; i < 4; ++i) c[i] = lds128(src ^ (16u * kStep * (i0 + i)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+      uint32_t o[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // bytes 0, 1 (2, 3) sign-extended to 16 bits, moved up by four bits
+        const uint32_t lo = (prmt<0x9180>(w[e]) << 4) & 0x87f087f0u;
+        const uint32_t hi = (prmt<0xb3a2>(w[e]) << 4) & 0x87f087f0u;
+        o[2 * e] = mul_bf16x2(lo, m1);
+        o[2 * e + 1] = mul_bf16x2(hi, m1);
+        if (kTwo) {
+          o[2 * e] = mul_bf16x2(o[2 * e], m2);
+          o[2 * e + 1] = mul_bf16x2(o[2 * e + 1], m2);
+        }
       }
+      const uint32_t x = kStep * (i0 + i);   // piece u0 ^ x
+      const uint32_t d = (x & 4 ? d1 : d0) ^ ((x & 3) << 5);
+      sts128(d, o[0], o[1], o[2], o[3]);
+      sts128(d ^ 16u, o[4], o[5], o[6], o[7]);
     }
-    const uint32_t d = (i & 2 ? d1 : d0) ^ (i & 1 ? 64u : 0u);
-    sts128(d, o[0], o[1], o[2], o[3]);
-    sts128(d ^ 16u, o[4], o[5], o[6], o[7]);
   }
 }
 
+template <int kPieces>
 __device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, int x, bool zero) {
   // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
   const bool two = x > 134 && x <= kExpMax;
@@ -194,30 +206,162 @@ __device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, i
   if (zero) m1 = 0;
   m1 |= m1 << 16;
   m2 |= m2 << 16;
-  if (__any_sync(0xffffffffu, two)) decode_half_row<true>(src, d0, d1, m1, m2);
-  else decode_half_row<false>(src, d0, d1, m1, m2);
+  if (__any_sync(0xffffffffu, two)) decode_row<kPieces, true>(src, d0, d1, m1, m2);
+  else decode_row<kPieces, false>(src, d0, d1, m1, m2);
 }
 
-// The exponent bytes of row lrow of four half tiles from half h on (zero from row `left` on).
+// The exponent bytes of row lrow of four ring entries of kRows rows from entry e on (zero from row `left` on).
+template <int kRows>
 struct FourBytes {
   uint32_t v[4];
-  __device__ __forceinline__ void load(const uint8_t* exps, int h, int lrow, int left) {
+  __device__ __forceinline__ void load(const uint8_t* exps, int e, int lrow, int left) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = (h + i) * kHalf + lrow;
+      const int row = (e + i) * kRows + lrow;
       v[i] = row < left ? __ldg(exps + row) : 0u;
     }
   }
-  __device__ __forceinline__ uint32_t packed() const { return v[0] | (v[1] << 8) | (v[2] << 16) | (v[3] << 24); }
+  // (the asm keeps the compiler from packing them, and so waiting for the loads, where they are issued)
+  __device__ __forceinline__ uint32_t packed() {
+    asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]));
+    return v[0] | (v[1] << 8) | (v[2] << 16) | (v[3] << 24);
+  }
 };
+
+// Barriers and tensor memory, by one warp.
+__device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32_t tmem_columns) {
+  if ((threadIdx.x & 31) == 0) {
+    mbar_init(&ctl.q_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      for (int w = 0; w < 2; ++w) {
+        mbar_init(&ctl.c_full[w][i], 1);
+        mbar_init(&ctl.c_empty[w][i], 128);
+      }
+      mbar_init(&ctl.k_full[i], 128);
+      mbar_init(&ctl.k_empty[i], 1);
+      mbar_init(&ctl.v_full[i], 128);
+      mbar_init(&ctl.v_empty[i], 1);
+      mbar_init(&ctl.s_full[i], 1);
+      mbar_init(&ctl.p_full[i], 128);
+    }
+    mbar_init(&ctl.o_full, 1);
+    mbar_init(&ctl.drain, 1);
+    ctl.abort = 0;
+    ctl.lo = 0x7fffffff;
+    ctl.hi = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(tm_q);
+  }
+  __syncwarp();
+  tmem_alloc(&ctl.tmem_base, tmem_columns);
+  tmem_relinquish();
+}
+
+// Copies the codes of K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 through their ring of kRing entries of kRows
+// rows; one thread. With which = 0 its Q tiles are on their way to ctl.q_full already.
+template <int kRing, int kRows>
+__device__ __forceinline__ void copy_codes(Ctl& ctl, const Params& p, int which, uint8_t* ring, size_t mem0, int j0, int nt) {
+  const uint8_t* src = (which ? p.v8 : p.k8) + mem0 * kD;
+  const uint32_t dst = smem_u32(ring) + which * kRing * kRows * kD;
+  const int left = min(p.Lk - j0 * kBN, nt * kBN);   // keys of this part
+  const int entries = (left + kRows - 1) / kRows;
+  int e = 0;
+  bool ok = true;
+  for (; e < entries; ++e) {
+    const int st = e % kRing;
+    if (e >= kRing) ok = mbar_wait(&ctl.c_empty[which][st], (e / kRing - 1) & 1, &ctl.abort);
+    if (!ok) break;
+    const uint32_t bytes = static_cast<uint32_t>(min(kRows, left - e * kRows)) * kD;
+    mbar_arrive_expect_tx(&ctl.c_full[which][st], bytes);
+    bulk_load(dst + st * kRows * kD, src + (static_cast<size_t>(j0) * kBN + static_cast<size_t>(e) * kRows) * kD, bytes,
+              &ctl.c_full[which][st]);
+  }
+  if (!ok) {
+    if (!ctl.abort) report_status(p.status, kStatusTimeout, 70);
+    ctl.abort = 1;
+  }
+  // every copy lands before the CTA's shared memory is released, whatever the other roles did
+  if (which == 0) mbar_wait(&ctl.q_full, 0, nullptr);
+  for (int f = max(0, e - kRing); f < e; ++f) mbar_wait(&ctl.c_full[which][f % kRing], (f / kRing) & 1, nullptr);
+}
+
+// Decodes K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 into two bf16 tiles in turn; 128 threads, one or two a
+// row of a ring entry.
+template <int kRing, int kRows>
+__device__ __forceinline__ void decode_tiles(Ctl& ctl, const Params& p, int which, uint8_t* ring, uint8_t* k_tiles,
+                                             uint8_t* v_tiles, size_t mem0, int j0, int nt) {
+  constexpr int kPerTile = kBN / kRows;          // ring entries of a KV tile
+  const int t = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const int lrow = t & (kRows - 1);
+  const uint32_t u0 = static_cast<uint32_t>((lrow ^ (t / kRows)) & 7);
+  const uint32_t codes = smem_u32(ring) + which * kRing * kRows * kD + lrow * kD + u0 * 16;
+  const uint32_t tile = smem_u32(which ? v_tiles : k_tiles) + lrow * 128 + (((u0 & 3) << 5) ^ ((lrow & 7) << 4));
+  const uint32_t box = (u0 >> 2) * kBoxBytes;
+  const int first = j0 * kBN;                    // this part's first key
+  const int left = min(p.Lk - first, nt * kBN);  // keys of this part
+  // exponent bytes are fetched four entries at a time, four to eight ahead of their use
+  const uint8_t* exps = (which ? p.v_exp : p.k_exp) + mem0 + first;
+  const uint8_t* v_exps = p.v_exp + mem0 + first;
+  FourBytes<kRows> x_next, v_next;
+  x_next.load(exps, 0, lrow, left);
+  v_next.load(v_exps, 0, lrow, left);
+  uint32_t xs = 0, vs = 0;
+  bool ok = true;
+  for (int h = 0; h < kPerTile * nt; ++h) {
+    const int j = h / kPerTile, st = j & 1, part = h % kPerTile;
+    if ((h & 3) == 0) {
+      xs = x_next.packed();
+      x_next.load(exps, h + 4, lrow, left);
+      if (which == 0) {
+        vs = v_next.packed();
+        v_next.load(v_exps, h + 4, lrow, left);
+      }
+    }
+    const bool zero = h * kRows + lrow >= left;
+    const int x = (xs >> (8 * (h & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (h & 3))) & 255);
+    const bool v_nan = xv > kExpMax;
+    const uint32_t nans = __ballot_sync(0xffffffffu, v_nan);
+    if (part == 0 && j >= 2) ok = warp_wait(which ? &ctl.v_empty[st] : &ctl.k_empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
+    const bool copied = h * kRows < left;        // an entry past the memory is not copied
+    ok = ok && (!copied || warp_wait(&ctl.c_full[which][h % kRing], (h / kRing) & 1, &ctl.abort));
+    if (!ok) break;
+    // tile j - 4 has passed its softmax: S of tile j - 2 came after it
+    if (which == 0 && t < kRows && lane == 0)
+      reinterpret_cast<uint32_t*>(&ctl.nan_keys[j & 3])[kRows / 32 * part + (t >> 5)] = nans;
+    // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the scores of their
+    // keys are made NaN instead
+    const uint32_t to = tile + st * kTileBytes + part * kRows * 128;
+    decode<kRows / 16>(codes + (h % kRing) * kRows * kD, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
+    if (copied) mbar_arrive(&ctl.c_empty[which][h % kRing]);
+    if (part == kPerTile - 1) {
+      fence_proxy_async_smem();
+      mbar_arrive(which ? &ctl.v_full[st] : &ctl.k_full[st]);
+    }
+  }
+  if (!ok && lane == 0) {
+    if (!ctl.abort) report_status(p.status, kStatusTimeout, 72);
+    ctl.abort = 1;
+  }
+}
+
+// This part's KV tiles among those that the CTA's rows see.
+struct Part {
+  int j0, nt;
+};
+__device__ __forceinline__ Part part_of(int lo, int hi, int ks, int nsplit) {
+  const int t0 = hi > 0 ? lo / kBN : 0, t1 = hi > 0 ? (hi + kBN - 1) / kBN : 0;
+  const int each = (t1 - t0) / nsplit, more = (t1 - t0) % nsplit;
+  return Part{t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0)};
+}
 
 template <bool kPair, bool kCap>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_prefix8_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Ctl& ctl = sm.ctl;
   constexpr int kQTiles = kPair ? 2 : 1;
-  constexpr int kRing = kPair ? 2 : 4;   // entries of each ring
+  constexpr int kRing = 2, kEntry = kPair ? 64 : 128;   // entries of each ring, and their rows
   uint8_t* const sm_q = sm.q_and_ring;
   uint8_t* const ring = sm.q_and_ring + kQTiles * kTileBytes;
 
@@ -234,39 +378,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;    // packed row 0 in [B Hq Lq, D]
   const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;                  // the KV head's first memory row
 
-  if (warp == kMmaWarp) {
-    if (lane == 0) {
-      mbar_init(&sm.q_full, 1);
-      for (int i = 0; i < 4; ++i)
-        for (int w = 0; w < 2; ++w) {
-          mbar_init(&sm.c_full[w][i], 1);
-          mbar_init(&sm.c_empty[w][i], 128);
-        }
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&sm.k_full[i], 128);
-        mbar_init(&sm.k_empty[i], 1);
-        mbar_init(&sm.v_full[i], 128);
-        mbar_init(&sm.v_empty[i], 1);
-        mbar_init(&sm.s_full[i], 1);
-        mbar_init(&sm.p_full[i], kBM);
-      }
-      mbar_init(&sm.o_full, 1);
-      mbar_init(&sm.drain, 1);
-      sm.abort = 0;
-      sm.lo = 0x7fffffff;
-      sm.hi = 0;
-      fence_mbar_init();
-      tma_prefetch_desc(&tm_q);
-    }
-    __syncwarp();
-    tmem_alloc(&sm.tmem_base, 512);
-    tmem_relinquish();
-  }
+  if (warp == kMmaWarp) set_up(ctl, &tm_q, 512);
   if (p.n_seeds > 0 && tid < 2 * kBM) sm.slot[tid] = kNoSlot;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tbase = sm.tmem_base;
+  const uint32_t tbase = ctl.tmem_base;
   griddep_wait();
   griddep_launch_dependents();
 
@@ -280,62 +397,35 @@ __global__ void __launch_bounds__(kThreads, 1)
   int row_lo = 0, row_hi = p.Lk;
   if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
   if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
-  int t0 = 0, t1 = (p.Lk + kBN - 1) / kBN;            // KV tiles of which some row sees a key
+  int lo_key = 0, hi_key = p.Lk;                      // keys that some row sees
   if (p.key_lo != nullptr || p.key_hi != nullptr) {
     if (warp < kDecodeWarp) {
       const bool some = valid && row_lo < row_hi;
       const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff);
       const int hi = __reduce_max_sync(0xffffffffu, some ? row_hi : 0);
       if (lane == 0 && hi > 0) {
-        atomicMin(&sm.lo, lo);
-        atomicMax(&sm.hi, hi);
+        atomicMin(&ctl.lo, lo);
+        atomicMax(&ctl.hi, hi);
       }
     }
     __syncthreads();
-    const int lo = sm.lo, hi = sm.hi;
-    t0 = hi > 0 ? lo / kBN : 0;
-    t1 = hi > 0 ? (hi + kBN - 1) / kBN : 0;
+    lo_key = ctl.lo, hi_key = ctl.hi;
   }
-  // this part's KV tiles: j0 .. j0 + nt - 1
-  const int each = (t1 - t0) / p.nsplit, more = (t1 - t0) % p.nsplit;
-  const int j0 = t0 + ks * each + min(ks, more);
-  const int nt = each + (ks < more ? 1 : 0);
+  const Part part = part_of(lo_key, hi_key, ks, p.nsplit);
+  const int j0 = part.j0, nt = part.nt;
   const bool two_tiles = kPair && p0 + kBM < n_packed;   // the pair's second Q tile has rows
 
   if (warp >= kMmaWarp) {
     setmaxnreg_dec<kIssueRegs>();
-    const int which = warp - kLoadWarp;   // 0: K (and Q), 1: V
-    if ((which == 0 || which == 1) && lane == 0 && nt > 0) {
-      // ---------------- copies ----------------
-      if (which == 0) {
-        mbar_arrive_expect_tx(&sm.q_full, kQTiles * kTileBytes);
+    if ((warp == kLoadWarp || warp == kLoadWarp + 1) && lane == 0 && nt > 0) {
+      if (warp == kLoadWarp) {
+        mbar_arrive_expect_tx(&ctl.q_full, kQTiles * kTileBytes);
         for (int t = 0; t < kQTiles; ++t)
           for (int h = 0; h < 2; ++h)
-            tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &sm.q_full, 64 * h,
+            tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &ctl.q_full, 64 * h,
                         static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
       }
-      const uint8_t* src = (which ? p.v8 : p.k8) + mem0 * kD;
-      uint8_t* const dst = ring + which * kRing * kCodeBytes;
-      // half tiles with a key of the memory
-      const int halves = min(2 * nt, (p.Lk - j0 * kBN + kHalf - 1) / kHalf);
-      int e = 0;
-      bool ok = true;
-      for (; e < halves; ++e) {
-        const int st = e % kRing;
-        if (e >= kRing) ok = mbar_wait(&sm.c_empty[which][st], (e / kRing - 1) & 1, &sm.abort);
-        if (!ok) break;
-        const int key0 = j0 * kBN + e * kHalf;
-        const uint32_t bytes = static_cast<uint32_t>(min(kHalf, p.Lk - key0)) * kD;
-        mbar_arrive_expect_tx(&sm.c_full[which][st], bytes);
-        bulk_load(smem_u32(dst + st * kCodeBytes), src + static_cast<size_t>(key0) * kD, bytes, &sm.c_full[which][st]);
-      }
-      if (!ok) {
-        if (!sm.abort) report_status(p.status, kStatusTimeout, 70);
-        sm.abort = 1;
-      }
-      // every copy lands before the CTA's shared memory is released, whatever the other roles did
-      if (which == 0) mbar_wait(&sm.q_full, 0, nullptr);
-      for (int f = max(0, e - kRing); f < e; ++f) mbar_wait(&sm.c_full[which][f % kRing], (f / kRing) & 1, nullptr);
+      copy_codes<kRing, kEntry>(ctl, p, warp - kLoadWarp, ring, mem0, j0, nt);
     } else if (warp == kMmaWarp && lane == 0 && nt > 0) {
       // ---------------- products ----------------
       constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
@@ -353,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint64_t off = static_cast<uint64_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
           umma_ss(tbase + s * kBN, a + off, kb + off, id_qk, kk > 0 ? 1u : 0u);
         }
-        umma_commit(&sm.s_full[s]);
+        umma_commit(&ctl.s_full[s]);
       };
       // O[s] (+)= P[s] . V(stage)
       auto issue_pv = [&](int s, int st, bool acc) {
@@ -365,125 +455,73 @@ __global__ void __launch_bounds__(kThreads, 1)
                   vb + static_cast<uint64_t>((kk * 2048) >> 4), id_pv, (acc || kk > 0) ? 1u : 0u);
       };
       auto wait = [&](uint64_t* bar, int phase) {
-        const bool ok = mbar_wait(bar, phase & 1, &sm.abort);
+        const bool ok = mbar_wait(bar, phase & 1, &ctl.abort);
         if (ok) tc_fence_after_sync();
         return ok;
       };
-      bool ok = wait(&sm.q_full, 0);
+      bool ok = wait(&ctl.q_full, 0);
       if (kPair) {
-        if (ok && (ok = wait(&sm.k_full[0], 0))) {
+        if (ok && (ok = wait(&ctl.k_full[0], 0))) {
           issue_s(0, 0);
           if (two_tiles) issue_s(1, 0);
-          umma_commit(&sm.k_empty[0]);
+          umma_commit(&ctl.k_empty[0]);
         }
         for (int j = 0; j < nt && ok; ++j) {
           const int st = j & 1;
           const bool next = j + 1 < nt;
-          ok = wait(&sm.p_full[0], j) && wait(&sm.v_full[st], j >> 1);
+          ok = wait(&ctl.p_full[0], j) && wait(&ctl.v_full[st], j >> 1);
           if (!ok) break;
           issue_pv(0, st, j > 0);
           if (next) {
-            ok = wait(&sm.k_full[st ^ 1], (j + 1) >> 1);
+            ok = wait(&ctl.k_full[st ^ 1], (j + 1) >> 1);
             if (!ok) break;
             issue_s(0, st ^ 1);
           }
           if (two_tiles) {
-            ok = wait(&sm.p_full[1], j);
+            ok = wait(&ctl.p_full[1], j);
             if (!ok) break;
             issue_pv(1, st, j > 0);
             if (next) issue_s(1, st ^ 1);
           }
-          umma_commit(&sm.v_empty[st]);
-          if (next) umma_commit(&sm.k_empty[st ^ 1]);
+          umma_commit(&ctl.v_empty[st]);
+          if (next) umma_commit(&ctl.k_empty[st ^ 1]);
         }
       } else {
         // stream j & 1 takes tile j, from stage j & 1
         for (int j = 0; j < 2 && j < nt && ok; ++j) {
-          ok = wait(&sm.k_full[j], 0);
+          ok = wait(&ctl.k_full[j], 0);
           if (!ok) break;
           issue_s(j, j);
-          umma_commit(&sm.k_empty[j]);
+          umma_commit(&ctl.k_empty[j]);
         }
         for (int j = 0; j < nt && ok; ++j) {
           const int s = j & 1;
-          ok = wait(&sm.p_full[s], j >> 1) && wait(&sm.v_full[s], j >> 1);
+          ok = wait(&ctl.p_full[s], j >> 1) && wait(&ctl.v_full[s], j >> 1);
           if (!ok) break;
           issue_pv(s, s, j > 1);
-          umma_commit(&sm.v_empty[s]);
+          umma_commit(&ctl.v_empty[s]);
           if (j + 2 < nt) {
-            ok = wait(&sm.k_full[s], (j + 2) >> 1);
+            ok = wait(&ctl.k_full[s], (j + 2) >> 1);
             if (!ok) break;
             issue_s(s, s);
-            umma_commit(&sm.k_empty[s]);
+            umma_commit(&ctl.k_empty[s]);
           }
         }
       }
       if (ok) {
-        umma_commit(&sm.o_full);
+        umma_commit(&ctl.o_full);
       } else {
-        if (!sm.abort) report_status(p.status, kStatusTimeout, 71);
-        sm.abort = 1;
+        if (!ctl.abort) report_status(p.status, kStatusTimeout, 71);
+        ctl.abort = 1;
       }
       // all tensor-core work of this CTA completes before tensor memory is released
-      umma_commit(&sm.drain);
-      mbar_wait(&sm.drain, 0, nullptr);
+      umma_commit(&ctl.drain);
+      mbar_wait(&ctl.drain, 0, nullptr);
     }
     __syncwarp();
   } else if (warp >= kDecodeWarp) {
-    // ---------------- decoding ----------------
     setmaxnreg_dec<kDecodeRegs>();
-    const int which = (warp - kDecodeWarp) >> 2;   // 0: K, 1: V
-    const int t = tid & 127;
-    const int lrow = t & (kHalf - 1);              // two threads a row of a half tile
-    const uint32_t u0 = static_cast<uint32_t>((lrow ^ (t >> 6)) & 7);
-    const uint32_t codes = smem_u32(ring + which * kRing * kCodeBytes + lrow * kD) + u0 * 16;
-    const uint32_t tile = smem_u32(which ? sm.v[0] : sm.k[0]) + lrow * 128 + (((u0 & 3) << 5) ^ ((lrow & 7) << 4));
-    const uint32_t box = (u0 >> 2) * kBoxBytes;
-    const int first = j0 * kBN;                    // this part's first key
-    const int left = min(p.Lk - first, nt * kBN);  // keys of this part
-    // exponent bytes are fetched four half tiles at a time, four to eight ahead of their use
-    const uint8_t* exps = (which ? p.v_exp : p.k_exp) + mem0 + first;
-    const uint8_t* v_exps = p.v_exp + mem0 + first;
-    FourBytes x_next, v_next;
-    x_next.load(exps, 0, lrow, left);
-    v_next.load(v_exps, 0, lrow, left);
-    uint32_t xs = 0, vs = 0;
-    bool ok = true;
-    for (int h = 0; h < 2 * nt; ++h) {   // half h & 1 of tile h / 2
-      const int j = h >> 1, st = j & 1;
-      if ((h & 3) == 0) {
-        xs = x_next.packed();
-        x_next.load(exps, h + 4, lrow, left);
-        if (which == 0) {
-          vs = v_next.packed();
-          v_next.load(v_exps, h + 4, lrow, left);
-        }
-      }
-      const bool zero = h * kHalf + lrow >= left;
-      const int x = (xs >> (8 * (h & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (h & 3))) & 255);
-      const bool v_nan = xv > kExpMax;
-      const uint32_t nans = __ballot_sync(0xffffffffu, v_nan);
-      if ((h & 1) == 0 && j >= 2) ok = warp_wait(which ? &sm.v_empty[st] : &sm.k_empty[st], ((j >> 1) - 1) & 1, &sm.abort);
-      const bool copied = h * kHalf < left;        // a half past the memory is not copied
-      ok = ok && (!copied || warp_wait(&sm.c_full[which][h % kRing], (h / kRing) & 1, &sm.abort));
-      if (!ok) break;
-      // tile j - 4 has passed its softmax: S of tile j - 2 came after it
-      if (which == 0 && t < kHalf && lane == 0)
-        reinterpret_cast<uint32_t*>(&sm.nan_keys[j & 3])[2 * (h & 1) + (t >> 5)] = nans;
-      // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the scores of their
-      // keys are made NaN instead
-      const uint32_t to = tile + st * kTileBytes + (h & 1) * kHalf * 128;
-      decode(codes + (h % kRing) * kCodeBytes, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
-      if (copied) mbar_arrive(&sm.c_empty[which][h % kRing]);
-      if (h & 1) {
-        fence_proxy_async_smem();
-        mbar_arrive(which ? &sm.v_full[st] : &sm.k_full[st]);
-      }
-    }
-    if (!ok && lane == 0) {
-      if (!sm.abort) report_status(p.status, kStatusTimeout, 72);
-      sm.abort = 1;
-    }
+    decode_tiles<kRing, kEntry>(ctl, p, (warp - kDecodeWarp) >> 2, ring, sm.k[0], sm.v[0], mem0, j0, nt);
   } else {
     // ---------------- softmax ----------------
     setmaxnreg_inc<kSoftmaxRegs>();
@@ -533,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int jend = kPair && stream == 1 && !two_tiles ? 0 : nt;
     int i = 0;   // the stream's step
     for (int j = kPair ? 0 : stream; j < jend; j += jstep, ++i) {
-      ok = warp_wait(&sm.s_full[stream], i & 1, &sm.abort);
+      ok = warp_wait(&ctl.s_full[stream], i & 1, &ctl.abort);
       if (!ok) break;
       tc_fence_after_sync();
       const int key0 = (j0 + j) * kBN;
@@ -547,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_st_wait();
         }
         tc_fence_before_sync();
-        mbar_arrive(&sm.p_full[stream]);
+        mbar_arrive(&ctl.p_full[stream]);
         continue;
       }
       uint32_t raw[4][32];
@@ -560,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < kBN; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
       }
-      const uint4 nan4 = sm.nan_keys[j & 3];
+      const uint4 nan4 = ctl.nan_keys[j & 3];
       if ((nan4.x | nan4.y | nan4.z | nan4.w) != 0) {
         const uint32_t nw[4] = {nan4.x, nan4.y, nan4.z, nan4.w};
 #pragma unroll
@@ -635,12 +673,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tmem_st_wait();
       tc_fence_before_sync();
-      mbar_arrive(&sm.p_full[stream]);
+      mbar_arrive(&ctl.p_full[stream]);
     }
-    if (ok && nt > 0) ok = warp_wait(&sm.o_full, 0, &sm.abort);
+    if (ok && nt > 0) ok = warp_wait(&ctl.o_full, 0, &ctl.abort);
     if (!ok && lane == 0) {
-      if (!sm.abort) report_status(p.status, kStatusTimeout, 73);
-      sm.abort = 1;
+      if (!ctl.abort) report_status(p.status, kStatusTimeout, 73);
+      ctl.abort = 1;
     }
 
     // ---------------- the rows' results ----------------
@@ -737,6 +775,636 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// ---------------------------------------------------------------------------
+// Few rows
+// ---------------------------------------------------------------------------
+// Decoding a KV tile moves 192 KB through shared memory (codes in and out, bf16 in, both products' operands), which
+// takes longer than the tile's 32 KB take from HBM, and a Q tile of 128 rows costs the tensor cores the same for one
+// row as for 128. For up to kN = 16 or 32 packed rows nothing is decoded: the products are turned over,
+//   S^T = K Q^T (128 keys x rows),  O^T += V^T P^T (128 columns x rows),
+// and read the e4m3 codes as they are (kind::f8f6f4). Q and P are 8-bit operands there, so each is split in three: a fp16 number of at
+// most 9 significant bits is the sum of three e5m2 numbers (e5m2 is the upper byte of fp16: the parts
+// are truncations of what the parts before leave, each exact). The parts are columns of their own, 3 kN in all, whose
+// products add up in fp32.
+//   Q: bf16 has 8 bits, so the parts are exact; a row is scaled by a power of two to a maximum of 2^14 .. 2^15 first.
+//   P: the V rows' scales belong to the contracted index, so they are taken into the weights: with e_j = x_j - 127 of
+//      the V row, P'_j = 2^(s_j + e_j - m), m the row's reference for s_j + e_j, and the sum has 2^(s_j - m) of its
+//      own. P' is rounded to 9 bits (off by at most 2^-9 of it; bf16 is by 2^-8) and scaled by 2^12: what is
+//      2^-28 of the largest is still held (e5m2's smallest is 2^-16). References take max(e_j, -90) for e_j, so that a row
+//      whose largest weight meets a V row far smaller or larger than the others' has a sum within fp32's range.
+// A softmax thread is a key: its scales are scalars of the thread. The keys' maximum of a row is only taken
+// when some score is above the row's reference by more than the threshold (one vote a tile); sums stay with the
+// threads until the end. V codes of NaN would reach every row (0 * NaN), so four warps look for them, put zeros in
+// their places and report their keys, whose scores become NaN.
+// Streams: alternate KV tiles with sums and an accumulator of their own, merged at the end.
+// Roles (480 threads): warps 0-3, 4-7 softmax of the streams; 8-11 NaN codes; 12 products; 13, 14 copies of K, V.
+// Tensor memory: S0 | S1 | O0 | O1, 3 kN columns each.
+constexpr int kRowsThreads = 480;
+constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsLoadWarp = 13;
+constexpr float kRowsThreshold = 2.0f;  // log2 units, of the references' changes
+constexpr float kPBits = 12.0f;         // P' carries 2^12 (and is at most 2^14, below fp16's largest)
+constexpr int kEvFloor = -90;
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// Completes the warp's loads; the registers pass through so that none is used before.
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// D[tmem] (+)= A[smem] . B[smem] of 8-bit operands
+__device__ __forceinline__ void umma_ss_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor for kind::f8f6f4: A e4m3, B e5m2, fp32 accumulation; mn: both are MN-major.
+__host__ __device__ constexpr uint32_t idesc_e4m3_e5m2(int M, int N, bool mn) {
+  return (1u << 4) | (0u << 7) | (1u << 10) | ((mn ? 3u : 0u) << 15) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// Barrier of one stream's 128 softmax threads, and with the vote whether any of them says so.
+__device__ __forceinline__ void stream_sync(int stream) { asm volatile("bar.sync %0, 128;" ::"r"(2 + stream) : "memory"); }
+__device__ __forceinline__ bool stream_any(int stream, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(x ? 1u : 0u), "r"(2 + stream)
+      : "memory");
+  return r != 0;
+}
+
+// fp32 numbers as integers of the same order (no NaN), and back.
+__device__ __forceinline__ int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+
+// Two fp16 numbers of at most 9 significant bits as three pairs of e5m2 numbers (in the upper bytes of the halves).
+__device__ __forceinline__ void split3(uint32_t x, uint32_t (&part)[3]) {
+  part[0] = x & 0xff00ff00u;
+  const __half2 r1 = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&part[0]));
+  const uint32_t u1 = *reinterpret_cast<const uint32_t*>(&r1);
+  part[1] = u1 & 0xff00ff00u;
+  const __half2 r2 = __hsub2(r1, *reinterpret_cast<const __half2*>(&part[1]));
+  part[2] = *reinterpret_cast<const uint32_t*>(&r2);
+}
+
+template <int kN>
+struct RowsSmem {
+  static constexpr int kStages = 5;
+  uint8_t k[kStages][kBN * kD];
+  uint8_t v[kStages][kBN * kD];
+  uint8_t q[3 * kN * kD];         // parts of Q, [part, row][column]
+  uint8_t pt[2][kBN * 128];       // parts of each stream's P^T, [key][part, row], rows of 128 bytes
+  uint64_t q_full;
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t v_clean[kStages];      // looked through for NaN codes
+  uint64_t s_full[2], p_full[2], o_full, drain;
+  uint4 nan_keys[kStages];        // keys with a NaN code in V
+  int4 row[kN];                   // lo, hi, position of a seed row or -1
+  float4 fin[kN];                 // weights of the two accumulators and of the masked-input value, 1 / l
+  float m[2][kN];                 // per stream: the rows' references m - 12
+  float step[2][kN], alpha[2][kN];   // of the last change: the new reference less the old one, 2 to its opposite
+  int unseen[2][kN], any_unseen[2];  // per stream: rows that have seen no key, whose reference is not set
+  float red[2][4][kN];            // per stream and warp
+  float s_self[kN];
+  float q_scale[kN];              // power of two of a row, times log2(e) / sqrt(d) (capped: 2 log2(e) / (c sqrt(d)))
+  int slot[kN];
+  uint32_t tmem_base;
+  int abort;
+  int lo, hi;                     // keys that some row sees
+  int all_lo, all_hi;             // keys that every row sees
+};
+
+template <int kN, bool kCap>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+    attn_prefix8_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                             const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  using Sm = RowsSmem<kN>;
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int kStages = Sm::kStages;
+  constexpr int kCols = 3 * kN;
+  constexpr uint32_t kTmem = kN == 16 ? 256 : 512;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int ks = static_cast<int>(blockIdx.x) % p.nsplit;
+  int rest = static_cast<int>(blockIdx.x) / p.nsplit;
+  const int group = rest % p.n_groups;
+  rest /= p.n_groups;
+  const int hkv = rest % p.Hkv;
+  const int b = rest / p.Hkv;
+  const int n_packed = p.G * p.Lq;
+  const int p0 = group * kN;
+  const int n_rows = min(kN, n_packed - p0);
+  const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
+  const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;
+
+  if (warp == kRowsMmaWarp) {
+    if (lane == 0) {
+      mbar_init(&sm.q_full, 256);
+      for (int i = 0; i < kStages; ++i) {
+        mbar_init(&sm.k_full[i], 1);
+        mbar_init(&sm.k_empty[i], 1);
+        mbar_init(&sm.v_full[i], 1);
+        mbar_init(&sm.v_empty[i], 1);
+        mbar_init(&sm.v_clean[i], 128);
+      }
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&sm.s_full[i], 1);
+        mbar_init(&sm.p_full[i], 128);
+      }
+      mbar_init(&sm.o_full, 1);
+      mbar_init(&sm.drain, 1);
+      sm.abort = 0;
+      sm.any_unseen[0] = sm.any_unseen[1] = 1;
+      sm.lo = 0x7fffffff;
+      sm.hi = 0;
+      sm.all_lo = 0;
+      sm.all_hi = p.Lk;
+      fence_mbar_init();
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+    }
+    __syncwarp();
+    tmem_alloc(&sm.tmem_base, kTmem);
+    tmem_relinquish();
+  }
+  if (tid < kN) {
+    sm.slot[tid] = kNoSlot;
+    sm.s_self[tid] = -INFINITY;
+    sm.m[0][tid] = sm.m[1][tid] = 0.0f;
+    sm.unseen[0][tid] = sm.unseen[1][tid] = tid < n_rows ? 1 : 0;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tbase = sm.tmem_base;
+  griddep_wait();
+  griddep_launch_dependents();
+
+  // ---------------- the rows ----------------
+  const bool ranges = p.key_lo != nullptr || p.key_hi != nullptr;
+  const int r0 = p.Lq <= kN ? 0 : p0 % p.Lq;   // the rows stand at up to kN positions: r itself, or r - r0 around Lq
+  if (p.n_seeds > 0) {
+    const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
+    for (int s = tid; s < p.n_seeds; s += kRowsThreads) {
+      const int at = __ldg(seeds + s) - p.q0;
+      if (at < 0 || at >= p.Lq) continue;
+      const int i = at >= r0 ? at - r0 : at - r0 + p.Lq;
+      if (i < kN) atomicMin(&sm.slot[i], s);
+    }
+    __syncthreads();
+  }
+  if (ranges || p.n_seeds > 0) {
+    int my_slot = kNoSlot;
+    if (tid < kN) {
+      int lo = 0, hi = p.Lk, at = -1;
+      if (tid < n_rows) {
+        const int r = (p0 + tid) % p.Lq;
+        const size_t i = static_cast<size_t>(b) * p.Lq + r;
+        if (p.key_lo != nullptr) lo = max(0, __ldg(p.key_lo + i));
+        if (p.key_hi != nullptr) hi = min(p.Lk, __ldg(p.key_hi + i));
+        if (p.n_seeds > 0) {
+          my_slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
+          if (my_slot != kNoSlot) at = p.q0 + r;
+        }
+        if (ranges) {
+          if (lo < hi) {
+            atomicMin(&sm.lo, lo);
+            atomicMax(&sm.hi, hi);
+          }
+          atomicMax(&sm.all_lo, lo);
+          atomicMin(&sm.all_hi, hi);
+        }
+      }
+      sm.row[tid] = make_int4(lo, hi, at, 0);
+    }
+    __syncthreads();
+    // the slots by row, now that they are read by position
+    if (tid < kN) sm.slot[tid] = my_slot;
+    __syncthreads();
+  } else if (tid < kN) {
+    sm.row[tid] = make_int4(0, p.Lk, -1, 0);   // read by the softmax warps, after their barrier
+  }
+  const Part part = ranges ? part_of(sm.lo, sm.hi, ks, p.nsplit) : part_of(0, p.Lk, ks, p.nsplit);
+  const int j0 = part.j0, nt = part.nt;
+
+  if (warp >= kRowsMmaWarp) {
+    if ((warp == kRowsLoadWarp || warp == kRowsLoadWarp + 1) && lane == 0 && nt > 0) {
+      // ---------------- copies ----------------
+      const int which = warp - kRowsLoadWarp;
+      const CUtensorMap* tm = which ? &tm_v : &tm_k;
+      uint64_t* const full = which ? sm.v_full : sm.k_full;
+      uint64_t* const empty = which ? sm.v_empty : sm.k_empty;
+      bool ok = true;
+      int j = 0;
+      for (; j < nt; ++j) {
+        const int st = j % kStages;
+        if (j >= kStages) ok = mbar_wait(&empty[st], (j / kStages - 1) & 1, &sm.abort);
+        if (!ok) break;
+        mbar_arrive_expect_tx(&full[st], kBN * kD);
+        tma_load_4d(which ? sm.v[st] : sm.k[st], tm, &full[st], 0, (j0 + j) * kBN, hkv, b);   // zeros past the memory
+      }
+      if (!ok) {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 70);
+        sm.abort = 1;
+      }
+      // every copy lands before the CTA's shared memory is released, whatever the other roles did
+      for (int f = max(0, j - kStages); f < j; ++f) mbar_wait(&full[f % kStages], (f / kStages) & 1, nullptr);
+    } else if (warp == kRowsMmaWarp && lane == 0 && nt > 0) {
+      // ---------------- products ----------------
+      constexpr uint32_t id_s = idesc_e4m3_e5m2(kBN, kCols, false);
+      constexpr uint32_t id_o = idesc_e4m3_e5m2(kD, kCols, true);
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q), 16, 1024);
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
+      const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), 16, 1024);
+      const uint64_t dp = sdesc_sw128(smem_u32(sm.pt[0]), 16, 1024);
+      constexpr uint64_t kStageDesc = (kBN * kD) >> 4;
+      // S^T[s] = K(tile j) . Q^T
+      auto issue_s = [&](int j) {
+        const int s = j & 1, st = j % kStages;
+#pragma unroll
+        for (int kk = 0; kk < kD / 32; ++kk)
+          umma_ss_f8(tbase + s * kCols, dk + st * kStageDesc + ((kk * 32) >> 4), dq + ((kk * 32) >> 4), id_s, kk > 0 ? 1u : 0u);
+        umma_commit(&sm.s_full[s]);
+        umma_commit(&sm.k_empty[st]);
+      };
+      // O^T[s] (+)= V(tile j)^T . P[s]^T
+      auto issue_o = [&](int j) {
+        const int s = j & 1, st = j % kStages;
+#pragma unroll
+        for (int kk = 0; kk < kBN / 32; ++kk)
+          umma_ss_f8(tbase + (2 + s) * kCols, dv + st * kStageDesc + ((kk * 32 * kD) >> 4),
+                     dp + s * ((kBN * 128) >> 4) + ((kk * 32 * 128) >> 4), id_o, (j > 1 || kk > 0) ? 1u : 0u);
+        umma_commit(&sm.v_empty[st]);
+      };
+      auto wait = [&](uint64_t* bar, int phase) {
+        const bool ok = mbar_wait(bar, phase & 1, &sm.abort);
+        if (ok) tc_fence_after_sync();
+        return ok;
+      };
+      bool ok = wait(&sm.q_full, 0);
+      for (int j = 0; j < 2 && j < nt && ok; ++j) {
+        ok = wait(&sm.k_full[j], 0);
+        if (ok) issue_s(j);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        ok = wait(&sm.p_full[j & 1], j >> 1) && wait(&sm.v_clean[j % kStages], j / kStages);
+        if (!ok) break;
+        issue_o(j);
+        if (j + 2 < nt) {
+          ok = wait(&sm.k_full[(j + 2) % kStages], (j + 2) / kStages);
+          if (ok) issue_s(j + 2);
+        }
+      }
+      if (ok) {
+        umma_commit(&sm.o_full);
+      } else {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 74);
+        sm.abort = 1;
+      }
+      // all tensor-core work of this CTA completes before tensor memory is released
+      umma_commit(&sm.drain);
+      mbar_wait(&sm.drain, 0, nullptr);
+    }
+    __syncwarp();
+  } else if (warp >= kScreenWarp) {
+    // ---------------- NaN codes of V (thread = key; the swizzle moves no byte out of its row) ----------------
+    const int key = tid - kScreenWarp * 32;
+    bool ok = true;
+    for (int j = 0; j < nt; ++j) {
+      const int st = j % kStages;
+      ok = warp_wait(&sm.v_full[st], (j / kStages) & 1, &sm.abort);
+      if (!ok) break;
+      const uint32_t row = smem_u32(sm.v[st]) + key * kD;
+      uint32_t hit = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint4 c = lds128(row + ((i ^ (key & 7)) << 4));
+        hit |= ((c.x & 0x7f7f7f7fu) + 0x01010101u) | ((c.y & 0x7f7f7f7fu) + 0x01010101u) |
+               ((c.z & 0x7f7f7f7fu) + 0x01010101u) | ((c.w & 0x7f7f7f7fu) + 0x01010101u);
+      }
+      const bool bad = (hit & 0x80808080u) != 0;
+      const uint32_t nans = __ballot_sync(0xffffffffu, bad);
+      if (bad) {
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) sts128(row + 16 * i, 0, 0, 0, 0);
+      }
+      if (lane == 0) reinterpret_cast<uint32_t*>(&sm.nan_keys[st])[key >> 5] = nans;
+      fence_proxy_async_smem();
+      mbar_arrive(&sm.v_clean[st]);
+    }
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 72);
+      sm.abort = 1;
+    }
+  } else {
+    // ---------------- softmax (thread = key of a KV tile) ----------------
+    const int stream = warp >> 2, key = tid & (kBN - 1), w4 = warp & 3;
+    const size_t masked0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds;   // masked-input rows of this KV head
+    // the exponent bytes of the thread's first two tiles are on their way while Q is made ready
+    const uint8_t* kx = p.k_exp + mem0 + static_cast<size_t>(j0) * kBN + key;
+    const uint8_t* vx = p.v_exp + mem0 + static_cast<size_t>(j0) * kBN + key;
+    const int left = p.Lk - j0 * kBN - key;   // the thread's key of tile j is in the memory if j * kBN < left
+    uint32_t xk[2], xv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = (stream + 2 * i) * kBN;
+      const bool in = stream + 2 * i < nt && at < left;
+      xk[i] = in ? __ldg(kx + at) : 127u;
+      xv[i] = in ? __ldg(vx + at) : 127u;
+    }
+    // parts of Q, a warp a row: lane's columns 4 lane .. 4 lane + 3
+    for (int n = warp; n < kN; n += 8) {
+      uint2 a = make_uint2(0, 0);
+      if (n < n_rows) a = __ldg(reinterpret_cast<const uint2*>(p.q + (rowbase + p0 + n) * kD) + lane);
+      const float f[4] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xffff0000u), __uint_as_float(a.y << 16),
+                          __uint_as_float(a.y & 0xffff0000u)};
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+      top = __reduce_max_sync(0xffffffffu, top);
+      // a maximum of 2^e .. 2^(e + 1) goes to 2^14 .. 2^15; e held to -112 .. 127 (subnormal rows lose their last bits)
+      const int e = min(max(static_cast<int>(top >> 23) - 127, -112), 127);
+      const float up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23);
+      const bool bad = (top >> 23) == 255;   // a row with an element that is not finite has NaN scores
+      uint32_t part0[3], part1[3];
+      const __half2 h0 = __floats2half2_rn(bad ? 0.0f : f[0] * up, bad ? 0.0f : f[1] * up);
+      const __half2 h1 = __floats2half2_rn(bad ? 0.0f : f[2] * up, bad ? 0.0f : f[3] * up);
+      split3(*reinterpret_cast<const uint32_t*>(&h0), part0);
+      split3(*reinterpret_cast<const uint32_t*>(&h1), part1);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int row = i * kN + n;
+        const uint32_t four = __byte_perm(part0[i], part1[i], 0x7531);   // the upper bytes of four halves
+        *reinterpret_cast<uint32_t*>(sm.q + row * kD + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4) = four;
+      }
+      if (lane == 0)
+        sm.q_scale[n] = bad ? __uint_as_float(0x7fc00000u)
+                            : __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23) * (kCap ? p.cap_in : p.scale_log2);
+    }
+    fence_proxy_async_smem();
+    mbar_arrive(&sm.q_full);
+    // the seed rows' own scores (log2 units), in the first part alone: a warp a row, four columns a lane
+    if (p.n_seeds > 0 && ks == 0) {
+      for (int n = warp; n < n_rows; n += 8) {
+        const int4 info = sm.row[n];
+        if (info.z < 0 || info.z < info.x || info.z >= info.y) continue;
+        const uint2 a = __ldg(reinterpret_cast<const uint2*>(p.q + (rowbase + p0 + n) * kD) + lane);
+        const uint2 c = __ldg(reinterpret_cast<const uint2*>(p.k_seedmask + (masked0 + sm.slot[n]) * kD) + lane);
+        float dot = __uint_as_float(a.x << 16) * __uint_as_float(c.x << 16);
+        dot = fmaf(__uint_as_float(a.x & 0xffff0000u), __uint_as_float(c.x & 0xffff0000u), dot);
+        dot = fmaf(__uint_as_float(a.y << 16), __uint_as_float(c.y << 16), dot);
+        dot = fmaf(__uint_as_float(a.y & 0xffff0000u), __uint_as_float(c.y & 0xffff0000u), dot);
+        for (int d = 16; d >= 1; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        if (lane == 0) sm.s_self[n] = kCap ? capped(dot, p.cap_in, p.cap_log2) : dot * p.scale_log2;
+      }
+    }
+    softmax_sync();   // q_scale and row are written
+    const uint32_t quad = tbase + (static_cast<uint32_t>(w4 * 32) << 16);
+    const uint32_t s_addr = quad + stream * kCols, o_addr = quad + (2 + stream) * kCols;
+    const float* m = sm.m[stream];
+    const uint32_t pt = smem_u32(sm.pt[stream]) + key * 128;
+    const uint32_t sw = static_cast<uint32_t>(key & 7) << 4;
+    const int all_lo = sm.all_lo, all_hi = sm.all_hi;
+    float l[kN];
+#pragma unroll
+    for (int n = 0; n < kN; ++n) l[n] = 0.0f;
+    bool ok = true;
+    int i = 0;
+    for (int j = stream; j < nt; j += 2, ++i) {
+      // (the asm keeps the bytes' loads from being waited for before this tile)
+      asm volatile("" : "+r"(xk[0]), "+r"(xv[0]));
+      const int k_byte = static_cast<int>(xk[0]), v_byte = static_cast<int>(xv[0]);
+      xk[0] = xk[1], xv[0] = xv[1];
+      if (j + 4 < nt && (j + 4) * kBN < left) {
+        xk[1] = __ldg(kx + (j + 4) * kBN);
+        xv[1] = __ldg(vx + (j + 4) * kBN);
+      }
+      const int st = j % kStages;
+      ok = warp_wait(&sm.s_full[stream], i & 1, &sm.abort) && warp_wait(&sm.v_clean[st], (j / kStages) & 1, &sm.abort);
+      float t[kN];        // s_j + e_j - m + 12, in log2 units
+      bool over = !ok;    // a warp whose wait gave up votes all the same: the stream's barriers take 128 threads
+      // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
+      const float e_v = static_cast<float>(v_byte - 127);
+      const float lift = fmaxf(e_v, static_cast<float>(kEvFloor)) - e_v;
+      if (ok) {
+        tc_fence_after_sync();
+        const bool nan_key = v_byte > kExpMax || k_byte > kExpMax ||
+                             ((reinterpret_cast<const uint32_t*>(&sm.nan_keys[st])[key >> 5] >> (key & 31)) & 1u);
+        const float k_scale = nan_key ? __uint_as_float(0x7fc00000u) : e4m3_scale(k_byte);
+#pragma unroll
+        for (int c = 0; c < kN; c += 16) {
+          uint32_t x[3][16];
+#pragma unroll
+          for (int h = 0; h < 3; ++h) tmem_ld16(s_addr + h * kN + c, x[h]);
+#pragma unroll
+          for (int h = 0; h < 3; ++h) tmem_ld_wait16(x[h]);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float sum = (__uint_as_float(x[2][e]) + __uint_as_float(x[1][e])) + __uint_as_float(x[0][e]);
+            const float f = k_scale * sm.q_scale[c + e];
+            t[c + e] = (kCap ? capped(sum, f, p.cap_log2) + e_v : fmaf(sum, f, e_v)) - m[c + e];
+          }
+        }
+        // keys that some row does not see, among them a seed row's own cached column
+        const int key0 = (j0 + j) * kBN, at = key0 + key;
+        if (key0 < all_lo || key0 + kBN > all_hi ||
+            (p.n_seeds > 0 && key0 < p.q0 + p.Lq && key0 + kBN > p.q0)) {
+#pragma unroll
+          for (int n = 0; n < kN; ++n) {
+            const int4 info = sm.row[n];
+            if (at < info.x || at >= info.y || at == info.z) t[n] = -INFINITY;
+          }
+        }
+        const float margin = kRowsThreshold + kPBits - lift;
+#pragma unroll
+        for (int n = 0; n < kN; ++n) over |= t[n] > margin;
+        over |= sm.any_unseen[stream] != 0;
+        __syncwarp();
+      }
+      if (stream_any(stream, over)) {
+        if (stream_any(stream, !ok)) {
+          ok = false;
+          break;
+        }
+        // new references: the rows' maxima where they are above the old ones by more than the threshold
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          const int top = __reduce_max_sync(0xffffffffu, ordered(t[n] == t[n] ? t[n] + lift : -INFINITY));
+          if (lane == (n & 31)) sm.red[stream][w4][n] = from_ordered(top);
+        }
+        stream_sync(stream);
+        if (key < kN) {
+          const float up = fmaxf(fmaxf(sm.red[stream][0][key], sm.red[stream][1][key]),
+                                 fmaxf(sm.red[stream][2][key], sm.red[stream][3][key])) - kPBits;
+          // a row's first keys set its reference, wherever they lie
+          const bool first = sm.unseen[stream][key] != 0 && up > -INFINITY;
+          const float step = first || up > kRowsThreshold ? up : 0.0f;
+          sm.step[stream][key] = step;
+          sm.alpha[stream][key] = first ? 0.0f : ex2_approx(-step);
+          sm.m[stream][key] = m[key] + step;
+          if (first) sm.unseen[stream][key] = 0;
+          const uint32_t mask = kN == 32 ? 0xffffffffu : 0xffffu;
+          const uint32_t still = __ballot_sync(mask, sm.unseen[stream][key] != 0);
+          if (key == 0) sm.any_unseen[stream] = still != 0 ? 1 : 0;
+        }
+        stream_sync(stream);
+#pragma unroll
+        for (int n = 0; n < kN; ++n) {
+          t[n] -= sm.step[stream][n];
+          l[n] *= sm.alpha[stream][n];
+        }
+        if (i > 0) {
+          // O holds the stream's earlier products (complete: the commit of this S came after them)
+#pragma unroll
+          for (int c = 0; c < kCols; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_addr + c, o);
+            tmem_ld_wait16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sm.alpha[stream][c % kN + e]);
+            tmem_st16(o_addr + c, o);
+          }
+          tmem_st_wait();
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < kN; c += 16) {
+        uint32_t out[3][4];   // parts of 16 rows
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          uint32_t parts[2][3];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int n = c + 4 * q4 + 2 * h;
+            const float e0 = ex2_approx(t[n]), e1 = ex2_approx(t[n + 1]);
+            l[n] += ex2_approx(t[n] - e_v);
+            l[n + 1] += ex2_approx(t[n + 1] - e_v);
+            // to 9 significant bits, half up: P' is at most 2^14, so that no carry leaves a half
+            const __half2 x = __floats2half2_rn(e0, e1);
+            split3((*reinterpret_cast<const uint32_t*>(&x) + 0x00020002u) & 0xfffcfffcu, parts[h]);
+          }
+#pragma unroll
+          for (int i3 = 0; i3 < 3; ++i3) out[i3][q4] = __byte_perm(parts[0][i3], parts[1][i3], 0x7531);
+        }
+#pragma unroll
+        for (int i3 = 0; i3 < 3; ++i3)
+          sts128(pt + ((static_cast<uint32_t>(i3 * kN + c)) ^ sw), out[i3][0], out[i3][1], out[i3][2], out[i3][3]);
+      }
+      fence_proxy_async_smem();
+      tc_fence_before_sync();
+      mbar_arrive(&sm.p_full[stream]);
+    }
+    if (ok && nt > 0) ok = warp_wait(&sm.o_full, 0, &sm.abort);
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 75);
+      sm.abort = 1;
+    }
+
+    // ---------------- the rows' results ----------------
+    tc_fence_after_sync();
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      float x = l[n];
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      if (lane == (n & 31)) sm.red[stream][w4][n] = x;
+    }
+    softmax_sync();
+    const bool split = p.nsplit > 1;
+    if (ok && tid < n_rows) {
+      const int n = tid;
+      const long long orow = rowbase + p0 + n;
+      const float s_self = sm.s_self[n];
+      float l2[2];
+      for (int s = 0; s < 2; ++s) l2[s] = (sm.red[s][0][n] + sm.red[s][1][n]) + (sm.red[s][2][n] + sm.red[s][3][n]);
+      const float m0 = sm.unseen[0][n] ? -INFINITY : sm.m[0][n], m1 = sm.unseen[1][n] ? -INFINITY : sm.m[1][n];
+      const float top = fmaxf(fmaxf(m0, m1), s_self);
+      const float w0 = m0 == -INFINITY ? 0.0f : ex2_approx(m0 - top), w1 = m1 == -INFINITY ? 0.0f : ex2_approx(m1 - top);
+      const float p_self = s_self == -INFINITY ? 0.0f : ex2_approx(s_self - top);
+      // (NaN scores leave the references alone: they are in the sums)
+      float sum = fmaf(w0, l2[0], fmaf(w1, l2[1], p_self));
+      if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
+      if (s_self != s_self) sum = s_self;
+      sm.fin[n] = make_float4(w0, w1, p_self, split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+      if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(top, sum);
+      else if (p.lse != nullptr) p.lse[orow] = (top + lg2_approx(sum)) * 0.6931471805599453f;
+    }
+    softmax_sync();
+    // thread = output column; the streams' warps take 16 rows in turn
+    const int col = key;
+    for (int c = 16 * stream; c < n_rows; c += 32) {
+      if (!ok) break;
+      float o0[16] = {}, o1[16] = {};
+      if (nt > 0) {
+#pragma unroll
+        for (int h = 2; h >= 0; --h) {
+          uint32_t x[16];
+          tmem_ld16(quad + 2 * kCols + h * kN + c, x);
+          tmem_ld_wait16(x);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o0[e] += __uint_as_float(x[e]);
+          if (nt > 1) {
+            tmem_ld16(quad + 3 * kCols + h * kN + c, x);
+            tmem_ld_wait16(x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o1[e] += __uint_as_float(x[e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int n = c + e;
+        if (n < n_rows) {
+          const float4 f = sm.fin[n];
+          float o = f.x == 0.0f ? 0.0f : o0[e] * f.x;
+          if (f.y != 0.0f) o = fmaf(o1[e], f.y, o);
+          if (f.z != 0.0f) o = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.slot[n]) * kD + col]), o);
+          const long long orow = rowbase + p0 + n;
+          if (split) p.part_o[(static_cast<size_t>(ks) * p.rows + orow) * kD + col] = o;
+          else p.out[orow * kD + col] = __float2bfloat16_rn(o * f.w);
+        }
+      }
+      __syncwarp();
+    }
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  if (warp == kRowsMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tbase, kTmem);
+  }
+}
+
 // Combines the parts of every row: one warp a row, four columns a lane.
 constexpr int kCombineWarps = 4;
 __global__ void __launch_bounds__(kCombineWarps * 32)
@@ -771,28 +1439,32 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
   if (lane == 0 && lse != nullptr) lse[row] = (m + lg2_approx(l)) * 0.6931471805599453f;
 }
 
+enum Mode { kRows16, kRows32, kShared, kPairs };
+constexpr int kModeRows[] = {16, 32, kBM, 2 * kBM};   // packed rows of a CTA
+
 struct Plan {
-  bool pair;
+  Mode mode;
   int n_groups, nsplit;
 };
 
-// One Q tile or two of a KV head a CTA, and the parts of the keys.
+// The kernel and the parts of the keys.
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int L) {
   Plan best{};
   double best_us = 0.0;
-  const int G = Hq / Hkv;
-  const long long n_qt = (static_cast<long long>(G) * Lq + kBM - 1) / kBM;
+  const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
+  const long long rows = static_cast<long long>(B) * Hq * Lq;
   const int nkv = (L + kBN - 1) / kBN;
-  for (int pair = 0; pair < 2; ++pair) {
-    if (pair && n_qt < 2) continue;
-    const long long groups = pair ? (n_qt + 1) / 2 : n_qt;
+  constexpr double kTileUs[] = {0.75, 0.75, 1.1, 1.8};
+  for (int mode = 0; mode < 4; ++mode) {
+    if (mode > 0 && kModeRows[mode - 1] >= packed) continue;   // a smaller one holds all rows
+    const long long groups = (packed + kModeRows[mode] - 1) / kModeRows[mode];
     const long long units = groups * Hkv * B;
     for (int ns = 1; ns <= nkv && ns <= 64; ++ns) {
       const long long waves = (units * ns + kSms - 1) / kSms;
       const int tiles = (nkv + ns - 1) / ns;
-      const double us = waves * (3.0 + (pair ? 1.3 : 0.75) * tiles) + (ns > 1 ? 1.5 + 0.0000003 * ns * units * (pair ? 256 : 128) * 528 / 4 : 0.0);
+      const double us = waves * (3.0 + kTileUs[mode] * tiles) + (ns > 1 ? 1.5 + 2.0e-7 * rows * ns * 520 : 0.0);
       if (best.nsplit == 0 || us < best_us) {
-        best = Plan{pair != 0, static_cast<int>(groups), ns};
+        best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns};
         best_us = us;
       }
       if (units * ns > 8 * kSms) break;
@@ -800,6 +1472,15 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L) {
   }
   return best;
 }
+
+using TileKernel = void (*)(const CUtensorMap, const Params);
+using RowsKernel = void (*)(const CUtensorMap, const CUtensorMap, const Params);
+constexpr TileKernel kTileKernels[2][2] = {{attn_prefix8_kernel<false, false>, attn_prefix8_kernel<false, true>},
+                                           {attn_prefix8_kernel<true, false>, attn_prefix8_kernel<true, true>}};
+constexpr RowsKernel kRowsKernels[2][2] = {{attn_prefix8_rows_kernel<16, false>, attn_prefix8_rows_kernel<16, true>},
+                                           {attn_prefix8_rows_kernel<32, false>, attn_prefix8_rows_kernel<32, true>}};
+constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSmem<32>) + 1024};
+static_assert(kRowsSmemBytes[0] <= 227 * 1024 && kRowsSmemBytes[1] <= 227 * 1024, "shared memory of a CTA");
 
 size_t part_bytes(long long rows, int nsplit) {
   return nsplit <= 1 ? 0 : static_cast<size_t>(rows) * nsplit * (kD * sizeof(float) + sizeof(float2));
@@ -820,20 +1501,26 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   static ContextCache<int> setup;
   int unused = 0;
   const int rc = setup.get(&unused, [&](int&) {
-    for (auto fn : {attn_prefix8_kernel<false, false>, attn_prefix8_kernel<false, true>, attn_prefix8_kernel<true, false>,
-                    attn_prefix8_kernel<true, true>}) {
-      if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes)) != cudaSuccess)
-        return -3;
-      // the register split inside the kernel assumes exactly kLaunchRegs per thread at launch; any
-      // other count could leave setmaxnreg.inc waiting, so refuse to launch
-      cudaFuncAttributes fa;
-      if (cudaFuncGetAttributes(&fa, fn) != cudaSuccess || fa.numRegs != kLaunchRegs) return -2;
-    }
+    for (int m = 0; m < 2; ++m)
+      for (int c = 0; c < 2; ++c) {
+        if (cudaFuncSetAttribute(kTileKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(kSmemBytes)) != cudaSuccess ||
+            cudaFuncSetAttribute(kRowsKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(kRowsSmemBytes[m])) != cudaSuccess)
+          return -3;
+        // the register split inside the kernel assumes exactly kLaunchRegs per thread at launch; any
+        // other count could leave setmaxnreg.inc waiting, so refuse to launch
+        cudaFuncAttributes fa;
+        if (cudaFuncGetAttributes(&fa, kTileKernels[m][c]) != cudaSuccess || fa.numRegs != kLaunchRegs) return -2;
+      }
     return 0;
   });
   if (rc != 0) return rc;
-  CUtensorMap tq;
-  if (!make_bf16_map_4d(&tq, a.q, kD, static_cast<uint64_t>(rows), 1, 1, kBM)) return -3;
+  const bool few = plan.mode == kRows16 || plan.mode == kRows32;
+  CUtensorMap t0, t1;
+  if (few ? !make_u8_map_4d(&t0, a.k8, kD, a.L, a.Hkv, a.B, kBN) || !make_u8_map_4d(&t1, a.v8, kD, a.L, a.Hkv, a.B, kBN)
+          : !make_bf16_map_4d(&t0, a.q, kD, static_cast<uint64_t>(rows), 1, 1, kBM))
+    return -3;
   const float log2e = 1.4426950408889634f, root = sqrtf(static_cast<float>(kD));
   Params p{};
   p.q = static_cast<const __nv_bfloat16*>(a.q);
@@ -866,10 +1553,17 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.cap_log2 = a.softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (a.softcap * root) : 0.0f;
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), kSmemBytes, stream, attr);
-  auto kernel = plan.pair ? (cap ? attn_prefix8_kernel<true, true> : attn_prefix8_kernel<true, false>)
-                          : (cap ? attn_prefix8_kernel<false, true> : attn_prefix8_kernel<false, false>);
-  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tq, p);
+  const dim3 ctas(static_cast<unsigned>(grid));
+  cudaLaunchConfig_t cfg;
+  cudaError_t e;
+  if (few) {
+    const int m = plan.mode == kRows16 ? 0 : 1;
+    cfg = pdl_config(ctas, dim3(kRowsThreads), kRowsSmemBytes[m], stream, attr);
+    e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], t0, t1, p);
+  } else {
+    cfg = pdl_config(ctas, dim3(kThreads), kSmemBytes, stream, attr);
+    e = cudaLaunchKernelEx(&cfg, kTileKernels[plan.mode == kPairs ? 1 : 0][cap ? 1 : 0], t0, p);
+  }
   if (e == cudaSuccess && plan.nsplit > 1) {
     cfg = pdl_config(dim3(static_cast<unsigned>((rows + kCombineWarps - 1) / kCombineWarps)), dim3(kCombineWarps * 32), 0,
                      stream, attr);

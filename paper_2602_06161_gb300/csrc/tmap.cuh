@@ -20,4 +20,7 @@ EncodeTiledFn encode_tiled_fn();
 bool make_bf16_map_4d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t d3,
                       uint32_t box1);
 
+// The same for bytes: a 4-D tensor [d3][d2][d1][d0] of uint8, a box of box1 rows of 128 columns, 128-byte swizzle.
+bool make_u8_map_4d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t d3, uint32_t box1);
+
 }  // namespace cover
