@@ -105,6 +105,30 @@ int cover_debug_window_model(int B, int Hq, int Hkv, int Lq, int Lk, int q0, int
                              const int32_t* max_clusters, int32_t* choice, double* times);
 
 /*
+ * cover_attn_fwd_prefix8 on a kernel of the caller's choice and with the keys in nsplit parts (1 .. 64), whatever the call
+ * itself would take. mode: 0, 1 rows of a KV head in groups of 16 or 32, codes as matrix operands; 2 in Q tiles
+ * of 128, codes decoded by the kernel; 3 in pairs of Q tiles over a memory decoded by a pass of its own; 4 the kernels of
+ * cover_attn_fwd_prefix over such a memory (nsplit 1, no key ranges, no cap; else COVER_ERR_UNSUPPORTED).
+ * workspace_bytes: of the workspace; what is needed: modes 3, 4 4 B Hkv Lk 128 bytes, and nsplit > 1 another
+ * B Hq Lq nsplit 520 (rounded up to 16); COVER_ERR_INVALID_ARG if there is less. Otherwise as cover_attn_fwd_prefix8.
+ */
+int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8,
+                             const uint8_t* k_exp, const uint8_t* v_exp,
+                             const void* k_seedmask, const void* v_seedmask,
+                             const int32_t* seed_idx, int n_seeds,
+                             int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D,
+                             const int32_t* key_lo, const int32_t* key_hi, float softcap,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes,
+                             int mode, int nsplit, void* stream);
+
+/*
+ * What cover_attn_fwd_prefix8 takes for these sizes (plain: without key ranges and cap): choice[3] = {mode, groups of rows
+ * a KV head, parts of the keys}, us[0] = the predicted time. Host arithmetic only. COVER_ERR_INVALID_ARG for
+ * invalid sizes or a null pointer.
+ */
+int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int32_t* choice, double* us);
+
+/*
  * Like cover_device_status, and also returns where the failure came from:
  * synchronises `stream`, copies the current device's status block to the
  * host array detail[3] = {status code, site id, linear block id} (all 0 when
@@ -112,7 +136,8 @@ int cover_debug_window_model(int B, int Hq, int Hkv, int Lq, int Lk, int q0, int
  * call fails). Site ids of the bf16 attention kernel: 10 TMA thread, 20 MMA
  * thread, 30 / 31 softmax warpgroup of Q tile 0 / 1, 40 routing warp,
  * 50 / 51 seed-score warp; of the packed window kernel: 60 TMA / MMA thread,
- * 61 softmax warps, 62 combine (receive barrier), 63 copy issue.
+ * 61 softmax warps, 62 combine (receive barrier), 63 copy issue; of the 8-bit memory's kernels: 70, 76 copies,
+ * 71, 74 MMA thread, 72 decoding or screening warps, 73, 75 softmax warps.
  */
 int cover_debug_status_detail(int32_t* detail, void* stream);
 

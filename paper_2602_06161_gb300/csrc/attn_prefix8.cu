@@ -45,15 +45,21 @@ constexpr int kBM = 128;                   // rows per Q tile
 constexpr int kBN = 128;                   // keys per KV tile
 constexpr int kTileBytes = kBM * kD * 2;   // 32 KB
 constexpr int kBoxBytes = kTileBytes / 2;  // one 64-column, 128-byte-swizzled box
+constexpr int kCodeBytes = kBN * kD;       // 16 KB of codes
 constexpr int kThreads = 640;
-constexpr int kDecodeWarp = 8, kMmaWarp = 16, kLoadWarp = 17;
+constexpr int kDecodeWarp = 8;
 constexpr int kLaunchRegs = 96;            // registers per thread at launch (65536 / 640, rounded down to 8)
 // registers of the softmax, decode and issuing threads: a Q tile's softmax threads hold 128 scores each
 constexpr int kSoftmaxRegs = 160, kDecodeRegs = 56, kIssueRegs = 40;
 static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "register split");
 // setmaxnreg.inc takes no count below the thread's own, .dec none above it
 static_assert(kSoftmaxRegs >= kLaunchRegs && kDecodeRegs <= kLaunchRegs && kIssueRegs <= kLaunchRegs, "register split");
+// of the kernel that reads decoded tiles: no decode threads
+constexpr int kReadThreads = 384, kReadLaunchRegs = 168, kReadSoftmaxRegs = 208, kReadIssueRegs = 88;
+static_assert(2 * 128 * kReadSoftmaxRegs + 128 * kReadIssueRegs <= kReadThreads * kReadLaunchRegs, "register split");
+static_assert(kReadSoftmaxRegs >= kReadLaunchRegs && kReadIssueRegs <= kReadLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr int kMaxParts = 64;              // of the keys
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
 
 // Barriers and tables of a CTA.
@@ -100,6 +106,8 @@ struct Params {
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
+  float cap_x;       // 1 / (cap sqrt(d))
+  float cap_ref;     // reference of all rows under a small cap, or -inf (see fixed_reference)
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -132,6 +140,12 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
+// tanh(x) / x = T0 + T1 z + T2 z^2 + T3 z^3 with z = x^2 for |x| <= 0.4: the polynomial through the function at 2000
+// Chebyshev nodes of z in [0, 0.16] by least squares, off by at most 1e-7 of it (2e-7 in fp32). Scores are seldom above
+// 0.4 of their cap, and then two special-function operations an element are saved.
+constexpr float kTanhRange = 0.4f;
+constexpr float kTanh0 = 0.999999903f, kTanh1 = -0.333313733f, kTanh2 = 0.132711566f, kTanh3 = -0.0475610772f;
+
 // Shared memory by its 32-bit address.
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
@@ -157,21 +171,19 @@ __device__ __forceinline__ float capped(float s, float cap_in, float cap_log2) {
   return fmaf(-2.0f * cap_log2, rcp_approx(1.0f + t), cap_log2);
 }
 
-// Decodes a row of codes, or every other one of its eight 16-byte pieces (kPieces = 4), into its row of a bf16 tile (two
-// 64-column boxes, 16-byte chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are
+// Decodes a row of codes, eight 16-byte pieces, into its row of a bf16 tile (two 64-column boxes, 16-byte chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are
 // the bf16 number code * 2^-120 (subnormal codes included), and one multiplication by m1 = 2^(120 + x - 127) gives the
 // value; where that is above bf16's range, m1 = 2^120 and kTwo says to multiply by m2 = 2^(x - 127) too. Both are
-// exact. A row's pieces are taken in the order u0 ^ 0, 1, ... (u0 ^ 0, 2, ... of the half) with u0 the row's low bits, so
-// that the reads and writes of eight lanes meet every bank. src: address of piece u0; d0, d1: of its first chunk, in
+// exact. A row's pieces are taken in the order u0 ^ 0, u0 ^ 1, ... with u0 the row's low bits, so that the reads and writes
+// of eight lanes meet every bank. src: address of piece u0; d0, d1: of its first chunk, in
 // its box and in the other one.
-template <int kPieces, bool kTwo>
+template <bool kTwo>
 __device__ __forceinline__ void decode_row(uint32_t src, uint32_t d0, uint32_t d1, uint32_t m1, uint32_t m2) {
-  constexpr int kStep = 8 / kPieces;
 #pragma unroll
-  for (int i0 = 0; i0 < kPieces; i0 += 4) {
+  for (int i0 = 0; i0 < 8; i0 += 4) {
     uint4 c[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = lds128(src ^ (16u * kStep * (i0 + i)));
+    for (int i = 0; i < 4; ++i) c[i] = lds128(src ^ (16u * (i0 + i)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
@@ -188,7 +200,7 @@ __device__ __forceinline__ void decode_row(uint32_t src, uint32_t d0, uint32_t d
           o[2 * e + 1] = mul_bf16x2(o[2 * e + 1], m2);
         }
       }
-      const uint32_t x = kStep * (i0 + i);   // piece u0 ^ x
+      const uint32_t x = i0 + i;   // piece u0 ^ x
       const uint32_t d = (x & 4 ? d1 : d0) ^ ((x & 3) << 5);
       sts128(d, o[0], o[1], o[2], o[3]);
       sts128(d ^ 16u, o[4], o[5], o[6], o[7]);
@@ -196,7 +208,6 @@ __device__ __forceinline__ void decode_row(uint32_t src, uint32_t d0, uint32_t d
   }
 }
 
-template <int kPieces>
 __device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, int x, bool zero) {
   // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
   const bool two = x > 134 && x <= kExpMax;
@@ -206,19 +217,18 @@ __device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, i
   if (zero) m1 = 0;
   m1 |= m1 << 16;
   m2 |= m2 << 16;
-  if (__any_sync(0xffffffffu, two)) decode_row<kPieces, true>(src, d0, d1, m1, m2);
-  else decode_row<kPieces, false>(src, d0, d1, m1, m2);
+  if (__any_sync(0xffffffffu, two)) decode_row<true>(src, d0, d1, m1, m2);
+  else decode_row<false>(src, d0, d1, m1, m2);
 }
 
-// The exponent bytes of row lrow of four ring entries of kRows rows from entry e on (zero from row `left` on).
-template <int kRows>
+// The exponent bytes of row `row` of four KV tiles from tile j on (zero from row `left` of the part on).
 struct FourBytes {
   uint32_t v[4];
-  __device__ __forceinline__ void load(const uint8_t* exps, int e, int lrow, int left) {
+  __device__ __forceinline__ void load(const uint8_t* exps, int j, int row, int left) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = (e + i) * kRows + lrow;
-      v[i] = row < left ? __ldg(exps + row) : 0u;
+      const int at = (j + i) * kBN + row;
+      v[i] = at < left ? __ldg(exps + at) : 0u;
     }
   }
   // (the asm keeps the compiler from packing them, and so waiting for the loads, where they are issued)
@@ -229,7 +239,8 @@ struct FourBytes {
 };
 
 // Barriers and tensor memory, by one warp.
-__device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32_t tmem_columns) {
+// fills: arrivals that fill a K or V tile (128 decoding threads, or the thread that issues its copies).
+__device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32_t tmem_columns, uint32_t fills) {
   if ((threadIdx.x & 31) == 0) {
     mbar_init(&ctl.q_full, 1);
     for (int i = 0; i < 2; ++i) {
@@ -237,9 +248,9 @@ __device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32
         mbar_init(&ctl.c_full[w][i], 1);
         mbar_init(&ctl.c_empty[w][i], 128);
       }
-      mbar_init(&ctl.k_full[i], 128);
+      mbar_init(&ctl.k_full[i], fills);
       mbar_init(&ctl.k_empty[i], 1);
-      mbar_init(&ctl.v_full[i], 128);
+      mbar_init(&ctl.v_full[i], fills);
       mbar_init(&ctl.v_empty[i], 1);
       mbar_init(&ctl.s_full[i], 1);
       mbar_init(&ctl.p_full[i], 128);
@@ -257,24 +268,20 @@ __device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32
   tmem_relinquish();
 }
 
-// Copies the codes of K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 through their ring of kRing entries of kRows
-// rows; one thread. With which = 0 its Q tiles are on their way to ctl.q_full already.
-template <int kRing, int kRows>
+// Copies the codes of K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 through their ring of two tiles; one thread. With
+// which = 0 its Q tiles are on their way to ctl.q_full already.
 __device__ __forceinline__ void copy_codes(Ctl& ctl, const Params& p, int which, uint8_t* ring, size_t mem0, int j0, int nt) {
-  const uint8_t* src = (which ? p.v8 : p.k8) + mem0 * kD;
-  const uint32_t dst = smem_u32(ring) + which * kRing * kRows * kD;
-  const int left = min(p.Lk - j0 * kBN, nt * kBN);   // keys of this part
-  const int entries = (left + kRows - 1) / kRows;
-  int e = 0;
+  const uint8_t* src = (which ? p.v8 : p.k8) + (mem0 + static_cast<size_t>(j0) * kBN) * kD;
+  const uint32_t dst = smem_u32(ring) + which * 2 * kCodeBytes;
+  int j = 0;
   bool ok = true;
-  for (; e < entries; ++e) {
-    const int st = e % kRing;
-    if (e >= kRing) ok = mbar_wait(&ctl.c_empty[which][st], (e / kRing - 1) & 1, &ctl.abort);
+  for (; j < nt; ++j) {
+    const int st = j & 1;
+    if (j >= 2) ok = mbar_wait(&ctl.c_empty[which][st], ((j >> 1) - 1) & 1, &ctl.abort);
     if (!ok) break;
-    const uint32_t bytes = static_cast<uint32_t>(min(kRows, left - e * kRows)) * kD;
+    const uint32_t bytes = static_cast<uint32_t>(min(kBN, p.Lk - (j0 + j) * kBN)) * kD;
     mbar_arrive_expect_tx(&ctl.c_full[which][st], bytes);
-    bulk_load(dst + st * kRows * kD, src + (static_cast<size_t>(j0) * kBN + static_cast<size_t>(e) * kRows) * kD, bytes,
-              &ctl.c_full[which][st]);
+    bulk_load(dst + st * kCodeBytes, src + static_cast<size_t>(j) * kCodeBytes, bytes, &ctl.c_full[which][st]);
   }
   if (!ok) {
     if (!ctl.abort) report_status(p.status, kStatusTimeout, 70);
@@ -282,61 +289,53 @@ __device__ __forceinline__ void copy_codes(Ctl& ctl, const Params& p, int which,
   }
   // every copy lands before the CTA's shared memory is released, whatever the other roles did
   if (which == 0) mbar_wait(&ctl.q_full, 0, nullptr);
-  for (int f = max(0, e - kRing); f < e; ++f) mbar_wait(&ctl.c_full[which][f % kRing], (f / kRing) & 1, nullptr);
+  for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&ctl.c_full[which][f & 1], (f >> 1) & 1, nullptr);
 }
 
-// Decodes K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 into two bf16 tiles in turn; 128 threads, one or two a
-// row of a ring entry.
-template <int kRing, int kRows>
+// Decodes K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1 into two bf16 tiles in turn; 128 threads, one a key.
 __device__ __forceinline__ void decode_tiles(Ctl& ctl, const Params& p, int which, uint8_t* ring, uint8_t* k_tiles,
                                              uint8_t* v_tiles, size_t mem0, int j0, int nt) {
-  constexpr int kPerTile = kBN / kRows;          // ring entries of a KV tile
-  const int t = threadIdx.x & 127, lane = threadIdx.x & 31;
-  const int lrow = t & (kRows - 1);
-  const uint32_t u0 = static_cast<uint32_t>((lrow ^ (t / kRows)) & 7);
-  const uint32_t codes = smem_u32(ring) + which * kRing * kRows * kD + lrow * kD + u0 * 16;
-  const uint32_t tile = smem_u32(which ? v_tiles : k_tiles) + lrow * 128 + (((u0 & 3) << 5) ^ ((lrow & 7) << 4));
+  const int row = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const uint32_t u0 = static_cast<uint32_t>(row & 7);
+  const uint32_t codes = smem_u32(ring) + which * 2 * kCodeBytes + row * kD + u0 * 16;
+  const uint32_t tile = smem_u32(which ? v_tiles : k_tiles) + row * 128 + (((u0 & 3) << 5) ^ (u0 << 4));
   const uint32_t box = (u0 >> 2) * kBoxBytes;
   const int first = j0 * kBN;                    // this part's first key
   const int left = min(p.Lk - first, nt * kBN);  // keys of this part
-  // exponent bytes are fetched four entries at a time, four to eight ahead of their use
+  // exponent bytes are fetched four tiles at a time, four to eight ahead of their use
   const uint8_t* exps = (which ? p.v_exp : p.k_exp) + mem0 + first;
   const uint8_t* v_exps = p.v_exp + mem0 + first;
-  FourBytes<kRows> x_next, v_next;
-  x_next.load(exps, 0, lrow, left);
-  v_next.load(v_exps, 0, lrow, left);
+  FourBytes x_next, v_next;
+  x_next.load(exps, 0, row, left);
+  v_next.load(v_exps, 0, row, left);
   uint32_t xs = 0, vs = 0;
   bool ok = true;
-  for (int h = 0; h < kPerTile * nt; ++h) {
-    const int j = h / kPerTile, st = j & 1, part = h % kPerTile;
-    if ((h & 3) == 0) {
+  for (int j = 0; j < nt; ++j) {
+    const int st = j & 1;
+    if ((j & 3) == 0) {
       xs = x_next.packed();
-      x_next.load(exps, h + 4, lrow, left);
+      x_next.load(exps, j + 4, row, left);
       if (which == 0) {
         vs = v_next.packed();
-        v_next.load(v_exps, h + 4, lrow, left);
+        v_next.load(v_exps, j + 4, row, left);
       }
     }
-    const bool zero = h * kRows + lrow >= left;
-    const int x = (xs >> (8 * (h & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (h & 3))) & 255);
+    const bool zero = j * kBN + row >= left;
+    const int x = (xs >> (8 * (j & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (j & 3))) & 255);
     const bool v_nan = xv > kExpMax;
     const uint32_t nans = __ballot_sync(0xffffffffu, v_nan);
-    if (part == 0 && j >= 2) ok = warp_wait(which ? &ctl.v_empty[st] : &ctl.k_empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
-    const bool copied = h * kRows < left;        // an entry past the memory is not copied
-    ok = ok && (!copied || warp_wait(&ctl.c_full[which][h % kRing], (h / kRing) & 1, &ctl.abort));
+    if (j >= 2) ok = warp_wait(which ? &ctl.v_empty[st] : &ctl.k_empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
+    ok = ok && warp_wait(&ctl.c_full[which][st], (j >> 1) & 1, &ctl.abort);
     if (!ok) break;
     // tile j - 4 has passed its softmax: S of tile j - 2 came after it
-    if (which == 0 && t < kRows && lane == 0)
-      reinterpret_cast<uint32_t*>(&ctl.nan_keys[j & 3])[kRows / 32 * part + (t >> 5)] = nans;
+    if (which == 0 && lane == 0) reinterpret_cast<uint32_t*>(&ctl.nan_keys[j & 3])[row >> 5] = nans;
     // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the scores of their
     // keys are made NaN instead
-    const uint32_t to = tile + st * kTileBytes + part * kRows * 128;
-    decode<kRows / 16>(codes + (h % kRing) * kRows * kD, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
-    if (copied) mbar_arrive(&ctl.c_empty[which][h % kRing]);
-    if (part == kPerTile - 1) {
-      fence_proxy_async_smem();
-      mbar_arrive(which ? &ctl.v_full[st] : &ctl.k_full[st]);
-    }
+    const uint32_t to = tile + st * kTileBytes;
+    decode(codes + st * kCodeBytes, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
+    mbar_arrive(&ctl.c_empty[which][st]);
+    fence_proxy_async_smem();
+    mbar_arrive(which ? &ctl.v_full[st] : &ctl.k_full[st]);
   }
   if (!ok && lane == 0) {
     if (!ctl.abort) report_status(p.status, kStatusTimeout, 72);
@@ -354,14 +353,42 @@ __device__ __forceinline__ Part part_of(int lo, int hi, int ks, int nsplit) {
   return Part{t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0)};
 }
 
-template <bool kPair, bool kCap>
-__global__ void __launch_bounds__(kThreads, 1)
-    attn_prefix8_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ Params p) {
+// Copies K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1, decoded already, into the two bf16 tiles in turn; one thread.
+__device__ __forceinline__ void copy_tiles(Ctl& ctl, const Params& p, int which, const CUtensorMap* tm, uint8_t* tiles, int hkv,
+                                           int b, int j0, int nt) {
+  uint64_t* const full = which ? ctl.v_full : ctl.k_full;
+  uint64_t* const empty = which ? ctl.v_empty : ctl.k_empty;
+  int j = 0;
+  bool ok = true;
+  for (; j < nt; ++j) {
+    const int st = j & 1;
+    if (j >= 2) ok = mbar_wait(&empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
+    if (!ok) break;
+    mbar_arrive_expect_tx(&full[st], kTileBytes);
+    for (int h = 0; h < 2; ++h)
+      tma_load_4d(tiles + st * kTileBytes + h * kBoxBytes, tm, &full[st], 64 * h, (j0 + j) * kBN, hkv, b);
+  }
+  if (!ok) {
+    if (!ctl.abort) report_status(p.status, kStatusTimeout, 76);
+    ctl.abort = 1;
+  }
+  // every copy lands before the CTA's shared memory is released, whatever the other roles did
+  if (which == 0) mbar_wait(&ctl.q_full, 0, nullptr);
+  for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&full[f & 1], (f >> 1) & 1, nullptr);
+}
+
+// kDecoded: pairs of Q tiles, K and V read from the workspace, where a pass of its own has decoded them (a row whose K or V
+// is NaN has a NaN key and a zero value there).
+template <bool kDecoded, bool kCap>
+__global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
+    attn_prefix8_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
+  constexpr int kMmaWarp = kDecoded ? 8 : 16, kLoadWarp = kMmaWarp + 1;
+  constexpr int kSoftmaxWarps = 8;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Ctl& ctl = sm.ctl;
-  constexpr int kQTiles = kPair ? 2 : 1;
-  constexpr int kRing = 2, kEntry = kPair ? 64 : 128;   // entries of each ring, and their rows
+  constexpr int kQTiles = kDecoded ? 2 : 1;
   uint8_t* const sm_q = sm.q_and_ring;
   uint8_t* const ring = sm.q_and_ring + kQTiles * kTileBytes;
 
@@ -378,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;    // packed row 0 in [B Hq Lq, D]
   const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;                  // the KV head's first memory row
 
-  if (warp == kMmaWarp) set_up(ctl, &tm_q, 512);
+  if (warp == kMmaWarp) set_up(ctl, &tm_q, 512, kDecoded ? 1 : 128);
   if (p.n_seeds > 0 && tid < 2 * kBM) sm.slot[tid] = kNoSlot;
   tc_fence_before_sync();
   __syncthreads();
@@ -391,15 +418,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   // softmax thread: its row, the keys [row_lo, row_hi) that it sees
   const int stream = warp >> 2;                       // of a softmax warp
   const int R = tid & (kBM - 1);
-  const int P = p0 + (kPair ? stream * kBM : 0) + R;
-  const bool valid = warp < kDecodeWarp && P < n_packed;
+  const int P = p0 + (kDecoded ? stream * kBM : 0) + R;
+  const bool valid = warp < kSoftmaxWarps && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
   int row_lo = 0, row_hi = p.Lk;
   if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
   if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
   int lo_key = 0, hi_key = p.Lk;                      // keys that some row sees
   if (p.key_lo != nullptr || p.key_hi != nullptr) {
-    if (warp < kDecodeWarp) {
+    if (warp < kSoftmaxWarps) {
       const bool some = valid && row_lo < row_hi;
       const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff);
       const int hi = __reduce_max_sync(0xffffffffu, some ? row_hi : 0);
@@ -413,10 +440,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   const Part part = part_of(lo_key, hi_key, ks, p.nsplit);
   const int j0 = part.j0, nt = part.nt;
-  const bool two_tiles = kPair && p0 + kBM < n_packed;   // the pair's second Q tile has rows
+  const bool two_tiles = kDecoded && p0 + kBM < n_packed;   // the pair's second Q tile has rows
 
   if (warp >= kMmaWarp) {
-    setmaxnreg_dec<kIssueRegs>();
+    setmaxnreg_dec<kDecoded ? kReadIssueRegs : kIssueRegs>();
     if ((warp == kLoadWarp || warp == kLoadWarp + 1) && lane == 0 && nt > 0) {
       if (warp == kLoadWarp) {
         mbar_arrive_expect_tx(&ctl.q_full, kQTiles * kTileBytes);
@@ -425,7 +452,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &ctl.q_full, 64 * h,
                         static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
       }
-      copy_codes<kRing, kEntry>(ctl, p, warp - kLoadWarp, ring, mem0, j0, nt);
+      if (kDecoded) copy_tiles(ctl, p, warp - kLoadWarp, warp == kLoadWarp ? &tm_k : &tm_v, warp == kLoadWarp ? sm.k[0] : sm.v[0], hkv, b, j0, nt);
+      else copy_codes(ctl, p, warp - kLoadWarp, ring, mem0, j0, nt);
     } else if (warp == kMmaWarp && lane == 0 && nt > 0) {
       // ---------------- products ----------------
       constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
@@ -436,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
       // S[s] = Q . K(stage)^T
       auto issue_s = [&](int s, int st) {
-        uint64_t a = dq + (kPair ? s * kTileDesc : 0), kb = dk + st * kTileDesc;
+        uint64_t a = dq + (kDecoded ? s * kTileDesc : 0), kb = dk + st * kTileDesc;
         asm volatile("" : "+l"(a), "+l"(kb));   // descriptors are added up here, not kept in registers
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
@@ -460,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return ok;
       };
       bool ok = wait(&ctl.q_full, 0);
-      if (kPair) {
+      if (kDecoded) {
         if (ok && (ok = wait(&ctl.k_full[0], 0))) {
           issue_s(0, 0);
           if (two_tiles) issue_s(1, 0);
@@ -519,12 +547,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(&ctl.drain, 0, nullptr);
     }
     __syncwarp();
-  } else if (warp >= kDecodeWarp) {
+  } else if (!kDecoded && warp >= kDecodeWarp) {
     setmaxnreg_dec<kDecodeRegs>();
-    decode_tiles<kRing, kEntry>(ctl, p, (warp - kDecodeWarp) >> 2, ring, sm.k[0], sm.v[0], mem0, j0, nt);
+    decode_tiles(ctl, p, (warp - kDecodeWarp) >> 2, ring, sm.k[0], sm.v[0], mem0, j0, nt);
   } else {
     // ---------------- softmax ----------------
-    setmaxnreg_inc<kSoftmaxRegs>();
+    setmaxnreg_inc<kDecoded ? kReadSoftmaxRegs : kSoftmaxRegs>();
     int slot = kNoSlot;
     if (p.n_seeds > 0) {
       // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
@@ -565,12 +593,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t s_addr = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + stream * kBN;
     const uint32_t o_addr = s_addr + 2 * kBN;
     const float scale = kCap ? 1.0f : p.scale_log2;
-    const int jstep = kPair ? 1 : 2;
-    float m_run = -INFINITY, l_run = 0.0f;
+    const int jstep = kDecoded ? 1 : 2;
+    const bool fixed = kCap && p.cap_ref != -INFINITY;
+    float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
-    const int jend = kPair && stream == 1 && !two_tiles ? 0 : nt;
+    const int jend = kDecoded && stream == 1 && !two_tiles ? 0 : nt;
     int i = 0;   // the stream's step
-    for (int j = kPair ? 0 : stream; j < jend; j += jstep, ++i) {
+    for (int j = kDecoded ? 0 : stream; j < jend; j += jstep, ++i) {
       ok = warp_wait(&ctl.s_full[stream], i & 1, &ctl.abort);
       if (!ok) break;
       tc_fence_after_sync();
@@ -594,66 +623,106 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_ld_wait(raw[c]);
       float* s = reinterpret_cast<float*>(&raw[0][0]);
+      const uint4 nan4 = kDecoded ? make_uint4(0, 0, 0, 0) : ctl.nan_keys[j & 3];
+      const bool nans = (nan4.x | nan4.y | nan4.z | nan4.w) != 0;
+      const bool edge = __any_sync(0xffffffffu, valid && (cl > 0 || ch < kBN));
+      const bool own_column = warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kBN);
+      // capped scores: by the polynomial where the warp's are all small and none is masked, else one by one
+      bool small = false;
       if (kCap) {
+        if (fixed && !(nans || edge || own_column)) {
+          float hi[4] = {};
 #pragma unroll
-        for (int c = 0; c < kBN; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
+          for (int c = 0; c < kBN; c += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) hi[e] = fmax3(hi[e], fabsf(s[c + 2 * e]), fabsf(s[c + 2 * e + 1]));
+          small = __all_sync(0xffffffffu, fmax3(hi[0], hi[1], fmaxf(hi[2], hi[3])) * p.cap_x <= kTanhRange || !valid);
+        }
+        if (!small) {
+#pragma unroll
+          for (int c = 0; c < kBN; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
+        }
       }
-      const uint4 nan4 = ctl.nan_keys[j & 3];
-      if ((nan4.x | nan4.y | nan4.z | nan4.w) != 0) {
+      if (nans) {
         const uint32_t nw[4] = {nan4.x, nan4.y, nan4.z, nan4.w};
 #pragma unroll
         for (int c = 0; c < kBN; ++c)
           if ((nw[c >> 5] >> (c & 31)) & 1u) s[c] = __uint_as_float(0x7fc00000u);
       }
-      if (__any_sync(0xffffffffu, valid && (cl > 0 || ch < kBN))) {
+      if (edge) {
 #pragma unroll
         for (int c = 0; c < kBN; ++c)
           if (c < cl || c >= ch) s[c] = -INFINITY;
       }
-      if (warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kBN)) {
+      if (own_column) {
         // a seed row does not see its own cached column
         const int dc = is_seed ? pos - key0 : -1;
 #pragma unroll
         for (int c = 0; c < kBN; ++c)
           if (c == dc) s[c] = -INFINITY;
       }
-      // row maximum: four independent 3-input max chains
-      float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
-#pragma unroll
-      for (int c = 4; c + 8 <= kBN; c += 8) {
-        mx0 = fmax3(mx0, s[c], s[c + 1]);
-        mx1 = fmax3(mx1, s[c + 2], s[c + 3]);
-        mx2 = fmax3(mx2, s[c + 4], s[c + 5]);
-        mx3 = fmax3(mx3, s[c + 6], s[c + 7]);
-      }
-      mx0 = fmax3(mx0, s[kBN - 4], s[kBN - 3]);
-      mx1 = fmax3(mx1, s[kBN - 2], s[kBN - 1]);
-      const float m_tile = fmax3(mx0, mx1, fmaxf(mx2, mx3)) * scale;
       float alpha = 1.0f;
       bool rescaled = false;
-      if (m_tile > m_run + kRescaleThreshold) {
-        alpha = (m_run == -INFINITY) ? 0.0f : ex2_approx(m_run - m_tile);
-        m_run = m_tile;
-        rescaled = true;
+      if (!fixed) {
+        // row maximum: four independent 3-input max chains
+        float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
+#pragma unroll
+        for (int c = 4; c + 8 <= kBN; c += 8) {
+          mx0 = fmax3(mx0, s[c], s[c + 1]);
+          mx1 = fmax3(mx1, s[c + 2], s[c + 3]);
+          mx2 = fmax3(mx2, s[c + 4], s[c + 5]);
+          mx3 = fmax3(mx3, s[c + 6], s[c + 7]);
+        }
+        mx0 = fmax3(mx0, s[kBN - 4], s[kBN - 3]);
+        mx1 = fmax3(mx1, s[kBN - 2], s[kBN - 1]);
+        const float m_tile = fmax3(mx0, mx1, fmaxf(mx2, mx3)) * scale;
+        if (m_tile > m_run + kRescaleThreshold) {
+          alpha = (m_run == -INFINITY) ? 0.0f : ex2_approx(m_run - m_tile);
+          m_run = m_tile;
+          rescaled = true;
+        }
       }
       const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
       // p = 2^(s * scale - m) on pairs; four independent partial row sums
       const uint64_t scale2 = f2_pack(scale, scale);
       const uint64_t negm2 = f2_pack(-m_use, -m_use);
       uint64_t acc2[4] = {0, 0, 0, 0};
+      if (kCap && small) {
+        // C x P(x^2) with x = s cap_x, the powers of cap_x in the coefficients
+        const float xx = p.cap_x * p.cap_x, k0 = kTanh0 * p.cap_log2 * p.cap_x, k1 = kTanh1 * p.cap_log2 * p.cap_x * xx,
+                    k2 = kTanh2 * p.cap_log2 * p.cap_x * xx * xx, k3 = kTanh3 * p.cap_log2 * p.cap_x * xx * xx * xx;
+        const uint64_t t0 = f2_pack(k0, k0), t1 = f2_pack(k1, k1), t2 = f2_pack(k2, k2), t3 = f2_pack(k3, k3);
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        uint32_t packed[32];
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t packed[32];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          float x0, x1;
-          f2_unpack(f2_fma(f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]), scale2, negm2), x0, x1);
-          const float e0 = ex2_approx(x0);
-          const float e1 = ex2_approx(x1);
-          packed[c] = pack_bf16x2(e0, e1);
-          acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
+          for (int c = 0; c < 32; ++c) {
+            const uint64_t x = f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]);
+            const uint64_t z = f2_mul(x, x);
+            float x0, x1;
+            f2_unpack(f2_fma(x, f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0), negm2), x0, x1);
+            const float e0 = ex2_approx(x0);
+            const float e1 = ex2_approx(x1);
+            packed[c] = pack_bf16x2(e0, e1);
+            acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
+          }
+          tmem_st32(s_addr + 32 * hf, packed);
         }
-        tmem_st32(s_addr + 32 * hf, packed);
+      } else {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t packed[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            float x0, x1;
+            f2_unpack(f2_fma(f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]), scale2, negm2), x0, x1);
+            const float e0 = ex2_approx(x0);
+            const float e1 = ex2_approx(x1);
+            packed[c] = pack_bf16x2(e0, e1);
+            acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
+          }
+          tmem_st32(s_addr + 32 * hf, packed);
+        }
       }
       float rs[4];
       f2_unpack(f2_add(acc2[0], acc2[1]), rs[0], rs[1]);
@@ -687,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     float m = m_run, l = l_run, w[2] = {1.0f, 1.0f};
     const uint32_t o0 = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 2 * kBN;
     int c0 = 0, c1 = 4;   // 32-column chunks that this thread finishes
-    if (!kPair) {
+    if (!kDecoded) {
       float2* ml = reinterpret_cast<float2*>(sm_q);   // every product is complete: Q is not read any more
       if (ok) ml[stream * kBM + R] = make_float2(m_run, l_run);
       softmax_sync();
@@ -720,11 +789,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         float o[32];
         if (nt > 0) {
           uint32_t x[32];
-          tmem_ld32((kPair ? o_addr : o0) + 32 * c, x);
+          tmem_ld32((kDecoded ? o_addr : o0) + 32 * c, x);
           tmem_ld_wait(x);
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = w[0] == 0.0f ? 0.0f : __uint_as_float(x[e]) * w[0];
-          if (!kPair && nt > 1) {
+          if (!kDecoded && nt > 1) {
             tmem_ld32(o0 + kD + 32 * c, x);
             tmem_ld_wait(x);
 #pragma unroll
@@ -791,11 +860,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 //      the V row, P'_j = 2^(s_j + e_j - m), m the row's reference for s_j + e_j, and the sum has 2^(s_j - m) of its
 //      own. P' is rounded to 9 bits (off by at most 2^-9 of it; bf16 is by 2^-8) and scaled by 2^12: what is
 //      2^-28 of the largest is still held (e5m2's smallest is 2^-16). References take max(e_j, -90) for e_j, so that a row
-//      whose largest weight meets a V row far smaller or larger than the others' has a sum within fp32's range.
+//      whose largest weight meets a V row far smaller or larger than the others' has a sum within fp32's range; a V row of
+//      zeros has e_j = -90.
 // A softmax thread is a key: its scales are scalars of the thread. The keys' maximum of a row is only taken
 // when some score is above the row's reference by more than the threshold (one vote a tile); sums stay with the
 // threads until the end. V codes of NaN would reach every row (0 * NaN), so four warps look for them, put zeros in
-// their places and report their keys, whose scores become NaN.
+// their places and report their keys, whose scores become NaN; they report rows of zeros too.
 // Streams: alternate KV tiles with sums and an accumulator of their own, merged at the end.
 // Roles (480 threads): warps 0-3, 4-7 softmax of the streams; 8-11 NaN codes; 12 products; 13, 14 copies of K, V.
 // Tensor memory: S0 | S1 | O0 | O1, 3 kN columns each.
@@ -888,6 +958,7 @@ struct RowsSmem {
   uint64_t v_clean[kStages];      // looked through for NaN codes
   uint64_t s_full[2], p_full[2], o_full, drain;
   uint4 nan_keys[kStages];        // keys with a NaN code in V
+  uint4 zero_keys[kStages];       // keys whose V row is zeros
   int4 row[kN];                   // lo, hi, position of a seed row or -1
   float4 fin[kN];                 // weights of the two accumulators and of the masked-input value, 1 / l
   float m[2][kN];                 // per stream: the rows' references m - 12
@@ -1105,20 +1176,24 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       ok = warp_wait(&sm.v_full[st], (j / kStages) & 1, &sm.abort);
       if (!ok) break;
       const uint32_t row = smem_u32(sm.v[st]) + key * kD;
-      uint32_t hit = 0;
+      uint32_t hit = 0, any = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint4 c = lds128(row + ((i ^ (key & 7)) << 4));
+        any |= c.x | c.y | c.z | c.w;
         hit |= ((c.x & 0x7f7f7f7fu) + 0x01010101u) | ((c.y & 0x7f7f7f7fu) + 0x01010101u) |
                ((c.z & 0x7f7f7f7fu) + 0x01010101u) | ((c.w & 0x7f7f7f7fu) + 0x01010101u);
       }
       const bool bad = (hit & 0x80808080u) != 0;
-      const uint32_t nans = __ballot_sync(0xffffffffu, bad);
+      const uint32_t nans = __ballot_sync(0xffffffffu, bad), zeros = __ballot_sync(0xffffffffu, (any & 0x7f7f7f7fu) == 0);
       if (bad) {
 #pragma unroll 1
         for (int i = 0; i < 8; ++i) sts128(row + 16 * i, 0, 0, 0, 0);
       }
-      if (lane == 0) reinterpret_cast<uint32_t*>(&sm.nan_keys[st])[key >> 5] = nans;
+      if (lane == 0) {
+        reinterpret_cast<uint32_t*>(&sm.nan_keys[st])[key >> 5] = nans;
+        reinterpret_cast<uint32_t*>(&sm.zero_keys[st])[key >> 5] = zeros;
+      }
       fence_proxy_async_smem();
       mbar_arrive(&sm.v_clean[st]);
     }
@@ -1214,7 +1289,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       float t[kN];        // s_j + e_j - m + 12, in log2 units
       bool over = !ok;    // a warp whose wait gave up votes all the same: the stream's barriers take 128 threads
       // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
-      const float e_v = static_cast<float>(v_byte - 127);
+      // a V row of zeros has the smallest exponent, whatever its byte: however large its key's weight, it leaves the
+      // reference to the others
+      const bool zero_v = ok && ((reinterpret_cast<const uint32_t*>(&sm.zero_keys[st])[key >> 5] >> (key & 31)) & 1u);
+      const float e_v = static_cast<float>(zero_v ? kEvFloor : v_byte - 127);
       const float lift = fmaxf(e_v, static_cast<float>(kEvFloor)) - e_v;
       if (ok) {
         tc_fence_after_sync();
@@ -1439,41 +1517,74 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
   if (lane == 0 && lse != nullptr) lse[row] = (m + lg2_approx(l)) * 0.6931471805599453f;
 }
 
-enum Mode { kRows16, kRows32, kShared, kPairs };
-constexpr int kModeRows[] = {16, 32, kBM, 2 * kBM};   // packed rows of a CTA
+// kDecodedPairs: pairs of Q tiles over a memory that a pass of its own decodes first; kReadBack: cover_attn_fwd_prefix's
+// kernels over such a memory, where every row sees every key and scores are not capped
+enum Mode { kRows16, kRows32, kTile, kDecodedPairs, kReadBack };
+constexpr int kModes = 5;
+constexpr int kModeRows[kModes] = {16, 32, kBM, 2 * kBM, 1};   // packed rows of a CTA
+
+// Capped scores lie in [-C, C], C = cap log2(e). For C <= 75 (caps up to 52) every row takes the same reference, C - 45 or
+// 0, and no maxima are looked for: the weights lie in [2^(45 - 2 C), 2^45], at least 2^-105, and 2^17 of
+// the largest times values of up to 2^65 stay below fp32's largest number. (Caps below 2^-10 would put powers of 1 / cap
+// beyond it.)
+float fixed_reference(float cap_log2) {
+  return cap_log2 >= 1.0f / 1024.0f && cap_log2 <= 75.0f ? fmaxf(0.0f, cap_log2 - 45.0f) : -INFINITY;
+}
 
 struct Plan {
   Mode mode;
   int n_groups, nsplit;
+  double us;
 };
 
-// The kernel and the parts of the keys.
-Plan plan_of(int B, int Hq, int Hkv, int Lq, int L) {
+// Resident clusters of 1 .. 8 CTAs, one CTA an SM, that the prediction for cover_attn_fwd_prefix's kernels goes by.
+constexpr int kClusters[8] = {152, 76, 48, 36, 28, 24, 20, 18};
+
+// The kernel and the parts of the keys. plain: no key ranges, no cap.
+//
+// Predicted microseconds, fitted to 433 calls back to back on GB300 (24 windows of 1 to 1024 rows over 300 to 20000
+// keys, batches of 1 to 16, 1 to 64 parts; off by 4 to 5 %, at most 26 %): a base, and for every wave of one CTA an SM a
+// start and a time per KV tile; where the keys are in parts, the second kernel's start, its walk over the parts, and
+// the parts' rows. Decoding a memory takes 1e-4 us a row.
+struct ModeCost {
+  double base, wave, tile, combine, row;
+};
+constexpr ModeCost kCosts[kReadBack] = {
+    {2.2, 4.5, 0.72, 0.8, 6.4e-4}, {2.4, 6.0, 0.92, 0.8, 4.8e-4}, {3.0, 4.1, 1.34, 1.5, 2.5e-4}, {5.0, 3.5, 1.72, 2.4, 1.9e-4}};
+constexpr double kPartUs = 0.15, kDecodeRowUs = 1.0e-4, kDecodeUs = 1.8;
+
+Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
   Plan best{};
-  double best_us = 0.0;
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
-  const long long rows = static_cast<long long>(B) * Hq * Lq;
+  const double rows = static_cast<double>(B) * Hq * Lq, decode_us = kDecodeRowUs * B * Hkv * L;
   const int nkv = (L + kBN - 1) / kBN;
-  constexpr double kTileUs[] = {0.75, 0.75, 1.1, 1.8};
-  for (int mode = 0; mode < 4; ++mode) {
+  for (int mode = 0; mode < kReadBack; ++mode) {
     if (mode > 0 && kModeRows[mode - 1] >= packed) continue;   // a smaller one holds all rows
+    const ModeCost& k = kCosts[mode];
     const long long groups = (packed + kModeRows[mode] - 1) / kModeRows[mode];
     const long long units = groups * Hkv * B;
-    for (int ns = 1; ns <= nkv && ns <= 64; ++ns) {
+    for (int ns = 1; ns <= nkv && ns <= kMaxParts; ++ns) {
       const long long waves = (units * ns + kSms - 1) / kSms;
       const int tiles = (nkv + ns - 1) / ns;
-      const double us = waves * (3.0 + kTileUs[mode] * tiles) + (ns > 1 ? 1.5 + 2.0e-7 * rows * ns * 520 : 0.0);
-      if (best.nsplit == 0 || us < best_us) {
-        best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns};
-        best_us = us;
-      }
+      const double us = k.base + waves * (k.wave + k.tile * tiles) + (mode == kDecodedPairs ? decode_us : 0.0) +
+                        (ns > 1 ? k.combine + kPartUs * ns + k.row * rows * ns : 0.0);
+      if (best.nsplit == 0 || us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, us};
       if (units * ns > 8 * kSms) break;
     }
+  }
+  if (plain) {
+    AttnArgs a{};
+    a.B = B, a.Hq = Hq, a.Hkv = Hkv, a.L = L, a.D = kD, a.Lq = Lq, a.q0 = 0;
+    double us = window_square_us(a, kSms);
+    const WindowChoice c = window_gqa_model(a, kSms, kClusters);
+    if (c.packed) us = std::min(us, c.packed_us);
+    us += kDecodeUs + decode_us;
+    if (us < best.us) best = Plan{kReadBack, 1, 1, us};
   }
   return best;
 }
 
-using TileKernel = void (*)(const CUtensorMap, const Params);
+using TileKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
 using RowsKernel = void (*)(const CUtensorMap, const CUtensorMap, const Params);
 constexpr TileKernel kTileKernels[2][2] = {{attn_prefix8_kernel<false, false>, attn_prefix8_kernel<false, true>},
                                            {attn_prefix8_kernel<true, false>, attn_prefix8_kernel<true, true>}};
@@ -1482,20 +1593,60 @@ constexpr RowsKernel kRowsKernels[2][2] = {{attn_prefix8_rows_kernel<16, false>,
 constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSmem<32>) + 1024};
 static_assert(kRowsSmemBytes[0] <= 227 * 1024 && kRowsSmemBytes[1] <= 227 * 1024, "shared memory of a CTA");
 
+// The workspace: the parts' accumulators and sums, or the decoded K and V (both where both are needed).
 size_t part_bytes(long long rows, int nsplit) {
-  return nsplit <= 1 ? 0 : static_cast<size_t>(rows) * nsplit * (kD * sizeof(float) + sizeof(float2));
+  return nsplit <= 1 ? 0 : (static_cast<size_t>(rows) * nsplit * (kD * sizeof(float) + sizeof(float2)) + 15) & ~size_t{15};
+}
+size_t decoded_bytes(const Plan& plan, int B, int Hkv, int L) {
+  return plan.mode >= kDecodedPairs ? static_cast<size_t>(B) * Hkv * L * kD * 2 : 0;   // of K, and of V
+}
+size_t plan_bytes(const Plan& plan, int B, int Hq, int Hkv, int Lq, int L) {
+  return 2 * decoded_bytes(plan, B, Hkv, L) + part_bytes(static_cast<long long>(B) * Hq * Lq, plan.nsplit);
 }
 
 }  // namespace
 
 size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L) {
-  return part_bytes(static_cast<long long>(B) * Hq * Lq, plan_of(B, Hq, Hkv, Lq, L).nsplit);
+  return std::max(plan_bytes(plan_of(B, Hq, Hkv, Lq, L, false), B, Hq, Hkv, Lq, L),
+                  plan_bytes(plan_of(B, Hq, Hkv, Lq, L, true), B, Hq, Hkv, Lq, L));
+}
+
+void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, int* choice, double* us) {
+  const Plan p = plan_of(B, Hq, Hkv, Lq, L, plain);
+  choice[0] = p.mode;
+  choice[1] = p.n_groups;
+  choice[2] = p.nsplit;
+  *us = p.us;
+}
+
+size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit) {
+  return plan_bytes(Plan{static_cast<Mode>(mode), 1, nsplit, 0.0}, B, Hq, Hkv, Lq, L);
 }
 
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
   if (rows + 2 * kBM > 0x7fffffffLL) return -2;
-  const Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.L);
+  const bool plain = a.key_lo == nullptr && a.key_hi == nullptr && !(a.softcap > 0.0f);
+  Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.L, plain);
+  if (a.mode >= 0) {   // a debug call says which
+    plan.mode = static_cast<Mode>(a.mode);
+    plan.nsplit = a.nsplit;
+    plan.n_groups = static_cast<int>((static_cast<long long>(a.Hq / a.Hkv) * a.Lq + kModeRows[a.mode] - 1) / kModeRows[a.mode]);
+  }
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  const size_t kv_bytes = decoded_bytes(plan, a.B, a.Hkv, a.L);
+  if (kv_bytes > 0) {
+    const Kv8Args d{ws, ws + kv_bytes, nullptr, nullptr, 0, a.L, a.B, a.Hkv, a.L, kD, 2, const_cast<void*>(a.k8),
+                    const_cast<void*>(a.v8), const_cast<uint8_t*>(a.k_exp), const_cast<uint8_t*>(a.v_exp)};
+    const int rd = launch_kv8_decode(d, stream);
+    if (rd != 0) return rd;
+  }
+  if (plan.mode == kReadBack) {
+    AttnArgs w{a.q, ws, ws + kv_bytes, a.k_seedmask, a.v_seedmask, a.seed_idx, a.n_seeds, a.B, a.Hq, a.Hkv, a.L, kD, a.out,
+               a.lse, a.Lq, a.q0};
+    const int rc = try_launch_attn_window_gqa(w, status, stream, false);
+    return rc != kWindowGqaNotTaken ? rc : launch_attn_bf16_sm103(w, status, stream);
+  }
   const long long grid = static_cast<long long>(plan.n_groups) * a.Hkv * a.B * plan.nsplit;
   if (grid > 0x7fffffffLL) return -2;
   static ContextCache<int> setup;
@@ -1503,23 +1654,28 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   const int rc = setup.get(&unused, [&](int&) {
     for (int m = 0; m < 2; ++m)
       for (int c = 0; c < 2; ++c) {
-        if (cudaFuncSetAttribute(kTileKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(kSmemBytes)) != cudaSuccess ||
-            cudaFuncSetAttribute(kRowsKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(kRowsSmemBytes[m])) != cudaSuccess)
+        if (cudaFuncSetAttribute(kRowsKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(kRowsSmemBytes[m])) != cudaSuccess ||
+            cudaFuncSetAttribute(kTileKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(kSmemBytes)) != cudaSuccess)
           return -3;
-        // the register split inside the kernel assumes exactly kLaunchRegs per thread at launch; any
-        // other count could leave setmaxnreg.inc waiting, so refuse to launch
+        // the register splits inside the kernels assume exactly these counts per thread at launch; any
+        // other could leave setmaxnreg.inc waiting, so refuse to launch
         cudaFuncAttributes fa;
-        if (cudaFuncGetAttributes(&fa, kTileKernels[m][c]) != cudaSuccess || fa.numRegs != kLaunchRegs) return -2;
+        if (cudaFuncGetAttributes(&fa, kTileKernels[m][c]) != cudaSuccess || fa.numRegs != (m ? kReadLaunchRegs : kLaunchRegs))
+          return -2;
       }
     return 0;
   });
   if (rc != 0) return rc;
   const bool few = plan.mode == kRows16 || plan.mode == kRows32;
-  CUtensorMap t0, t1;
-  if (few ? !make_u8_map_4d(&t0, a.k8, kD, a.L, a.Hkv, a.B, kBN) || !make_u8_map_4d(&t1, a.v8, kD, a.L, a.Hkv, a.B, kBN)
-          : !make_bf16_map_4d(&t0, a.q, kD, static_cast<uint64_t>(rows), 1, 1, kBM))
+  const bool decoded = plan.mode == kDecodedPairs;
+  CUtensorMap tq{}, tk{}, tv{};
+  if (few ? !make_u8_map_4d(&tk, a.k8, kD, a.L, a.Hkv, a.B, kBN) || !make_u8_map_4d(&tv, a.v8, kD, a.L, a.Hkv, a.B, kBN)
+          : !make_bf16_map_4d(&tq, a.q, kD, static_cast<uint64_t>(rows), 1, 1, kBM))
+    return -3;
+  if (decoded &&
+      (!make_bf16_map_4d(&tk, ws, kD, a.L, a.Hkv, a.B, kBN) || !make_bf16_map_4d(&tv, ws + kv_bytes, kD, a.L, a.Hkv, a.B, kBN)))
     return -3;
   const float log2e = 1.4426950408889634f, root = sqrtf(static_cast<float>(kD));
   Params p{};
@@ -1535,7 +1691,7 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.key_hi = a.key_hi;
   p.out = static_cast<__nv_bfloat16*>(a.out);
   p.lse = a.lse;
-  p.part_o = static_cast<float*>(a.workspace);
+  p.part_o = reinterpret_cast<float*>(ws + 2 * kv_bytes);
   p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows) * plan.nsplit * kD);
   p.status = status;
   p.rows = rows;
@@ -1552,6 +1708,8 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   const bool cap = a.softcap > 0.0f;
   p.cap_log2 = a.softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (a.softcap * root) : 0.0f;
+  p.cap_x = cap ? 1.0f / (a.softcap * root) : 0.0f;
+  p.cap_ref = cap ? fixed_reference(p.cap_log2) : -INFINITY;
   cudaLaunchAttribute attr[1];
   const dim3 ctas(static_cast<unsigned>(grid));
   cudaLaunchConfig_t cfg;
@@ -1559,10 +1717,10 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   if (few) {
     const int m = plan.mode == kRows16 ? 0 : 1;
     cfg = pdl_config(ctas, dim3(kRowsThreads), kRowsSmemBytes[m], stream, attr);
-    e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], t0, t1, p);
+    e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], tk, tv, p);
   } else {
-    cfg = pdl_config(ctas, dim3(kThreads), kSmemBytes, stream, attr);
-    e = cudaLaunchKernelEx(&cfg, kTileKernels[plan.mode == kPairs ? 1 : 0][cap ? 1 : 0], t0, p);
+    cfg = pdl_config(ctas, dim3(decoded ? kReadThreads : kThreads), kSmemBytes, stream, attr);
+    e = cudaLaunchKernelEx(&cfg, kTileKernels[decoded ? 1 : 0][cap ? 1 : 0], tq, tk, tv, p);
   }
   if (e == cudaSuccess && plan.nsplit > 1) {
     cfg = pdl_config(dim3(static_cast<unsigned>((rows + kCombineWarps - 1) / kCombineWarps)), dim3(kCombineWarps * 32), 0,

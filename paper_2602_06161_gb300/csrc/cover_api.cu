@@ -265,25 +265,33 @@ size_t cover_attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk
   return cover::attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk);
 }
 
+static int attn_prefix8_call(cover::Attn8Args a, int D, size_t workspace_bytes, void* stream) {
+  int rc = check_window(a.Lq, a.L, a.q0);
+  if (rc != COVER_OK) return rc;
+  rc = check_attn_args(a.q, a.k8, a.v8, a.k_seedmask, a.v_seedmask, a.seed_idx, a.n_seeds, a.B, a.Hq, a.Hkv, a.L, D, a.out,
+                       a.lse, 16);
+  if (rc != COVER_OK) return rc;
+  if (a.k_exp == nullptr || a.v_exp == nullptr || !aligned(a.key_lo, 4) || !aligned(a.key_hi, 4) ||
+      !aligned(a.workspace, 16))
+    return COVER_ERR_INVALID_ARG;
+  if (!(a.softcap >= 0.0f) || a.softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
+  if (D != 128) return COVER_ERR_UNSUPPORTED;
+  const size_t need = a.mode < 0 ? cover::attn_prefix8_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L)
+                                 : cover::attn_prefix8_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L, a.mode, a.nsplit);
+  if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return COVER_ERR_INVALID_ARG;
+  int* st = status_block();
+  if (st == nullptr) return COVER_ERR_CUDA;
+  return cover::launch_attn_prefix8(a, st, static_cast<cudaStream_t>(stream));
+}
+
 int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8, const uint8_t* k_exp, const uint8_t* v_exp,
                            const void* k_seedmask, const void* v_seedmask, const int32_t* seed_idx, int n_seeds,
                            int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D, const int32_t* key_lo,
                            const int32_t* key_hi, float softcap, void* out, float* lse, void* workspace,
                            void* stream) {
-  int rc = check_window(Lq, Lk, q0);
-  if (rc != COVER_OK) return rc;
-  rc = check_attn_args(q, k8, v8, k_seedmask, v_seedmask, seed_idx, n_seeds, B, Hq, Hkv, Lk, D, out, lse, 16);
-  if (rc != COVER_OK) return rc;
-  if (k_exp == nullptr || v_exp == nullptr || !aligned(key_lo, 4) || !aligned(key_hi, 4) || !aligned(workspace, 16))
-    return COVER_ERR_INVALID_ARG;
-  if (!(softcap >= 0.0f) || softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
-  if (D != 128) return COVER_ERR_UNSUPPORTED;
-  if (workspace == nullptr && cover::attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) > 0) return COVER_ERR_INVALID_ARG;
-  int* st = status_block();
-  if (st == nullptr) return COVER_ERR_CUDA;
-  const cover::Attn8Args a{q,  k8,  v8,  k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,        Hq, Hkv,
-                           Lq, Lk,  q0,  key_lo, key_hi, softcap,  out,        lse,      workspace};
-  return cover::launch_attn_prefix8(a, st, static_cast<cudaStream_t>(stream));
+  const cover::Attn8Args a{q,  k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,   Hq,       Hkv,
+                           Lq, Lk, q0, key_lo, key_hi, softcap,  out,        lse,      workspace};
+  return attn_prefix8_call(a, D, ~size_t{0}, stream);
 }
 
 size_t cover_decide_workspace_bytes(int N, int n_seq) {
@@ -470,6 +478,28 @@ int cover_debug_window_model(int B, int Hq, int Hkv, int Lq, int Lk, int q0, int
   choice[5] = c.n_qt;
   times[0] = c.packed_us;
   times[1] = c.square_us;
+  return COVER_OK;
+}
+
+int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8, const uint8_t* k_exp, const uint8_t* v_exp,
+                             const void* k_seedmask, const void* v_seedmask, const int32_t* seed_idx, int n_seeds,
+                             int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D, const int32_t* key_lo,
+                             const int32_t* key_hi, float softcap, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, int mode, int nsplit, void* stream) {
+  if (mode < 0 || mode >= cover::kAttn8Modes || nsplit < 1 || nsplit > 64) return COVER_ERR_INVALID_ARG;
+  if (mode == cover::kAttn8ReadBack && (nsplit != 1 || key_lo != nullptr || key_hi != nullptr || softcap != 0.0f))
+    return COVER_ERR_UNSUPPORTED;
+  cover::Attn8Args a{q,  k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,   Hq,       Hkv,
+                     Lq, Lk, q0, key_lo, key_hi, softcap,  out,        lse,      workspace};
+  a.mode = mode;
+  a.nsplit = nsplit;
+  return attn_prefix8_call(a, D, workspace_bytes, stream);
+}
+
+int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int32_t* choice, double* us) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Lq < 1 || Lk < Lq || choice == nullptr || us == nullptr)
+    return COVER_ERR_INVALID_ARG;
+  cover::attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, plain != 0, choice, us);
   return COVER_OK;
 }
 

@@ -170,6 +170,8 @@ struct Kv8Args {
   uint8_t* v_exp;
 };
 int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream);
+// Every row of the memory in bf16 for an attention kernel: a row whose K or V is NaN gets a NaN key and a zero value.
+int launch_kv8_decode(const Kv8Args& a, cudaStream_t stream);
 
 // Window attention over an 8-bit memory (attn_prefix8.cu).
 struct Attn8Args {
@@ -189,8 +191,14 @@ struct Attn8Args {
   void* out;
   float* lse;
   void* workspace;
+  int mode = -1, nsplit = 0;   // debug calls: the kernel and the parts of the keys, whatever the plan says
 };
+constexpr int kAttn8Modes = 5;      // attn_prefix8.cu's Mode
+constexpr int kAttn8ReadBack = 4;
 size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L);
+size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit);
+// choice: mode, groups of rows a KV head, parts of the keys; us: predicted. plain: no key ranges, no cap.
+void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, int* choice, double* us);
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream);
 
 int launch_umma_tile(const void* a, const void* b, const void* p, const void* v, float* c1, float* c2, int* status,

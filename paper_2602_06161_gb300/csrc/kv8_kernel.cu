@@ -8,8 +8,9 @@
 //   read:  row = code * 2^(x - 127); a position out of [0, L) gives zeros.
 //
 // Bound by memory: each row is read and written once. D / N lanes hold a row (N elements of 16 bytes on the wide
-// side), and a thread has the K and V vectors of kTok consecutive slots in flight (128 bytes), so that
-// the exponent bytes of consecutive positions leave in one request too.
+// side), and a thread has the K and V vectors of kTok = 2 consecutive slots in flight, 64 bytes, with six CTAs of 256
+// threads an SM (4 x 8 heads, 8191 rows of 128 bf16 from a projection written in 39 us; with one slot and six
+// CTAs 46, with four and four 42, eight and two 47).
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -23,7 +24,7 @@ namespace cover {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTok = 4;   // slots of a lane group
+constexpr int kTok = 2;   // slots of a lane group
 
 struct Kv8Params {
   const uint8_t* src[2];     // k, v rows (write) or codes (read)
@@ -94,9 +95,15 @@ struct Codes<4> {
   }
 };
 
-// CTA (slot tile, head group, b): T slots, of p.heads heads one after the other.
-template <typename T, int D, bool kWrite>
-__global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ Kv8Params p) {
+// CTA of kSlots slots, of p.heads heads one after the other. Rows to be written mostly come from a projection, where a
+// token's heads are neighbours, so the heads' CTAs are neighbours too; rows read lie by heads on both sides.
+enum Kv8 { kRead, kWriteRows, kDecode };
+
+// kDecode: reads, and a row whose K or V is NaN gets a NaN key and a zero value (an attention kernel's weight of
+// zero times NaN would be NaN; a NaN score reaches the rows that see the key alone).
+template <typename T, int D, Kv8 kKind>
+__global__ void __launch_bounds__(kThreads, 6) kv8_kernel(const __grid_constant__ Kv8Params p) {
+  constexpr bool kWrite = kKind == kWriteRows;
   using W = Wide<T>;
   constexpr int N = W::kN;
   constexpr int kLanes = D / N;                      // lanes of a row
@@ -107,7 +114,8 @@ __global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ K
   griddep_launch_dependents();
   const int tid = threadIdx.x;
   const int b = blockIdx.z;
-  const int slot0 = blockIdx.x * kSlots;
+  const int slot0 = static_cast<int>(kWrite ? blockIdx.y : blockIdx.x) * kSlots;
+  const int head_group = static_cast<int>(kWrite ? blockIdx.x : blockIdx.y);
   const int32_t* list = p.pos == nullptr ? nullptr : p.pos + static_cast<size_t>(b) * p.n;
   for (int i = tid; i < kSlots; i += kThreads) {
     const int s = slot0 + i;
@@ -139,8 +147,8 @@ __global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ K
   int at[kTok];
 #pragma unroll
   for (int j = 0; j < kTok; ++j) at[j] = s_pos[group * kTok + j];
-  const int h1 = min(p.Hkv, static_cast<int>(blockIdx.y + 1) * p.heads);
-  for (int h = blockIdx.y * p.heads; h < h1; ++h) {
+  const int h1 = min(p.Hkv, (head_group + 1) * p.heads);
+  for (int h = head_group * p.heads; h < h1; ++h) {
     const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + h) * p.L;   // the head's first memory row
     if (kWrite) {
       uint4 r[2][kTok];
@@ -192,6 +200,20 @@ __global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ K
             e[w][j] = __ldg(p.exps[w] + mem0 + at[j]);
           }
         }
+      bool nan[kTok] = {};
+      if constexpr (kKind == kDecode) {
+        // a row with a NaN code in its K or V counts as a NaN row too
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) {
+          uint32_t hit = 0;
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            hit |= ((c[w][j].x & 0x7f7f7f7fu) + 0x01010101u) | ((c[w][j].y & 0x7f7f7f7fu) + 0x01010101u);
+          const uint32_t rows = __ballot_sync(0xffffffffu, (hit & 0x80808080u) != 0);
+          const uint32_t mine = (0xffffffffu >> (32 - kLanes)) << (tid & 31 & ~(kLanes - 1));
+          nan[j] = e[0][j] > kExpMax || e[1][j] > kExpMax || (rows & mine) != 0;
+        }
+      }
 #pragma unroll
       for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -199,7 +221,11 @@ __global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ K
           const int s = slot0 + group * kTok + j;
           if (s >= p.n) continue;
           float x[N];
-          Codes<N>::decode(c[w][j], e4m3_scale(e[w][j]), x);
+          int byte = e[w][j];
+          if (kKind == kDecode) {
+            if (nan[j]) c[w][j] = C{}, byte = w ? kExpZero : kExpNan;
+          }
+          Codes<N>::decode(c[w][j], e4m3_scale(byte), x);
           T* out = reinterpret_cast<T*>(p.dst[w]) + ((static_cast<size_t>(b) * p.Hkv + h) * p.n + s) * D + lane * N;
           *reinterpret_cast<uint4*>(out) = W::pack(x);
         }
@@ -208,7 +234,8 @@ __global__ void __launch_bounds__(kThreads) kv8_kernel(const __grid_constant__ K
 }
 
 template <typename T, int D>
-int launch(Kv8Params p, int B, bool write, cudaStream_t stream) {
+int launch(Kv8Params p, int B, Kv8 kind, cudaStream_t stream) {
+  const bool write = kind == kWriteRows;
   constexpr int kSlots = kThreads / (D / Wide<T>::kN) * kTok;
   const long long tiles = (p.n + kSlots - 1) / kSlots;
   if (B > 65535) return -2;
@@ -218,19 +245,22 @@ int launch(Kv8Params p, int B, bool write, cudaStream_t stream) {
   if (write && p.pos != nullptr) groups = std::min<long long>(p.Hkv, std::max<long long>(1, 2 * 152 * 4 / (tiles * B)));
   p.heads = static_cast<int>((p.Hkv + groups - 1) / groups);
   groups = (p.Hkv + p.heads - 1) / p.heads;
-  if (groups > 65535) return -2;
-  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(groups), static_cast<unsigned>(B));
+  if ((write ? tiles : groups) > 65535) return -2;
+  const unsigned x = static_cast<unsigned>(tiles), y = static_cast<unsigned>(groups);
+  const dim3 grid(write ? y : x, write ? x : y, static_cast<unsigned>(B));
   cudaLaunchAttribute attr[1];
   const cudaLaunchConfig_t cfg = pdl_config(grid, dim3(kThreads), 0, stream, attr);
-  const cudaError_t e = write ? cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, true>, p)
-                              : cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, false>, p);
+  cudaError_t e;
+  if (write) e = cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, kWriteRows>, p);
+  else e = cudaLaunchKernelEx(&cfg, kv8_kernel<T, D, kRead>, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
 }  // namespace
 
-int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
-  if (a.n == 0) return 0;
+namespace {
+
+Kv8Params params_of(const Kv8Args& a, bool write) {
   Kv8Params p{};
   for (int w = 0; w < 2; ++w) {
     uint8_t* codes = static_cast<uint8_t*>(w ? a.v8 : a.k8);
@@ -245,9 +275,30 @@ int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
   p.n = a.n;
   p.L = a.L;
   p.Hkv = a.Hkv;
+  p.heads = 1;
+  return p;
+}
+
+}  // namespace
+
+int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
+  if (a.n == 0) return 0;
+  const Kv8Params p = params_of(a, write);
+  const Kv8 kind = write ? kWriteRows : kRead;
   using bf16 = __nv_bfloat16;
-  if (a.elem_bytes == 2) return a.D == 64 ? launch<bf16, 64>(p, a.B, write, stream) : launch<bf16, 128>(p, a.B, write, stream);
-  return a.D == 64 ? launch<float, 64>(p, a.B, write, stream) : launch<float, 128>(p, a.B, write, stream);
+  if (a.elem_bytes == 2) return a.D == 64 ? launch<bf16, 64>(p, a.B, kind, stream) : launch<bf16, 128>(p, a.B, kind, stream);
+  return a.D == 64 ? launch<float, 64>(p, a.B, kind, stream) : launch<float, 128>(p, a.B, kind, stream);
+}
+
+int launch_kv8_decode(const Kv8Args& a, cudaStream_t stream) {
+  using bf16 = __nv_bfloat16;
+  constexpr int kSlots = kThreads / (128 / Wide<bf16>::kN) * kTok;
+  if (a.B > 65535 || a.Hkv > 65535) return -2;
+  const dim3 grid(static_cast<unsigned>((a.n + kSlots - 1) / kSlots), static_cast<unsigned>(a.Hkv), static_cast<unsigned>(a.B));
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = pdl_config(grid, dim3(kThreads), 0, stream, attr);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv8_kernel<bf16, 128, kDecode>, params_of(a, false));
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
 }  // namespace cover

@@ -12,8 +12,11 @@
 // by t 2^-53 turns from the fp64 frequency and 2^-26 turns from the conversion to fp32).
 //
 // Bound by memory: each row is read and written once. A thread holds one 16-byte vector column (two, R / 2
-// apart, in the layout of halves) of one token and walks over heads, so that its sines and cosines
-// serve all of them; the next kHeadsInFlight heads' loads are in flight together.
+// apart, in the layout of halves) of one token and walks over up to eight heads, so that its sines and cosines serve
+// all of them. More threads with fewer loads each are faster than the opposite: 4 x 40 heads, 8191 tokens of 128 bf16
+// took 118 us with one head in flight a thread and four CTAs of 256 an SM, 137 with two and three, 165 with four and
+// two, 253 with eight; in neighbouring pairs 121 with two heads and four CTAs, 148 with one, 162 with four and two; fp32 (32 + 32
+// heads, 4096 tokens) 85 with four heads, 87 with two, 103 with one. Walks over 16 or 40 heads: 127 and 142 us.
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -26,7 +29,6 @@ namespace cover {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeadsInFlight = 4;
 
 struct RopeTensor {
   const uint8_t* in;
@@ -78,7 +80,8 @@ struct alignas(sizeof(T) * N) Vec {
 // T: element; N: elements of a thread's vector (16 bytes, or one element where a size, a stride or
 // a pointer does not allow more); kInter: pairs of neighbours (a vector of N >= 2 holds N / 2 pairs).
 template <typename T, int N, bool kInter>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) rope_kernel(const __grid_constant__ RopeParams p) {
+  constexpr int kHeadsInFlight = sizeof(T) == 2 ? (kInter ? 2 : 1) : 4;
   extern __shared__ uint64_t turns[];   // [R / 2] fractions of a turn per position, 2^64 = one turn
   griddep_wait();
   griddep_launch_dependents();
@@ -122,22 +125,26 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
   }
   const int which = c >= p.chunks0 ? 1 : 0;
   const RopeTensor& t = p.t[which];
-  const int h0 = (which ? c - p.chunks0 : c) * p.chunk;
-  const int h1 = min(h0 + p.chunk, t.heads);
+  // heads h0, h0 + step, ...: the chunks' threads, neighbours in a warp, read and write neighbouring heads
+  const int step = which ? p.chunks - p.chunks0 : p.chunks0;
+  const int h0 = which ? c - p.chunks0 : c;
+  const int n = (t.heads - h0 + step - 1) / step;
   const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + l * t.in_l;
   T* out = reinterpret_cast<T*>(t.out) + b * t.out_b + l * t.out_l;
   using V = Vec<T, N>;
-  for (int h = h0; h < h1; h += kHeadsInFlight) {
+  for (int i0 = 0; i0 < n; i0 += kHeadsInFlight) {
     V x[kHeadsInFlight][2];
 #pragma unroll
     for (int j = 0; j < kHeadsInFlight; ++j) {
-      if (h + j >= h1) break;
-      x[j][0] = *reinterpret_cast<const V*>(in + (h + j) * t.in_h + col0);
-      if (kVecs == 2 && turn) x[j][1] = *reinterpret_cast<const V*>(in + (h + j) * t.in_h + col1);
+      if (i0 + j >= n) break;
+      const T* row = in + (h0 + (i0 + j) * step) * t.in_h;
+      x[j][0] = *reinterpret_cast<const V*>(row + col0);
+      if (kVecs == 2 && turn) x[j][1] = *reinterpret_cast<const V*>(row + col1);
     }
 #pragma unroll
     for (int j = 0; j < kHeadsInFlight; ++j) {
-      if (h + j >= h1) break;
+      if (i0 + j >= n) break;
+      T* row = out + (h0 + (i0 + j) * step) * t.out_h;
       if (turn) {
 #pragma unroll
         for (int i = 0; i < kHalf; ++i) {
@@ -148,8 +155,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
           xb = from_f<T>(a * sn[i] + d * cs[i]);
         }
       }
-      *reinterpret_cast<V*>(out + (h + j) * t.out_h + col0) = x[j][0];
-      if (kVecs == 2 && turn) *reinterpret_cast<V*>(out + (h + j) * t.out_h + col1) = x[j][1];
+      *reinterpret_cast<V*>(row + col0) = x[j][0];
+      if (kVecs == 2 && turn) *reinterpret_cast<V*>(row + col1) = x[j][1];
     }
   }
 }

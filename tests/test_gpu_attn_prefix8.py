@@ -238,6 +238,81 @@ def test_agrees_with_the_bf16_attention_of_what_is_read_back():
         assert (out.float() - ref.float()).abs().max() <= 2 * (2 * 2.0 ** -8 + 4 * 2.0 ** -20 * big) * mass
 
 
+KERNELS = [(0, 1), (0, 3), (1, 1), (1, 2), (2, 1), (2, 4), (3, 1), (3, 3), (2, 64)]
+
+
+@pytest.mark.parametrize("mode,nsplit", KERNELS)
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1, 1, 0, 0), (2, 28, 4, 3, 700, 4, 300), (1, 8, 2, 40, 385, 9, 200), (1, 4, 1, 150, 640, 20, 400),
+                                   (2, 2, 2, 300, 512, 30, 100)])
+def test_every_kernel(shape, mode, nsplit):
+    """Every kernel on every kind of call, whichever the call itself would take: seeds, key ranges, capped scores, parts of the
+    keys that see nothing."""
+    B, Hq, Hkv, Lq, Lk, S, q0 = shape
+    d = _inputs(*shape[:6], q0, scale=2.0)
+    for kind, cap in ((None, 0.0), ("docs", 0.0), ("any", 30.0), (None, 2.0), ("window", 1e4)):
+        lo, hi = (None, None) if kind is None else _ranges(kind, B, Lq, Lk, q0)
+        out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], d["km"], d["vm"], d["seeds"], q0=q0, mode=mode, nsplit=nsplit,
+                                                key_lo=lo, key_hi=hi, softcap=cap)
+        torch.cuda.synchronize()
+        assert api.cover_device_status() == 0
+        _check(d, out, lse, lo, hi, cap)
+
+
+@pytest.mark.parametrize("mode", range(5))
+def test_every_kernel_and_what_is_not_seen(mode):
+    """Codes and bytes of NaN behind the keys that rows see change no bit, whatever the kernel; seen, they are NaN."""
+    B, Hq, Hkv, Lq, Lk, S, q0 = 1, 8, 2, 40, 600, 6, 200
+    d = _inputs(B, Hq, Hkv, Lq, Lk, S, q0)
+    hi = torch.full((B, Lq), 450, device="cuda", dtype=torch.int32)
+    kw = dict(q0=q0, mode=mode) if mode == 4 else dict(q0=q0, mode=mode, key_hi=hi, nsplit=2)
+    call = lambda m: api.cover_debug_attn_prefix8(d["q"], *m, d["km"], d["vm"], d["seeds"], **kw)  # noqa: E731
+    if mode < 4:
+        ref = call(d["mem"])
+        for codes, byte in ((0x7f, 255), (0xff, 120), (0x7e, 250)):
+            m = tuple(x.clone() for x in d["mem"])
+            for i in range(2):
+                m[i].view(torch.uint8)[:, :, 450:] = codes
+                m[2 + i][:, :, 450:] = byte
+            out = call(m)
+            assert torch.equal(out[0], ref[0]) and torch.equal(out[1], ref[1])
+    for i in range(2):
+        m = tuple(x.clone() for x in d["mem"])
+        m[2 + i][0, 1, 30] = 255
+        out, lse = call(m)
+        assert out[:, 4:].isnan().all() and lse[:, 4:].isnan().all() and not out[:, :4].isnan().any()
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+
+
+@pytest.mark.parametrize("shape", [(2, 28, 4, 32, 700, 4, 300), (1, 8, 8, 40, 385, 9, 345), (1, 2, 1, 300, 300, 7, 0)])
+def test_read_back_kernel(shape):
+    d = _inputs(*shape)
+    out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], d["km"], d["vm"], d["seeds"], q0=shape[6], mode=4)
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+    _check(d, out, lse)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_weights_of_every_size(mode):
+    """Few rows: the weights of a key whose V row is far smaller or larger than the others' count as they are, and tails of
+    weights far below the largest do not vanish."""
+    d = _inputs(1, 2, 1, 5, 300, 0, 0)
+    d["mem"][3].copy_(torch.randint(17, 187, (1, 1, 300), generator=_gen(2), device="cuda").to(torch.uint8))
+    out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], q0=0, mode=mode)
+    _check(d, out, lse)
+    # one key with nearly all of the weight and a V row of zeros; the others share 2^-12 of it
+    d = _inputs(1, 1, 1, 1, 4000, 0, 0)
+    d["q"].fill_(0.25)
+    d["mem"][0].view(torch.uint8).fill_(0)
+    d["mem"][0].view(torch.uint8)[0, 0, 77] = 0x70            # 128: a score of 128 * 128 * 2^x * 0.25 / sqrt(128)
+    d["mem"][2].fill_(127)
+    d["mem"][2][0, 0, 77] = 127 - 4                           # about 22.6, against zero
+    d["mem"][1].view(torch.uint8)[0, 0, 77] = 0
+    out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], q0=0, mode=mode)
+    _check(d, out, lse)
+
+
 def test_outputs_given_and_repeated():
     d = _inputs(2, 8, 2, 50, 3000, 8, 100)
     ref, ref_lse = _run(d)
@@ -296,6 +371,9 @@ def test_refusals():
         api.cover_attn_fwd_prefix8(d["q"].transpose(1, 2), *d["mem"], q0=0)
     with pytest.raises(ValueError, match="out must match"):
         api.cover_attn_fwd_prefix8(*a, q0=0, out=torch.empty((1, 4, 7, 128), device="cuda", dtype=torch.bfloat16))
+    for kw in (dict(mode=5), dict(mode=-1), dict(mode=0, nsplit=0), dict(mode=2, nsplit=65), dict(mode=4, nsplit=2), dict(mode=4, softcap=1.0)):
+        with pytest.raises(CoverError):
+            api.cover_debug_attn_prefix8(*a, q0=0, **kw)
     small = api.kv8_memory(1, 2, 64, 64)
     with pytest.raises(CoverError):
         api.cover_attn_fwd_prefix8(d["q"][..., :64].contiguous(), *small, q0=0)
