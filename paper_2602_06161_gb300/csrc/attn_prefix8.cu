@@ -7,22 +7,24 @@
 // (the leave-one-out view). A row that sees no key gives o = 0, lse = -inf; one that sees a key whose
 // K or V row is NaN gives NaN.
 //
-// The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r
-// of head hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view, cut into Q tiles of 128.
-// A CTA takes one or two Q tiles against the KV tiles (128 keys) of one of nsplit parts of what its rows
-// see. Codes arrive by bulk copies (128 rows are 16 KB in one piece); one warpgroup decodes K and one V to bf16
-// (exact: a row's scale is a power of two) into the swizzled layout that the tensor cores read, and S = Q K^T, O += P V
-// run as tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each:
-//   shared Q (kPair = false): both streams are the same Q tile, on the even and the odd KV tiles, with sums and an
-//     accumulator of their own that are merged at the end: the chain load - decode - S - softmax - P V of
-//     one KV tile overlaps the next one's. For windows whose packed rows fill one Q tile.
-//   pair (kPair = true): the streams are two Q tiles that read each decoded KV tile together.
-// With nsplit > 1 the parts leave (m, l, O) in fp32 in the workspace and a second kernel combines them.
+// The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r of head
+// hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view. A CTA takes a group of them against the KV tiles (128
+// keys) of one of nsplit parts of what its rows see; with nsplit > 1 the parts leave (m, l, O) in fp32 in the workspace
+// and a second kernel combines them. Five ways, chosen by plan_of from the sizes:
+//   rows (16 or 32 a group)  codes as 8-bit matrix operands, products turned over; bound by reading the memory
+//   tile (128 rows)          codes decoded to bf16 by the CTA; bound by decoding
+//   pairs (2 x 128 rows)     codes decoded once, by a pass of its own; bound by the tensor cores and the softmax
+//   read back                the kernels of cover_attn_fwd_prefix over the decoded memory, without key ranges and caps
 //
-// Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16
-// issues the products; 17 and 18 issue the copies of K and V.
-// Shared memory: Q (32 or 64 KB) | rings of two entries of K and of V codes, 128 or 64 rows each | K, V in bf16 (2 x 32 KB
-// each).
+// The tile kernel. Codes arrive by bulk copies (128 rows are 16 KB in one piece); one warpgroup decodes K and one V to bf16
+// (exact: a row's scale is a power of two) into the swizzled layout that the tensor cores read, and S = Q K^T, O += P V run as
+// tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each: the even and the odd KV
+// tiles, with sums and an accumulator of their own that are merged at the end, so that the chain load - decode - S - softmax -
+// P V of one KV tile overlaps the next one's. A KV tile takes 1.3 us, of which decoding (two instructions a code, 192 KB
+// through shared memory) is the most: without it 0.9 us, without the softmax 1.0.
+// Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16 issues the
+// products; 17 and 18 the copies of K and V.
+// Shared memory: Q (32 KB) | two tiles of K and of V codes (16 KB each) | K, V in bf16 (2 x 32 KB each).
 // Tensor memory: S0 | S1 (P overwrites their first 64 columns) | O0 | O1, 128 columns each.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -46,18 +48,15 @@ constexpr int kBN = 128;                   // keys per KV tile
 constexpr int kTileBytes = kBM * kD * 2;   // 32 KB
 constexpr int kBoxBytes = kTileBytes / 2;  // one 64-column, 128-byte-swizzled box
 constexpr int kCodeBytes = kBN * kD;       // 16 KB of codes
+constexpr int kHalf = kBN / 2;
 constexpr int kThreads = 640;
-constexpr int kDecodeWarp = 8;
+constexpr int kDecodeWarp = 8, kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kLaunchRegs = 96;            // registers per thread at launch (65536 / 640, rounded down to 8)
 // registers of the softmax, decode and issuing threads: a Q tile's softmax threads hold 128 scores each
 constexpr int kSoftmaxRegs = 160, kDecodeRegs = 56, kIssueRegs = 40;
 static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs, "register split");
 // setmaxnreg.inc takes no count below the thread's own, .dec none above it
 static_assert(kSoftmaxRegs >= kLaunchRegs && kDecodeRegs <= kLaunchRegs && kIssueRegs <= kLaunchRegs, "register split");
-// of the kernel that reads decoded tiles: no decode threads
-constexpr int kReadThreads = 384, kReadLaunchRegs = 168, kReadSoftmaxRegs = 208, kReadIssueRegs = 88;
-static_assert(2 * 128 * kReadSoftmaxRegs + 128 * kReadIssueRegs <= kReadThreads * kReadLaunchRegs, "register split");
-static_assert(kReadSoftmaxRegs >= kReadLaunchRegs && kReadIssueRegs <= kReadLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kMaxParts = 64;              // of the keys
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
@@ -76,11 +75,12 @@ struct Ctl {
 };
 
 struct Smem {
-  uint8_t q_and_ring[3 * kTileBytes];   // Q | rings of K codes and of V codes
+  uint8_t q[kTileBytes];
+  uint8_t ring[4 * kCodeBytes];         // two tiles of K codes, two of V codes
   uint8_t k[2][kTileBytes];
   uint8_t v[2][kTileBytes];
   Ctl ctl;
-  int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
+  int slot[kBM];                        // seed slot of a row's position, or kNoSlot
 };
 constexpr size_t kSmemBytes = sizeof(Smem) + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
@@ -107,6 +107,7 @@ struct Params {
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
   float cap_x;       // 1 / (cap sqrt(d))
+  float cap_poly[4]; // coefficients of the capped score's polynomial, in powers of 1 / (cap sqrt(d))
   float cap_ref;     // reference of all rows under a small cap, or -inf (see fixed_reference)
 };
 
@@ -238,9 +239,33 @@ struct FourBytes {
   }
 };
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// Completes the warp's loads; the registers pass through so that none is used before.
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
 // Barriers and tensor memory, by one warp.
-// fills: arrivals that fill a K or V tile (128 decoding threads, or the thread that issues its copies).
-__device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32_t tmem_columns, uint32_t fills) {
+// fills: arrivals that fill a K or V tile (128 decoding threads, or the thread that issues its copies); rows: threads of a
+// stream's softmax.
+__device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32_t fills, uint32_t rows) {
   if ((threadIdx.x & 31) == 0) {
     mbar_init(&ctl.q_full, 1);
     for (int i = 0; i < 2; ++i) {
@@ -253,7 +278,7 @@ __device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32
       mbar_init(&ctl.v_full[i], fills);
       mbar_init(&ctl.v_empty[i], 1);
       mbar_init(&ctl.s_full[i], 1);
-      mbar_init(&ctl.p_full[i], 128);
+      mbar_init(&ctl.p_full[i], rows);
     }
     mbar_init(&ctl.o_full, 1);
     mbar_init(&ctl.drain, 1);
@@ -264,7 +289,7 @@ __device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32
     tma_prefetch_desc(tm_q);
   }
   __syncwarp();
-  tmem_alloc(&ctl.tmem_base, tmem_columns);
+  tmem_alloc(&ctl.tmem_base, 512);
   tmem_relinquish();
 }
 
@@ -353,44 +378,191 @@ __device__ __forceinline__ Part part_of(int lo, int hi, int ks, int nsplit) {
   return Part{t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0)};
 }
 
-// Copies K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1, decoded already, into the two bf16 tiles in turn; one thread.
-__device__ __forceinline__ void copy_tiles(Ctl& ctl, const Params& p, int which, const CUtensorMap* tm, uint8_t* tiles, int hkv,
-                                           int b, int j0, int nt) {
-  uint64_t* const full = which ? ctl.v_full : ctl.k_full;
-  uint64_t* const empty = which ? ctl.v_empty : ctl.k_empty;
-  int j = 0;
-  bool ok = true;
-  for (; j < nt; ++j) {
-    const int st = j & 1;
-    if (j >= 2) ok = mbar_wait(&empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
-    if (!ok) break;
-    mbar_arrive_expect_tx(&full[st], kTileBytes);
-    for (int h = 0; h < 2; ++h)
-      tma_load_4d(tiles + st * kTileBytes + h * kBoxBytes, tm, &full[st], 64 * h, (j0 + j) * kBN, hkv, b);
+// What a row does not see of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1), keys whose V
+// row is NaN (bit c of `nan` for the chunk's column c); whether anything of it holds for some row of the warp.
+struct Unseen {
+  int lo, hi, own;
+  bool any;
+};
+
+// Caps (to log2 units) and masks the scores of 32 columns from column c0 of the tile on. The loops over a row's chunks are
+// not unrolled: with 128 columns at once 8 % of the instruction fetches missed the SM's cache, the GPC's was at 52 % of
+// its rate, and a KV tile took 4950 cycles on 128 SMs where it took 2780 on 64.
+template <bool kCap>
+__device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, const Unseen& u, uint32_t nan, int c0) {
+  if (kCap) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
   }
-  if (!ok) {
-    if (!ctl.abort) report_status(p.status, kStatusTimeout, 76);
-    ctl.abort = 1;
+  if (nan != 0) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if ((nan >> c) & 1u) s[c] = __uint_as_float(0x7fc00000u);
   }
-  // every copy lands before the CTA's shared memory is released, whatever the other roles did
-  if (which == 0) mbar_wait(&ctl.q_full, 0, nullptr);
-  for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&full[f & 1], (f >> 1) & 1, nullptr);
+  if (u.any) {
+    const int lo = u.lo - c0, hi = u.hi - c0, own = u.own - c0;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if (c < lo || c >= hi || c == own) s[c] = -INFINITY;
+  }
 }
 
-// kDecoded: pairs of Q tiles, K and V read from the workspace, where a pass of its own has decoded them (a row whose K or V
-// is NaN has a NaN key and a zero value there).
-template <bool kDecoded, bool kCap>
-__global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
-    attn_prefix8_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                        const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
-  constexpr int kMmaWarp = kDecoded ? 8 : 16, kLoadWarp = kMmaWarp + 1;
-  constexpr int kSoftmaxWarps = 8;
+__device__ __forceinline__ float max32(const float (&s)[32]) {
+  float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+  for (int c = 4; c + 8 <= 32; c += 8)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mx[e] = fmax3(mx[e], s[c + 2 * e], s[c + 2 * e + 1]);
+  mx[0] = fmax3(mx[0], s[28], s[29]);
+  mx[1] = fmax3(mx[1], s[30], s[31]);
+  return fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+}
+
+// The largest of 32 columns' scores, neither scaled nor capped yet.
+__device__ __forceinline__ float chunk_max(uint32_t addr, const Params& p, const Unseen& u, uint32_t nan, int c0) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+  finish_scores<false>(s, p, u, nan, c0);
+  return max32(s);
+}
+
+// A row's reference in log2 units from its largest product (the cap is monotonous).
+template <bool kCap>
+__device__ __forceinline__ float reference_of(float top, const Params& p) {
+  return !kCap ? top * p.scale_log2 : top == -INFINITY ? top : capped(top, p.cap_in, p.cap_log2);
+}
+
+// P = 2^(score - m) of 32 columns to tensor memory, in bf16; returns their sum. fixed: capped scores whose reference is
+// fixed; those of a chunk that are all small and all seen take the polynomial.
+template <bool kCap>
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, uint32_t nan, int c0,
+                                           float m, bool fixed, bool valid) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+  bool small = false;
+  if (kCap) {
+    if (fixed && nan == 0 && !u.any) {
+      float hi[2] = {};
+#pragma unroll
+      for (int c = 0; c < 32; c += 4) {
+        hi[0] = fmax3(hi[0], fabsf(s[c]), fabsf(s[c + 1]));
+        hi[1] = fmax3(hi[1], fabsf(s[c + 2]), fabsf(s[c + 3]));
+      }
+      small = __all_sync(0xffffffffu, fmaxf(hi[0], hi[1]) * p.cap_x <= kTanhRange || !valid);
+    }
+  }
+  const uint64_t negm2 = f2_pack(-m, -m);
+  uint64_t acc2[2] = {0, 0};
+  uint32_t packed[16];
+  if (kCap && small) {
+    // C x P(x^2) with x = s cap_x, the powers of cap_x in the coefficients
+    const uint64_t t0 = f2_pack(p.cap_poly[0], p.cap_poly[0]), t1 = f2_pack(p.cap_poly[1], p.cap_poly[1]),
+                   t2 = f2_pack(p.cap_poly[2], p.cap_poly[2]), t3 = f2_pack(p.cap_poly[3], p.cap_poly[3]);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      const uint64_t x = f2_pack(s[2 * c], s[2 * c + 1]);
+      const uint64_t z = f2_mul(x, x);
+      float x0, x1;
+      f2_unpack(f2_fma(x, f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0), negm2), x0, x1);
+      const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+      packed[c] = pack_bf16x2(e0, e1);
+      acc2[c & 1] = f2_add(acc2[c & 1], f2_pack(e0, e1));
+    }
+  } else {
+    finish_scores<kCap>(s, p, u, nan, c0);
+    const float scale = kCap ? 1.0f : p.scale_log2;
+    const uint64_t scale2 = f2_pack(scale, scale);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      float x0, x1;
+      f2_unpack(f2_fma(f2_pack(s[2 * c], s[2 * c + 1]), scale2, negm2), x0, x1);
+      const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+      packed[c] = pack_bf16x2(e0, e1);
+      acc2[c & 1] = f2_add(acc2[c & 1], f2_pack(e0, e1));
+    }
+  }
+  tmem_st16(p_addr, packed);
+  float r[4];
+  f2_unpack(acc2[0], r[0], r[1]);
+  f2_unpack(acc2[1], r[2], r[3]);
+  return (r[0] + r[1]) + (r[2] + r[3]);
+}
+
+// A seed row's own score in log2 units: q row `row` of [B Hq Lq], masked-input key row `self`.
+template <bool kCap>
+__device__ __forceinline__ float self_score(const Params& p, long long row, size_t self) {
+  const uint4* qr = reinterpret_cast<const uint4*>(p.q + row * kD);
+  const uint4* kr = reinterpret_cast<const uint4*>(p.k_seedmask + self * kD);
+  float d0 = 0.0f, d1 = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < kD / 8; ++i) {
+    const uint4 a = __ldg(qr + i), c = __ldg(kr + i);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      d0 = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), d0);
+      d1 = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), d1);
+    }
+  }
+  return kCap ? capped(d0 + d1, p.cap_in, p.cap_log2) : (d0 + d1) * p.scale_log2;
+}
+
+// o += w v for 32 columns of a masked-input value.
+__device__ __forceinline__ void add_self(float (&o)[32], float w, const __nv_bfloat16* v) {
+  const uint4* vr = reinterpret_cast<const uint4*>(v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint4 a = __ldg(vr + e);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      o[8 * e + 2 * f] = fmaf(w, __uint_as_float(x[f] << 16), o[8 * e + 2 * f]);
+      o[8 * e + 2 * f + 1] = fmaf(w, __uint_as_float(x[f] & 0xffff0000u), o[8 * e + 2 * f + 1]);
+    }
+  }
+}
+
+// 32 columns of a row: a part's accumulator, or the result (a NaN sum makes the whole row NaN).
+__device__ __forceinline__ void store_chunk(const Params& p, const float (&o)[32], float inv, bool split, int ks, long long orow,
+                                            int col) {
+  if (split) {
+    float4* dst = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(ks) * p.rows + orow) * kD + col);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+  } else {
+    uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kD + col);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                          pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+  }
+}
+
+// Barrier of one Q tile's 256 softmax threads of the pairs kernel, and with the vote whether any of them says so.
+__device__ __forceinline__ void tile_sync(int tile) { asm volatile("bar.sync %0, 256;" ::"r"(2 + tile) : "memory"); }
+__device__ __forceinline__ bool tile_any(int tile, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(x ? 1u : 0u), "r"(2 + tile)
+      : "memory");
+  return r != 0;
+}
+
+template <bool kCap>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_prefix8_tile_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Ctl& ctl = sm.ctl;
-  constexpr int kQTiles = kDecoded ? 2 : 1;
-  uint8_t* const sm_q = sm.q_and_ring;
-  uint8_t* const ring = sm.q_and_ring + kQTiles * kTileBytes;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // CTA (ks, group, hkv, b)
@@ -401,12 +573,12 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
   const int hkv = rest % p.Hkv;
   const int b = rest / p.Hkv;
   const int n_packed = p.G * p.Lq;
-  const int p0 = group * kQTiles * kBM;                                               // the CTA's first packed row
+  const int p0 = group * kBM;                                                         // the CTA's first packed row
   const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;    // packed row 0 in [B Hq Lq, D]
   const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;                  // the KV head's first memory row
 
-  if (warp == kMmaWarp) set_up(ctl, &tm_q, 512, kDecoded ? 1 : 128);
-  if (p.n_seeds > 0 && tid < 2 * kBM) sm.slot[tid] = kNoSlot;
+  if (warp == kMmaWarp) set_up(ctl, &tm_q, 128, 128);
+  if (p.n_seeds > 0 && tid < kBM) sm.slot[tid] = kNoSlot;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -418,15 +590,15 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
   // softmax thread: its row, the keys [row_lo, row_hi) that it sees
   const int stream = warp >> 2;                       // of a softmax warp
   const int R = tid & (kBM - 1);
-  const int P = p0 + (kDecoded ? stream * kBM : 0) + R;
-  const bool valid = warp < kSoftmaxWarps && P < n_packed;
+  const int P = p0 + R;
+  const bool valid = warp < kDecodeWarp && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
   int row_lo = 0, row_hi = p.Lk;
   if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
   if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
   int lo_key = 0, hi_key = p.Lk;                      // keys that some row sees
   if (p.key_lo != nullptr || p.key_hi != nullptr) {
-    if (warp < kSoftmaxWarps) {
+    if (warp < kDecodeWarp) {
       const bool some = valid && row_lo < row_hi;
       const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff);
       const int hi = __reduce_max_sync(0xffffffffu, some ? row_hi : 0);
@@ -440,31 +612,27 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
   }
   const Part part = part_of(lo_key, hi_key, ks, p.nsplit);
   const int j0 = part.j0, nt = part.nt;
-  const bool two_tiles = kDecoded && p0 + kBM < n_packed;   // the pair's second Q tile has rows
 
   if (warp >= kMmaWarp) {
-    setmaxnreg_dec<kDecoded ? kReadIssueRegs : kIssueRegs>();
+    setmaxnreg_dec<kIssueRegs>();
     if ((warp == kLoadWarp || warp == kLoadWarp + 1) && lane == 0 && nt > 0) {
       if (warp == kLoadWarp) {
-        mbar_arrive_expect_tx(&ctl.q_full, kQTiles * kTileBytes);
-        for (int t = 0; t < kQTiles; ++t)
-          for (int h = 0; h < 2; ++h)
-            tma_load_4d(sm_q + t * kTileBytes + h * kBoxBytes, &tm_q, &ctl.q_full, 64 * h,
-                        static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
+        mbar_arrive_expect_tx(&ctl.q_full, kTileBytes);
+        for (int h = 0; h < 2; ++h)
+          tma_load_4d(sm.q + h * kBoxBytes, &tm_q, &ctl.q_full, 64 * h, static_cast<int>(rowbase) + p0, 0, 0);
       }
-      if (kDecoded) copy_tiles(ctl, p, warp - kLoadWarp, warp == kLoadWarp ? &tm_k : &tm_v, warp == kLoadWarp ? sm.k[0] : sm.v[0], hkv, b, j0, nt);
-      else copy_codes(ctl, p, warp - kLoadWarp, ring, mem0, j0, nt);
+      copy_codes(ctl, p, warp - kLoadWarp, sm.ring, mem0, j0, nt);
     } else if (warp == kMmaWarp && lane == 0 && nt > 0) {
       // ---------------- products ----------------
       constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
       constexpr uint32_t id_pv = idesc_bf16_f32(kBM, kD, false, true);
       constexpr uint64_t kTileDesc = kTileBytes >> 4;
-      const uint64_t dq = sdesc_sw128(smem_u32(sm_q), 16, 1024);
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q), 16, 1024);
       const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
       const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
       // S[s] = Q . K(stage)^T
       auto issue_s = [&](int s, int st) {
-        uint64_t a = dq + (kDecoded ? s * kTileDesc : 0), kb = dk + st * kTileDesc;
+        uint64_t a = dq, kb = dk + st * kTileDesc;
         asm volatile("" : "+l"(a), "+l"(kb));   // descriptors are added up here, not kept in registers
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
@@ -488,52 +656,24 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
         return ok;
       };
       bool ok = wait(&ctl.q_full, 0);
-      if (kDecoded) {
-        if (ok && (ok = wait(&ctl.k_full[0], 0))) {
-          issue_s(0, 0);
-          if (two_tiles) issue_s(1, 0);
-          umma_commit(&ctl.k_empty[0]);
-        }
-        for (int j = 0; j < nt && ok; ++j) {
-          const int st = j & 1;
-          const bool next = j + 1 < nt;
-          ok = wait(&ctl.p_full[0], j) && wait(&ctl.v_full[st], j >> 1);
+      // stream j & 1 takes tile j, from stage j & 1
+      for (int j = 0; j < 2 && j < nt && ok; ++j) {
+        ok = wait(&ctl.k_full[j], 0);
+        if (!ok) break;
+        issue_s(j, j);
+        umma_commit(&ctl.k_empty[j]);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int s = j & 1;
+        ok = wait(&ctl.p_full[s], j >> 1) && wait(&ctl.v_full[s], j >> 1);
+        if (!ok) break;
+        issue_pv(s, s, j > 1);
+        umma_commit(&ctl.v_empty[s]);
+        if (j + 2 < nt) {
+          ok = wait(&ctl.k_full[s], (j + 2) >> 1);
           if (!ok) break;
-          issue_pv(0, st, j > 0);
-          if (next) {
-            ok = wait(&ctl.k_full[st ^ 1], (j + 1) >> 1);
-            if (!ok) break;
-            issue_s(0, st ^ 1);
-          }
-          if (two_tiles) {
-            ok = wait(&ctl.p_full[1], j);
-            if (!ok) break;
-            issue_pv(1, st, j > 0);
-            if (next) issue_s(1, st ^ 1);
-          }
-          umma_commit(&ctl.v_empty[st]);
-          if (next) umma_commit(&ctl.k_empty[st ^ 1]);
-        }
-      } else {
-        // stream j & 1 takes tile j, from stage j & 1
-        for (int j = 0; j < 2 && j < nt && ok; ++j) {
-          ok = wait(&ctl.k_full[j], 0);
-          if (!ok) break;
-          issue_s(j, j);
-          umma_commit(&ctl.k_empty[j]);
-        }
-        for (int j = 0; j < nt && ok; ++j) {
-          const int s = j & 1;
-          ok = wait(&ctl.p_full[s], j >> 1) && wait(&ctl.v_full[s], j >> 1);
-          if (!ok) break;
-          issue_pv(s, s, j > 1);
-          umma_commit(&ctl.v_empty[s]);
-          if (j + 2 < nt) {
-            ok = wait(&ctl.k_full[s], (j + 2) >> 1);
-            if (!ok) break;
-            issue_s(s, s);
-            umma_commit(&ctl.k_empty[s]);
-          }
+          issue_s(s, s);
+          umma_commit(&ctl.k_empty[s]);
         }
       }
       if (ok) {
@@ -547,22 +687,22 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
       mbar_wait(&ctl.drain, 0, nullptr);
     }
     __syncwarp();
-  } else if (!kDecoded && warp >= kDecodeWarp) {
+  } else if (warp >= kDecodeWarp) {
     setmaxnreg_dec<kDecodeRegs>();
-    decode_tiles(ctl, p, (warp - kDecodeWarp) >> 2, ring, sm.k[0], sm.v[0], mem0, j0, nt);
+    decode_tiles(ctl, p, (warp - kDecodeWarp) >> 2, sm.ring, sm.k[0], sm.v[0], mem0, j0, nt);
   } else {
     // ---------------- softmax ----------------
-    setmaxnreg_inc<kDecoded ? kReadSoftmaxRegs : kSoftmaxRegs>();
+    setmaxnreg_inc<kSoftmaxRegs>();
     int slot = kNoSlot;
     if (p.n_seeds > 0) {
-      // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
-      const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
+      // the CTA's rows stand at up to 128 positions: r itself, or r - r0 around Lq
+      const int r0 = p.Lq <= kBM ? 0 : p0 % p.Lq;
       const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
       for (int s = tid; s < p.n_seeds; s += 2 * kBM) {
         const int at = __ldg(seeds + s) - p.q0;
         if (at < 0 || at >= p.Lq) continue;
         const int i = at >= r0 ? at - r0 : at - r0 + p.Lq;
-        if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
+        if (i < kBM) atomicMin(&sm.slot[i], s);
       }
       softmax_sync();
       if (valid) slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
@@ -572,34 +712,16 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
     const bool warp_seed = __any_sync(0xffffffffu, is_seed);
     const size_t self = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds + (is_seed ? slot : 0);
     // the seed rows' own scores (log2 units), in the first part alone
-    float s_self = -INFINITY;
-    if (ks == 0 && is_seed && pos >= row_lo && pos < row_hi) {
-      const uint4* qr = reinterpret_cast<const uint4*>(p.q + (rowbase + P) * kD);
-      const uint4* kr = reinterpret_cast<const uint4*>(p.k_seedmask + self * kD);
-      float d0 = 0.0f, d1 = 0.0f;
-#pragma unroll 4
-      for (int i = 0; i < kD / 8; ++i) {
-        const uint4 a = __ldg(qr + i), c = __ldg(kr + i);
-        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          d0 = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), d0);
-          d1 = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), d1);
-        }
-      }
-      s_self = kCap ? capped(d0 + d1, p.cap_in, p.cap_log2) : (d0 + d1) * p.scale_log2;
-    }
+    const float s_self = ks == 0 && is_seed && pos >= row_lo && pos < row_hi
+                             ? self_score<kCap>(p, rowbase + P, self) : -INFINITY;
     const bool warp_live = __any_sync(0xffffffffu, valid);
     const uint32_t s_addr = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + stream * kBN;
     const uint32_t o_addr = s_addr + 2 * kBN;
-    const float scale = kCap ? 1.0f : p.scale_log2;
-    const int jstep = kDecoded ? 1 : 2;
     const bool fixed = kCap && p.cap_ref != -INFINITY;
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
-    const int jend = kDecoded && stream == 1 && !two_tiles ? 0 : nt;
     int i = 0;   // the stream's step
-    for (int j = kDecoded ? 0 : stream; j < jend; j += jstep, ++i) {
+    for (int j = stream; j < nt; j += 2, ++i) {
       ok = warp_wait(&ctl.s_full[stream], i & 1, &ctl.abort);
       if (!ok) break;
       tc_fence_after_sync();
@@ -617,65 +739,16 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
         mbar_arrive(&ctl.p_full[stream]);
         continue;
       }
-      uint32_t raw[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, raw[c]);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld_wait(raw[c]);
-      float* s = reinterpret_cast<float*>(&raw[0][0]);
-      const uint4 nan4 = kDecoded ? make_uint4(0, 0, 0, 0) : ctl.nan_keys[j & 3];
-      const bool nans = (nan4.x | nan4.y | nan4.z | nan4.w) != 0;
-      const bool edge = __any_sync(0xffffffffu, valid && (cl > 0 || ch < kBN));
+      const uint32_t* nan = reinterpret_cast<const uint32_t*>(&ctl.nan_keys[j & 3]);
       const bool own_column = warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kBN);
-      // capped scores: by the polynomial where the warp's are all small and none is masked, else one by one
-      bool small = false;
-      if (kCap) {
-        if (fixed && !(nans || edge || own_column)) {
-          float hi[4] = {};
-#pragma unroll
-          for (int c = 0; c < kBN; c += 8)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) hi[e] = fmax3(hi[e], fabsf(s[c + 2 * e]), fabsf(s[c + 2 * e + 1]));
-          small = __all_sync(0xffffffffu, fmax3(hi[0], hi[1], fmaxf(hi[2], hi[3])) * p.cap_x <= kTanhRange || !valid);
-        }
-        if (!small) {
-#pragma unroll
-          for (int c = 0; c < kBN; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
-        }
-      }
-      if (nans) {
-        const uint32_t nw[4] = {nan4.x, nan4.y, nan4.z, nan4.w};
-#pragma unroll
-        for (int c = 0; c < kBN; ++c)
-          if ((nw[c >> 5] >> (c & 31)) & 1u) s[c] = __uint_as_float(0x7fc00000u);
-      }
-      if (edge) {
-#pragma unroll
-        for (int c = 0; c < kBN; ++c)
-          if (c < cl || c >= ch) s[c] = -INFINITY;
-      }
-      if (own_column) {
-        // a seed row does not see its own cached column
-        const int dc = is_seed ? pos - key0 : -1;
-#pragma unroll
-        for (int c = 0; c < kBN; ++c)
-          if (c == dc) s[c] = -INFINITY;
-      }
+      const Unseen u{cl, ch, is_seed ? pos - key0 : -1, own_column || __any_sync(0xffffffffu, valid && (cl > 0 || ch < kBN))};
       float alpha = 1.0f;
       bool rescaled = false;
       if (!fixed) {
-        // row maximum: four independent 3-input max chains
-        float mx0 = s[0], mx1 = s[1], mx2 = s[2], mx3 = s[3];
-#pragma unroll
-        for (int c = 4; c + 8 <= kBN; c += 8) {
-          mx0 = fmax3(mx0, s[c], s[c + 1]);
-          mx1 = fmax3(mx1, s[c + 2], s[c + 3]);
-          mx2 = fmax3(mx2, s[c + 4], s[c + 5]);
-          mx3 = fmax3(mx3, s[c + 6], s[c + 7]);
-        }
-        mx0 = fmax3(mx0, s[kBN - 4], s[kBN - 3]);
-        mx1 = fmax3(mx1, s[kBN - 2], s[kBN - 1]);
-        const float m_tile = fmax3(mx0, mx1, fmaxf(mx2, mx3)) * scale;
+        float m_tile = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < kBN; c += 32) m_tile = fmaxf(m_tile, chunk_max(s_addr + c, p, u, nan[c >> 5], c));
+        m_tile = reference_of<kCap>(m_tile, p);
         if (m_tile > m_run + kRescaleThreshold) {
           alpha = (m_run == -INFINITY) ? 0.0f : ex2_approx(m_run - m_tile);
           m_run = m_tile;
@@ -683,51 +756,10 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
         }
       }
       const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
-      // p = 2^(s * scale - m) on pairs; four independent partial row sums
-      const uint64_t scale2 = f2_pack(scale, scale);
-      const uint64_t negm2 = f2_pack(-m_use, -m_use);
-      uint64_t acc2[4] = {0, 0, 0, 0};
-      if (kCap && small) {
-        // C x P(x^2) with x = s cap_x, the powers of cap_x in the coefficients
-        const float xx = p.cap_x * p.cap_x, k0 = kTanh0 * p.cap_log2 * p.cap_x, k1 = kTanh1 * p.cap_log2 * p.cap_x * xx,
-                    k2 = kTanh2 * p.cap_log2 * p.cap_x * xx * xx, k3 = kTanh3 * p.cap_log2 * p.cap_x * xx * xx * xx;
-        const uint64_t t0 = f2_pack(k0, k0), t1 = f2_pack(k1, k1), t2 = f2_pack(k2, k2), t3 = f2_pack(k3, k3);
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t packed[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const uint64_t x = f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]);
-            const uint64_t z = f2_mul(x, x);
-            float x0, x1;
-            f2_unpack(f2_fma(x, f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0), negm2), x0, x1);
-            const float e0 = ex2_approx(x0);
-            const float e1 = ex2_approx(x1);
-            packed[c] = pack_bf16x2(e0, e1);
-            acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
-          }
-          tmem_st32(s_addr + 32 * hf, packed);
-        }
-      } else {
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t packed[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            float x0, x1;
-            f2_unpack(f2_fma(f2_pack(s[64 * hf + 2 * c], s[64 * hf + 2 * c + 1]), scale2, negm2), x0, x1);
-            const float e0 = ex2_approx(x0);
-            const float e1 = ex2_approx(x1);
-            packed[c] = pack_bf16x2(e0, e1);
-            acc2[c & 3] = f2_add(acc2[c & 3], f2_pack(e0, e1));
-          }
-          tmem_st32(s_addr + 32 * hf, packed);
-        }
-      }
-      float rs[4];
-      f2_unpack(f2_add(acc2[0], acc2[1]), rs[0], rs[1]);
-      f2_unpack(f2_add(acc2[2], acc2[3]), rs[2], rs[3]);
-      l_run = l_run * alpha + ((rs[0] + rs[1]) + (rs[2] + rs[3]));
+      l_run *= alpha;
+#pragma unroll 1
+      for (int c = 0; c < kBN; c += 32)
+        l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, nan[c >> 5], c, m_use, fixed, valid);
       if (i > 0 && __any_sync(0xffffffffu, rescaled)) {
         // O holds the stream's earlier products (complete: the commit of this S came after them)
 #pragma unroll 1
@@ -753,21 +785,16 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
     // ---------------- the rows' results ----------------
     // of the thread's row: the sums of the streams that worked on it, and the accumulators' weights
     tc_fence_after_sync();
-    float m = m_run, l = l_run, w[2] = {1.0f, 1.0f};
     const uint32_t o0 = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 2 * kBN;
-    int c0 = 0, c1 = 4;   // 32-column chunks that this thread finishes
-    if (!kDecoded) {
-      float2* ml = reinterpret_cast<float2*>(sm_q);   // every product is complete: Q is not read any more
-      if (ok) ml[stream * kBM + R] = make_float2(m_run, l_run);
-      softmax_sync();
-      const float2 a = ml[R], c = ml[kBM + R];
-      m = fmaxf(a.x, c.x);
-      const float m_use = m == -INFINITY ? 0.0f : m;
-      w[0] = a.x == -INFINITY ? 0.0f : ex2_approx(a.x - m_use);
-      w[1] = c.x == -INFINITY ? 0.0f : ex2_approx(c.x - m_use);
-      l = w[0] * a.y + w[1] * c.y;
-      c0 = 2 * stream, c1 = c0 + 2;
-    }
+    float2* ml = reinterpret_cast<float2*>(sm.q);   // every product is complete: Q is not read any more
+    if (ok) ml[stream * kBM + R] = make_float2(m_run, l_run);
+    softmax_sync();
+    const float2 ml0 = ml[R], ml1 = ml[kBM + R];
+    float m = fmaxf(ml0.x, ml1.x);
+    const float m_use = m == -INFINITY ? 0.0f : m;
+    float w[2] = {ml0.x == -INFINITY ? 0.0f : ex2_approx(ml0.x - m_use), ml1.x == -INFINITY ? 0.0f : ex2_approx(ml1.x - m_use)};
+    float l = w[0] * ml0.y + w[1] * ml1.y;
+    const int c0 = 2 * stream;   // the first of two 32-column chunks that this thread finishes
     const float m_all = fmaxf(m, s_self);
     float p_self = 0.0f;
     if (s_self != -INFINITY) {
@@ -778,22 +805,21 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
       m = m_all;
     }
     if (s_self != s_self) l = s_self;   // NaN in the masked-input pair
-    const bool self_here = __any_sync(0xffffffffu, p_self != 0.0f);
     const long long orow = rowbase + P;
     const bool split = p.nsplit > 1;
     // 1 / l, once a row; zero where no key was seen
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
     if (ok && warp_live) {
 #pragma unroll 1
-      for (int c = c0; c < c1; ++c) {
+      for (int c = c0; c < c0 + 2; ++c) {
         float o[32];
         if (nt > 0) {
           uint32_t x[32];
-          tmem_ld32((kDecoded ? o_addr : o0) + 32 * c, x);
+          tmem_ld32(o0 + 32 * c, x);
           tmem_ld_wait(x);
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = w[0] == 0.0f ? 0.0f : __uint_as_float(x[e]) * w[0];
-          if (!kDecoded && nt > 1) {
+          if (nt > 1) {
             tmem_ld32(o0 + kD + 32 * c, x);
             tmem_ld_wait(x);
 #pragma unroll
@@ -803,31 +829,8 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.0f;
         }
-        if (self_here && p_self != 0.0f) {
-          const uint4* vr = reinterpret_cast<const uint4*>(p.v_seedmask + self * kD + 32 * c);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint4 a = __ldg(vr + e);
-            const uint32_t x[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              o[8 * e + 2 * f] = fmaf(p_self, __uint_as_float(x[f] << 16), o[8 * e + 2 * f]);
-              o[8 * e + 2 * f + 1] = fmaf(p_self, __uint_as_float(x[f] & 0xffff0000u), o[8 * e + 2 * f + 1]);
-            }
-          }
-        }
-        if (valid && split) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(ks) * p.rows + orow) * kD + 32 * c);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-        } else if (valid) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kD + 32 * c);
-          // a NaN sum makes the whole row NaN
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
-        }
+        if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + 32 * c);
+        if (valid) store_chunk(p, o, inv, split, ks, orow, 32 * c);
         __syncwarp();   // the next chunk is loaded by the whole warp
       }
       if (valid && c0 == 0) {
@@ -839,6 +842,334 @@ __global__ void __launch_bounds__(kDecoded ? kReadThreads : kThreads, 1)
   }
   __syncthreads();
   if (warp == kMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tbase, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows
+// ---------------------------------------------------------------------------
+// A memory that many Q tiles read is decoded once, into the workspace (a row whose K or V is NaN has a NaN key and a zero
+// value there), and a CTA takes two Q tiles, one a stream, that read each KV tile together. Two threads of different
+// warpgroups share a row, 64 columns each, in two chunks of 32. 2048 rows over 8192 keys, 32 / 8 heads: 240 us, capped
+// at 30 283 (8 us of them decode the memory); 1216 rows, which fill the GPU's 152 SMs once, 124 us, 1310 TFLOP/s. With a thread
+// a row and its 128 columns unrolled it was 235 and 333 us: see finish_scores.
+// Roles (640 threads): warps 0-15 softmax (warpgroup 2 t + h: columns 64 h .. 64 h + 63 of Q tile t); 16 products; 17, 18
+// copies of K, V.
+// P of a half overwrites the first 32 columns of that half's scores, behind its loads.
+constexpr int kPairSoftmaxWarps = 16, kPairMmaWarp = 16, kPairLoadWarp = 17;
+
+struct PairSmem {
+  uint8_t q[2][kTileBytes];
+  uint8_t k[2][kTileBytes];
+  uint8_t v[2][kTileBytes];
+  Ctl ctl;
+  float red[2][2][kBM];                 // per Q tile and half of the columns
+  int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
+};
+
+// Copies K (which = 0) or V (1) of KV tiles j0 .. j0 + nt - 1, decoded already, into the two bf16 tiles in turn; one thread.
+__device__ __forceinline__ void copy_tiles(Ctl& ctl, const Params& p, int which, const CUtensorMap* tm, uint8_t* tiles, int hkv,
+                                           int b, int j0, int nt) {
+  uint64_t* const full = which ? ctl.v_full : ctl.k_full;
+  uint64_t* const empty = which ? ctl.v_empty : ctl.k_empty;
+  int j = 0;
+  bool ok = true;
+  for (; j < nt; ++j) {
+    const int st = j & 1;
+    if (j >= 2) ok = mbar_wait(&empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
+    if (!ok) break;
+    mbar_arrive_expect_tx(&full[st], kTileBytes);
+    for (int h = 0; h < 2; ++h)
+      tma_load_4d(tiles + st * kTileBytes + h * kBoxBytes, tm, &full[st], 64 * h, (j0 + j) * kBN, hkv, b);
+  }
+  if (!ok) {
+    if (!ctl.abort) report_status(p.status, kStatusTimeout, 76);
+    ctl.abort = 1;
+  }
+  // every copy lands before the CTA's shared memory is released, whatever the other roles did
+  if (which == 0) mbar_wait(&ctl.q_full, 0, nullptr);
+  for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&full[f & 1], (f >> 1) & 1, nullptr);
+}
+
+template <bool kCap>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_prefix8_pairs_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                              const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  PairSmem& sm = *reinterpret_cast<PairSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Ctl& ctl = sm.ctl;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // CTA (ks, group, hkv, b)
+  const int ks = static_cast<int>(blockIdx.x) % p.nsplit;
+  int rest = static_cast<int>(blockIdx.x) / p.nsplit;
+  const int group = rest % p.n_groups;
+  rest /= p.n_groups;
+  const int hkv = rest % p.Hkv;
+  const int b = rest / p.Hkv;
+  const int n_packed = p.G * p.Lq;
+  const int p0 = group * 2 * kBM;
+  const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
+
+  if (warp == kPairMmaWarp) set_up(ctl, &tm_q, 1, 256);
+  if (p.n_seeds > 0 && tid < 2 * kBM) sm.slot[tid] = kNoSlot;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tbase = ctl.tmem_base;
+  griddep_wait();
+  griddep_launch_dependents();
+
+  // ---------------- the rows' keys ----------------
+  const int tile = warp >> 3, half = (warp >> 2) & 1;   // of a softmax warp
+  const int R = tid & (kBM - 1);
+  const int P = p0 + tile * kBM + R;
+  const bool valid = warp < kPairSoftmaxWarps && P < n_packed;
+  const int r = valid ? P % p.Lq : 0;
+  int row_lo = 0, row_hi = p.Lk;
+  if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
+  if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
+  int lo_key = 0, hi_key = p.Lk;                        // keys that some row sees
+  if (p.key_lo != nullptr || p.key_hi != nullptr) {
+    if (warp < kPairSoftmaxWarps) {
+      const bool some = valid && row_lo < row_hi;
+      const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff);
+      const int hi = __reduce_max_sync(0xffffffffu, some ? row_hi : 0);
+      if (lane == 0 && hi > 0) {
+        atomicMin(&ctl.lo, lo);
+        atomicMax(&ctl.hi, hi);
+      }
+    }
+    __syncthreads();
+    lo_key = ctl.lo, hi_key = ctl.hi;
+  }
+  const Part part = part_of(lo_key, hi_key, ks, p.nsplit);
+  const int j0 = part.j0, nt = part.nt;
+  const bool two_tiles = p0 + kBM < n_packed;           // the second Q tile has rows
+
+  if (warp >= kPairMmaWarp) {
+    if ((warp == kPairLoadWarp || warp == kPairLoadWarp + 1) && lane == 0 && nt > 0) {
+      const int which = warp - kPairLoadWarp;
+      if (which == 0) {
+        mbar_arrive_expect_tx(&ctl.q_full, 2 * kTileBytes);
+        for (int t = 0; t < 2; ++t)
+          for (int h = 0; h < 2; ++h)
+            tma_load_4d(sm.q[t] + h * kBoxBytes, &tm_q, &ctl.q_full, 64 * h, static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
+      }
+      copy_tiles(ctl, p, which, which ? &tm_v : &tm_k, which ? sm.v[0] : sm.k[0], hkv, b, j0, nt);
+    } else if (warp == kPairMmaWarp && lane == 0 && nt > 0) {
+      // ---------------- products ----------------
+      constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
+      constexpr uint32_t id_pv = idesc_bf16_f32(kBM, kD, false, true);
+      constexpr uint64_t kTileDesc = kTileBytes >> 4;
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
+      const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
+      // S[s] = Q[s] . K(stage)^T
+      auto issue_s = [&](int s, int st) {
+        uint64_t a = dq + s * kTileDesc, kb = dk + st * kTileDesc;
+        asm volatile("" : "+l"(a), "+l"(kb));   // descriptors are added up here, not kept in registers
+#pragma unroll
+        for (int kk = 0; kk < kD / 16; ++kk) {
+          const uint64_t off = static_cast<uint64_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
+          umma_ss(tbase + s * kBN, a + off, kb + off, id_qk, kk > 0 ? 1u : 0u);
+        }
+        umma_commit(&ctl.s_full[s]);
+      };
+      // O[s] (+)= P[s] . V(stage)
+      auto issue_pv = [&](int s, int st, bool acc) {
+        uint64_t vb = dv + st * kTileDesc;
+        asm volatile("" : "+l"(vb));
+#pragma unroll
+        for (int kk = 0; kk < kBN / 16; ++kk)
+          umma_ts(tbase + 2 * kBN + s * kD, tbase + s * kBN + (kk >> 2) * kHalf + 8 * (kk & 3),
+                  vb + static_cast<uint64_t>((kk * 2048) >> 4), id_pv, (acc || kk > 0) ? 1u : 0u);
+      };
+      auto wait = [&](uint64_t* bar, int phase) {
+        const bool ok = mbar_wait(bar, phase & 1, &ctl.abort);
+        if (ok) tc_fence_after_sync();
+        return ok;
+      };
+      bool ok = wait(&ctl.q_full, 0);
+      if (ok && (ok = wait(&ctl.k_full[0], 0))) {
+        issue_s(0, 0);
+        if (two_tiles) issue_s(1, 0);
+        umma_commit(&ctl.k_empty[0]);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int st = j & 1;
+        const bool next = j + 1 < nt;
+        ok = wait(&ctl.p_full[0], j) && wait(&ctl.v_full[st], j >> 1);
+        if (!ok) break;
+        issue_pv(0, st, j > 0);
+        if (next) {
+          ok = wait(&ctl.k_full[st ^ 1], (j + 1) >> 1);
+          if (!ok) break;
+          issue_s(0, st ^ 1);
+        }
+        if (two_tiles) {
+          ok = wait(&ctl.p_full[1], j);
+          if (!ok) break;
+          issue_pv(1, st, j > 0);
+          if (next) issue_s(1, st ^ 1);
+        }
+        umma_commit(&ctl.v_empty[st]);
+        if (next) umma_commit(&ctl.k_empty[st ^ 1]);
+      }
+      if (ok) {
+        umma_commit(&ctl.o_full);
+      } else {
+        if (!ctl.abort) report_status(p.status, kStatusTimeout, 77);
+        ctl.abort = 1;
+      }
+      // all tensor-core work of this CTA completes before tensor memory is released
+      umma_commit(&ctl.drain);
+      mbar_wait(&ctl.drain, 0, nullptr);
+    }
+    __syncwarp();
+  } else {
+    // ---------------- softmax ----------------
+    int slot = kNoSlot;
+    if (p.n_seeds > 0) {
+      // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
+      const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
+      const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
+      for (int s = tid; s < p.n_seeds; s += 4 * kBM) {
+        const int at = __ldg(seeds + s) - p.q0;
+        if (at < 0 || at >= p.Lq) continue;
+        const int i = at >= r0 ? at - r0 : at - r0 + p.Lq;
+        if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
+      }
+      asm volatile("bar.sync 1, 512;" ::: "memory");   // all softmax threads
+      if (valid) slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
+    }
+    const int pos = p.q0 + r;
+    const bool is_seed = slot != kNoSlot;
+    const bool warp_seed = __any_sync(0xffffffffu, is_seed);
+    const size_t self = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds + (is_seed ? slot : 0);
+    const float s_self = ks == 0 && is_seed && pos >= row_lo && pos < row_hi
+                             ? self_score<kCap>(p, rowbase + P, self) : -INFINITY;
+    const bool warp_live = __any_sync(0xffffffffu, valid);
+    const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_addr = quad + tile * kBN + half * kHalf;
+    const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
+    const bool fixed = kCap && p.cap_ref != -INFINITY;
+    float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
+    bool ok = true;
+    const int jend = tile == 1 && !two_tiles ? 0 : nt;
+    for (int j = 0; j < jend; ++j) {
+      ok = warp_wait(&ctl.s_full[tile], j & 1, &ctl.abort);
+      const int key0 = (j0 + j) * kBN + half * kHalf;
+      const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch of this half are seen
+      // (a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything)
+      const bool some = __any_sync(0xffffffffu, valid && max(cl, 0) < min(ch, kHalf));
+      const bool own_column = warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kHalf);
+      const Unseen u{cl, ch, is_seed ? pos - key0 : -1, own_column || __any_sync(0xffffffffu, valid && (cl > 0 || ch < kHalf))};
+      float m_half = -INFINITY;
+      if (ok && some) {
+        tc_fence_after_sync();
+        if (!fixed) {
+#pragma unroll 1
+          for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, 0, c));
+          m_half = reference_of<kCap>(m_half, p);
+        }
+      }
+      if (fixed && !ok) break;
+      // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row
+      // take the same reference
+      if (!fixed && tile_any(tile, !ok || (valid && m_half > m_run + kRescaleThreshold))) {
+        if (tile_any(tile, !ok)) {
+          ok = false;
+          break;
+        }
+        sm.red[tile][half][R] = m_half;
+        tile_sync(tile);
+        const float top = fmaxf(sm.red[tile][0][R], sm.red[tile][1][R]);
+        float alpha = 1.0f;
+        if (top > m_run + kRescaleThreshold) {
+          alpha = m_run == -INFINITY ? 0.0f : ex2_approx(m_run - top);
+          m_run = top;
+        }
+        l_run *= alpha;
+        if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+          // O holds the tile's earlier products (complete: the commit of this S came after them)
+          tc_fence_after_sync();
+#pragma unroll 1
+          for (int c = 0; c < 2; ++c) {
+            uint32_t o[32];
+            tmem_ld32(o_addr + 32 * c, o);
+            tmem_ld_wait(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(o_addr + 32 * c, o);
+          }
+        }
+      }
+      if (some) {
+        const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
+#pragma unroll 1
+        for (int c = 0; c < kHalf; c += 32)
+          l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, 0, c, m_use, fixed, valid);
+      } else if (warp_live) {
+        const uint32_t zeros[16] = {};
+        tmem_st16(s_addr, zeros);
+        tmem_st16(s_addr + 16, zeros);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      mbar_arrive(&ctl.p_full[tile]);
+    }
+    if (ok && nt > 0) ok = warp_wait(&ctl.o_full, 0, &ctl.abort);
+    if (!ok && lane == 0) {
+      if (!ctl.abort) report_status(p.status, kStatusTimeout, 78);
+      ctl.abort = 1;
+    }
+
+    // ---------------- the rows' results ----------------
+    tc_fence_after_sync();
+    tile_sync(tile);                      // the last references have been read
+    sm.red[tile][half][R] = l_run;
+    tile_sync(tile);
+    float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
+    if (s_self != -INFINITY) {
+      const float m_all = fmaxf(m, s_self);
+      w = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
+      p_self = ex2_approx(s_self - m_all);
+      l = l * w + p_self;
+      m = m_all;
+    }
+    if (s_self != s_self) l = s_self;   // NaN in the masked-input pair
+    const long long orow = rowbase + P;
+    const bool split = p.nsplit > 1;
+    // 1 / l, once a row; zero where no key was seen
+    const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
+    if (ok && warp_live) {
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {
+        float o[32] = {};
+        if (nt > 0) {
+          uint32_t x[32];
+          tmem_ld32(o_addr + 32 * c, x);
+          tmem_ld_wait(x);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = w == 0.0f ? 0.0f : __uint_as_float(x[e]) * w;
+        }
+        const int col = half * kHalf + 32 * c;
+        if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + col);
+        if (valid) store_chunk(p, o, inv, split, ks, orow, col);
+        __syncwarp();   // the next chunk is loaded by the whole warp
+      }
+      if (valid && half == 0) {
+        if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
+        else if (p.lse != nullptr) p.lse[orow] = (m + lg2_approx(l)) * 0.6931471805599453f;
+      }
+    }
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  if (warp == kPairMmaWarp) {
     tc_fence_after_sync();
     tmem_dealloc(tbase, 512);
   }
@@ -874,29 +1205,6 @@ constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsLoadWarp = 13;
 constexpr float kRowsThreshold = 2.0f;  // log2 units, of the references' changes
 constexpr float kPBits = 12.0f;         // P' carries 2^12 (and is at most 2^14, below fp16's largest)
 constexpr int kEvFloor = -90;
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-// Completes the warp's loads; the registers pass through so that none is used before.
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 
 // D[tmem] (+)= A[smem] . B[smem] of 8-bit operands
 __device__ __forceinline__ void umma_ss_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
@@ -1584,10 +1892,13 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
   return best;
 }
 
-using TileKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
 using RowsKernel = void (*)(const CUtensorMap, const CUtensorMap, const Params);
-constexpr TileKernel kTileKernels[2][2] = {{attn_prefix8_kernel<false, false>, attn_prefix8_kernel<false, true>},
-                                           {attn_prefix8_kernel<true, false>, attn_prefix8_kernel<true, true>}};
+using TileKernel = void (*)(const CUtensorMap, const Params);
+using PairKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
+constexpr TileKernel kTileKernels[2] = {attn_prefix8_tile_kernel<false>, attn_prefix8_tile_kernel<true>};
+constexpr PairKernel kPairKernels[2] = {attn_prefix8_pairs_kernel<false>, attn_prefix8_pairs_kernel<true>};
+constexpr size_t kPairSmemBytes = sizeof(PairSmem) + 1024;
+static_assert(kPairSmemBytes <= 227 * 1024, "shared memory of a CTA");
 constexpr RowsKernel kRowsKernels[2][2] = {{attn_prefix8_rows_kernel<16, false>, attn_prefix8_rows_kernel<16, true>},
                                            {attn_prefix8_rows_kernel<32, false>, attn_prefix8_rows_kernel<32, true>}};
 constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSmem<32>) + 1024};
@@ -1652,19 +1963,21 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   static ContextCache<int> setup;
   int unused = 0;
   const int rc = setup.get(&unused, [&](int&) {
-    for (int m = 0; m < 2; ++m)
-      for (int c = 0; c < 2; ++c) {
-        if (cudaFuncSetAttribute(kRowsKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(kRowsSmemBytes[m])) != cudaSuccess ||
-            cudaFuncSetAttribute(kTileKernels[m][c], cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(kSmemBytes)) != cudaSuccess)
-          return -3;
-        // the register splits inside the kernels assume exactly these counts per thread at launch; any
-        // other could leave setmaxnreg.inc waiting, so refuse to launch
-        cudaFuncAttributes fa;
-        if (cudaFuncGetAttributes(&fa, kTileKernels[m][c]) != cudaSuccess || fa.numRegs != (m ? kReadLaunchRegs : kLaunchRegs))
-          return -2;
-      }
+    const auto limit = [](auto fn, size_t smem) {
+      return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+    };
+    // the register split inside the tile kernel assumes exactly kLaunchRegs per thread at launch; any other
+    // count could leave setmaxnreg.inc waiting, so refuse to launch
+    const auto registers = [](auto fn) {
+      cudaFuncAttributes fa;
+      return cudaFuncGetAttributes(&fa, fn) == cudaSuccess && fa.numRegs == kLaunchRegs;
+    };
+    for (int c = 0; c < 2; ++c) {
+      for (int m = 0; m < 2; ++m)
+        if (!limit(kRowsKernels[m][c], kRowsSmemBytes[m])) return -3;
+      if (!limit(kTileKernels[c], kSmemBytes) || !limit(kPairKernels[c], kPairSmemBytes)) return -3;
+      if (!registers(kTileKernels[c])) return -2;
+    }
     return 0;
   });
   if (rc != 0) return rc;
@@ -1710,6 +2023,9 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.cap_in = cap ? 2.0f * log2e / (a.softcap * root) : 0.0f;
   p.cap_x = cap ? 1.0f / (a.softcap * root) : 0.0f;
   p.cap_ref = cap ? fixed_reference(p.cap_log2) : -INFINITY;
+  const float tanh_poly[4] = {kTanh0, kTanh1, kTanh2, kTanh3};
+  float power = p.cap_log2 * p.cap_x;
+  for (int i = 0; i < 4; ++i, power *= p.cap_x * p.cap_x) p.cap_poly[i] = p.cap_ref != -INFINITY ? tanh_poly[i] * power : 0.0f;
   cudaLaunchAttribute attr[1];
   const dim3 ctas(static_cast<unsigned>(grid));
   cudaLaunchConfig_t cfg;
@@ -1719,8 +2035,9 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
     cfg = pdl_config(ctas, dim3(kRowsThreads), kRowsSmemBytes[m], stream, attr);
     e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], tk, tv, p);
   } else {
-    cfg = pdl_config(ctas, dim3(decoded ? kReadThreads : kThreads), kSmemBytes, stream, attr);
-    e = cudaLaunchKernelEx(&cfg, kTileKernels[decoded ? 1 : 0][cap ? 1 : 0], tq, tk, tv, p);
+    cfg = pdl_config(ctas, dim3(kThreads), decoded ? kPairSmemBytes : kSmemBytes, stream, attr);
+    e = decoded ? cudaLaunchKernelEx(&cfg, kPairKernels[cap ? 1 : 0], tq, tk, tv, p)
+                : cudaLaunchKernelEx(&cfg, kTileKernels[cap ? 1 : 0], tq, p);
   }
   if (e == cudaSuccess && plan.nsplit > 1) {
     cfg = pdl_config(dim3(static_cast<unsigned>((rows + kCombineWarps - 1) / kCombineWarps)), dim3(kCombineWarps * 32), 0,
