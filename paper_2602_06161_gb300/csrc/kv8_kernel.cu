@@ -34,6 +34,7 @@ struct Kv8Params {
   const int32_t* pos;        // [B, n] or null
   int pos0, n, L, Hkv;
   int heads;                 // heads of a CTA
+  int tiles, groups;         // of slots, and of heads
 };
 
 template <typename T>
@@ -96,7 +97,8 @@ struct Codes<4> {
 };
 
 // CTA of kSlots slots, of p.heads heads one after the other. Rows to be written mostly come from a projection, where a
-// token's heads are neighbours, so the heads' CTAs are neighbours too; rows read lie by heads on both sides.
+// token's heads are neighbours, so the heads' CTAs of a tile of slots are neighbours too; rows read lie by heads on both
+// sides.
 enum Kv8 { kRead, kWriteRows, kDecode };
 
 // kDecode: reads, and a row whose K or V is NaN gets a NaN key and a zero value (an attention kernel's weight of
@@ -113,9 +115,10 @@ __global__ void __launch_bounds__(kThreads, 6) kv8_kernel(const __grid_constant_
   griddep_wait();
   griddep_launch_dependents();
   const int tid = threadIdx.x;
-  const int b = blockIdx.z;
-  const int slot0 = static_cast<int>(kWrite ? blockIdx.y : blockIdx.x) * kSlots;
-  const int head_group = static_cast<int>(kWrite ? blockIdx.x : blockIdx.y);
+  const int b = blockIdx.y;
+  const int cta = blockIdx.x;
+  const int slot0 = (kWrite ? cta / p.groups : cta % p.tiles) * kSlots;
+  const int head_group = kWrite ? cta % p.groups : cta / p.tiles;
   const int32_t* list = p.pos == nullptr ? nullptr : p.pos + static_cast<size_t>(b) * p.n;
   for (int i = tid; i < kSlots; i += kThreads) {
     const int s = slot0 + i;
@@ -238,16 +241,17 @@ int launch(Kv8Params p, int B, Kv8 kind, cudaStream_t stream) {
   const bool write = kind == kWriteRows;
   constexpr int kSlots = kThreads / (D / Wide<T>::kN) * kTok;
   const long long tiles = (p.n + kSlots - 1) / kSlots;
-  if (B > 65535) return -2;
+  if (B > 65535 || p.n > 0x7fffffff - kSlots) return -2;
   // A CTA takes one head; with a list to search for repeats, as many as leave the GPU about two waves
   // of CTAs, so that the search is not made again for each head.
   long long groups = p.Hkv;
   if (write && p.pos != nullptr) groups = std::min<long long>(p.Hkv, std::max<long long>(1, 2 * 152 * 4 / (tiles * B)));
   p.heads = static_cast<int>((p.Hkv + groups - 1) / groups);
   groups = (p.Hkv + p.heads - 1) / p.heads;
-  if ((write ? tiles : groups) > 65535) return -2;
-  const unsigned x = static_cast<unsigned>(tiles), y = static_cast<unsigned>(groups);
-  const dim3 grid(write ? y : x, write ? x : y, static_cast<unsigned>(B));
+  if (tiles * groups > 0x7fffffffLL) return -2;
+  p.tiles = static_cast<int>(tiles);
+  p.groups = static_cast<int>(groups);
+  const dim3 grid(static_cast<unsigned>(tiles * groups), static_cast<unsigned>(B));
   cudaLaunchAttribute attr[1];
   const cudaLaunchConfig_t cfg = pdl_config(grid, dim3(kThreads), 0, stream, attr);
   cudaError_t e;
@@ -293,11 +297,15 @@ int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
 int launch_kv8_decode(const Kv8Args& a, cudaStream_t stream) {
   using bf16 = __nv_bfloat16;
   constexpr int kSlots = kThreads / (128 / Wide<bf16>::kN) * kTok;
-  if (a.B > 65535 || a.Hkv > 65535) return -2;
-  const dim3 grid(static_cast<unsigned>((a.n + kSlots - 1) / kSlots), static_cast<unsigned>(a.Hkv), static_cast<unsigned>(a.B));
+  Kv8Params p = params_of(a, false);
+  const long long tiles = (a.n + kSlots - 1) / kSlots;
+  if (a.B > 65535 || tiles * a.Hkv > 0x7fffffffLL) return -2;
+  p.tiles = static_cast<int>(tiles);
+  p.groups = a.Hkv;
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = pdl_config(grid, dim3(kThreads), 0, stream, attr);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv8_kernel<bf16, 128, kDecode>, params_of(a, false));
+  const cudaLaunchConfig_t cfg =
+      pdl_config(dim3(static_cast<unsigned>(tiles * a.Hkv), static_cast<unsigned>(a.B)), dim3(kThreads), 0, stream, attr);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv8_kernel<bf16, 128, kDecode>, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
