@@ -322,13 +322,19 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  *     those before, documents. A row that sees no key gets out = 0, lse = -inf.
  *     A seed row's own pair is seen where its position is.
  *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c).
- * What a row does not see does not reach it, NaN included; a row that sees a key with
- * k_exp or v_exp 255 gets NaN in out and lse.
+ * What a row does not see does not reach it, NaN included; a row that sees a key with k_exp or
+ * v_exp above 246 gets NaN in out and lse. (A NaN code, 0x7f or 0xff, which cover_kv8_write does
+ * not write, counts as NaN or as 480 where it is seen.)
+ * Which kernel runs depends on the sizes; equal rows of different calls agree up to rounding. The
+ * weights are rounded to bf16 or to 9 significant bits for their products with V, and a weight that
+ * is, times its value's scale, below 2^-28 of the row's largest such product may count as zero in
+ * out (not in lse).
  * workspace: cover_attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) bytes, 16-byte aligned, no initialisation
  * needed (NULL if that is 0). It is scratch of the call alone: calls that share one must not
  * run concurrently on the GPU.
- * Errors as cover_attn_fwd_prefix, plus COVER_ERR_INVALID_ARG for NULL k_exp or v_exp, a missing
- * workspace, and a softcap that is negative or not finite.
+ * The inputs must not alias out, lse or workspace. Errors as cover_attn_fwd_prefix, plus
+ * COVER_ERR_INVALID_ARG for NULL k_exp or v_exp, a missing workspace, and a softcap that is
+ * negative or not finite.
  */
 size_t cover_attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk);
 int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8,

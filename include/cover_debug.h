@@ -136,8 +136,8 @@ int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int pl
  * call fails). Site ids of the bf16 attention kernel: 10 TMA thread, 20 MMA
  * thread, 30 / 31 softmax warpgroup of Q tile 0 / 1, 40 routing warp,
  * 50 / 51 seed-score warp; of the packed window kernel: 60 TMA / MMA thread,
- * 61 softmax warps, 62 combine (receive barrier), 63 copy issue; of the 8-bit memory's kernels: 70, 76 copies,
- * 71, 74 MMA thread, 72 decoding or screening warps, 73, 75 softmax warps.
+ * 61 softmax warps, 62 combine (receive barrier), 63 copy issue; of the 8-bit memory's kernels:
+ * 70, 76 copies, 71, 74, 77 MMA thread, 72 decoding or screening warps, 73, 75, 78 softmax warps.
  */
 int cover_debug_status_detail(int32_t* detail, void* stream);
 

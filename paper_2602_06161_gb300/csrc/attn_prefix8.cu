@@ -20,8 +20,8 @@
 // (exact: a row's scale is a power of two) into the swizzled layout that the tensor cores read, and S = Q K^T, O += P V run as
 // tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each: the even and the odd KV
 // tiles, with sums and an accumulator of their own that are merged at the end, so that the chain load - decode - S - softmax -
-// P V of one KV tile overlaps the next one's. A KV tile takes 1.3 us, of which decoding (two instructions a code, 192 KB
-// through shared memory) is the most: without it 0.9 us, without the softmax 1.0.
+// P V of one KV tile overlaps the next one's. A KV tile takes 1.34 us; the most of it is decoding: two instructions a
+// code, and the 192 KB a tile that it and the products move through shared memory take 0.8 us at 128 bytes a clock.
 // Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16 issues the
 // products; 17 and 18 the copies of K and V.
 // Shared memory: Q (32 KB) | two tiles of K and of V codes (16 KB each) | K, V in bf16 (2 x 32 KB each).
@@ -1850,10 +1850,11 @@ constexpr int kClusters[8] = {152, 76, 48, 36, 28, 24, 20, 18};
 
 // The kernel and the parts of the keys. plain: no key ranges, no cap.
 //
-// Predicted microseconds, fitted to 433 calls back to back on GB300 (24 windows of 1 to 1024 rows over 300 to 20000
-// keys, batches of 1 to 16, 1 to 64 parts; off by 4 to 5 %, at most 26 %): a base, and for every wave of one CTA an SM a
-// start and a time per KV tile; where the keys are in parts, the second kernel's start, its walk over the parts, and
-// the parts' rows. Decoding a memory takes 1e-4 us a row.
+// Predicted microseconds, fitted to 409 calls back to back on GB300 (24 windows of 1 to 1024 rows over 300 to 20000
+// keys, batches of 1 to 16, 1 to 64 parts; off by 3 to 6 % in the mean, at most 30 %): a base, and for every wave of one
+// CTA an SM a start and a time per KV tile; where the keys are in parts, the second kernel's start, its walk over the
+// parts, and the parts' rows. Decoding a memory takes 1e-4 us a row. In each of the 24 the call's choice took at most 5 %
+// longer than the fastest of all kernels and parts.
 struct ModeCost {
   double base, wave, tile, combine, row;
 };
