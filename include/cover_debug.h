@@ -105,8 +105,9 @@ int cover_debug_window_model(int B, int Hq, int Hkv, int Lq, int Lk, int q0, int
                              const int32_t* max_clusters, int32_t* choice, double* times);
 
 /*
- * cover_attn_fwd_prefix8 on a kernel of the caller's choice and with the keys in nsplit parts (1 .. 64), whatever the call
- * itself would take. mode: 0, 1 rows of a KV head in groups of 16 or 32, codes as matrix operands; 2 in Q tiles
+ * cover_attn_fwd_prefix8 on a kernel of the caller's choice and with the keys in nsplit parts (1 .. 64, whose results a
+ * second kernel adds up; or -2 .. -8 in modes 0 to 2: 2 .. 8 parts, each a CTA of a cluster that does so itself), whatever
+ * the call itself would take. mode: 0, 1 rows of a KV head in groups of 16 or 32, codes as matrix operands; 2 in Q tiles
  * of 128, codes decoded by the kernel; 3 in pairs of Q tiles over a memory decoded by a pass of its own; 4 the kernels of
  * cover_attn_fwd_prefix over such a memory (nsplit 1, no key ranges, no cap; else COVER_ERR_UNSUPPORTED).
  * workspace_bytes: of the workspace; what is needed: modes 3, 4 4 B Hkv Lk 128 bytes, and nsplit > 1 another
@@ -123,7 +124,7 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8,
 
 /*
  * What cover_attn_fwd_prefix8 takes for these sizes (plain: without key ranges and cap): choice[3] = {mode, groups of rows
- * a KV head, parts of the keys}, us[0] = the predicted time. Host arithmetic only. COVER_ERR_INVALID_ARG for
+ * a KV head, parts of the keys (negative: joined in a cluster)}, us[0] = the predicted time. Host arithmetic only. COVER_ERR_INVALID_ARG for
  * invalid sizes or a null pointer.
  */
 int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int32_t* choice, double* us);

@@ -811,7 +811,8 @@ def cover_debug_attn_fault(q, k_cached, v_cached, k_seedmask=None, v_seedmask=No
 
 def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0: int, mode: int,
                              nsplit: int = 1, key_lo=None, key_hi=None, softcap: float = 0.0):
-    """cover_attn_fwd_prefix8 on the kernel ``mode`` with the keys in ``nsplit`` parts. Returns (out, lse)."""
+    """cover_attn_fwd_prefix8 on the kernel ``mode`` with the keys in ``nsplit`` parts (negative: -nsplit parts, joined
+    in a cluster). Returns (out, lse)."""
     B, Hq, Lq, D = q.shape
     Hkv, Lk = k8.shape[1], k8.shape[2]
     S = 0 if seed_idx is None else int(seed_idx.shape[1])
@@ -827,7 +828,8 @@ def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmas
 
 
 def cover_debug_attn_prefix8_plan(B: int, Hq: int, Hkv: int, Lq: int, Lk: int, plain: bool):
-    """(mode, groups of rows a KV head, parts of the keys, predicted us) that cover_attn_fwd_prefix8 takes (no device needed)."""
+    """(mode, groups of rows a KV head, parts of the keys (negative: joined in a cluster), predicted us) that
+    cover_attn_fwd_prefix8 takes (no device needed)."""
     choice, us = (ctypes.c_int32 * 3)(), ctypes.c_double()
     code = _lib.load().cover_debug_attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, 1 if plain else 0, ctypes.addressof(choice),
                                                      ctypes.addressof(us))

@@ -9,8 +9,9 @@
 //
 // The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r of head
 // hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view. A CTA takes a group of them against the KV tiles (128
-// keys) of one of nsplit parts of what its rows see; with nsplit > 1 the parts leave (m, l, O) in fp32 in the workspace
-// and a second kernel combines them. Five ways, chosen by plan_of from the sizes:
+// keys) of one of nsplit parts of what its rows see; with nsplit > 1 the parts' CTAs are a cluster that adds up their (m, l, O)
+// in fp32 itself (rows and tile, up to 8 parts), or leave them in the workspace for a second kernel. Five ways, chosen by
+// plan_of from the sizes:
 //   rows (16 or 32 a group)  codes as 8-bit matrix operands, products turned over; bound by reading the memory
 //   tile (128 rows)          codes decoded to bf16 by the CTA; bound by decoding
 //   pairs (2 x 128 rows)     codes decoded once, by a pass of its own; bound by the tensor cores and the softmax
@@ -29,9 +30,12 @@
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
 
 #include <algorithm>
+#include <cmath>
 
+#include "cluster.cuh"
 #include "context.cuh"
 #include "e4m3.cuh"
 #include "kernels.cuh"
@@ -59,6 +63,7 @@ static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs 
 static_assert(kSoftmaxRegs >= kLaunchRegs && kDecodeRegs <= kLaunchRegs && kIssueRegs <= kLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kMaxParts = 64;              // of the keys
+constexpr int kMaxJoined = 8;              // parts whose CTAs are a cluster (its portable size)
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
 
 // Barriers and tables of a CTA.
@@ -103,6 +108,7 @@ struct Params {
   int* status;
   long long rows;    // B * Hq * Lq
   int n_seeds, Hq, Hkv, G, Lq, Lk, q0, n_groups, nsplit;
+  int joined;        // the parts' CTAs are a cluster and add their results up themselves
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
@@ -153,6 +159,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t x) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
@@ -542,6 +549,90 @@ __device__ __forceinline__ void store_chunk(const Params& p, const float (&o)[32
   }
 }
 
+// Parts that a cluster's CTAs add up themselves: each stages its rows' accumulators [row][128] fp32 and (m, l) in its own
+// shared memory, and CTA ks finishes the rows ks, ks + nsplit, .., a warp a row, reading all CTAs'. Rows' 16-byte
+// pieces are swizzled, for the threads that write a row each.
+__device__ __forceinline__ uint32_t staged_at(int row, int c4) { return row * (kD * 4) + ((c4 ^ (row & 31)) << 4); }
+
+__device__ __forceinline__ float4 lds_cluster128(uint32_t addr) {
+  float4 r;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(addr) : "memory");
+  return r;
+}
+__device__ __forceinline__ float2 lds_cluster64(uint32_t addr) {
+  float2 r;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(addr) : "memory");
+  return r;
+}
+
+// kPad: nsplit rounded up to 4 or 8. A warp works on kBatch rows at once.
+template <int kPad, int kBatch>
+__device__ __forceinline__ void join_rows(const Params& p, uint32_t o, uint32_t ml, int n_rows, long long orow0, int ks) {
+  static_assert(kPad * kBatch <= 32, "a lane for every part of the rows at work");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int first = ks + p.nsplit * warp; first < n_rows; first += 8 * p.nsplit * kBatch) {
+    // lane: part lane % kPad of the batch's row lane / kPad (row numbers past the last one are held to it)
+    const auto row = [&](int i) { return min(first + 8 * p.nsplit * i, n_rows - 1); };
+    const int j = lane % kPad;
+    const float2 part = lds_cluster64(cluster_map(ml + 8 * row(min(lane / kPad, kBatch - 1)), min(j, p.nsplit - 1)));
+    float4 x[kBatch][kPad];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+      for (int k = 0; k < kPad; ++k) {
+        x[i][k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (k < p.nsplit) x[i][k] = lds_cluster128(cluster_map(o + staged_at(row(i), lane), k));
+      }
+    const float my_m = j < p.nsplit ? part.x : -INFINITY;
+    float m = my_m;
+#pragma unroll
+    for (int d = kPad / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    const float w = my_m == -INFINITY ? 0.0f : ex2_approx(my_m - m);
+    float l = j < p.nsplit ? w * part.y : 0.0f;
+#pragma unroll
+    for (int d = kPad / 2; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int n = first + 8 * p.nsplit * i;
+      float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kPad; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, w, i * kPad + k);   // (parts that saw no key hold zeros)
+        acc.x = fmaf(wk, x[i][k].x, acc.x);
+        acc.y = fmaf(wk, x[i][k].y, acc.y);
+        acc.z = fmaf(wk, x[i][k].z, acc.z);
+        acc.w = fmaf(wk, x[i][k].w, acc.w);
+      }
+      const float f = __shfl_sync(0xffffffffu, inv, i * kPad);
+      if (n < n_rows)
+        reinterpret_cast<uint2*>(p.out + (orow0 + n) * kD)[lane] =
+            make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+    }
+    const int n = first + 8 * p.nsplit * (lane / kPad);
+    if (p.lse != nullptr && j == 0 && lane / kPad < kBatch && n < n_rows) p.lse[orow0 + n] = (m + lg2_approx(l)) * 0.6931471805599453f;
+  }
+}
+
+// kMany: Q tiles of 128 rows, whose warps have 2 rows and more to finish: four of four parts at once, or two (1 x 32 heads,
+// 256 x 1024, two parts: 17.7 us with one row after the other, 16.0 us so). With 16 or 32 rows a warp has one
+// or two; there the longer code costs more than it saves (rows of 32: 10.4 against 11.3 us).
+template <bool kMany>
+__device__ __forceinline__ void join_parts(const Params& p, uint32_t o, uint32_t ml, int n_rows, long long orow0, int ks) {
+  __syncwarp();
+  cluster_sync();   // every CTA's rows are staged
+  if (kMany && p.nsplit <= 4) join_rows<4, 4>(p, o, ml, n_rows, orow0, ks);
+  else join_rows<8, kMany ? 2 : 1>(p, o, ml, n_rows, orow0, ks);
+  __syncwarp();
+  cluster_sync();   // no CTA leaves while its rows are read
+}
+// The other roles' warps take part in the cluster's barriers.
+__device__ __forceinline__ void join_pass() {
+  __syncwarp();
+  cluster_sync();
+  cluster_sync();
+}
+
 // Barrier of one Q tile's 256 softmax threads of the pairs kernel, and with the vote whether any of them says so.
 __device__ __forceinline__ void tile_sync(int tile) { asm volatile("bar.sync %0, 256;" ::"r"(2 + tile) : "memory"); }
 __device__ __forceinline__ bool tile_any(int tile, bool x) {
@@ -687,9 +778,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(&ctl.drain, 0, nullptr);
     }
     __syncwarp();
+    if (p.joined) join_pass();
   } else if (warp >= kDecodeWarp) {
     setmaxnreg_dec<kDecodeRegs>();
     decode_tiles(ctl, p, (warp - kDecodeWarp) >> 2, sm.ring, sm.k[0], sm.v[0], mem0, j0, nt);
+    if (p.joined) join_pass();
   } else {
     // ---------------- softmax ----------------
     setmaxnreg_inc<kSoftmaxRegs>();
@@ -807,6 +900,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (s_self != s_self) l = s_self;   // NaN in the masked-input pair
     const long long orow = rowbase + P;
     const bool split = p.nsplit > 1;
+    const uint32_t staged = smem_u32(sm.k);   // nor are K's tiles
     // 1 / l, once a row; zero where no key was seen
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);
     if (ok && warp_live) {
@@ -830,15 +924,24 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int e = 0; e < 32; ++e) o[e] = 0.0f;
         }
         if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + 32 * c);
-        if (valid) store_chunk(p, o, inv, split, ks, orow, 32 * c);
+        if (valid && p.joined) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            sts128(staged + staged_at(R, 8 * c + e), __float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                   __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+        } else if (valid) {
+          store_chunk(p, o, inv, split, ks, orow, 32 * c);
+        }
         __syncwarp();   // the next chunk is loaded by the whole warp
       }
       if (valid && c0 == 0) {
-        if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
+        if (p.joined) ml[2 * kBM + R] = make_float2(m, l);
+        else if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
         else if (p.lse != nullptr) p.lse[orow] = (m + lg2_approx(l)) * 0.6931471805599453f;
       }
     }
     tc_fence_before_sync();
+    if (p.joined) join_parts<true>(p, staged, smem_u32(ml + 2 * kBM), min(kBM, n_packed - p0), rowbase + p0, ks);
   }
   __syncthreads();
   if (warp == kMmaWarp) {
@@ -1274,6 +1377,7 @@ struct RowsSmem {
   int unseen[2][kN], any_unseen[2];  // per stream: rows that have seen no key, whose reference is not set
   float red[2][4][kN];            // per stream and warp
   float s_self[kN];
+  float2 ml[kN];                  // of a part that the cluster adds up
   float q_scale[kN];              // power of two of a row, times log2(e) / sqrt(d) (capped: 2 log2(e) / (c sqrt(d)))
   int slot[kN];
   uint32_t tmem_base;
@@ -1474,7 +1578,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       umma_commit(&sm.drain);
       mbar_wait(&sm.drain, 0, nullptr);
     }
-    __syncwarp();
+    if (p.joined) join_pass();
   } else if (warp >= kScreenWarp) {
     // ---------------- NaN codes of V (thread = key; the swizzle moves no byte out of its row) ----------------
     const int key = tid - kScreenWarp * 32;
@@ -1509,6 +1613,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (!sm.abort) report_status(p.status, kStatusTimeout, 72);
       sm.abort = 1;
     }
+    if (p.joined) join_pass();
   } else {
     // ---------------- softmax (thread = key of a KV tile) ----------------
     const int stream = warp >> 2, key = tid & (kBN - 1), w4 = warp & 3;
@@ -1727,6 +1832,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     }
     softmax_sync();
     const bool split = p.nsplit > 1;
+    const uint32_t staged = smem_u32(sm.k[0]);   // every product is complete: K is not read any more
     if (ok && tid < n_rows) {
       const int n = tid;
       const long long orow = rowbase + p0 + n;
@@ -1742,7 +1848,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
       if (s_self != s_self) sum = s_self;
       sm.fin[n] = make_float4(w0, w1, p_self, split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
-      if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(top, sum);
+      if (p.joined) sm.ml[n] = make_float2(top, sum);
+      else if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(top, sum);
       else if (p.lse != nullptr) p.lse[orow] = (top + lg2_approx(sum)) * 0.6931471805599453f;
     }
     softmax_sync();
@@ -1776,13 +1883,15 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           if (f.y != 0.0f) o = fmaf(o1[e], f.y, o);
           if (f.z != 0.0f) o = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.slot[n]) * kD + col]), o);
           const long long orow = rowbase + p0 + n;
-          if (split) p.part_o[(static_cast<size_t>(ks) * p.rows + orow) * kD + col] = o;
+          if (p.joined) sts32(staged + staged_at(n, col >> 2) + 4 * (col & 3), __float_as_uint(o));
+          else if (split) p.part_o[(static_cast<size_t>(ks) * p.rows + orow) * kD + col] = o;
           else p.out[orow * kD + col] = __float2bfloat16_rn(o * f.w);
         }
       }
       __syncwarp();
     }
     tc_fence_before_sync();
+    if (p.joined) join_parts<false>(p, staged, smem_u32(sm.ml), n_rows, rowbase + p0, ks);
   }
   __syncthreads();
   if (warp == kRowsMmaWarp) {
@@ -1842,24 +1951,32 @@ float fixed_reference(float cap_log2) {
 struct Plan {
   Mode mode;
   int n_groups, nsplit;
+  bool joined;   // the parts' CTAs are clusters
   double us;
 };
 
 // Resident clusters of 1 .. 8 CTAs, one CTA an SM, that the prediction for cover_attn_fwd_prefix's kernels goes by.
 constexpr int kClusters[8] = {152, 76, 48, 36, 28, 24, 20, 18};
+// The same for the parts joined in a cluster: at least so many on every GPU measured (they differ: 15 or 18 of 8 CTAs),
+// and calls of 28 clusters of 5 took two turns where 28 fitted.
+constexpr int kJoinedClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
 
 // The kernel and the parts of the keys. plain: no key ranges, no cap.
 //
-// Predicted microseconds, fitted to 409 calls back to back on GB300 (24 windows of 1 to 1024 rows over 300 to 20000
-// keys, batches of 1 to 16, 1 to 64 parts; off by 3 to 6 % in the mean, at most 30 %): a base, and for every wave of one
+// Predicted microseconds, fitted to 631 calls back to back on GB300 (24 windows of 1 to 1024 rows over 300 to 20000
+// keys, batches of 1 to 16, 1 to 64 parts; off by 4 to 9 % in the mean, at most 40 %): a base, and for every wave of one
 // CTA an SM a start and a time per KV tile; where the keys are in parts, the second kernel's start, its walk over the
-// parts, and the parts' rows. Decoding a memory takes 1e-4 us a row. In each of the 24 the call's choice took at most 5 %
-// longer than the fastest of all kernels and parts.
+// parts, and the parts' rows, or, joined in a cluster, the cluster's barriers and the rows that a CTA finishes. Decoding a
+// memory takes 1e-4 us a row. In each of the 24 the call's choice took at most 4 % longer than the fastest of all
+// kernels and parts. Joined against added up by a second kernel, each with its best parts: 8.3 against 10.0 us (1 x 28 / 4
+// heads, 1 x 777), 10.3 / 11.9 (1 x 4000), 12.9 / 15.1 (1 x 32 / 8, 128 x 1024), 22.7 / 24.8 (4 x 16 / 2, 64 x 4096);
+// the second kernel's where more than 8 parts pay: 22.5 / 19.5 (1 x 28 / 4, 32 x 8192).
 struct ModeCost {
-  double base, wave, tile, combine, row;
+  double base, wave, tile, combine, row, join, join_row;
 };
 constexpr ModeCost kCosts[kReadBack] = {
-    {2.2, 4.5, 0.72, 0.8, 6.4e-4}, {2.4, 6.0, 0.92, 0.8, 4.8e-4}, {3.0, 4.1, 1.34, 1.5, 2.5e-4}, {5.0, 3.5, 1.72, 2.4, 1.9e-4}};
+    {2.2, 4.5, 0.72, 0.8, 6.4e-4, 0.8, 0.07}, {2.4, 6.0, 0.92, 0.8, 4.8e-4, 0.6, 0.13},
+    {3.0, 4.1, 1.34, 1.5, 2.5e-4, 2.0, 0.036}, {5.0, 3.5, 1.72, 2.4, 1.9e-4, 0.0, 0.0}};
 constexpr double kPartUs = 0.15, kDecodeRowUs = 1.0e-4, kDecodeUs = 1.8;
 
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
@@ -1877,7 +1994,13 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
       const int tiles = (nkv + ns - 1) / ns;
       const double us = k.base + waves * (k.wave + k.tile * tiles) + (mode == kDecodedPairs ? decode_us : 0.0) +
                         (ns > 1 ? k.combine + kPartUs * ns + k.row * rows * ns : 0.0);
-      if (best.nsplit == 0 || us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, us};
+      if (best.nsplit == 0 || us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, false, us};
+      if (mode != kDecodedPairs && ns > 1 && ns <= kMaxJoined) {
+        const long long turns = (units + kJoinedClusters[ns - 1] - 1) / kJoinedClusters[ns - 1];
+        const double own_rows = std::ceil(std::min<double>(packed, kModeRows[mode]) / ns);
+        const double join_us = k.base + turns * (k.wave + k.tile * tiles + k.join + k.join_row * own_rows);
+        if (join_us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, true, join_us};
+      }
       if (units * ns > 8 * kSms) break;
     }
   }
@@ -1888,7 +2011,7 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
     const WindowChoice c = window_gqa_model(a, kSms, kClusters);
     if (c.packed) us = std::min(us, c.packed_us);
     us += kDecodeUs + decode_us;
-    if (us < best.us) best = Plan{kReadBack, 1, 1, us};
+    if (us < best.us) best = Plan{kReadBack, 1, 1, false, us};
   }
   return best;
 }
@@ -1913,7 +2036,7 @@ size_t decoded_bytes(const Plan& plan, int B, int Hkv, int L) {
   return plan.mode >= kDecodedPairs ? static_cast<size_t>(B) * Hkv * L * kD * 2 : 0;   // of K, and of V
 }
 size_t plan_bytes(const Plan& plan, int B, int Hq, int Hkv, int Lq, int L) {
-  return 2 * decoded_bytes(plan, B, Hkv, L) + part_bytes(static_cast<long long>(B) * Hq * Lq, plan.nsplit);
+  return 2 * decoded_bytes(plan, B, Hkv, L) + (plan.joined ? 0 : part_bytes(static_cast<long long>(B) * Hq * Lq, plan.nsplit));
 }
 
 }  // namespace
@@ -1927,12 +2050,12 @@ void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, int* c
   const Plan p = plan_of(B, Hq, Hkv, Lq, L, plain);
   choice[0] = p.mode;
   choice[1] = p.n_groups;
-  choice[2] = p.nsplit;
+  choice[2] = p.joined ? -p.nsplit : p.nsplit;
   *us = p.us;
 }
 
 size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit) {
-  return plan_bytes(Plan{static_cast<Mode>(mode), 1, nsplit, 0.0}, B, Hq, Hkv, Lq, L);
+  return plan_bytes(Plan{static_cast<Mode>(mode), 1, std::abs(nsplit), nsplit < 0, 0.0}, B, Hq, Hkv, Lq, L);
 }
 
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
@@ -1942,7 +2065,8 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.L, plain);
   if (a.mode >= 0) {   // a debug call says which
     plan.mode = static_cast<Mode>(a.mode);
-    plan.nsplit = a.nsplit;
+    plan.nsplit = std::abs(a.nsplit);
+    plan.joined = a.nsplit < 0;
     plan.n_groups = static_cast<int>((static_cast<long long>(a.Hq / a.Hkv) * a.Lq + kModeRows[a.mode] - 1) / kModeRows[a.mode]);
   }
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
@@ -2018,6 +2142,7 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.q0 = a.q0;
   p.n_groups = plan.n_groups;
   p.nsplit = plan.nsplit;
+  p.joined = plan.joined ? 1 : 0;
   p.scale_log2 = log2e / root;
   const bool cap = a.softcap > 0.0f;
   p.cap_log2 = a.softcap * log2e;
@@ -2027,22 +2152,25 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   const float tanh_poly[4] = {kTanh0, kTanh1, kTanh2, kTanh3};
   float power = p.cap_log2 * p.cap_x;
   for (int i = 0; i < 4; ++i, power *= p.cap_x * p.cap_x) p.cap_poly[i] = p.cap_ref != -INFINITY ? tanh_poly[i] * power : 0.0f;
-  cudaLaunchAttribute attr[1];
-  const dim3 ctas(static_cast<unsigned>(grid));
-  cudaLaunchConfig_t cfg;
-  cudaError_t e;
-  if (few) {
-    const int m = plan.mode == kRows16 ? 0 : 1;
-    cfg = pdl_config(ctas, dim3(kRowsThreads), kRowsSmemBytes[m], stream, attr);
-    e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], tk, tv, p);
-  } else {
-    cfg = pdl_config(ctas, dim3(kThreads), decoded ? kPairSmemBytes : kSmemBytes, stream, attr);
-    e = decoded ? cudaLaunchKernelEx(&cfg, kPairKernels[cap ? 1 : 0], tq, tk, tv, p)
-                : cudaLaunchKernelEx(&cfg, kTileKernels[cap ? 1 : 0], tq, p);
+  cudaLaunchAttribute pdl[1], attr[2];
+  const int m = plan.mode == kRows16 ? 0 : 1;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(few ? kRowsThreads : kThreads),
+                                      few ? kRowsSmemBytes[m] : decoded ? kPairSmemBytes : kSmemBytes, stream, pdl);
+  attr[0] = pdl[0];
+  if (plan.joined) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(plan.nsplit);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
   }
-  if (e == cudaSuccess && plan.nsplit > 1) {
+  cudaError_t e;
+  if (few) e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], tk, tv, p);
+  else if (decoded) e = cudaLaunchKernelEx(&cfg, kPairKernels[cap ? 1 : 0], tq, tk, tv, p);
+  else e = cudaLaunchKernelEx(&cfg, kTileKernels[cap ? 1 : 0], tq, p);
+  if (e == cudaSuccess && plan.nsplit > 1 && !plan.joined) {
     cfg = pdl_config(dim3(static_cast<unsigned>((rows + kCombineWarps - 1) / kCombineWarps)), dim3(kCombineWarps * 32), 0,
-                     stream, attr);
+                     stream, pdl);
     e = cudaLaunchKernelEx(&cfg, attn_prefix8_combine_kernel, static_cast<const float*>(p.part_o),
                            static_cast<const float2*>(p.part_ml), plan.nsplit, rows, p.out, p.lse);
   }

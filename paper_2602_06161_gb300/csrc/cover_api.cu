@@ -486,7 +486,9 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8, cons
                              int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D, const int32_t* key_lo,
                              const int32_t* key_hi, float softcap, void* out, float* lse, void* workspace,
                              size_t workspace_bytes, int mode, int nsplit, void* stream) {
-  if (mode < 0 || mode >= cover::kAttn8Modes || nsplit < 1 || nsplit > 64) return COVER_ERR_INVALID_ARG;
+  if (mode < 0 || mode >= cover::kAttn8Modes || nsplit < -8 || nsplit > 64 || nsplit == 0 || nsplit == -1)
+    return COVER_ERR_INVALID_ARG;
+  if (nsplit < 0 && mode > cover::kAttn8Tile) return COVER_ERR_UNSUPPORTED;
   if (mode == cover::kAttn8ReadBack && (nsplit != 1 || key_lo != nullptr || key_hi != nullptr || softcap != 0.0f))
     return COVER_ERR_UNSUPPORTED;
   cover::Attn8Args a{q,  k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,   Hq,       Hkv,

@@ -194,7 +194,7 @@ struct Attn8Args {
   int mode = -1, nsplit = 0;   // debug calls: the kernel and the parts of the keys, whatever the plan says
 };
 constexpr int kAttn8Modes = 5;      // attn_prefix8.cu's Mode
-constexpr int kAttn8ReadBack = 4;
+constexpr int kAttn8Tile = 2, kAttn8ReadBack = 4;
 size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L);
 size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit);
 // choice: mode, groups of rows a KV head, parts of the keys; us: predicted. plain: no key ranges, no cap.

@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 6) kv8_kernel(const __grid_constant_
 }
 
 // Launches the grid's rows, at most 65535 (a grid's height) at a time. (All of a grid in its first
-// dimension would leave the kernel an integer division and 28 bytes of spills: 8 x 32 heads of 2048 rows took 50.8 us to
+// dimension would leave the kernel an integer division and 28 bytes of spills: 4 x 8 heads of 8191 rows took 50.8 us to
 // write instead of 37.9.)
 int launch_rows(void (*fn)(const Kv8Params), Kv8Params p, long long columns, long long rows, int B, cudaStream_t stream) {
   for (long long at = 0; at < rows; at += 65535) {

@@ -238,7 +238,7 @@ def test_agrees_with_the_bf16_attention_of_what_is_read_back():
         assert (out.float() - ref.float()).abs().max() <= 2 * (2 * 2.0 ** -8 + 4 * 2.0 ** -20 * big) * mass
 
 
-KERNELS = [(0, 1), (0, 3), (1, 1), (1, 2), (2, 1), (2, 4), (3, 1), (3, 3), (2, 64)]
+KERNELS = [(0, 1), (0, 3), (1, 1), (1, 2), (2, 1), (2, 4), (3, 1), (3, 3), (2, 64), (0, -2), (0, -7), (1, -3), (1, -8), (2, -2), (2, -5), (2, -8)]
 
 
 @pytest.mark.parametrize("mode,nsplit", KERNELS)
@@ -256,6 +256,28 @@ def test_every_kernel(shape, mode, nsplit):
         torch.cuda.synchronize()
         assert api.cover_device_status() == 0
         _check(d, out, lse, lo, hi, cap)
+
+
+@pytest.mark.parametrize("mode,nsplit", [(0, 8), (1, 5), (2, 7)])
+def test_parts_joined_in_a_cluster(mode, nsplit):
+    """The same parts added up by the cluster and by the second kernel: their terms differ by a rounding of the weights at most,
+    and rows without a key, parts without a key, NaN and masked-input scores are the same."""
+    B, Hq, Hkv, Lq, Lk, S, q0 = 2, 28, 4, 19, 1500, 9, 1400
+    d = _inputs(B, Hq, Hkv, Lq, Lk, S, q0)
+    d["mem"][2][1, 2, 1100] = 255
+    for kind in (None, "any", "lens", "window"):
+        lo, hi = (None, None) if kind is None else _ranges(kind, B, Lq, Lk, q0)
+        a, b = (api.cover_debug_attn_prefix8(d["q"], *d["mem"], d["km"], d["vm"], d["seeds"], q0=q0, mode=mode, nsplit=n, key_lo=lo,
+                                             key_hi=hi, softcap=20.0) for n in (-nsplit, nsplit))
+        assert torch.equal(a[0].isnan(), b[0].isnan()) and torch.equal(a[1].isnan(), b[1].isnan())
+        assert kind is not None or a[1].isnan().any()
+        assert torch.equal(a[1] == -math.inf, b[1] == -math.inf)
+        x, y = (t.float().nan_to_num(0.0) for t in (a[0], b[0]))
+        assert ((x - y).abs() <= 2.0 ** -7 * y.abs() + 2.0 ** -18).all()
+        x, y = (t.nan_to_num(0.0, neginf=0.0) for t in (a[1], b[1]))
+        assert ((x - y).abs() <= 2.0 ** -20 * (1 + y.abs())).all()
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
 
 
 @pytest.mark.parametrize("mode", range(5))
@@ -371,7 +393,8 @@ def test_refusals():
         api.cover_attn_fwd_prefix8(d["q"].transpose(1, 2), *d["mem"], q0=0)
     with pytest.raises(ValueError, match="out must match"):
         api.cover_attn_fwd_prefix8(*a, q0=0, out=torch.empty((1, 4, 7, 128), device="cuda", dtype=torch.bfloat16))
-    for kw in (dict(mode=5), dict(mode=-1), dict(mode=0, nsplit=0), dict(mode=2, nsplit=65), dict(mode=4, nsplit=2), dict(mode=4, softcap=1.0)):
+    for kw in (dict(mode=5), dict(mode=-1), dict(mode=0, nsplit=0), dict(mode=2, nsplit=65), dict(mode=4, nsplit=2), dict(mode=4, softcap=1.0),
+               dict(mode=0, nsplit=-1), dict(mode=2, nsplit=-9), dict(mode=3, nsplit=-2), dict(mode=4, nsplit=-2)):
         with pytest.raises(CoverError):
             api.cover_debug_attn_prefix8(*a, q0=0, **kw)
     small = api.kv8_memory(1, 2, 64, 64)

@@ -25,7 +25,7 @@ def test_parts_and_workspace(B, heads, Lq, Lk):
     need = 0
     for plain in (False, True):
         mode, groups, nsplit, us = plan(B, Hq, Hkv, Lq, Lk, plain=plain)
-        assert us > 0 and 1 <= nsplit <= 64 and nsplit <= (Lk + 127) // 128
+        assert us > 0 and (1 <= nsplit <= 64 or -8 <= nsplit <= -2 and mode <= TILE) and abs(nsplit) <= (Lk + 127) // 128
         assert plain or mode != READ_BACK
         if mode != READ_BACK:
             size = (16, 32, 128, 256)[mode]
