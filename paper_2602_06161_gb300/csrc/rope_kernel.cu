@@ -13,10 +13,14 @@
 //
 // Bound by memory: each row is read and written once. A thread holds one 16-byte vector column (two, R / 2
 // apart, in the layout of halves) of one token and walks over up to eight heads, so that its sines and cosines serve
-// all of them. More threads with fewer loads each are faster than the opposite: 4 x 40 heads, 8191 tokens of 128 bf16
-// took 118 us with one head in flight a thread and four CTAs of 256 an SM, 137 with two and three, 165 with four and
-// two, 253 with eight; in neighbouring pairs 121 with two heads and four CTAs, 148 with one, 162 with four and two; fp32 (32 + 32
-// heads, 4096 tokens) 85 with four heads, 87 with two, 103 with one. Walks over 16 or 40 heads: 127 and 142 us.
+// all of them. The first rows and the position are loaded before the frequencies are made ready and waited for (8 x 32 + 32 heads,
+// 64 tokens of 64 fp32: 8.7 us without that and with a head a thread, 3.5 so; 4 tokens of 28 + 4 heads 2.9 and 2.3).
+// More threads with fewer loads each are faster than the opposite where the rows come from HBM: 4 x 40 heads, 8191
+// tokens of 128 bf16 took 117 us with one head in flight a thread and four CTAs of 256 an SM, 132 with two and three, 165
+// with four and two, 253 with eight (2048 tokens of one sequence, which stay in L2: 10.3 and 8.7 with two and three); in
+// neighbouring pairs 121 with two heads and four CTAs, 140 with two and three, 162 with four and two; fp32 (32 + 32
+// heads, 4096 tokens of 64, halves) 81 with four heads and three CTAs, 94 with four and two or two and three. Walks over
+// 16 or 40 heads: 127 and 142 us.
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -80,22 +84,25 @@ struct alignas(sizeof(T) * N) Vec {
 // T: element; N: elements of a thread's vector (16 bytes, or one element where a size, a stride or
 // a pointer does not allow more); kInter: pairs of neighbours (a vector of N >= 2 holds N / 2 pairs).
 template <typename T, int N, bool kInter>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) rope_kernel(const __grid_constant__ RopeParams p) {
   constexpr int kHeadsInFlight = sizeof(T) == 2 ? (kInter ? 2 : 1) : 4;
   extern __shared__ uint64_t turns[];   // [R / 2] fractions of a turn per position, 2^64 = one turn
-  griddep_wait();
-  griddep_launch_dependents();
-  for (int i = threadIdx.x; i < p.R / 2; i += kThreads) {
-    const double t = p.inv_freq[i] * 0.15915494309189535;   // / 2 pi
-    turns[i] = __double2ull_rn((t - floor(t)) * 18446744073709551616.0);
-  }
-  __syncthreads();
   const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-  if (item >= p.items) return;
-  const int u = static_cast<int>(item % p.units);
-  long long rest = item / p.units;
-  const int c = static_cast<int>(rest % p.chunks);
-  rest /= p.chunks;                                          // token b * L + l
+  const bool live = item < p.items;
+  int u, c;
+  long long rest;                                            // token b * L + l
+  if (p.items <= 0x7fffffffLL) {
+    const unsigned i = live ? static_cast<unsigned>(item) : 0u, r = i / static_cast<unsigned>(p.units);
+    u = static_cast<int>(i - r * static_cast<unsigned>(p.units));
+    rest = r / static_cast<unsigned>(p.chunks);
+    c = static_cast<int>(r - static_cast<unsigned>(rest) * static_cast<unsigned>(p.chunks));
+  } else {
+    const long long i = live ? item : 0;
+    u = static_cast<int>(i % p.units);
+    rest = i / p.units;
+    c = static_cast<int>(rest % p.chunks);
+    rest /= p.chunks;
+  }
   const long long b = rest / p.L;
   const int l = static_cast<int>(rest - b * p.L);
   const bool turn = u < p.turn_units;
@@ -109,9 +116,38 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) rope_kernel(
   } else {
     col0 = p.R + (u - p.turn_units) * N;
   }
+  const int which = c >= p.chunks0 ? 1 : 0;
+  const RopeTensor& t = p.t[which];
+  // heads h0, h0 + step, ...: the chunks' threads, neighbours in a warp, read and write neighbouring heads
+  const int step = which ? p.chunks - p.chunks0 : p.chunks0;
+  const int h0 = which ? c - p.chunks0 : c;
+  const int n = live ? (t.heads - h0 + step - 1) / step : 0;
+  const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + l * t.in_l;
+  T* out = reinterpret_cast<T*>(t.out) + b * t.out_b + l * t.out_l;
+  using V = Vec<T, N>;
+  V x[kHeadsInFlight][2];
+  const auto load = [&](int i0) {
+#pragma unroll
+    for (int j = 0; j < kHeadsInFlight; ++j) {
+      if (i0 + j >= n) break;
+      const T* row = in + (h0 + (i0 + j) * step) * t.in_h;
+      x[j][0] = *reinterpret_cast<const V*>(row + col0);
+      if (kVecs == 2 && turn) x[j][1] = *reinterpret_cast<const V*>(row + col1);
+    }
+  };
+  griddep_wait();
+  griddep_launch_dependents();
+  // the first rows and the position are on their way while the frequencies are made ready
+  int32_t at = static_cast<int32_t>(static_cast<uint32_t>(p.pos0) + l);
+  if (p.pos != nullptr && turn) at = p.pos[rest];
+  load(0);
+  for (int i = threadIdx.x; i < p.R / 2; i += kThreads) {
+    const double f = p.inv_freq[i] * 0.15915494309189535;   // / 2 pi
+    turns[i] = __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+  }
+  __syncthreads();
   float cs[kHalf], sn[kHalf];
   if (turn) {
-    const int32_t at = p.pos != nullptr ? p.pos[rest] : static_cast<int32_t>(static_cast<uint32_t>(p.pos0) + l);
 #pragma unroll
     for (int i = 0; i < kHalf; ++i) {
       const uint64_t a = static_cast<uint64_t>(static_cast<int64_t>(at)) * turns[u * kHalf + i];
@@ -123,24 +159,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2) rope_kernel(
       sn[i] = (p.inverse ? -s : s) * p.mscale;
     }
   }
-  const int which = c >= p.chunks0 ? 1 : 0;
-  const RopeTensor& t = p.t[which];
-  // heads h0, h0 + step, ...: the chunks' threads, neighbours in a warp, read and write neighbouring heads
-  const int step = which ? p.chunks - p.chunks0 : p.chunks0;
-  const int h0 = which ? c - p.chunks0 : c;
-  const int n = (t.heads - h0 + step - 1) / step;
-  const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + l * t.in_l;
-  T* out = reinterpret_cast<T*>(t.out) + b * t.out_b + l * t.out_l;
-  using V = Vec<T, N>;
   for (int i0 = 0; i0 < n; i0 += kHeadsInFlight) {
-    V x[kHeadsInFlight][2];
-#pragma unroll
-    for (int j = 0; j < kHeadsInFlight; ++j) {
-      if (i0 + j >= n) break;
-      const T* row = in + (h0 + (i0 + j) * step) * t.in_h;
-      x[j][0] = *reinterpret_cast<const V*>(row + col0);
-      if (kVecs == 2 && turn) x[j][1] = *reinterpret_cast<const V*>(row + col1);
-    }
+    if (i0 > 0) load(i0);
 #pragma unroll
     for (int j = 0; j < kHeadsInFlight; ++j) {
       if (i0 + j >= n) break;
@@ -195,10 +215,11 @@ int launch_rope(const RopeArgs& a, cudaStream_t stream) {
   p.turn_units = a.R / 2 / per_unit;
   p.units = p.turn_units + (a.D - a.R) / n;
   // Heads a thread walks over: all work items of a small call are spread over the GPU (one head each), a
-  // large call's threads share their sines and cosines between eight heads.
+  // large call's threads share their sines and cosines between eight heads. In between two CTAs an SM are enough: 8 x
+  // 64 heads, 64 tokens of 128 fp32 take 6.0 us so and 11.9 with eight (256 threads more or less an SM: 5.2, 6.5).
   const long long tokens = static_cast<long long>(a.B) * a.L;
   const long long all = tokens * p.units * (a.Hq + a.Hkv);
-  p.chunk = static_cast<int>(std::min<long long>(8, std::max<long long>(1, all / (152 * 2048))));
+  p.chunk = static_cast<int>(std::min<long long>(8, std::max<long long>(1, all / (152 * 512))));
   p.chunks0 = (a.Hq + p.chunk - 1) / p.chunk;
   p.chunks = p.chunks0 + (a.Hkv + p.chunk - 1) / p.chunk;
   p.items = tokens * p.chunks * p.units;
