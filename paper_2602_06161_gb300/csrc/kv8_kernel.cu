@@ -9,8 +9,10 @@
 //
 // Bound by memory: each row is read and written once. D / N lanes hold a row (N elements of 16 bytes on the wide
 // side), and a thread has the K and V vectors of kTok = 2 consecutive slots in flight, 64 bytes, with six CTAs of 256
-// threads an SM (4 x 8 heads, 8191 rows of 128 bf16 from a projection written in 39 us; with one slot and six
-// CTAs 46, with four and four 42, eight and two 47).
+// threads an SM: 4 x 8 heads, 8191 rows of 128 bf16 from a projection are written in 35 us (with one slot and six
+// CTAs 46, with four and four 42, eight and two 47, each with the positions taken from shared memory, where this took
+// 37). A listed write loads its rows before it looks through the list: 8 x 32 heads, 64 rows of 64 fp32 5.2 us, and 5.8
+// with the list first and a slot at a time.
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -120,50 +122,62 @@ __global__ void __launch_bounds__(kThreads, 6) kv8_kernel(const __grid_constant_
   const int slot0 = (kWrite ? row : static_cast<int>(blockIdx.x)) * kSlots;
   const int head_group = kWrite ? static_cast<int>(blockIdx.x) : row;
   const int32_t* list = p.pos == nullptr ? nullptr : p.pos + static_cast<size_t>(b) * p.n;
-  for (int i = tid; i < kSlots; i += kThreads) {
-    const int s = slot0 + i;
-    int at = -1;
-    if (s < p.n) at = list != nullptr ? list[s] : p.pos0 + s;
-    s_pos[i] = at >= 0 && at < p.L ? at : -1;
-  }
-  __syncthreads();
-  if (kWrite && list != nullptr) {
-    // a slot whose position a lower slot names does not write it
-    __shared__ uint8_t s_dup[kSlots];
-    for (int i = tid; i < kSlots; i += kThreads) s_dup[i] = 0;
-    __syncthreads();
-    const int live = min(kSlots, p.n - slot0);
-    // one warp per slot in turn, its lanes over the lower slots
-    for (int i = tid >> 5; i < live; i += kThreads / 32) {
-      const int at = s_pos[i];
-      if (at < 0) continue;
-      bool hit = false;
-      for (int o = tid & 31; o < slot0 + i; o += 32) hit |= __ldg(list + o) == at;
-      if (hit) s_dup[i] = 1;
+  const int lane = tid % kLanes, group = tid / kLanes;
+  // the rows to be written of head h; those of the first are on their way while a list is looked through
+  uint4 r[2][kTok];
+  const auto load = [&](int h) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const T* x = reinterpret_cast<const T*>(p.src[w]) + b * p.sb[w] + h * p.sh[w] + lane * N;
+#pragma unroll
+      for (int j = 0; j < kTok; ++j) {
+        const int s = slot0 + group * kTok + j;
+        r[w][j] = make_uint4(0, 0, 0, 0);
+        if (s < p.n) r[w][j] = __ldcs(reinterpret_cast<const uint4*>(x + s * p.sl[w]));
+      }
+    }
+  };
+  if (kWrite) load(head_group * p.heads);
+  int at[kTok];
+  if (list == nullptr) {
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) {
+      const int s = slot0 + group * kTok + j;
+      at[j] = s < p.n ? p.pos0 + s : -1;
+    }
+  } else {
+    for (int i = tid; i < kSlots; i += kThreads) {
+      const int s = slot0 + i, x = s < p.n ? __ldg(list + s) : -1;
+      s_pos[i] = x >= 0 && x < p.L ? x : -1;
     }
     __syncthreads();
-    for (int i = tid; i < kSlots; i += kThreads)
-      if (s_dup[i]) s_pos[i] = -1;
-    __syncthreads();
-  }
-  const int lane = tid % kLanes, group = tid / kLanes;
-  int at[kTok];
+    if (kWrite) {
+      // a slot whose position a lower slot names does not write it: a warp looks through the list for kMine slots
+      constexpr int kMine = kSlots / (kThreads / 32);
+      const int first = (tid >> 5) * kMine;
+      int mine[kMine];
 #pragma unroll
-  for (int j = 0; j < kTok; ++j) at[j] = s_pos[group * kTok + j];
+      for (int k = 0; k < kMine; ++k) mine[k] = s_pos[first + k];
+      uint32_t hit = 0;
+#pragma unroll 2
+      for (int o = tid & 31; o < min(p.n, slot0 + first + kMine); o += 32) {
+        const int x = __ldg(list + o);
+#pragma unroll
+        for (int k = 0; k < kMine; ++k)
+          if (x == mine[k] && o < slot0 + first + k) hit |= 1u << k;
+      }
+      hit = __reduce_or_sync(0xffffffffu, hit);
+      if ((tid & 31) < kMine && ((hit >> (tid & 31)) & 1u)) s_pos[first + (tid & 31)] = -1;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < kTok; ++j) at[j] = s_pos[group * kTok + j];
+  }
   const int h1 = min(p.Hkv, (head_group + 1) * p.heads);
   for (int h = head_group * p.heads; h < h1; ++h) {
     const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + h) * p.L;   // the head's first memory row
     if (kWrite) {
-      uint4 r[2][kTok];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const T* x = reinterpret_cast<const T*>(p.src[w]) + b * p.sb[w] + h * p.sh[w] + lane * N;
-#pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-          r[w][j] = make_uint4(0, 0, 0, 0);
-          if (at[j] >= 0) r[w][j] = __ldcs(reinterpret_cast<const uint4*>(x + (slot0 + group * kTok + j) * p.sl[w]));
-        }
-      }
+      if (h > head_group * p.heads) load(h);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
 #pragma unroll
