@@ -106,12 +106,13 @@ int cover_debug_window_model(int B, int Hq, int Hkv, int Lq, int Lk, int q0, int
 
 /*
  * cover_attn_fwd_prefix8 on a kernel of the caller's choice and with the keys in nsplit parts (1 .. 64, whose results a
- * second kernel adds up; or -2 .. -8 in modes 0 to 2: 2 .. 8 parts, each a CTA of a cluster that does so itself), whatever
- * the call itself would take. mode: 0, 1 rows of a KV head in groups of 16 or 32, codes as matrix operands; 2 in Q tiles
+ * second kernel adds up; -2 .. -8 in modes 0 to 2: 2 .. 8 parts, each a CTA of a cluster that does so itself;
+ * 100 + n in modes 0 and 1, with key ranges, 2 <= B <= 32, B Lq <= 2048 and B <= n <= 4096: n parts of a KV head, shared
+ * out to the sequences by their lengths), whatever the call itself would take; COVER_ERR_UNSUPPORTED otherwise. mode: 0, 1 rows of a KV head in groups of 16 or 32, codes as matrix operands; 2 in Q tiles
  * of 128, codes decoded by the kernel; 3 in pairs of Q tiles over a memory decoded by a pass of its own; 4 the kernels of
  * cover_attn_fwd_prefix over such a memory (nsplit 1, no key ranges, no cap; else COVER_ERR_UNSUPPORTED).
  * workspace_bytes: of the workspace; what is needed: modes 3, 4 4 B Hkv Lk 128 bytes, and nsplit > 1 another
- * B Hq Lq nsplit 520 (rounded up to 16); COVER_ERR_INVALID_ARG if there is less. Otherwise as cover_attn_fwd_prefix8.
+ * B Hq Lq nsplit 520 (rounded up to 16), nsplit = 100 + n: (n + B) Hq Lq 520 + 256; COVER_ERR_INVALID_ARG if there is less. Otherwise as cover_attn_fwd_prefix8.
  */
 int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8,
                              const uint8_t* k_exp, const uint8_t* v_exp,
@@ -123,11 +124,11 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8,
                              int mode, int nsplit, void* stream);
 
 /*
- * What cover_attn_fwd_prefix8 takes for these sizes (plain: without key ranges and cap): choice[3] = {mode, groups of rows
- * a KV head, parts of the keys (negative: joined in a cluster)}, us[0] = the predicted time. Host arithmetic only. COVER_ERR_INVALID_ARG for
+ * What cover_attn_fwd_prefix8 takes for these sizes (plain: without key ranges and cap; ranges: with key ranges): choice[3]
+ * = {mode, groups of rows a KV head, parts of the keys (as nsplit above)}, us[0] = the predicted time. Host arithmetic only. COVER_ERR_INVALID_ARG for
  * invalid sizes or a null pointer.
  */
-int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int32_t* choice, double* us);
+int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int ranges, int32_t* choice, double* us);
 
 /*
  * Like cover_device_status, and also returns where the failure came from:

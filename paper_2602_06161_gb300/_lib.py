@@ -60,7 +60,7 @@ _SIGNATURES = {
     "cover_debug_status_detail": (_I, [_P, _P]),
     "cover_debug_attn_prefix8": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P,
                                       ctypes.c_float, _P, _P, _P, ctypes.c_size_t, _I, _I, _P]),
-    "cover_debug_attn_prefix8_plan": (_I, [_I, _I, _I, _I, _I, _I, _P, _P]),
+    "cover_debug_attn_prefix8_plan": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P]),
     "cover_debug_window_model": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P, _P]),
 }
 

@@ -812,13 +812,14 @@ def cover_debug_attn_fault(q, k_cached, v_cached, k_seedmask=None, v_seedmask=No
 def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0: int, mode: int,
                              nsplit: int = 1, key_lo=None, key_hi=None, softcap: float = 0.0):
     """cover_attn_fwd_prefix8 on the kernel ``mode`` with the keys in ``nsplit`` parts (negative: -nsplit parts, joined
-    in a cluster). Returns (out, lse)."""
+    in a cluster; above 100: nsplit - 100 parts of a KV head, shared out to the sequences). Returns (out, lse)."""
     B, Hq, Lq, D = q.shape
     Hkv, Lk = k8.shape[1], k8.shape[2]
     S = 0 if seed_idx is None else int(seed_idx.shape[1])
     out = torch.empty_like(q)
     lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
-    nbytes = (4 * B * Hkv * Lk * D if mode >= 3 else 0) + (B * Hq * Lq * nsplit * 520 + 16 if nsplit > 1 else 0)
+    nbytes = (4 * B * Hkv * Lk * D if mode >= 3 else 0) + (
+        (nsplit - 100 + B) * Hq * Lq * 520 + 256 if nsplit > 100 else B * Hq * Lq * nsplit * 520 + 16 if nsplit > 1 else 0)
     ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
     _launch("cover_debug_attn_prefix8", q.device, None,
             (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
@@ -827,11 +828,11 @@ def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmas
     return out, lse
 
 
-def cover_debug_attn_prefix8_plan(B: int, Hq: int, Hkv: int, Lq: int, Lk: int, plain: bool):
-    """(mode, groups of rows a KV head, parts of the keys (negative: joined in a cluster), predicted us) that
-    cover_attn_fwd_prefix8 takes (no device needed)."""
+def cover_debug_attn_prefix8_plan(B: int, Hq: int, Hkv: int, Lq: int, Lk: int, plain: bool, ranges: bool = False):
+    """(mode, groups of rows a KV head, parts of the keys (as nsplit of cover_debug_attn_prefix8), predicted us)
+    that cover_attn_fwd_prefix8 takes (no device needed)."""
     choice, us = (ctypes.c_int32 * 3)(), ctypes.c_double()
-    code = _lib.load().cover_debug_attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, 1 if plain else 0, ctypes.addressof(choice),
+    code = _lib.load().cover_debug_attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, 1 if plain else 0, 1 if ranges else 0, ctypes.addressof(choice),
                                                      ctypes.addressof(us))
     _lib.check("cover_debug_attn_prefix8_plan", code)
     return choice[0], choice[1], choice[2], us.value

@@ -10,7 +10,8 @@
 // The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r of head
 // hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view. A CTA takes a group of them against the KV tiles (128
 // keys) of one of nsplit parts of what its rows see; with nsplit > 1 the parts' CTAs are a cluster that adds up their (m, l, O)
-// in fp32 itself (rows and tile, up to 8 parts), or leave them in the workspace for a second kernel. Five ways, chosen by
+// in fp32 itself (rows and tile, up to 8 parts), or leave them in the workspace for a second kernel (the rows kernels' parts
+// of a batch with key ranges shared out to the sequences by their lengths, see share_of). Five ways, chosen by
 // plan_of from the sizes:
 //   rows (16 or 32 a group)  codes as 8-bit matrix operands, products turned over; bound by reading the memory
 //   tile (128 rows)          codes decoded to bf16 by the CTA; bound by decoding
@@ -63,6 +64,7 @@ static_assert(2 * 128 * kSoftmaxRegs + 2 * 128 * kDecodeRegs + 128 * kIssueRegs 
 static_assert(kSoftmaxRegs >= kLaunchRegs && kDecodeRegs <= kLaunchRegs && kIssueRegs <= kLaunchRegs, "register split");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kMaxParts = 64;              // of the keys
+constexpr int kMaxShared = 32;             // sequences that share the parts out by their lengths
 constexpr int kMaxJoined = 8;              // parts whose CTAs are a cluster (its portable size)
 constexpr int kSms = 152;                  // of this GPU; the split of the keys is chosen for it
 
@@ -103,11 +105,13 @@ struct Params {
   const int32_t* key_hi;
   __nv_bfloat16* out;
   float* lse;
-  float* part_o;     // [nsplit][rows][128]
-  float2* part_ml;   // [nsplit][rows]
+  float* part_o;     // [nsplit][rows][128]; shared out by length: [slots + B][rows / B][128]
+  float2* part_ml;   // as part_o's rows
+  int2* shares;      // [B] shared out by length: a sequence's first slot and its slots; or null
   int* status;
   long long rows;    // B * Hq * Lq
-  int n_seeds, Hq, Hkv, G, Lq, Lk, q0, n_groups, nsplit;
+  int B, n_seeds, Hq, Hkv, G, Lq, Lk, q0, n_groups, nsplit;
+  int slots;         // parts of a KV head that the sequences share
   int joined;        // the parts' CTAs are a cluster and add their results up themselves
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
@@ -383,6 +387,34 @@ __device__ __forceinline__ Part part_of(int lo, int hi, int ks, int nsplit) {
   const int t0 = hi > 0 ? lo / kBN : 0, t1 = hi > 0 ? (hi + kBN - 1) / kBN : 0;
   const int each = (t1 - t0) / nsplit, more = (t1 - t0) % nsplit;
   return Part{t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0)};
+}
+
+// Parts shared out to a batch's sequences by their lengths (rows kernels, with key ranges): of `slots` parts for a KV head every
+// sequence gets as many as its KV tiles need for parts of at most t, and t is the least for which they are enough.
+// Empty sequences have a part each, behind those. Returns the first part and the parts of sequence lane (all lanes
+// of a warp; B <= 32, B <= slots).
+__device__ __forceinline__ int2 share_of(const int* seq_lo, const int* seq_hi, int B, int slots) {
+  const int lane = threadIdx.x & 31;
+  int tiles = 0;
+  if (lane < B && seq_hi[lane] > 0) tiles = (seq_hi[lane] + kBN - 1) / kBN - seq_lo[lane] / kBN;
+  int hi = __reduce_max_sync(0xffffffffu, tiles), lo = max(1, (hi + kMaxParts - 1) / kMaxParts);   // t is among lo .. hi
+  hi = max(hi, lo);
+  while (lo < hi) {
+    const int t = (lo + hi) / 2;
+    if (__reduce_add_sync(0xffffffffu, (tiles + t - 1) / t) <= slots) hi = t;
+    else lo = t + 1;
+  }
+  const int n = (tiles + hi - 1) / hi;
+  int first = n;   // an inclusive sum over the sequences
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, first, d);
+    if (lane >= d) first += x;
+  }
+  const int all = __shfl_sync(0xffffffffu, first, 31);
+  const uint32_t empty = __ballot_sync(0xffffffffu, lane < B && n == 0);
+  if (n > 0) return make_int2(first - n, n);
+  return make_int2(all + __popc(empty & ((1u << lane) - 1u)), lane < B ? 1 : 0);
 }
 
 // What a row does not see of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1), keys whose V
@@ -1382,6 +1414,7 @@ struct RowsSmem {
   int slot[kN];
   uint32_t tmem_base;
   int abort;
+  int seq_lo[kMaxShared], seq_hi[kMaxShared];   // keys that some row of a sequence sees
   int lo, hi;                     // keys that some row sees
   int all_lo, all_hi;             // keys that every row sees
 };
@@ -1398,17 +1431,26 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   constexpr uint32_t kTmem = kN == 16 ? 256 : 512;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int ks = static_cast<int>(blockIdx.x) % p.nsplit;
-  int rest = static_cast<int>(blockIdx.x) / p.nsplit;
-  const int group = rest % p.n_groups;
-  rest /= p.n_groups;
-  const int hkv = rest % p.Hkv;
-  const int b = rest / p.Hkv;
+  // CTA (ks, group, hkv, b); with parts shared out to the sequences (hkv, group, part), so that those left over come last
+  const bool shared_out = p.shares != nullptr;
+  int ks, group, hkv, b = 0, slot = 0, nsplit = p.nsplit;
+  int rest = static_cast<int>(blockIdx.x);
+  if (shared_out) {
+    hkv = rest % p.Hkv;
+    rest /= p.Hkv;
+    group = rest % p.n_groups;
+    ks = slot = rest / p.n_groups;
+  } else {
+    ks = rest % nsplit;
+    rest /= nsplit;
+    group = rest % p.n_groups;
+    rest /= p.n_groups;
+    hkv = rest % p.Hkv;
+    b = rest / p.Hkv;
+  }
   const int n_packed = p.G * p.Lq;
   const int p0 = group * kN;
-  const int n_rows = min(kN, n_packed - p0);
-  const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
-  const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;
+  int n_rows = min(kN, n_packed - p0);
 
   if (warp == kRowsMmaWarp) {
     if (lane == 0) {
@@ -1446,12 +1488,40 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     sm.m[0][tid] = sm.m[1][tid] = 0.0f;
     sm.unseen[0][tid] = sm.unseen[1][tid] = tid < n_rows ? 1 : 0;
   }
+  if (tid < kMaxShared) {
+    sm.seq_lo[tid] = 0x7fffffff;
+    sm.seq_hi[tid] = 0;
+  }
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tbase = sm.tmem_base;
   griddep_wait();
   griddep_launch_dependents();
+
+  // ---------------- the sequence ----------------
+  if (shared_out) {
+    for (int i = tid; i < p.B * p.Lq; i += kRowsThreads) {
+      const int lo = p.key_lo != nullptr ? max(0, __ldg(p.key_lo + i)) : 0;
+      const int hi = p.key_hi != nullptr ? min(p.Lk, __ldg(p.key_hi + i)) : p.Lk;
+      if (lo < hi) {
+        atomicMin(&sm.seq_lo[i / p.Lq], lo);
+        atomicMax(&sm.seq_hi[i / p.Lq], hi);
+      }
+    }
+    __syncthreads();
+    const int2 share = share_of(sm.seq_lo, sm.seq_hi, p.B, p.slots);   // of the lane's sequence
+    const uint32_t mine = __ballot_sync(0xffffffffu, slot >= share.x && slot < share.x + share.y);
+    b = mine != 0 ? __ffs(mine) - 1 : 0;
+    ks = slot - __shfl_sync(0xffffffffu, share.x, b);
+    nsplit = __shfl_sync(0xffffffffu, share.y, b);
+    if (mine == 0) n_rows = 0, ks = nsplit;   // a part that is left over: no rows, no keys
+    if (blockIdx.x == 0 && tid < p.B) p.shares[tid] = share;
+  }
+  const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
+  const size_t mem0 = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;
+  // the part's first row, less the first row of what it is a part of
+  const long long part0 = shared_out ? (static_cast<long long>(slot) - b) * p.Hq * p.Lq : ks * p.rows;
 
   // ---------------- the rows ----------------
   const bool ranges = p.key_lo != nullptr || p.key_hi != nullptr;
@@ -1497,7 +1567,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   } else if (tid < kN) {
     sm.row[tid] = make_int4(0, p.Lk, -1, 0);   // read by the softmax warps, after their barrier
   }
-  const Part part = ranges ? part_of(sm.lo, sm.hi, ks, p.nsplit) : part_of(0, p.Lk, ks, p.nsplit);
+  Part part = ranges ? part_of(sm.lo, sm.hi, ks, nsplit) : part_of(0, p.Lk, ks, nsplit);
+  if (ks >= nsplit) part.nt = 0;
   const int j0 = part.j0, nt = part.nt;
 
   if (warp >= kRowsMmaWarp) {
@@ -1831,7 +1902,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (lane == (n & 31)) sm.red[stream][w4][n] = x;
     }
     softmax_sync();
-    const bool split = p.nsplit > 1;
+    const bool split = shared_out || p.nsplit > 1;
     const uint32_t staged = smem_u32(sm.k[0]);   // every product is complete: K is not read any more
     if (ok && tid < n_rows) {
       const int n = tid;
@@ -1849,7 +1920,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (s_self != s_self) sum = s_self;
       sm.fin[n] = make_float4(w0, w1, p_self, split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
       if (p.joined) sm.ml[n] = make_float2(top, sum);
-      else if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(top, sum);
+      else if (split) p.part_ml[part0 + orow] = make_float2(top, sum);
       else if (p.lse != nullptr) p.lse[orow] = (top + lg2_approx(sum)) * 0.6931471805599453f;
     }
     softmax_sync();
@@ -1884,7 +1955,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           if (f.z != 0.0f) o = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.slot[n]) * kD + col]), o);
           const long long orow = rowbase + p0 + n;
           if (p.joined) sts32(staged + staged_at(n, col >> 2) + 4 * (col & 3), __float_as_uint(o));
-          else if (split) p.part_o[(static_cast<size_t>(ks) * p.rows + orow) * kD + col] = o;
+          else if (split) p.part_o[(part0 + orow) * kD + col] = o;
           else p.out[orow * kD + col] = __float2bfloat16_rn(o * f.w);
         }
       }
@@ -1904,22 +1975,30 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 constexpr int kCombineWarps = 4;
 __global__ void __launch_bounds__(kCombineWarps * 32)
     attn_prefix8_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, int nsplit,
-                                long long rows, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
+                                const int2* shares, long long seq_rows, long long rows, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
   griddep_wait();
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31;
   const long long row = static_cast<long long>(blockIdx.x) * kCombineWarps + (threadIdx.x >> 5);
   if (row >= rows) return;
+  long long first = row, step = rows;   // the row in its first part, and from part to part
+  if (shares != nullptr) {
+    const long long b = row / seq_rows;
+    const int2 share = shares[b];
+    first = (share.x - b) * seq_rows + row;
+    nsplit = share.y;
+    step = seq_rows;
+  }
   float m = -INFINITY;
-  for (int j = lane; j < nsplit; j += 32) m = fmaxf(m, part_ml[j * rows + row].x);
+  for (int j = lane; j < nsplit; j += 32) m = fmaxf(m, part_ml[first + j * step].x);
   for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   const float m_use = m == -INFINITY ? 0.0f : m;
   float l = 0.0f;
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
   for (int j = 0; j < nsplit; ++j) {
-    const float2 ml = part_ml[j * rows + row];
-    const float4 o = *reinterpret_cast<const float4*>(part_o + (j * rows + row) * kD + 4 * lane);
+    const float2 ml = part_ml[first + j * step];
+    const float4 o = *reinterpret_cast<const float4*>(part_o + (first + j * step) * kD + 4 * lane);
     const float w = ml.x == -INFINITY ? 0.0f : ex2_approx(ml.x - m_use);
     l = fmaf(w, ml.y, l);
     // parts that saw no key hold zeros; what rounds a weight to zero adds nothing
@@ -1948,10 +2027,14 @@ float fixed_reference(float cap_log2) {
   return cap_log2 >= 1.0f / 1024.0f && cap_log2 <= 75.0f ? fmaxf(0.0f, cap_log2 - 45.0f) : -INFINITY;
 }
 
+// Whether the parts of a batch with key ranges can be shared out to its sequences (every CTA looks through the ranges).
+bool shares_out(int B, int Lq) { return B > 1 && B <= kMaxShared && static_cast<long long>(B) * Lq <= 2048; }
+
 struct Plan {
   Mode mode;
   int n_groups, nsplit;
   bool joined;   // the parts' CTAs are clusters
+  int slots;     // parts of a KV head shared out to the sequences (0: nsplit each)
   double us;
 };
 
@@ -1977,9 +2060,10 @@ struct ModeCost {
 constexpr ModeCost kCosts[kReadBack] = {
     {2.2, 4.5, 0.72, 0.8, 6.4e-4, 0.8, 0.07}, {2.4, 6.0, 0.92, 0.8, 4.8e-4, 0.6, 0.13},
     {3.0, 4.1, 1.34, 1.5, 2.5e-4, 2.0, 0.036}, {5.0, 3.5, 1.72, 2.4, 1.9e-4, 0.0, 0.0}};
+constexpr double kFill = 0.75, kShareUs = 1.0;
 constexpr double kPartUs = 0.15, kDecodeRowUs = 1.0e-4, kDecodeUs = 1.8;
 
-Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
+Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain, bool ranges) {
   Plan best{};
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
   const double rows = static_cast<double>(B) * Hq * Lq, decode_us = kDecodeRowUs * B * Hkv * L;
@@ -1994,14 +2078,24 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
       const int tiles = (nkv + ns - 1) / ns;
       const double us = k.base + waves * (k.wave + k.tile * tiles) + (mode == kDecodedPairs ? decode_us : 0.0) +
                         (ns > 1 ? k.combine + kPartUs * ns + k.row * rows * ns : 0.0);
-      if (best.nsplit == 0 || us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, false, us};
+      if (best.nsplit == 0 || us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, false, 0, us};
       if (mode != kDecodedPairs && ns > 1 && ns <= kMaxJoined) {
         const long long turns = (units + kJoinedClusters[ns - 1] - 1) / kJoinedClusters[ns - 1];
         const double own_rows = std::ceil(std::min<double>(packed, kModeRows[mode]) / ns);
         const double join_us = k.base + turns * (k.wave + k.tile * tiles + k.join + k.join_row * own_rows);
-        if (join_us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, true, join_us};
+        if (join_us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), ns, true, 0, join_us};
       }
       if (units * ns > 8 * kSms) break;
+    }
+    if (ranges && mode <= kRows32 && shares_out(B, Lq)) {
+      // one wave of parts, of kFill of the memories' tiles. Rounded to whole parts the sequences' shares are fair from three
+      // parts a sequence on: 4 x 32 / 8 heads over 131072, 79828, 102273 and 0 keys 117 us (9 parts each 145; with all
+      // four full 205 and 197), 8 x 28 / 4 over 15681 to 40000 keys 51 (joined in fours 72), but 16 x 32 / 8 over 2786
+      // to 8192 keys 59 (57 without parts). Two waves of parts: 132, 64, 53.
+      const long long slots = std::min<long long>(kSms / (groups * Hkv), static_cast<long long>(B) * kMaxParts);
+      const double tiles = std::ceil(kFill * B * nkv / std::max<long long>(slots, 1)) + 1, parts = static_cast<double>(slots) / B;
+      const double us = k.base + kShareUs + k.wave + k.tile * tiles + k.combine + kPartUs * parts + k.row * rows * parts;
+      if (slots >= 3 * B && us < best.us) best = Plan{static_cast<Mode>(mode), static_cast<int>(groups), 1, false, static_cast<int>(slots), us};
     }
   }
   if (plain) {
@@ -2011,7 +2105,7 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain) {
     const WindowChoice c = window_gqa_model(a, kSms, kClusters);
     if (c.packed) us = std::min(us, c.packed_us);
     us += kDecodeUs + decode_us;
-    if (us < best.us) best = Plan{kReadBack, 1, 1, false, us};
+    if (us < best.us) best = Plan{kReadBack, 1, 1, false, 0, us};
   }
   return best;
 }
@@ -2029,44 +2123,59 @@ constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSm
 static_assert(kRowsSmemBytes[0] <= 227 * 1024 && kRowsSmemBytes[1] <= 227 * 1024, "shared memory of a CTA");
 
 // The workspace: the parts' accumulators and sums, or the decoded K and V (both where both are needed).
-size_t part_bytes(long long rows, int nsplit) {
-  return nsplit <= 1 ? 0 : (static_cast<size_t>(rows) * nsplit * (kD * sizeof(float) + sizeof(float2)) + 15) & ~size_t{15};
-}
 size_t decoded_bytes(const Plan& plan, int B, int Hkv, int L) {
   return plan.mode >= kDecodedPairs ? static_cast<size_t>(B) * Hkv * L * kD * 2 : 0;   // of K, and of V
 }
+// rows of all parts
+size_t part_rows(const Plan& plan, int B, int Hq, int Lq) {
+  if (plan.slots > 0) return static_cast<size_t>(plan.slots + B) * Hq * Lq;
+  return plan.nsplit <= 1 || plan.joined ? 0 : static_cast<size_t>(B) * Hq * Lq * plan.nsplit;
+}
 size_t plan_bytes(const Plan& plan, int B, int Hq, int Hkv, int Lq, int L) {
-  return 2 * decoded_bytes(plan, B, Hkv, L) + (plan.joined ? 0 : part_bytes(static_cast<long long>(B) * Hq * Lq, plan.nsplit));
+  const size_t parts = part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2));
+  return 2 * decoded_bytes(plan, B, Hkv, L) + (plan.slots > 0 ? parts + kMaxShared * sizeof(int2) : (parts + 15) & ~size_t{15});
+}
+
+// The keys' parts as one number: 1 .. 64 for the second kernel, -2 .. -8 joined, kSharedCode + the parts shared out.
+int parts_code(const Plan& p) { return p.slots > 0 ? kAttn8SharedCode + p.slots : p.joined ? -p.nsplit : p.nsplit; }
+void set_parts(Plan& p, int code) {
+  p.slots = code > kAttn8SharedCode ? code - kAttn8SharedCode : 0;
+  p.joined = code < 0;
+  p.nsplit = p.slots > 0 ? 1 : std::abs(code);
 }
 
 }  // namespace
 
 size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L) {
-  return std::max(plan_bytes(plan_of(B, Hq, Hkv, Lq, L, false), B, Hq, Hkv, Lq, L),
-                  plan_bytes(plan_of(B, Hq, Hkv, Lq, L, true), B, Hq, Hkv, Lq, L));
+  size_t most = 0;
+  for (int i = 0; i < 3; ++i)
+    most = std::max(most, plan_bytes(plan_of(B, Hq, Hkv, Lq, L, i == 0, i == 1), B, Hq, Hkv, Lq, L));
+  return most;
 }
 
-void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, int* choice, double* us) {
-  const Plan p = plan_of(B, Hq, Hkv, Lq, L, plain);
+void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, bool ranges, int* choice, double* us) {
+  const Plan p = plan_of(B, Hq, Hkv, Lq, L, plain, ranges);
   choice[0] = p.mode;
   choice[1] = p.n_groups;
-  choice[2] = p.joined ? -p.nsplit : p.nsplit;
+  choice[2] = parts_code(p);
   *us = p.us;
 }
 
-size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit) {
-  return plan_bytes(Plan{static_cast<Mode>(mode), 1, std::abs(nsplit), nsplit < 0, 0.0}, B, Hq, Hkv, Lq, L);
+size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int parts) {
+  Plan p{static_cast<Mode>(mode), 1, 1, false, 0, 0.0};
+  set_parts(p, parts);
+  return plan_bytes(p, B, Hq, Hkv, Lq, L);
 }
 
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
   if (rows + 2 * kBM > 0x7fffffffLL) return -2;
-  const bool plain = a.key_lo == nullptr && a.key_hi == nullptr && !(a.softcap > 0.0f);
-  Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.L, plain);
+  const bool ranges = a.key_lo != nullptr || a.key_hi != nullptr;
+  Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.L, !ranges && !(a.softcap > 0.0f), ranges);
   if (a.mode >= 0) {   // a debug call says which
     plan.mode = static_cast<Mode>(a.mode);
-    plan.nsplit = std::abs(a.nsplit);
-    plan.joined = a.nsplit < 0;
+    set_parts(plan, a.parts);
+    if (plan.slots > 0 && (plan.mode > kRows32 || !ranges || !shares_out(a.B, a.Lq) || plan.slots < a.B)) return -2;
     plan.n_groups = static_cast<int>((static_cast<long long>(a.Hq / a.Hkv) * a.Lq + kModeRows[a.mode] - 1) / kModeRows[a.mode]);
   }
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
@@ -2083,7 +2192,7 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
     const int rc = try_launch_attn_window_gqa(w, status, stream, false);
     return rc != kWindowGqaNotTaken ? rc : launch_attn_bf16_sm103(w, status, stream);
   }
-  const long long grid = static_cast<long long>(plan.n_groups) * a.Hkv * a.B * plan.nsplit;
+  const long long grid = static_cast<long long>(plan.n_groups) * a.Hkv * (plan.slots > 0 ? plan.slots + a.B : a.B * static_cast<long long>(plan.nsplit));
   if (grid > 0x7fffffffLL) return -2;
   static ContextCache<int> setup;
   int unused = 0;
@@ -2130,9 +2239,12 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.out = static_cast<__nv_bfloat16*>(a.out);
   p.lse = a.lse;
   p.part_o = reinterpret_cast<float*>(ws + 2 * kv_bytes);
-  p.part_ml = reinterpret_cast<float2*>(p.part_o + static_cast<size_t>(rows) * plan.nsplit * kD);
+  const size_t parts = part_rows(plan, a.B, a.Hq, a.Lq);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + parts * kD);
+  if (plan.slots > 0) p.shares = reinterpret_cast<int2*>(p.part_ml + parts);
   p.status = status;
   p.rows = rows;
+  p.B = a.B;
   p.n_seeds = a.n_seeds;
   p.Hq = a.Hq;
   p.Hkv = a.Hkv;
@@ -2142,6 +2254,7 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.q0 = a.q0;
   p.n_groups = plan.n_groups;
   p.nsplit = plan.nsplit;
+  p.slots = plan.slots;
   p.joined = plan.joined ? 1 : 0;
   p.scale_log2 = log2e / root;
   const bool cap = a.softcap > 0.0f;
@@ -2168,11 +2281,12 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   if (few) e = cudaLaunchKernelEx(&cfg, kRowsKernels[m][cap ? 1 : 0], tk, tv, p);
   else if (decoded) e = cudaLaunchKernelEx(&cfg, kPairKernels[cap ? 1 : 0], tq, tk, tv, p);
   else e = cudaLaunchKernelEx(&cfg, kTileKernels[cap ? 1 : 0], tq, p);
-  if (e == cudaSuccess && plan.nsplit > 1 && !plan.joined) {
+  if (e == cudaSuccess && parts > 0) {
     cfg = pdl_config(dim3(static_cast<unsigned>((rows + kCombineWarps - 1) / kCombineWarps)), dim3(kCombineWarps * 32), 0,
                      stream, pdl);
     e = cudaLaunchKernelEx(&cfg, attn_prefix8_combine_kernel, static_cast<const float*>(p.part_o),
-                           static_cast<const float2*>(p.part_ml), plan.nsplit, rows, p.out, p.lse);
+                           static_cast<const float2*>(p.part_ml), plan.nsplit,
+                           static_cast<const int2*>(p.shares), static_cast<long long>(a.Hq) * a.Lq, rows, p.out, p.lse);
   }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }

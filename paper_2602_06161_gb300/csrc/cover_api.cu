@@ -277,7 +277,7 @@ static int attn_prefix8_call(cover::Attn8Args a, int D, size_t workspace_bytes, 
   if (!(a.softcap >= 0.0f) || a.softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
   if (D != 128) return COVER_ERR_UNSUPPORTED;
   const size_t need = a.mode < 0 ? cover::attn_prefix8_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L)
-                                 : cover::attn_prefix8_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L, a.mode, a.nsplit);
+                                 : cover::attn_prefix8_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L, a.mode, a.parts);
   if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return COVER_ERR_INVALID_ARG;
   int* st = status_block();
   if (st == nullptr) return COVER_ERR_CUDA;
@@ -486,7 +486,8 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8, cons
                              int B, int Hq, int Hkv, int Lq, int Lk, int q0, int D, const int32_t* key_lo,
                              const int32_t* key_hi, float softcap, void* out, float* lse, void* workspace,
                              size_t workspace_bytes, int mode, int nsplit, void* stream) {
-  if (mode < 0 || mode >= cover::kAttn8Modes || nsplit < -8 || nsplit > 64 || nsplit == 0 || nsplit == -1)
+  if (mode < 0 || mode >= cover::kAttn8Modes || nsplit < -8 || nsplit == 0 || nsplit == -1 ||
+      (nsplit > 64 && nsplit <= cover::kAttn8SharedCode) || nsplit > cover::kAttn8SharedCode + 4096)
     return COVER_ERR_INVALID_ARG;
   if (nsplit < 0 && mode > cover::kAttn8Tile) return COVER_ERR_UNSUPPORTED;
   if (mode == cover::kAttn8ReadBack && (nsplit != 1 || key_lo != nullptr || key_hi != nullptr || softcap != 0.0f))
@@ -494,14 +495,16 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8, cons
   cover::Attn8Args a{q,  k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, n_seeds, B,   Hq,       Hkv,
                      Lq, Lk, q0, key_lo, key_hi, softcap,  out,        lse,      workspace};
   a.mode = mode;
-  a.nsplit = nsplit;
+  a.parts = nsplit;
   return attn_prefix8_call(a, D, workspace_bytes, stream);
 }
 
-int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int32_t* choice, double* us) {
-  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Lq < 1 || Lk < Lq || choice == nullptr || us == nullptr)
+int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int ranges, int32_t* choice,
+                                  double* us) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Lq < 1 || Lk < Lq || choice == nullptr || us == nullptr ||
+      (plain != 0 && ranges != 0))
     return COVER_ERR_INVALID_ARG;
-  cover::attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, plain != 0, choice, us);
+  cover::attn_prefix8_plan(B, Hq, Hkv, Lq, Lk, plain != 0, ranges != 0, choice, us);
   return COVER_OK;
 }
 

@@ -191,14 +191,15 @@ struct Attn8Args {
   void* out;
   float* lse;
   void* workspace;
-  int mode = -1, nsplit = 0;   // debug calls: the kernel and the parts of the keys, whatever the plan says
+  int mode = -1, parts = 0;   // debug calls: the kernel and the parts of the keys, whatever the plan says
 };
 constexpr int kAttn8Modes = 5;      // attn_prefix8.cu's Mode
-constexpr int kAttn8Tile = 2, kAttn8ReadBack = 4;
+constexpr int kAttn8Rows32 = 1, kAttn8Tile = 2, kAttn8ReadBack = 4;
+constexpr int kAttn8SharedCode = 100;   // 100 + n: n parts of a KV head, shared out to the sequences
 size_t attn_prefix8_workspace_bytes(int B, int Hq, int Hkv, int Lq, int L);
-size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int nsplit);
+size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, int parts);
 // choice: mode, groups of rows a KV head, parts of the keys; us: predicted. plain: no key ranges, no cap.
-void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, int* choice, double* us);
+void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, bool ranges, int* choice, double* us);
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream);
 
 int launch_umma_tile(const void* a, const void* b, const void* p, const void* v, float* c1, float* c2, int* status,

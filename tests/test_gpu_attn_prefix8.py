@@ -258,6 +258,22 @@ def test_every_kernel(shape, mode, nsplit):
         _check(d, out, lse, lo, hi, cap)
 
 
+@pytest.mark.parametrize("mode,more", [(0, 0), (0, 1), (0, 70), (1, 5)])
+@pytest.mark.parametrize("B,Lq,lens", [(5, 2, [900, 0, 130, 1, 511]), (32, 1, [900] + [0] * 30 + [3]), (3, 4, [0, 0, 0]), (2, 9, [900, 900])])
+def test_parts_of_uneven_sequences(B, Lq, lens, mode, more):
+    """A batch's parts go to its sequences by their lengths: long ones among empty ones, all empty, all alike; as many parts as
+    sequences, and more than there are KV tiles."""
+    d = _inputs(B, 8, 2, Lq, 900, 3, 500)
+    hi = torch.tensor([[n] * Lq for n in lens], device="cuda", dtype=torch.int32)
+    lo = (hi // 3).contiguous()
+    lo[:, 0] = 0
+    for kw in (dict(key_hi=hi), dict(key_lo=lo, key_hi=hi), dict(key_lo=lo)):
+        out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], d["km"], d["vm"], d["seeds"], q0=500, mode=mode, nsplit=100 + B + more, **kw)
+        torch.cuda.synchronize()
+        assert api.cover_device_status() == 0
+        _check(d, out, lse, kw.get("key_lo"), kw.get("key_hi"))
+
+
 @pytest.mark.parametrize("mode,nsplit", [(0, 8), (1, 5), (2, 7)])
 def test_parts_joined_in_a_cluster(mode, nsplit):
     """The same parts added up by the cluster and by the second kernel: their terms differ by a rounding of the weights at most,
@@ -394,7 +410,8 @@ def test_refusals():
     with pytest.raises(ValueError, match="out must match"):
         api.cover_attn_fwd_prefix8(*a, q0=0, out=torch.empty((1, 4, 7, 128), device="cuda", dtype=torch.bfloat16))
     for kw in (dict(mode=5), dict(mode=-1), dict(mode=0, nsplit=0), dict(mode=2, nsplit=65), dict(mode=4, nsplit=2), dict(mode=4, softcap=1.0),
-               dict(mode=0, nsplit=-1), dict(mode=2, nsplit=-9), dict(mode=3, nsplit=-2), dict(mode=4, nsplit=-2)):
+               dict(mode=0, nsplit=-1), dict(mode=2, nsplit=-9), dict(mode=3, nsplit=-2), dict(mode=4, nsplit=-2), dict(mode=0, nsplit=100), dict(mode=0, nsplit=110),
+               dict(mode=0, nsplit=4197)):
         with pytest.raises(CoverError):
             api.cover_debug_attn_prefix8(*a, q0=0, **kw)
     small = api.kv8_memory(1, 2, 64, 64)
