@@ -276,9 +276,12 @@ static int attn_prefix8_call(cover::Attn8Args a, int D, size_t workspace_bytes, 
     return COVER_ERR_INVALID_ARG;
   if (!(a.softcap >= 0.0f) || a.softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
   if (D != 128) return COVER_ERR_UNSUPPORTED;
-  const size_t need = a.mode < 0 ? cover::attn_prefix8_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L)
-                                 : cover::attn_prefix8_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L, a.mode, a.parts);
-  if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return COVER_ERR_INVALID_ARG;
+  if (a.mode >= 0) {
+    const size_t need = cover::attn_prefix8_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L, a.mode, a.parts);
+    if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return COVER_ERR_INVALID_ARG;
+  } else if (a.workspace == nullptr && cover::attn_prefix8_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.L) > 0) {
+    return COVER_ERR_INVALID_ARG;
+  }
   int* st = status_block();
   if (st == nullptr) return COVER_ERR_CUDA;
   return cover::launch_attn_prefix8(a, st, static_cast<cudaStream_t>(stream));
