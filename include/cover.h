@@ -321,7 +321,8 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  *     only (held to 0 .. Lk): a padded batch's lengths, a prefix, blocks that see themselves and
  *     those before, documents. A row that sees no key gets out = 0, lse = -inf.
  *     A seed row's own pair is seen where its position is.
- *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c).
+ *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c)
+ *     (c above 2^60 counts as 2^60).
  * What a row does not see does not reach it, NaN included; a row that sees a key with k_exp or
  * v_exp above 246 gets NaN in out and lse. (A NaN code, 0x7f or 0xff, which cover_kv8_write does
  * not write, counts as NaN or as 480 where it is seen.)

@@ -155,6 +155,7 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // Chebyshev nodes of z in [0, 0.16] by least squares, off by at most 1e-7 of it (2e-7 in fp32). Scores are seldom above
 // 0.4 of their cap, and then two special-function operations an element are saved.
 constexpr float kTanhRange = 0.4f;
+constexpr float kMaxCap = 1.1529215e18f;   // 2^60: larger caps count as this one; its reciprocal times the rows' scales is a normal number
 constexpr float kTanh0 = 0.999999903f, kTanh1 = -0.333313733f, kTanh2 = 0.132711566f, kTanh3 = -0.0475610772f;
 
 // Shared memory by its 32-bit address.
@@ -176,11 +177,16 @@ __device__ __forceinline__ uint32_t prmt(uint32_t x) {
   return d;
 }
 
-// A capped score in log2 units, c tanh(s / c) log2(e) = C (1 - 2 / (1 + e^{2 s / c})), C = c log2(e); the
-// infinite and the vanishing exponential give the caps themselves.
+// A capped score in log2 units, c tanh(s / c) log2(e) = C (1 - 2 / (1 + 2^y)), C = c log2(e), y = 2 log2(e) s / c
+// (y = s cap_in); the infinite and the vanishing exponential give the caps themselves. That is off by 2^-23 of the cap, so
+// for |s / c| <= 0.4 it is C x P(x^2) instead, off by 2e-7 of the score: a cap far above the scores changes nothing.
 __device__ __forceinline__ float capped(float s, float cap_in, float cap_log2) {
-  const float t = ex2_approx(s * cap_in);
-  return fmaf(-2.0f * cap_log2, rcp_approx(1.0f + t), cap_log2);
+  constexpr float kX = 0.34657359f, kX2 = kX * kX;   // x = y ln(2) / 2
+  constexpr float a0 = kTanh0 * kX, a1 = kTanh1 * kX * kX2, a2 = kTanh2 * kX * kX2 * kX2, a3 = kTanh3 * kX * kX2 * kX2 * kX2;
+  const float y = s * cap_in, z = y * y;
+  const float far = fmaf(-2.0f * cap_log2, rcp_approx(1.0f + ex2_approx(y)), cap_log2);
+  const float near = cap_log2 * y * fmaf(z, fmaf(z, fmaf(z, a3, a2), a1), a0);
+  return fabsf(y) <= kTanhRange / kX ? near : far;
 }
 
 // Decodes a row of codes, eight 16-byte pieces, into its row of a bf16 tile (two 64-column boxes, 16-byte chunks swizzled by row & 7). An e4m3 code's bits s eeee mmm, moved to s 0000eeee mmm0000, are
@@ -2258,9 +2264,10 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.joined = plan.joined ? 1 : 0;
   p.scale_log2 = log2e / root;
   const bool cap = a.softcap > 0.0f;
-  p.cap_log2 = a.softcap * log2e;
-  p.cap_in = cap ? 2.0f * log2e / (a.softcap * root) : 0.0f;
-  p.cap_x = cap ? 1.0f / (a.softcap * root) : 0.0f;
+  const float softcap = fminf(a.softcap, kMaxCap);
+  p.cap_log2 = softcap * log2e;
+  p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
+  p.cap_x = cap ? 1.0f / (softcap * root) : 0.0f;
   p.cap_ref = cap ? fixed_reference(p.cap_log2) : -INFINITY;
   const float tanh_poly[4] = {kTanh0, kTanh1, kTanh2, kTanh3};
   float power = p.cap_log2 * p.cap_x;

@@ -60,9 +60,9 @@ def _reference(d, key_lo=None, key_hi=None, softcap=0.0):
                         q0=d["q0"], key_lo=n(key_lo), key_hi=n(key_hi), softcap=softcap)
 
 
-def _check(d, out, lse, key_lo=None, key_hi=None, softcap=0.0):
+def _check(d, out, lse, key_lo=None, key_hi=None, softcap=0.0, per_score=2.0 ** -20):
     ref, ref_lse, mass, size = _reference(d, key_lo, key_hi, softcap)
-    delta = (2.0 ** -20 * size + 2.0 ** -20 * softcap)[..., None]
+    delta = (per_score * size + 2.0 ** -20 * softcap)[..., None]
     tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 4 * delta) * mass * (1 + 2.0 ** -6)
     err = np.abs(_h(out) - ref)
     assert (err <= tol).all(), float((err / np.maximum(tol, 1e-30)).max())
@@ -117,6 +117,20 @@ def test_capped_scores(cap, kind):
     lo, hi = _ranges(kind, B, Lq, Lk, q0)
     out, lse = _run(d, key_lo=lo, key_hi=hi, softcap=cap)
     _check(d, out, lse, lo, hi, cap)
+
+
+@pytest.mark.parametrize("cap", [3e5, 1e9, 1e18, 3e38])
+@pytest.mark.parametrize("mode", range(4))
+def test_caps_far_above_the_scores(cap, mode):
+    """They change nothing: c tanh(s / c) is s but for (s / c)^2 / 3 < 2^-30 of it. The polynomial is off by 2^-22 of the score and six
+    roundings of 2^-24, which with what an uncapped score is off by is at most 2^-19 of sum |q_i k_i| / sqrt(D)."""
+    d = _inputs(2, 8, 2, 30, 500, 6, 400, scale=2.0)
+    lo, hi = _ranges("prefix", 2, 30, 500, 400)
+    out, lse = api.cover_debug_attn_prefix8(d["q"], *d["mem"], d["km"], d["vm"], d["seeds"], q0=400, mode=mode, key_lo=lo, key_hi=hi,
+                                            softcap=cap)
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+    _check(d, out, lse, lo, hi, per_score=2.0 ** -19)
 
 
 @pytest.mark.parametrize("scale", [0.01, 8.0, 60.0])
