@@ -204,3 +204,32 @@ def test_a_padded_batch_ends_where_its_sequences_end():
             x[b, :, 100 + m if m else 0:] = 255
     again, lse2 = api.cover_attn_fwd_prefix8(q, *mem, q0=100, key_hi=hi)
     assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+def test_lengths_that_change_between_replays():
+    """A captured call follows the lengths that its key ranges hold when it is replayed (parts are shared out on the device)."""
+    B, Hq, Hkv, L = 3, 32, 8, 20000
+    assert api.cover_debug_attn_prefix8_plan(B, Hq, Hkv, 1, L, False, True)[2] > 100
+    mem, q = _mem(B, Hkv, L, 140), _r(B, Hq, 1, 128, seed=141)
+    hi = torch.full((B, 1), L, device="cuda", dtype=torch.int32)
+    api.cover_attn_fwd_prefix8(q, *mem, q0=0, key_hi=hi)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out, lse = api.cover_attn_fwd_prefix8(q, *mem, q0=0, key_hi=hi)
+    k, v = (t.double() for t in api.cover_kv8_read(*mem, dtype=torch.float32))
+    for lens in ([20000, 20000, 20000], [1, 19999, 0], [0, 0, 0], [0, 0, 12345], [4000, 8000, 20000]):
+        hi.copy_(torch.tensor(lens, dtype=torch.int32)[:, None])
+        g.replay()
+        torch.cuda.synchronize()
+        assert api.cover_device_status() == 0
+        for b, n in enumerate(lens):
+            if n == 0:
+                assert not out[b].any() and (lse[b] == -float("inf")).all()
+                continue
+            s = torch.einsum("hgd,hnd->hgn", q[b, :, 0].double().view(Hkv, Hq // Hkv, 128), k[b, :, :n]) / 128 ** 0.5
+            w = torch.softmax(s, -1)
+            want, mass = torch.einsum("hgn,hnd->hgd", w, v[b, :, :n]), torch.einsum("hgn,hnd->hgd", w, v[b, :, :n].abs())
+            # weights rounded to 9 bits or bf16 (2^-8), scores off by 2^-20 of sum |q_i k_i| / sqrt(D) <= 2^7, the output to bf16
+            err = (out[b, :, 0].double().view_as(want) - want).abs()
+            assert (err <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 4 * 2.0 ** -13) * mass).all()
+            assert (lse[b, :, 0].double().view(Hkv, -1) - torch.logsumexp(s, -1)).abs().max() <= 2.0 ** -13 + 2.0 ** -15
