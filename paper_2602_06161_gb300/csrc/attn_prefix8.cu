@@ -794,7 +794,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       for (int j = 0; j < nt && ok; ++j) {
         const int s = j & 1;
-        ok = wait(&ctl.p_full[s], j >> 1) && wait(&ctl.v_full[s], j >> 1);
+        ok = wait(&ctl.v_full[s], j >> 1) && wait(&ctl.p_full[s], j >> 1);
         if (!ok) break;
         issue_pv(s, s, j > 1);
         umma_commit(&ctl.v_empty[s]);
@@ -993,9 +993,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------
 // A memory that many Q tiles read is decoded once, into the workspace (a row whose K or V is NaN has a NaN key and a zero
 // value there), and a CTA takes two Q tiles, one a stream, that read each KV tile together. Two threads of different
-// warpgroups share a row, 64 columns each, in two chunks of 32. 2048 rows over 8192 keys, 32 / 8 heads: 240 us, capped
-// at 30 283 (8 us of them decode the memory); 1216 rows, which fill the GPU's 152 SMs once, 124 us, 1310 TFLOP/s. With a thread
-// a row and its 128 columns unrolled it was 235 and 333 us: see finish_scores.
+// warpgroups share a row, 64 columns each, in two chunks of 32. 2048 rows over 8192 keys, 32 / 8 heads: 222 us, capped
+// at 30 261 (8 us of them decode the memory); 1216 rows, which fill the GPU's 152 SMs once, 116 us, 1400 TFLOP/s: a KV tile takes
+// 1.6 us, the products 1.1 of them; each Q tile's chain (S, maxima, exponentials, P V) is longer than the other's products. With a
+// thread a row and its 128 columns unrolled it was 235 and 333 us: see finish_scores. One CTA an SM that walks over even shares of all
+// tiles, units cut where a share ends, was tried: 1216 rows 130 us (a KV tile takes 0.1 us longer in such a loop), 2048 232 and 263.
 // Roles (640 threads): warps 0-15 softmax (warpgroup 2 t + h: columns 64 h .. 64 h + 63 of Q tile t); 16 products; 17, 18
 // copies of K, V.
 // P of a half overwrites the first 32 columns of that half's scores, behind its loads.
@@ -1108,25 +1110,28 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
       const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
       const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
+      const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
+      const uint32_t qk_hi = static_cast<uint32_t>(dq >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+      // What this thread does between a barrier and its products is on every tile's way: descriptors are added up in their
+      // lower words, and of several barriers the one that completes last is waited for last (1216 rows over 8192 keys 124 -> 116 us).
+      const auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
       // S[s] = Q[s] . K(stage)^T
       auto issue_s = [&](int s, int st) {
-        uint64_t a = dq + s * kTileDesc, kb = dk + st * kTileDesc;
-        asm volatile("" : "+l"(a), "+l"(kb));   // descriptors are added up here, not kept in registers
+        const uint32_t a = q_lo + s * static_cast<uint32_t>(kTileDesc), kb = k_lo + st * static_cast<uint32_t>(kTileDesc);
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
-          const uint64_t off = static_cast<uint64_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
-          umma_ss(tbase + s * kBN, a + off, kb + off, id_qk, kk > 0 ? 1u : 0u);
+          const uint32_t off = static_cast<uint32_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
+          umma_ss(tbase + s * kBN, desc(a + off, qk_hi), desc(kb + off, qk_hi), id_qk, kk > 0 ? 1u : 0u);
         }
         umma_commit(&ctl.s_full[s]);
       };
       // O[s] (+)= P[s] . V(stage)
       auto issue_pv = [&](int s, int st, bool acc) {
-        uint64_t vb = dv + st * kTileDesc;
-        asm volatile("" : "+l"(vb));
+        const uint32_t vb = v_lo + st * static_cast<uint32_t>(kTileDesc);
 #pragma unroll
         for (int kk = 0; kk < kBN / 16; ++kk)
           umma_ts(tbase + 2 * kBN + s * kD, tbase + s * kBN + (kk >> 2) * kHalf + 8 * (kk & 3),
-                  vb + static_cast<uint64_t>((kk * 2048) >> 4), id_pv, (acc || kk > 0) ? 1u : 0u);
+                  desc(vb + static_cast<uint32_t>((kk * 2048) >> 4), v_hi), id_pv, (acc || kk > 0) ? 1u : 0u);
       };
       auto wait = [&](uint64_t* bar, int phase) {
         const bool ok = mbar_wait(bar, phase & 1, &ctl.abort);
@@ -1142,14 +1147,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < nt && ok; ++j) {
         const int st = j & 1;
         const bool next = j + 1 < nt;
-        ok = wait(&ctl.p_full[0], j) && wait(&ctl.v_full[st], j >> 1);
+        ok = (!next || wait(&ctl.k_full[st ^ 1], (j + 1) >> 1)) && wait(&ctl.v_full[st], j >> 1) && wait(&ctl.p_full[0], j);
         if (!ok) break;
         issue_pv(0, st, j > 0);
-        if (next) {
-          ok = wait(&ctl.k_full[st ^ 1], (j + 1) >> 1);
-          if (!ok) break;
-          issue_s(0, st ^ 1);
-        }
+        if (next) issue_s(0, st ^ 1);
         if (two_tiles) {
           ok = wait(&ctl.p_full[1], j);
           if (!ok) break;
@@ -1637,7 +1638,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         if (ok) issue_s(j);
       }
       for (int j = 0; j < nt && ok; ++j) {
-        ok = wait(&sm.p_full[j & 1], j >> 1) && wait(&sm.v_clean[j % kStages], j / kStages);
+        ok = wait(&sm.v_clean[j % kStages], j / kStages) && wait(&sm.p_full[j & 1], j >> 1);
         if (!ok) break;
         issue_o(j);
         if (j + 2 < nt) {
@@ -2056,8 +2057,8 @@ constexpr int kJoinedClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
 // keys, batches of 1 to 16, 1 to 64 parts; off by 4 to 9 % in the mean, at most 40 %): a base, and for every wave of one
 // CTA an SM a start and a time per KV tile; where the keys are in parts, the second kernel's start, its walk over the
 // parts, and the parts' rows, or, joined in a cluster, the cluster's barriers and the rows that a CTA finishes. Decoding a
-// memory takes 1e-4 us a row. In each of the 24 the call's choice took at most 4 % longer than the fastest of all
-// kernels and parts. Joined against added up by a second kernel, each with its best parts: 8.3 against 10.0 us (1 x 28 / 4
+// memory takes 1e-4 us a row. In each of the 24 the call's choice took at most 5 % longer than the fastest of all
+// kernels and parts (one of them 9 %, where two launches would be faster on the device and slower on the host). Joined against added up by a second kernel, each with its best parts: 8.3 against 10.0 us (1 x 28 / 4
 // heads, 1 x 777), 10.3 / 11.9 (1 x 4000), 12.9 / 15.1 (1 x 32 / 8, 128 x 1024), 22.7 / 24.8 (4 x 16 / 2, 64 x 4096);
 // the second kernel's where more than 8 parts pay: 22.5 / 19.5 (1 x 28 / 4, 32 x 8192).
 struct ModeCost {
@@ -2065,7 +2066,7 @@ struct ModeCost {
 };
 constexpr ModeCost kCosts[kReadBack] = {
     {2.2, 4.5, 0.72, 0.8, 6.4e-4, 0.8, 0.07}, {2.4, 6.0, 0.92, 0.8, 4.8e-4, 0.6, 0.13},
-    {3.0, 4.1, 1.34, 1.5, 2.5e-4, 2.0, 0.036}, {5.0, 3.5, 1.72, 2.4, 1.9e-4, 0.0, 0.0}};
+    {3.0, 4.1, 1.34, 1.5, 2.5e-4, 2.0, 0.036}, {5.0, 3.5, 1.60, 2.4, 1.9e-4, 0.0, 0.0}};
 constexpr double kFill = 0.75, kShareUs = 1.0;
 constexpr double kPartUs = 0.15, kDecodeRowUs = 1.0e-4, kDecodeUs = 1.8;
 
@@ -2107,7 +2108,7 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int L, bool plain, bool ranges) {
   if (plain) {
     AttnArgs a{};
     a.B = B, a.Hq = Hq, a.Hkv = Hkv, a.L = L, a.D = kD, a.Lq = Lq, a.q0 = 0;
-    double us = window_square_us(a, kSms);
+    double us = 4.0 + 0.91 * window_square_us(a, kSms);   // as measured behind the decoding pass (250 us where it says 272, 14 for 12)
     const WindowChoice c = window_gqa_model(a, kSms, kClusters);
     if (c.packed) us = std::min(us, c.packed_us);
     us += kDecodeUs + decode_us;
