@@ -233,3 +233,44 @@ def test_lengths_that_change_between_replays():
             err = (out[b, :, 0].double().view_as(want) - want).abs()
             assert (err <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 4 * 2.0 ** -13) * mass).all()
             assert (lse[b, :, 0].double().view(Hkv, -1) - torch.logsumexp(s, -1)).abs().max() <= 2.0 ** -13 + 2.0 ** -15
+
+
+@pytest.mark.parametrize("mode,parts", [(0, 16), (0, -8), (1, 16), (2, 16), (3, 16), (4, 1)])
+def test_attention_over_more_than_32_bits_of_codes(mode, parts):
+    """4.6e9 codes: zeros but for the last rows of every head, which have scores of their own; the rows before count exp(0)."""
+    H, L, n = 9, 4000000, 700
+    mem = api.kv8_memory(1, H, L)
+    rows = _r(1, H, n, 128, seed=150)
+    api.cover_kv8_write(rows, -rows, *mem, pos0=L - n)
+    k, _ = api.cover_kv8_read(*mem, pos0=L - n, dtype=torch.float32)
+    q = (k[:, :, [5, n - 1]] * 1.5).bfloat16()
+    out, lse = api.cover_debug_attn_prefix8(q, *mem, q0=100, mode=mode, nsplit=parts)
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+    s = torch.einsum("bhrd,bhnd->bhrn", q.double(), k.double()) / 128 ** 0.5
+    z = torch.logaddexp(torch.logsumexp(s, -1), torch.full_like(s[..., 0], L - n).log())
+    w = torch.exp(s - z[..., None])
+    want, mass = -torch.einsum("bhrn,bhnd->bhrd", w, k.double()), torch.einsum("bhrn,bhnd->bhrd", w, k.double().abs())
+    # weights and output rounded to bf16; scores off by 2^-20 of sum |q_i k_i| / sqrt(D) <= 2^6; sums of up to 2^22 equal terms in
+    # fp32, 128 and more threads or 32 columns at a time, off by 2^-24 for each of at most 2^15 additions
+    rel = 4 * 2.0 ** -14 + 2.0 ** -9
+    assert ((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + rel) * mass * (1 + 2.0 ** -6)).all()
+    assert (lse.double() - z).abs().max() <= rel
+
+
+def test_more_sequences_than_share_their_parts():
+    """33 sequences of uneven lengths, some empty."""
+    B, Hq, Hkv, L = 33, 8, 2, 700
+    mem, q = _mem(B, Hkv, L, 160), _r(B, Hq, 1, 128, seed=161)
+    hi = torch.tensor([[(37 * b) % (L + 1)] for b in range(B)], device="cuda", dtype=torch.int32)
+    out, lse = api.cover_attn_fwd_prefix8(q, *mem, q0=0, key_hi=hi)
+    for b in (0, 1, 15, 18, 32):
+        n = int(hi[b])
+        if n == 0:
+            assert not out[b].any() and (lse[b] == -float("inf")).all()
+            continue
+        one = tuple(m[b:b + 1].contiguous() for m in mem)
+        ref, ref_lse = api.cover_attn_fwd_prefix8(q[b:b + 1].contiguous(), *one, q0=0, key_hi=hi[b:b + 1].contiguous())
+        v = api.cover_kv8_read(*one, dtype=torch.float32)[1].abs().max()
+        assert (out[b:b + 1].float() - ref.float()).abs().max() <= 2 * 2.0 ** -7 * v    # each rounds weights and output by 2^-8
+        assert (lse[b:b + 1] - ref_lse).abs().max() <= 2.0 ** -12
