@@ -1114,7 +1114,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t qk_hi = static_cast<uint32_t>(dq >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
       // What this thread does between a barrier and its products is on every tile's way: descriptors are added up in their
       // lower words, and of several barriers the one that completes last is waited for last (1216 rows over 8192 keys 124 -> 116 us).
-      // A thread for each Q tile took 170 us, P taken in two pieces as its chunks get ready 131.
+      // A thread for each Q tile took 170 us, P taken in two pieces as its chunks get ready 131, a thread that polls its barriers
+      // 129, the two Q tiles' softmax in turns 122 to 126.
       const auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
       // S[s] = Q[s] . K(stage)^T
       auto issue_s = [&](int s, int st) {
