@@ -1610,23 +1610,29 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
       const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), 16, 1024);
       const uint64_t dp = sdesc_sw128(smem_u32(sm.pt[0]), 16, 1024);
-      constexpr uint64_t kStageDesc = (kBN * kD) >> 4;
+      constexpr uint32_t kStageDesc = (kBN * kD) >> 4;
+      // descriptors are added up in their lower words (4 x 131072 keys, 32 / 8 heads: 187 -> 182.6 us)
+      const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv),
+                     p_lo = static_cast<uint32_t>(dp), hi = static_cast<uint32_t>(dq >> 32);   // (all four have the same upper words)
+      const auto desc = [&](uint32_t lo) { return (static_cast<uint64_t>(hi) << 32) | lo; };
       // S^T[s] = K(tile j) . Q^T
       auto issue_s = [&](int j) {
         const int s = j & 1, st = j % kStages;
+        const uint32_t k = k_lo + st * kStageDesc;
 #pragma unroll
         for (int kk = 0; kk < kD / 32; ++kk)
-          umma_ss_f8(tbase + s * kCols, dk + st * kStageDesc + ((kk * 32) >> 4), dq + ((kk * 32) >> 4), id_s, kk > 0 ? 1u : 0u);
+          umma_ss_f8(tbase + s * kCols, desc(k + ((kk * 32) >> 4)), desc(q_lo + ((kk * 32) >> 4)), id_s, kk > 0 ? 1u : 0u);
         umma_commit(&sm.s_full[s]);
         umma_commit(&sm.k_empty[st]);
       };
       // O^T[s] (+)= V(tile j)^T . P[s]^T
       auto issue_o = [&](int j) {
         const int s = j & 1, st = j % kStages;
+        const uint32_t v = v_lo + st * kStageDesc, pt = p_lo + s * ((kBN * 128) >> 4);
 #pragma unroll
         for (int kk = 0; kk < kBN / 32; ++kk)
-          umma_ss_f8(tbase + (2 + s) * kCols, dv + st * kStageDesc + ((kk * 32 * kD) >> 4),
-                     dp + s * ((kBN * 128) >> 4) + ((kk * 32 * 128) >> 4), id_o, (j > 1 || kk > 0) ? 1u : 0u);
+          umma_ss_f8(tbase + (2 + s) * kCols, desc(v + ((kk * 32 * kD) >> 4)), desc(pt + ((kk * 32 * 128) >> 4)), id_o,
+                     (j > 1 || kk > 0) ? 1u : 0u);
         umma_commit(&sm.v_empty[st]);
       };
       auto wait = [&](uint64_t* bar, int phase) {
