@@ -1205,6 +1205,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
     for (int j = 0; j < jend; ++j) {
       ok = warp_wait(&ctl.s_full[tile], j & 1, &ctl.abort);
+      tc_fence_after_sync();   // zeros are stored over S too, where no row sees a key
       const int key0 = (j0 + j) * kBN + half * kHalf;
       const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch of this half are seen
       // (a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything)
@@ -1212,13 +1213,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool own_column = warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kHalf);
       const Unseen u{cl, ch, is_seed ? pos - key0 : -1, own_column || __any_sync(0xffffffffu, valid && (cl > 0 || ch < kHalf))};
       float m_half = -INFINITY;
-      if (ok && some) {
-        tc_fence_after_sync();
-        if (!fixed) {
+      if (ok && some && !fixed) {
 #pragma unroll 1
-          for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, 0, c));
-          m_half = reference_of<kCap>(m_half, p);
-        }
+        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, 0, c));
+        m_half = reference_of<kCap>(m_half, p);
       }
       if (fixed && !ok) break;
       // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row

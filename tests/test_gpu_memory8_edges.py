@@ -1,0 +1,69 @@
+"""The rotary and 8-bit memory calls at the ends of what their documentation allows: rows and bounds of every kind, values and bytes
+of every size, tensors of another stream. Against the fp64 oracle, with the tolerances of the operators' own tests."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import memory8_oracle as M8
+from paper_2602_06161_gb300 import api
+
+pytestmark = pytest.mark.gpu
+
+
+def _r(*shape, seed=0, scale=1.0, dtype=torch.bfloat16):
+    return (torch.randn(shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda") * scale).to(dtype)
+
+
+def _h(t):
+    return t.view(torch.uint8).cpu().numpy() if t.dtype == torch.float8_e4m3fn else t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def _mem(B, H, L, seed=1, scale=1.0):
+    m = api.kv8_memory(B, H, L)
+    api.cover_kv8_write(_r(B, H, L, 128, seed=seed, scale=scale), _r(B, H, L, 128, seed=seed + 1), *m)
+    return m
+
+
+def _i32(x):
+    return torch.tensor(x, device="cuda", dtype=torch.int32)
+
+
+def _attn(q, mem, mode=None, seeds=(None, None, None), **kw):
+    """The call itself, or the kernel ``mode``."""
+    r = api.cover_attn_fwd_prefix8(q, *mem, *seeds, **kw) if mode is None else api.cover_debug_attn_prefix8(q, *mem, *seeds, mode=mode, **kw)
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+    return r
+
+
+def _check(got, q, mem, seeds=(None, None, None), *, q0, key_lo=None, key_hi=None, softcap=0.0):
+    """The weights and the output are rounded to bf16 (half a step each, 2^-8); scores are off by at most 2^-20 of
+    sum |q_i k_i| / sqrt(D) and, capped, of the cap; that is at most a factor e^{2d} of a weight. lse is off by d and 2^-20 of its
+    sums' rounding."""
+    n = lambda t: None if t is None else _h(t)  # noqa: E731
+    k, v = (M8.decode(_h(mem[i]), _h(mem[2 + i])) for i in range(2))
+    ref, ref_lse, mass, size = M8.attention(_h(q), k, v, *(n(t) for t in seeds), q0=q0, key_lo=n(key_lo), key_hi=n(key_hi), softcap=softcap)
+    out, lse = (_h(t) for t in got)
+    d = 2.0 ** -20 * (size + softcap)
+    tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 4 * d[..., None]) * mass * (1 + 2.0 ** -6)
+    assert (np.abs(out - ref) <= tol).all()
+    none = ref_lse == -math.inf
+    assert np.array_equal(lse == -math.inf, none)
+    assert (np.abs(np.where(none, 0, lse) - np.where(none, 0, ref_lse)) <= d + 2.0 ** -20 * (1 + np.abs(np.where(none, 0, ref_lse)))).all()
+
+
+@pytest.mark.parametrize("mode", [2, 3])
+@pytest.mark.parametrize("softcap", [0.0, 30.0, 100.0])
+def test_warps_that_see_no_key_of_a_tile(mode, softcap):
+    """Neighbouring groups of 32 rows see different KV tiles, or half of one, in turns: in every tile some warps store zeros while
+    others read their scores."""
+    Lq, Lk = 256, 1000
+    mem, q = _mem(1, 2, Lk), _r(1, 2, Lq, 128, seed=3)
+    group = torch.arange(Lq, device="cuda") // 32
+    lo = ((group * 5) % 8 * 128 + (group % 2) * 64).int()[None].contiguous()
+    hi = torch.where(group % 3 == 0, lo + 64, lo + 300).int().contiguous()
+    for kw in (dict(), dict(nsplit=3)):
+        got = _attn(q, mem, mode, q0=100, key_lo=lo, key_hi=hi, softcap=softcap, **kw)
+        _check(got, q, mem, q0=100, key_lo=lo, key_hi=hi, softcap=softcap)
