@@ -45,6 +45,32 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _maker(stream, device):
+    """make(shape, dtype, zero=False): a tensor that a call makes for itself, a result or a workspace. Of a given stream
+    that is not the current one it comes from that stream's memory: a block of the current stream's may still be read
+    or written by work that is pending there. The block is kept until the current stream, on which the caller goes on with it,
+    is done with it too."""
+    def make(shape, dtype, zero=False):
+        return (torch.zeros if zero else torch.empty)(shape, dtype=dtype, device=device)
+
+    if stream is None:
+        return make
+    current, s = torch.cuda.current_stream(device), _stream(stream)
+    if s == current.cuda_stream:
+        return make
+    if isinstance(stream, torch.cuda.Stream):
+        on = stream
+    else:   # (ExternalStream(0) would be a stream of its own)
+        on = torch.cuda.ExternalStream(s, device=current.device) if s else torch.cuda.default_stream(current.device)
+
+    def make_there(shape, dtype, zero=False):
+        with torch.cuda.stream(on):
+            t = make(shape, dtype, zero)
+        t.record_stream(current)
+        return t
+    return make_there
+
+
 def _need(t: torch.Tensor, name: str, dtype, ndim: int):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -75,12 +101,13 @@ def _attn(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, seed_id
             raise ValueError("seed_idx must be [B, S]")
         if tuple(k_seedmask.shape) != (B, Hkv, n_seeds, D) or tuple(v_seedmask.shape) != (B, Hkv, n_seeds, D):
             raise ValueError("k_seedmask / v_seedmask must be [B, Hkv, S, D]")
+    make = _maker(stream, q.device)
     if out is None:
-        out = torch.empty_like(q)
+        out = make(q.shape, q.dtype)
     else:
         _need(out, "out", dtype, 4)
     if lse is None and want_lse:
-        lse = torch.empty((B, Hq, L), dtype=torch.float32, device=q.device)
+        lse = make((B, Hq, L), torch.float32)
     elif lse is not None:
         _need(lse, "lse", torch.float32, 3)
     lib = _lib.load()
@@ -135,12 +162,13 @@ def _attn_prefix(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, 
             raise ValueError("seed_idx must be [B, S]")
         if tuple(k_seedmask.shape) != (B, Hkv, n_seeds, D) or tuple(v_seedmask.shape) != (B, Hkv, n_seeds, D):
             raise ValueError("k_seedmask / v_seedmask must be [B, Hkv, S, D]")
+    make = _maker(stream, q.device)
     if out is None:
-        out = torch.empty_like(q)
+        out = make(q.shape, q.dtype)
     else:
         _need(out, "out", dtype, 4)
     if lse is None and want_lse:
-        lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
+        lse = make((B, Hq, Lq), torch.float32)
     elif lse is not None:
         _need(lse, "lse", torch.float32, 3)
     code = getattr(_lib.load(), fn_name)(
@@ -182,9 +210,10 @@ def _seed_route(fn_name, seed_idx, B, L, device, stream):
         _need(seed_idx, "seed_idx", torch.int32, 2)
         device = seed_idx.device
     device = device or torch.device("cuda")
-    slot = torch.empty((B, L), dtype=torch.int32, device=device)
-    bitmap = torch.empty((B, (L + 127) // 128, 4), dtype=torch.int32, device=device)
-    n_invalid = torch.empty((1,), dtype=torch.int32, device=device)
+    make = _maker(stream, device)
+    slot = make((B, L), torch.int32)
+    bitmap = make((B, (L + 127) // 128, 4), torch.int32)
+    n_invalid = make((1,), torch.int32)
     code = getattr(_lib.load(), fn_name)(_ptr(seed_idx) if n_seeds else None, n_seeds, B, L, _ptr(slot),
                                          _ptr(bitmap), _ptr(n_invalid), _stream(stream))
     _lib.check(fn_name, code)
@@ -205,10 +234,14 @@ def cover_score_workspace_bytes(n_seq: int) -> int:
     return int(_lib.load().cover_score_workspace_bytes(int(n_seq)))
 
 
+def _score_workspace(n_seq):
+    """Its shape and type."""
+    return (max(cover_score_workspace_bytes(n_seq), 4) + 3) // 4, torch.int32
+
+
 def score_workspace(n_seq: int, device=None) -> torch.Tensor:
     """A zero-filled workspace for cover_score_fwd (reusable across calls on one stream)."""
-    nbytes = cover_score_workspace_bytes(n_seq)
-    return torch.zeros((max(nbytes, 4) + 3) // 4, dtype=torch.int32, device=device or "cuda")
+    return _maker(None, device or "cuda")(*_score_workspace(n_seq), zero=True)
 
 
 def cover_score_fwd(logits, n_seq: int, topk: int, *, cur_tok=None, d_in=None, d_out=None, eligible=None,
@@ -233,17 +266,15 @@ def cover_score_fwd(logits, n_seq: int, topk: int, *, cur_tok=None, d_in=None, d
         _need(d_out, "d_out", torch.float32, 1)
     if eligible is not None:
         _need(eligible, "eligible", torch.uint8, 1)
+    make = _maker(stream, dev)
     if out is None:
         out = dict(
-            maxprob=torch.empty(N, dtype=torch.float32, device=dev),
-            entropy=torch.empty(N, dtype=torch.float32, device=dev),
-            argmax=torch.empty(N, dtype=torch.int32, device=dev),
-            score=torch.empty(N, dtype=torch.float32, device=dev),
-            topk_idx=torch.empty((n_seq, max(topk, 0)), dtype=torch.int32, device=dev),
-            topk_score=torch.empty((n_seq, max(topk, 0)), dtype=torch.float32, device=dev),
+            maxprob=make(N, torch.float32), entropy=make(N, torch.float32), argmax=make(N, torch.int32),
+            score=make(N, torch.float32), topk_idx=make((n_seq, max(topk, 0)), torch.int32),
+            topk_score=make((n_seq, max(topk, 0)), torch.float32),
         )
     if workspace is None and topk > 0:
-        workspace = score_workspace(n_seq, dev)
+        workspace = make(*_score_workspace(n_seq), zero=True)
     code = _lib.load().cover_score_fwd(
         _ptr(logits), N, V, n_seq, _ptr(cur_tok), _ptr(d_in), _ptr(d_out), _ptr(eligible), topk,
         _ptr(out["maxprob"]), _ptr(out["entropy"]), _ptr(out["argmax"]), _ptr(out["score"]),
@@ -269,14 +300,12 @@ def cover_score_fwd_noalloc(logits, n_seq: int, topk: int, *, cur_tok=None, d_in
                         ("d_out", d_out, torch.float32), ("eligible", eligible, torch.uint8)):
         if t is not None:
             _need(t, name, dt, 1)
+    make = _maker(stream, dev)
     if out is None:
         out = dict(
-            maxprob=torch.empty(N, dtype=torch.float32, device=dev),
-            entropy=torch.empty(N, dtype=torch.float32, device=dev),
-            argmax=torch.empty(N, dtype=torch.int32, device=dev),
-            score=torch.empty(N, dtype=torch.float32, device=dev),
-            topk_idx=torch.empty((n_seq, max(topk, 0)), dtype=torch.int32, device=dev),
-            topk_score=torch.empty((n_seq, max(topk, 0)), dtype=torch.float32, device=dev),
+            maxprob=make(N, torch.float32), entropy=make(N, torch.float32), argmax=make(N, torch.int32),
+            score=make(N, torch.float32), topk_idx=make((n_seq, max(topk, 0)), torch.int32),
+            topk_score=make((n_seq, max(topk, 0)), torch.float32),
         )
     code = _lib.load().cover_score_fwd_noalloc(
         _ptr(logits), N, V, n_seq, _ptr(cur_tok), _ptr(d_in), _ptr(d_out), _ptr(eligible), topk,
@@ -305,8 +334,8 @@ def _seed_kv(fn_name, k, v, seed_idx, k_cache, v_cache, stream):
         if tuple(seed_idx.shape) != (B, S):
             raise ValueError("seed_idx must be [B, S]")
         if k_cache is None:
-            k_cache = torch.empty((B, Hkv, S, D), dtype=k.dtype, device=k.device)
-            v_cache = torch.empty_like(k_cache)
+            make = _maker(stream, k.device)
+            k_cache, v_cache = (make((B, Hkv, S, D), k.dtype) for _ in range(2))
         _need(k_cache, "k_cache", k.dtype, 4)
         _need(v_cache, "v_cache", k.dtype, 4)
         if tuple(k_cache.shape) != (B, Hkv, S, D) or tuple(v_cache.shape) != (B, Hkv, S, D):
@@ -358,16 +387,10 @@ def _strides(*tensors):
     return (ctypes.c_int64 * len(vals))(*vals)
 
 
-def _launch(fn_name, device, stream, args, made=()):
-    """Calls the entry point on the tensors' device. Tensors made for the call are not handed out again by the
-    allocator before another stream that was given is done with them."""
+def _launch(fn_name, device, stream, args):
+    """Calls the entry point on the tensors' device."""
     with torch.cuda.device(device):
-        s = _stream(stream)
-        if stream is not None and s != torch.cuda.current_stream().cuda_stream:
-            on = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(s, device=device)
-            for t in made:
-                t.record_stream(on)
-        code = getattr(_lib.load(), fn_name)(*args, s)
+        code = getattr(_lib.load(), fn_name)(*args, _stream(stream))
     _lib.check(fn_name, code)
 
 
@@ -388,10 +411,10 @@ def _overlap(a, b):
     return a0 < b1 and b0 < a1
 
 
-def _rope_out(x, out, name, others):
+def _rope_out(x, out, name, others, make):
     """The output for x: a new dense tensor, x itself (in place), or one that overlaps none of ``others``."""
     if out is None:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return make(x.shape, x.dtype)
     _rows_need(out, name, (x.dtype,), x.device)
     if out.shape != x.shape:
         raise ValueError(f"{name} must have the shape {tuple(x.shape)}")
@@ -432,15 +455,15 @@ def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool
     _same_device(dev, inv_freq=inv_freq, pos=pos)
     if 2 * inv_freq.shape[0] > D:
         raise ValueError("inv_freq must have at most D / 2 entries")
-    oq = _rope_out(q, out_q, "out_q", (q, k, out_k))
-    ok = None if k is None else _rope_out(k, out_k, "out_k", (q, k, oq))
+    make = _maker(stream, dev)
+    oq = _rope_out(q, out_q, "out_q", (q, k, out_k), make)
+    ok = None if k is None else _rope_out(k, out_k, "out_k", (q, k, oq), make)
     has_k = k is not None and k.shape[1] > 0
     st = _strides(q, k if has_k else q, oq, ok if has_k else oq)
     _launch("cover_rope_fwd", dev, stream,
             (_ptr(q), _ptr(k) if has_k else None, _ptr(oq), _ptr(ok) if has_k else None, ctypes.addressof(st), B, Hq,
              k.shape[1] if has_k else 0, L, D, 2 * inv_freq.shape[0], _ptr(inv_freq) or None, _ptr(pos), int(pos0),
-             1 if interleaved else 0, float(mscale), 1 if inverse else 0, q.element_size()),
-            [t for t, given in ((oq, out_q), (ok, out_k)) if t is not None and given is None])
+             1 if interleaved else 0, float(mscale), 1 if inverse else 0, q.element_size()))
     return oq, ok
 
 
@@ -543,11 +566,11 @@ def cover_kv8_read(k8, v8, k_exp, v_exp, *, pos=None, pos0: int = 0, n: Optional
     if n < 0:
         raise ValueError("n must not be negative")
     _kv8_pos(pos, B, n, k8.device)
-    k = torch.empty((B, Hkv, n, D), dtype=dtype, device=k8.device)
-    v = torch.empty_like(k)
+    make = _maker(stream, k8.device)
+    k, v = (make((B, Hkv, n, D), dtype) for _ in range(2))
     _launch("cover_kv8_read", k8.device, stream,
             (_ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(pos) if n else None, int(pos0), n, B, Hkv, L, D,
-             k.element_size(), _ptr(k) if n else None, _ptr(v) if n else None), (k, v))
+             k.element_size(), _ptr(k) if n else None, _ptr(v) if n else None))
     return k, v
 
 
@@ -591,17 +614,15 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
             _need(t, name, torch.int32, 2)
             if tuple(t.shape) != (B, Lq):
                 raise ValueError(f"{name} must be [B, Lq]")
-    made = []
+    make = _maker(stream, dev)
     if out is None:
-        out = torch.empty_like(q)
-        made.append(out)
+        out = make(q.shape, q.dtype)
     else:
         _need(out, "out", torch.bfloat16, 4)
         if out.shape != q.shape:
             raise ValueError("out must match q")
     if lse is None and want_lse:
-        lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=dev)
-        made.append(lse)
+        lse = make((B, Hq, Lq), torch.float32)
     elif lse is not None:
         _need(lse, "lse", torch.float32, 3)
         if tuple(lse.shape) != (B, Hq, Lq):
@@ -612,13 +633,12 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
         if workspace.numel() < nbytes:
             raise ValueError(f"workspace must have at least {nbytes} bytes")
     elif nbytes:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        made.append(workspace)
+        workspace = make(nbytes, torch.uint8)
     _same_device(dev, k8=k8, key_lo=key_lo, key_hi=key_hi, out=out, lse=lse, workspace=workspace)
     _launch("cover_attn_fwd_prefix8", dev, stream,
             (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
              _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, int(q0), D,
-             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(workspace) if nbytes else None), made)
+             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(workspace) if nbytes else None))
     return out, lse
 
 
@@ -626,10 +646,14 @@ def cover_decide_workspace_bytes(N: int, n_seq: int) -> int:
     return int(_lib.load().cover_decide_workspace_bytes(int(N), int(n_seq)))
 
 
+def _decide_workspace(N, n_seq):
+    """Its shape and type."""
+    return ((max(cover_decide_workspace_bytes(N, n_seq), 16) + 15) // 16, 4), torch.int32
+
+
 def decide_workspace(N: int, n_seq: int, device=None) -> torch.Tensor:
     """A zero-filled workspace for cover_score_decide_fwd (reusable across calls on one stream)."""
-    nbytes = cover_decide_workspace_bytes(N, n_seq)
-    return torch.zeros((max(nbytes, 16) + 15) // 16, 4, dtype=torch.int32, device=device or "cuda")
+    return _maker(None, device or "cuda")(*_decide_workspace(N, n_seq), zero=True)
 
 
 COVER_DECIDE_ALL = 0
@@ -666,18 +690,15 @@ def cover_score_decide_fwd(logits, n_seq: int, tok, flags, remask_cnt, *, tau_dr
                         ("draft_ok", draft_ok, torch.uint8)):
         if t is not None:
             _need(t, name, dt, 1)
+    make = _maker(stream, dev)
     if out is None:
         out = dict(
-            maxprob=torch.empty(N, dtype=torch.float32, device=dev),
-            entropy=torch.empty(N, dtype=torch.float32, device=dev),
-            argmax=torch.empty(N, dtype=torch.int32, device=dev),
-            score=torch.empty(N, dtype=torch.float32, device=dev),
-            seed_idx=torch.empty((n_seq, max(max_seeds, 0)), dtype=torch.int32, device=dev),
-            n_seeds=torch.empty(n_seq, dtype=torch.int32, device=dev),
-            stats=torch.empty((n_seq, 6), dtype=torch.int32, device=dev),
+            maxprob=make(N, torch.float32), entropy=make(N, torch.float32), argmax=make(N, torch.int32),
+            score=make(N, torch.float32), seed_idx=make((n_seq, max(max_seeds, 0)), torch.int32),
+            n_seeds=make(n_seq, torch.int32), stats=make((n_seq, 6), torch.int32),
         )
     if workspace is None:
-        workspace = decide_workspace(N, n_seq, dev)
+        workspace = make(*_decide_workspace(N, n_seq), zero=True)
     code = _lib.load().cover_score_decide_fwd(
         _ptr(logits), N, V, n_seq, _ptr(d_in), _ptr(d_out), _ptr(draft_ok), float(tau_draft), int(draft_budget),
         int(remask_budget), int(mask_id), 1 if min_one else 0, int(pos0), int(max_seeds), int(phase),
@@ -705,10 +726,9 @@ def cover_seed_select_fwd(n_seq: int, tok, flags, remask_cnt, workspace, *, rema
         if t is not None:
             _need(t, name, torch.float32, 1)
     if out is None:
-        out = dict(score=torch.empty(N, dtype=torch.float32, device=dev),
-                   seed_idx=torch.empty((n_seq, max(max_seeds, 0)), dtype=torch.int32, device=dev),
-                   n_seeds=torch.empty(n_seq, dtype=torch.int32, device=dev),
-                   stats=torch.zeros((n_seq, 6), dtype=torch.int32, device=dev))
+        make = _maker(stream, dev)
+        out = dict(score=make(N, torch.float32), seed_idx=make((n_seq, max(max_seeds, 0)), torch.int32),
+                   n_seeds=make(n_seq, torch.int32), stats=make((n_seq, 6), torch.int32, zero=True))
     code = _lib.load().cover_seed_select_fwd(
         N, n_seq, _ptr(d_in), _ptr(d_out), int(remask_budget), int(mask_id), int(pos0), int(max_seeds),
         _ptr(tok), _ptr(flags), _ptr(remask_cnt), _ptr(out["score"]),
@@ -748,13 +768,14 @@ def cover_attn_mass_fwd(q, k_cached, lse, tok, flags, *, mask_id: int, pos0: int
         _need(k_seedmask, "k_seedmask", torch.bfloat16, 4)
     if tok.shape[0] != B * per or flags.shape[0] != B * per:
         raise ValueError("tok / flags must have B * per entries")
+    make = _maker(stream, q.device)
     if workspace is None:
         nbytes = cover_attn_mass_workspace_bytes(B, Hq, per)
-        workspace = torch.empty((nbytes + 15) // 16, 4, dtype=torch.int32, device=q.device)
+        workspace = make(((nbytes + 15) // 16, 4), torch.int32)
     if d_in is None:
-        d_in = torch.empty(B * per, dtype=torch.float32, device=q.device)
+        d_in = make(B * per, torch.float32)
     if d_out is None:
-        d_out = torch.empty(B * per, dtype=torch.float32, device=q.device)
+        d_out = make(B * per, torch.float32)
     code = _lib.load().cover_attn_mass_fwd(
         _ptr(q), _ptr(k_cached), _ptr(k_seedmask) if n_seeds else None, _ptr(seed_idx) if n_seeds else None,
         n_seeds, _ptr(lse), B, Hq, Hkv, L, D, _ptr(tok), _ptr(flags), int(mask_id), int(pos0), int(per),
@@ -777,8 +798,8 @@ def cover_debug_umma_tile(a, b, p, v, *, stream=None):
         _need(t, name, torch.bfloat16, 2)
         if tuple(t.shape) != (128, 128):
             raise ValueError(f"{name} must be [128, 128]")
-    c1 = torch.empty((128, 128), dtype=torch.float32, device=a.device)
-    c2 = torch.empty((128, 128), dtype=torch.float32, device=a.device)
+    make = _maker(stream, a.device)
+    c1, c2 = (make((128, 128), torch.float32) for _ in range(2))
     code = _lib.load().cover_debug_umma_tile(_ptr(a), _ptr(b), _ptr(p), _ptr(v), _ptr(c1), _ptr(c2),
                                              _stream(stream))
     _lib.check("cover_debug_umma_tile", code)
