@@ -397,22 +397,49 @@ def _launch(fn_name, device, stream, args):
 _ROWS = (torch.bfloat16, torch.float32)
 
 
-def _span(t):
-    """The bytes that a tensor's elements lie in, as (first, end)."""
-    if t.numel() == 0:
-        return 0, 0
-    lo = t.data_ptr() + t.element_size() * sum(min(0, (n - 1) * st) for n, st in zip(t.shape, t.stride()))
-    hi = t.data_ptr() + t.element_size() * (1 + sum(max(0, (n - 1) * st) for n, st in zip(t.shape, t.stride())))
-    return lo, hi
-
-
 def _overlap(a, b):
-    (a0, a1), (b0, b1) = _span(a), _span(b)
-    return a0 < b1 and b0 < a1
+    """Whether two tensors share a byte. Rows of one that lie between rows of the other do not (a projection's q and k).
+    Exact but for layouts of many strides that no view of a projection has, which count as sharing one."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    pa, pb, ea, eb = a.data_ptr(), b.data_ptr(), a.element_size(), b.element_size()
+    end = lambda t, p, e: p + e * (1 + sum((n - 1) * st for n, st in zip(t.shape, t.stride())))  # noqa: E731
+    if pa >= end(b, pb, eb) or pb >= end(a, pa, ea):
+        return False
+    # the bytes between an element of a and one of b: base + sum_i c_i x_i with x_i in [lo_i, hi_i], a dimension each, those of
+    # equal strides c as one; the elements share a byte if that is in (-size of a's element, size of b's)
+    span = {}
+    for t, e, sign in ((a, ea, 1), (b, eb, -1)):
+        for n, st in zip(t.shape, t.stride()):
+            if n > 1 and st:
+                c = st * e
+                lo, hi = span.get(c, (0, 0))
+                span[c] = (lo, hi + n - 1) if sign > 0 else (lo - n + 1, hi)
+    dims = sorted(span.items(), reverse=True)
+    below, above = [0], [0]   # what the dimensions from the last one up add at least, at most
+    for c, (lo, hi) in reversed(dims):
+        below.append(below[-1] + c * lo)
+        above.append(above[-1] + c * hi)
+    left = 4096               # values to be looked at
+
+    def meets(at, i):
+        nonlocal left
+        lowest, highest = 1 - ea - at, eb - 1 - at   # what the dimensions from i on have to add
+        if i == len(dims):
+            return lowest <= 0 <= highest
+        c, (lo, hi) = dims[i]
+        rest = len(dims) - i - 1
+        # x_i with lowest <= c x_i + rest <= highest for some value of the rest
+        for x in range(max(lo, -((above[rest] - lowest) // c)), min(hi, (highest - below[rest]) // c) + 1):
+            left -= 1
+            if left < 0 or meets(at + c * x, i + 1):
+                return True
+        return False
+    return meets(pa - pb, 0)
 
 
-def _rope_out(x, out, name, others, make):
-    """The output for x: a new dense tensor, x itself (in place), or one that overlaps none of ``others``."""
+def _rope_out(x, out, name, make):
+    """The output for x: a new dense tensor, x itself (in place) or another one."""
     if out is None:
         return make(x.shape, x.dtype)
     _rows_need(out, name, (x.dtype,), x.device)
@@ -420,16 +447,30 @@ def _rope_out(x, out, name, others, make):
         raise ValueError(f"{name} must have the shape {tuple(x.shape)}")
     if any(n > 1 and st == 0 for n, st in zip(out.shape, out.stride())):
         raise ValueError(f"{name} must not be expanded")
-    in_place = out.data_ptr() == x.data_ptr() and out.stride() == x.stride()
-    if not in_place and any(_overlap(out, t) for t in others if t is not None):
-        raise ValueError(f"{name} must be its input or overlap none of the tensors")
     return out
+
+
+def _rope_aliases(pairs, rest):
+    """Refuses given outputs that overlap anything but their own inputs, as which they lie in memory. pairs: (name, input, given output);
+    rest: the other inputs."""
+    seen = set()
+    for i, (name, x, out) in enumerate(pairs):
+        if out is None:
+            continue
+        in_place = out.data_ptr() == x.data_ptr() and all(n <= 1 or s == t for n, s, t in zip(x.shape, out.stride(), x.stride()))
+        others = [t for j, p in enumerate(pairs) if j != i for t in p[1:]] + rest + ([] if in_place else [x])
+        for t in others:
+            if t is None or frozenset((id(out), id(t))) in seen:
+                continue
+            seen.add(frozenset((id(out), id(t))))
+            if _overlap(out, t):
+                raise ValueError(f"{name} must be its input or not overlap it, and overlap none of the other tensors")
 
 
 def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool = False, mscale: float = 1.0,
                    inverse: bool = False, out_q=None, out_k=None, stream=None):
-    """Rotary positions of queries and keys. Returns (q, k) turned, dense unless out_q / out_k are given (which may be
-    q / k themselves: in place).
+    """Rotary positions of queries and keys. Returns (q, k) turned, dense unless out_q / out_k are given, which may be
+    q / k themselves (in place) and share no byte with any other of the tensors.
 
     q [B, Hq, L, D], k [B, Hkv, L, D] (or None): bf16 or fp32, dense in the last dimension only (a projection's
     [B, L, H, D] transposed will do). inv_freq: fp64 [R / 2], radians per position (rope_frequencies); the first
@@ -456,8 +497,10 @@ def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool
     if 2 * inv_freq.shape[0] > D:
         raise ValueError("inv_freq must have at most D / 2 entries")
     make = _maker(stream, dev)
-    oq = _rope_out(q, out_q, "out_q", (q, k, out_k), make)
-    ok = None if k is None else _rope_out(k, out_k, "out_k", (q, k, oq), make)
+    oq = _rope_out(q, out_q, "out_q", make)
+    ok = None if k is None else _rope_out(k, out_k, "out_k", make)
+    if out_q is not None or out_k is not None:
+        _rope_aliases([("out_q", q, out_q)] + ([] if k is None else [("out_k", k, out_k)]), [inv_freq, pos])
     has_k = k is not None and k.shape[1] > 0
     st = _strides(q, k if has_k else q, oq, ok if has_k else oq)
     _launch("cover_rope_fwd", dev, stream,

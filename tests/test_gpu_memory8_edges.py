@@ -67,3 +67,24 @@ def test_warps_that_see_no_key_of_a_tile(mode, softcap):
     for kw in (dict(), dict(nsplit=3)):
         got = _attn(q, mem, mode, q0=100, key_lo=lo, key_hi=hi, softcap=softcap, **kw)
         _check(got, q, mem, q0=100, key_lo=lo, key_hi=hi, softcap=softcap)
+
+
+def test_rotation_beside_other_tensors():
+    """Outputs in one buffer, rows of q between rows of k, are written as they are apart; an output that overlaps another tensor is
+    refused, in place too."""
+    B, L, D = 2, 37, 64
+    qkv, out = _r(B, L, 10, D, seed=20), torch.zeros((B, L, 10, D), device="cuda", dtype=torch.bfloat16)
+    parts = lambda t: (t[:, :, :6].transpose(1, 2), t[:, :, 6:8].transpose(1, 2))  # noqa: E731
+    (q, k), (oq, ok) = parts(qkv), parts(out)
+    f, _ = api.rope_frequencies(D)
+    ref = api.cover_rope_fwd(q, k, f, pos0=5)
+    got = api.cover_rope_fwd(q, k, f, pos0=5, out_q=oq, out_k=ok)
+    assert got[0] is oq and torch.equal(oq, ref[0]) and torch.equal(ok, ref[1]) and not out[:, :, 8:].any()
+    for kw in (dict(out_q=q), dict(out_k=q), dict(out_q=q, out_k=q)):
+        with pytest.raises(ValueError, match="overlap"):
+            api.cover_rope_fwd(q, q, f, **kw)
+    shifted = qkv[:, :, 4:8].transpose(1, 2)          # shares two heads with q
+    with pytest.raises(ValueError, match="overlap"):
+        api.cover_rope_fwd(q, shifted, f, out_q=q)
+    with pytest.raises(ValueError, match="overlap"):
+        api.cover_rope_fwd(q, shifted, f, out_k=shifted)

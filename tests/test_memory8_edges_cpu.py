@@ -1,0 +1,50 @@
+"""CPU checks of the host logic around the rotary and 8-bit memory calls."""
+import itertools
+import random
+
+import pytest
+import torch
+
+from paper_2602_06161_gb300 import api
+
+
+def _bytes(t):
+    return {t.data_ptr() + t.element_size() * sum(i * s for i, s in zip(at, t.stride())) + e
+            for at in itertools.product(*(range(n) for n in t.shape)) for e in range(t.element_size())}
+
+
+def test_overlap_is_that_of_the_bytes():
+    rng = random.Random(1)
+    flat = torch.zeros(4000, dtype=torch.uint8)
+    met = 0
+    for _ in range(3000):
+        a, b = (torch.as_strided(flat.view(rng.choice([torch.bfloat16, torch.float32])), [rng.choice([1, 1, 2, 3, 4]) for _ in range(4)],
+                                 rng.choice([[64, 16, 4, 1], [64, 4, 16, 1], [48, 12, 24, 1], [rng.randint(0, 60) for _ in range(3)] + [1]]),
+                                 rng.randint(0, 200)) for _ in range(2))
+        want = bool(_bytes(a) & _bytes(b))
+        assert api._overlap(a, b) == want
+        met += want
+    assert 300 < met < 2700
+
+
+def test_rotated_rows_lie_apart_or_in_place():
+    """In place, an output is still held against the other tensors; rows that only lie between another's are no overlap."""
+    qkv = torch.zeros((2, 5, 8, 16), dtype=torch.bfloat16)
+    q, k = qkv[:, :, :4].transpose(1, 2), qkv[:, :, 4:6].transpose(1, 2)
+    f, pos = torch.zeros(8, dtype=torch.float64), torch.zeros((2, 5), dtype=torch.int32)
+    out = torch.zeros_like(qkv)
+    oq, ok = out[:, :, :4].transpose(1, 2), out[:, :, 4:6].transpose(1, 2)
+    check = lambda pairs: api._rope_aliases(pairs, [f, pos])  # noqa: E731
+    check([("out_q", q, q), ("out_k", k, k)])
+    check([("out_q", q, oq), ("out_k", k, ok)])
+    check([("out_q", q, None), ("out_k", k, k)])
+    check([("out_q", q, oq)])
+    one = q[:1]      # a dimension of one entry has any stride
+    check([("out_q", one, one.as_strided(one.shape, (7, *one.stride()[1:])))])
+    for pairs in ([("out_q", q, q), ("out_k", q, None)], [("out_q", q, q), ("out_k", q, q)], [("out_q", q, None), ("out_k", q, q)],
+                  [("out_q", q, k.expand_as(k)), ("out_k", k, None)], [("out_q", q, oq), ("out_k", k, oq[:, :2])],
+                  [("out_q", q, qkv[:, :, 1:5].transpose(1, 2)), ("out_k", k, None)],
+                  [("out_q", q, None), ("out_k", k, qkv[:, :, 3:5].transpose(1, 2))],
+                  [("out_q", pos[:, None, :, None], pos[:, None, :, None]), ("out_k", k, None)]):
+        with pytest.raises(ValueError, match="overlap"):
+            check(pairs)
