@@ -621,20 +621,8 @@ def cover_attn_prefix8_workspace_bytes(B: int, Hq: int, Hkv: int, Lq: int, Lk: i
     return int(_lib.load().cover_attn_prefix8_workspace_bytes(int(B), int(Hq), int(Hkv), int(Lq), int(Lk)))
 
 
-def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0: int,
-                           key_lo=None, key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True,
-                           workspace=None, stream=None):
-    """cover_attn_fwd_prefix over an 8-bit memory. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
-
-    key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees (all where None; none: out 0, lse -inf).
-    softcap c > 0: scores become c tanh(score / c). workspace: uint8, at least cover_attn_prefix8_workspace_bytes,
-    scratch of the call; allocated where None.
-    """
-    if stream is None and type(softcap) is float:
-        r = (_nat or _native()).attn8(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
-                                      softcap, out, lse, want_lse, workspace)
-        if r is not None:
-            return _done("cover_attn_fwd_prefix8", r)
+def _attn8_need(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, key_lo, key_hi):
+    """Checks the inputs; returns the number of seeds."""
     _need(q, "q", torch.bfloat16, 4)
     _kv8_need(k8, v8, k_exp, v_exp)
     B, Hq, Lq, D = q.shape
@@ -657,6 +645,28 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
             _need(t, name, torch.int32, 2)
             if tuple(t.shape) != (B, Lq):
                 raise ValueError(f"{name} must be [B, Lq]")
+    _same_device(dev, k8=k8, key_lo=key_lo, key_hi=key_hi)
+    return S
+
+
+def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0: int,
+                           key_lo=None, key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True,
+                           workspace=None, stream=None):
+    """cover_attn_fwd_prefix over an 8-bit memory. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
+
+    key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees (all where None; none: out 0, lse -inf).
+    softcap c > 0: scores become c tanh(score / c). workspace: uint8, at least cover_attn_prefix8_workspace_bytes,
+    scratch of the call; allocated where None.
+    """
+    if stream is None and type(softcap) is float:
+        r = (_nat or _native()).attn8(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
+                                      softcap, out, lse, want_lse, workspace)
+        if r is not None:
+            return _done("cover_attn_fwd_prefix8", r)
+    S = _attn8_need(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, key_lo, key_hi)
+    B, Hq, Lq, D = q.shape
+    Hkv, Lk = k8.shape[1], k8.shape[2]
+    dev = q.device
     make = _maker(stream, dev)
     if out is None:
         out = make(q.shape, q.dtype)
@@ -677,7 +687,7 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
             raise ValueError(f"workspace must have at least {nbytes} bytes")
     elif nbytes:
         workspace = make(nbytes, torch.uint8)
-    _same_device(dev, k8=k8, key_lo=key_lo, key_hi=key_hi, out=out, lse=lse, workspace=workspace)
+    _same_device(dev, out=out, lse=lse, workspace=workspace)
     _launch("cover_attn_fwd_prefix8", dev, stream,
             (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
              _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, int(q0), D,
@@ -877,9 +887,9 @@ def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmas
                              nsplit: int = 1, key_lo=None, key_hi=None, softcap: float = 0.0):
     """cover_attn_fwd_prefix8 on the kernel ``mode`` with the keys in ``nsplit`` parts (negative: -nsplit parts, joined
     in a cluster; above 100: nsplit - 100 parts of a KV head, shared out to the sequences). Returns (out, lse)."""
+    S = _attn8_need(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, key_lo, key_hi)
     B, Hq, Lq, D = q.shape
     Hkv, Lk = k8.shape[1], k8.shape[2]
-    S = 0 if seed_idx is None else int(seed_idx.shape[1])
     out = torch.empty_like(q)
     lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
     nbytes = (4 * B * Hkv * Lk * D if mode >= 3 else 0) + (

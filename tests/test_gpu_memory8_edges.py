@@ -88,3 +88,16 @@ def test_rotation_beside_other_tensors():
         api.cover_rope_fwd(q, shifted, f, out_q=q)
     with pytest.raises(ValueError, match="overlap"):
         api.cover_rope_fwd(q, shifted, f, out_k=shifted)
+
+
+def test_the_debug_call_checks_its_tensors():
+    q, mem = _r(1, 4, 8, 128), api.kv8_memory(1, 2, 64)
+    seeds = (_r(1, 2, 2, 128), _r(1, 2, 2, 128), _i32([[3, 4]]))
+    for kw, what in ((dict(key_hi=torch.zeros((1, 8), device="cuda", dtype=torch.int64)), "key_hi"), (dict(key_lo=_i32([[0] * 7])), "key_lo")):
+        with pytest.raises((TypeError, ValueError), match=what):
+            api.cover_debug_attn_prefix8(q, *mem, q0=0, mode=0, **kw)
+    for args in ((seeds[0][:, :1].contiguous(), *seeds[1:]), (*seeds[:2], seeds[2].expand(2, 2).contiguous()), (None, None, seeds[2])):
+        with pytest.raises((TypeError, ValueError), match="seed"):
+            api.cover_debug_attn_prefix8(q, *mem, *args, q0=0, mode=0)
+    with pytest.raises(ValueError, match="k_exp"):
+        api.cover_debug_attn_prefix8(q, *mem[:2], mem[2][:, :, :32].contiguous(), mem[3], q0=0, mode=0)

@@ -48,3 +48,12 @@ def test_rotated_rows_lie_apart_or_in_place():
                   [("out_q", pos[:, None, :, None], pos[:, None, :, None]), ("out_k", k, None)]):
         with pytest.raises(ValueError, match="overlap"):
             check(pairs)
+
+
+def test_the_debug_call_checks_its_tensors():
+    mem = api.kv8_memory(1, 2, 16, device="cpu")
+    q = torch.zeros(1, 2, 4, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="q must be a CUDA tensor"):
+        api.cover_debug_attn_prefix8(q, *mem, q0=0, mode=0)
+    with pytest.raises(TypeError, match="q must be"):
+        api.cover_debug_attn_prefix8(q.float(), *mem, q0=0, mode=0)
