@@ -625,8 +625,8 @@ __device__ __forceinline__ void join_rows(const Params& p, uint32_t o, uint32_t 
     float m = my_m;
 #pragma unroll
     for (int d = kPad / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const float w = my_m == -INFINITY ? 0.0f : ex2_approx(my_m - m);
-    float l = j < p.nsplit ? w * part.y : 0.0f;
+    const float half = my_m == -INFINITY ? 0.0f : ex2_approx(0.5f * (my_m - m)), w = half * half;
+    float l = j < p.nsplit ? half * part.y * half : 0.0f;
 #pragma unroll
     for (int d = kPad / 2; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -1334,7 +1334,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 //      own. P' is rounded to 9 bits (off by at most 2^-9 of it; bf16 is by 2^-8) and scaled by 2^12: what is
 //      2^-28 of the largest is still held (e5m2's smallest is 2^-16). References take max(e_j, -90) for e_j, so that a row
 //      whose largest weight meets a V row far smaller or larger than the others' has a sum within fp32's range; a V row of
-//      zeros has e_j = -90.
+//      zeros has e_j = -90. A reference holds V's exponent, so it can change by more than the sum does: from a tile of zeros
+//      to one of rows around 2^60 by 150, with a sum of 2^102 before and 2^-48 behind. 2^-150 is no fp32 number, so
+//      sums take a change in two halves, within a stream and where streams and parts are added up. (Accumulators need
+//      not: where the factor vanishes, what they hold is below 2^-28 of what comes.)
 // A softmax thread is a key: its scales are scalars of the thread. The keys' maximum of a row is only taken
 // when some score is above the row's reference by more than the threshold (one vote a tile); sums stay with the
 // threads until the end. V codes of NaN would reach every row (0 * NaN), so four warps look for them, put zeros in
@@ -1412,7 +1415,7 @@ struct RowsSmem {
   int4 row[kN];                   // lo, hi, position of a seed row or -1
   float4 fin[kN];                 // weights of the two accumulators and of the masked-input value, 1 / l
   float m[2][kN];                 // per stream: the rows' references m - 12
-  float step[2][kN], alpha[2][kN];   // of the last change: the new reference less the old one, 2 to its opposite
+  float step[2][kN], half[2][kN];    // of the last change: the new reference less the old one, 2 to the opposite of its half
   int unseen[2][kN], any_unseen[2];  // per stream: rows that have seen no key, whose reference is not set
   float red[2][4][kN];            // per stream and warp
   float s_self[kN];
@@ -1845,7 +1848,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           const bool first = sm.unseen[stream][key] != 0 && up > -INFINITY;
           const float step = first || up > kRowsThreshold ? up : 0.0f;
           sm.step[stream][key] = step;
-          sm.alpha[stream][key] = first ? 0.0f : ex2_approx(-step);
+          sm.half[stream][key] = first ? 0.0f : ex2_approx(-0.5f * step);
           sm.m[stream][key] = m[key] + step;
           if (first) sm.unseen[stream][key] = 0;
           const uint32_t mask = kN == 32 ? 0xffffffffu : 0xffffu;
@@ -1855,8 +1858,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         stream_sync(stream);
 #pragma unroll
         for (int n = 0; n < kN; ++n) {
+          const float half = sm.half[stream][n];
           t[n] -= sm.step[stream][n];
-          l[n] *= sm.alpha[stream][n];
+          l[n] = l[n] * half * half;
         }
         if (i > 0) {
           // O holds the stream's earlier products (complete: the commit of this S came after them)
@@ -1866,7 +1870,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             tmem_ld16(o_addr + c, o);
             tmem_ld_wait16(o);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sm.alpha[stream][c % kN + e]);
+            for (int e = 0; e < 16; ++e) {
+              const float half = sm.half[stream][c % kN + e];
+              o[e] = __float_as_uint(__uint_as_float(o[e]) * (half * half));
+            }
             tmem_st16(o_addr + c, o);
           }
           tmem_st_wait();
@@ -1925,13 +1932,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       for (int s = 0; s < 2; ++s) l2[s] = (sm.red[s][0][n] + sm.red[s][1][n]) + (sm.red[s][2][n] + sm.red[s][3][n]);
       const float m0 = sm.unseen[0][n] ? -INFINITY : sm.m[0][n], m1 = sm.unseen[1][n] ? -INFINITY : sm.m[1][n];
       const float top = fmaxf(fmaxf(m0, m1), s_self);
-      const float w0 = m0 == -INFINITY ? 0.0f : ex2_approx(m0 - top), w1 = m1 == -INFINITY ? 0.0f : ex2_approx(m1 - top);
+      // halves of the streams' factors: a factor itself may be no fp32 number where its sum is large
+      const float h0 = m0 == -INFINITY ? 0.0f : ex2_approx(0.5f * (m0 - top)), h1 = m1 == -INFINITY ? 0.0f : ex2_approx(0.5f * (m1 - top));
       const float p_self = s_self == -INFINITY ? 0.0f : ex2_approx(s_self - top);
       // (NaN scores leave the references alone: they are in the sums)
-      float sum = fmaf(w0, l2[0], fmaf(w1, l2[1], p_self));
+      float sum = fmaf(h0 * l2[0], h0, fmaf(h1 * l2[1], h1, p_self));
       if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
       if (s_self != s_self) sum = s_self;
-      sm.fin[n] = make_float4(w0, w1, p_self, split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+      sm.fin[n] = make_float4(h0 * h0, h1 * h1, p_self, split ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
       if (p.joined) sm.ml[n] = make_float2(top, sum);
       else if (split) p.part_ml[part0 + orow] = make_float2(top, sum);
       else if (p.lse != nullptr) p.lse[orow] = (top + lg2_approx(sum)) * 0.6931471805599453f;
@@ -2012,8 +2020,8 @@ __global__ void __launch_bounds__(kCombineWarps * 32)
   for (int j = 0; j < nsplit; ++j) {
     const float2 ml = part_ml[first + j * step];
     const float4 o = *reinterpret_cast<const float4*>(part_o + (first + j * step) * kD + 4 * lane);
-    const float w = ml.x == -INFINITY ? 0.0f : ex2_approx(ml.x - m_use);
-    l = fmaf(w, ml.y, l);
+    const float half = ml.x == -INFINITY ? 0.0f : ex2_approx(0.5f * (ml.x - m_use)), w = half * half;
+    l = fmaf(half * ml.y, half, l);
     // parts that saw no key hold zeros; what rounds a weight to zero adds nothing
     acc.x = fmaf(w, o.x, acc.x);
     acc.y = fmaf(w, o.y, acc.y);

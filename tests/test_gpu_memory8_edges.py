@@ -101,3 +101,29 @@ def test_the_debug_call_checks_its_tensors():
             api.cover_debug_attn_prefix8(q, *mem, *args, q0=0, mode=0)
     with pytest.raises(ValueError, match="k_exp"):
         api.cover_debug_attn_prefix8(q, *mem[:2], mem[2][:, :, :32].contiguous(), mem[3], q0=0, mode=0)
+
+
+PARTS = [(0, 1), (0, 2), (0, 4), (0, -2), (0, -4), (0, 102), (0, 107), (1, 1), (1, 4), (1, -4), (1, 105), (2, 1), (2, 4), (2, -4), (3, 1), (3, 4)]
+
+
+@pytest.mark.parametrize("mode,parts", PARTS)
+@pytest.mark.parametrize("order", ["small first", "large first", "in turns", "in pairs"])
+@pytest.mark.parametrize("large", [2, 36, 60, 90])
+def test_values_of_whole_tiles(mode, parts, order, large):
+    """KV tiles of zero value rows before, behind and between tiles of rows around 2^(large + 8): the keys of both count alike, in lse
+    and in the weights."""
+    L, B = 1024, 2
+    big = {"small first": [0] * 4 + [1] * 4, "large first": [1] * 4 + [0] * 4, "in turns": [0, 1] * 4, "in pairs": [0, 0, 1, 1, 0, 0, 0, 1]}[order]
+    mem, q = _mem(B, 1, L, scale=0.5), _r(B, 2, 3, 128, seed=3, scale=0.5)
+    rows = torch.tensor(big, device="cuda", dtype=torch.bool).repeat_interleave(128)
+    mem[3][:, :, rows] += large
+    mem[1].view(torch.uint8)[:, :, ~rows] = 0
+    mem[3][:, :, ~rows] = 127
+    kw = dict(key_hi=_i32([[L] * 3, [L - 200] * 3])) if parts > 100 else {}
+    got = _attn(q, mem, mode, nsplit=parts, q0=0, **kw)
+    _check(got, q, mem, q0=0, **kw)
+    # and where the first rows are small, not zero
+    mem[1].view(torch.uint8)[:, :, ~rows] = 0x3a
+    mem[3][:, :, ~rows] = 20
+    got = _attn(q, mem, mode, nsplit=parts, q0=0, **kw)
+    _check(got, q, mem, q0=0, **kw)
