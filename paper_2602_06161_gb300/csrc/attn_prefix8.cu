@@ -121,6 +121,13 @@ struct Params {
   float cap_ref;     // reference of all rows under a small cap, or -inf (see fixed_reference)
 };
 
+// The keys lo .. hi - 1 that row i of [B Lq] sees, held to 0 .. Lk: the bounds given may be any, and columns of a
+// KV tile are counted from them.
+__device__ __forceinline__ int2 keys_of(const Params& p, size_t i) {
+  const int lo = p.key_lo != nullptr ? __ldg(p.key_lo + i) : 0, hi = p.key_hi != nullptr ? __ldg(p.key_hi + i) : p.Lk;
+  return make_int2(min(max(lo, 0), p.Lk), min(max(hi, 0), p.Lk));
+}
+
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
@@ -723,8 +730,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool valid = warp < kDecodeWarp && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
   int row_lo = 0, row_hi = p.Lk;
-  if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
-  if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
+  if (valid) {
+    const int2 keys = keys_of(p, static_cast<size_t>(b) * p.Lq + r);
+    row_lo = keys.x, row_hi = keys.y;
+  }
   int lo_key = 0, hi_key = p.Lk;                      // keys that some row sees
   if (p.key_lo != nullptr || p.key_hi != nullptr) {
     if (warp < kDecodeWarp) {
@@ -1072,8 +1081,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool valid = warp < kPairSoftmaxWarps && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
   int row_lo = 0, row_hi = p.Lk;
-  if (valid && p.key_lo != nullptr) row_lo = max(0, __ldg(p.key_lo + static_cast<size_t>(b) * p.Lq + r));
-  if (valid && p.key_hi != nullptr) row_hi = min(p.Lk, __ldg(p.key_hi + static_cast<size_t>(b) * p.Lq + r));
+  if (valid) {
+    const int2 keys = keys_of(p, static_cast<size_t>(b) * p.Lq + r);
+    row_lo = keys.x, row_hi = keys.y;
+  }
   int lo_key = 0, hi_key = p.Lk;                        // keys that some row sees
   if (p.key_lo != nullptr || p.key_hi != nullptr) {
     if (warp < kPairSoftmaxWarps) {
@@ -1512,11 +1523,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   // ---------------- the sequence ----------------
   if (shared_out) {
     for (int i = tid; i < p.B * p.Lq; i += kRowsThreads) {
-      const int lo = p.key_lo != nullptr ? max(0, __ldg(p.key_lo + i)) : 0;
-      const int hi = p.key_hi != nullptr ? min(p.Lk, __ldg(p.key_hi + i)) : p.Lk;
-      if (lo < hi) {
-        atomicMin(&sm.seq_lo[i / p.Lq], lo);
-        atomicMax(&sm.seq_hi[i / p.Lq], hi);
+      const int2 keys = keys_of(p, i);
+      if (keys.x < keys.y) {
+        atomicMin(&sm.seq_lo[i / p.Lq], keys.x);
+        atomicMax(&sm.seq_hi[i / p.Lq], keys.y);
       }
     }
     __syncthreads();
@@ -1552,9 +1562,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       int lo = 0, hi = p.Lk, at = -1;
       if (tid < n_rows) {
         const int r = (p0 + tid) % p.Lq;
-        const size_t i = static_cast<size_t>(b) * p.Lq + r;
-        if (p.key_lo != nullptr) lo = max(0, __ldg(p.key_lo + i));
-        if (p.key_hi != nullptr) hi = min(p.Lk, __ldg(p.key_hi + i));
+        const int2 keys = keys_of(p, static_cast<size_t>(b) * p.Lq + r);
+        lo = keys.x, hi = keys.y;
         if (p.n_seeds > 0) {
           my_slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
           if (my_slot != kNoSlot) at = p.q0 + r;

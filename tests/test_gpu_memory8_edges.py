@@ -127,3 +127,20 @@ def test_values_of_whole_tiles(mode, parts, order, large):
     mem[3][:, :, ~rows] = 20
     got = _attn(q, mem, mode, nsplit=parts, q0=0, **kw)
     _check(got, q, mem, q0=0, **kw)
+
+
+@pytest.mark.parametrize("mode", [None, 0, 1, 2, 3])
+def test_bounds_of_every_size(mode):
+    """Rows whose bounds are the ends of int32, or say nothing in another way, among rows that see keys beyond the first KV tile: each
+    is held to the memory, whatever its neighbours see."""
+    Lq, Lk, q0 = 300, 700, 50
+    mem, q = _mem(1, 1, Lk), _r(1, 2, Lq, 128, seed=3)
+    seeds = (_r(1, 1, 4, 128, seed=4), _r(1, 1, 4, 128, seed=5), _i32([[60, 61, 62, 349]]))
+    ends = [-2 ** 31, -2 ** 31 + 1, -5, 0, 1, 300, Lk, Lk + 1, 2 ** 31 - 1, 2 ** 31 - 128]
+    pairs = [(a, b) for a in ends for b in ends] + [(300, 600), (0, 130), (500, Lk)] * 67
+    lo, hi = (_i32([[p[i] for p in pairs[:Lq]]]) for i in range(2))
+    at = torch.randperm(Lq, generator=torch.Generator().manual_seed(0)).cuda()
+    lo, hi = lo[:, at].contiguous(), hi[:, at].contiguous()
+    for kw in (dict(key_hi=hi), dict(key_lo=lo), dict(key_lo=lo, key_hi=hi), dict(key_lo=lo, key_hi=hi, softcap=20.0)):
+        got = _attn(q, mem, mode, seeds, q0=q0, **kw)
+        _check(got, q, mem, seeds, q0=q0, **kw)
