@@ -324,8 +324,8 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c)
  *     (c above 2^60 counts as 2^60).
  * What a row does not see does not reach it, NaN included; a row that sees a key with k_exp or
- * v_exp above 246 gets NaN in out and lse. (A NaN code, 0x7f or 0xff, which cover_kv8_write does
- * not write, counts as NaN or as 480 where it is seen.)
+ * v_exp above 246, or with a NaN code in its K or V row (0x7f or 0xff, which cover_kv8_write does
+ * not write), gets NaN in out and lse.
  * Which kernel runs depends on the sizes, and on whether key ranges and a cap are given; equal rows of
  * different calls agree up to rounding. The
  * weights are rounded to bf16 or to 9 significant bits for their products with V, and a weight that

@@ -23,7 +23,9 @@
 // tcgen05.mma with S, P and O in tensor memory. Two softmax warpgroups keep one stream each: the even and the odd KV
 // tiles, with sums and an accumulator of their own that are merged at the end, so that the chain load - decode - S - softmax -
 // P V of one KV tile overlaps the next one's. A KV tile takes 1.34 us; the most of it is decoding: two instructions a
-// code, and the 192 KB a tile that it and the products move through shared memory take 0.8 us at 128 bytes a clock.
+// code, and the 224 KB a tile that it, the look for NaN codes and the products move through shared memory take 0.9 us at 128 bytes a
+// clock. Codes are looked through before their bf16 tile is free, where the decoding threads would wait (8 x 32 heads, 64 x
+// 2048: 60 us; with the look inside the decoding 64, and 62 without any).
 // Roles (640 threads): warps 0-3, 4-7 softmax of stream 0, 1 (thread = row); 8-11 decode K, 12-15 V; 16 issues the
 // products; 17 and 18 the copies of K and V.
 // Shared memory: Q (32 KB) | two tiles of K and of V codes (16 KB each) | K, V in bf16 (2 x 32 KB each).
@@ -78,7 +80,7 @@ struct Ctl {
   uint32_t tmem_base;
   int abort;
   int lo, hi;                           // keys that some row of the CTA sees
-  uint4 nan_keys[4];                    // per KV tile in turn: keys with a V row of NaN
+  uint4 nan_keys[4];                    // per KV tile in turn: keys whose V row is NaN
 };
 
 struct Smem {
@@ -233,6 +235,18 @@ __device__ __forceinline__ void decode_row(uint32_t src, uint32_t d0, uint32_t d
   }
 }
 
+// Whether a row of codes holds a NaN; src as in decode_row.
+__device__ __forceinline__ bool nan_code(uint32_t src) {
+  uint32_t hit = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 c = lds128(src ^ (16u * i));
+    hit |= ((c.x & 0x7f7f7f7fu) + 0x01010101u) | ((c.y & 0x7f7f7f7fu) + 0x01010101u) | ((c.z & 0x7f7f7f7fu) + 0x01010101u) |
+           ((c.w & 0x7f7f7f7fu) + 0x01010101u);
+  }
+  return (hit & 0x80808080u) != 0;
+}
+
 __device__ __forceinline__ void decode(uint32_t src, uint32_t d0, uint32_t d1, int x, bool zero) {
   // bytes above 246 count as NaN (cover_kv8_write writes none but 255)
   const bool two = x > 134 && x <= kExpMax;
@@ -353,35 +367,31 @@ __device__ __forceinline__ void decode_tiles(Ctl& ctl, const Params& p, int whic
   const int left = min(p.Lk - first, nt * kBN);  // keys of this part
   // exponent bytes are fetched four tiles at a time, four to eight ahead of their use
   const uint8_t* exps = (which ? p.v_exp : p.k_exp) + mem0 + first;
-  const uint8_t* v_exps = p.v_exp + mem0 + first;
-  FourBytes x_next, v_next;
+  FourBytes x_next;
   x_next.load(exps, 0, row, left);
-  v_next.load(v_exps, 0, row, left);
-  uint32_t xs = 0, vs = 0;
+  uint32_t xs = 0;
   bool ok = true;
   for (int j = 0; j < nt; ++j) {
     const int st = j & 1;
     if ((j & 3) == 0) {
       xs = x_next.packed();
       x_next.load(exps, j + 4, row, left);
-      if (which == 0) {
-        vs = v_next.packed();
-        v_next.load(v_exps, j + 4, row, left);
-      }
     }
     const bool zero = j * kBN + row >= left;
-    const int x = (xs >> (8 * (j & 3))) & 255, xv = which ? x : static_cast<int>((vs >> (8 * (j & 3))) & 255);
-    const bool v_nan = xv > kExpMax;
-    const uint32_t nans = __ballot_sync(0xffffffffu, v_nan);
-    if (j >= 2) ok = warp_wait(which ? &ctl.v_empty[st] : &ctl.k_empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
-    ok = ok && warp_wait(&ctl.c_full[which][st], (j >> 1) & 1, &ctl.abort);
+    int x = (xs >> (8 * (j & 3))) & 255;
+    // codes are looked through while the bf16 tile is still read
+    ok = warp_wait(&ctl.c_full[which][st], (j >> 1) & 1, &ctl.abort);
     if (!ok) break;
-    // tile j - 4 has passed its softmax: S of tile j - 2 came after it
-    if (which == 0 && lane == 0) reinterpret_cast<uint32_t*>(&ctl.nan_keys[j & 3])[row >> 5] = nans;
-    // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the scores of their
-    // keys are made NaN instead
+    if (!zero && nan_code(codes + st * kCodeBytes)) x = kExpNan;
+    const uint32_t nans = __ballot_sync(0xffffffffu, x > kExpMax);
+    if (j >= 2) ok = warp_wait(which ? &ctl.v_empty[st] : &ctl.k_empty[st], ((j >> 1) - 1) & 1, &ctl.abort);
+    if (!ok) break;
+    // V: the softmax of tile j - 2, which read what stood here, is behind its products
+    if (which && lane == 0) reinterpret_cast<uint32_t*>(&ctl.nan_keys[j & 3])[row >> 5] = nans;
+    // a weight of zero times NaN is NaN: V rows of NaN are decoded as zeros, and the sums of the
+    // rows that see their keys are made NaN instead
     const uint32_t to = tile + st * kTileBytes;
-    decode(codes + st * kCodeBytes, to + box, to + (kBoxBytes - box), x, zero || (which && v_nan));
+    decode(codes + st * kCodeBytes, to + box, to + (kBoxBytes - box), x, zero || (which && x > kExpMax));
     mbar_arrive(&ctl.c_empty[which][st]);
     fence_proxy_async_smem();
     mbar_arrive(which ? &ctl.v_full[st] : &ctl.k_full[st]);
@@ -860,11 +870,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool fixed = kCap && p.cap_ref != -INFINITY;
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
+    // A row that sees a key whose V row is NaN has a NaN sum. V is decoded beside K, and that its tile is behind the softmax of the
+    // keys is no matter: the rows are known when its products are (waiting for them before took 5 % of a call).
+    const auto nan_values = [&](int t) {
+      const uint32_t* nan = reinterpret_cast<const uint32_t*>(&ctl.nan_keys[t & 3]);
+#pragma unroll 1
+      for (int w = 0; w < 4; ++w) {
+        for (uint32_t bits = nan[w]; bits != 0; bits &= bits - 1) {
+          const int at = (j0 + t) * kBN + 32 * w + __ffs(bits) - 1;
+          if (at >= row_lo && at < row_hi && !(is_seed && at == pos)) l_run = __uint_as_float(0x7fc00000u);
+        }
+      }
+    };
     int i = 0;   // the stream's step
     for (int j = stream; j < nt; j += 2, ++i) {
       ok = warp_wait(&ctl.s_full[stream], i & 1, &ctl.abort);
       if (!ok) break;
       tc_fence_after_sync();
+      if (i > 0) nan_values(j - 2);   // its products were issued before this S, and V's tile j + 2 waits for this one's
       const int key0 = (j0 + j) * kBN;
       const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch are seen
       if (!__any_sync(0xffffffffu, valid && max(cl, 0) < min(ch, kBN))) {
@@ -879,7 +902,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(&ctl.p_full[stream]);
         continue;
       }
-      const uint32_t* nan = reinterpret_cast<const uint32_t*>(&ctl.nan_keys[j & 3]);
       const bool own_column = warp_seed && __any_sync(0xffffffffu, is_seed && pos >= key0 && pos < key0 + kBN);
       const Unseen u{cl, ch, is_seed ? pos - key0 : -1, own_column || __any_sync(0xffffffffu, valid && (cl > 0 || ch < kBN))};
       float alpha = 1.0f;
@@ -887,7 +909,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!fixed) {
         float m_tile = -INFINITY;
 #pragma unroll 1
-        for (int c = 0; c < kBN; c += 32) m_tile = fmaxf(m_tile, chunk_max(s_addr + c, p, u, nan[c >> 5], c));
+        for (int c = 0; c < kBN; c += 32) m_tile = fmaxf(m_tile, chunk_max(s_addr + c, p, u, 0, c));
         m_tile = reference_of<kCap>(m_tile, p);
         if (m_tile > m_run + kRescaleThreshold) {
           alpha = (m_run == -INFINITY) ? 0.0f : ex2_approx(m_run - m_tile);
@@ -899,7 +921,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       l_run *= alpha;
 #pragma unroll 1
       for (int c = 0; c < kBN; c += 32)
-        l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, nan[c >> 5], c, m_use, fixed, valid);
+        l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, 0, c, m_use, fixed, valid);
       if (i > 0 && __any_sync(0xffffffffu, rescaled)) {
         // O holds the stream's earlier products (complete: the commit of this S came after them)
 #pragma unroll 1
@@ -917,6 +939,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_arrive(&ctl.p_full[stream]);
     }
     if (ok && nt > 0) ok = warp_wait(&ctl.o_full, 0, &ctl.abort);
+    if (ok && i > 0) nan_values(stream + 2 * (i - 1));
     if (!ok && lane == 0) {
       if (!ctl.abort) report_status(p.status, kStatusTimeout, 73);
       ctl.abort = 1;

@@ -144,3 +144,26 @@ def test_bounds_of_every_size(mode):
     for kw in (dict(key_hi=hi), dict(key_lo=lo), dict(key_lo=lo, key_hi=hi), dict(key_lo=lo, key_hi=hi, softcap=20.0)):
         got = _attn(q, mem, mode, seeds, q0=q0, **kw)
         _check(got, q, mem, seeds, q0=q0, **kw)
+
+
+@pytest.mark.parametrize("mode,parts", [(0, 1), (0, 3), (1, 1), (2, 1), (2, 3), (2, -2), (3, 1), (3, 3), (4, 1), (None, None)])
+@pytest.mark.parametrize("code", [0x7f, 0xff])
+@pytest.mark.parametrize("which", [0, 1])
+def test_nan_codes(mode, parts, code, which):
+    """A code of NaN in a key or value row is a NaN row of the keys' readers, whichever kernel runs; to others it is nothing."""
+    Lq, L = 200, 700
+    mem, q = _mem(1, 2, L), _r(1, 4, Lq, 128, seed=3)
+    kw = dict(q0=0) if mode is None else dict(q0=0, nsplit=parts)
+    hi = None
+    if mode != 4:
+        hi = _i32([[400] * 40 + [L] * (Lq - 40)])
+        kw["key_hi"] = hi
+    ref = _attn(q, mem, mode, **kw)
+    for at, column in ((450, 0), (600, 127), (511, 77)):
+        m = tuple(x.clone() for x in mem)
+        m[which].view(torch.uint8)[0, 1, at, column] = code
+        out, lse = _attn(q, m, mode, **kw)
+        sees = torch.ones((1, 4, Lq), dtype=torch.bool, device="cuda") if hi is None else (hi > at)[:, None].repeat(1, 4, 1)
+        sees[:, :2] = False
+        assert out.isnan().all(-1)[sees].all() and lse.isnan()[sees].all()
+        assert torch.equal(out[~sees], ref[0][~sees]) and torch.equal(lse[~sees], ref[1][~sees])
