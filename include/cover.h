@@ -331,6 +331,8 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  * weights are rounded to bf16 or to 9 significant bits for their products with V, and a weight that
  * is, times its value's scale, below 2^-28 of the row's largest such product may count as zero in
  * out (not in lse).
+ * Scores and sums are fp32: they hold where the largest elements of a query row and a key row multiply to less than 2^120 and
+ * the values seen are at most 2^100, and 2^119 / Lk, in magnitude; beyond, a row may get infinities or NaN or lose small weights.
  * workspace: cover_attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) bytes, 16-byte aligned, no initialisation
  * needed (NULL if that is 0). It is scratch of the call alone: calls that share one must not
  * run concurrently on the GPU.

@@ -80,6 +80,7 @@ struct Ctl {
   uint32_t tmem_base;
   int abort;
   int lo, hi;                           // keys that some row of the CTA sees
+  int wide;                             // a V row's byte is outside those that a fixed reference serves
   uint4 nan_keys[4];                    // per KV tile in turn: keys whose V row is NaN
 };
 
@@ -121,6 +122,7 @@ struct Params {
   float cap_x;       // 1 / (cap sqrt(d))
   float cap_poly[4]; // coefficients of the capped score's polynomial, in powers of 1 / (cap sqrt(d))
   float cap_ref;     // reference of all rows under a small cap, or -inf (see fixed_reference)
+  uint32_t v_lo, v_hi;   // bytes of the V rows that it serves, in all four bytes
 };
 
 // The keys lo .. hi - 1 that row i of [B Lq] sees, held to 0 .. Lk: the bounds given may be any, and columns of a
@@ -323,6 +325,7 @@ __device__ __forceinline__ void set_up(Ctl& ctl, const CUtensorMap* tm_q, uint32
     ctl.abort = 0;
     ctl.lo = 0x7fffffff;
     ctl.hi = 0;
+    ctl.wide = 0;
     fence_mbar_init();
     tma_prefetch_desc(tm_q);
   }
@@ -554,6 +557,21 @@ __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const
   return (r[0] + r[1]) + (r[2] + r[3]);
 }
 
+// Whether some of n bytes lies outside those of lo .. hi (four copies each); the threads' parts of it, tid of kAll.
+template <int kAll>
+__device__ __forceinline__ bool bytes_outside(const uint8_t* bytes, int n, int tid, uint32_t lo, uint32_t hi) {
+  const auto one = [&](int i) { return __ldg(bytes + i) < (lo & 255u) || __ldg(bytes + i) > (hi & 255u); };
+  const int head = min(n, static_cast<int>(-reinterpret_cast<uintptr_t>(bytes) & 15)), wide = (n - head) / 16;
+  uint32_t out = tid < head && one(tid) ? 1 : 0;
+  for (int i = tid; i < wide; i += kAll) {
+    const uint4 w = __ldg(reinterpret_cast<const uint4*>(bytes + head) + i);
+    out |= __vcmpltu4(w.x, lo) | __vcmpgtu4(w.x, hi) | __vcmpltu4(w.y, lo) | __vcmpgtu4(w.y, hi);
+    out |= __vcmpltu4(w.z, lo) | __vcmpgtu4(w.z, hi) | __vcmpltu4(w.w, lo) | __vcmpgtu4(w.w, hi);
+  }
+  const int last = head + 16 * wide + tid;
+  return out != 0 || (last < n && one(last));
+}
+
 // A seed row's own score in log2 units: q row `row` of [B Hq Lq], masked-input key row `self`.
 template <bool kCap>
 __device__ __forceinline__ float self_score(const Params& p, long long row, size_t self) {
@@ -687,6 +705,9 @@ __device__ __forceinline__ void join_pass() {
   cluster_sync();
   cluster_sync();
 }
+
+// All 512 softmax threads of the pairs kernel.
+__device__ __forceinline__ void pairs_sync() { asm volatile("bar.sync 1, 512;" ::: "memory"); }
 
 // Barrier of one Q tile's 256 softmax threads of the pairs kernel, and with the vote whether any of them says so.
 __device__ __forceinline__ void tile_sync(int tile) { asm volatile("bar.sync %0, 256;" ::"r"(2 + tile) : "memory"); }
@@ -867,7 +888,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool warp_live = __any_sync(0xffffffffu, valid);
     const uint32_t s_addr = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + stream * kBN;
     const uint32_t o_addr = s_addr + 2 * kBN;
-    const bool fixed = kCap && p.cap_ref != -INFINITY;
+    // a reference of all rows where the part's V rows allow it
+    bool fixed = kCap && p.cap_ref != -INFINITY;
+    if (fixed) {
+      if (bytes_outside<2 * kBM>(p.v_exp + mem0 + static_cast<size_t>(j0) * kBN, min(p.Lk - j0 * kBN, nt * kBN), tid, p.v_lo, p.v_hi))
+        ctl.wide = 1;
+      softmax_sync();
+      fixed = ctl.wide == 0;
+    }
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
     // A row that sees a key whose V row is NaN has a NaN sum. V is decoded beside K, and that its tile is behind the softmax of the
@@ -1220,7 +1248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int i = at >= r0 ? at - r0 : at - r0 + p.Lq;
         if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
       }
-      asm volatile("bar.sync 1, 512;" ::: "memory");   // all softmax threads
+      pairs_sync();
       if (valid) slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
     }
     const int pos = p.q0 + r;
@@ -1233,7 +1261,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = quad + tile * kBN + half * kHalf;
     const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
-    const bool fixed = kCap && p.cap_ref != -INFINITY;
+    // a reference of all rows where the part's V rows allow it
+    bool fixed = kCap && p.cap_ref != -INFINITY;
+    if (fixed) {
+      const size_t first = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk + static_cast<size_t>(j0) * kBN;
+      if (bytes_outside<4 * kBM>(p.v_exp + first, min(p.Lk - j0 * kBN, nt * kBN), tid, p.v_lo, p.v_hi)) ctl.wide = 1;
+      pairs_sync();
+      fixed = ctl.wide == 0;
+    }
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
@@ -2073,11 +2108,18 @@ constexpr int kModes = 5;
 constexpr int kModeRows[kModes] = {16, 32, kBM, 2 * kBM, 1};   // packed rows of a CTA
 
 // Capped scores lie in [-C, C], C = cap log2(e). For C <= 75 (caps up to 52) every row takes the same reference, C - 45 or
-// 0, and no maxima are looked for: the weights lie in [2^(45 - 2 C), 2^45], at least 2^-105, and 2^17 of
-// the largest times values of up to 2^65 stay below fp32's largest number. (Caps below 2^-10 would put powers of 1 / cap
-// beyond it.)
+// 0, and no maxima are looked for: the weights lie in [2^(45 - 2 C), 2^45], at least 2^-105. (Caps below 2^-10 would put powers
+// of 1 / cap beyond fp32's largest number.)
 float fixed_reference(float cap_log2) {
   return cap_log2 >= 1.0f / 1024.0f && cap_log2 <= 75.0f ? fmaxf(0.0f, cap_log2 - 45.0f) : -INFINITY;
+}
+// The bytes of V rows that such a reference serves: L keys of the largest weight and the largest code (below 2^9) stay below
+// 2^126, and the smallest weight times the smallest code (2^-9) is not below 2^-126. Cap 30 over 8192 keys: 53 .. 188, values up
+// to 2^70; cap 50: 110 .. 187, rows whose largest element is above 0.002. A CTA one of whose V rows has another byte looks
+// for maxima.
+void fixed_bytes(float cap_log2, float cap_ref, int L, uint32_t* lo, uint32_t* hi) {
+  *lo = static_cast<uint32_t>(std::max(0.0f, std::ceil(10.0f + cap_log2 + cap_ref)));
+  *hi = static_cast<uint32_t>(std::floor(127.0f + 126.0f - 9.0f - (cap_log2 - cap_ref) - std::ceil(std::log2(static_cast<float>(L)))));
 }
 
 // Whether the parts of a batch with key ranges can be shared out to its sequences (every CTA looks through the ranges).
@@ -2316,6 +2358,10 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
   p.cap_x = cap ? 1.0f / (softcap * root) : 0.0f;
   p.cap_ref = cap ? fixed_reference(p.cap_log2) : -INFINITY;
+  if (p.cap_ref != -INFINITY) {
+    fixed_bytes(p.cap_log2, p.cap_ref, a.L, &p.v_lo, &p.v_hi);
+    p.v_lo *= 0x01010101u, p.v_hi *= 0x01010101u;
+  }
   const float tanh_poly[4] = {kTanh0, kTanh1, kTanh2, kTanh3};
   float power = p.cap_log2 * p.cap_x;
   for (int i = 0; i < 4; ++i, power *= p.cap_x * p.cap_x) p.cap_poly[i] = p.cap_ref != -INFINITY ? tanh_poly[i] * power : 0.0f;

@@ -167,3 +167,40 @@ def test_nan_codes(mode, parts, code, which):
         sees[:, :2] = False
         assert out.isnan().all(-1)[sees].all() and lse.isnan()[sees].all()
         assert torch.equal(out[~sees], ref[0][~sees]) and torch.equal(lse[~sees], ref[1][~sees])
+
+
+@pytest.mark.parametrize("mode", [None, 0, 1, 2, 3])
+@pytest.mark.parametrize("cap", [5.0, 30.0, 50.0, 51.9])
+@pytest.mark.parametrize("byte", [20, 60, 95, 119, 160, 184, 200, 218])
+def test_capped_values_of_every_size(mode, cap, byte):
+    """Scores at both ends of the cap with value rows of every size: sums neither overflow nor vanish."""
+    B, Lq, L = 2, 40, 900
+    mem, q = _mem(B, 2, L, scale=0.3), _r(B, 4, Lq, 128, seed=3, scale=0.3)
+    mem[3].fill_(byte)
+    mem[3][:, :, ::3] -= 2
+    for shift in (0.0, 30.0, -30.0):       # all scores alike, near the cap, near its opposite
+        k = (_r(B, 2, L, 128, seed=8, scale=0.3) + shift * torch.sign(q[:, ::2, :1].float())).bfloat16()
+        v = api.kv8_memory(B, 2, L)
+        api.cover_kv8_write(k, k, *v)
+        m = (v[0], mem[1], v[2], mem[3])
+        got = _attn((q + 0.1 * torch.sign(q[:, :, :1])).bfloat16() if shift else q, m, mode, q0=0, softcap=cap)
+        _check(got, (q + 0.1 * torch.sign(q[:, :, :1])).bfloat16() if shift else q, m, q0=0, softcap=cap)
+
+
+@pytest.mark.parametrize("mode", [2, 3])
+@pytest.mark.parametrize("L,H", [(900, 3), (1025, 2), (129, 1)])
+@pytest.mark.parametrize("byte", [30, 210, 255])
+def test_one_value_row_outside_the_others_range(mode, L, H, byte):
+    """Wherever it lies in the memory, of which a head may start at any byte: its CTA's sums hold, and so do the others'."""
+    mem, q = _mem(1, H, L), _r(1, H, 60, 128, seed=3)
+    at = _i32([[L - 60 + i for i in range(60)]])
+    for row in (0, 1, 15, 16, 17, 127, 128, L // 2, L - 17, L - 2, L - 1):
+        m = tuple(x.clone() for x in mem)
+        m[3][0, H - 1, row] = byte
+        for kw in (dict(), dict(nsplit=2, key_hi=(at + 1).contiguous())):
+            got = _attn(q, m, mode, q0=L - 60, softcap=50.0, **kw)
+            if byte < 255:
+                _check(got, q, m, q0=L - 60, softcap=50.0, key_hi=kw.get("key_hi"))
+            else:
+                sees = torch.ones((1, 1, 60), dtype=torch.bool, device="cuda") if "key_hi" not in kw else (kw["key_hi"] > row)[:, None]
+                assert torch.equal(got[1][:, -1:].isnan(), sees) and not got[1][:, :-1].isnan().any()
