@@ -322,7 +322,7 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  *     those before, documents. A row that sees no key gets out = 0, lse = -inf.
  *     A seed row's own pair is seen where its position is.
  *   softcap  0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c)
- *     (c above 2^60 counts as 2^60).
+ *     (c above 2^60 counts as 2^60, c below 2^-30 as 2^-30).
  * What a row does not see does not reach it, NaN included; a row that sees a key with k_exp or
  * v_exp above 246, or with a NaN code in its K or V row (0x7f or 0xff, which cover_kv8_write does
  * not write), gets NaN in out and lse.

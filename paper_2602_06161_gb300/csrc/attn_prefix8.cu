@@ -167,6 +167,8 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // 0.4 of their cap, and then two special-function operations an element are saved.
 constexpr float kTanhRange = 0.4f;
 constexpr float kMaxCap = 1.1529215e18f;   // 2^60: larger caps count as this one; its reciprocal times the rows' scales is a normal number
+// 2^-30: smaller caps count as this one, whose scores change no weight in fp32 (its reciprocal is a number, 0 times infinity none)
+constexpr float kMinCap = 9.3132257e-10f;
 constexpr float kTanh0 = 0.999999903f, kTanh1 = -0.333313733f, kTanh2 = 0.132711566f, kTanh3 = -0.0475610772f;
 
 // Shared memory by its 32-bit address.
@@ -2353,7 +2355,7 @@ int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream) {
   p.joined = plan.joined ? 1 : 0;
   p.scale_log2 = log2e / root;
   const bool cap = a.softcap > 0.0f;
-  const float softcap = fminf(a.softcap, kMaxCap);
+  const float softcap = fminf(fmaxf(a.softcap, kMinCap), kMaxCap);
   p.cap_log2 = softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
   p.cap_x = cap ? 1.0f / (softcap * root) : 0.0f;

@@ -204,3 +204,14 @@ def test_one_value_row_outside_the_others_range(mode, L, H, byte):
             else:
                 sees = torch.ones((1, 1, 60), dtype=torch.bool, device="cuda") if "key_hi" not in kw else (kw["key_hi"] > row)[:, None]
                 assert torch.equal(got[1][:, -1:].isnan(), sees) and not got[1][:, :-1].isnan().any()
+
+
+@pytest.mark.parametrize("mode", [None, 0, 1, 2, 3])
+@pytest.mark.parametrize("cap", [1e-3, 1e-9, 1e-20, 1e-38, 1e-45])
+def test_small_caps(mode, cap):
+    """Scores that are all capped to nothing weigh alike, a score of 0 among them."""
+    mem, q = _mem(1, 2, 300), _r(1, 4, 40, 128, seed=3)
+    q[:, :, ::3] = 0
+    mem[0].view(torch.uint8)[:, :, ::2] = 0
+    got = _attn(q, mem, mode, q0=0, softcap=cap)
+    _check(got, q, mem, q0=0, softcap=cap)
