@@ -266,7 +266,7 @@ int cover_seed_kv_override(void* k, void* v, const int32_t* seed_idx, int n_seed
  *            last dimension is dense); read before the call returns. Rows laid out as a
  *            projection leaves them ([B, L, H, D] in memory) need no transposition.
  *   inv_freq [R / 2] fp64; the angle is reduced exactly modulo a turn, so positions
- *            far out lose nothing
+ *            far out lose nothing (the columns of one that is not finite are NaN)
  *   pos      [B, L] int32 position of every row (any value), or NULL: row l is at pos0 + l
  * k is NULL and Hkv is 0 where only q is wanted. q_out may be q with the same
  * strides (in place), likewise k; outputs that overlap an input in another way, or

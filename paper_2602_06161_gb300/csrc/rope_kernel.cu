@@ -14,7 +14,9 @@
 // Bound by memory: each row is read and written once. A thread holds one 16-byte vector column (two, R / 2
 // apart, in the layout of halves) of one token and walks over up to eight heads, so that its sines and cosines serve
 // all of them. The first rows and the position are loaded before the frequencies are made ready and waited for (8 x 32 + 32 heads,
-// 64 tokens of 64 fp32: 8.7 us without that and with a head a thread, 3.5 so; 4 tokens of 28 + 4 heads 2.9 and 2.3).
+// 64 tokens of 64 fp32: 8.7 us without that and with a head a thread, 3.9 so; 4 tokens of 28 + 4 heads 2.9 and 2.4).
+// A frequency that is not finite has no turns: the CTA's barrier says whether there is one, and its columns are NaN then (a mark
+// among the turns, looked at pair by pair, took 1 % of a prompt's time).
 // More threads with fewer loads each are faster than the opposite where the rows come from HBM: 4 x 40 heads, 8191
 // tokens of 128 bf16 took 117 us with one head in flight a thread and four CTAs of 256 an SM, 132 with two and three, 165
 // with four and two, 253 with eight (2048 tokens of one sequence, which stay in L2: 10.3 and 8.7 with two and three); in
@@ -75,6 +77,8 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_f(float x) {
   return __float2bfloat16_rn(x);
 }
+
+__device__ __forceinline__ int not_finite(double x) { return (__double2hiint(x) & 0x7ff00000) == 0x7ff00000; }
 
 template <typename T, int N>
 struct alignas(sizeof(T) * N) Vec {
@@ -141,11 +145,13 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) rope_kernel(
   int32_t at = static_cast<int32_t>(static_cast<uint32_t>(p.pos0) + l);
   if (p.pos != nullptr && turn) at = p.pos[rest];
   load(0);
+  int bad = 0;   // some frequency is not finite: the exponent bits are all set
   for (int i = threadIdx.x; i < p.R / 2; i += kThreads) {
-    const double f = p.inv_freq[i] * 0.15915494309189535;   // / 2 pi
+    const double radians = p.inv_freq[i], f = radians * 0.15915494309189535;   // / 2 pi
     turns[i] = __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+    bad |= not_finite(radians);
   }
-  __syncthreads();
+  bad = __syncthreads_or(bad);
   float cs[kHalf], sn[kHalf];
   if (turn) {
 #pragma unroll
@@ -157,6 +163,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) rope_kernel(
       sincospif(x, &s, &co);
       cs[i] = co * p.mscale;
       sn[i] = (p.inverse ? -s : s) * p.mscale;
+    }
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i)
+        if (not_finite(p.inv_freq[u * kHalf + i])) cs[i] = sn[i] = __uint_as_float(0x7fc00000u);
     }
   }
   for (int i0 = 0; i0 < n; i0 += kHeadsInFlight) {

@@ -215,3 +215,32 @@ def test_small_caps(mode, cap):
     mem[0].view(torch.uint8)[:, :, ::2] = 0
     got = _attn(q, mem, mode, q0=0, softcap=cap)
     _check(got, q, mem, q0=0, softcap=cap)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D", [64, 6])
+def test_frequencies_that_are_not_finite(dtype, inter, D):
+    """Their columns are NaN, as the formula's are; the others are as without them."""
+    x = _r(1, 2, 5, D, seed=3, dtype=dtype)
+    f, _ = api.rope_frequencies(D)
+    ref, _ = api.cover_rope_fwd(x, None, f, pos0=3, interleaved=inter)
+    g = f.clone()
+    g[0], g[2] = math.inf, math.nan
+    y, _ = api.cover_rope_fwd(x, None, g, pos0=3, interleaved=inter)
+    cols = torch.zeros(D, dtype=torch.bool, device="cuda")
+    for i in (0, 2):
+        cols[[2 * i, 2 * i + 1] if inter else [i, i + D // 2]] = True
+    assert y[..., cols].isnan().all() and torch.equal(y[..., ~cols], ref[..., ~cols])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_columns_that_do_not_turn_are_copied(inter, inverse):
+    """By the rotation and by its gradient alike, bit for bit, NaN and infinities too."""
+    x = _r(2, 3, 5, 16, seed=3, dtype=torch.float32)
+    x[0, 0, 0, 12], x[1, 2, 3, 15], x[0, 1, 1, 14] = math.nan, math.inf, -0.0
+    f, _ = api.rope_frequencies(12)
+    y, _ = api.cover_rope_fwd(x, None, f, pos0=5, interleaved=inter, mscale=1.5, inverse=inverse)
+    assert torch.equal(y[..., 12:].contiguous().view(torch.int32), x[..., 12:].contiguous().view(torch.int32))
+    assert not torch.equal(y[..., :12], x[..., :12])
