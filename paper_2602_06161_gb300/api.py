@@ -45,6 +45,19 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _int32(name, x):
+    """A number for an int of the C ABI, which ctypes would cut to its lower 32 bits."""
+    x = int(x)
+    if not -0x80000000 <= x <= 0x7fffffff:
+        raise ValueError(f"{name} must fit 32 bits, got {x}")
+    return x
+
+
+def _sizes_fit(t, name):
+    if t.numel() > 0x7fffffff and max(t.shape) > 0x7fffffff:
+        raise ValueError(f"{name} must not be longer than 2^31 - 1 in a dimension, got {tuple(t.shape)}")
+
+
 def _maker(stream, device):
     """make(shape, dtype, zero=False): a tensor that a call makes for itself, a result or a workspace. Of a given stream
     that is not the current one it comes from that stream's memory: a block of the current stream's may still be read
@@ -82,6 +95,7 @@ def _need(t: torch.Tensor, name: str, dtype, ndim: int):
         raise ValueError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    _sizes_fit(t, name)
 
 
 def _attn(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, seed_idx, out, lse, want_lse, stream):
@@ -174,7 +188,7 @@ def _attn_prefix(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, 
     code = getattr(_lib.load(), fn_name)(
         _ptr(q), _ptr(k_cached), _ptr(v_cached),
         _ptr(k_seedmask) if n_seeds else None, _ptr(v_seedmask) if n_seeds else None,
-        _ptr(seed_idx) if n_seeds else None, n_seeds, B, Hq, Hkv, Lq, Lk, int(q0), D,
+        _ptr(seed_idx) if n_seeds else None, n_seeds, B, Hq, Hkv, Lq, Lk, _int32("q0", q0), D,
         _ptr(out), _ptr(lse), *extra, _stream(stream))
     _lib.check(fn_name, code)
     return out, lse
@@ -371,6 +385,7 @@ def _rows_need(t, name: str, dtypes, device=None):
         raise ValueError(f"{name} must have 4 dims, got {tuple(t.shape)}")
     if t.shape[3] > 1 and t.stride(3) != 1:
         raise ValueError(f"{name} must be dense in its last dimension")
+    _sizes_fit(t, name)
     if device is not None and t.device != device:
         raise ValueError(f"{name} must be on {device}, got {t.device}")
 
@@ -505,7 +520,7 @@ def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool
     st = _strides(q, k if has_k else q, oq, ok if has_k else oq)
     _launch("cover_rope_fwd", dev, stream,
             (_ptr(q), _ptr(k) if has_k else None, _ptr(oq), _ptr(ok) if has_k else None, ctypes.addressof(st), B, Hq,
-             k.shape[1] if has_k else 0, L, D, 2 * inv_freq.shape[0], _ptr(inv_freq) or None, _ptr(pos), int(pos0),
+             k.shape[1] if has_k else 0, L, D, 2 * inv_freq.shape[0], _ptr(inv_freq) or None, _ptr(pos), _int32("pos0", pos0),
              1 if interleaved else 0, float(mscale), 1 if inverse else 0, q.element_size()))
     return oq, ok
 
@@ -588,7 +603,7 @@ def cover_kv8_write(k, v, k8, v8, k_exp, v_exp, *, pos=None, pos0: int = 0, stre
     _kv8_pos(pos, B, n, k8.device)
     st = _strides(k, v)
     _launch("cover_kv8_write", k8.device, stream,
-            (_ptr(k), _ptr(v), ctypes.addressof(st), _ptr(pos) if n else None, int(pos0), n, B, Hkv, L, D, k.element_size(),
+            (_ptr(k), _ptr(v), ctypes.addressof(st), _ptr(pos) if n else None, _int32("pos0", pos0), n, B, Hkv, L, D, k.element_size(),
              _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp)))
 
 
@@ -605,20 +620,21 @@ def cover_kv8_read(k8, v8, k_exp, v_exp, *, pos=None, pos0: int = 0, n: Optional
         raise TypeError(f"dtype must be torch.bfloat16 or torch.float32, got {dtype}")
     B, Hkv, L, D = k8.shape
     if n is None:
-        n = int(pos.shape[1]) if pos is not None else max(0, L - int(pos0))
-    if n < 0:
+        n = int(pos.shape[1]) if pos is not None else max(0, L - _int32("pos0", pos0))
+    if _int32("n", n) < 0:
         raise ValueError("n must not be negative")
     _kv8_pos(pos, B, n, k8.device)
     make = _maker(stream, k8.device)
     k, v = (make((B, Hkv, n, D), dtype) for _ in range(2))
     _launch("cover_kv8_read", k8.device, stream,
-            (_ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(pos) if n else None, int(pos0), n, B, Hkv, L, D,
+            (_ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(pos) if n else None, _int32("pos0", pos0), n, B, Hkv, L, D,
              k.element_size(), _ptr(k) if n else None, _ptr(v) if n else None))
     return k, v
 
 
 def cover_attn_prefix8_workspace_bytes(B: int, Hq: int, Hkv: int, Lq: int, Lk: int) -> int:
-    return int(_lib.load().cover_attn_prefix8_workspace_bytes(int(B), int(Hq), int(Hkv), int(Lq), int(Lk)))
+    sizes = [_int32(name, x) for name, x in (("B", B), ("Hq", Hq), ("Hkv", Hkv), ("Lq", Lq), ("Lk", Lk))]
+    return int(_lib.load().cover_attn_prefix8_workspace_bytes(*sizes))
 
 
 def _attn8_need(q, k8, v8, k_exp, v_exp, k_seedmask, v_seedmask, seed_idx, key_lo, key_hi):
@@ -690,7 +706,7 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
     _same_device(dev, out=out, lse=lse, workspace=workspace)
     _launch("cover_attn_fwd_prefix8", dev, stream,
             (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
-             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, int(q0), D,
+             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, _int32("q0", q0), D,
              _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(workspace) if nbytes else None))
     return out, lse
 
@@ -754,7 +770,7 @@ def cover_score_decide_fwd(logits, n_seq: int, tok, flags, remask_cnt, *, tau_dr
         workspace = make(*_decide_workspace(N, n_seq), zero=True)
     code = _lib.load().cover_score_decide_fwd(
         _ptr(logits), N, V, n_seq, _ptr(d_in), _ptr(d_out), _ptr(draft_ok), float(tau_draft), int(draft_budget),
-        int(remask_budget), int(mask_id), 1 if min_one else 0, int(pos0), int(max_seeds), int(phase),
+        int(remask_budget), int(mask_id), 1 if min_one else 0, _int32("pos0", pos0), int(max_seeds), int(phase),
         _ptr(tok), _ptr(flags), _ptr(remask_cnt), _ptr(out["maxprob"]), _ptr(out["entropy"]), _ptr(out["argmax"]),
         _ptr(out["score"]), _ptr(out["seed_idx"]) if max_seeds > 0 else None, _ptr(out["n_seeds"]),
         _ptr(out["stats"]), _ptr(workspace), _stream(stream))
@@ -783,7 +799,7 @@ def cover_seed_select_fwd(n_seq: int, tok, flags, remask_cnt, workspace, *, rema
         out = dict(score=make(N, torch.float32), seed_idx=make((n_seq, max(max_seeds, 0)), torch.int32),
                    n_seeds=make(n_seq, torch.int32), stats=make((n_seq, 6), torch.int32, zero=True))
     code = _lib.load().cover_seed_select_fwd(
-        N, n_seq, _ptr(d_in), _ptr(d_out), int(remask_budget), int(mask_id), int(pos0), int(max_seeds),
+        N, n_seq, _ptr(d_in), _ptr(d_out), int(remask_budget), int(mask_id), _int32("pos0", pos0), int(max_seeds),
         _ptr(tok), _ptr(flags), _ptr(remask_cnt), _ptr(out["score"]),
         _ptr(out["seed_idx"]) if max_seeds > 0 else None, _ptr(out["n_seeds"]), _ptr(out["stats"]),
         _ptr(workspace), _stream(stream))
@@ -831,7 +847,7 @@ def cover_attn_mass_fwd(q, k_cached, lse, tok, flags, *, mask_id: int, pos0: int
         d_out = make(B * per, torch.float32)
     code = _lib.load().cover_attn_mass_fwd(
         _ptr(q), _ptr(k_cached), _ptr(k_seedmask) if n_seeds else None, _ptr(seed_idx) if n_seeds else None,
-        n_seeds, _ptr(lse), B, Hq, Hkv, L, D, _ptr(tok), _ptr(flags), int(mask_id), int(pos0), int(per),
+        n_seeds, _ptr(lse), B, Hq, Hkv, L, D, _ptr(tok), _ptr(flags), int(mask_id), _int32("pos0", pos0), int(per),
         _ptr(workspace), _ptr(d_in), _ptr(d_out), _stream(stream))
     _lib.check("cover_attn_mass_fwd", code)
     return d_in, d_out
@@ -897,8 +913,8 @@ def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmas
     ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
     _launch("cover_debug_attn_prefix8", q.device, None,
             (_ptr(q), _ptr(k8), _ptr(v8), _ptr(k_exp), _ptr(v_exp), _ptr(k_seedmask) if S else None,
-             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, int(q0), D,
-             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), int(mode), int(nsplit)))
+             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, B, Hq, Hkv, Lq, Lk, _int32("q0", q0), D,
+             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _int32("mode", mode), _int32("nsplit", nsplit)))
     return out, lse
 
 

@@ -57,3 +57,32 @@ def test_the_debug_call_checks_its_tensors():
         api.cover_debug_attn_prefix8(q, *mem, q0=0, mode=0)
     with pytest.raises(TypeError, match="q must be"):
         api.cover_debug_attn_prefix8(q.float(), *mem, q0=0, mode=0)
+
+
+def test_numbers_above_32_bits_are_refused(monkeypatch):
+    """ctypes cuts them: row 2^32 of a memory would be row 0. (On tensors that pass for CUDA ones; nothing is launched.)"""
+    def launch(*a):
+        raise AssertionError("launched")
+
+    class Hands:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(api, "_launch", launch)
+    monkeypatch.setattr(api, "_nat", Hands())
+    monkeypatch.setattr(api, "_need", lambda *a: None)
+    monkeypatch.setattr(api, "_rows_need", lambda *a: None)
+    mem, x = api.kv8_memory(1, 2, 16, device="cpu"), torch.zeros(1, 2, 4, 128, dtype=torch.bfloat16)
+    f = torch.zeros(64, dtype=torch.float64)
+    for big in (2 ** 32, 2 ** 31, -2 ** 31 - 1, 2 ** 63, 2 ** 64 + 1):
+        for call in (lambda: api.cover_rope_fwd(x, x, f, pos0=big), lambda: api.cover_kv8_write(x, x, *mem, pos0=big),
+                     lambda: api.cover_kv8_read(*mem, pos0=big, n=1), lambda: api.cover_kv8_read(*mem, pos0=big),
+                     lambda: api.cover_attn_fwd_prefix8(x, *mem, q0=big), lambda: api.cover_debug_attn_prefix8(x, *mem, q0=0, mode=big),
+                     lambda: api.cover_attn_fwd_prefix(x, x, x, q0=big), lambda: api.cover_attn_prefix8_workspace_bytes(1, 2, 2, 4, big)):
+            with pytest.raises(ValueError, match="32 bits"):
+                call()
+    with pytest.raises(ValueError, match="32 bits"):
+        api.cover_kv8_read(*mem, n=2 ** 32 + 1)
+    with pytest.raises(ValueError, match="longer than"):
+        api._sizes_fit(torch.empty(1, device="meta").expand(2 ** 31, 1), "q")
+    api._sizes_fit(torch.empty(1, device="meta").expand(2 ** 31 - 1, 7), "q")
