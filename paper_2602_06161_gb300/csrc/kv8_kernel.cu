@@ -318,8 +318,12 @@ int launch_kv8(const Kv8Args& a, bool write, cudaStream_t stream) {
 int launch_kv8_decode(const Kv8Args& a, cudaStream_t stream) {
   using bf16 = __nv_bfloat16;
   constexpr int kSlots = kThreads / (128 / Wide<bf16>::kN) * kTok;
-  if (a.B > 65535) return -2;
-  return launch_rows(kv8_kernel<bf16, 128, kDecode>, params_of(a, false), (a.n + kSlots - 1) / kSlots, a.Hkv, a.B, stream);
+  // whole memories lie one behind the other: the heads of all sequences are those of one (a grid's depth is 65535 too)
+  Kv8Params p = params_of(a, false);
+  const long long heads = static_cast<long long>(a.B) * a.Hkv;
+  if (heads > 0x7fffffffLL) return -2;
+  p.Hkv = static_cast<int>(heads);
+  return launch_rows(kv8_kernel<bf16, 128, kDecode>, p, (a.n + kSlots - 1) / kSlots, heads, 1, stream);
 }
 
 }  // namespace cover

@@ -244,3 +244,19 @@ def test_columns_that_do_not_turn_are_copied(inter, inverse):
     y, _ = api.cover_rope_fwd(x, None, f, pos0=5, interleaved=inter, mscale=1.5, inverse=inverse)
     assert torch.equal(y[..., 12:].contiguous().view(torch.int32), x[..., 12:].contiguous().view(torch.int32))
     assert not torch.equal(y[..., :12], x[..., :12])
+
+
+@pytest.mark.parametrize("mode", [2, 3, 4])
+def test_more_sequences_than_a_grid_is_deep(mode):
+    """70000 sequences of three positions, also where the memory is decoded first."""
+    B = 70000
+    heads = _mem(1, B, 3)
+    mem, q = tuple(m.view(B, 1, *m.shape[2:]) for m in heads), _r(B, 2, 1, 128, seed=3)
+    ref, ref_lse = _attn(q, mem, 0, q0=1)
+    out, lse = _attn(q, mem, mode, q0=1)
+    v = api.cover_kv8_read(*heads, dtype=torch.float32)[1].abs().amax()
+    assert (out.float() - ref.float()).abs().max() <= 2 * 2.0 ** -7 * v    # each rounds weights and output by 2^-8
+    assert (lse - ref_lse).abs().max() <= 2.0 ** -12
+    for b in (0, 65535, 65536, B - 1):
+        one = tuple(m[b:b + 1].contiguous() for m in mem)
+        _check((out[b:b + 1], lse[b:b + 1]), q[b:b + 1], one, q0=1)
