@@ -593,6 +593,20 @@ __device__ __forceinline__ float self_score(const Params& p, long long row, size
   return kCap ? capped(d0 + d1, p.cap_in, p.cap_log2) : (d0 + d1) * p.scale_log2;
 }
 
+// A row's sum l under a fixed reference m, which may be far from the row's scores: the sum goes to [1, 2), the reference with it
+// (to -inf for a sum of zero: a row or a part without keys), and the accumulator's factor, 2 to a whole number, is returned. So a row's
+// reference is that of its largest weights within the sum's bits when it meets those of other parts and of the masked-input
+// pair, whose values may be of any size.
+__device__ __forceinline__ float follow_sum(float& m, float& l) {
+  if (l == 0.0f) m = -INFINITY;
+  const int e = static_cast<int>(__float_as_uint(l) >> 23);   // (l > 0 is a normal number)
+  if (e == 0 || e == 255) return 1.0f;
+  m += static_cast<float>(e - 127);
+  const float f = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+  l *= f;
+  return f;
+}
+
 // o += w v for 32 columns of a masked-input value.
 __device__ __forceinline__ void add_self(float (&o)[32], float w, const __nv_bfloat16* v) {
   const uint4* vr = reinterpret_cast<const uint4*>(v);
@@ -987,6 +1001,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const float m_use = m == -INFINITY ? 0.0f : m;
     float w[2] = {ml0.x == -INFINITY ? 0.0f : ex2_approx(ml0.x - m_use), ml1.x == -INFINITY ? 0.0f : ex2_approx(ml1.x - m_use)};
     float l = w[0] * ml0.y + w[1] * ml1.y;
+    if (fixed) {
+      const float f = follow_sum(m, l);
+      w[0] *= f, w[1] *= f;
+    }
     const int c0 = 2 * stream;   // the first of two 32-column chunks that this thread finishes
     const float m_all = fmaxf(m, s_self);
     float p_self = 0.0f;
@@ -1346,11 +1364,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     sm.red[tile][half][R] = l_run;
     tile_sync(tile);
     float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
+    if (fixed) w = follow_sum(m, l);
     if (s_self != -INFINITY) {
       const float m_all = fmaxf(m, s_self);
-      w = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
+      const float f = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
       p_self = ex2_approx(s_self - m_all);
-      l = l * w + p_self;
+      l = l * f + p_self;
+      w *= f;
       m = m_all;
     }
     if (s_self != s_self) l = s_self;   // NaN in the masked-input pair

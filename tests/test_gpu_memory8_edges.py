@@ -260,3 +260,34 @@ def test_more_sequences_than_a_grid_is_deep(mode):
     for b in (0, 65535, 65536, B - 1):
         one = tuple(m[b:b + 1].contiguous() for m in mem)
         _check((out[b:b + 1], lse[b:b + 1]), q[b:b + 1], one, q0=1)
+
+
+@pytest.mark.parametrize("mode,parts", [(0, 3), (0, -3), (1, 3), (2, 1), (2, 3), (2, -3), (3, 1), (3, 3)])
+@pytest.mark.parametrize("cap", [30.0, 50.0])
+def test_capped_parts_of_different_values(mode, parts, cap):
+    """Parts of the keys without a key, with values of other sizes than the others', and masked-input values of every size: what a part's
+    reference is changes nothing."""
+    q = _r(1, 4, 20, 128, seed=3)
+    for L, byte in ((5, 23), (5, 119), (300, 23), (300, 119), (700, 119)):
+        mem = _mem(1, 2, L)
+        if L == 5:                            # scores near the cap's opposite
+            api.cover_kv8_write((_r(1, 2, L, 128, seed=9) - 16 * torch.sign(q[:, ::2, :1])).bfloat16(), _r(1, 2, L, 128, seed=8), *mem)
+        mem[3].fill_(byte)
+        if L == 700:
+            mem[3][:, :, :256] = 60           # the first part's: far smaller, with nearly all of the weight
+            api.cover_kv8_write((_r(1, 2, 256, 128, seed=9, scale=0.2) + 4 * torch.sign(q[:, ::2, :1])).bfloat16(), _r(1, 2, 256, 128, seed=8), *mem)
+            mem[3][:, :, :256] = 60
+        kw = dict(q0=0, softcap=cap)
+        if L < 20:
+            qq = q[:, :, :L].contiguous()
+        else:
+            qq = q
+        got = _attn(qq, mem, mode, nsplit=parts, **kw)
+        _check(got, qq, mem, **kw)
+        n = min(L, 4)
+        for e in (-90.0, 0.0, 60.0, 90.0):
+            for shift in (0.0, 16.0, -16.0):    # the masked-input keys: any, near the cap, near its opposite
+                km = (_r(1, 2, n, 128, seed=11) + shift * torch.sign(qq[:, ::2, :n])).bfloat16()
+                seeds = (km, (_r(1, 2, n, 128, seed=12) * 2.0 ** e).bfloat16(), torch.arange(n, device="cuda", dtype=torch.int32)[None].contiguous())
+                got = _attn(qq, mem, mode, seeds, nsplit=parts, **kw)
+                _check(got, qq, mem, seeds, **kw)
