@@ -92,3 +92,22 @@ def test_a_result_is_kept_until_the_current_stream_is_done_with_it():
         assert not (_span(other)[0] < hi and lo < _span(other)[1])
     torch.cuda.synchronize()
     assert torch.equal(kept, api.cover_rope_fwd(q, None, f)[0])
+
+
+def test_a_captured_call_on_another_stream():
+    """A call on a stream that a capture has forked to makes its tensors in the graph's memory."""
+    call = _calls()["attn8"]
+    ref = call()
+    torch.cuda.synchronize()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        side.wait_stream(torch.cuda.current_stream())
+        out, lse = call(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        kept = out.clone(), lse.clone()
+    others = [torch.full_like(out, 7.0) for _ in range(50)]      # of the allocator's other memory
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    assert api.cover_device_status() == 0
+    assert torch.equal(kept[0], ref[0]) and torch.equal(kept[1], ref[1]) and all((o == 7.0).all() for o in others)
