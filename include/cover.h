@@ -297,7 +297,9 @@ int cover_rope_fwd(const void* q, const void* k, void* q_out, void* k_out, const
  *   dimension dense. Slot s goes to position pos0 + s, or to pos[b, s] (int32 [B, n]) where pos is not
  *   NULL: a listed position outside [0, L) is left out, and where a position is listed again
  *   the lowest slot is taken (as in cover_attn_fwd). Every other row of the memory is left as it
- *   was. With pos = seed_idx this overrides the memory at the seeds with their cached states.
+ *   was. With pos = seed_idx this overrides the memory at the seeds with their cached states. A listed
+ *   write compares every slot with the lower ones: 4 x 8 heads, 512 rows of 128 bf16 take 8 us (5 at consecutive
+ *   positions), 8191 rows 99 (36).
  * cover_kv8_read reads rows back into k, v [B, Hkv, n, D] (dense, bf16 or fp32): row s from
  *   position pos0 + s or pos[b, s]; a listed position outside [0, L) reads as zeros.
  *
@@ -333,8 +335,11 @@ int cover_kv8_read(const void* k8, const void* v8, const uint8_t* k_exp, const u
  * out (not in lse).
  * Scores and sums are fp32: they hold where the largest elements of a query row and a key row multiply to less than 2^120 and
  * the values seen are at most 2^100, and 2^119 / Lk, in magnitude; beyond, a row may get infinities or NaN or lose small weights.
+ * Value rows that are below 2^-80 throughout may lose bits, or count as zeros, beside rows of zeros. lse carries an error of
+ * up to 2^-17 where the value rows seen are all zeros or their scales are far from 1.
  * workspace: cover_attn_prefix8_workspace_bytes(B, Hq, Hkv, Lq, Lk) bytes, 16-byte aligned, no initialisation
- * needed (NULL if that is 0). It is scratch of the call alone: calls that share one must not
+ * needed (NULL if that is 0): parts of the keys' results, and for windows that fill several tiles of 128 rows the whole
+ * memory in bf16 (2048 rows, 32 / 8 heads over 131072 keys: 673 MB, beside a memory of 271). It is scratch of the call alone: calls that share one must not
  * run concurrently on the GPU.
  * The inputs must not alias out, lse or workspace. Errors as cover_attn_fwd_prefix, plus
  * COVER_ERR_INVALID_ARG for NULL k_exp or v_exp, a missing workspace, and a softcap that is

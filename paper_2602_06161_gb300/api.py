@@ -485,7 +485,8 @@ def _rope_aliases(pairs, rest):
 def cover_rope_fwd(q, k, inv_freq, *, pos=None, pos0: int = 0, interleaved: bool = False, mscale: float = 1.0,
                    inverse: bool = False, out_q=None, out_k=None, stream=None):
     """Rotary positions of queries and keys. Returns (q, k) turned, dense unless out_q / out_k are given, which may be
-    q / k themselves (in place) and share no byte with any other of the tensors.
+    q / k themselves (in place) and share no byte with any other of the tensors (which is looked at in Python: such a
+    call takes 37 us of host time, one that makes its results 5).
 
     q [B, Hq, L, D], k [B, Hkv, L, D] (or None): bf16 or fp32, dense in the last dimension only (a projection's
     [B, L, H, D] transposed will do). inv_freq: fp64 [R / 2], radians per position (rope_frequencies); the first
@@ -532,8 +533,8 @@ def rope_frequencies(R: int, base: float = 10000.0, *, scaling: str = "none", fa
 
     scaling: "none"; "linear": every frequency divided by the factor; "ntk": the base raised so that the slowest
     frequency is divided by it and the fastest kept; "yarn": pairs that turn at most ``slow`` times in the trained
-    context are divided, those that turn ``fast`` times or more are kept, with a ramp between, and mscale =
-    0.1 ln(factor) + 1.
+    context are divided, those that turn ``fast`` times or more are kept, with a ramp between that is linear in the number of
+    turns (code that ramps by the pair's index gives other frequencies: pass its own), and mscale = 0.1 ln(factor) + 1.
     """
     if R < 2 or R % 2:
         raise ValueError("R must be even and at least 2")

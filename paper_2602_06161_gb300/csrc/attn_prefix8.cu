@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // A memory that many Q tiles read is decoded once, into the workspace (a row whose K or V is NaN has a NaN key and a zero
 // value there), and a CTA takes two Q tiles, one a stream, that read each KV tile together. Two threads of different
 // warpgroups share a row, 64 columns each, in two chunks of 32. 2048 rows over 8192 keys, 32 / 8 heads: 222 us, capped
-// at 30 261 (8 us of them decode the memory); 1216 rows, which fill the GPU's 152 SMs once, 116 us, 1400 TFLOP/s: a KV tile takes
+// at 30 252 (8 us of them decode the memory); 1216 rows, which fill the GPU's 152 SMs once, 116 us, 1400 TFLOP/s: a KV tile takes
 // 1.6 us, the products 1.1 of them; each Q tile's chain (S, maxima, exponentials, P V) is longer than the other's products. With a
 // thread a row and its 128 columns unrolled it was 235 and 333 us: see finish_scores. One CTA an SM that walks over even shares of all
 // tiles, units cut where a share ends, was tried: 1216 rows 130 us (a KV tile takes 0.1 us longer in such a loop), 2048 232 and 263.
@@ -1419,7 +1419,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 // most 9 significant bits is the sum of three e5m2 numbers (e5m2 is the upper byte of fp16: the parts
 // are truncations of what the parts before leave, each exact). The parts are columns of their own, 3 kN in all, whose
 // products add up in fp32.
-//   Q: bf16 has 8 bits, so the parts are exact; a row is scaled by a power of two to a maximum of 2^14 .. 2^15 first.
+//   Q: a row is scaled by a power of two to a maximum of 2^14 .. 2^15 first. bf16 has 8 bits, so the parts are exact down to 2^-23
+//      of the row's largest element; what is smaller is cut at e5m2's last bit, 2^-16, below 2^-30 of the largest.
 //   P: the V rows' scales belong to the contracted index, so they are taken into the weights: with e_j = x_j - 127 of
 //      the V row, P'_j = 2^(s_j + e_j - m), m the row's reference for s_j + e_j, and the sum has 2^(s_j - m) of its
 //      own. P' is rounded to 9 bits (off by at most 2^-9 of it; bf16 is by 2^-8) and scaled by 2^12: what is
