@@ -559,16 +559,23 @@ __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const
   return (r[0] + r[1]) + (r[2] + r[3]);
 }
 
-// Whether some of n bytes lies outside those of lo .. hi (four copies each); the threads' parts of it, tid of kAll.
+// Whether V rows from .. to - 1 hold an exponent byte outside p.v_lo .. p.v_hi (bytes above 246, rows of NaN, are not meant: their values are
+// taken as zeros); the part of it that thread tid of kAll looks at. exps: of row 0.
 template <int kAll>
-__device__ __forceinline__ bool bytes_outside(const uint8_t* bytes, int n, int tid, uint32_t lo, uint32_t hi) {
-  const auto one = [&](int i) { return __ldg(bytes + i) < (lo & 255u) || __ldg(bytes + i) > (hi & 255u); };
+__device__ __forceinline__ bool bytes_outside(const Params& p, const uint8_t* exps, int from, int to, int tid) {
+  constexpr uint32_t kNumbers = 0x01010101u * kExpMax;
+  const uint8_t* bytes = exps + from;
+  const int n = max(to - from, 0);
+  const auto one = [&](int i) {
+    const uint32_t x = __ldg(bytes + i);
+    return x < (p.v_lo & 255u) || (x > (p.v_hi & 255u) && x <= kExpMax);
+  };
+  const auto four = [&](uint32_t x) { return __vcmpltu4(x, p.v_lo) | (__vcmpgtu4(x, p.v_hi) & __vcmpleu4(x, kNumbers)); };
   const int head = min(n, static_cast<int>(-reinterpret_cast<uintptr_t>(bytes) & 15)), wide = (n - head) / 16;
   uint32_t out = tid < head && one(tid) ? 1 : 0;
   for (int i = tid; i < wide; i += kAll) {
     const uint4 w = __ldg(reinterpret_cast<const uint4*>(bytes + head) + i);
-    out |= __vcmpltu4(w.x, lo) | __vcmpgtu4(w.x, hi) | __vcmpltu4(w.y, lo) | __vcmpgtu4(w.y, hi);
-    out |= __vcmpltu4(w.z, lo) | __vcmpgtu4(w.z, hi) | __vcmpltu4(w.w, lo) | __vcmpgtu4(w.w, hi);
+    out |= four(w.x) | four(w.y) | four(w.z) | four(w.w);
   }
   const int last = head + 16 * wide + tid;
   return out != 0 || (last < n && one(last));
@@ -904,11 +911,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool warp_live = __any_sync(0xffffffffu, valid);
     const uint32_t s_addr = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16) + stream * kBN;
     const uint32_t o_addr = s_addr + 2 * kBN;
-    // a reference of all rows where the part's V rows allow it
+    // a reference of all rows where the part's V rows, those that some row sees, allow it
     bool fixed = kCap && p.cap_ref != -INFINITY;
     if (fixed) {
-      if (bytes_outside<2 * kBM>(p.v_exp + mem0 + static_cast<size_t>(j0) * kBN, min(p.Lk - j0 * kBN, nt * kBN), tid, p.v_lo, p.v_hi))
-        ctl.wide = 1;
+      if (bytes_outside<2 * kBM>(p, p.v_exp + mem0, max(lo_key, j0 * kBN), min(hi_key, (j0 + nt) * kBN), tid)) ctl.wide = 1;
       softmax_sync();
       fixed = ctl.wide == 0;
     }
@@ -1281,11 +1287,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = quad + tile * kBN + half * kHalf;
     const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
-    // a reference of all rows where the part's V rows allow it
+    // a reference of all rows where the part's V rows, those that some row sees, allow it
     bool fixed = kCap && p.cap_ref != -INFINITY;
     if (fixed) {
-      const size_t first = (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk + static_cast<size_t>(j0) * kBN;
-      if (bytes_outside<4 * kBM>(p.v_exp + first, min(p.Lk - j0 * kBN, nt * kBN), tid, p.v_lo, p.v_hi)) ctl.wide = 1;
+      const uint8_t* exps = p.v_exp + (static_cast<size_t>(b) * p.Hkv + hkv) * p.Lk;
+      if (bytes_outside<4 * kBM>(p, exps, max(lo_key, j0 * kBN), min(hi_key, (j0 + nt) * kBN), tid)) ctl.wide = 1;
       pairs_sync();
       fixed = ctl.wide == 0;
     }

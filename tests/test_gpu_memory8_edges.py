@@ -291,3 +291,29 @@ def test_capped_parts_of_different_values(mode, parts, cap):
                 seeds = (km, (_r(1, 2, n, 128, seed=12) * 2.0 ** e).bfloat16(), torch.arange(n, device="cuda", dtype=torch.int32)[None].contiguous())
                 got = _attn(qq, mem, mode, seeds, nsplit=parts, **kw)
                 _check(got, qq, mem, seeds, **kw)
+
+
+@pytest.mark.parametrize("mode,parts", [(0, 1), (0, 3), (1, 1), (2, 1), (2, 2), (2, -2), (3, 1), (3, 2)])
+@pytest.mark.parametrize("cap", [30.0, 50.0])
+def test_what_is_not_seen_under_a_cap(mode, parts, cap):
+    """Rows behind, before and between the keys that a call's rows see change no bit, whatever their bytes and codes; nor do rows of NaN
+    that other rows see."""
+    Lq, L = 150, 600
+    mem, q = _mem(1, 2, L), _r(1, 4, Lq, 128, seed=3)
+    lo, hi = _i32([[70] * Lq]), _i32([[300] * 75 + [530] * 75])
+    call = lambda m: _attn(q, m, mode, q0=0, nsplit=parts, key_lo=lo, key_hi=hi, softcap=cap)  # noqa: E731
+    ref = call(mem)
+    for code, byte in ((0x7f, 119), (0x38, 255), (0x7e, 246), (0x7e, 250), (0x01, 0), (0x7e, 20)):
+        m = tuple(x.clone() for x in mem)
+        for i in range(2):
+            for rows in (slice(0, 70), slice(530, L)):
+                m[i].view(torch.uint8)[:, :, rows] = code
+                m[2 + i][:, :, rows] = byte
+        out = call(m)
+        assert torch.equal(out[0], ref[0]) and torch.equal(out[1], ref[1])
+    for i in range(2):
+        m = tuple(x.clone() for x in mem)
+        m[2 + i][0, 1, 400] = 255
+        out, lse = call(m)
+        assert torch.equal(out[:, :, :75], ref[0][:, :, :75]) and torch.equal(lse[:, :, :75], ref[1][:, :, :75])
+        assert out[:, 2:, 75:].isnan().all() and torch.equal(out[:, :2], ref[0][:, :2])
