@@ -445,8 +445,8 @@ __device__ __forceinline__ int2 share_of(const int* seq_lo, const int* seq_hi, i
   return make_int2(all + __popc(empty & ((1u << lane) - 1u)), lane < B ? 1 : 0);
 }
 
-// What a row does not see of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1), keys whose V
-// row is NaN (bit c of `nan` for the chunk's column c); whether anything of it holds for some row of the warp.
+// What a row does not see of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1); whether
+// anything of it holds for some row of the warp.
 struct Unseen {
   int lo, hi, own;
   bool any;
@@ -456,15 +456,10 @@ struct Unseen {
 // not unrolled: with 128 columns at once 8 % of the instruction fetches missed the SM's cache, the GPC's was at 52 % of
 // its rate, and a KV tile took 4950 cycles on 128 SMs where it took 2780 on 64.
 template <bool kCap>
-__device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, const Unseen& u, uint32_t nan, int c0) {
+__device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, const Unseen& u, int c0) {
   if (kCap) {
 #pragma unroll
     for (int c = 0; c < 32; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
-  }
-  if (nan != 0) {
-#pragma unroll
-    for (int c = 0; c < 32; ++c)
-      if ((nan >> c) & 1u) s[c] = __uint_as_float(0x7fc00000u);
   }
   if (u.any) {
     const int lo = u.lo - c0, hi = u.hi - c0, own = u.own - c0;
@@ -486,12 +481,12 @@ __device__ __forceinline__ float max32(const float (&s)[32]) {
 }
 
 // The largest of 32 columns' scores, neither scaled nor capped yet.
-__device__ __forceinline__ float chunk_max(uint32_t addr, const Params& p, const Unseen& u, uint32_t nan, int c0) {
+__device__ __forceinline__ float chunk_max(uint32_t addr, const Params& p, const Unseen& u, int c0) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
   float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
-  finish_scores<false>(s, p, u, nan, c0);
+  finish_scores<false>(s, p, u, c0);
   return max32(s);
 }
 
@@ -504,15 +499,15 @@ __device__ __forceinline__ float reference_of(float top, const Params& p) {
 // P = 2^(score - m) of 32 columns to tensor memory, in bf16; returns their sum. fixed: capped scores whose reference is
 // fixed; those of a chunk that are all small and all seen take the polynomial.
 template <bool kCap>
-__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, uint32_t nan, int c0,
-                                           float m, bool fixed, bool valid) {
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m,
+                                           bool fixed, bool valid) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
   float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
   bool small = false;
   if (kCap) {
-    if (fixed && nan == 0 && !u.any) {
+    if (fixed && !u.any) {
       float hi[2] = {};
 #pragma unroll
       for (int c = 0; c < 32; c += 4) {
@@ -540,7 +535,7 @@ __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const
       acc2[c & 1] = f2_add(acc2[c & 1], f2_pack(e0, e1));
     }
   } else {
-    finish_scores<kCap>(s, p, u, nan, c0);
+    finish_scores<kCap>(s, p, u, c0);
     const float scale = kCap ? 1.0f : p.scale_log2;
     const uint64_t scale2 = f2_pack(scale, scale);
 #pragma unroll
@@ -959,7 +954,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!fixed) {
         float m_tile = -INFINITY;
 #pragma unroll 1
-        for (int c = 0; c < kBN; c += 32) m_tile = fmaxf(m_tile, chunk_max(s_addr + c, p, u, 0, c));
+        for (int c = 0; c < kBN; c += 32) m_tile = fmaxf(m_tile, chunk_max(s_addr + c, p, u, c));
         m_tile = reference_of<kCap>(m_tile, p);
         if (m_tile > m_run + kRescaleThreshold) {
           alpha = (m_run == -INFINITY) ? 0.0f : ex2_approx(m_run - m_tile);
@@ -971,7 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       l_run *= alpha;
 #pragma unroll 1
       for (int c = 0; c < kBN; c += 32)
-        l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, 0, c, m_use, fixed, valid);
+        l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, c, m_use, fixed, valid);
       if (i > 0 && __any_sync(0xffffffffu, rescaled)) {
         // O holds the stream's earlier products (complete: the commit of this S came after them)
 #pragma unroll 1
@@ -1310,7 +1305,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m_half = -INFINITY;
       if (ok && some && !fixed) {
 #pragma unroll 1
-        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, 0, c));
+        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, c));
         m_half = reference_of<kCap>(m_half, p);
       }
       if (fixed && !ok) break;
@@ -1348,7 +1343,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
 #pragma unroll 1
         for (int c = 0; c < kHalf; c += 32)
-          l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, 0, c, m_use, fixed, valid);
+          l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, c, m_use, fixed, valid);
       } else if (warp_live) {
         const uint32_t zeros[16] = {};
         tmem_st16(s_addr, zeros);
