@@ -120,10 +120,14 @@ def _attn(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, seed_id
         out = make(q.shape, q.dtype)
     else:
         _need(out, "out", dtype, 4)
+        if out.shape != q.shape:
+            raise ValueError("out must match q")
     if lse is None and want_lse:
         lse = make((B, Hq, L), torch.float32)
     elif lse is not None:
         _need(lse, "lse", torch.float32, 3)
+        if tuple(lse.shape) != (B, Hq, L):
+            raise ValueError("lse must be [B, Hq, L]")
     lib = _lib.load()
     code = getattr(lib, fn_name)(
         _ptr(q), _ptr(k_cached), _ptr(v_cached),
@@ -181,10 +185,14 @@ def _attn_prefix(fn_name, dtype, q, k_cached, v_cached, k_seedmask, v_seedmask, 
         out = make(q.shape, q.dtype)
     else:
         _need(out, "out", dtype, 4)
+        if out.shape != q.shape:
+            raise ValueError("out must match q")
     if lse is None and want_lse:
         lse = make((B, Hq, Lq), torch.float32)
     elif lse is not None:
         _need(lse, "lse", torch.float32, 3)
+        if tuple(lse.shape) != (B, Hq, Lq):
+            raise ValueError("lse must be [B, Hq, Lq]")
     code = getattr(_lib.load(), fn_name)(
         _ptr(q), _ptr(k_cached), _ptr(v_cached),
         _ptr(k_seedmask) if n_seeds else None, _ptr(v_seedmask) if n_seeds else None,

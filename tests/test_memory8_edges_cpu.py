@@ -86,3 +86,29 @@ def test_numbers_above_32_bits_are_refused(monkeypatch):
     with pytest.raises(ValueError, match="longer than"):
         api._sizes_fit(torch.empty(1, device="meta").expand(2 ** 31, 1), "q")
     api._sizes_fit(torch.empty(1, device="meta").expand(2 ** 31 - 1, 7), "q")
+
+
+def test_outputs_of_another_shape_are_refused(monkeypatch):
+    """By every attention call, before anything is launched: the kernels write what q's shape says."""
+    class Lib:
+        def __getattr__(self, name):
+            raise AssertionError("launched")
+
+    class Hands:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(api._lib, "load", lambda: Lib())
+    monkeypatch.setattr(api, "_launch", lambda *a: Lib().launch)
+    monkeypatch.setattr(api, "_nat", Hands())
+    monkeypatch.setattr(api, "_need", lambda *a: None)
+    monkeypatch.setattr(api, "cover_attn_prefix8_workspace_bytes", lambda *a: 0)
+    q, lse = torch.zeros(1, 2, 4, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 4)
+    mem = api.kv8_memory(1, 2, 4, device="cpu")
+    for call in (lambda **kw: api.cover_attn_fwd(q, q, q, **kw), lambda **kw: api.cover_attn_fwd_prefix(q, q, q, q0=0, **kw),
+                 lambda **kw: api.cover_attn_fwd_prefix8(q, *mem, q0=0, **kw)):
+        for kw in (dict(out=q[:, :, :3]), dict(out=q[:, :1]), dict(lse=lse[:, :, :3]), dict(out=q, lse=lse[:, :1])):
+            with pytest.raises(ValueError, match="must"):
+                call(**kw)
+        with pytest.raises(AssertionError, match="launched"):
+            call(out=q, lse=lse)
