@@ -496,7 +496,8 @@ __device__ __forceinline__ float reference_of(float top, const Params& p) {
   return !kCap ? top * p.scale_log2 : top == -INFINITY ? top : capped(top, p.cap_in, p.cap_log2);
 }
 
-// P = 2^(score - m) of 32 columns to tensor memory, in bf16; returns their sum. fixed: capped scores whose reference is
+// P = 2^(score - m) of 32 columns to tensor memory, in bf16: V's operands are, so P's have to be. A weight is off by at most 2^-8 of
+// itself, as the output is of itself; TF32 operands would be exacter at half the rate. Returns the sum of the unrounded weights. fixed: capped scores whose reference is
 // fixed; those of a chunk that are all small and all seen take the polynomial.
 template <bool kCap>
 __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m,
