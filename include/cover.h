@@ -355,6 +355,92 @@ int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8,
                            void* out, float* lse, void* workspace, void* stream);
 
 /*
+ * A key/value memory in pages, shared by the sequences of a server (the prefix cache of Section 6.6 for sequences that come and
+ * go), per layer:
+ *   k_pages, v_pages [n_pages, Hkv, page, D] bf16
+ *   table            [B, M] int32: position t of sequence b is row t % page of the page table[b, t / page]; an entry
+ *                    outside [0, n_pages) is a page that the sequence does not have
+ * page is 16, 32, 64, 128 or 256, and M * page is below 2^31.
+ *
+ * cover_paged_append writes n rows of every sequence and rotates them on the way: row s of sequence b goes to position
+ * start[b] + s where s < count[b] (count NULL: all n; the other rows are padding), or to pos[b, s] where pos is not NULL (start
+ * and count are NULL then): of rows that name one position the lowest is taken (as in cover_kv8_write). A position below 0 or
+ * without a page is left out; every other row of the pages is left as it was. Sequences that share a page must not write the
+ * same of its rows in one call (one of them stays, which is not said).
+ *   k, v [B, Hkv, n, D], q [B, Hq, n, D] (NULL with Hq = 0): elements of elem_bytes (2: bf16, 4: fp32); strides: HOST int64
+ *     [9], strides in elements of (B, H, n) of k, v, q (the last dimension is dense)
+ *   q_out [B, Hq, n, D], k_out [B, Hkv, n, D] (NULL: not wanted): dense, of the same type; all n rows of q and k turned,
+ *     k_out where the program needs the rows besides (the seeds' masked-input rows)
+ *   inv_freq [R / 2], interleaved, mscale: as in cover_rope_fwd (R = 0: nothing turns); k and q turn by rope_pos[b, s] (int32
+ *     [B, n]), or by the row's position in the memory where it is NULL. Rows are turned in fp32 and rounded once.
+ * k, v and q must overlap neither the pages nor the outputs. n = 0 is a no-op.
+ * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hkv, D, M or n_pages < 1, Hq or n < 0, R odd, negative or above
+ * D, elem_bytes not 2 or 4, neither or both of start and pos, count with pos, a pointer that is not aligned to its elements (the pages:
+ * to 16 bytes); COVER_ERR_UNSUPPORTED for D other than 64 and 128, another page, M * page >= 2^31; COVER_ERR_CUDA for a
+ * launch failure. Rows that are all 16-byte aligned (and an R that splits into 16-byte vectors) run on 16-byte accesses.
+ */
+int cover_paged_append(const void* k, const void* v, const void* q, void* q_out, void* k_out, const int64_t* strides,
+                       const int32_t* table, int n_pages, int M, int page,
+                       const int32_t* start, const int32_t* count, const int32_t* pos, const int32_t* rope_pos,
+                       int n, int B, int Hq, int Hkv, int D, int R, const double* inv_freq, int interleaved,
+                       float mscale, int elem_bytes, void* k_pages, void* v_pages, void* stream);
+
+/*
+ * cover_attn_fwd_prefix over a memory in pages (D = 128): bf16 queries q [B, Hq, Lq, D], bf16 out, fp32 lse [B, Hq, Lq]
+ * (NULL = skip), the seeds' masked-input pairs k_seedmask, v_seedmask [B, Hkv, n_seeds, D] in bf16.
+ *   lens [B] int32: keys of each sequence (held to 0 .. M * page). A position without a page holds no key.
+ *   q0 [B] int32: position of each sequence's first query row; row r is at q0[b] + r (any value; NULL without seeds). It says which
+ *     row is a seed's; what a row sees is said by the lengths and the ranges alone.
+ *   key_lo, key_hi [B, Lq] int32 or NULL (0, lens[b]): row r of sequence b sees the keys key_lo <= j < key_hi only (any
+ *     values): positions up to its own, blocks, windows, documents. A row that sees no key gets out = 0, lse = -inf.
+ *     A seed row's own pair is seen where its position is.
+ *   softcap 0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c) (c above 2^60 counts as
+ *     2^60, c below 2^-30 as 2^-30).
+ * What a row does not see does not reach it, NaN included: rows of a page behind a sequence's length may hold anything.
+ * A row that sees an element of V that is not finite has no finite number in that column at least.
+ * workspace: cover_attn_paged_workspace_bytes bytes, 16-byte aligned, no initialisation needed (NULL if that is 0): scratch of the
+ * call alone; calls that share one must not run concurrently on the GPU. The inputs must not alias out, lse or workspace.
+ * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hq, Hkv, Lq, M or n_pages < 1, Hq % Hkv != 0, n_seeds < 0, a
+ * softcap that is negative or not finite, a misaligned pointer, a missing workspace; COVER_ERR_UNSUPPORTED for D != 128, another
+ * page, M * page >= 2^31, B Hq Lq >= 2^31 - 256; COVER_ERR_CUDA for a launch failure; COVER_ERR_DEVICE_TIMEOUT via
+ * cover_device_status.
+ */
+size_t cover_attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page);
+int cover_attn_fwd_paged(const void* q, const void* k_pages, const void* v_pages,
+                         const int32_t* table, int n_pages, int M, int page, const int32_t* lens,
+                         const void* k_seedmask, const void* v_seedmask, const int32_t* seed_idx, int n_seeds,
+                         const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
+                         const int32_t* key_lo, const int32_t* key_hi, float softcap,
+                         void* out, float* lse, void* workspace, void* stream);
+
+/*
+ * Log probabilities of given tokens (softmax at temperature 1 over rows of V logits), beside cover_score_fwd's u = -log p
+ * for programs that score, compare or learn from answers: with the row's entropy, its logsumexp and its best alternatives.
+ *   logits [N, V], elements of elem_bytes (2: bf16, 4: fp32)
+ *   tok [N] int32 or NULL (then logp is not written): logp[i] = log p(tok[i]); a token outside [0, V) has logp = 0 (a row
+ *     to be left out of sums)
+ *   entropy, lse [N] fp32: H = -sum p ln p, lse = ln sum e^logit
+ *   topk 0 .. 64: top_idx [N, topk] int32, top_logp [N, topk] fp32: the tokens of the largest logits (descending; equal
+ *     ones by ascending index) and their log probabilities; -1 and -inf where V < topk. (NULL for topk = 0)
+ * A logit of -inf is a token of probability 0. A row with NaN or +inf has NaN in logp (of a token in [0, V)), entropy and lse,
+ * and unspecified alternatives (indexes in [-1, V)); a row of -inf alone has lse = -inf and NaN in logp, entropy and top_logp.
+ * cover_logprob_bwd is the gradient: with p_j = e^(logit_j - lse),
+ *   d_logits_j = p_j (d_lse - d_logp - sum_k d_top_k - d_entropy (ln p_j + entropy)) + [j = tok] d_logp
+ *                + sum_k [j = top_idx_k] d_top_k,
+ * rounded once to the logits' type. d_logp (with tok), d_entropy (with entropy), d_lse [N] and d_top [N, topk] (with
+ * top_idx) are fp32 or NULL (0); a token or alternative outside [0, V) gets no gradient; a token listed again gets each
+ * share. entropy and lse are the forward call's. d_logits may be logits itself, or must not overlap it.
+ * N = 0 is a no-op. Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, N < 0, V < 1, topk < 0, elem_bytes not 2 or 4,
+ * a pointer that is not aligned to its elements; COVER_ERR_UNSUPPORTED for topk > 64; COVER_ERR_CUDA for a launch failure.
+ */
+int cover_logprob_fwd(const void* logits, int N, int V, int elem_bytes, const int32_t* tok, int topk,
+                      float* logp, float* entropy, float* lse, int32_t* top_idx, float* top_logp, void* stream);
+int cover_logprob_bwd(const void* logits, int N, int V, int elem_bytes, const float* lse,
+                      const int32_t* tok, const float* d_logp, const float* entropy, const float* d_entropy,
+                      const float* d_lse, const int32_t* top_idx, const float* d_top, int topk,
+                      void* d_logits, void* stream);
+
+/*
  * One decoding step's decisions, fused behind the scoring pass
  * (Section 5.2 "Threshold drafting" and the Keep / Replace / ReMask revision
  * rule, Section 3 state update, Section 5.3 stability-aware seed score,

@@ -22,7 +22,8 @@ _native = None
 _BOUND = ("cover_attn_fwd", "cover_attn_fwd_f32", "cover_attn_fwd_prefix", "cover_attn_fwd_prefix_f32",
           "cover_score_fwd", "cover_score_decide_fwd", "cover_attn_mass_fwd", "cover_seed_kv_gather",
           "cover_seed_kv_override", "cover_rope_fwd", "cover_kv8_write", "cover_kv8_read",
-          "cover_attn_prefix8_workspace_bytes", "cover_attn_fwd_prefix8")
+          "cover_attn_prefix8_workspace_bytes", "cover_attn_fwd_prefix8", "cover_paged_append",
+          "cover_attn_paged_workspace_bytes", "cover_attn_fwd_paged", "cover_logprob_fwd", "cover_logprob_bwd")
 
 # name -> (restype, argtypes)
 _SIGNATURES = {
@@ -43,6 +44,13 @@ _SIGNATURES = {
     "cover_attn_prefix8_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I, _I]),
     "cover_attn_fwd_prefix8": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P,
                                     ctypes.c_float, _P, _P, _P, _P]),
+    "cover_paged_append": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _I,
+                                ctypes.c_float, _I, _P, _P, _P]),
+    "cover_attn_paged_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I, _I, _I]),
+    "cover_attn_fwd_paged": (_I, [_P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _I, _I, _I, _I, _I, _P, _P,
+                                  ctypes.c_float, _P, _P, _P, _P]),
+    "cover_logprob_fwd": (_I, [_P, _I, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P]),
+    "cover_logprob_bwd": (_I, [_P, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P]),
     "cover_decide_workspace_bytes": (ctypes.c_size_t, [_I, _I]),
     "cover_score_decide_fwd": (_I, [_P, _I, _I, _I, _P, _P, _P, ctypes.c_float, _I, _I, _I, _I, _I, _I, _I,
                                     _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
@@ -101,7 +109,7 @@ class _Declines:
     def attn(*args):
         return None
 
-    score = decide = mass = kv = rope = kv8_write = kv8_read = attn8 = attn
+    score = decide = mass = kv = rope = kv8_write = kv8_read = attn8 = paged_append = attn_paged = logprob = logprob_grad = attn
 
 
 def native():

@@ -720,6 +720,240 @@ def cover_attn_fwd_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmask=
     return out, lse
 
 
+def paged_memory(n_pages: int, Hkv: int, page: int = 64, D: int = 128, device=None):
+    """A key/value memory in pages, of zeros: (k_pages, v_pages), bf16 [n_pages, Hkv, page, D]."""
+    k, v = (torch.zeros((n_pages, Hkv, page, D), dtype=torch.bfloat16, device=device or "cuda") for _ in range(2))
+    return k, v
+
+
+def _pages_need(k_pages, v_pages, table):
+    _need(k_pages, "k_pages", torch.bfloat16, 4)
+    _need(v_pages, "v_pages", torch.bfloat16, 4)
+    _need(table, "table", torch.int32, 2)
+    if v_pages.shape != k_pages.shape:
+        raise ValueError("v_pages must match k_pages [n_pages, Hkv, page, D]")
+    _same_device(k_pages.device, v_pages=v_pages, table=table)
+
+
+def _ints_need(shape, device, **tensors):
+    for name, t in tensors.items():
+        if t is not None:
+            _need(t, name, torch.int32, len(shape))
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} must have the shape {shape}")
+    _same_device(device, **tensors)
+
+
+def cover_paged_append(k, v, k_pages, v_pages, table, *, start=None, count=None, pos=None, rope_pos=None, q=None, inv_freq=None,
+                       interleaved: bool = False, mscale: float = 1.0, want_k: bool = False, stream=None):
+    """Write new rows k, v [B, Hkv, n, D] (bf16 or fp32, dense in the last dimension only) into the pages, in place, k turned
+    to its positions on the way. Returns (q, k): q [B, Hq, n, D] turned by the same positions (None without q) and, with
+    ``want_k``, k turned (else None), dense.
+
+    Row s of sequence b goes to position start[b] + s where s < count[b] (int32 [B]; all rows where count is None), or to pos[b, s]
+    (int32 [B, n]; of rows that name one position the lowest is taken). table: int32 [B, M], the sequences' pages; a position without
+    one is left out. inv_freq: fp64 [R / 2] (rope_frequencies; None: nothing turns), with ``interleaved`` and ``mscale`` as in
+    cover_rope_fwd. rope_pos: int32 [B, n], positions to turn by where they are not those in the memory.
+    """
+    if stream is None and type(mscale) is float:
+        r = (_nat or _native()).paged_append(k, v, k_pages, v_pages, table, start, count, pos, rope_pos, q, inv_freq, interleaved,
+                                             mscale, want_k)
+        if r is not None:
+            return _done("cover_paged_append", r)
+    _pages_need(k_pages, v_pages, table)
+    n_pages, Hkv, page, D = k_pages.shape
+    dev = k_pages.device
+    _rows_need(k, "k", _ROWS, dev)
+    _rows_need(v, "v", (k.dtype,), dev)
+    B, n = k.shape[0], k.shape[2]
+    if tuple(k.shape) != (B, Hkv, n, D) or v.shape != k.shape:
+        raise ValueError("k and v must be [B, Hkv, n, D] matching the pages")
+    if q is not None:
+        _rows_need(q, "q", (k.dtype,), dev)
+        if q.shape[0] != B or tuple(q.shape[2:]) != (n, D):
+            raise ValueError("q must be [B, Hq, n, D] matching k")
+    if table.shape[0] != B:
+        raise ValueError("table must be [B, M]")
+    if (start is None) == (pos is None) or (count is not None and pos is not None):
+        raise ValueError("one of start (with or without count) and pos must be given")
+    _ints_need((B,), dev, start=start, count=count)
+    _ints_need((B, n), dev, pos=pos, rope_pos=rope_pos)
+    R = 0
+    if inv_freq is not None:
+        _need(inv_freq, "inv_freq", torch.float64, 1)
+        _same_device(dev, inv_freq=inv_freq)
+        R = 2 * inv_freq.shape[0]
+        if R > D:
+            raise ValueError("inv_freq must have at most D / 2 entries")
+    make = _maker(stream, dev)
+    q_out = None if q is None else make(q.shape, q.dtype)
+    k_out = make(k.shape, k.dtype) if want_k else None
+    has_q = q is not None and q.shape[1] > 0
+    st = _strides(k, v, q if has_q else k)
+    _launch("cover_paged_append", dev, stream,
+            (_ptr(k), _ptr(v), _ptr(q) if has_q else None, _ptr(q_out) if has_q else None, _ptr(k_out), ctypes.addressof(st),
+             _ptr(table), n_pages, table.shape[1], page, _ptr(start), _ptr(count), _ptr(pos), _ptr(rope_pos), n, B,
+             q.shape[1] if has_q else 0, Hkv, D, R, _ptr(inv_freq) if R else None, 1 if interleaved else 0, float(mscale), k.element_size(),
+             _ptr(k_pages), _ptr(v_pages)))
+    return q_out, k_out
+
+
+def cover_attn_paged_workspace_bytes(B: int, Hq: int, Hkv: int, Lq: int, M: int, page: int) -> int:
+    sizes = [_int32(name, x) for name, x in (("B", B), ("Hq", Hq), ("Hkv", Hkv), ("Lq", Lq), ("M", M), ("page", page))]
+    return int(_lib.load().cover_attn_paged_workspace_bytes(*sizes))
+
+
+def cover_attn_fwd_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0=None, key_lo=None,
+                         key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True, workspace=None, stream=None):
+    """cover_attn_fwd_prefix over a memory in pages. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
+
+    table: int32 [B, M], the sequences' pages; lens: int32 [B], their keys. q0: int32 [B], the position of each sequence's
+    first query row (needed with seeds). key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees of its
+    sequence's (all where None; none: out 0, lse -inf). softcap c > 0: scores become c tanh(score / c). workspace: uint8, at
+    least cover_attn_paged_workspace_bytes, scratch of the call; allocated where None.
+    """
+    if stream is None and type(softcap) is float:
+        r = (_nat or _native()).attn_paged(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
+                                           softcap, out, lse, want_lse, workspace)
+        if r is not None:
+            return _done("cover_attn_fwd_paged", r)
+    _need(q, "q", torch.bfloat16, 4)
+    _pages_need(k_pages, v_pages, table)
+    B, Hq, Lq, D = q.shape
+    n_pages, Hkv, page, _ = k_pages.shape
+    dev = q.device
+    if k_pages.shape[3] != D:
+        raise ValueError("the pages must be [n_pages, Hkv, page, D] matching q")
+    if table.shape[0] != B:
+        raise ValueError("table must be [B, M]")
+    S = 0 if seed_idx is None else int(seed_idx.shape[1])
+    if S > 0:
+        _ints_need((B, S), dev, seed_idx=seed_idx)
+        for name, t in (("k_seedmask", k_seedmask), ("v_seedmask", v_seedmask)):
+            _need(t, name, torch.bfloat16, 4)
+            if tuple(t.shape) != (B, Hkv, S, D):
+                raise ValueError(f"{name} must be [B, Hkv, S, D]")
+        _same_device(dev, k_seedmask=k_seedmask, v_seedmask=v_seedmask)
+        if q0 is None:
+            raise ValueError("q0 must be given with seeds")
+    if lens is None:
+        raise TypeError("lens must be a torch.Tensor")
+    _ints_need((B,), dev, lens=lens, q0=q0)
+    _ints_need((B, Lq), dev, key_lo=key_lo, key_hi=key_hi)
+    make = _maker(stream, dev)
+    if out is None:
+        out = make(q.shape, q.dtype)
+    else:
+        _need(out, "out", torch.bfloat16, 4)
+        if out.shape != q.shape:
+            raise ValueError("out must match q")
+    if lse is None and want_lse:
+        lse = make((B, Hq, Lq), torch.float32)
+    elif lse is not None:
+        _need(lse, "lse", torch.float32, 3)
+        if tuple(lse.shape) != (B, Hq, Lq):
+            raise ValueError("lse must be [B, Hq, Lq]")
+    M = table.shape[1]
+    nbytes = cover_attn_paged_workspace_bytes(B, Hq, Hkv, Lq, M, page)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8, 1)
+        if workspace.numel() < nbytes:
+            raise ValueError(f"workspace must have at least {nbytes} bytes")
+    elif nbytes:
+        workspace = make(nbytes, torch.uint8)
+    _same_device(dev, k_pages=k_pages, out=out, lse=lse, workspace=workspace)
+    _launch("cover_attn_fwd_paged", dev, stream,
+            (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), n_pages, M, page, _ptr(lens), _ptr(k_seedmask) if S else None,
+             _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, _ptr(q0), B, Hq, Hkv, Lq, D,
+             _ptr(key_lo), _ptr(key_hi), float(softcap), _ptr(out), _ptr(lse), _ptr(workspace) if nbytes else None))
+    return out, lse
+
+
+def _logits_need(logits):
+    dt = getattr(logits, "dtype", None)
+    if isinstance(logits, torch.Tensor) and dt not in _ROWS:
+        raise TypeError(f"logits must be torch.bfloat16 or torch.float32, got {dt}")
+    _need(logits, "logits", dt, 2)
+
+
+def cover_logprob_fwd(logits, tok=None, *, topk: int = 0, stream=None):
+    """Log probabilities of given tokens. Returns a dict of CUDA tensors: logp [N] (with tok int32 [N]; 0 for a token outside
+    [0, V)), entropy and lse [N] f32 and, with topk (at most 64), top_idx [N, topk] int32 and top_logp [N, topk] f32: the
+    tokens of the largest logits, equal ones by ascending index. logits: bf16 or fp32 [N, V]."""
+    if stream is None:
+        r = (_nat or _native()).logprob(logits, tok, topk)
+        if r is not None:
+            return _done("cover_logprob_fwd", r)
+    _logits_need(logits)
+    N, V = logits.shape
+    dev = logits.device
+    _ints_need((N,), dev, tok=tok)
+    K = _int32("topk", topk)
+    make = _maker(stream, dev)
+    out = {} if tok is None else dict(logp=make((N,), torch.float32))
+    out.update(entropy=make((N,), torch.float32), lse=make((N,), torch.float32))
+    if 0 < K <= 64:
+        out.update(top_idx=make((N, K), torch.int32), top_logp=make((N, K), torch.float32))
+    o = lambda name: _ptr(out.get(name))  # noqa: E731
+    # (of a topk that is refused there are no outputs: the entry point says so before it looks at them)
+    some = _ptr(logits) if K > 64 else None
+    _launch("cover_logprob_fwd", dev, stream,
+            (_ptr(logits), N, V, logits.element_size(), _ptr(tok), K, o("logp"), o("entropy"), o("lse"), o("top_idx") or some,
+             o("top_logp") or some))
+    return out
+
+
+def cover_logprob_bwd(logits, lse, *, tok=None, d_logp=None, entropy=None, d_entropy=None, d_lse=None, top_idx=None, d_top=None,
+                      out=None, stream=None):
+    """The gradient of cover_logprob_fwd's results in the logits, in their type: logits, lse, entropy, tok and top_idx as they
+    went into and came out of that call; d_logp, d_entropy, d_lse f32 [N] and d_top f32 [N, topk] where they are wanted. out: a
+    tensor for it, which may be the logits themselves."""
+    if stream is None and out is None:
+        r = (_nat or _native()).logprob_grad(logits, lse, tok, entropy, d_logp, d_entropy, d_lse, top_idx, d_top)
+        if r is not None:
+            return _done("cover_logprob_bwd", r)
+    _logits_need(logits)
+    N, V = logits.shape
+    dev = logits.device
+    for (name, t), (other, u) in ((("d_logp", d_logp), ("tok", tok)), (("d_entropy", d_entropy), ("entropy", entropy)),
+                                  (("d_top", d_top), ("top_idx", top_idx))):
+        if t is not None and u is None:
+            raise ValueError(f"{name} needs {other}")
+    given = dict(lse=lse, d_logp=d_logp, entropy=entropy, d_entropy=d_entropy, d_lse=d_lse)
+    for name, t in given.items():
+        if t is not None or name == "lse":
+            _need(t, name, torch.float32, 1)
+            if t.shape[0] != N:
+                raise ValueError(f"{name} must be [N]")
+    _same_device(dev, **given)
+    _ints_need((N,), dev, tok=tok)
+    K = 0
+    if d_top is not None:
+        _need(d_top, "d_top", torch.float32, 2)
+        K = d_top.shape[1]
+        if tuple(d_top.shape) != (N, K):
+            raise ValueError("d_top must be [N, topk]")
+        _same_device(dev, d_top=d_top)
+        _ints_need((N, K), dev, top_idx=top_idx)
+    if out is None:
+        out = _maker(stream, dev)(logits.shape, logits.dtype)
+    else:
+        _need(out, "out", logits.dtype, 2)
+        if out.shape != logits.shape:
+            raise ValueError("out must match logits")
+        _same_device(dev, out=out)
+        others = dict(given, tok=tok, top_idx=top_idx, d_top=d_top)
+        if out.data_ptr() != logits.data_ptr():
+            others["logits"] = logits
+        for name, t in others.items():
+            if t is not None and _overlap(out, t):
+                raise ValueError(f"out must not overlap {name}")
+    _launch("cover_logprob_bwd", dev, stream,
+            (_ptr(logits), N, V, logits.element_size(), _ptr(lse), _ptr(tok), _ptr(d_logp), _ptr(entropy), _ptr(d_entropy), _ptr(d_lse),
+             _ptr(top_idx) if K else None, _ptr(d_top) if K else None, K, _ptr(out)))
+    return out
+
+
 def cover_decide_workspace_bytes(N: int, n_seq: int) -> int:
     return int(_lib.load().cover_decide_workspace_bytes(int(N), int(n_seq)))
 

@@ -30,7 +30,7 @@ BINDING_TAG = os.path.join(BUILD, "binding.tag")   # what _binding.so was compil
 
 SOURCES = ["cover_api.cu", "context.cu", "tmap.cu", "route_kernel.cu", "attn_f32.cu", "attn_bf16_sm103.cu", "attn_window_gqa.cu",
            "score_kernel.cu", "kv_kernel.cu", "mass_kernel.cu", "rope_kernel.cu", "kv8_kernel.cu", "attn_prefix8.cu",
-           "debug_kernels.cu"]
+           "paged_append.cu", "attn_paged.cu", "logprob_kernel.cu", "debug_kernels.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

@@ -42,6 +42,11 @@ decltype(&cover_kv8_write) f_kv8_write;
 decltype(&cover_kv8_read) f_kv8_read;
 decltype(&cover_attn_prefix8_workspace_bytes) f_attn8_bytes;
 decltype(&cover_attn_fwd_prefix8) f_attn8;
+decltype(&cover_paged_append) f_append;
+decltype(&cover_attn_paged_workspace_bytes) f_paged_bytes;
+decltype(&cover_attn_fwd_paged) f_paged;
+decltype(&cover_logprob_fwd) f_logprob;
+decltype(&cover_logprob_bwd) f_logprob_grad;
 
 bool none(PyObject* o) { return o == Py_None; }
 
@@ -595,15 +600,229 @@ PyObject* attn8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A memory in pages and its table: arguments k_pages, v_pages, table.
+struct Pages {
+  void *k, *v;
+  const int32_t* table;
+  int n, Hkv, page, D, B, M;
+  Pages(Args& in, PyObject* const* a) {
+    const Tensor &tk = in.local(a[0], at::kBFloat16, 4), &tv = in.local(a[1], at::kBFloat16, 4), &tt = in.local(a[2], at::kInt, 2);
+    if (!in.ok) return;
+    in.need(tv.sizes() == tk.sizes() && tk.numel() > 0 && tt.numel() > 0);
+    n = dim(tk, 0), Hkv = dim(tk, 1), page = dim(tk, 2), D = dim(tk, 3), B = dim(tt, 0), M = dim(tt, 1);
+    k = ptr<void>(tk), v = ptr<void>(tv), table = ptr<int32_t>(tt);
+  }
+};
+
+// An optional int32 [B] or [B, n] (n < 0: the former), a float [N] with dtype.
+const int32_t* ints(Args& in, PyObject* o, int B, int n = -1) {
+  if (none(o)) return nullptr;
+  const Tensor& t = in.local(o, at::kInt, n < 0 ? 1 : 2);
+  in.need(in.ok && t.size(0) == B && (n < 0 || t.size(1) == n));
+  return in.ok ? ptr<int32_t>(t) : nullptr;
+}
+const float* floats(Args& in, PyObject* o, int N) {
+  if (none(o)) return nullptr;
+  const Tensor& t = in.local(o, at::kFloat, 1);
+  in.need(in.ok && t.size(0) == N);
+  return in.ok ? ptr<float>(t) : nullptr;
+}
+
+// paged_append(k, v, k_pages, v_pages, table, start, count, pos, rope_pos, q, inv_freq, interleaved, mscale, want_k)
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 14, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor &k = in.rows(a[0]), &v = in.rows(a[1]);
+    if (!in.ok) return nullptr;
+    const Pages m(in, a + 2);
+    if (!in.ok) return nullptr;
+    const int B = dim(k, 0), rows = dim(k, 2);
+    in.need(v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes() && m.B == B && dim(k, 1) == m.Hkv && dim(k, 3) == m.D &&
+            rows > 0);
+    if (!in.ok) return nullptr;
+    const int32_t *start = ints(in, a[5], B), *count = ints(in, a[6], B), *pos = ints(in, a[7], B, rows),
+                  *rope_pos = ints(in, a[8], B, rows);
+    in.need((start == nullptr) != (pos == nullptr) && (count == nullptr || pos == nullptr));
+    const bool has_q = !none(a[9]);
+    const Tensor& q = has_q ? in.rows(a[9]) : k;
+    if (!in.ok) return nullptr;
+    if (has_q) in.need(q.scalar_type() == k.scalar_type() && dim(q, 0) == B && dim(q, 1) > 0 && dim(q, 2) == rows && dim(q, 3) == m.D);
+    const double* freq = nullptr;
+    int R = 0;
+    if (!none(a[10])) {
+      const Tensor& f = in.local(a[10], at::kDouble, 1);
+      if (!in.ok) return nullptr;
+      in.need(2 * f.size(0) <= m.D);
+      R = 2 * dim(f, 0);
+      if (R > 0) freq = ptr<double>(f);
+    }
+    const int inter = in.truth(a[11]) ? 1 : 0;
+    const float mscale = static_cast<float>(in.real(a[12]));
+    const bool want_k = in.truth(a[13]);
+    if (!in.ok) return nullptr;
+    int64_t st[9];
+    strides_of(k, st);
+    strides_of(v, st + 3);
+    strides_of(q, st + 6);
+    Tensor new_q, new_k;
+    void *q_out = nullptr, *k_out = nullptr;
+    if (has_q) q_out = ptr<void>(new_q = empty(q.sizes(), q.scalar_type(), q));
+    if (want_k) k_out = ptr<void>(new_k = empty(k.sizes(), k.scalar_type(), k));
+    const void *pk = ptr<void>(k), *pv = ptr<void>(v), *pq = has_q ? ptr<void>(q) : nullptr;
+    const int elem = static_cast<int>(k.element_size()), Hq = has_q ? dim(q, 1) : 0;
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] {
+      return f_append(pk, pv, pq, q_out, k_out, st, m.table, m.n, m.M, m.page, start, count, pos, rope_pos, rows, B, Hq, m.Hkv, m.D, R,
+                      freq, inter, mscale, elem, m.k, m.v, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return pair(Py_None, std::move(new_q), Py_None, std::move(new_k));
+  });
+}
+
+// attn_paged(q, k_pages, v_pages, table, lens, km, vm, seed_idx, q0, key_lo, key_hi, softcap, out, lse, want_lse, workspace)
+PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor& q = in.local(a[0], at::kBFloat16, 4);
+    if (!in.ok) return nullptr;
+    const Pages m(in, a + 1);
+    if (!in.ok) return nullptr;
+    const int B = dim(q, 0), Hq = dim(q, 1), Lq = dim(q, 2);
+    in.need(m.B == B && m.D == dim(q, 3) && q.numel() > 0 && !none(a[4]));
+    int S = 0;
+    const void *km = nullptr, *vm = nullptr;
+    const int32_t* idx = nullptr;
+    if (!none(a[7])) {
+      const Tensor& seeds = in.any_tensor(a[7]);
+      if (!in.ok || seeds.dim() != 2) return nullptr;
+      if (seeds.size(1) > 0) {
+        const Tensor &si = in.local(a[7], at::kInt, 2), &tk = in.local(a[5], at::kBFloat16, 4),
+                     &tv = in.local(a[6], at::kBFloat16, 4);
+        if (!in.ok) return nullptr;
+        S = dim(si, 1);
+        in.need(dim(si, 0) == B && dim(tk, 0) == B && dim(tk, 1) == m.Hkv && dim(tk, 2) == S && dim(tk, 3) == m.D &&
+                tv.sizes() == tk.sizes() && !none(a[8]));
+        if (!in.ok) return nullptr;
+        km = ptr<void>(tk), vm = ptr<void>(tv), idx = ptr<int32_t>(si);
+      }
+    }
+    if (!in.ok) return nullptr;
+    const int32_t *lens = ints(in, a[4], B), *q0 = ints(in, a[8], B), *lo = ints(in, a[9], B, Lq), *hi = ints(in, a[10], B, Lq);
+    const float cap = static_cast<float>(in.real(a[11]));
+    void* out = nullptr;
+    float* lse = nullptr;
+    if (!none(a[12])) {
+      const Tensor& t = in.local(a[12], at::kBFloat16, 4);
+      in.need(in.ok && t.sizes() == q.sizes());
+      if (in.ok) out = ptr<void>(t);
+    }
+    if (!none(a[13])) {
+      const Tensor& t = in.local(a[13], at::kFloat, 3);
+      in.need(in.ok && t.sizes() == q.sizes().slice(0, 3));
+      if (in.ok) lse = ptr<float>(t);
+    }
+    const bool make_lse = none(a[13]) && in.truth(a[14]);
+    if (!in.ok) return nullptr;
+    void* ws = nullptr;
+    Tensor new_out, new_lse, new_ws;
+    const size_t bytes = Hq % m.Hkv == 0 ? f_paged_bytes(B, Hq, m.Hkv, Lq, m.M, m.page) : 0;
+    if (!none(a[15])) {
+      const Tensor& t = in.local(a[15], at::kByte, 1);
+      in.need(in.ok && static_cast<size_t>(t.numel()) >= bytes);
+      if (!in.ok) return nullptr;
+      ws = bytes > 0 ? ptr<void>(t) : nullptr;
+    } else if (bytes > 0) {
+      ws = ptr<void>(new_ws = empty({static_cast<int64_t>(bytes)}, at::kByte, q));
+    }
+    if (out == nullptr) out = ptr<void>(new_out = empty(q.sizes(), at::kBFloat16, q));
+    if (make_lse) lse = ptr<float>(new_lse = empty(q.sizes().slice(0, 3), at::kFloat, q));
+    const void* pq = ptr<void>(q);
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] {
+      return f_paged(pq, m.k, m.v, m.table, m.n, m.M, m.page, lens, km, vm, idx, S, q0, B, Hq, m.Hkv, Lq, m.D, lo, hi, cap, out, lse,
+                     ws, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return pair(a[12], std::move(new_out), a[13], std::move(new_lse));
+  });
+}
+
+// Logits [N, V] on the current device, bf16 or fp32.
+const Tensor& logits_of(Args& in, PyObject* o) {
+  const Tensor& x = in.any_tensor(o);
+  if (!in.ok) return x;
+  in.need(x.scalar_type() == at::kBFloat16 || x.scalar_type() == at::kFloat);
+  if (in.ok) in.local(o, x.scalar_type(), 2);
+  if (in.ok) in.need(x.numel() > 0);
+  return x;
+}
+
+// logprob(logits, tok, topk)
+PyObject* logprob(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 3, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor& x = logits_of(in, a[0]);
+    if (!in.ok) return nullptr;
+    const int N = dim(x, 0), V = dim(x, 1), K = in.integer(a[2]), elem = static_cast<int>(x.element_size());
+    in.need(!none(a[1]) && K >= 0 && K <= 64);   // (other forms: the caller)
+    if (!in.ok) return nullptr;
+    const int32_t* tok = ints(in, a[1], N);
+    if (!in.ok) return nullptr;
+    Item r[] = {{"logp", empty({N}, at::kFloat, x)}, {"entropy", empty({N}, at::kFloat, x)}, {"lse", empty({N}, at::kFloat, x)}};
+    Item top[] = {{"logp", r[0].value}, {"entropy", r[1].value}, {"lse", r[2].value}, {"top_idx", Tensor()}, {"top_logp", Tensor()}};
+    if (K > 0) top[3].value = empty({N, K}, at::kInt, x), top[4].value = empty({N, K}, at::kFloat, x);
+    const void* px = ptr<void>(x);
+    float *lp = ptr<float>(r[0].value), *ent = ptr<float>(r[1].value), *lse = ptr<float>(r[2].value),
+          *tl = K > 0 ? ptr<float>(top[4].value) : nullptr;
+    int32_t* ti = K > 0 ? ptr<int32_t>(top[3].value) : nullptr;
+    void* stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] { return f_logprob(px, N, V, elem, tok, K, lp, ent, lse, ti, tl, stream); });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return K > 0 ? dict_of(top) : dict_of(r);
+  });
+}
+
+// logprob_grad(logits, lse, tok, entropy, d_logp, d_entropy, d_lse, top_idx, d_top)
+PyObject* logprob_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&](Args& in, bool& launched) -> PyObject* {
+    const Tensor& x = logits_of(in, a[0]);
+    if (!in.ok) return nullptr;
+    const int N = dim(x, 0), V = dim(x, 1), elem = static_cast<int>(x.element_size());
+    const float* lse = floats(in, a[1], N);
+    const int32_t* tok = ints(in, a[2], N);
+    const float *ent = floats(in, a[3], N), *g_lp = floats(in, a[4], N), *g_ent = floats(in, a[5], N), *g_lse = floats(in, a[6], N);
+    in.need(lse != nullptr && (g_lp == nullptr || tok != nullptr) && (g_ent == nullptr || ent != nullptr));
+    if (!in.ok) return nullptr;
+    int K = 0;
+    const int32_t* idx = nullptr;
+    const float* g_top = nullptr;
+    if (!none(a[8])) {
+      const Tensor& t = in.local(a[8], at::kFloat, 2);
+      if (!in.ok) return nullptr;
+      K = dim(t, 1);
+      in.need(t.size(0) == N && K > 0 && K <= 64 && !none(a[7]));
+      if (!in.ok) return nullptr;
+      idx = ints(in, a[7], N, K);
+      if (!in.ok) return nullptr;
+      g_top = ptr<float>(t);
+    }
+    Tensor d = empty(x.sizes(), x.scalar_type(), x);
+    const void* px = ptr<void>(x);
+    void *pd = ptr<void>(d), *stream = c10::cuda::getCurrentCUDAStream().stream();
+    const int rc = call(launched, [&] {
+      return f_logprob_grad(px, N, V, elem, lse, tok, g_lp, ent, g_ent, g_lse, idx, g_top, K, pd, stream);
+    });
+    return rc != 0 ? PyLong_FromLong(rc) : wrap(std::move(d));
+  });
+}
+
 // bind(addresses): the entry points' addresses, in the order below
 PyObject* bind(PyObject*, PyObject* list) {
-  constexpr int kBound = 14;
+  constexpr int kBound = 19;
   unsigned long long p[kBound];
   PyObject* t = PySequence_Tuple(list);
   if (t == nullptr) return nullptr;
   if (PyTuple_GET_SIZE(t) != kBound) {
     Py_DECREF(t);
-    PyErr_SetString(PyExc_ValueError, "fourteen addresses are expected");
+    PyErr_SetString(PyExc_ValueError, "nineteen addresses are expected");
     return nullptr;
   }
   for (int i = 0; i < kBound; ++i) p[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(t, i));
@@ -624,6 +843,11 @@ PyObject* bind(PyObject*, PyObject* list) {
   f_kv8_read = reinterpret_cast<decltype(f_kv8_read)>(at(11));
   f_attn8_bytes = reinterpret_cast<decltype(f_attn8_bytes)>(at(12));
   f_attn8 = reinterpret_cast<decltype(f_attn8)>(at(13));
+  f_append = reinterpret_cast<decltype(f_append)>(at(14));
+  f_paged_bytes = reinterpret_cast<decltype(f_paged_bytes)>(at(15));
+  f_paged = reinterpret_cast<decltype(f_paged)>(at(16));
+  f_logprob = reinterpret_cast<decltype(f_logprob)>(at(17));
+  f_logprob_grad = reinterpret_cast<decltype(f_logprob_grad)>(at(18));
   Py_RETURN_NONE;
 }
 
@@ -637,6 +861,10 @@ PyMethodDef methods[] = {
     {"kv8_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv8_write)), METH_FASTCALL, nullptr},
     {"kv8_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv8_read)), METH_FASTCALL, nullptr},
     {"attn8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn8)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+    {"attn_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn_paged)), METH_FASTCALL, nullptr},
+    {"logprob", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(logprob)), METH_FASTCALL, nullptr},
+    {"logprob_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(logprob_grad)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -297,6 +297,115 @@ int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8, const 
   return attn_prefix8_call(a, D, ~size_t{0}, stream);
 }
 
+static int check_pages(const void* k_pages, const void* v_pages, const int32_t* table, int n_pages, int M, int page) {
+  if (k_pages == nullptr || v_pages == nullptr || table == nullptr || n_pages < 1 || M < 1) return COVER_ERR_INVALID_ARG;
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(table, 4)) return COVER_ERR_INVALID_ARG;
+  if (page != 16 && page != 32 && page != 64 && page != 128 && page != 256) return COVER_ERR_UNSUPPORTED;
+  return static_cast<long long>(M) * page < 0x80000000LL ? COVER_OK : COVER_ERR_UNSUPPORTED;
+}
+
+int cover_paged_append(const void* k, const void* v, const void* q, void* q_out, void* k_out, const int64_t* strides,
+                       const int32_t* table, int n_pages, int M, int page, const int32_t* start, const int32_t* count,
+                       const int32_t* pos, const int32_t* rope_pos, int n, int B, int Hq, int Hkv, int D, int R,
+                       const double* inv_freq, int interleaved, float mscale, int elem_bytes, void* k_pages,
+                       void* v_pages, void* stream) {
+  if (B < 1 || Hkv < 1 || Hq < 0 || n < 0 || D < 1 || R < 0 || R % 2 != 0 || R > D) return COVER_ERR_INVALID_ARG;
+  if (elem_bytes != 2 && elem_bytes != 4) return COVER_ERR_INVALID_ARG;
+  const int rc = check_pages(k_pages, v_pages, table, n_pages, M, page);
+  if (rc == COVER_ERR_INVALID_ARG) return rc;
+  if (n > 0) {
+    if (k == nullptr || v == nullptr || strides == nullptr || (R > 0 && inv_freq == nullptr)) return COVER_ERR_INVALID_ARG;
+    if (Hq > 0 && (q == nullptr || q_out == nullptr)) return COVER_ERR_INVALID_ARG;
+    if ((start == nullptr) == (pos == nullptr) || (count != nullptr && pos != nullptr)) return COVER_ERR_INVALID_ARG;
+    const size_t e = static_cast<size_t>(elem_bytes);
+    for (const void* p : {k, v, q, static_cast<const void*>(q_out), static_cast<const void*>(k_out)})
+      if (!aligned(p, e)) return COVER_ERR_INVALID_ARG;
+    for (const int32_t* p : {start, count, pos, rope_pos})
+      if (!aligned(p, 4)) return COVER_ERR_INVALID_ARG;
+    if (!aligned(inv_freq, 8)) return COVER_ERR_INVALID_ARG;
+  }
+  if (rc != COVER_OK || (D != 64 && D != 128)) return COVER_ERR_UNSUPPORTED;
+  if (n == 0) return COVER_OK;
+  const cover::PagedAppendArgs a{k,     v,        q, q_out, k_out, strides, table, n_pages, M,        page,        start,  count,      pos,
+                                 rope_pos, n, B, Hq,    Hkv,   D,       R,     inv_freq, interleaved, mscale, elem_bytes, k_pages, v_pages};
+  return cover::launch_paged_append(a, static_cast<cudaStream_t>(stream));
+}
+
+size_t cover_attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Lq < 1 || M < 1 || page < 1) return 0;
+  return cover::attn_paged_workspace_bytes(B, Hq, Hkv, Lq, M, page);
+}
+
+int cover_attn_fwd_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* table, int n_pages,
+                         int M, int page, const int32_t* lens, const void* k_seedmask, const void* v_seedmask,
+                         const int32_t* seed_idx, int n_seeds, const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
+                         const int32_t* key_lo, const int32_t* key_hi, float softcap, void* out, float* lse,
+                         void* workspace, void* stream) {
+  if (q == nullptr || lens == nullptr || out == nullptr) return COVER_ERR_INVALID_ARG;
+  if (B < 1 || Hq < 1 || Hkv < 1 || Lq < 1 || D < 1 || Hq % Hkv != 0 || n_seeds < 0) return COVER_ERR_INVALID_ARG;
+  if (n_seeds > 0 && (k_seedmask == nullptr || v_seedmask == nullptr || seed_idx == nullptr || q0 == nullptr))
+    return COVER_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(lens, 4) || !aligned(lse, 4) ||
+      !aligned(key_lo, 4) || !aligned(key_hi, 4))
+    return COVER_ERR_INVALID_ARG;
+  if (n_seeds > 0 && (!aligned(k_seedmask, 16) || !aligned(v_seedmask, 16) || !aligned(seed_idx, 4) || !aligned(q0, 4)))
+    return COVER_ERR_INVALID_ARG;
+  if (!(softcap >= 0.0f) || softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
+  const int rc = check_pages(k_pages, v_pages, table, n_pages, M, page);
+  if (rc != COVER_OK) return rc;
+  if (D != 128 || static_cast<long long>(B) * Hq > 0x7fffff00LL / Lq) return COVER_ERR_UNSUPPORTED;
+  if (workspace == nullptr && cover::attn_paged_workspace_bytes(B, Hq, Hkv, Lq, M, page) > 0) return COVER_ERR_INVALID_ARG;
+  int* st = status_block();
+  if (st == nullptr) return COVER_ERR_CUDA;
+  const cover::AttnPagedArgs a{q,        k_pages, v_pages, table, n_pages, M,   page, lens,   k_seedmask, v_seedmask, seed_idx,
+                               n_seeds,  q0,      B,       Hq,    Hkv,     Lq,  key_lo, key_hi, softcap,    out,        lse, workspace};
+  return cover::launch_attn_paged(a, st, static_cast<cudaStream_t>(stream));
+}
+
+static int check_logits(const void* logits, int N, int V, int elem_bytes, int topk) {
+  if (N < 0 || V < 1 || topk < 0 || (elem_bytes != 2 && elem_bytes != 4)) return COVER_ERR_INVALID_ARG;
+  if (N > 0 && (logits == nullptr || !aligned(logits, static_cast<size_t>(elem_bytes)))) return COVER_ERR_INVALID_ARG;
+  return COVER_OK;
+}
+
+int cover_logprob_fwd(const void* logits, int N, int V, int elem_bytes, const int32_t* tok, int topk, float* logp,
+                      float* entropy, float* lse, int32_t* top_idx, float* top_logp, void* stream) {
+  const int rc = check_logits(logits, N, V, elem_bytes, topk);
+  if (rc != COVER_OK) return rc;
+  if (N > 0) {
+    if (entropy == nullptr || lse == nullptr || (tok != nullptr && logp == nullptr)) return COVER_ERR_INVALID_ARG;
+    if (topk > 0 && (top_idx == nullptr || top_logp == nullptr)) return COVER_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(tok), static_cast<const void*>(logp), static_cast<const void*>(entropy),
+                          static_cast<const void*>(lse), static_cast<const void*>(top_idx), static_cast<const void*>(top_logp)})
+      if (!aligned(p, 4)) return COVER_ERR_INVALID_ARG;
+  }
+  if (topk > cover::kMaxTopLogprob) return COVER_ERR_UNSUPPORTED;
+  if (N == 0) return COVER_OK;
+  const cover::LogprobArgs a{logits, N, V, elem_bytes, tok, topk, tok == nullptr ? nullptr : logp, entropy, lse, top_idx, top_logp};
+  return cover::launch_logprob_fwd(a, static_cast<cudaStream_t>(stream));
+}
+
+int cover_logprob_bwd(const void* logits, int N, int V, int elem_bytes, const float* lse, const int32_t* tok,
+                      const float* d_logp, const float* entropy, const float* d_entropy, const float* d_lse,
+                      const int32_t* top_idx, const float* d_top, int topk, void* d_logits, void* stream) {
+  const int rc = check_logits(logits, N, V, elem_bytes, topk);
+  if (rc != COVER_OK) return rc;
+  if (N > 0) {
+    if (lse == nullptr || d_logits == nullptr || (d_logp != nullptr && tok == nullptr) || (d_entropy != nullptr && entropy == nullptr))
+      return COVER_ERR_INVALID_ARG;
+    if (topk > 0 && (top_idx == nullptr || d_top == nullptr)) return COVER_ERR_INVALID_ARG;
+    if (!aligned(d_logits, static_cast<size_t>(elem_bytes))) return COVER_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(lse), static_cast<const void*>(tok), static_cast<const void*>(d_logp),
+                          static_cast<const void*>(entropy), static_cast<const void*>(d_entropy), static_cast<const void*>(d_lse),
+                          static_cast<const void*>(top_idx), static_cast<const void*>(d_top)})
+      if (!aligned(p, 4)) return COVER_ERR_INVALID_ARG;
+  }
+  if (topk > cover::kMaxTopLogprob) return COVER_ERR_UNSUPPORTED;
+  if (N == 0) return COVER_OK;
+  const cover::LogprobGradArgs a{logits, N, V, elem_bytes, lse, tok, d_logp, entropy, d_entropy, d_lse, top_idx, d_top, topk, d_logits};
+  return cover::launch_logprob_bwd(a, static_cast<cudaStream_t>(stream));
+}
+
 size_t cover_decide_workspace_bytes(int N, int n_seq) {
   if (N < 1 || n_seq < 1) return 0;
   // per-segment counters, then u and ln Z per row

@@ -202,6 +202,86 @@ size_t attn_prefix8_mode_bytes(int B, int Hq, int Hkv, int Lq, int L, int mode, 
 void attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int L, bool plain, bool ranges, int* choice, double* us);
 int launch_attn_prefix8(const Attn8Args& a, int* status, cudaStream_t stream);
 
+// New rows into a memory in pages (paged_append.cu). strides: (b, h, s) in elements of k, v, q (Hq = 0 without q); q_out, k_out dense,
+// k_out may be null.
+struct PagedAppendArgs {
+  const void* k;
+  const void* v;
+  const void* q;
+  void* q_out;
+  void* k_out;
+  const int64_t* strides;
+  const int32_t* table;
+  int n_pages, M, page;
+  const int32_t* start;
+  const int32_t* count;
+  const int32_t* pos;
+  const int32_t* rope_pos;
+  int n, B, Hq, Hkv, D, R;
+  const double* inv_freq;
+  int interleaved;
+  float mscale;
+  int elem_bytes;
+  void* k_pages;
+  void* v_pages;
+};
+int launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream);
+
+// Window attention over a memory in pages (attn_paged.cu).
+struct AttnPagedArgs {
+  const void* q;
+  const void* k_pages;
+  const void* v_pages;
+  const int32_t* table;
+  int n_pages, M, page;
+  const int32_t* lens;
+  const void* k_seedmask;
+  const void* v_seedmask;
+  const int32_t* seed_idx;
+  int n_seeds;
+  const int32_t* q0;
+  int B, Hq, Hkv, Lq;
+  const int32_t* key_lo;
+  const int32_t* key_hi;
+  float softcap;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+size_t attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page);
+int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream);
+
+// Log probabilities of given tokens and their gradient (logprob_kernel.cu). tok may be null (logp too), and of the
+// gradient's inputs any but lse.
+constexpr int kMaxTopLogprob = 64;
+struct LogprobArgs {
+  const void* logits;
+  int N, V, elem_bytes;
+  const int32_t* tok;
+  int topk;
+  float* logp;
+  float* entropy;
+  float* lse;
+  int32_t* top_idx;
+  float* top_logp;
+};
+int launch_logprob_fwd(const LogprobArgs& a, cudaStream_t stream);
+struct LogprobGradArgs {
+  const void* logits;
+  int N, V, elem_bytes;
+  const float* lse;
+  const int32_t* tok;
+  const float* d_logp;
+  const float* entropy;
+  const float* d_entropy;
+  const float* d_lse;
+  const int32_t* top_idx;
+  const float* d_top;
+  int topk;
+  void* d_logits;
+};
+int launch_logprob_bwd(const LogprobGradArgs& a, cudaStream_t stream);
+
 int launch_umma_tile(const void* a, const void* b, const void* p, const void* v, float* c1, float* c2, int* status,
                      cudaStream_t stream);
 int launch_wait_timeout(uint64_t limit_ns, int* status, cudaStream_t stream);

@@ -30,6 +30,7 @@
 
 #include "kernels.cuh"
 #include "ptx.cuh"
+#include "rope.cuh"
 
 namespace cover {
 namespace {
@@ -55,34 +56,6 @@ struct RopeParams {
   long long items;         // B * L * chunks * units
   float mscale;
   int inverse;
-};
-
-template <typename T>
-__device__ __forceinline__ float to_f(T x);
-template <>
-__device__ __forceinline__ float to_f(float x) {
-  return x;
-}
-template <>
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) {
-  return __bfloat162float(x);
-}
-template <typename T>
-__device__ __forceinline__ T from_f(float x);
-template <>
-__device__ __forceinline__ float from_f(float x) {
-  return x;
-}
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f(float x) {
-  return __float2bfloat16_rn(x);
-}
-
-__device__ __forceinline__ int not_finite(double x) { return (__double2hiint(x) & 0x7ff00000) == 0x7ff00000; }
-
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-  T v[N];
 };
 
 // T: element; N: elements of a thread's vector (16 bytes, or one element where a size, a stride or
@@ -147,8 +120,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) rope_kernel(
   load(0);
   int bad = 0;   // some frequency is not finite: the exponent bits are all set
   for (int i = threadIdx.x; i < p.R / 2; i += kThreads) {
-    const double radians = p.inv_freq[i], f = radians * 0.15915494309189535;   // / 2 pi
-    turns[i] = __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+    const double radians = p.inv_freq[i];
+    turns[i] = rope_turns(radians);
     bad |= not_finite(radians);
   }
   bad = __syncthreads_or(bad);
@@ -156,11 +129,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) rope_kernel(
   if (turn) {
 #pragma unroll
     for (int i = 0; i < kHalf; ++i) {
-      const uint64_t a = static_cast<uint64_t>(static_cast<int64_t>(at)) * turns[u * kHalf + i];
-      // the nearest of 2^-32 turns, in units of pi: [-1, 1]
-      const float x = static_cast<float>(static_cast<int32_t>((a + 0x80000000ull) >> 32)) * 4.656612873077393e-10f;
       float s, co;
-      sincospif(x, &s, &co);
+      rope_sincos(at, turns[u * kHalf + i], &s, &co);
       cs[i] = co * p.mscale;
       sn[i] = (p.inverse ? -s : s) * p.mscale;
     }
