@@ -6,26 +6,48 @@
 // A seed row's own column (its position is q0[b] + r), where it is among them, is the masked-input pair (k_i, v_i) instead. A row
 // that sees no key gives o = 0, lse = -inf.
 //
-// One CTA a row, 128 keys at a time: a thread holds a key's score, then a column of the sum.
+// The G = Hq / Hkv query heads of a KV head are packed: row p = g Lq + r of KV head (b, hkv) is query row r of head
+// hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view. Two ways, chosen by plan_of:
+//   rows (16 or 32 a group)  few rows: bound by reading the memory
+//   pairs (2 x 128 rows)     many rows: bound by the tensor cores and the softmax
+// A KV tile is 128 keys, fetched a page (or half a page of 256) at a time: boxes of 64 columns by the page's rows land one below the other
+// in the tile, whose 128-byte swizzle goes by the row, so that pages of 16 rows and more make the same tile as one run of
+// rows. A position without a page is fetched from outside the tensor, which reads as zeros, and its scores count as unseen.
+//
+// What no row sees must not reach the sums: scores are taken out by selection, but a weight of zero times a value that is not finite
+// is NaN. KV tiles of which some row does not see some key (the last one of a sequence, diagonals, windows, seeds' own
+// columns) are looked through: a V row with an element that is not finite is set to zeros and reported, and the sums of the rows that see
+// it are made NaN instead. Tiles that all rows see whole are not (there the products give what they give).
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
+#include "attn_common.cuh"
+#include "context.cuh"
 #include "kernels.cuh"
 #include "ptx.cuh"
 #include "route.cuh"
+#include "tmap.cuh"
 
 namespace cover {
 namespace {
 
 constexpr int kD = 128;
+constexpr int kBM = 128;                   // rows per Q tile (pairs)
+constexpr int kBN = 128;                   // keys per KV tile
+constexpr int kTileBytes = kBN * kD * 2;   // 32 KB
+constexpr int kBoxBytes = kTileBytes / 2;  // 64 columns, 128-byte swizzled
+constexpr int kHalf = kBN / 2;
+constexpr int kMaxTilePages = kBN / 16;
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr int kSms = 152;                  // of this GPU
+constexpr float kNan = __builtin_nanf("");
 
 struct Params {
   const __nv_bfloat16* q;
-  const __nv_bfloat16* k_pages;
-  const __nv_bfloat16* v_pages;
   const int32_t* table;
   const int32_t* lens;
   const __nv_bfloat16* k_seedmask;
@@ -36,91 +58,1378 @@ struct Params {
   const int32_t* key_hi;
   __nv_bfloat16* out;
   float* lse;
-  int n_pages, M, page_log2, n_seeds, Hq, Hkv, G, Lq;
-  float scale, cap;
+  float* part_o;     // rows: [2 CTAs][kN][128]; pairs: [nsplit][rows][128]
+  float2* part_ml;   // as part_o's rows: reference (log2 units) and sum
+  int4* joins;       // rows: [CTAs] what the second kernel adds up
+  int* status;
+  long long rows;    // B * Hq * Lq
+  int n_pages, M, page_log2, B, n_seeds, Hq, Hkv, G, Lq, n_groups, nsplit;
+  float scale_log2;  // log2(e) / sqrt(d)
+  float cap_log2;    // cap * log2(e)
+  float cap_in;      // 2 log2(e) / (cap sqrt(d))
 };
 
-__global__ void __launch_bounds__(kD) attn_paged_row_kernel(const __grid_constant__ Params p) {
-  __shared__ float s_q[kD], s_w[kD], s_red[4];
-  __shared__ int64_t s_place[kD];   // element of the pages where the key's row starts, or -1
-  __shared__ int s_slot;
+// Keys of sequence b.
+__device__ __forceinline__ int length_of(const Params& p, int b) {
+  const long long most = static_cast<long long>(p.M) << p.page_log2;
+  return static_cast<int>(min(static_cast<long long>(max(__ldg(p.lens + b), 0)), most));
+}
+// The keys lo .. hi - 1 that row i of [B Lq] sees of its sequence's len, held to 0 .. len; (0, 0) where it sees none.
+__device__ __forceinline__ int2 keys_of(const Params& p, long long i, int len) {
+  const int lo = p.key_lo != nullptr ? max(__ldg(p.key_lo + i), 0) : 0, hi = p.key_hi != nullptr ? min(__ldg(p.key_hi + i), len) : len;
+  return lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
+}
+// Entry of the table for the page that holds key `key` of sequence b, -1 where there is none.
+__device__ __forceinline__ int page_of(const Params& p, int b, int key) {
+  const int i = key >> p.page_log2;
+  const int e = i < p.M ? __ldg(p.table + static_cast<size_t>(b) * p.M + i) : -1;
+  return e >= 0 && e < p.n_pages ? e : -1;
+}
+// Position of query row r of sequence b, or -1 where it is none that a key can have.
+__device__ __forceinline__ int position_of(const Params& p, int b, int r) {
+  const long long at = static_cast<long long>(__ldg(p.q0 + b)) + r;
+  return at >= 0 && at <= 0x7fffffffLL ? static_cast<int>(at) : -1;
+}
+
+// Issues the boxes of one KV tile whose first key is key0 into `tile`, a lane a box; entry: of the lane's page, -1 for none.
+__device__ __forceinline__ void copy_tile(const CUtensorMap* tm, uint8_t* tile, uint64_t* full, int key0, int entry, int h, int page_log2,
+                                          int lane) {
+  const int rows_log2 = min(page_log2, 7), pages = kBN >> rows_log2;
+  if (lane < 2 * pages) {
+    const int half = lane & 1, i = lane >> 1;
+    tma_load_4d(tile + half * kBoxBytes + (i << rows_log2) * 128, tm, full, 64 * half, page_log2 > 7 ? key0 & ((1 << page_log2) - 1) : 0, h,
+                entry);
+  }
+}
+
+// Whether V row `key` of a tile holds an element that is not finite; it is set to zeros then. One thread a key.
+__device__ __forceinline__ bool screen_row(uint32_t tile, int key) {
+  const uint32_t row = tile + key * 128;
+  uint32_t hit = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint4 c = lds128(row + (i >> 3) * kBoxBytes + (((i & 7) ^ (key & 7)) << 4));
+    // an exponent of all ones carries into the sign's place
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hit |= (w[e] & 0x7fff7fffu) + 0x00800080u;
+  }
+  const bool bad = (hit & 0x80008000u) != 0;
+  if (bad) {
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i) sts128(row + (i >> 3) * kBoxBytes + ((i & 7) << 4), 0, 0, 0, 0);
+  }
+  return bad;
+}
+
+// Whether any of 128 or 256 threads of a named barrier says so.
+template <int kAll>
+__device__ __forceinline__ bool any_of(int barrier, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, %3, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(x ? 1u : 0u), "r"(barrier), "n"(kAll)
+      : "memory");
+  return r != 0;
+}
+template <int kAll>
+__device__ __forceinline__ void sync_of(int barrier) {
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kAll) : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Few rows
+// ---------------------------------------------------------------------------
+// The products are turned over, S^T = K Q^T (128 keys x kN rows), O^T += V^T P^T (128 columns x kN rows): a Q tile of 128 rows
+// would cost the tensor cores and the softmax the same for one row as for 128. A softmax thread is a key. The rows' largest
+// scores are only looked for when some score is above its row's reference by more than the threshold (one vote a tile); sums stay with
+// the threads until the keys of a unit are through. Two streams take alternate KV tiles, with sums and an accumulator of their own.
+//
+// One CTA an SM, and the KV tiles of all units (sequence, KV head, group of rows) are one row of tiles of which every CTA takes an even
+// share, whatever the lengths: a batch of sequences of 1 to 1000 tiles keeps all SMs reading until the end. Where a
+// share's border cuts a unit, its CTAs leave their parts to a second kernel: at most two a CTA. Loads run on across units, so that a
+// unit's end is hidden behind the next one's tiles.
+//
+// Roles (512 threads): warps 0-3, 4-7 softmax of the streams; 8-11 look V tiles through; 12 products; 13 copies; 14 lays out what
+// is to be done, tile by tile: pages, masks and rows, up to 8 tiles ahead.
+// Shared memory: five tiles of K or V in the order K0 K1 V0 K2 V1 .., Q of two units, P^T of two streams (rows of 128 bytes).
+// Tensor memory: S0 | S1 | O0 | O1, kN columns each.
+constexpr int kRowsThreads = 512;
+constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsCopyWarp = 13, kRowsPlanWarp = 14;
+constexpr int kSlots = 5, kRing = 8, kUnits = 4;
+
+struct TileJob {
+  int page[kMaxTilePages];   // entries of its pages, -1 for none
+  int key0, h, q_row;
+  uint32_t valid;            // bit i: page i is there
+  int first, last;           // of the unit's tiles in this CTA
+  int partial;               // some row does not see some key
+  int unit;                  // number of the unit in this CTA
+};
+
+template <int kN>
+struct RowsSmem {
+  uint8_t kv[kSlots][kTileBytes];
+  uint8_t q[2][kN * kD * 2];
+  uint8_t pt[2][kBN * 128];
+  uint64_t full[kSlots], empty[kSlots];
+  uint64_t q_full[2], q_empty[2];
+  uint64_t job_full[kRing], job_empty[kRing], v_clean[kRing];
+  uint64_t unit_full[kUnits], unit_empty[kUnits];
+  uint64_t s_full[2], p_full[2], o_full, drain;
+  TileJob job[kRing];
+  uint4 nan_keys[kRing];
+  int4 row[kUnits][kN];      // per unit: keys lo, hi, position of a seed row or -1, its slot
+  int4 unit[kUnits];         // tiles here, rows, first row of [B Hq Lq], part's place: -1 whole, else its number
+  int2 unit_mask[kUnits];    // masked-input rows of the KV head, whether the unit's first tile is here
+  float4 fin[kN];            // weights of the two accumulators and of the masked-input value, 1 / l
+  float m[2][kN], step[2][kN], factor[2][kN];
+  int unseen[2][kN], any_unseen[2];
+  float red[2][4][kN];
+  float s_self[kN];
+  int slot[kN];
+  long long scan[kRowsThreads / 32];
+  long long t0, t1, before;  // this CTA's tiles, those before the first sequence of them
+  int b0;
+  uint32_t tmem_base;
+  int abort;
+};
+
+// First of the tiles of CTA c of n, of T.
+__device__ __forceinline__ long long share_start(long long c, long long n, long long T) { return c * T / n; }
+
+// KV tiles of a unit of sequence b, and the first of them; one at least. One warp, or (kAlone) one thread.
+template <bool kAlone>
+__device__ __forceinline__ int2 tiles_of(const Params& p, int b) {
+  const int len = length_of(p, b);
+  int lo = 0x7fffffff, hi = 0;
+  if (p.key_lo == nullptr && p.key_hi == nullptr) {
+    lo = 0, hi = len;
+  } else {
+    for (int r = kAlone ? 0 : threadIdx.x & 31; r < p.Lq; r += kAlone ? 1 : 32) {
+      const int2 k = keys_of(p, static_cast<long long>(b) * p.Lq + r, len);
+      if (k.y > 0) lo = min(lo, k.x), hi = max(hi, k.y);
+    }
+    if (!kAlone) lo = __reduce_min_sync(0xffffffffu, lo), hi = __reduce_max_sync(0xffffffffu, hi);
+  }
+  if (hi == 0) return make_int2(1, 0);
+  const int first = lo / kBN;
+  return make_int2((hi - 1) / kBN + 1 - first, first);
+}
+
+template <int kN, bool kCap>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+    attn_paged_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                           const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  using Sm = RowsSmem<kN>;
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr uint32_t kTmem = 4 * kN;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (warp == kRowsMmaWarp) {
+    if (lane == 0) {
+      for (int i = 0; i < kSlots; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < kRing; ++i) {
+        mbar_init(&sm.job_full[i], 1);
+        mbar_init(&sm.job_empty[i], 10);   // copies, products, four warps that look V through, four of a stream
+        mbar_init(&sm.v_clean[i], 128);
+      }
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&sm.q_full[i], 1);
+        mbar_init(&sm.q_empty[i], 1);
+        mbar_init(&sm.s_full[i], 1);
+        mbar_init(&sm.p_full[i], 128);
+      }
+      for (int i = 0; i < kUnits; ++i) mbar_init(&sm.unit_full[i], 1), mbar_init(&sm.unit_empty[i], 8);
+      mbar_init(&sm.o_full, 1);
+      mbar_init(&sm.drain, 1);
+      sm.abort = 0;
+      sm.b0 = 0;
+      fence_mbar_init();
+      tma_prefetch_desc(&tm_q);
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+    }
+    __syncwarp();
+    tmem_alloc(&sm.tmem_base, kTmem);
+    tmem_relinquish();
+  }
   griddep_wait();
   griddep_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long row = blockIdx.x;
-  const int r = static_cast<int>(row % p.Lq), hq = static_cast<int>(row / p.Lq % p.Hq), b = static_cast<int>(row / p.Lq / p.Hq);
-  const int h = hq / p.G;
-  s_q[tid] = __bfloat162float(p.q[row * kD + tid]) * p.scale;
-  if (tid == 0) s_slot = kNoSlot;
+
+  // ---------------- the CTA's share of all tiles ----------------
+  const long long heads = static_cast<long long>(p.Hkv) * p.n_groups;   // units of a sequence
+  const int each = (p.B + kRowsThreads - 1) / kRowsThreads;             // sequences of a thread
+  const int b_lo = min(tid * each, p.B), b_hi = min(b_lo + each, p.B);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) mine += tiles_of<true>(p, b).x * heads;
+  long long incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += x;
+  }
+  if (lane == 31) sm.scan[warp] = incl;
+  tc_fence_before_sync();
   __syncthreads();
-  const long long i = static_cast<long long>(b) * p.Lq + r;
-  const int64_t len = min(static_cast<int64_t>(__ldg(p.lens + b)), static_cast<int64_t>(p.M) << p.page_log2);
-  const int64_t lo = max(0, p.key_lo != nullptr ? __ldg(p.key_lo + i) : 0);
-  const int64_t hi = p.key_hi != nullptr ? min(len, static_cast<int64_t>(__ldg(p.key_hi + i))) : len;
-  int64_t own = -1;
+  tc_fence_after_sync();
+  const uint32_t tbase = sm.tmem_base;
+  long long before = 0, all = 0;
+  for (int w = 0; w < kRowsThreads / 32; ++w) {
+    if (w < warp) before += sm.scan[w];
+    all += sm.scan[w];
+  }
+  const long long n_ctas = min(static_cast<long long>(gridDim.x), all), c = blockIdx.x;
+  const long long t0 = c < n_ctas ? share_start(c, n_ctas, all) : 0, t1 = c < n_ctas ? share_start(c + 1, n_ctas, all) : 0;
+  before += incl - mine;
+  if (t0 < t1 && t0 >= before && t0 < before + mine) {
+    int b = b_lo;
+    for (long long x; before + (x = tiles_of<true>(p, b).x * heads) <= t0; ++b) before += x;
+    sm.b0 = b;
+    sm.before = before;
+  }
+  __syncthreads();
+  const int n = static_cast<int>(t1 - t0);   // tiles of this CTA
+  const int n_packed = p.G * p.Lq;
+
+  if (warp == kRowsPlanWarp) {
+    // ---------------- what is to be done ----------------
+    bool ok = true;
+    int b = sm.b0, g = 0, unit = 0;
+    long long first = sm.before;   // of the sequence's tiles
+    int2 tiles = n > 0 ? tiles_of<false>(p, b) : make_int2(1, 0);
+    if (n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    bool joined = false;
+    for (long long t = t0; t < t1 && ok; ++unit) {
+      while (t >= first + tiles.x * heads) first += tiles.x * heads, tiles = tiles_of<false>(p, ++b);
+      const int u = static_cast<int>((t - first) / tiles.x), j = static_cast<int>((t - first) % tiles.x);
+      const int nt = static_cast<int>(min(static_cast<long long>(tiles.x - j), t1 - t));
+      const int h = u / p.n_groups, p0 = (u % p.n_groups) * kN, n_rows = min(kN, n_packed - p0);
+      const long long rowbase = (static_cast<long long>(b) * p.Hq + h * p.G) * p.Lq;
+      const int len = length_of(p, b), buf = unit % kUnits;
+      if (unit >= kUnits) ok = warp_wait(&sm.unit_empty[buf], (unit / kUnits - 1) & 1, &sm.abort);
+      if (!ok) break;
+      // seed rows: the rows stand at up to kN positions, r itself or r - r0 around Lq
+      const int r0 = p.Lq <= kN ? 0 : p0 % p.Lq;
+      if (p.n_seeds > 0) {
+        if (lane < kN) sm.slot[lane] = kNoSlot;
+        __syncwarp();
+        for (int s = lane; s < p.n_seeds; s += 32) {
+          const long long at = static_cast<long long>(__ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + s)) - __ldg(p.q0 + b);
+          if (at < 0 || at >= p.Lq) continue;
+          const int i = static_cast<int>(at >= r0 ? at - r0 : at - r0 + p.Lq);
+          if (i < kN) atomicMin(&sm.slot[i], s);
+        }
+        __syncwarp();
+      }
+      int all_lo = 0, all_hi = 0x7fffffff, own_lo = 0x7fffffff, own_hi = -1;   // keys that every row sees, seed rows' positions
+      if (lane < kN) {
+        int4 row = make_int4(0, 0, -1, 0);
+        if (lane < n_rows) {
+          const int r = (p0 + lane) % p.Lq;
+          const int2 k = keys_of(p, static_cast<long long>(b) * p.Lq + r, len);
+          row.x = k.x, row.y = k.y;
+          if (p.n_seeds > 0) {
+            const int slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
+            if (slot != kNoSlot && at >= k.x && at < k.y && page_of(p, b, at) >= 0) {
+              row.z = at, row.w = slot;
+              own_lo = own_hi = at;
+            }
+          }
+          all_lo = row.x, all_hi = row.y;   // (a row that sees nothing makes every tile partial)
+        }
+        sm.row[buf][lane] = row;
+      }
+      all_lo = __reduce_max_sync(0xffffffffu, all_lo), all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+      own_lo = __reduce_min_sync(0xffffffffu, own_lo), own_hi = __reduce_max_sync(0xffffffffu, own_hi);
+      const bool whole = nt == tiles.x;
+      __syncwarp();
+      if (lane == 0) {
+        // a part that begins its unit comes last in its CTA, any other first
+        const int place = whole ? -1 : static_cast<int>(2 * c) + (j == 0 ? 1 : 0);
+        sm.unit[buf] = make_int4(nt, n_rows, static_cast<int>(rowbase + p0), place);
+        sm.unit_mask[buf] = make_int2(static_cast<int>((static_cast<long long>(b) * p.Hkv + h)), j == 0 ? 1 : 0);
+        if (j == 0 && !whole) {
+          // the unit's last tile is of CTA ((tile + 1) n - 1) / T
+          const long long last = first + static_cast<long long>(u + 1) * tiles.x - 1;
+          p.joins[blockIdx.x] = make_int4(static_cast<int>(((last + 1) * n_ctas - 1) / all - c) + 1, n_rows, static_cast<int>(rowbase + p0), 0);
+          joined = true;
+        }
+        mbar_arrive(&sm.unit_full[buf]);
+      }
+      const int pages = kBN >> min(p.page_log2, 7);
+      for (int i = 0; i < nt && ok; ++i, ++g) {
+        const int key0 = (tiles.y + j + i) * kBN, at = g % kRing;
+        const int entry = lane < pages ? page_of(p, b, key0 + (lane << min(p.page_log2, 7))) : -1;
+        if (g >= kRing) ok = warp_wait(&sm.job_empty[at], (g / kRing - 1) & 1, &sm.abort);
+        if (!ok) break;
+        TileJob& job = sm.job[at];
+        const uint32_t valid = __ballot_sync(0xffffffffu, entry >= 0);
+        if (lane < pages) job.page[lane] = entry;
+        if (lane == 0) {
+          job.key0 = key0;
+          job.h = h;
+          job.q_row = static_cast<int>(rowbase + p0);
+          job.valid = valid;
+          job.first = i == 0;
+          job.last = i == nt - 1;
+          job.partial = key0 < all_lo || all_hi - key0 < kBN || valid != (1u << pages) - 1u || (own_hi >= key0 && own_lo - key0 < kBN);
+          job.unit = unit;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.job_full[at]);
+      }
+      t += nt;
+    }
+    if (lane == 0 && n > 0 && !joined) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 80);
+      sm.abort = 1;
+    }
+  } else if (warp == kRowsCopyWarp) {
+    // ---------------- copies ----------------
+    bool ok = true;
+    int issued = 0, q_issued = 0;   // tiles of K and V, units
+    for (int i = 0; i < 2 * n && ok; ++i) {
+      // K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1)
+      const bool is_v = i > 0 && ((i & 1) == 0 || i == 2 * n - 1);
+      const int g = i == 0 ? 0 : is_v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2;
+      const int at = g % kRing, slot = i % kSlots;
+      if (!is_v) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);
+      if (ok && i >= kSlots) ok = warp_wait(&sm.empty[slot], (i / kSlots - 1) & 1, &sm.abort);
+      if (!ok) break;
+      const TileJob& job = sm.job[at];
+      if (!is_v && job.first) {
+        const int buf = job.unit & 1;
+        if (job.unit >= 2) ok = warp_wait(&sm.q_empty[buf], ((job.unit >> 1) - 1) & 1, &sm.abort);
+        if (!ok) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&sm.q_full[buf], kN * kD * 2);
+          for (int h = 0; h < 2; ++h) tma_load_4d(sm.q[buf] + h * kN * 128, &tm_q, &sm.q_full[buf], 64 * h, job.q_row, 0, 0);
+        }
+        q_issued = job.unit + 1;
+      }
+      if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], kTileBytes);
+      __syncwarp();
+      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], job.key0, job.page[(lane >> 1) % kMaxTilePages], job.h, p.page_log2, lane);
+      __syncwarp();
+      if (is_v && lane == 0) mbar_arrive(&sm.job_empty[at]);
+      issued = i + 1;
+    }
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 81);
+      sm.abort = 1;
+    }
+    // every copy lands before the CTA's shared memory is released, whatever the other roles did
+    if (lane == 0) {
+      for (int f = max(0, issued - kSlots); f < issued; ++f) mbar_wait(&sm.full[f % kSlots], (f / kSlots) & 1, nullptr);
+      for (int f = max(0, q_issued - 2); f < q_issued; ++f) mbar_wait(&sm.q_full[f & 1], (f >> 1) & 1, nullptr);
+    }
+  } else if (warp == kRowsMmaWarp) {
+    if (lane == 0 && n > 0) {
+      // ---------------- products ----------------
+      constexpr uint32_t id_s = idesc_bf16_f32(kBN, kN, false, false);
+      constexpr uint32_t id_o = idesc_bf16_f32(kD, kN, true, true);
+      // descriptors are added up in their lower words; K's, Q's and P's upper words are the same
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, 1024), dv = sdesc_sw128(smem_u32(sm.kv[0]), kBoxBytes, 1024);
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024), dp = sdesc_sw128(smem_u32(sm.pt[0]), 16, 1024);
+      const uint32_t k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv), q_lo = static_cast<uint32_t>(dq),
+                     p_lo = static_cast<uint32_t>(dp), hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+      const auto desc = [](uint32_t lo, uint32_t up) { return (static_cast<uint64_t>(up) << 32) | lo; };
+      const auto wait = [&](uint64_t* bar, int phase) {
+        const bool done = mbar_wait(bar, phase & 1, &sm.abort);
+        if (done) tc_fence_after_sync();
+        return done;
+      };
+      const auto k_load = [](int g) { return g == 0 ? 0 : 2 * g - 1; };   // number of a tile's copy
+      bool ok = true;
+      int unit = -1;   // of the last S
+      // S^T[g & 1] = K(tile g) . Q^T
+      const auto issue_s = [&](int g) {
+        const int at = g % kRing, i = k_load(g), slot = i % kSlots;
+        ok = wait(&sm.job_full[at], g / kRing) && wait(&sm.full[slot], i / kSlots);
+        if (!ok) return;
+        if (sm.job[at].first) {
+          ++unit;
+          ok = wait(&sm.q_full[unit & 1], unit >> 1);
+          if (!ok) return;
+        }
+        const uint32_t k = k_lo + ((slot * kTileBytes) >> 4), q = q_lo + (((unit & 1) * kN * kD * 2) >> 4);
+#pragma unroll
+        for (int kk = 0; kk < kD / 16; ++kk)
+          umma_ss(tbase + (g & 1) * kN, desc(k + (((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4), hi),
+                  desc(q + (((kk >> 2) * kN * 128 + (kk & 3) * 32) >> 4), hi), id_s, kk > 0 ? 1u : 0u);
+        umma_commit(&sm.s_full[g & 1]);
+        umma_commit(&sm.empty[slot]);
+        if (sm.job[at].last) umma_commit(&sm.q_empty[unit & 1]);
+      };
+      for (int g = 0; g < 2 && g < n && ok; ++g) issue_s(g);
+      int in_unit = 0;   // the tile's number in its unit
+      for (int g = 0; g < n && ok; ++g, ++in_unit) {
+        const int at = g % kRing, i = g == n - 1 ? 2 * n - 1 : 2 * g + 2, slot = i % kSlots, s = g & 1;
+        ok = wait(&sm.full[slot], i / kSlots) && wait(&sm.v_clean[at], g / kRing) && wait(&sm.p_full[s], g >> 1);
+        if (!ok) break;
+        if (sm.job[at].first) in_unit = 0;
+        const bool last = sm.job[at].last != 0;
+        const uint32_t v = v_lo + ((slot * kTileBytes) >> 4), pt = p_lo + ((s * kBN * 128) >> 4);
+        // O^T[s] (+)= V(tile g)^T . P^T
+#pragma unroll
+        for (int kk = 0; kk < kBN / 16; ++kk)
+          umma_ss(tbase + (2 + s) * kN, desc(v + ((kk * 2048) >> 4), v_hi), desc(pt + ((kk * 2048) >> 4), hi), id_o,
+                  (in_unit > 1 || kk > 0) ? 1u : 0u);
+        umma_commit(&sm.empty[slot]);
+        if (last) umma_commit(&sm.o_full);
+        mbar_arrive(&sm.job_empty[at]);
+        if (g + 2 < n) issue_s(g + 2);
+      }
+      if (!ok) {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 82);
+        sm.abort = 1;
+      }
+      // all tensor-core work of this CTA completes before tensor memory is released
+      umma_commit(&sm.drain);
+      mbar_wait(&sm.drain, 0, nullptr);
+    }
+    __syncwarp();
+  } else if (warp >= kScreenWarp && warp < kRowsMmaWarp) {
+    // ---------------- V rows that are not finite (thread = key) ----------------
+    const int key = tid - kScreenWarp * 32;
+    bool ok = true;
+    int waited = 0;   // every copy is waited for, in their order: a slot's barrier tells a copy from the one before it alone
+    for (int g = 0; g < n; ++g) {
+      const int at = g % kRing, i = g == n - 1 ? 2 * n - 1 : 2 * g + 2, slot = i % kSlots;
+      ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);
+      for (; waited <= i && ok; ++waited) ok = warp_wait(&sm.full[waited % kSlots], (waited / kSlots) & 1, &sm.abort);
+      if (!ok) break;
+      uint32_t bad = 0;
+      if (sm.job[at].partial) {
+        bad = __ballot_sync(0xffffffffu, screen_row(smem_u32(sm.kv[slot]), key));
+        fence_proxy_async_smem();
+      }
+      if (lane == 0) reinterpret_cast<uint32_t*>(&sm.nan_keys[at])[key >> 5] = bad;
+      __syncwarp();
+      mbar_arrive(&sm.v_clean[at]);
+      if (lane == 0) mbar_arrive(&sm.job_empty[at]);
+    }
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 83);
+      sm.abort = 1;
+    }
+  } else if (warp < kScreenWarp) {
+    // ---------------- softmax (thread = key of a KV tile) ----------------
+    const int stream = warp >> 2, key = tid & (kBN - 1), w4 = warp & 3;
+    const uint32_t quad = tbase + (static_cast<uint32_t>(w4 * 32) << 16);
+    const uint32_t s_addr = quad + stream * kN, o_addr = quad + (2 + stream) * kN;
+    const float* m = sm.m[stream];
+    const uint32_t pt = smem_u32(sm.pt[stream]) + key * 128;
+    const uint32_t sw = static_cast<uint32_t>(key & 7) << 4;
+    const int page_rows = min(p.page_log2, 7);
+    bool ok = true;
+    int g = 0;
+    for (int unit = 0; g < n; ++unit) {
+      const int buf = unit % kUnits;
+      ok = warp_wait(&sm.unit_full[buf], (unit / kUnits) & 1, &sm.abort);
+      if (any_of<256>(1, !ok)) {
+        ok = false;
+        break;
+      }
+      const int4 info = sm.unit[buf];
+      const int nt = info.x, n_rows = info.y;
+      const long long orow0 = info.z;
+      const int place = info.w;
+      const bool own_rows = sm.unit_mask[buf].y != 0 && p.n_seeds > 0;   // the masked-input pairs are added where the unit begins
+      const size_t masked0 = static_cast<size_t>(sm.unit_mask[buf].x) * p.n_seeds;
+      if (key < kN) {
+        sm.m[stream][key] = 0.0f;
+        sm.unseen[stream][key] = key < n_rows ? 1 : 0;
+        if (key == 0) sm.any_unseen[stream] = 1;
+        if (stream == 0) sm.s_self[key] = -INFINITY;
+      }
+      sync_of<256>(1);
+      if (own_rows) {
+        // the seed rows' own scores (log2 units): a warp a row, four columns a lane
+        for (int i = warp; i < n_rows; i += 8) {
+          const int4 row = sm.row[buf][i];
+          if (row.z < 0) continue;
+          const uint2 a = __ldg(reinterpret_cast<const uint2*>(p.q + (orow0 + i) * kD) + lane);
+          const uint2 b = __ldg(reinterpret_cast<const uint2*>(p.k_seedmask + (masked0 + row.w) * kD) + lane);
+          float dot = __uint_as_float(a.x << 16) * __uint_as_float(b.x << 16);
+          dot = fmaf(__uint_as_float(a.x & 0xffff0000u), __uint_as_float(b.x & 0xffff0000u), dot);
+          dot = fmaf(__uint_as_float(a.y << 16), __uint_as_float(b.y << 16), dot);
+          dot = fmaf(__uint_as_float(a.y & 0xffff0000u), __uint_as_float(b.y & 0xffff0000u), dot);
+          for (int d = 16; d >= 1; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+          if (lane == 0) sm.s_self[i] = kCap ? capped(dot, p.cap_in, p.cap_log2) : dot * p.scale_log2;
+        }
+      }
+      float l[kN];
+#pragma unroll
+      for (int i = 0; i < kN; ++i) l[i] = 0.0f;
+      const int g0 = g;
+      for (; g < g0 + nt; ++g) {
+        if ((g & 1) != stream) continue;
+        const int at = g % kRing;
+        ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort) && warp_wait(&sm.s_full[stream], (g >> 1) & 1, &sm.abort);
+        const bool partial = ok && sm.job[at].partial != 0;
+        if (partial) ok = warp_wait(&sm.v_clean[at], (g / kRing) & 1, &sm.abort);
+        float t[kN];        // scores less the references, in log2 units
+        bool over = !ok;    // a warp whose wait gave up votes all the same: the stream's barriers take 128 threads
+        if (ok) {
+          tc_fence_after_sync();
+#pragma unroll
+          for (int c0 = 0; c0 < kN; c0 += 16) {
+            uint32_t x[16];
+            tmem_ld16(s_addr + c0, x);
+            tmem_ld_wait16(x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float f = __uint_as_float(x[e]);
+              t[c0 + e] = kCap ? capped(f, p.cap_in, p.cap_log2) - m[c0 + e] : fmaf(f, p.scale_log2, -m[c0 + e]);
+            }
+          }
+          if (partial) {
+            const int pos = sm.job[at].key0 + key;
+            const bool held = ((sm.job[at].valid >> (key >> page_rows)) & 1u) != 0;
+            const bool nan = ((reinterpret_cast<const uint32_t*>(&sm.nan_keys[at])[key >> 5] >> (key & 31)) & 1u) != 0;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+              const int4 row = sm.row[buf][i];
+              if (nan) t[i] = kNan;
+              if (!held || pos < row.x || pos >= row.y || pos == row.z) t[i] = -INFINITY;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kN; ++i) over |= i < n_rows && t[i] > kRescaleThreshold;
+          over |= sm.any_unseen[stream] != 0;
+          __syncwarp();
+        }
+        if (any_of<128>(2 + stream, over)) {
+          if (any_of<128>(2 + stream, !ok)) {
+            ok = false;
+            break;
+          }
+          // new references: the rows' maxima where they are above the old ones by more than the threshold
+#pragma unroll
+          for (int i = 0; i < kN; ++i) {
+            const int top = __reduce_max_sync(0xffffffffu, ordered(t[i] == t[i] ? t[i] : -INFINITY));
+            if (lane == (i & 31)) sm.red[stream][w4][i] = from_ordered(top);
+          }
+          sync_of<128>(2 + stream);
+          if (key < kN) {
+            const float up = fmaxf(fmaxf(sm.red[stream][0][key], sm.red[stream][1][key]),
+                                   fmaxf(sm.red[stream][2][key], sm.red[stream][3][key]));
+            // a row's first keys set its reference, wherever they lie
+            const bool first = sm.unseen[stream][key] != 0 && up > -INFINITY;
+            const float step = first || up > kRescaleThreshold ? up : 0.0f;
+            sm.step[stream][key] = step;
+            sm.factor[stream][key] = first ? 0.0f : ex2_approx(-step);
+            sm.m[stream][key] = m[key] + step;
+            if (first) sm.unseen[stream][key] = 0;
+            const uint32_t mask = kN == 32 ? 0xffffffffu : 0xffffu;
+            const uint32_t still = __ballot_sync(mask, sm.unseen[stream][key] != 0);
+            if (key == 0) sm.any_unseen[stream] = still != 0 ? 1 : 0;
+          }
+          sync_of<128>(2 + stream);
+#pragma unroll
+          for (int i = 0; i < kN; ++i) {
+            t[i] -= sm.step[stream][i];
+            l[i] *= sm.factor[stream][i];
+          }
+          if (g - g0 >= 2) {
+            // O holds the stream's earlier products of the unit (complete: the commit of this S came after them)
+#pragma unroll
+            for (int c0 = 0; c0 < kN; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16(o_addr + c0, o);
+              tmem_ld_wait16(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sm.factor[stream][c0 + e]);
+              tmem_st16(o_addr + c0, o);
+            }
+            tmem_st_wait();
+          }
+        }
+#pragma unroll
+        for (int c0 = 0; c0 < kN; c0 += 8) {
+          if (c0 >= n_rows) break;   // (columns of P^T behind the rows hold anything: so do those of O^T)
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float e0 = ex2_approx(t[c0 + 2 * e]), e1 = ex2_approx(t[c0 + 2 * e + 1]);
+            l[c0 + 2 * e] += e0;
+            l[c0 + 2 * e + 1] += e1;
+            w[e] = pack_bf16x2(e0, e1);   // V's operands are bf16, so P's have to be; a weight is off by 2^-8 of itself
+          }
+          sts128(pt + (static_cast<uint32_t>(c0 * 2) ^ sw), w[0], w[1], w[2], w[3]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        mbar_arrive(&sm.p_full[stream]);
+        if (lane == 0) mbar_arrive(&sm.job_empty[at]);
+      }
+      if (ok) ok = warp_wait(&sm.o_full, unit & 1, &sm.abort);
+      if (any_of<256>(1, !ok)) {
+        ok = false;
+        break;
+      }
+
+      // ---------------- the rows' results ----------------
+      tc_fence_after_sync();
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        if (i >= n_rows) break;
+        float x = l[i];
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (lane == (i & 31)) sm.red[stream][w4][i] = x;
+      }
+      sync_of<256>(1);
+      // a stream without a tile here has seen nothing
+      if (tid < n_rows) {
+        const float s_self = sm.s_self[tid];
+        float l2[2];
+        for (int s = 0; s < 2; ++s) l2[s] = (sm.red[s][0][tid] + sm.red[s][1][tid]) + (sm.red[s][2][tid] + sm.red[s][3][tid]);
+        const float m0 = sm.unseen[0][tid] ? -INFINITY : sm.m[0][tid], m1 = sm.unseen[1][tid] ? -INFINITY : sm.m[1][tid];
+        const float top = fmaxf(fmaxf(m0, m1), s_self);
+        const float f0 = m0 == -INFINITY ? 0.0f : ex2_approx(m0 - top), f1 = m1 == -INFINITY ? 0.0f : ex2_approx(m1 - top);
+        const float p_self = s_self == -INFINITY ? 0.0f : ex2_approx(s_self - top);
+        // (NaN scores leave the references alone: they are in the sums)
+        float sum = fmaf(f0, l2[0], fmaf(f1, l2[1], p_self));
+        if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
+        if (s_self != s_self) sum = s_self;
+        sm.fin[tid] = make_float4(f0, f1, p_self, place >= 0 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+        if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + tid] = make_float2(top, sum);
+        else if (p.lse != nullptr) p.lse[orow0 + tid] = (top + lg2_approx(sum)) * 0.6931471805599453f;
+      }
+      sync_of<256>(1);
+      // thread = output column; the streams' warps take 16 rows in turn
+      for (int c0 = 16 * stream; c0 < n_rows; c0 += 32) {
+        uint32_t o[2][16];
+        tmem_ld16(quad + 2 * kN + c0, o[0]);
+        tmem_ld16(quad + 3 * kN + c0, o[1]);
+        tmem_ld_wait16(o[0]);
+        tmem_ld_wait16(o[1]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int i = c0 + e;
+          if (i < n_rows) {
+            const float4 f = sm.fin[i];
+            float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
+            if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
+            if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
+            if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
+            else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
+          }
+        }
+        __syncwarp();
+      }
+      tc_fence_before_sync();
+      // both accumulators have been read before a stream lets the next unit's products begin
+      sync_of<256>(1);
+      if (lane == 0) mbar_arrive(&sm.unit_empty[buf]);
+    }
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 84);
+      sm.abort = 1;
+    }
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  if (warp == kRowsMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tbase, kTmem);
+  }
+}
+
+// Adds up the parts of a unit that began in main CTA blockIdx.y: a warp a row, four columns a lane.
+constexpr int kJoinWarps = 4;
+template <int kN>
+__global__ void __launch_bounds__(kJoinWarps * 32) attn_paged_join_rows_kernel(const __grid_constant__ Params p) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, i = blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+  const int4 join = p.joins[blockIdx.y];   // parts, rows, first row
+  if (i >= join.y) return;
+  // the first part is the last of its CTA, the others the first of theirs
+  const auto at = [&](int k) { return (2 * (static_cast<size_t>(blockIdx.y) + k) + (k == 0 ? 1 : 0)) * kN + i; };
+  float m = -INFINITY;
+  for (int k = lane; k < join.x; k += 32) m = fmaxf(m, p.part_ml[at(k)].x);
+  for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  float l = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int k = 0; k < join.x; ++k) {
+    const float2 ml = p.part_ml[at(k)];
+    const float4 o = *reinterpret_cast<const float4*>(p.part_o + at(k) * kD + 4 * lane);
+    const float w = ml.x == -INFINITY ? 0.0f : ex2_approx(ml.x - m);
+    l = ml.x == -INFINITY ? l + ml.y : fmaf(w, ml.y, l);   // (a sum of NaN is taken along)
+    acc.x = fmaf(w, o.x, acc.x), acc.y = fmaf(w, o.y, acc.y), acc.z = fmaf(w, o.z, acc.z), acc.w = fmaf(w, o.w, acc.w);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const long long row = static_cast<long long>(join.z) + i;
+  reinterpret_cast<uint2*>(p.out + row * kD)[lane] =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + lg2_approx(l)) * 0.6931471805599453f;
+}
+
+// ---------------------------------------------------------------------------
+// Many rows
+// ---------------------------------------------------------------------------
+// A CTA takes two Q tiles of 128 packed rows, a stream each, that read each KV tile together, against one of nsplit parts of the keys that its
+// rows see. Two threads of different warpgroups share a row, 64 columns each, in two chunks of 32.
+// Roles (640 threads): warps 0-15 softmax (warpgroup 2 t + h: columns 64 h .. 64 h + 63 of Q tile t); 16 products; 17, 18 copies of K and V;
+// 19 looks V tiles through.
+// Shared memory: Q (2 x 32 KB) | two tiles of K, two of V. Tensor memory: S0 | S1 (the P of a half overwrites the first 32 columns of that
+// half's scores, behind its loads) | O0 | O1, 128 columns each.
+constexpr int kPairsThreads = 640;
+constexpr int kPairSoftmaxWarps = 16, kPairMmaWarp = 16, kPairCopyWarp = 17, kPairScreenWarp = 19;
+
+struct PairSmem {
+  uint8_t q[2][kTileBytes];
+  uint8_t k[2][kTileBytes];
+  uint8_t v[2][kTileBytes];
+  uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], v_clean[2];
+  uint64_t s_full[2], p_full[2], o_full, drain;
+  uint4 nan_keys[4];                    // per KV tile in turn: keys whose V row is not finite
+  float red[2][2][kBM];                 // per Q tile and half of the columns
+  int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
+  int lo, hi;                           // keys that some row sees
+  int all_lo[2], all_hi[2];             // keys that every row of a Q tile sees that sees any
+  int own_lo, own_hi;                   // seed rows' positions
+  uint32_t tmem_base;
+  int abort;
+};
+
+// This part's KV tiles among those that the CTA's rows see.
+__device__ __forceinline__ int2 part_of(int lo, int hi, int ks, int nsplit) {
+  const int t0 = hi > 0 ? lo / kBN : 0, t1 = hi > 0 ? (hi - 1) / kBN + 1 : 0;
+  const int each = (t1 - t0) / nsplit, more = (t1 - t0) % nsplit;
+  return make_int2(t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0));
+}
+
+// What a row does not see of 64 columns of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1), those without
+// a page (bit i of holes: keys i * 2^page_rows on of these 64); whether anything of it holds for some row of the warp.
+struct Unseen {
+  int lo, hi, own;
+  uint32_t holes;
+  int page_rows;
+  bool any;
+};
+
+// Caps (to log2 units) and masks the scores of 32 columns from column c0 on.
+template <bool kCap>
+__device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, const Unseen& u, int c0) {
+  if (kCap) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
+  }
+  if (u.any) {
+    const int lo = u.lo - c0, hi = u.hi - c0, own = u.own - c0;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if (c < lo || c >= hi || c == own) s[c] = -INFINITY;
+    if (u.holes != 0) {
+#pragma unroll
+      for (int c = 0; c < 32; c += 16)
+        if ((u.holes >> ((c0 + c) >> u.page_rows)) & 1u) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[c + e] = -INFINITY;
+        }
+    }
+  }
+}
+
+// The largest of 32 columns' scores, neither scaled nor capped yet.
+__device__ __forceinline__ float chunk_max(uint32_t addr, const Params& p, const Unseen& u, int c0) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+  finish_scores<false>(s, p, u, c0);
+  return max32(s);
+}
+
+// P = 2^(score - m) of 32 columns to tensor memory, in bf16 (V's operands are, so P's have to be: a weight is off by at most 2^-8 of itself).
+// Returns the sum of the unrounded weights.
+template <bool kCap>
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+  finish_scores<kCap>(s, p, u, c0);
+  const float scale = kCap ? 1.0f : p.scale_log2;
+  const uint64_t negm2 = f2_pack(-m, -m), scale2 = f2_pack(scale, scale);
+  uint64_t acc2[2] = {0, 0};
+  uint32_t packed[16];
+#pragma unroll
+  for (int c = 0; c < 16; ++c) {
+    float x0, x1;
+    f2_unpack(f2_fma(f2_pack(s[2 * c], s[2 * c + 1]), scale2, negm2), x0, x1);
+    const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+    packed[c] = pack_bf16x2(e0, e1);
+    acc2[c & 1] = f2_add(acc2[c & 1], f2_pack(e0, e1));
+  }
+  tmem_st16(p_addr, packed);
+  float r[4];
+  f2_unpack(acc2[0], r[0], r[1]);
+  f2_unpack(acc2[1], r[2], r[3]);
+  return (r[0] + r[1]) + (r[2] + r[3]);
+}
+
+// A seed row's own score in log2 units: q row `row` of [B Hq Lq], masked-input key row `self`.
+template <bool kCap>
+__device__ __forceinline__ float self_score(const Params& p, long long row, size_t self) {
+  const uint4* qr = reinterpret_cast<const uint4*>(p.q + row * kD);
+  const uint4* kr = reinterpret_cast<const uint4*>(p.k_seedmask + self * kD);
+  float d0 = 0.0f, d1 = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < kD / 8; ++i) {
+    const uint4 a = __ldg(qr + i), c = __ldg(kr + i);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      d0 = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), d0);
+      d1 = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), d1);
+    }
+  }
+  return kCap ? capped(d0 + d1, p.cap_in, p.cap_log2) : (d0 + d1) * p.scale_log2;
+}
+
+// o += w v for 32 columns of a masked-input value.
+__device__ __forceinline__ void add_self(float (&o)[32], float w, const __nv_bfloat16* v) {
+  const uint4* vr = reinterpret_cast<const uint4*>(v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint4 a = __ldg(vr + e);
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      o[8 * e + 2 * f] = fmaf(w, __uint_as_float(x[f] << 16), o[8 * e + 2 * f]);
+      o[8 * e + 2 * f + 1] = fmaf(w, __uint_as_float(x[f] & 0xffff0000u), o[8 * e + 2 * f + 1]);
+    }
+  }
+}
+
+template <bool kCap>
+__global__ void __launch_bounds__(kPairsThreads, 1)
+    attn_paged_pairs_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  PairSmem& sm = *reinterpret_cast<PairSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // CTA (ks, group, hkv, b)
+  const int ks = static_cast<int>(blockIdx.x) % p.nsplit;
+  int rest = static_cast<int>(blockIdx.x) / p.nsplit;
+  const int group = rest % p.n_groups;
+  rest /= p.n_groups;
+  const int hkv = rest % p.Hkv;
+  const int b = rest / p.Hkv;
+  const int n_packed = p.G * p.Lq;
+  const int p0 = group * 2 * kBM;
+  const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
+
+  if (warp == kPairMmaWarp) {
+    if (lane == 0) {
+      mbar_init(&sm.q_full, 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&sm.k_full[i], 1);
+        mbar_init(&sm.k_empty[i], 1);
+        mbar_init(&sm.v_full[i], 1);
+        mbar_init(&sm.v_empty[i], 1);
+        mbar_init(&sm.v_clean[i], 1);
+        mbar_init(&sm.s_full[i], 1);
+        mbar_init(&sm.p_full[i], 256);
+        sm.all_lo[i] = 0;
+        sm.all_hi[i] = 0x7fffffff;
+      }
+      mbar_init(&sm.o_full, 1);
+      mbar_init(&sm.drain, 1);
+      sm.abort = 0;
+      sm.lo = 0x7fffffff;
+      sm.hi = 0;
+      sm.own_lo = 0x7fffffff;
+      sm.own_hi = -1;
+      fence_mbar_init();
+      tma_prefetch_desc(&tm_q);
+    }
+    __syncwarp();
+    tmem_alloc(&sm.tmem_base, 512);
+    tmem_relinquish();
+  }
+  if (p.n_seeds > 0 && tid < 2 * kBM) sm.slot[tid] = kNoSlot;
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tbase = sm.tmem_base;
+  griddep_wait();
+  griddep_launch_dependents();
+
+  // ---------------- the rows' keys ----------------
+  const int tile = warp >> 3, half = (warp >> 2) & 1;   // of a softmax warp
+  const int R = tid & (kBM - 1);
+  const int P = p0 + tile * kBM + R;
+  const bool softmax = warp < kPairSoftmaxWarps;
+  const bool valid = softmax && P < n_packed;
+  const int r = valid ? P % p.Lq : 0;
+  const int len = length_of(p, b);
+  int row_lo = 0, row_hi = 0;
+  if (valid) {
+    const int2 keys = keys_of(p, static_cast<long long>(b) * p.Lq + r, len);
+    row_lo = keys.x, row_hi = keys.y;
+  }
   if (p.n_seeds > 0) {
-    own = static_cast<int64_t>(__ldg(p.q0 + b)) + r;
-    for (int s = tid; s < p.n_seeds; s += kD)
-      if (__ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + s) == own) atomicMin(&s_slot, s);
-    __syncthreads();
-    if (s_slot == kNoSlot) own = -1;
-  }
-  const size_t self = ((static_cast<size_t>(b) * p.Hkv + h) * p.n_seeds + (own >= 0 ? s_slot : 0)) * kD;
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  for (int64_t j0 = lo; j0 < hi; j0 += kD) {
-    const int64_t j = j0 + tid;
-    int64_t place = -1;
-    float s = -INFINITY;
-    if (j < hi) {
-      const int entry = __ldg(p.table + static_cast<size_t>(b) * p.M + (j >> p.page_log2));
-      if (entry >= 0 && entry < p.n_pages)
-        place = ((((static_cast<int64_t>(entry) * p.Hkv + h) << p.page_log2) + (j & ((1 << p.page_log2) - 1)))) * kD;
-    }
-    if (place >= 0) {
-      const __nv_bfloat16* k = j == own ? p.k_seedmask + self : p.k_pages + place;
-      s = 0.0f;
-      for (int d = 0; d < kD; ++d) s = fmaf(s_q[d], __bfloat162float(k[d]), s);
-      if (p.cap > 0.0f) s = p.cap * tanhf(s / p.cap);
-    }
-    s_place[tid] = place;
-    float top = s;
-    for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (lane == 0) s_red[warp] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    const float to = fmaxf(m, top), f = m == -INFINITY ? 0.0f : __expf(m - to);
-    float w = s == -INFINITY ? 0.0f : __expf(s - to);
-    s_w[tid] = w;
-    for (int d = 16; d >= 1; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
-    __syncthreads();
-    if (lane == 0) s_red[warp] = w;
-    __syncthreads();
-    l = l * f + (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
-    o *= f;
-    m = to;
-    for (int k = 0; k < kD && j0 + k < hi; ++k) {
-      if (s_place[k] < 0) continue;
-      const __nv_bfloat16* v = j0 + k == own ? p.v_seedmask + self : p.v_pages + s_place[k];
-      o = fmaf(s_w[k], __bfloat162float(v[tid]), o);
+    // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
+    const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
+    const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
+    const long long first = __ldg(p.q0 + b);
+    for (int s = tid; s < p.n_seeds; s += kPairsThreads) {
+      const long long at = __ldg(seeds + s) - first;
+      if (at < 0 || at >= p.Lq) continue;
+      const long long i = at >= r0 ? at - r0 : at - r0 + p.Lq;
+      if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
     }
     __syncthreads();
   }
-  p.out[row * kD + tid] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o / l);
-  if (tid == 0 && p.lse != nullptr) p.lse[row] = m + logf(l);
+  int slot = kNoSlot, pos = -1;   // of a seed row that sees its position
+  if (valid && p.n_seeds > 0) {
+    const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
+    const int s = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
+    if (s != kNoSlot && at >= row_lo && at < row_hi && page_of(p, b, at) >= 0) slot = s, pos = at;
+  }
+  const bool is_seed = slot != kNoSlot;
+  if (softmax) {
+    const bool some = row_lo < row_hi;
+    const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, row_hi);
+    const int all_lo = __reduce_max_sync(0xffffffffu, row_lo), all_hi = __reduce_min_sync(0xffffffffu, some ? row_hi : 0x7fffffff);
+    const int own_lo = __reduce_min_sync(0xffffffffu, is_seed ? pos : 0x7fffffff), own_hi = __reduce_max_sync(0xffffffffu, pos);
+    if (lane == 0 && hi > 0) {
+      atomicMin(&sm.lo, lo);
+      atomicMax(&sm.hi, hi);
+      atomicMax(&sm.all_lo[tile], all_lo);
+      atomicMin(&sm.all_hi[tile], all_hi);
+      if (own_hi >= 0) atomicMin(&sm.own_lo, own_lo), atomicMax(&sm.own_hi, own_hi);
+    }
+  }
+  __syncthreads();
+  const int2 part = part_of(sm.lo, sm.hi, ks, p.nsplit);
+  const int j0 = part.x, nt = part.y;
+  const int page_rows = min(p.page_log2, 7), pages = kBN >> page_rows;   // of a KV tile
+  bool hole = false;   // some page with keys that rows see is not there
+  for (int i = tid; i < nt * pages; i += kPairsThreads) {
+    const int key = j0 * kBN + (i << page_rows);
+    if (key < sm.hi && sm.lo - key < 1 << page_rows) hole |= page_of(p, b, key) < 0;
+  }
+  const bool holes = __syncthreads_or(hole) != 0;
+  const bool two_tiles = p0 + kBM < n_packed;   // the second Q tile has rows
+  // whether some row does not see some key of KV tile j of the part
+  const int all_lo = max(sm.all_lo[0], sm.all_lo[1]), all_hi = min(sm.all_hi[0], sm.all_hi[1]), own_lo = sm.own_lo, own_hi = sm.own_hi;
+  const auto partial = [&](int j) {
+    const int key0 = (j0 + j) * kBN;
+    return holes || key0 < all_lo || all_hi - key0 < kBN || (own_hi >= key0 && own_lo - key0 < kBN);
+  };
+
+  if (warp >= kPairMmaWarp) {
+    if (warp == kPairMmaWarp && lane == 0 && nt > 0) {
+      // ---------------- products ----------------
+      constexpr uint32_t id_qk = idesc_bf16_f32(kBM, kBN, false, false);
+      constexpr uint32_t id_pv = idesc_bf16_f32(kBM, kD, false, true);
+      constexpr uint32_t kTileDesc = kTileBytes >> 4;
+      const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
+      const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
+      // descriptors are added up in their lower words, and of several barriers the one that completes last is waited for last: what
+      // this thread does between a barrier and its products is on every tile's way
+      const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
+      const uint32_t qk_hi = static_cast<uint32_t>(dq >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+      const auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
+      // S[s] = Q[s] . K(stage)^T
+      auto issue_s = [&](int s, int st) {
+        const uint32_t a = q_lo + s * kTileDesc, kb = k_lo + st * kTileDesc;
+#pragma unroll
+        for (int kk = 0; kk < kD / 16; ++kk) {
+          const uint32_t off = static_cast<uint32_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
+          umma_ss(tbase + s * kBN, desc(a + off, qk_hi), desc(kb + off, qk_hi), id_qk, kk > 0 ? 1u : 0u);
+        }
+        umma_commit(&sm.s_full[s]);
+      };
+      // O[s] (+)= P[s] . V(stage)
+      auto issue_pv = [&](int s, int st, bool acc) {
+        const uint32_t vb = v_lo + st * kTileDesc;
+#pragma unroll
+        for (int kk = 0; kk < kBN / 16; ++kk)
+          umma_ts(tbase + 2 * kBN + s * kD, tbase + s * kBN + (kk >> 2) * kHalf + 8 * (kk & 3),
+                  desc(vb + static_cast<uint32_t>((kk * 2048) >> 4), v_hi), id_pv, (acc || kk > 0) ? 1u : 0u);
+      };
+      auto wait = [&](uint64_t* bar, int phase) {
+        const bool ok = mbar_wait(bar, phase & 1, &sm.abort);
+        if (ok) tc_fence_after_sync();
+        return ok;
+      };
+      bool ok = wait(&sm.q_full, 0);
+      if (ok && (ok = wait(&sm.k_full[0], 0))) {
+        issue_s(0, 0);
+        if (two_tiles) issue_s(1, 0);
+        umma_commit(&sm.k_empty[0]);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int st = j & 1;
+        const bool next = j + 1 < nt;
+        ok = (!next || wait(&sm.k_full[st ^ 1], (j + 1) >> 1)) && wait(&sm.v_full[st], j >> 1) && wait(&sm.v_clean[st], j >> 1) &&
+             wait(&sm.p_full[0], j);
+        if (!ok) break;
+        issue_pv(0, st, j > 0);
+        if (next) issue_s(0, st ^ 1);
+        if (two_tiles) {
+          ok = wait(&sm.p_full[1], j);
+          if (!ok) break;
+          issue_pv(1, st, j > 0);
+          if (next) issue_s(1, st ^ 1);
+        }
+        umma_commit(&sm.v_empty[st]);
+        if (next) umma_commit(&sm.k_empty[st ^ 1]);
+      }
+      if (ok) {
+        umma_commit(&sm.o_full);
+      } else {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 85);
+        sm.abort = 1;
+      }
+      // all tensor-core work of this CTA completes before tensor memory is released
+      umma_commit(&sm.drain);
+      mbar_wait(&sm.drain, 0, nullptr);
+    } else if ((warp == kPairCopyWarp || warp == kPairCopyWarp + 1) && nt > 0) {
+      // ---------------- copies ----------------
+      const int which = warp - kPairCopyWarp;
+      const CUtensorMap* tm = which ? &tm_v : &tm_k;
+      uint64_t* const full = which ? sm.v_full : sm.k_full;
+      uint64_t* const empty = which ? sm.v_empty : sm.k_empty;
+      if (which == 0 && lane == 0) {
+        mbar_arrive_expect_tx(&sm.q_full, 2 * kTileBytes);
+        for (int t = 0; t < 2; ++t)
+          for (int h = 0; h < 2; ++h)
+            tma_load_4d(sm.q[t] + h * kBoxBytes, &tm_q, &sm.q_full, 64 * h, static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
+      }
+      // a lane's page of the next tile is looked up a tile ahead
+      const int my_key = ((lane >> 1) % pages) << page_rows;
+      int entry = page_of(p, b, j0 * kBN + my_key);
+      int j = 0;
+      bool ok = true;
+      for (; j < nt; ++j) {
+        const int st = j & 1;
+        const int next = j + 1 < nt ? page_of(p, b, (j0 + j + 1) * kBN + my_key) : -1;
+        if (j >= 2) ok = warp_wait(&empty[st], ((j >> 1) - 1) & 1, &sm.abort);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(&full[st], kTileBytes);
+        __syncwarp();
+        copy_tile(tm, which ? sm.v[st] : sm.k[st], &full[st], (j0 + j) * kBN, entry, hkv, p.page_log2, lane);
+        __syncwarp();
+        entry = next;
+      }
+      if (!ok && lane == 0) {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 86);
+        sm.abort = 1;
+      }
+      // every copy lands before the CTA's shared memory is released, whatever the other roles did
+      if (lane == 0) {
+        if (which == 0) mbar_wait(&sm.q_full, 0, nullptr);
+        for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&full[f & 1], (f >> 1) & 1, nullptr);
+      }
+    } else if (warp == kPairScreenWarp) {
+      // ---------------- V rows that are not finite (a lane four keys) ----------------
+      bool ok = true;
+      for (int j = 0; j < nt; ++j) {
+        const int st = j & 1;
+        if (j >= 2) ok = warp_wait(&sm.v_empty[st], ((j >> 1) - 1) & 1, &sm.abort);   // no tile ahead of the copies
+        if (ok && partial(j)) {
+          ok = warp_wait(&sm.v_full[st], (j >> 1) & 1, &sm.abort);
+          if (ok) {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t hit = __ballot_sync(0xffffffffu, screen_row(smem_u32(sm.v[st]), 32 * i + lane));
+              if (lane == i) reinterpret_cast<uint32_t*>(&sm.nan_keys[j & 3])[i] = hit;
+            }
+            fence_proxy_async_smem();
+          }
+        }
+        if (!ok) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.v_clean[st]);
+      }
+      if (!ok && lane == 0) {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 87);
+        sm.abort = 1;
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------- softmax ----------------
+    const size_t self = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds + (is_seed ? slot : 0);
+    // the seed rows' own scores (log2 units), in the first part alone
+    const float s_self = ks == 0 && is_seed ? self_score<kCap>(p, rowbase + P, self) : -INFINITY;
+    const bool warp_live = __any_sync(0xffffffffu, valid);
+    const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t s_addr = quad + tile * kBN + half * kHalf;
+    const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
+    float m_run = -INFINITY, l_run = 0.0f;
+    bool ok = true;
+    const int jend = tile == 1 && !two_tiles ? 0 : nt;
+    for (int j = 0; j < jend; ++j) {
+      ok = warp_wait(&sm.s_full[tile], j & 1, &sm.abort);
+      tc_fence_after_sync();   // zeros are stored over S too, where no row sees a key
+      const int key0 = (j0 + j) * kBN + half * kHalf;
+      const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch of this half are seen
+      // (a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything)
+      const bool some = __any_sync(0xffffffffu, valid && max(cl, 0) < min(ch, kHalf));
+      Unseen u{cl, ch, is_seed ? pos - key0 : -1, 0u, page_rows, false};
+      u.any = __any_sync(0xffffffffu, valid && (cl > 0 || ch < kHalf || (u.own >= 0 && u.own < kHalf)));
+      if (holes) {
+        const int i = lane << page_rows;   // the half's pages, a lane each (pages of 128 and 256: one)
+        u.holes = __ballot_sync(0xffffffffu, (lane == 0 || i < kHalf) && page_of(p, b, key0 + i) < 0);
+        u.any |= u.holes != 0;
+      }
+      float m_half = -INFINITY;
+      if (ok && some) {
+#pragma unroll 1
+        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, c));
+        m_half = !kCap ? m_half * p.scale_log2 : m_half == -INFINITY ? m_half : capped(m_half, p.cap_in, p.cap_log2);   // (the cap is monotonous)
+      }
+      // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row
+      // take the same reference
+      if (any_of<256>(2 + tile, !ok || (valid && m_half > m_run + kRescaleThreshold))) {
+        if (any_of<256>(2 + tile, !ok)) {
+          ok = false;
+          break;
+        }
+        sm.red[tile][half][R] = m_half;
+        sync_of<256>(2 + tile);
+        const float top = fmaxf(sm.red[tile][0][R], sm.red[tile][1][R]);
+        float alpha = 1.0f;
+        if (top > m_run + kRescaleThreshold) {
+          alpha = m_run == -INFINITY ? 0.0f : ex2_approx(m_run - top);
+          m_run = top;
+        }
+        l_run *= alpha;
+        if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+          // O holds the tile's earlier products (complete: the commit of this S came after them)
+          tc_fence_after_sync();
+#pragma unroll 1
+          for (int c = 0; c < 2; ++c) {
+            uint32_t o[32];
+            tmem_ld32(o_addr + 32 * c, o);
+            tmem_ld_wait(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(o_addr + 32 * c, o);
+          }
+        }
+      }
+      if (some) {
+        const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
+#pragma unroll 1
+        for (int c = 0; c < kHalf; c += 32) l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, c, m_use);
+      } else if (warp_live) {
+        const uint32_t zeros[16] = {};
+        tmem_st16(s_addr, zeros);
+        tmem_st16(s_addr + 16, zeros);
+      }
+      if (partial(j)) {
+        // V was looked through: a row that sees one of these keys has a sum of NaN (both threads of it look, for all 128)
+        ok = warp_wait(&sm.v_clean[j & 1], (j >> 1) & 1, &sm.abort);
+        if (!ok && lane == 0) sm.abort = 1;   // (the next wait ends the loop, at a vote)
+        if (ok) {
+          const uint32_t* nan = reinterpret_cast<const uint32_t*>(&sm.nan_keys[j & 3]);
+#pragma unroll 1
+          for (int w = 0; w < 4; ++w) {
+            for (uint32_t bits = nan[w]; bits != 0; bits &= bits - 1) {
+              const int at = (j0 + j) * kBN + 32 * w + __ffs(bits) - 1;
+              if (at >= row_lo && at < row_hi && !(is_seed && at == pos)) l_run = kNan;
+            }
+          }
+        }
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      mbar_arrive(&sm.p_full[tile]);
+    }
+    if (ok && nt > 0) ok = warp_wait(&sm.o_full, 0, &sm.abort);
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 88);
+      sm.abort = 1;
+    }
+
+    // ---------------- the rows' results ----------------
+    tc_fence_after_sync();
+    sync_of<256>(2 + tile);                     // the last references have been read
+    sm.red[tile][half][R] = l_run;
+    sync_of<256>(2 + tile);
+    float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
+    if (s_self != -INFINITY) {
+      const float m_all = fmaxf(m, s_self);
+      const float f = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
+      p_self = ex2_approx(s_self - m_all);
+      l = l * f + p_self;
+      w = f;
+      m = m_all;
+    }
+    if (s_self != s_self) l = s_self;           // NaN in the masked-input pair
+    const long long orow = rowbase + P;
+    const bool split = p.nsplit > 1;
+    const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);   // 1 / l, once a row; zero where no key was seen
+    if (ok && warp_live) {
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {
+        float o[32] = {};
+        if (nt > 0) {
+          uint32_t x[32];
+          tmem_ld32(o_addr + 32 * c, x);
+          tmem_ld_wait(x);
+          // (a row that has seen nothing may hold what other rows' values made of zero weights)
+          const bool nothing = m_run == -INFINITY && l_run == 0.0f;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = w == 0.0f || nothing ? 0.0f : __uint_as_float(x[e]) * w;
+        }
+        const int col = half * kHalf + 32 * c;
+        if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + col);
+        if (valid && split) {
+          float4* dst = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(ks) * p.rows + orow) * kD + col);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        } else if (valid) {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kD + col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+        }
+        __syncwarp();   // the next chunk is loaded by the whole warp
+      }
+      if (valid && half == 0) {
+        if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
+        else if (p.lse != nullptr) p.lse[orow] = (m + lg2_approx(l)) * 0.6931471805599453f;
+      }
+    }
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  if (warp == kPairMmaWarp) {
+    tc_fence_after_sync();
+    tmem_dealloc(tbase, 512);
+  }
+}
+
+// Adds up the parts of every row: a warp a row, four columns a lane.
+__global__ void __launch_bounds__(kJoinWarps * 32) attn_paged_join_pairs_kernel(const __grid_constant__ Params p) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const long long row = static_cast<long long>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
+  float m = -INFINITY;
+  for (int k = lane; k < p.nsplit; k += 32) m = fmaxf(m, p.part_ml[row + k * p.rows].x);
+  for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  float l = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int k = 0; k < p.nsplit; ++k) {
+    const float2 ml = p.part_ml[row + k * p.rows];
+    const float4 o = *reinterpret_cast<const float4*>(p.part_o + (row + k * p.rows) * kD + 4 * lane);
+    const float w = ml.x == -INFINITY ? 0.0f : ex2_approx(ml.x - m);
+    l = ml.x == -INFINITY ? l + ml.y : fmaf(w, ml.y, l);   // (a sum of NaN is taken along)
+    acc.x = fmaf(w, o.x, acc.x), acc.y = fmaf(w, o.y, acc.y), acc.z = fmaf(w, o.z, acc.z), acc.w = fmaf(w, o.w, acc.w);
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  reinterpret_cast<uint2*>(p.out + row * kD)[lane] =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + lg2_approx(l)) * 0.6931471805599453f;
+}
+
+enum Mode { kRows16, kRows32, kPairs };
+
+struct Plan {
+  Mode mode;
+  int n_groups, nsplit;
+  int ctas;   // rows: of the main kernel
+};
+
+Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
+  const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
+  const long long nkv = (static_cast<long long>(M) * page + kBN - 1) / kBN;   // KV tiles of a sequence at most
+  if (packed <= 32) {
+    const long long most = std::min<long long>(static_cast<long long>(B) * Hkv, kSms) * std::min<long long>(nkv, kSms);
+    return Plan{packed <= 16 ? kRows16 : kRows32, 1, 1, static_cast<int>(std::min<long long>(kSms, most))};
+  }
+  Plan best{kPairs, static_cast<int>((packed + 2 * kBM - 1) / (2 * kBM)), 0, 0};
+  const double rows = static_cast<double>(B) * Hq * Lq;
+  const long long units = static_cast<long long>(best.n_groups) * Hkv * B;
+  double best_us = 0.0;
+  for (int ns = 1; ns <= nkv && ns <= 64; ++ns) {
+    const long long waves = (units * ns + kSms - 1) / kSms, tiles = (nkv + ns - 1) / ns;
+    const double us = 5.0 + waves * (3.5 + 1.6 * tiles) + (ns > 1 ? 2.4 + 0.15 * ns + 1.9e-4 * rows * ns : 0.0);
+    if (best.nsplit == 0 || us < best_us) best.nsplit = ns, best_us = us;
+    if (units * ns > 8 * kSms) break;
+  }
+  return best;
+}
+
+constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSmem<32>) + 1024};
+constexpr size_t kPairSmemBytes = sizeof(PairSmem) + 1024;
+static_assert(kRowsSmemBytes[1] <= 227 * 1024 && kPairSmemBytes <= 227 * 1024, "shared memory of a CTA");
+
+using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
+constexpr Kernel kRowsKernels[2][2] = {{attn_paged_rows_kernel<16, false>, attn_paged_rows_kernel<16, true>},
+                                       {attn_paged_rows_kernel<32, false>, attn_paged_rows_kernel<32, true>}};
+constexpr Kernel kPairKernels[2] = {attn_paged_pairs_kernel<false>, attn_paged_pairs_kernel<true>};
+
+// rows of all parts
+size_t part_rows(const Plan& plan, int B, int Hq, int Lq) {
+  if (plan.mode != kPairs) return static_cast<size_t>(2 * plan.ctas) * (plan.mode == kRows16 ? 16 : 32);
+  return plan.nsplit > 1 ? static_cast<size_t>(B) * Hq * Lq * plan.nsplit : 0;
 }
 
 }  // namespace
 
-size_t attn_paged_workspace_bytes(int, int, int, int, int, int) { return 0; }
+size_t attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page) {
+  const Plan plan = plan_of(B, Hq, Hkv, Lq, M, page);
+  return part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2)) + (plan.mode != kPairs ? plan.ctas * sizeof(int4) : 0);
+}
 
-int launch_attn_paged(const AttnPagedArgs& a, int*, cudaStream_t stream) {
-  const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
-  if (rows > 0x7fffffffLL) return -2;
+int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) {
   using bf16 = __nv_bfloat16;
+  const Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.M, a.page);
+  const bool few = plan.mode != kPairs;
+  const int width = plan.mode == kRows16 ? 16 : 32;
+  const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
+  const long long grid = few ? plan.ctas : static_cast<long long>(plan.n_groups) * a.Hkv * a.B * plan.nsplit;
+  if (grid > 0x7fffffffLL) return -2;
+  static ContextCache<int> setup;
+  int unused = 0;
+  const int rc = setup.get(&unused, [&](int&) {
+    const auto limit = [](auto fn, size_t smem) {
+      return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+    };
+    for (int c = 0; c < 2; ++c) {
+      for (int m = 0; m < 2; ++m)
+        if (!limit(kRowsKernels[m][c], kRowsSmemBytes[m])) return -3;
+      if (!limit(kPairKernels[c], kPairSmemBytes)) return -3;
+    }
+    return 0;
+  });
+  if (rc != 0) return rc;
+  CUtensorMap tq{}, tk{}, tv{};
+  const uint32_t box = static_cast<uint32_t>(std::min(a.page, kBN));
+  if (!make_bf16_map_4d(&tq, a.q, kD, static_cast<uint64_t>(rows), 1, 1, few ? width : kBM) ||
+      !make_bf16_map_4d(&tk, a.k_pages, kD, a.page, a.Hkv, a.n_pages, box) || !make_bf16_map_4d(&tv, a.v_pages, kD, a.page, a.Hkv, a.n_pages, box))
+    return -3;
+  const float log2e = 1.4426950408889634f, root = sqrtf(static_cast<float>(kD));
+  const bool cap = a.softcap > 0.0f;
+  const float softcap = fminf(fmaxf(a.softcap, kMinCap), kMaxCap);
   Params p{};
   p.q = static_cast<const bf16*>(a.q);
-  p.k_pages = static_cast<const bf16*>(a.k_pages);
-  p.v_pages = static_cast<const bf16*>(a.v_pages);
   p.table = a.table;
   p.lens = a.lens;
   p.k_seedmask = static_cast<const bf16*>(a.k_seedmask);
@@ -131,19 +1440,36 @@ int launch_attn_paged(const AttnPagedArgs& a, int*, cudaStream_t stream) {
   p.key_hi = a.key_hi;
   p.out = static_cast<bf16*>(a.out);
   p.lse = a.lse;
+  const size_t parts = part_rows(plan, a.B, a.Hq, a.Lq);
+  p.part_o = static_cast<float*>(a.workspace);
+  p.part_ml = reinterpret_cast<float2*>(p.part_o + parts * kD);
+  p.joins = reinterpret_cast<int4*>(p.part_ml + parts);
+  p.status = status;
+  p.rows = rows;
   p.n_pages = a.n_pages;
   p.M = a.M;
   while ((1 << p.page_log2) < a.page) ++p.page_log2;
+  p.B = a.B;
   p.n_seeds = a.n_seeds;
   p.Hq = a.Hq;
   p.Hkv = a.Hkv;
   p.G = a.Hq / a.Hkv;
   p.Lq = a.Lq;
-  p.scale = 1.0f / sqrtf(static_cast<float>(kD));
-  p.cap = a.softcap;
+  p.n_groups = plan.n_groups;
+  p.nsplit = plan.nsplit;
+  p.scale_log2 = log2e / root;
+  p.cap_log2 = softcap * log2e;
+  p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(rows)), dim3(kD), 0, stream, attr);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, attn_paged_row_kernel, p);
+  const int m = plan.mode == kRows16 ? 0 : 1;
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(few ? kRowsThreads : kPairsThreads),
+                                      few ? kRowsSmemBytes[m] : kPairSmemBytes, stream, attr);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, few ? kRowsKernels[m][cap ? 1 : 0] : kPairKernels[cap ? 1 : 0], tq, tk, tv, p);
+  if (e == cudaSuccess && parts > 0) {
+    const dim3 join_grid = few ? dim3(width / kJoinWarps, plan.ctas) : dim3(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps));
+    cfg = pdl_config(join_grid, dim3(kJoinWarps * 32), 0, stream, attr);
+    e = cudaLaunchKernelEx(&cfg, few ? (m == 0 ? attn_paged_join_rows_kernel<16> : attn_paged_join_rows_kernel<32>) : attn_paged_join_pairs_kernel, p);
+  }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
