@@ -131,6 +131,21 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8,
 int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int ranges, int32_t* choice, double* us);
 
 /*
+ * cover_attn_fwd_paged on a kernel of the caller's choice, whatever the call itself would take. mode 0, 1: rows of a KV head in
+ * groups of 16 or 32 on `parts` CTAs (1 .. 1024), each with an even share of the KV tiles; 2: pairs of Q tiles of 128 rows, the
+ * keys in `parts` parts (1 .. 64); COVER_ERR_UNSUPPORTED otherwise. workspace_bytes: of the workspace; what is needed: modes 0, 1
+ * parts (2 w 520 + 16), w = 16 or 32; mode 2 with parts > 1 B Hq Lq parts 520; COVER_ERR_INVALID_ARG if there is less. Otherwise as
+ * cover_attn_fwd_paged.
+ */
+int cover_debug_attn_paged(const void* q, const void* k_pages, const void* v_pages,
+                           const int32_t* table, int n_pages, int M, int page, const int32_t* lens,
+                           const void* k_seedmask, const void* v_seedmask, const int32_t* seed_idx, int n_seeds,
+                           const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
+                           const int32_t* key_lo, const int32_t* key_hi, float softcap,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes,
+                           int mode, int parts, void* stream);
+
+/*
  * Like cover_device_status, and also returns where the failure came from:
  * synchronises `stream`, copies the current device's status block to the
  * host array detail[3] = {status code, site id, linear block id} (all 0 when
@@ -139,7 +154,8 @@ int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int pl
  * thread, 30 / 31 softmax warpgroup of Q tile 0 / 1, 40 routing warp,
  * 50 / 51 seed-score warp; of the packed window kernel: 60 TMA / MMA thread,
  * 61 softmax warps, 62 combine (receive barrier), 63 copy issue; of the 8-bit memory's kernels:
- * 70, 76 copies, 71, 74, 77 MMA thread, 72 decoding or screening warps, 73, 75, 78 softmax warps.
+ * 70, 76 copies, 71, 74, 77 MMA thread, 72 decoding or screening warps, 73, 75, 78 softmax warps; of the paged
+ * memory's kernels: 80 planning warp, 81, 86 copies, 82, 85 MMA thread, 83, 87 screening warps, 84, 88 softmax warps.
  */
 int cover_debug_status_detail(int32_t* detail, void* stream);
 

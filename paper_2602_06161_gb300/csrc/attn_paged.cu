@@ -67,6 +67,7 @@ struct Params {
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
+  float cap_x;       // 1 / (cap sqrt(d))
 };
 
 // Keys of sequence b.
@@ -820,13 +821,32 @@ struct Unseen {
   bool any;
 };
 
-// Caps (to log2 units) and masks the scores of 32 columns from column c0 on.
-template <bool kCap>
-__device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, const Unseen& u, int c0) {
-  if (kCap) {
+// Caps the scores of 32 columns (to log2 units): those of a chunk that are all within the polynomial's range take it alone. With three
+// special-function operations a score a KV tile took 3.2 us of them.
+__device__ __forceinline__ void cap_scores(float (&s)[32], const Params& p, bool valid) {
+  float hi[2] = {};
 #pragma unroll
-    for (int c = 0; c < 32; ++c) s[c] = capped(s[c], p.cap_in, p.cap_log2);
+  for (int c = 0; c < 32; c += 4) {
+    hi[0] = fmax3(hi[0], fabsf(s[c]), fabsf(s[c + 1]));
+    hi[1] = fmax3(hi[1], fabsf(s[c + 2]), fabsf(s[c + 3]));
   }
+  if (__all_sync(0xffffffffu, !valid || fmaxf(hi[0], hi[1]) * p.cap_x <= kTanhRange)) {
+    // C x P(x^2), x = s cap_x (a NaN among the scores stays one)
+    const uint64_t cx = f2_pack(p.cap_x, p.cap_x), c = f2_pack(p.cap_log2, p.cap_log2), t0 = f2_pack(kTanh0, kTanh0),
+                   t1 = f2_pack(kTanh1, kTanh1), t2 = f2_pack(kTanh2, kTanh2), t3 = f2_pack(kTanh3, kTanh3);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      const uint64_t x = f2_mul(f2_pack(s[e], s[e + 1]), cx), z = f2_mul(x, x);
+      f2_unpack(f2_mul(f2_mul(x, c), f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0)), s[e], s[e + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = capped(s[e], p.cap_in, p.cap_log2);
+  }
+}
+
+// Masks the scores of 32 columns from column c0 on.
+__device__ __forceinline__ void mask_scores(float (&s)[32], const Unseen& u, int c0) {
   if (u.any) {
     const int lo = u.lo - c0, hi = u.hi - c0, own = u.own - c0;
 #pragma unroll
@@ -844,24 +864,26 @@ __device__ __forceinline__ void finish_scores(float (&s)[32], const Params& p, c
 }
 
 // The largest of 32 columns' scores, neither scaled nor capped yet.
-__device__ __forceinline__ float chunk_max(uint32_t addr, const Params& p, const Unseen& u, int c0) {
+__device__ __forceinline__ float chunk_max(uint32_t addr, const Unseen& u, int c0) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
   float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
-  finish_scores<false>(s, p, u, c0);
+  mask_scores(s, u, c0);
   return max32(s);
 }
 
 // P = 2^(score - m) of 32 columns to tensor memory, in bf16 (V's operands are, so P's have to be: a weight is off by at most 2^-8 of itself).
 // Returns the sum of the unrounded weights.
 template <bool kCap>
-__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m) {
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m,
+                                           bool valid) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
   float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
-  finish_scores<kCap>(s, p, u, c0);
+  if (kCap) cap_scores(s, p, valid);
+  mask_scores(s, u, c0);
   const float scale = kCap ? 1.0f : p.scale_log2;
   const uint64_t negm2 = f2_pack(-m, -m), scale2 = f2_pack(scale, scale);
   uint64_t acc2[2] = {0, 0};
@@ -1195,7 +1217,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       float m_half = -INFINITY;
       if (ok && some) {
 #pragma unroll 1
-        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, p, u, c));
+        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, u, c));
         m_half = !kCap ? m_half * p.scale_log2 : m_half == -INFINITY ? m_half : capped(m_half, p.cap_in, p.cap_log2);   // (the cap is monotonous)
       }
       // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row
@@ -1231,7 +1253,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       if (some) {
         const float m_use = (m_run == -INFINITY) ? 0.0f : m_run;
 #pragma unroll 1
-        for (int c = 0; c < kHalf; c += 32) l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, c, m_use);
+        for (int c = 0; c < kHalf; c += 32) l_run += chunk_exp<kCap>(s_addr + c, s_addr + c / 2, p, u, c, m_use, valid);
       } else if (warp_live) {
         const uint32_t zeros[16] = {};
         tmem_st16(s_addr, zeros);
@@ -1391,16 +1413,29 @@ size_t part_rows(const Plan& plan, int B, int Hq, int Lq) {
   return plan.nsplit > 1 ? static_cast<size_t>(B) * Hq * Lq * plan.nsplit : 0;
 }
 
+// The plan of a debug call.
+Plan forced(int Hq, int Hkv, int Lq, int mode, int parts) {
+  const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
+  const int width = mode == kPairs ? 2 * kBM : mode == kRows16 ? 16 : 32;
+  return Plan{static_cast<Mode>(mode), static_cast<int>((packed + width - 1) / width), mode == kPairs ? parts : 1, mode == kPairs ? 0 : parts};
+}
+
+size_t plan_bytes(const Plan& plan, int B, int Hq, int Lq) {
+  return part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2)) + (plan.mode != kPairs ? plan.ctas * sizeof(int4) : 0);
+}
+
 }  // namespace
 
 size_t attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page) {
-  const Plan plan = plan_of(B, Hq, Hkv, Lq, M, page);
-  return part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2)) + (plan.mode != kPairs ? plan.ctas * sizeof(int4) : 0);
+  return plan_bytes(plan_of(B, Hq, Hkv, Lq, M, page), B, Hq, Lq);
+}
+size_t attn_paged_mode_bytes(int B, int Hq, int Hkv, int Lq, int mode, int parts) {
+  return plan_bytes(forced(Hq, Hkv, Lq, mode, parts), B, Hq, Lq);
 }
 
 int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) {
   using bf16 = __nv_bfloat16;
-  const Plan plan = plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.M, a.page);
+  const Plan plan = a.mode >= 0 ? forced(a.Hq, a.Hkv, a.Lq, a.mode, a.parts) : plan_of(a.B, a.Hq, a.Hkv, a.Lq, a.M, a.page);
   const bool few = plan.mode != kPairs;
   const int width = plan.mode == kRows16 ? 16 : 32;
   const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
@@ -1460,6 +1495,7 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   p.scale_log2 = log2e / root;
   p.cap_log2 = softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
+  p.cap_x = cap ? 1.0f / (softcap * root) : 0.0f;
   cudaLaunchAttribute attr[1];
   const int m = plan.mode == kRows16 ? 0 : 1;
   cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(few ? kRowsThreads : kPairsThreads),

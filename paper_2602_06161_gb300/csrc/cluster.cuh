@@ -21,6 +21,14 @@ __device__ __forceinline__ uint32_t cluster_map(uint32_t saddr, uint32_t rank) {
   return r;
 }
 
+// The address, as a generic one, of what p points to in this CTA's shared memory in that of the cluster's CTA `rank`.
+template <typename T>
+__device__ __forceinline__ const T* cluster_ptr(const T* p, uint32_t rank) {
+  uint64_t r;
+  asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+  return reinterpret_cast<const T*>(r);
+}
+
 // Bulk copy of `bytes` (a multiple of 16, both addresses 16-byte aligned) from this CTA's shared
 // memory into the shared memory of a CTA of the cluster, completing `bytes` transactions on
 // that CTA's mbarrier (cluster addresses from cluster_map).

@@ -336,30 +336,36 @@ size_t cover_attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, i
   return cover::attn_paged_workspace_bytes(B, Hq, Hkv, Lq, M, page);
 }
 
+static int attn_paged_call(const cover::AttnPagedArgs& a, int D, size_t workspace_bytes, void* stream) {
+  if (a.q == nullptr || a.lens == nullptr || a.out == nullptr) return COVER_ERR_INVALID_ARG;
+  if (a.B < 1 || a.Hq < 1 || a.Hkv < 1 || a.Lq < 1 || D < 1 || a.Hq % a.Hkv != 0 || a.n_seeds < 0) return COVER_ERR_INVALID_ARG;
+  if (a.n_seeds > 0 && (a.k_seedmask == nullptr || a.v_seedmask == nullptr || a.seed_idx == nullptr || a.q0 == nullptr))
+    return COVER_ERR_INVALID_ARG;
+  if (!aligned(a.q, 16) || !aligned(a.out, 16) || !aligned(a.workspace, 16) || !aligned(a.lens, 4) || !aligned(a.lse, 4) ||
+      !aligned(a.key_lo, 4) || !aligned(a.key_hi, 4))
+    return COVER_ERR_INVALID_ARG;
+  if (a.n_seeds > 0 && (!aligned(a.k_seedmask, 16) || !aligned(a.v_seedmask, 16) || !aligned(a.seed_idx, 4) || !aligned(a.q0, 4)))
+    return COVER_ERR_INVALID_ARG;
+  if (!(a.softcap >= 0.0f) || a.softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
+  const int rc = check_pages(a.k_pages, a.v_pages, a.table, a.n_pages, a.M, a.page);
+  if (rc != COVER_OK) return rc;
+  if (D != 128 || static_cast<long long>(a.B) * a.Hq > 0x7fffff00LL / a.Lq) return COVER_ERR_UNSUPPORTED;
+  const size_t need = a.mode >= 0 ? cover::attn_paged_mode_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.mode, a.parts)
+                                  : cover::attn_paged_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.M, a.page);
+  if (need > 0 && (a.workspace == nullptr || workspace_bytes < need)) return COVER_ERR_INVALID_ARG;
+  int* st = status_block();
+  if (st == nullptr) return COVER_ERR_CUDA;
+  return cover::launch_attn_paged(a, st, static_cast<cudaStream_t>(stream));
+}
+
 int cover_attn_fwd_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* table, int n_pages,
                          int M, int page, const int32_t* lens, const void* k_seedmask, const void* v_seedmask,
                          const int32_t* seed_idx, int n_seeds, const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
                          const int32_t* key_lo, const int32_t* key_hi, float softcap, void* out, float* lse,
                          void* workspace, void* stream) {
-  if (q == nullptr || lens == nullptr || out == nullptr) return COVER_ERR_INVALID_ARG;
-  if (B < 1 || Hq < 1 || Hkv < 1 || Lq < 1 || D < 1 || Hq % Hkv != 0 || n_seeds < 0) return COVER_ERR_INVALID_ARG;
-  if (n_seeds > 0 && (k_seedmask == nullptr || v_seedmask == nullptr || seed_idx == nullptr || q0 == nullptr))
-    return COVER_ERR_INVALID_ARG;
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(lens, 4) || !aligned(lse, 4) ||
-      !aligned(key_lo, 4) || !aligned(key_hi, 4))
-    return COVER_ERR_INVALID_ARG;
-  if (n_seeds > 0 && (!aligned(k_seedmask, 16) || !aligned(v_seedmask, 16) || !aligned(seed_idx, 4) || !aligned(q0, 4)))
-    return COVER_ERR_INVALID_ARG;
-  if (!(softcap >= 0.0f) || softcap > 3.0e38f) return COVER_ERR_INVALID_ARG;
-  const int rc = check_pages(k_pages, v_pages, table, n_pages, M, page);
-  if (rc != COVER_OK) return rc;
-  if (D != 128 || static_cast<long long>(B) * Hq > 0x7fffff00LL / Lq) return COVER_ERR_UNSUPPORTED;
-  if (workspace == nullptr && cover::attn_paged_workspace_bytes(B, Hq, Hkv, Lq, M, page) > 0) return COVER_ERR_INVALID_ARG;
-  int* st = status_block();
-  if (st == nullptr) return COVER_ERR_CUDA;
   const cover::AttnPagedArgs a{q,        k_pages, v_pages, table, n_pages, M,   page, lens,   k_seedmask, v_seedmask, seed_idx,
                                n_seeds,  q0,      B,       Hq,    Hkv,     Lq,  key_lo, key_hi, softcap,    out,        lse, workspace};
-  return cover::launch_attn_paged(a, st, static_cast<cudaStream_t>(stream));
+  return attn_paged_call(a, D, ~size_t{0}, stream);
 }
 
 static int check_logits(const void* logits, int N, int V, int elem_bytes, int topk) {
@@ -609,6 +615,20 @@ int cover_debug_attn_prefix8(const void* q, const void* k8, const void* v8, cons
   a.mode = mode;
   a.parts = nsplit;
   return attn_prefix8_call(a, D, workspace_bytes, stream);
+}
+
+int cover_debug_attn_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* table, int n_pages,
+                           int M, int page, const int32_t* lens, const void* k_seedmask, const void* v_seedmask,
+                           const int32_t* seed_idx, int n_seeds, const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
+                           const int32_t* key_lo, const int32_t* key_hi, float softcap, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, int mode, int parts, void* stream) {
+  if (mode < 0 || mode >= cover::kAttnPagedModes || parts < 1 || parts > (mode == cover::kAttnPagedModes - 1 ? 64 : 1024))
+    return COVER_ERR_UNSUPPORTED;
+  cover::AttnPagedArgs a{q,        k_pages, v_pages, table, n_pages, M,   page, lens,   k_seedmask, v_seedmask, seed_idx,
+                         n_seeds,  q0,      B,       Hq,    Hkv,     Lq,  key_lo, key_hi, softcap,    out,        lse, workspace};
+  a.mode = mode;
+  a.parts = parts;
+  return attn_paged_call(a, D, workspace_bytes, stream);
 }
 
 int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int plain, int ranges, int32_t* choice,

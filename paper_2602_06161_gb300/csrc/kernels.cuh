@@ -247,8 +247,11 @@ struct AttnPagedArgs {
   void* out;
   float* lse;
   void* workspace;
+  int mode = -1, parts = 0;   // debug calls: the kernel and the parts of the keys (pairs) or the CTAs (rows), whatever the plan says
 };
+constexpr int kAttnPagedModes = 3;   // attn_paged.cu's Mode
 size_t attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page);
+size_t attn_paged_mode_bytes(int B, int Hq, int Hkv, int Lq, int mode, int parts);
 int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream);
 
 // Log probabilities of given tokens and their gradient (logprob_kernel.cu). tok may be null (logp too), and of the

@@ -147,37 +147,50 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) paged_append
     for (int j = 0; j < kHeadsInFlight; ++j) {
       if (i0 + j >= n) break;
       const int h = c + (i0 + j) * step;
-      float y[2][N];
+      if constexpr (sizeof(T) == 2) {
+        // pages and outputs are of one type: a vector is turned where it is
+        if (turn) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        y[0][e] = to_f(x[j][0].v[e]);
-        y[1][e] = kVecs == 2 && turn_unit ? to_f(x[j][1].v[e]) : 0.0f;
-      }
-      if (turn) {
-#pragma unroll
-        for (int k = 0; k < kHalf; ++k) {
-          float& a = kVecs == 1 ? y[0][(2 * k) % N] : y[0][k % N];
-          float& d = kVecs == 1 ? y[0][(2 * k + 1) % N] : y[1][k % N];
-          const float a0 = a, d0 = d;
-          a = a0 * cs[k] - d0 * sn[k];
-          d = a0 * sn[k] + d0 * cs[k];
+          for (int k = 0; k < kHalf; ++k) {
+            T& xa = kVecs == 1 ? x[j][0].v[(2 * k) % N] : x[j][0].v[k % N];
+            T& xb = kVecs == 1 ? x[j][0].v[(2 * k + 1) % N] : x[j][1].v[k % N];
+            const float a = to_f(xa), d = to_f(xb);
+            xa = from_f<T>(a * cs[k] - d * sn[k]);
+            xb = from_f<T>(a * sn[k] + d * cs[k]);
+          }
         }
-      }
-#pragma unroll
-      for (int w = 0; w < kVecs; ++w) {
-        if (w == 1 && !turn_unit) break;
-        const int col = w ? col1 : col0;
         if (out != nullptr) {
-          V r;
-#pragma unroll
-          for (int e = 0; e < N; ++e) r.v[e] = from_f<T>(y[w][e]);
-          *reinterpret_cast<V*>(out + static_cast<size_t>(h) * p.n * p.D + col) = r;
+          T* row = out + static_cast<size_t>(h) * p.n * p.D;
+          *reinterpret_cast<V*>(row + col0) = x[j][0];
+          if (kVecs == 2 && turn_unit) *reinterpret_cast<V*>(row + col1) = x[j][1];
         }
         if (place >= 0) {
-          Vec<bf16, N> r;
+          T* row = reinterpret_cast<T*>(t.pages) + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D;
+          *reinterpret_cast<V*>(row + col0) = x[j][0];
+          if (kVecs == 2 && turn_unit) *reinterpret_cast<V*>(row + col1) = x[j][1];
+        }
+      } else {
+        if (turn) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) r.v[e] = from_f<bf16>(y[w][e]);
-          *reinterpret_cast<Vec<bf16, N>*>(t.pages + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D + col) = r;
+          for (int k = 0; k < kHalf; ++k) {
+            T& xa = kVecs == 1 ? x[j][0].v[(2 * k) % N] : x[j][0].v[k % N];
+            T& xb = kVecs == 1 ? x[j][0].v[(2 * k + 1) % N] : x[j][1].v[k % N];
+            const float a = to_f(xa), d = to_f(xb);
+            xa = from_f<T>(a * cs[k] - d * sn[k]);
+            xb = from_f<T>(a * sn[k] + d * cs[k]);
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < kVecs; ++w) {
+          if (w == 1 && !turn_unit) break;
+          const int col = w ? col1 : col0;
+          if (out != nullptr) *reinterpret_cast<V*>(out + static_cast<size_t>(h) * p.n * p.D + col) = x[j][w];
+          if (place >= 0) {
+            Vec<bf16, N> r;
+#pragma unroll
+            for (int e = 0; e < N; ++e) r.v[e] = from_f<bf16>(to_f(x[j][w].v[e]));
+            *reinterpret_cast<Vec<bf16, N>*>(t.pages + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D + col) = r;
+          }
         }
       }
     }
