@@ -155,7 +155,8 @@ int cover_debug_attn_paged(const void* q, const void* k_pages, const void* v_pag
  * 50 / 51 seed-score warp; of the packed window kernel: 60 TMA / MMA thread,
  * 61 softmax warps, 62 combine (receive barrier), 63 copy issue; of the 8-bit memory's kernels:
  * 70, 76 copies, 71, 74, 77 MMA thread, 72 decoding or screening warps, 73, 75, 78 softmax warps; of the paged
- * memory's kernels: 80 planning warp, 81, 86 copies, 82, 85 MMA thread, 83, 87 screening warps, 84, 88 softmax warps.
+ * memory's kernels: 80 planning warp, 81, 86 copies, 82, 85 MMA thread, 83, 87 screening warps, 84, 88 softmax warps; of the
+ * log probabilities' kernel: 90 copies, 91 adding warps, 92 finishing warp.
  */
 int cover_debug_status_detail(int32_t* detail, void* stream);
 

@@ -388,7 +388,9 @@ int cover_logprob_fwd(const void* logits, int N, int V, int elem_bytes, const in
   if (topk > cover::kMaxTopLogprob) return COVER_ERR_UNSUPPORTED;
   if (N == 0) return COVER_OK;
   const cover::LogprobArgs a{logits, N, V, elem_bytes, tok, topk, tok == nullptr ? nullptr : logp, entropy, lse, top_idx, top_logp};
-  return cover::launch_logprob_fwd(a, static_cast<cudaStream_t>(stream));
+  int* st = status_block();
+  if (st == nullptr) return COVER_ERR_CUDA;
+  return cover::launch_logprob_fwd(a, st, static_cast<cudaStream_t>(stream));
 }
 
 int cover_logprob_bwd(const void* logits, int N, int V, int elem_bytes, const float* lse, const int32_t* tok,

@@ -268,7 +268,7 @@ struct LogprobArgs {
   int32_t* top_idx;
   float* top_logp;
 };
-int launch_logprob_fwd(const LogprobArgs& a, cudaStream_t stream);
+int launch_logprob_fwd(const LogprobArgs& a, int* status, cudaStream_t stream);
 struct LogprobGradArgs {
   const void* logits;
   int N, V, elem_bytes;

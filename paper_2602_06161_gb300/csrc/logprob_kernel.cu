@@ -16,19 +16,24 @@
 // by more than kSlack. Logits far below it, -inf among them, are raised to where their weight still is 0 (0 * -inf would be NaN).
 // References beyond 2^20, where that correction is no small one, and infinities are left to a second, careful walk.
 //
-// The K best. Thread t of a CTA keeps the best of its vectors (every 256th) as (largest element, vector). The K-th best of the
-// threads' pairs is behind or among the K best vectors, so every one of the K best elements lies in a vector whose pair
-// is not behind it, and those are among the K threads in front: their vectors are read again (they are in L2), and the elements that
-// are not behind the bound are ranked by counting. What passes the bound is little more than K, whatever ties there are (a row
-// of equal logits: the first K vectors). A row whose K best crowd in a few threads may pass more than kMaxFound: then
-// the K best are taken one after the other, a walk over the row each.
+// The K best. A thread keeps the best of its vectors (every 192nd) as (largest element, vector), and the largest element of the others.
+// The K-th best of the threads' pairs is a bound: every one of the K best elements lies in a vector whose pair is not behind it,
+// and those are among the K threads in front. Their vectors are read again, the best one alone where the others' largest element is
+// behind the bound, and the elements that are not behind it are ranked by counting. What passes the bound is little more than K, whatever
+// ties there are (a row of equal logits: the first K vectors). A row whose K best crowd in a few threads may pass more than
+// kMaxFound: then the K best are taken one after the other, a walk over the row each.
 //
-// Few rows are split over the CTAs of a cluster, whose sums and K best its first CTA puts together.
+// Bound by memory, and not far from it by the special-function units (an exponential an element: 56 us of the 76 that reading 2048 x
+// 126464 bf16 takes). A CTA's warps have parts: six add up; one keeps a ring of three 12 KB pieces of the row's whole vectors filled by
+// bulk copies, and runs on into the CTA's next row; one puts a row's sums and K best together while the others are at the next row
+// (together with them that took 17 us of 113 for 8 alternatives, 35 for 20). Four CTAs share an SM. Vectors at the row's ends are loaded by
+// two threads. Few rows are split over the CTAs of a cluster, whose sums and K best its first CTA puts together.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cluster.cuh"
 #include "kernels.cuh"
@@ -38,12 +43,14 @@ namespace cover {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kMaxFound = 1024;        // elements ranked at once
+constexpr int kMaxFound = 768;         // elements ranked at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -1000.0f;     // log2 units: 2^kFloor is 0, and 0 * kFloor too (0 * -inf is not)
 constexpr float kSlack = 6.0f;         // the reference follows maxima that are above it by more
 constexpr int kMaxParts = 8;           // of a row: CTAs of a cluster
+// the forward kernel's warps: those that add up, one that copies, one that finishes rows
+constexpr int kAddWarps = 6, kCopyWarp = 6, kAdders = 32 * kAddWarps, kFwdThreads = kAdders + 64;
+constexpr int kEach = 4, kPiece = kEach * kAdders, kStages = 3;   // vectors of a thread, of a piece; pieces in flight
 
 // Elements of a 16-byte vector in fp32.
 template <typename T>
@@ -149,10 +156,20 @@ struct Row {
     whole1 = static_cast<int>((static_cast<long long>(V) + skip) / N);
   }
   __device__ __forceinline__ bool whole(int i) const { return i >= whole0 && i < whole1; }
+  // the whole vectors x .. y - 1 of one of `parts` parts
+  __device__ __forceinline__ int2 part(int i, int parts) const {
+    const int each = (n_vecs + parts - 1) / parts, v0 = min(i * each, n_vecs), v1 = min(v0 + each, n_vecs), w0 = max(v0, whole0);
+    return make_int2(w0, max(w0, min(v1, whole1)));
+  }
   // whether element e of vector i is in the row
   __device__ __forceinline__ bool has(int i, int e) const {
     const long long j = static_cast<long long>(i) * Vec16<T>::kN + e - skip;
     return j >= 0 && j < V;
+  }
+  // whether vector i, the row's first (side 0) or last, is one of the part's and not whole
+  __device__ __forceinline__ bool is_end(int i, int side, int k, int parts) const {
+    const int each = (n_vecs + parts - 1) / parts, v0 = min(k * each, n_vecs), v1 = min(v0 + each, n_vecs);
+    return i >= v0 && i < v1 && !whole(i) && (side == 0 || i > 0);
   }
   // a vector at the row's ends, -inf in the places of other rows
   __device__ __forceinline__ uint4 load_end(int i) const {
@@ -183,6 +200,15 @@ __device__ __forceinline__ Sums merge(Sums a, Sums b) {
   return Sums{to, a.s + b.s, a.w + b.w};
 }
 
+__device__ __forceinline__ bool warp_wait_all(uint64_t* bar, uint32_t parity, const volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
 struct FwdParams {
   const void* logits;
   const int32_t* tok;
@@ -191,292 +217,440 @@ struct FwdParams {
   float* lse;
   int32_t* top_idx;
   float* top_logp;
-  int V, topk, parts;
+  int* status;
+  int N, V, topk, parts;
 };
 
-// A thread's sums over vectors i, i + kThreads, .. below end, for logits of any size.
+// A thread's sums for logits of any size: over whole vectors w0 + tid, w0 + tid + kAdders, .. below w1, and one at the row's ends.
 template <typename T>
-__device__ __noinline__ Sums careful_sums(const Row<T>& row, int i, int end) {
+__device__ __noinline__ Sums careful_sums(const Row<T>& row, int w0, int w1, bool has_end, uint4 end_raw) {
   constexpr int N = Vec16<T>::kN;
   Sums a{-INFINITY, 0.0f, 0.0f};
-  for (int k = i; k < end; k += kThreads) a.m = fmaxf(a.m, Vec16<T>::top(row.load(k)));
-  for (int k = i; k < end; k += kThreads) {
+  const auto add = [&](const uint4& raw) {
     float x[N];
-    Vec16<T>::unpack(row.load(k), x);
+    Vec16<T>::unpack(raw, x);
+#pragma unroll
     for (int e = 0; e < N; ++e) {
       if (x[e] == -INFINITY) continue;
       const float t = max_nan((x[e] - a.m) * kLog2e, kFloor), f = ex2_approx(t);
       a.s += f;
       a.w = fmaf(f, t, a.w);
     }
-  }
+  };
+  for (int k = w0 + threadIdx.x; k < w1; k += kAdders) a.m = fmaxf(a.m, Vec16<T>::top(__ldg(row.base + k)));
+  if (has_end) a.m = fmaxf(a.m, Vec16<T>::top(end_raw));
+  for (int k = w0 + threadIdx.x; k < w1; k += kAdders) add(__ldg(row.base + k));
+  if (has_end) add(end_raw);
   return a;
 }
 
+// A row's sums and pairs, from the adding warps to the finishing one.
+template <bool kTop>
+struct Handover {
+  Sums sums[kAddWarps];
+  unsigned long long pairs[kTop ? kAdders : 1];
+  float others[kTop ? kAdders : 1];   // the largest element of a thread's other vectors
+};
+
+template <bool kTop>
+struct FwdShared {
+  uint64_t full[kStages], empty[kStages], done[2], taken[2];
+  Handover<kTop> row[2];
+  Sums part;                          // the finishing warp's, read by the cluster's first CTA
+  unsigned long long best[kTop ? kMaxTopLogprob : 1];
+  unsigned long long found[kTop ? kMaxFound : 1];
+  int who[kTop ? kMaxTopLogprob : 1];
+  int n_found, abort;
+};
+
+// The K best of sorted lists, one a lane (`next(i)`: its i-th key, 0 behind the end), in order: take(k, key) by all lanes. Returns the last.
+template <typename Next, typename Take>
+__device__ __forceinline__ unsigned long long merge_best(int K, Next&& next, Take&& take) {
+  int at = 0;
+  unsigned long long mine = next(0), last = 0;
+  for (int k = 0; k < K; ++k) {
+    const uint32_t hi = static_cast<uint32_t>(mine >> 32), top = __reduce_max_sync(0xffffffffu, hi);
+    const uint32_t low = __reduce_max_sync(0xffffffffu, hi == top ? static_cast<uint32_t>(mine) : 0u);
+    last = (static_cast<unsigned long long>(top) << 32) | low;
+    take(k, last);
+    if (mine == last && last != 0) mine = next(++at);
+  }
+  return last;
+}
+
 template <typename T, bool kTop>
-__global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const __grid_constant__ FwdParams p) {
+__global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __grid_constant__ FwdParams p) {
   using V16 = Vec16<T>;
-  constexpr int N = V16::kN, kInFlight = 4;
-  __shared__ Sums s_sums[kWarps], s_part;
-  __shared__ unsigned long long s_groups[kTop ? kThreads : 1], s_found[kTop ? kMaxFound : 1], s_best[kTop ? kMaxTopLogprob : 1];
-  __shared__ unsigned long long s_bound;
-  __shared__ int s_who[kTop ? kMaxTopLogprob : 1], s_n_found;
-  __shared__ float2 s_row;   // m and ln s of the whole row
-  griddep_wait();
-  griddep_launch_dependents();
+  constexpr int N = V16::kN;
+  extern __shared__ uint4 ring[];   // [kStages][kPiece]
+  __shared__ FwdShared<kTop> sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int part = p.parts > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const long long r = blockIdx.x / p.parts;
-  const Row<T> row(static_cast<const T*>(p.logits), r, p.V);
-  const int each = (row.n_vecs + p.parts - 1) / p.parts;
-  const int v0 = min(part * each, row.n_vecs), v1 = min(v0 + each, row.n_vecs);
-  float x_tok = 0.0f;
-  bool has_tok = false;
-  if (tid == 0 && part == 0 && p.tok != nullptr) {
-    const int y = __ldg(p.tok + r);
-    has_tok = y >= 0 && y < p.V;
-    if (has_tok) x_tok = V16::value(static_cast<const T*>(p.logits)[r * p.V + y]);
-  }
-  if constexpr (kTop) {
-    if (tid == 0) s_n_found = 0;
-    if (tid < kMaxTopLogprob) s_best[tid] = 0;   // (NaN may leave places empty)
-  }
-
-  // ---------------- sums, and each thread's best vector ----------------
-  Sums a{-INFINITY, 0.0f, 0.0f};
-  bool careful = false;
-  {
-    constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf
-    float c = -INFINITY;
-    uint32_t floor = kNone;
-    uint64_t s2[2] = {0, 0}, w2[2] = {0, 0};
-    float best = 0.0f;
-    int best_vec = -1;
-    for (int i0 = v0 + tid; i0 < v1; i0 += kThreads * kInFlight) {
-      uint4 raw[kInFlight];
-#pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const int i = i0 + k * kThreads;
-        raw[k] = i < v1 ? row.load(i) : make_uint4(kNone, kNone, kNone, kNone);
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        const float t = V16::top(raw[k]);
-        const int i = i0 + k * kThreads;
-        if (kTop && (t > best || best_vec < 0) && i < v1) best = t, best_vec = i;
-        top = fmaxf(top, t);
-      }
-      if (top > a.m + kSlack) {
-        careful |= fabsf(top) > 1048576.0f;
-        const float to = top * kLog2e, d = fmaxf(c - to, kFloor), f = ex2_approx(d);
-        const uint64_t f2 = f2_pack(f, f), d2 = f2_pack(d, d);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          w2[e] = f2_mul(f2_fma(s2[e], d2, w2[e]), f2);
-          s2[e] = f2_mul(s2[e], f2);
-        }
-        a.m = top;
-        c = to;
-        floor = V16::floor_of(top - 800.0f);
-      }
-      if (a.m == -INFINITY) {   // nothing but -inf, or NaN, so far
-#pragma unroll
-        for (int k = 0; k < kInFlight; ++k) {
-          float x[N];
-          V16::unpack(raw[k], x);
-#pragma unroll
-          for (int e = 0; e < N; ++e) careful |= x[e] != x[e];
-        }
-        continue;
-      }
-      const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
-#pragma unroll
-      for (int k = 0; k < kInFlight; ++k) {
-        float x[N];
-        V16::unpack(V16::raise(raw[k], floor), x);
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const uint64_t t2 = f2_fma(f2_pack(x[e], x[e + 1]), l2, c2);
-          float t0, t1;
-          f2_unpack(t2, t0, t1);
-          const uint64_t e2 = f2_pack(ex2_approx(t0), ex2_approx(t1));
-          s2[(e >> 1) & 1] = f2_add(s2[(e >> 1) & 1], e2);
-          w2[(e >> 1) & 1] = f2_fma(e2, t2, w2[(e >> 1) & 1]);
-        }
-      }
-    }
-    if (careful) {
-      a = careful_sums(row, v0 + tid, v1);
-    } else if (a.m != -INFINITY) {
-      float x[4];
-      f2_unpack(f2_add(s2[0], s2[1]), x[0], x[1]);
-      f2_unpack(f2_add(w2[0], w2[1]), x[2], x[3]);
-      const float off = fmaf(a.m, kLog2e, -c), f = ex2_approx(-off);
-      a.s = (x[0] + x[1]) * f;
-      a.w = fmaf(-off, x[0] + x[1], x[2] + x[3]) * f;
-    }
-    if constexpr (kTop) s_groups[tid] = best_vec >= 0 ? key_of(best, static_cast<uint32_t>(best_vec)) : 0ull;
-  }
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1)
-    a = merge(a, Sums{__shfl_xor_sync(0xffffffffu, a.m, d), __shfl_xor_sync(0xffffffffu, a.s, d), __shfl_xor_sync(0xffffffffu, a.w, d)});
-  if (lane == 0) s_sums[warp] = a;
-  __syncthreads();
   if (tid == 0) {
-    Sums t = s_sums[0];
-    for (int i = 1; i < kWarps; ++i) t = merge(t, s_sums[i]);
-    s_part = t;
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], kAddWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.done[i], kAddWarps);
+      mbar_init(&sm.taken[i], 1);
+    }
+    sm.abort = 0;
+    fence_mbar_init();
   }
-  const int K = kTop ? min(p.topk, p.V) : 0;
-  if constexpr (kTop) {
-    // ---------------- the part's K best ----------------
-    if (warp == 0) {
-      // the K best pairs of the 256, a lane's eight in order first
-      constexpr int kEach = kThreads / 32;
-      unsigned long long mine[kEach];
-      int who[kEach];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        mine[i] = s_groups[32 * i + lane];
-        who[i] = 32 * i + lane;
-      }
-#pragma unroll
-      for (int i = 1; i < kEach; ++i)
-#pragma unroll
-        for (int j = i; j > 0; --j)
-          if (mine[j] > mine[j - 1]) {
-            const unsigned long long x = mine[j];
-            const int y = who[j];
-            mine[j] = mine[j - 1], who[j] = who[j - 1];
-            mine[j - 1] = x, who[j - 1] = y;
-          }
-      unsigned long long bound = 0;
-      for (int k = 0; k < K; ++k) {
-        const uint32_t hi = static_cast<uint32_t>(mine[0] >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-        const uint32_t low = __reduce_max_sync(0xffffffffu, hi == top ? static_cast<uint32_t>(mine[0]) : 0u);
-        bound = (static_cast<unsigned long long>(top) << 32) | low;
-        const bool first = bound != 0 && mine[0] == bound;   // (fewer threads than K have vectors: all elements are looked at)
-        if (lane == 0) s_who[k] = -1;
-        __syncwarp();
-        if (first) {
-          s_who[k] = who[0];
-#pragma unroll
-          for (int i = 0; i + 1 < kEach; ++i) mine[i] = mine[i + 1], who[i] = who[i + 1];
-          mine[kEach - 1] = 0;
-        }
-      }
-      if (lane == 0) s_bound = bound;
-    }
-    __syncthreads();
-    const unsigned long long bound = s_bound;
-    const int steps = (v1 - v0 + kThreads - 1) / kThreads;
-    for (int w = tid; w < K * steps; w += kThreads) {
-      const int i = v0 + s_who[w % K] + w / K * kThreads;
-      if (i < v0 || i >= v1) continue;
-      float x[N];
-      V16::unpack(row.load(i), x);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        if (key_of(x[e], static_cast<uint32_t>(i)) >= bound && row.has(i, e)) {
-          const int at = atomicAdd(&s_n_found, 1);
-          if (at < kMaxFound) s_found[at] = key_of(x[e], static_cast<uint32_t>(i * static_cast<long long>(N) + e - row.skip));
-        }
-      }
-    }
-    __syncthreads();
-    const int n = s_n_found;
-    if (n <= kMaxFound) {
-      for (int c = tid; c < n; c += kThreads) {
-        const unsigned long long key = s_found[c];
-        int rank = 0;
-        for (int o = 0; o < n; ++o) rank += s_found[o] > key ? 1 : 0;
-        if (rank < K) s_best[rank] = key;
-      }
-    } else {
-      unsigned long long last = ~0ull;
-      for (int k = 0; k < K; ++k) {
-        unsigned long long next = 0;
-        for (int i = v0 + tid; i < v1; i += kThreads) {
-          float x[N];
-          V16::unpack(row.load(i), x);
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const unsigned long long key = key_of(x[e], static_cast<uint32_t>(i * static_cast<long long>(N) + e - row.skip));
-            if (row.has(i, e) && key < last && key > next) next = key;
-          }
-        }
-        s_groups[tid] = next;
-        __syncthreads();
-        for (int d = kThreads / 2; d >= 1; d >>= 1) {
-          if (tid < d) s_groups[tid] = max(s_groups[tid], s_groups[tid + d]);
-          __syncthreads();
-        }
-        last = s_groups[0];
-        if (tid == 0) s_best[k] = last;
-        __syncthreads();
-      }
-    }
-    __syncthreads();
-  }
+  __syncthreads();
+  griddep_wait();
+  griddep_launch_dependents();
+  const int first_row = blockIdx.x / p.parts, row_step = p.parts > 1 ? p.N : static_cast<int>(gridDim.x);
 
-  // ---------------- the row's results ----------------
-  if (p.parts > 1) {
+  if (warp == kCopyWarp) {
+    // ---------------- copies ----------------
+    if (lane == 0) {
+      int piece = 0;
+      bool ok = true;
+      for (long long r = first_row; r < p.N && ok; r += row_step) {
+        const Row<T> row(static_cast<const T*>(p.logits), r, p.V);
+        const int2 w = row.part(part, p.parts);
+        for (int v = w.x; v < w.y && ok; v += kPiece, ++piece) {
+          const int st = piece % kStages;
+          if (piece >= kStages) ok = mbar_wait(&sm.empty[st], (piece / kStages - 1) & 1, &sm.abort);
+          if (!ok) break;
+          const uint32_t bytes = static_cast<uint32_t>(min(kPiece, w.y - v)) * 16;
+          mbar_arrive_expect_tx(&sm.full[st], bytes);
+          bulk_load(smem_u32(ring + st * kPiece), row.base + v, bytes, &sm.full[st]);
+        }
+      }
+      if (!ok) {
+        if (!sm.abort) report_status(p.status, kStatusTimeout, 90);
+        sm.abort = 1;
+      }
+      // every copy lands before the CTA's shared memory is released, whatever the other warps did
+      for (int f = max(0, piece - kStages); f < piece; ++f) mbar_wait(&sm.full[f % kStages], (f / kStages) & 1, nullptr);
+    }
     __syncwarp();
-    cluster_sync();   // every part's sums and best are there
-    if (part == 0) {
-      if (tid == 0) {
-        Sums t = s_part;
-        for (int c = 1; c < p.parts; ++c) t = merge(t, *cluster_ptr(&s_part, c));
-        s_part = t;
+  } else if (warp < kAddWarps) {
+    // ---------------- sums, and each thread's best vector ----------------
+    int piece = 0, n_row = 0;
+    bool ok = true;
+    for (long long r = first_row; r < p.N && ok; r += row_step, ++n_row) {
+      const Row<T> row(static_cast<const T*>(p.logits), r, p.V);
+      const int2 w = row.part(part, p.parts);
+      const int end = tid == 0 ? 0 : row.n_vecs - 1;
+      const bool has_end = tid < 2 && row.is_end(end, tid, part, p.parts);
+      uint4 end_raw = make_uint4(0, 0, 0, 0);
+      if (has_end) end_raw = row.load_end(end);
+      Sums a{-INFINITY, 0.0f, 0.0f};
+      bool careful = false;
+      float c = -INFINITY;
+      uint32_t floor = 0;
+      uint64_t s2[2] = {0, 0}, w2[2] = {0, 0};
+      float best = -INFINITY, others = -INFINITY;
+      int best_vec = w.x + tid;
+      const auto take = [&](const auto& raw, auto count, int i0) {
+        constexpr int n = decltype(count)::value;
+        float top = -INFINITY, t[n];
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+          t[k] = V16::top(raw[k]);
+          top = fmaxf(top, t[k]);
+        }
+        if (kTop) {
+          if (top > best) {
+            others = fmaxf(others, best);
+            best = top;
+            bool found = false;
+#pragma unroll
+            for (int k = 0; k < n; ++k) {
+              const bool this_one = !found && t[k] == top;
+              if (this_one) best_vec = i0 + k * kAdders;
+              else others = fmaxf(others, t[k]);
+              found |= this_one;
+            }
+          } else {
+            others = fmaxf(others, top);
+          }
+        }
+        if (top > a.m + kSlack) {
+          careful |= fabsf(top) > 1048576.0f;
+          const float to = top * kLog2e, d = fmaxf(c - to, kFloor), f = ex2_approx(d);
+          const uint64_t f2 = f2_pack(f, f), d2 = f2_pack(d, d);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            w2[e] = f2_mul(f2_fma(s2[e], d2, w2[e]), f2);
+            s2[e] = f2_mul(s2[e], f2);
+          }
+          a.m = top;
+          c = to;
+          floor = V16::floor_of(top - 800.0f);
+        }
+        if (a.m == -INFINITY) {   // nothing but -inf, or NaN, so far
+#pragma unroll
+          for (int k = 0; k < n; ++k) {
+            float x[N];
+            V16::unpack(raw[k], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) careful |= x[e] != x[e];
+          }
+          return;
+        }
+        const uint64_t l2 = f2_pack(kLog2e, kLog2e), c2 = f2_pack(-c, -c);
+#pragma unroll
+        for (int k = 0; k < n; ++k) {
+          float x[N];
+          V16::unpack(V16::raise(raw[k], floor), x);
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const uint64_t t2 = f2_fma(f2_pack(x[e], x[e + 1]), l2, c2);
+            float t0, t1;
+            f2_unpack(t2, t0, t1);
+            const uint64_t e2 = f2_pack(ex2_approx(t0), ex2_approx(t1));
+            s2[(e >> 1) & 1] = f2_add(s2[(e >> 1) & 1], e2);
+            w2[(e >> 1) & 1] = f2_fma(e2, t2, w2[(e >> 1) & 1]);
+          }
+        }
+      };
+      using Many = std::integral_constant<int, kEach>;
+      using One = std::integral_constant<int, 1>;
+      for (int v = w.x; v < w.y; v += kPiece, ++piece) {
+        const int st = piece % kStages;
+        ok = warp_wait_all(&sm.full[st], (piece / kStages) & 1, &sm.abort);
+        if (!ok) break;
+        const uint4* vecs = ring + st * kPiece + tid;
+        if (v + kPiece <= w.y) {
+          uint4 raw[kEach];
+#pragma unroll
+          for (int k = 0; k < kEach; ++k) raw[k] = vecs[k * kAdders];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.empty[st]);
+          take(raw, Many{}, v + tid);
+        } else {
+          for (int i = v + tid; i < w.y; i += kAdders, vecs += kAdders) {
+            const uint4 one[1] = {*vecs};
+            take(one, One{}, i);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.empty[st]);
+        }
+      }
+      const int buf = n_row & 1;
+      if (ok && n_row >= 2) ok = warp_wait_all(&sm.taken[buf], ((n_row >> 1) - 1) & 1, &sm.abort);
+      if (!ok) break;
+      if constexpr (kTop) {
+        sm.row[buf].pairs[tid] = w.x + tid < w.y ? key_of(best, static_cast<uint32_t>(best_vec)) : 0ull;
+        sm.row[buf].others[tid] = others;
+      }
+      // the row's ends are no thread's pairs (they are looked at anyway)
+      if (has_end) {
+        const uint4 one[1] = {end_raw};
+        take(one, One{}, end);
+      }
+      if (careful) {
+        a = careful_sums(row, w.x, w.y, has_end, end_raw);
+      } else if (a.m != -INFINITY) {
+        float x[4];
+        f2_unpack(f2_add(s2[0], s2[1]), x[0], x[1]);
+        f2_unpack(f2_add(w2[0], w2[1]), x[2], x[3]);
+        const float off = fmaf(a.m, kLog2e, -c), f = ex2_approx(-off);
+        a.s = (x[0] + x[1]) * f;
+        a.w = fmaf(-off, x[0] + x[1], x[2] + x[3]) * f;
+      }
+      float to = a.m;
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+      a.move_to(to);
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
+        a.w += __shfl_xor_sync(0xffffffffu, a.w, d);
+      }
+      if (lane == 0) sm.row[buf].sums[warp] = a;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.done[buf]);
+    }
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 91);
+      sm.abort = 1;
+    }
+  } else {
+    // ---------------- the rows' results ----------------
+    const int K = kTop ? min(p.topk, p.V) : 0;
+    int n_row = 0;
+    bool ok = true;
+    Sums all{-INFINITY, 0.0f, 0.0f};
+    float x_tok = 0.0f;
+    bool has_tok = false;
+    const auto write = [&](long long r) {
+      const float log_s = logf(all.s), nan = __uint_as_float(0x7fc00000u);
+      const bool none = all.s == 0.0f;
+      if (lane == 0) {
+        p.lse[r] = none ? -INFINITY : all.m + log_s;
+        p.entropy[r] = none ? nan : log_s - all.w * kLn2 / all.s;
+        if (p.logp != nullptr) p.logp[r] = !has_tok ? 0.0f : none ? nan : (x_tok - all.m) - log_s;
       }
       if constexpr (kTop) {
-        const int n = p.parts * K;   // at most kMaxParts * kMaxTopLogprob
-        static_assert(kMaxParts * kMaxTopLogprob <= kMaxFound, "the parts' best");
-        for (int i = tid; i < n; i += kThreads) s_found[i] = *(cluster_ptr(s_best, i / K) + i % K);
-        __syncthreads();
-        if (tid < kMaxTopLogprob) s_best[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kThreads) {
-          const unsigned long long key = s_found[i];
-          int rank = 0;
-          for (int o = 0; o < n; ++o) rank += s_found[o] > key ? 1 : 0;
-          if (key != 0 && rank < K) s_best[rank] = key;
+        for (int k = lane; k < p.topk; k += 32) {
+          const bool some = k < K;
+          const unsigned long long key = some ? sm.best[k] : 0;
+          p.top_idx[r * p.topk + k] = some ? static_cast<int32_t>(index_of(key)) : -1;
+          p.top_logp[r * p.topk + k] = !some ? -INFINITY : none ? nan : (from_ordered(static_cast<uint32_t>(key >> 32)) - all.m) - log_s;
         }
-        __syncthreads();
       }
-    }
-  }
-  if (part == 0 && tid == 0) {
-    const Sums t = s_part;
-    const float log_s = logf(t.s), nan = __uint_as_float(0x7fc00000u);
-    const bool none = t.s == 0.0f;
-    p.lse[r] = none ? -INFINITY : t.m + log_s;
-    p.entropy[r] = none ? nan : log_s - t.w * kLn2 / t.s;
-    if (p.logp != nullptr) p.logp[r] = !has_tok ? 0.0f : none ? nan : (x_tok - t.m) - log_s;
-    s_row = none ? make_float2(0.0f, nan) : make_float2(t.m, log_s);
-  }
-  if constexpr (kTop) {
-    __syncthreads();
-    if (part == 0) {
-      for (int k = tid; k < p.topk; k += kThreads) {
-        const bool some = k < K;
-        p.top_idx[r * p.topk + k] = some ? static_cast<int32_t>(index_of(s_best[k])) : -1;
-        p.top_logp[r * p.topk + k] = some ? (from_ordered(static_cast<uint32_t>(s_best[k] >> 32)) - s_row.x) - s_row.y : -INFINITY;
+    };
+    for (long long r = first_row; r < p.N && ok; r += row_step, ++n_row) {
+      const Row<T> row(static_cast<const T*>(p.logits), r, p.V);
+      const int2 w = row.part(part, p.parts);
+      has_tok = false;
+      if (part == 0 && p.tok != nullptr) {
+        const int y = __ldg(p.tok + r);
+        has_tok = y >= 0 && y < p.V;
+        if (has_tok) x_tok = V16::value(static_cast<const T*>(p.logits)[r * p.V + y]);
       }
+      const int buf = n_row & 1;
+      ok = warp_wait_all(&sm.done[buf], (n_row >> 1) & 1, &sm.abort);
+      if (!ok) break;
+      all = sm.row[buf].sums[0];
+#pragma unroll
+      for (int i = 1; i < kAddWarps; ++i) all = merge(all, sm.row[buf].sums[i]);
+      if constexpr (kTop) {
+        constexpr int kLists = kAdders / 32;
+        // the K best pairs: a lane's, in order
+        unsigned long long mine[kLists];
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) mine[i] = sm.row[buf].pairs[32 * i + lane];
+#pragma unroll
+        for (int i = 1; i < kLists; ++i)
+#pragma unroll
+          for (int j = i; j > 0; --j) {
+            const unsigned long long hi = max(mine[j - 1], mine[j]), lo = min(mine[j - 1], mine[j]);
+            mine[j - 1] = hi, mine[j] = lo;
+          }
+        const auto next = [&](int i) {
+          unsigned long long key = 0;
+#pragma unroll
+          for (int k = 0; k < kLists; ++k)
+            if (i == k) key = mine[k];
+          return key;
+        };
+        if (lane == 0) sm.n_found = 0;
+        for (int k = lane; k < kMaxTopLogprob; k += 32) sm.best[k] = 0;   // (NaN may leave places empty)
+        // (where fewer threads than K have vectors the bound is 0, and all their elements are looked at)
+        const unsigned long long bound =
+            merge_best(K, next, [&](int k, unsigned long long key) {
+              if (lane == 0) sm.who[k] = key != 0 ? static_cast<int>(index_of(key)) : -1;
+            });
+        const float bound_value = from_ordered(static_cast<uint32_t>(bound >> 32));
+        __syncwarp();
+        const auto look = [&](const uint4& raw, int i) {
+          if (key_of(V16::top(raw), static_cast<uint32_t>(i)) < bound) return;
+          float x[N];
+          V16::unpack(raw, x);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            if (bound != 0 && x[e] < bound_value) continue;
+            if (key_of(x[e], static_cast<uint32_t>(i)) >= bound && row.has(i, e)) {
+              const int at = atomicAdd(&sm.n_found, 1);
+              if (at < kMaxFound) sm.found[at] = key_of(x[e], static_cast<uint32_t>(i * static_cast<long long>(N) + e - row.skip));
+            }
+          }
+        };
+        for (int k0 = 0; k0 < K; k0 += 32) {
+          const int vec = k0 + lane < K ? sm.who[k0 + lane] : -1;
+          bool more = false;
+          if (vec >= 0) {
+            look(__ldg(row.base + vec), vec);
+            const float others = sm.row[buf].others[(vec - w.x) % kAdders];
+            more = bound == 0 || !(others < bound_value);
+          }
+          // threads whose other vectors may hold some too: all lanes look at them
+          for (uint32_t rest = __ballot_sync(0xffffffffu, more); rest != 0; rest &= rest - 1) {
+            const int v = __shfl_sync(0xffffffffu, vec, __ffs(rest) - 1), t = (v - w.x) % kAdders;
+            for (int i = w.x + t + lane * kAdders; i < w.y; i += 32 * kAdders)
+              if (i != v) look(__ldg(row.base + i), i);
+          }
+        }
+        if (lane < 2) {
+          const int end = lane == 0 ? 0 : row.n_vecs - 1;
+          if (row.is_end(end, lane, part, p.parts)) look(row.load_end(end), end);
+        }
+        __syncwarp();
+        const int n = sm.n_found;
+        if (n <= kMaxFound) {
+          for (int c = lane; c < n; c += 32) {
+            const unsigned long long key = sm.found[c];
+            int rank = 0;
+            for (int o = 0; o < n; ++o) rank += sm.found[o] > key ? 1 : 0;
+            if (rank < K) sm.best[rank] = key;
+          }
+        } else {
+          unsigned long long last = ~0ull;
+          for (int k = 0; k < K; ++k) {
+            unsigned long long top = 0;
+            const auto see = [&](const uint4& raw, int i) {
+              float x[N];
+              V16::unpack(raw, x);
+#pragma unroll
+              for (int e = 0; e < N; ++e) {
+                const unsigned long long key = key_of(x[e], static_cast<uint32_t>(i * static_cast<long long>(N) + e - row.skip));
+                if (row.has(i, e) && key < last && key > top) top = key;
+              }
+            };
+            for (int i = w.x + lane; i < w.y; i += 32) see(__ldg(row.base + i), i);
+            if (lane < 2) {
+              const int end = lane == 0 ? 0 : row.n_vecs - 1;
+              if (row.is_end(end, lane, part, p.parts)) see(row.load_end(end), end);
+            }
+            const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(top >> 32));
+            const uint32_t low = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(top >> 32) == hi ? static_cast<uint32_t>(top) : 0u);
+            last = (static_cast<unsigned long long>(hi) << 32) | low;
+            if (lane == 0) sm.best[k] = last;
+          }
+        }
+      }
+      __syncwarp();
+      if (p.parts == 1) write(r);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.taken[buf]);
     }
+    if (lane == 0) sm.part = all;
+    if (!ok && lane == 0) {
+      if (!sm.abort) report_status(p.status, kStatusTimeout, 92);
+      sm.abort = 1;
+    }
+    if (p.parts > 1) {
+      __syncwarp();
+      cluster_sync();   // every part's sums and best are there
+      if (part == 0 && ok) {
+        for (int c = 1; c < p.parts; ++c) all = merge(all, *cluster_ptr(&sm.part, c));
+        if constexpr (kTop) {
+          // the parts' lists, which are in order: brought here, then merged, one a lane
+          static_assert(kMaxParts * kMaxTopLogprob <= kMaxFound, "the parts' best");
+          for (int i = lane; i < p.parts * K; i += 32) sm.found[i] = cluster_ptr(sm.best, i / K)[i % K];
+          __syncwarp();
+          merge_best(K, [&](int i) { return lane < p.parts && i < K ? sm.found[lane * K + i] : 0ull; },
+                     [&](int k, unsigned long long key) {
+                       if (lane == 0) sm.best[k] = key;
+                     });
+          __syncwarp();
+        }
+        write(first_row);
+      }
+      __syncwarp();
+      cluster_sync();   // no CTA leaves while it is read
+    }
+    return;
   }
   if (p.parts > 1) {
     __syncwarp();
-    cluster_sync();   // no CTA leaves while it is read
+    cluster_sync();
+    cluster_sync();
   }
 }
 
-// Parts of a row, so that rows * parts CTAs fill the GPU's SMs `times` times over where a part has `least` vectors all the same. Rows alone do
-// from 1216 on: 1 x 152064 bf16 take XX us in eight parts and XX in one.
+// Parts of a row: as many as keep rows * parts at or below `times` CTAs an SM and leave a part `least` vectors. Rows alone do
+// from 1216 on:
 int parts_of(int N, long long vecs, int times, long long least) {
   int parts = 1;
-  while (parts < kMaxParts && static_cast<long long>(N) * parts < 152LL * times && vecs / (2 * parts) >= least) parts *= 2;
+  while (parts < kMaxParts && 2LL * N * parts <= 152LL * times && vecs / (2 * parts) >= least) parts *= 2;
   return parts;
 }
 
@@ -577,13 +751,14 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const __grid_c
 
 }  // namespace
 
-int launch_logprob_fwd(const LogprobArgs& a, cudaStream_t stream) {
+int launch_logprob_fwd(const LogprobArgs& a, int* status, cudaStream_t stream) {
   const long long vecs = (static_cast<long long>(a.V) * a.elem_bytes + 15) / 16;
-  const int parts = parts_of(a.N, vecs, 8, 512);
-  if (static_cast<long long>(a.N) * parts > 0x7fffffffLL) return -2;
-  FwdParams p{a.logits, a.tok, a.logp, a.entropy, a.lse, a.top_idx, a.top_logp, a.V, a.topk, parts};
+  const int parts = parts_of(a.N, vecs, 4, 512);
+  FwdParams p{a.logits, a.tok, a.logp, a.entropy, a.lse, a.top_idx, a.top_logp, status, a.N, a.V, a.topk, parts};
+  // rows that are not split: as many CTAs as the GPU holds at once, one row after the other each
+  const int ctas = parts > 1 ? a.N * parts : std::min(a.N, 4 * 152);
   cudaLaunchAttribute pdl[1], attr[2];
-  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(a.N * parts)), dim3(kThreads), 0, stream, pdl);
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(ctas)), dim3(kFwdThreads), kStages * kPiece * 16, stream, pdl);
   if (parts > 1) {
     attr[0] = pdl[0];
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -601,7 +776,7 @@ int launch_logprob_fwd(const LogprobArgs& a, cudaStream_t stream) {
 
 int launch_logprob_bwd(const LogprobGradArgs& a, cudaStream_t stream) {
   const long long vecs = (static_cast<long long>(a.V) * a.elem_bytes + 15) / 16;
-  const int parts = parts_of(a.N, vecs, 8, 512);
+  const int parts = parts_of(a.N, vecs, 12, 512);
   if (static_cast<long long>(a.N) * parts > 0x7fffffffLL) return -2;
   BwdParams p{a.logits, a.tok, a.lse, a.entropy, a.d_logp, a.d_entropy, a.d_lse, a.top_idx, a.d_top, a.d_logits, a.V, a.topk, parts};
   cudaLaunchAttribute attr[1];
