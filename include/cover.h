@@ -402,7 +402,7 @@ int cover_paged_append(const void* k, const void* v, const void* q, void* q_out,
  * call alone; calls that share one must not run concurrently on the GPU. The inputs must not alias out, lse or workspace.
  * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hq, Hkv, Lq, M or n_pages < 1, Hq % Hkv != 0, n_seeds < 0, a
  * softcap that is negative or not finite, a misaligned pointer, a missing workspace; COVER_ERR_UNSUPPORTED for D != 128, another
- * page, M * page >= 2^31, B Hq Lq >= 2^31 - 256; COVER_ERR_CUDA for a launch failure; COVER_ERR_DEVICE_TIMEOUT via
+ * page, M * page >= 2^31, B Hq Lq >= 2^31 - 256, n_pages Hkv page >= 2^34; COVER_ERR_CUDA for a launch failure; COVER_ERR_DEVICE_TIMEOUT via
  * cover_device_status.
  */
 size_t cover_attn_paged_workspace_bytes(int B, int Hq, int Hkv, int Lq, int M, int page);

@@ -10,9 +10,11 @@
 // hkv G + g, and the packed rows are one run of the [B Hq Lq, D] view. Two ways, chosen by plan_of:
 //   rows (16 or 32 a group)  few rows: bound by reading the memory
 //   pairs (2 x 128 rows)     many rows: bound by the tensor cores and the softmax
-// A KV tile is 128 keys, fetched a page (or half a page of 256) at a time: boxes of 64 columns by the page's rows land one below the other
-// in the tile, whose 128-byte swizzle goes by the row, so that pages of 16 rows and more make the same tile as one run of
-// rows. A position without a page is fetched from outside the tensor, which reads as zeros, and its scores count as unseen.
+// A KV tile is 128 keys, fetched a page (or half a page of 256) at a time, a copy each: the pool is one tensor of groups of eight rows, and a
+// group is in shared memory its first 64 columns and then its last 64 (2 x 8 x 128 bytes, swizzled), so that pages of any size
+// make the same tile, groups 2048 bytes apart. (A copy for each half of a page's columns, tiles of two halves: 64
+// sequences of up to 8191 keys in pages of 16 took 231 us, in pages of 32 and more 197.) A position without a page is fetched from outside
+// the tensor, which reads as zeros, and its scores count as unseen.
 //
 // What no row sees must not reach the sums: scores are taken out by selection, but a weight of zero times a value that is not finite
 // is NaN. KV tiles of which some row does not see some key (the last one of a sequence, diagonals, windows, seeds' own
@@ -39,7 +41,8 @@ constexpr int kD = 128;
 constexpr int kBM = 128;                   // rows per Q tile (pairs)
 constexpr int kBN = 128;                   // keys per KV tile
 constexpr int kTileBytes = kBN * kD * 2;   // 32 KB
-constexpr int kBoxBytes = kTileBytes / 2;  // 64 columns, 128-byte swizzled
+constexpr int kBoxBytes = kTileBytes / 2;  // of Q: 64 columns, 128-byte swizzled
+constexpr int kGroupBytes = 2048, kGroupHalf = 1024;   // of K and V: eight rows, their first 64 columns
 constexpr int kHalf = kBN / 2;
 constexpr int kMaxTilePages = kBN / 16;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
@@ -92,24 +95,24 @@ __device__ __forceinline__ int position_of(const Params& p, int b, int r) {
   return at >= 0 && at <= 0x7fffffffLL ? static_cast<int>(at) : -1;
 }
 
-// Issues the boxes of one KV tile whose first key is key0 into `tile`, a lane a box; entry: of the lane's page, -1 for none.
-__device__ __forceinline__ void copy_tile(const CUtensorMap* tm, uint8_t* tile, uint64_t* full, int key0, int entry, int h, int page_log2,
-                                          int lane) {
-  const int rows_log2 = min(page_log2, 7), pages = kBN >> rows_log2;
-  if (lane < 2 * pages) {
-    const int half = lane & 1, i = lane >> 1;
-    tma_load_4d(tile + half * kBoxBytes + (i << rows_log2) * 128, tm, full, 64 * half, page_log2 > 7 ? key0 & ((1 << page_log2) - 1) : 0, h,
-                entry);
+// Issues the copies of one KV tile whose first key is key0 into `tile`, a lane a page; entry: of the lane's page, -1 for none.
+__device__ __forceinline__ void copy_tile(const CUtensorMap* tm, uint8_t* tile, uint64_t* full, int key0, int entry, int h, int Hkv,
+                                          int page_log2, int lane) {
+  const int rows_log2 = min(page_log2, 7);
+  if (lane < kBN >> rows_log2) {
+    const int within = page_log2 > 7 ? (key0 & ((1 << page_log2) - 1)) >> 3 : 0;
+    const int group = entry < 0 ? -16 : ((entry * Hkv + h) << (page_log2 - 3)) + within;
+    tma_load_4d(tile + (lane << rows_log2) * (kD * 2), tm, full, 0, 0, 0, group);
   }
 }
 
 // Whether V row `key` of a tile holds an element that is not finite; it is set to zeros then. One thread a key.
 __device__ __forceinline__ bool screen_row(uint32_t tile, int key) {
-  const uint32_t row = tile + key * 128;
+  const uint32_t row = tile + (key >> 3) * kGroupBytes + (key & 7) * 128;
   uint32_t hit = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const uint4 c = lds128(row + (i >> 3) * kBoxBytes + (((i & 7) ^ (key & 7)) << 4));
+    const uint4 c = lds128(row + (i >> 3) * kGroupHalf + (((i & 7) ^ (key & 7)) << 4));
     // an exponent of all ones carries into the sign's place
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
@@ -118,7 +121,7 @@ __device__ __forceinline__ bool screen_row(uint32_t tile, int key) {
   const bool bad = (hit & 0x80008000u) != 0;
   if (bad) {
 #pragma unroll 1
-    for (int i = 0; i < 16; ++i) sts128(row + (i >> 3) * kBoxBytes + ((i & 7) << 4), 0, 0, 0, 0);
+    for (int i = 0; i < 16; ++i) sts128(row + (i >> 3) * kGroupHalf + ((i & 7) << 4), 0, 0, 0, 0);
   }
   return bad;
 }
@@ -417,7 +420,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       }
       if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], kTileBytes);
       __syncwarp();
-      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], job.key0, job.page[(lane >> 1) % kMaxTilePages], job.h, p.page_log2, lane);
+      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], job.key0, job.page[lane % kMaxTilePages], job.h, p.Hkv, p.page_log2, lane);
       __syncwarp();
       if (is_v && lane == 0) mbar_arrive(&sm.job_empty[at]);
       issued = i + 1;
@@ -436,11 +439,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       // ---------------- products ----------------
       constexpr uint32_t id_s = idesc_bf16_f32(kBN, kN, false, false);
       constexpr uint32_t id_o = idesc_bf16_f32(kD, kN, true, true);
-      // descriptors are added up in their lower words; K's, Q's and P's upper words are the same
-      const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, 1024), dv = sdesc_sw128(smem_u32(sm.kv[0]), kBoxBytes, 1024);
+      // descriptors are added up in their lower words; K's and V's upper words are the same, and Q's and P's
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, kGroupBytes), dv = sdesc_sw128(smem_u32(sm.kv[0]), kGroupHalf, kGroupBytes);
       const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024), dp = sdesc_sw128(smem_u32(sm.pt[0]), 16, 1024);
       const uint32_t k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv), q_lo = static_cast<uint32_t>(dq),
-                     p_lo = static_cast<uint32_t>(dp), hi = static_cast<uint32_t>(dk >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+                     p_lo = static_cast<uint32_t>(dp), kv_hi = static_cast<uint32_t>(dk >> 32), hi = static_cast<uint32_t>(dq >> 32);
       const auto desc = [](uint32_t lo, uint32_t up) { return (static_cast<uint64_t>(up) << 32) | lo; };
       const auto wait = [&](uint64_t* bar, int phase) {
         const bool done = mbar_wait(bar, phase & 1, &sm.abort);
@@ -463,7 +466,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const uint32_t k = k_lo + ((slot * kTileBytes) >> 4), q = q_lo + (((unit & 1) * kN * kD * 2) >> 4);
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk)
-          umma_ss(tbase + (g & 1) * kN, desc(k + (((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4), hi),
+          umma_ss(tbase + (g & 1) * kN, desc(k + (((kk >> 2) * kGroupHalf + (kk & 3) * 32) >> 4), kv_hi),
                   desc(q + (((kk >> 2) * kN * 128 + (kk & 3) * 32) >> 4), hi), id_s, kk > 0 ? 1u : 0u);
         umma_commit(&sm.s_full[g & 1]);
         umma_commit(&sm.empty[slot]);
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         // O^T[s] (+)= V(tile g)^T . P^T
 #pragma unroll
         for (int kk = 0; kk < kBN / 16; ++kk)
-          umma_ss(tbase + (2 + s) * kN, desc(v + ((kk * 2048) >> 4), v_hi), desc(pt + ((kk * 2048) >> 4), hi), id_o,
+          umma_ss(tbase + (2 + s) * kN, desc(v + ((kk * 2 * kGroupBytes) >> 4), kv_hi), desc(pt + ((kk * 2048) >> 4), hi), id_o,
                   (in_unit > 1 || kk > 0) ? 1u : 0u);
         umma_commit(&sm.empty[slot]);
         if (last) umma_commit(&sm.o_full);
@@ -1062,20 +1065,20 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       constexpr uint32_t id_pv = idesc_bf16_f32(kBM, kD, false, true);
       constexpr uint32_t kTileDesc = kTileBytes >> 4;
       const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
-      const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
-      const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kBoxBytes, 1024);
+      const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, kGroupBytes);
+      const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), kGroupHalf, kGroupBytes);
       // descriptors are added up in their lower words, and of several barriers the one that completes last is waited for last: what
       // this thread does between a barrier and its products is on every tile's way
       const uint32_t q_lo = static_cast<uint32_t>(dq), k_lo = static_cast<uint32_t>(dk), v_lo = static_cast<uint32_t>(dv);
-      const uint32_t qk_hi = static_cast<uint32_t>(dq >> 32), v_hi = static_cast<uint32_t>(dv >> 32);
+      const uint32_t q_hi = static_cast<uint32_t>(dq >> 32), kv_hi = static_cast<uint32_t>(dk >> 32);
       const auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
       // S[s] = Q[s] . K(stage)^T
       auto issue_s = [&](int s, int st) {
         const uint32_t a = q_lo + s * kTileDesc, kb = k_lo + st * kTileDesc;
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk) {
-          const uint32_t off = static_cast<uint32_t>(((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4);
-          umma_ss(tbase + s * kBN, desc(a + off, qk_hi), desc(kb + off, qk_hi), id_qk, kk > 0 ? 1u : 0u);
+          umma_ss(tbase + s * kBN, desc(a + (((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4), q_hi),
+                  desc(kb + (((kk >> 2) * kGroupHalf + (kk & 3) * 32) >> 4), kv_hi), id_qk, kk > 0 ? 1u : 0u);
         }
         umma_commit(&sm.s_full[s]);
       };
@@ -1085,7 +1088,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
 #pragma unroll
         for (int kk = 0; kk < kBN / 16; ++kk)
           umma_ts(tbase + 2 * kBN + s * kD, tbase + s * kBN + (kk >> 2) * kHalf + 8 * (kk & 3),
-                  desc(vb + static_cast<uint32_t>((kk * 2048) >> 4), v_hi), id_pv, (acc || kk > 0) ? 1u : 0u);
+                  desc(vb + ((kk * 2 * kGroupBytes) >> 4), kv_hi), id_pv, (acc || kk > 0) ? 1u : 0u);
       };
       auto wait = [&](uint64_t* bar, int phase) {
         const bool ok = mbar_wait(bar, phase & 1, &sm.abort);
@@ -1137,7 +1140,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
             tma_load_4d(sm.q[t] + h * kBoxBytes, &tm_q, &sm.q_full, 64 * h, static_cast<int>(rowbase) + p0 + t * kBM, 0, 0);
       }
       // a lane's page of the next tile is looked up a tile ahead
-      const int my_key = ((lane >> 1) % pages) << page_rows;
+      const int my_key = (lane % pages) << page_rows;
       int entry = page_of(p, b, j0 * kBN + my_key);
       int j = 0;
       bool ok = true;
@@ -1148,7 +1151,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         if (!ok) break;
         if (lane == 0) mbar_arrive_expect_tx(&full[st], kTileBytes);
         __syncwarp();
-        copy_tile(tm, which ? sm.v[st] : sm.k[st], &full[st], (j0 + j) * kBN, entry, hkv, p.page_log2, lane);
+        copy_tile(tm, which ? sm.v[st] : sm.k[st], &full[st], (j0 + j) * kBN, entry, hkv, p.Hkv, p.page_log2, lane);
         __syncwarp();
         entry = next;
       }
@@ -1456,9 +1459,11 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   });
   if (rc != 0) return rc;
   CUtensorMap tq{}, tk{}, tv{};
-  const uint32_t box = static_cast<uint32_t>(std::min(a.page, kBN));
+  const uint32_t box = static_cast<uint32_t>(std::min(a.page, kBN)) / 8;
+  const uint64_t groups = static_cast<uint64_t>(a.n_pages) * a.Hkv * a.page / 8;
+  if (groups > 0x7fffffffULL) return -2;
   if (!make_bf16_map_4d(&tq, a.q, kD, static_cast<uint64_t>(rows), 1, 1, few ? width : kBM) ||
-      !make_bf16_map_4d(&tk, a.k_pages, kD, a.page, a.Hkv, a.n_pages, box) || !make_bf16_map_4d(&tv, a.v_pages, kD, a.page, a.Hkv, a.n_pages, box))
+      !make_bf16_row_groups_map(&tk, a.k_pages, groups, box) || !make_bf16_row_groups_map(&tv, a.v_pages, groups, box))
     return -3;
   const float log2e = 1.4426950408889634f, root = sqrtf(static_cast<float>(kD));
   const bool cap = a.softcap > 0.0f;

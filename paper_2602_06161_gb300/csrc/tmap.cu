@@ -46,4 +46,17 @@ bool make_u8_map_4d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1
   return r == CUDA_SUCCESS;
 }
 
+bool make_bf16_row_groups_map(CUtensorMap* map, const void* base, uint64_t groups, uint32_t box_groups) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[4] = {64, 8, 2, groups};
+  const cuuint64_t strides[3] = {256, 128, 2048};   // bytes: rows, halves of their columns, groups
+  const cuuint32_t box[4] = {64, 8, 2, box_groups};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 }  // namespace cover
