@@ -46,6 +46,9 @@ constexpr int kGroupBytes = 2048, kGroupHalf = 1024;   // of K and V: eight rows
 constexpr int kHalf = kBN / 2;
 constexpr int kMaxTilePages = kBN / 16;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
+// Capped scores lie in [-C, C], C = cap log2(e). Up to C = kFixedCap (caps up to 55) the pairs kernel takes the same reference for every row, C - kFixedRange or 0,
+// and looks for no maxima: weights lie in [2^(kFixedRange - 2 C), 2^kFixedRange], at least 2^-100, and sums over L keys hold values up to 2^66 / L.
+constexpr float kFixedCap = 80.0f, kFixedRange = 60.0f;
 constexpr int kSms = 152;                  // of this GPU
 constexpr float kNan = __builtin_nanf("");
 
@@ -70,7 +73,9 @@ struct Params {
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
-  float cap_x;       // 1 / (cap sqrt(d))
+  float cap_poly[4]; // coefficients of the capped score's polynomial, in powers of 1 / (cap sqrt(d))
+  float cap_near;    // products up to this one may take it (below 0: none)
+  float cap_ref;     // reference of all rows under a small cap (below 0: rows have their own)
 };
 
 // Keys of sequence b.
@@ -824,30 +829,6 @@ struct Unseen {
   bool any;
 };
 
-// Caps the scores of 32 columns (to log2 units): those of a chunk that are all within the polynomial's range take it alone. With three
-// special-function operations a score a KV tile took 3.2 us of them.
-__device__ __forceinline__ void cap_scores(float (&s)[32], const Params& p, bool valid) {
-  float hi[2] = {};
-#pragma unroll
-  for (int c = 0; c < 32; c += 4) {
-    hi[0] = fmax3(hi[0], fabsf(s[c]), fabsf(s[c + 1]));
-    hi[1] = fmax3(hi[1], fabsf(s[c + 2]), fabsf(s[c + 3]));
-  }
-  if (__all_sync(0xffffffffu, !valid || fmaxf(hi[0], hi[1]) * p.cap_x <= kTanhRange)) {
-    // C x P(x^2), x = s cap_x (a NaN among the scores stays one)
-    const uint64_t cx = f2_pack(p.cap_x, p.cap_x), c = f2_pack(p.cap_log2, p.cap_log2), t0 = f2_pack(kTanh0, kTanh0),
-                   t1 = f2_pack(kTanh1, kTanh1), t2 = f2_pack(kTanh2, kTanh2), t3 = f2_pack(kTanh3, kTanh3);
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const uint64_t x = f2_mul(f2_pack(s[e], s[e + 1]), cx), z = f2_mul(x, x);
-      f2_unpack(f2_mul(f2_mul(x, c), f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0)), s[e], s[e + 1]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) s[e] = capped(s[e], p.cap_in, p.cap_log2);
-  }
-}
-
 // Masks the scores of 32 columns from column c0 on.
 __device__ __forceinline__ void mask_scores(float (&s)[32], const Unseen& u, int c0) {
   if (u.any) {
@@ -876,26 +857,15 @@ __device__ __forceinline__ float chunk_max(uint32_t addr, const Unseen& u, int c
   return max32(s);
 }
 
-// P = 2^(score - m) of 32 columns to tensor memory, in bf16 (V's operands are, so P's have to be: a weight is off by at most 2^-8 of itself).
-// Returns the sum of the unrounded weights.
-template <bool kCap>
-__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m,
-                                           bool valid) {
-  uint32_t raw[32];
-  tmem_ld32(addr, raw);
-  tmem_ld_wait(raw);
-  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
-  if (kCap) cap_scores(s, p, valid);
+// The weights of 32 columns whose scores less the reference, in log2 units, are s: in bf16 to tensor memory (V's operands are, so P's have to be: a
+// weight is off by at most 2^-8 of itself). Returns their sum before rounding.
+__device__ __forceinline__ float store_weights(float (&s)[32], uint32_t p_addr, const Unseen& u, int c0) {
   mask_scores(s, u, c0);
-  const float scale = kCap ? 1.0f : p.scale_log2;
-  const uint64_t negm2 = f2_pack(-m, -m), scale2 = f2_pack(scale, scale);
   uint64_t acc2[2] = {0, 0};
   uint32_t packed[16];
 #pragma unroll
   for (int c = 0; c < 16; ++c) {
-    float x0, x1;
-    f2_unpack(f2_fma(f2_pack(s[2 * c], s[2 * c + 1]), scale2, negm2), x0, x1);
-    const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+    const float e0 = ex2_approx(s[2 * c]), e1 = ex2_approx(s[2 * c + 1]);
     packed[c] = pack_bf16x2(e0, e1);
     acc2[c & 1] = f2_add(acc2[c & 1], f2_pack(e0, e1));
   }
@@ -904,6 +874,50 @@ __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const
   f2_unpack(acc2[0], r[0], r[1]);
   f2_unpack(acc2[1], r[2], r[3]);
   return (r[0] + r[1]) + (r[2] + r[3]);
+}
+
+// chunk_exp where some score is beyond the polynomial's range (kept out of the loop's code).
+__device__ __noinline__ float chunk_exp_far(uint32_t addr, uint32_t p_addr, float cap_in, float cap_log2, const Unseen u, int c0, float m) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+#pragma unroll
+  for (int e = 0; e < 32; ++e) s[e] = capped(s[e], cap_in, cap_log2) - m;
+  return store_weights(s, p_addr, u, c0);
+}
+
+// P = 2^(score - m) of 32 columns to tensor memory; returns the sum of the unrounded weights. Capped scores of a chunk that are all within the
+// polynomial's range take it, x P(x^2) with the scale's powers in its coefficients, and no special function (with three of them a score a KV
+// tile took 3.2 us).
+template <bool kCap>
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m, bool valid) {
+  uint32_t raw[32];
+  tmem_ld32(addr, raw);
+  tmem_ld_wait(raw);
+  float(&s)[32] = reinterpret_cast<float(&)[32]>(raw);
+  const uint64_t negm2 = f2_pack(-m, -m);
+  if (!kCap) {
+    const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) f2_unpack(f2_fma(f2_pack(s[e], s[e + 1]), scale2, negm2), s[e], s[e + 1]);
+  } else {
+    float hi[2] = {};
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+      hi[0] = fmax3(hi[0], fabsf(s[c]), fabsf(s[c + 1]));
+      hi[1] = fmax3(hi[1], fabsf(s[c + 2]), fabsf(s[c + 3]));
+    }
+    if (__any_sync(0xffffffffu, valid && !(fmaxf(hi[0], hi[1]) <= p.cap_near))) return chunk_exp_far(addr, p_addr, p.cap_in, p.cap_log2, u, c0, m);
+    const uint64_t t0 = f2_pack(p.cap_poly[0], p.cap_poly[0]), t1 = f2_pack(p.cap_poly[1], p.cap_poly[1]),
+                   t2 = f2_pack(p.cap_poly[2], p.cap_poly[2]), t3 = f2_pack(p.cap_poly[3], p.cap_poly[3]);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {   // (a NaN among the scores stays one)
+      const uint64_t x = f2_pack(s[e], s[e + 1]), z = f2_mul(x, x);
+      f2_unpack(f2_fma(x, f2_fma(z, f2_fma(z, f2_fma(z, t3, t2), t1), t0), negm2), s[e], s[e + 1]);
+    }
+  }
+  return store_weights(s, p_addr, u, c0);
 }
 
 // A seed row's own score in log2 units: q row `row` of [B Hq Lq], masked-input key row `self`.
@@ -947,13 +961,14 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   PairSmem& sm = *reinterpret_cast<PairSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // CTA (ks, group, hkv, b)
+  // CTA (ks, hkv, group, b). A sequence's last rows see the most keys where they see what is before them, so they come first: the CTAs
+  // that are left for the end are short ones (2048 rows over 8192 keys, blocks, 256 CTAs on 152 SMs: 225 us in the heads' order, 218 so).
   const int ks = static_cast<int>(blockIdx.x) % p.nsplit;
   int rest = static_cast<int>(blockIdx.x) / p.nsplit;
-  const int group = rest % p.n_groups;
-  rest /= p.n_groups;
   const int hkv = rest % p.Hkv;
-  const int b = rest / p.Hkv;
+  rest /= p.Hkv;
+  const int group = p.n_groups - 1 - rest % p.n_groups;
+  const int b = rest / p.n_groups;
   const int n_packed = p.G * p.Lq;
   const int p0 = group * 2 * kBM;
   const long long rowbase = (static_cast<long long>(b) * p.Hq + hkv * p.G) * p.Lq;
@@ -1200,7 +1215,8 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = quad + tile * kBN + half * kHalf;
     const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
-    float m_run = -INFINITY, l_run = 0.0f;
+    const bool fixed = kCap && p.cap_ref >= 0.0f;
+    float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     bool ok = true;
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
     for (int j = 0; j < jend; ++j) {
@@ -1217,39 +1233,43 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         u.holes = __ballot_sync(0xffffffffu, (lane == 0 || i < kHalf) && page_of(p, b, key0 + i) < 0);
         u.any |= u.holes != 0;
       }
-      float m_half = -INFINITY;
-      if (ok && some) {
+      if (fixed) {
+        if (!ok) break;
+      } else {
+        float m_half = -INFINITY;
+        if (ok && some) {
 #pragma unroll 1
-        for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, u, c));
-        m_half = !kCap ? m_half * p.scale_log2 : m_half == -INFINITY ? m_half : capped(m_half, p.cap_in, p.cap_log2);   // (the cap is monotonous)
-      }
-      // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row
-      // take the same reference
-      if (any_of<256>(2 + tile, !ok || (valid && m_half > m_run + kRescaleThreshold))) {
-        if (any_of<256>(2 + tile, !ok)) {
-          ok = false;
-          break;
+          for (int c = 0; c < kHalf; c += 32) m_half = fmaxf(m_half, chunk_max(s_addr + c, u, c));
+          m_half = !kCap ? m_half * p.scale_log2 : m_half == -INFINITY ? m_half : capped(m_half, p.cap_in, p.cap_log2);   // (the cap is monotonous)
         }
-        sm.red[tile][half][R] = m_half;
-        sync_of<256>(2 + tile);
-        const float top = fmaxf(sm.red[tile][0][R], sm.red[tile][1][R]);
-        float alpha = 1.0f;
-        if (top > m_run + kRescaleThreshold) {
-          alpha = m_run == -INFINITY ? 0.0f : ex2_approx(m_run - top);
-          m_run = top;
-        }
-        l_run *= alpha;
-        if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
-          // O holds the tile's earlier products (complete: the commit of this S came after them)
-          tc_fence_after_sync();
+        // The Q tile's 256 threads vote: a warp whose wait gave up takes part all the same, and both halves of a row
+        // take the same reference
+        if (any_of<256>(2 + tile, !ok || (valid && m_half > m_run + kRescaleThreshold))) {
+          if (any_of<256>(2 + tile, !ok)) {
+            ok = false;
+            break;
+          }
+          sm.red[tile][half][R] = m_half;
+          sync_of<256>(2 + tile);
+          const float top = fmaxf(sm.red[tile][0][R], sm.red[tile][1][R]);
+          float alpha = 1.0f;
+          if (top > m_run + kRescaleThreshold) {
+            alpha = m_run == -INFINITY ? 0.0f : ex2_approx(m_run - top);
+            m_run = top;
+          }
+          l_run *= alpha;
+          if (j > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+            // O holds the tile's earlier products (complete: the commit of this S came after them)
+            tc_fence_after_sync();
 #pragma unroll 1
-          for (int c = 0; c < 2; ++c) {
-            uint32_t o[32];
-            tmem_ld32(o_addr + 32 * c, o);
-            tmem_ld_wait(o);
+            for (int c = 0; c < 2; ++c) {
+              uint32_t o[32];
+              tmem_ld32(o_addr + 32 * c, o);
+              tmem_ld_wait(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-            tmem_st32(o_addr + 32 * c, o);
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              tmem_st32(o_addr + 32 * c, o);
+            }
           }
         }
       }
@@ -1293,6 +1313,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     sm.red[tile][half][R] = l_run;
     sync_of<256>(2 + tile);
     float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
+    if (l == 0.0f) m = -INFINITY, w = 0.0f;     // no key was seen
     if (s_self != -INFINITY) {
       const float m_all = fmaxf(m, s_self);
       const float f = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
@@ -1313,10 +1334,8 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
           uint32_t x[32];
           tmem_ld32(o_addr + 32 * c, x);
           tmem_ld_wait(x);
-          // (a row that has seen nothing may hold what other rows' values made of zero weights)
-          const bool nothing = m_run == -INFINITY && l_run == 0.0f;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = w == 0.0f || nothing ? 0.0f : __uint_as_float(x[e]) * w;
+          for (int e = 0; e < 32; ++e) o[e] = w == 0.0f ? 0.0f : __uint_as_float(x[e]) * w;
         }
         const int col = half * kHalf + 32 * c;
         if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + col);
@@ -1500,7 +1519,12 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   p.scale_log2 = log2e / root;
   p.cap_log2 = softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
-  p.cap_x = cap ? 1.0f / (softcap * root) : 0.0f;
+  // (caps below 2^-10 would put powers of 1 / cap beyond fp32's largest number)
+  const float cap_x = cap ? 1.0f / (softcap * root) : 0.0f, tanh_poly[4] = {kTanh0, kTanh1, kTanh2, kTanh3};
+  p.cap_ref = cap && p.cap_log2 <= kFixedCap ? fmaxf(0.0f, p.cap_log2 - kFixedRange) : -1.0f;
+  p.cap_near = cap && p.cap_log2 >= 1.0f / 1024.0f ? kTanhRange / cap_x : -1.0f;
+  float power = p.cap_log2 * cap_x;
+  for (int i = 0; i < 4; ++i, power *= cap_x * cap_x) p.cap_poly[i] = p.cap_near > 0.0f ? tanh_poly[i] * power : 0.0f;
   cudaLaunchAttribute attr[1];
   const int m = plan.mode == kRows16 ? 0 : 1;
   cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(few ? kRowsThreads : kPairsThreads),
