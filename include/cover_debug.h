@@ -133,9 +133,10 @@ int cover_debug_attn_prefix8_plan(int B, int Hq, int Hkv, int Lq, int Lk, int pl
 /*
  * cover_attn_fwd_paged on a kernel of the caller's choice, whatever the call itself would take. mode 0, 1: rows of a KV head in
  * groups of 16 or 32 on `parts` CTAs (1 .. 1024), each with an even share of the KV tiles; 2: pairs of Q tiles of 128 rows, the
- * keys in `parts` parts (1 .. 64); COVER_ERR_UNSUPPORTED otherwise. workspace_bytes: of the workspace; what is needed: modes 0, 1
- * parts (2 w 520 + 16), w = 16 or 32; mode 2 with parts > 1 B Hq Lq parts 520; COVER_ERR_INVALID_ARG if there is less. Otherwise as
- * cover_attn_fwd_paged.
+ * keys in `parts` parts (1 .. 64); parts = -1 .. -8 in any mode: -parts CTAs of a cluster share a unit's keys and add their results up;
+ * COVER_ERR_UNSUPPORTED otherwise. workspace_bytes: of the workspace; what is needed: modes 0, 1
+ * parts (2 w 520 + 16), w = 16 or 32; mode 2 with parts > 1 B Hq Lq parts 520; none in a cluster; COVER_ERR_INVALID_ARG if there is less.
+ * Otherwise as cover_attn_fwd_paged.
  */
 int cover_debug_attn_paged(const void* q, const void* k_pages, const void* v_pages,
                            const int32_t* table, int n_pages, int M, int page, const int32_t* lens,

@@ -1163,14 +1163,15 @@ def cover_debug_attn_prefix8(q, k8, v8, k_exp, v_exp, k_seedmask=None, v_seedmas
 
 def cover_debug_attn_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0=None, mode: int,
                            parts: int = 1, key_lo=None, key_hi=None, softcap: float = 0.0, workspace=None):
-    """cover_attn_fwd_paged on the kernel ``mode`` with the keys in ``parts`` parts (mode 2), or on that many CTAs. Returns (out, lse)."""
+    """cover_attn_fwd_paged on the kernel ``mode`` with the keys in ``parts`` parts (mode 2), or on that many CTAs (negative: on clusters of
+    -parts CTAs a unit). Returns (out, lse)."""
     B, Hq, Lq, D = q.shape
     n_pages, Hkv, page, _ = k_pages.shape
     S = 0 if seed_idx is None else int(seed_idx.shape[1])
     out, lse = torch.empty_like(q), torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
     if workspace is None:
         n = B * Hq * Lq * parts * 520 if mode == 2 else parts * (2 * (16 << mode) * 520 + 16)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
     _launch("cover_debug_attn_paged", q.device, None,
             (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), n_pages, table.shape[1], page, _ptr(lens), _ptr(k_seedmask) if S else None,
              _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, _ptr(q0), B, Hq, Hkv, Lq, D,

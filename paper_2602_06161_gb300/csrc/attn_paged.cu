@@ -28,6 +28,7 @@
 #include <cmath>
 
 #include "attn_common.cuh"
+#include "cluster.cuh"
 #include "context.cuh"
 #include "kernels.cuh"
 #include "ptx.cuh"
@@ -70,6 +71,7 @@ struct Params {
   int* status;
   long long rows;    // B * Hq * Lq
   int n_pages, M, page_log2, B, n_seeds, Hq, Hkv, G, Lq, n_groups, nsplit;
+  int joined;        // CTAs of a cluster that share a unit's keys and add their results up themselves, or 0
   float scale_log2;  // log2(e) / sqrt(d)
   float cap_log2;    // cap * log2(e)
   float cap_in;      // 2 log2(e) / (cap sqrt(d))
@@ -150,6 +152,63 @@ __device__ __forceinline__ void sync_of(int barrier) {
   asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kAll) : "memory");
 }
 
+// Parts that a cluster's CTAs add up themselves: each stages its rows' accumulators [row][128] fp32 and (m, l) in its own
+// shared memory, and CTA `rank` finishes the rows rank, rank + parts, .., a warp a row, reading all CTAs'. Rows' 16-byte
+// pieces are swizzled, for threads that write a row each.
+constexpr int kMaxJoined = 8;   // a cluster's portable size
+__device__ __forceinline__ uint32_t staged_at(int row, int c4) { return row * (kD * 4) + ((c4 ^ (row & 31)) << 4); }
+
+template <int kWarps>
+__device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint32_t ml, int n_rows, long long orow0, int rank, int parts) {
+  const int lane = threadIdx.x & 31;
+  for (int row = rank + parts * static_cast<int>(threadIdx.x >> 5); row < n_rows; row += parts * kWarps) {
+    float2 mine = make_float2(-INFINITY, 0.0f);
+    if (lane < parts) {
+      const uint32_t at = cluster_map(ml + 8 * row, lane);
+      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(mine.x), "=f"(mine.y) : "r"(at) : "memory");
+    }
+    float4 x[kMaxJoined];
+#pragma unroll
+    for (int k = 0; k < kMaxJoined; ++k) {
+      x[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (k < parts) {
+        const uint32_t at = cluster_map(staged + staged_at(row, lane), k);
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[k].x), "=f"(x[k].y), "=f"(x[k].z), "=f"(x[k].w)
+                     : "r"(at)
+                     : "memory");
+      }
+    }
+    float m = mine.x;
+#pragma unroll
+    for (int d = kMaxJoined / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    m = __shfl_sync(0xffffffffu, m, 0);
+    const float w = mine.x == -INFINITY ? 0.0f : ex2_approx(mine.x - m);
+    float l = mine.x == -INFINITY ? mine.y : w * mine.y;   // (a sum of NaN is taken along)
+#pragma unroll
+    for (int d = kMaxJoined / 2; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    l = __shfl_sync(0xffffffffu, l, 0);
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < kMaxJoined; ++k) {
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      if (wk != 0.0f) {   // (a part that saw no key holds anything)
+        acc.x = fmaf(wk, x[k].x, acc.x), acc.y = fmaf(wk, x[k].y, acc.y), acc.z = fmaf(wk, x[k].z, acc.z), acc.w = fmaf(wk, x[k].w, acc.w);
+      }
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    reinterpret_cast<uint2*>(p.out + (orow0 + row) * kD)[lane] =
+        make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    if (lane == 0 && p.lse != nullptr) p.lse[orow0 + row] = (m + lg2_approx(l)) * 0.6931471805599453f;
+  }
+}
+// The cluster's barriers around it, for warps that have no part in it.
+__device__ __forceinline__ void join_pass() {
+  __syncwarp();
+  cluster_sync();
+  cluster_sync();
+}
+
 // ---------------------------------------------------------------------------
 // Few rows
 // ---------------------------------------------------------------------------
@@ -162,6 +221,8 @@ __device__ __forceinline__ void sync_of(int barrier) {
 // share, whatever the lengths: a batch of sequences of 1 to 1000 tiles keeps all SMs reading until the end. Where a
 // share's border cuts a unit, its CTAs leave their parts to a second kernel: at most two a CTA. Loads run on across units, so that a
 // unit's end is hidden behind the next one's tiles.
+// Few short sequences are done faster by a cluster a unit, whose CTAs share its tiles and add their results up through each other's
+// shared memory: no look at the other sequences' lengths, no second kernel.
 //
 // Roles (512 threads): warps 0-3, 4-7 softmax of the streams; 8-11 look V tiles through; 12 products; 13 copies; 14 lays out what
 // is to be done, tile by tile: pages, masks and rows, up to 8 tiles ahead.
@@ -193,7 +254,7 @@ struct RowsSmem {
   TileJob job[kRing];
   uint4 nan_keys[kRing];
   int4 row[kUnits][kN];      // per unit: keys lo, hi, position of a seed row or -1, its slot
-  int4 unit[kUnits];         // tiles here, rows, first row of [B Hq Lq], part's place: -1 whole, else its number
+  int4 unit[kUnits];         // tiles here, rows, first row of [B Hq Lq], part's place: -1 whole, -2 joined, else its number
   int2 unit_mask[kUnits];    // masked-input rows of the KV head, whether the unit's first tile is here
   float4 fin[kN];            // weights of the two accumulators and of the masked-input value, 1 / l
   float m[2][kN], step[2][kN], factor[2][kN];
@@ -201,6 +262,7 @@ struct RowsSmem {
   float red[2][4][kN];
   float s_self[kN];
   int slot[kN];
+  float2 ml[kN];             // joined in a cluster: the rows' references and sums
   long long scan[kRowsThreads / 32];
   long long t0, t1, before;  // this CTA's tiles, those before the first sequence of them
   int b0;
@@ -268,51 +330,67 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     tmem_alloc(&sm.tmem_base, kTmem);
     tmem_relinquish();
   }
-  griddep_wait();
-  griddep_launch_dependents();
-
-  // ---------------- the CTA's share of all tiles ----------------
-  const long long heads = static_cast<long long>(p.Hkv) * p.n_groups;   // units of a sequence
-  const int each = (p.B + kRowsThreads - 1) / kRowsThreads;             // sequences of a thread
-  const int b_lo = min(tid * each, p.B), b_hi = min(b_lo + each, p.B);
-  long long mine = 0;
-  for (int b = b_lo; b < b_hi; ++b) mine += tiles_of<true>(p, b).x * heads;
-  long long incl = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += x;
-  }
-  if (lane == 31) sm.scan[warp] = incl;
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tbase = sm.tmem_base;
-  long long before = 0, all = 0;
-  for (int w = 0; w < kRowsThreads / 32; ++w) {
-    if (w < warp) before += sm.scan[w];
-    all += sm.scan[w];
-  }
-  const long long n_ctas = min(static_cast<long long>(gridDim.x), all), c = blockIdx.x;
-  const long long t0 = c < n_ctas ? share_start(c, n_ctas, all) : 0, t1 = c < n_ctas ? share_start(c + 1, n_ctas, all) : 0;
-  before += incl - mine;
-  if (t0 < t1 && t0 >= before && t0 < before + mine) {
-    int b = b_lo;
-    for (long long x; before + (x = tiles_of<true>(p, b).x * heads) <= t0; ++b) before += x;
-    sm.b0 = b;
-    sm.before = before;
-  }
-  __syncthreads();
-  const int n = static_cast<int>(t1 - t0);   // tiles of this CTA
+  griddep_wait();
+  griddep_launch_dependents();
+
+  // ---------------- the CTA's share of all tiles ----------------
   const int n_packed = p.G * p.Lq;
+  const long long heads = static_cast<long long>(p.Hkv) * p.n_groups;   // units of a sequence
+  long long t0, t1, all = 0, n_ctas = 0, c = blockIdx.x;
+  int b0;
+  long long before0 = 0;   // tiles before sequence b0's
+  if (p.joined) {
+    // tiles counted from the sequence's first: a part of those of the cluster's unit
+    const long long u = blockIdx.x / p.joined;
+    const int rank = static_cast<int>(blockIdx.x % p.joined);
+    b0 = static_cast<int>(u / heads);
+    const int tiles = tiles_of<false>(p, b0).x, share = tiles / p.joined, more = tiles % p.joined;
+    t0 = (u % heads) * tiles + rank * share + min(rank, more);
+    t1 = t0 + share + (rank < more ? 1 : 0);
+  } else {
+    const int each = (p.B + kRowsThreads - 1) / kRowsThreads;           // sequences of a thread
+    const int b_lo = min(tid * each, p.B), b_hi = min(b_lo + each, p.B);
+    long long mine = 0;
+    for (int b = b_lo; b < b_hi; ++b) mine += tiles_of<true>(p, b).x * heads;
+    long long incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += x;
+    }
+    if (lane == 31) sm.scan[warp] = incl;
+    __syncthreads();
+    long long before = 0;
+    for (int w = 0; w < kRowsThreads / 32; ++w) {
+      if (w < warp) before += sm.scan[w];
+      all += sm.scan[w];
+    }
+    n_ctas = min(static_cast<long long>(gridDim.x), all);
+    t0 = c < n_ctas ? share_start(c, n_ctas, all) : 0, t1 = c < n_ctas ? share_start(c + 1, n_ctas, all) : 0;
+    before += incl - mine;
+    if (t0 < t1 && t0 >= before && t0 < before + mine) {
+      int b = b_lo;
+      for (long long x; before + (x = tiles_of<true>(p, b).x * heads) <= t0; ++b) before += x;
+      sm.b0 = b;
+      sm.before = before;
+    }
+    __syncthreads();
+    b0 = sm.b0;
+    before0 = sm.before;
+  }
+  const int n = static_cast<int>(t1 - t0);   // tiles of this CTA
 
   if (warp == kRowsPlanWarp) {
     // ---------------- what is to be done ----------------
     bool ok = true;
-    int b = sm.b0, g = 0, unit = 0;
-    long long first = sm.before;   // of the sequence's tiles
+    int b = b0, g = 0, unit = 0;
+    long long first = before0;   // of the sequence's tiles
     int2 tiles = n > 0 ? tiles_of<false>(p, b) : make_int2(1, 0);
-    if (n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!p.joined && n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
     bool joined = false;
     for (long long t = t0; t < t1 && ok; ++unit) {
       while (t >= first + tiles.x * heads) first += tiles.x * heads, tiles = tiles_of<false>(p, ++b);
@@ -321,6 +399,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       const int h = u / p.n_groups, p0 = (u % p.n_groups) * kN, n_rows = min(kN, n_packed - p0);
       const long long rowbase = (static_cast<long long>(b) * p.Hq + h * p.G) * p.Lq;
       const int len = length_of(p, b), buf = unit % kUnits;
+      const int pages = kBN >> min(p.page_log2, 7);
+      // (looked up before the rows, whose keys and seeds take loads of their own)
+      int entry = lane < pages ? page_of(p, b, (tiles.y + j) * kBN + (lane << min(p.page_log2, 7))) : -1;
       if (unit >= kUnits) ok = warp_wait(&sm.unit_empty[buf], (unit / kUnits - 1) & 1, &sm.abort);
       if (!ok) break;
       // seed rows: the rows stand at up to kN positions, r itself or r - r0 around Lq
@@ -360,10 +441,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       __syncwarp();
       if (lane == 0) {
         // a part that begins its unit comes last in its CTA, any other first
-        const int place = whole ? -1 : static_cast<int>(2 * c) + (j == 0 ? 1 : 0);
+        const int place = p.joined ? -2 : whole ? -1 : static_cast<int>(2 * c) + (j == 0 ? 1 : 0);
         sm.unit[buf] = make_int4(nt, n_rows, static_cast<int>(rowbase + p0), place);
         sm.unit_mask[buf] = make_int2(static_cast<int>((static_cast<long long>(b) * p.Hkv + h)), j == 0 ? 1 : 0);
-        if (j == 0 && !whole) {
+        if (j == 0 && !whole && !p.joined) {
           // the unit's last tile is of CTA ((tile + 1) n - 1) / T
           const long long last = first + static_cast<long long>(u + 1) * tiles.x - 1;
           p.joins[blockIdx.x] = make_int4(static_cast<int>(((last + 1) * n_ctas - 1) / all - c) + 1, n_rows, static_cast<int>(rowbase + p0), 0);
@@ -371,10 +452,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         mbar_arrive(&sm.unit_full[buf]);
       }
-      const int pages = kBN >> min(p.page_log2, 7);
       for (int i = 0; i < nt && ok; ++i, ++g) {
         const int key0 = (tiles.y + j + i) * kBN, at = g % kRing;
-        const int entry = lane < pages ? page_of(p, b, key0 + (lane << min(p.page_log2, 7))) : -1;
+        if (i > 0) entry = lane < pages ? page_of(p, b, key0 + (lane << min(p.page_log2, 7))) : -1;
         if (g >= kRing) ok = warp_wait(&sm.job_empty[at], (g / kRing - 1) & 1, &sm.abort);
         if (!ok) break;
         TileJob& job = sm.job[at];
@@ -395,7 +475,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       }
       t += nt;
     }
-    if (lane == 0 && n > 0 && !joined) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (lane == 0 && n > 0 && !joined && !p.joined) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 80);
       sm.abort = 1;
@@ -538,8 +618,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const uint32_t pt = smem_u32(sm.pt[stream]) + key * 128;
     const uint32_t sw = static_cast<uint32_t>(key & 7) << 4;
     const int page_rows = min(p.page_log2, 7);
+    const uint32_t staged = smem_u32(sm.kv[0]);   // joined: every copy and product is complete by then
     bool ok = true;
     int g = 0;
+    if (n == 0 && tid < kN) sm.ml[tid] = make_float2(-INFINITY, 0.0f);
     for (int unit = 0; g < n; ++unit) {
       const int buf = unit % kUnits;
       ok = warp_wait(&sm.unit_full[buf], (unit / kUnits) & 1, &sm.abort);
@@ -710,8 +792,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         float sum = fmaf(f0, l2[0], fmaf(f1, l2[1], p_self));
         if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
         if (s_self != s_self) sum = s_self;
-        sm.fin[tid] = make_float4(f0, f1, p_self, place >= 0 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
-        if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + tid] = make_float2(top, sum);
+        sm.fin[tid] = make_float4(f0, f1, p_self, place != -1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+        if (place == -2) sm.ml[tid] = make_float2(top, sum);
+        else if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + tid] = make_float2(top, sum);
         else if (p.lse != nullptr) p.lse[orow0 + tid] = (top + lg2_approx(sum)) * 0.6931471805599453f;
       }
       sync_of<256>(1);
@@ -730,7 +813,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
             if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
             if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
-            if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
+            if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
+            else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
             else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
           }
         }
@@ -746,7 +830,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       sm.abort = 1;
     }
     tc_fence_before_sync();
+    if (p.joined) {
+      const long long u = blockIdx.x / p.joined % heads;
+      const int p0 = static_cast<int>(u % p.n_groups) * kN;
+      __syncwarp();
+      cluster_sync();   // every CTA's rows are staged
+      join_rows<8>(p, staged, smem_u32(sm.ml), min(kN, n_packed - p0),
+                   (static_cast<long long>(b0) * p.Hq + (u / p.n_groups) * p.G) * p.Lq + p0, static_cast<int>(blockIdx.x % p.joined), p.joined);
+      __syncwarp();
+      cluster_sync();   // no CTA leaves while its rows are read
+    }
   }
+  if (p.joined && warp >= kScreenWarp) join_pass();
   __syncthreads();
   if (warp == kRowsMmaWarp) {
     tc_fence_after_sync();
@@ -804,6 +899,7 @@ struct PairSmem {
   uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], v_clean[2];
   uint64_t s_full[2], p_full[2], o_full, drain;
   uint4 nan_keys[4];                    // per KV tile in turn: keys whose V row is not finite
+  float2 ml[2 * kBM];                   // joined in a cluster: the rows' references and sums
   float red[2][2][kBM];                 // per Q tile and half of the columns
   int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
   int lo, hi;                           // keys that some row sees
@@ -1326,6 +1422,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const long long orow = rowbase + P;
     const bool split = p.nsplit > 1;
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);   // 1 / l, once a row; zero where no key was seen
+    const uint32_t staged = smem_u32(sm.q[0]);   // joined: every product is complete, Q and K are not read any more
     if (ok && warp_live) {
 #pragma unroll 1
       for (int c = 0; c < 2; ++c) {
@@ -1339,7 +1436,12 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         }
         const int col = half * kHalf + 32 * c;
         if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + col);
-        if (valid && split) {
+        if (p.joined) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            sts128(staged + staged_at(tile * kBM + R, col / 4 + e), __float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                   __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+        } else if (valid && split) {
           float4* dst = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(ks) * p.rows + orow) * kD + col);
 #pragma unroll
           for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
@@ -1353,12 +1455,21 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         __syncwarp();   // the next chunk is loaded by the whole warp
       }
       if (valid && half == 0) {
-        if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
+        if (p.joined) sm.ml[tile * kBM + R] = make_float2(m, l);
+        else if (split) p.part_ml[static_cast<size_t>(ks) * p.rows + orow] = make_float2(m, l);
         else if (p.lse != nullptr) p.lse[orow] = (m + lg2_approx(l)) * 0.6931471805599453f;
       }
     }
     tc_fence_before_sync();
+    if (p.joined) {
+      __syncwarp();
+      cluster_sync();   // every CTA's rows are staged
+      join_rows<kPairSoftmaxWarps>(p, staged, smem_u32(sm.ml), min(2 * kBM, n_packed - p0), rowbase + p0, ks, p.nsplit);
+      __syncwarp();
+      cluster_sync();   // no CTA leaves while its rows are read
+    }
   }
+  if (p.joined && warp >= kPairMmaWarp) join_pass();
   __syncthreads();
   if (warp == kPairMmaWarp) {
     tc_fence_after_sync();
@@ -1397,7 +1508,8 @@ enum Mode { kRows16, kRows32, kPairs };
 struct Plan {
   Mode mode;
   int n_groups, nsplit;
-  int ctas;   // rows: of the main kernel
+  int ctas;     // rows: of the main kernel, where its shares cross units
+  int joined;   // CTAs of a cluster that share a unit, or 0
 };
 
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
@@ -1405,9 +1517,9 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
   const long long nkv = (static_cast<long long>(M) * page + kBN - 1) / kBN;   // KV tiles of a sequence at most
   if (packed <= 32) {
     const long long most = std::min<long long>(static_cast<long long>(B) * Hkv, kSms) * std::min<long long>(nkv, kSms);
-    return Plan{packed <= 16 ? kRows16 : kRows32, 1, 1, static_cast<int>(std::min<long long>(kSms, most))};
+    return Plan{packed <= 16 ? kRows16 : kRows32, 1, 1, static_cast<int>(std::min<long long>(kSms, most)), 0};
   }
-  Plan best{kPairs, static_cast<int>((packed + 2 * kBM - 1) / (2 * kBM)), 0, 0};
+  Plan best{kPairs, static_cast<int>((packed + 2 * kBM - 1) / (2 * kBM)), 0, 0, 0};
   const double rows = static_cast<double>(B) * Hq * Lq;
   const long long units = static_cast<long long>(best.n_groups) * Hkv * B;
   double best_us = 0.0;
@@ -1431,19 +1543,21 @@ constexpr Kernel kPairKernels[2] = {attn_paged_pairs_kernel<false>, attn_paged_p
 
 // rows of all parts
 size_t part_rows(const Plan& plan, int B, int Hq, int Lq) {
+  if (plan.joined) return 0;
   if (plan.mode != kPairs) return static_cast<size_t>(2 * plan.ctas) * (plan.mode == kRows16 ? 16 : 32);
   return plan.nsplit > 1 ? static_cast<size_t>(B) * Hq * Lq * plan.nsplit : 0;
 }
 
-// The plan of a debug call.
+// The plan of a debug call: `parts` parts of the keys or CTAs, negative: as many CTAs of a cluster.
 Plan forced(int Hq, int Hkv, int Lq, int mode, int parts) {
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
-  const int width = mode == kPairs ? 2 * kBM : mode == kRows16 ? 16 : 32;
-  return Plan{static_cast<Mode>(mode), static_cast<int>((packed + width - 1) / width), mode == kPairs ? parts : 1, mode == kPairs ? 0 : parts};
+  const int width = mode == kPairs ? 2 * kBM : mode == kRows16 ? 16 : 32, joined = parts < 0 ? -parts : 0;
+  return Plan{static_cast<Mode>(mode), static_cast<int>((packed + width - 1) / width), mode == kPairs ? std::abs(parts) : 1,
+              mode == kPairs || joined ? 0 : parts, joined};
 }
 
 size_t plan_bytes(const Plan& plan, int B, int Hq, int Lq) {
-  return part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2)) + (plan.mode != kPairs ? plan.ctas * sizeof(int4) : 0);
+  return part_rows(plan, B, Hq, Lq) * (kD * sizeof(float) + sizeof(float2)) + plan.ctas * sizeof(int4);
 }
 
 }  // namespace
@@ -1461,7 +1575,8 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   const bool few = plan.mode != kPairs;
   const int width = plan.mode == kRows16 ? 16 : 32;
   const long long rows = static_cast<long long>(a.B) * a.Hq * a.Lq;
-  const long long grid = few ? plan.ctas : static_cast<long long>(plan.n_groups) * a.Hkv * a.B * plan.nsplit;
+  const long long units = static_cast<long long>(plan.n_groups) * a.Hkv * a.B;
+  const long long grid = plan.joined ? units * plan.joined : few ? plan.ctas : units * plan.nsplit;
   if (grid > 0x7fffffffLL) return -2;
   static ContextCache<int> setup;
   int unused = 0;
@@ -1516,6 +1631,7 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   p.Lq = a.Lq;
   p.n_groups = plan.n_groups;
   p.nsplit = plan.nsplit;
+  p.joined = plan.joined;
   p.scale_log2 = log2e / root;
   p.cap_log2 = softcap * log2e;
   p.cap_in = cap ? 2.0f * log2e / (softcap * root) : 0.0f;
@@ -1525,14 +1641,22 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   p.cap_near = cap && p.cap_log2 >= 1.0f / 1024.0f ? kTanhRange / cap_x : -1.0f;
   float power = p.cap_log2 * cap_x;
   for (int i = 0; i < 4; ++i, power *= cap_x * cap_x) p.cap_poly[i] = p.cap_near > 0.0f ? tanh_poly[i] * power : 0.0f;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute pdl[1], attr[2];
   const int m = plan.mode == kRows16 ? 0 : 1;
   cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(few ? kRowsThreads : kPairsThreads),
-                                      few ? kRowsSmemBytes[m] : kPairSmemBytes, stream, attr);
+                                      few ? kRowsSmemBytes[m] : kPairSmemBytes, stream, pdl);
+  if (plan.joined) {
+    attr[0] = pdl[0];
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(plan.joined);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+  }
   cudaError_t e = cudaLaunchKernelEx(&cfg, few ? kRowsKernels[m][cap ? 1 : 0] : kPairKernels[cap ? 1 : 0], tq, tk, tv, p);
   if (e == cudaSuccess && parts > 0) {
     const dim3 join_grid = few ? dim3(width / kJoinWarps, plan.ctas) : dim3(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps));
-    cfg = pdl_config(join_grid, dim3(kJoinWarps * 32), 0, stream, attr);
+    cfg = pdl_config(join_grid, dim3(kJoinWarps * 32), 0, stream, pdl);
     e = cudaLaunchKernelEx(&cfg, few ? (m == 0 ? attn_paged_join_rows_kernel<16> : attn_paged_join_rows_kernel<32>) : attn_paged_join_pairs_kernel, p);
   }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;

@@ -624,7 +624,7 @@ int cover_debug_attn_paged(const void* q, const void* k_pages, const void* v_pag
                            const int32_t* seed_idx, int n_seeds, const int32_t* q0, int B, int Hq, int Hkv, int Lq, int D,
                            const int32_t* key_lo, const int32_t* key_hi, float softcap, void* out, float* lse,
                            void* workspace, size_t workspace_bytes, int mode, int parts, void* stream) {
-  if (mode < 0 || mode >= cover::kAttnPagedModes || parts < 1 || parts > (mode == cover::kAttnPagedModes - 1 ? 64 : 1024))
+  if (mode < 0 || mode >= cover::kAttnPagedModes || parts == 0 || parts < -8 || parts > (mode == cover::kAttnPagedModes - 1 ? 64 : 1024))
     return COVER_ERR_UNSUPPORTED;
   cover::AttnPagedArgs a{q,        k_pages, v_pages, table, n_pages, M,   page, lens,   k_seedmask, v_seedmask, seed_idx,
                          n_seeds,  q0,      B,       Hq,    Hkv,     Lq,  key_lo, key_hi, softcap,    out,        lse, workspace};

@@ -118,7 +118,28 @@ def test_against_oracle(shape, kind):
     _check(d, *_run(d, key_lo=lo, key_hi=hi), lo, hi)
 
 
-@pytest.mark.parametrize("cap", [30.0, 0.5, 1e4])
+FORCED = [(mode, parts) for mode in range(3) for parts in (1, 2, 7, 60, -1, -2, -3, -8)] + [(0, 152), (1, 700)]
+
+
+@pytest.mark.parametrize("mode,parts", FORCED)
+@pytest.mark.parametrize("shape", [([777], 28, 4, 1, 1, 16), ([300, 0, 129, 1], 12, 2, 5, 6, 32), ([1000, 130], 6, 2, 100, 20, 64), ([513] * 9, 2, 2, 1, 0, 256),
+                                   ([70, 640], 5, 1, 60, 9, 128)])
+@pytest.mark.parametrize("kind,cap", [(None, 0.0), ("any", 0.0), ("causal", 20.0)])
+def test_every_kernel(mode, parts, shape, kind, cap):
+    d = _inputs(*shape)
+    lo, hi = _ranges(kind, d)
+    for fill in (0, 255):      # what the workspace holds does not matter
+        B, Hq, Lq = d["q"].shape[:3]
+        n = 16 if parts < 0 else B * Hq * Lq * parts * 520 if mode == 2 else parts * (2 * (16 << mode) * 520 + 16)
+        out, lse = api.cover_debug_attn_paged(d["q"], d["kp"], d["vp"], d["table"], d["lens"], d["km"], d["vm"], d["seeds"], q0=d["q0"], mode=mode,
+                                              parts=parts, key_lo=lo, key_hi=hi, softcap=cap,
+                                              workspace=torch.full((n,), fill, device="cuda", dtype=torch.uint8))
+        torch.cuda.synchronize()
+        assert api.cover_device_status() == 0
+    _check(d, out, lse, lo, hi, cap)
+
+
+@pytest.mark.parametrize("cap", [30.0, 0.5, 1e4, 55.0, 56.0, 3e38, 1e-30])
 @pytest.mark.parametrize("Lq", [1, 4, 60])
 def test_capped_scores(cap, Lq):
     d = _inputs([700, 520], 14, 2, Lq, 12, 32, scale=4.0)
