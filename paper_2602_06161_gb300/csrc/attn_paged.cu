@@ -133,6 +133,14 @@ __device__ __forceinline__ bool screen_row(uint32_t tile, int key) {
   return bad;
 }
 
+// Four columns of tensor memory.
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait4(uint32_t (&r)[4]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3])::"memory");
+}
+
 // Whether any of 128 or 256 threads of a named barrier says so.
 template <int kAll>
 __device__ __forceinline__ bool any_of(int barrier, bool x) {
@@ -343,14 +351,21 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   long long t0, t1, all = 0, n_ctas = 0, c = blockIdx.x;
   int b0;
   long long before0 = 0;   // tiles before sequence b0's
+  int tile0 = 0;           // joined: the CTA's first tile of the sequence's
   if (p.joined) {
     // tiles counted from the sequence's first: a part of those of the cluster's unit
     const long long u = blockIdx.x / p.joined;
     const int rank = static_cast<int>(blockIdx.x % p.joined);
     b0 = static_cast<int>(u / heads);
-    const int tiles = tiles_of<false>(p, b0).x, share = tiles / p.joined, more = tiles % p.joined;
-    t0 = (u % heads) * tiles + rank * share + min(rank, more);
+    if (warp == kRowsCopyWarp) {   // the table is on its way while the length is
+      for (int i = lane * 32; i < min(p.M, 1024); i += 1024)
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.table + static_cast<size_t>(b0) * p.M + i));
+    }
+    const int2 tiles = tiles_of<false>(p, b0);
+    const int share = tiles.x / p.joined, more = tiles.x % p.joined, j = rank * share + min(rank, more);
+    t0 = (u % heads) * tiles.x + j;
     t1 = t0 + share + (rank < more ? 1 : 0);
+    tile0 = tiles.y + j;
   } else {
     const int each = (p.B + kRowsThreads - 1) / kRowsThreads;           // sequences of a thread
     const int b_lo = min(tid * each, p.B), b_hi = min(b_lo + each, p.B);
@@ -484,28 +499,47 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     // ---------------- copies ----------------
     bool ok = true;
     int issued = 0, q_issued = 0;   // tiles of K and V, units
+    const int rows_log2 = min(p.page_log2, 7);
+    const auto lookup = [&](int tile) { return lane < kBN >> rows_log2 ? page_of(p, b0, tile * kBN + (lane << rows_log2)) : -1; };
+    // joined: the pages of the CTA's tiles, looked up here and a tile ahead (a job from the planning warp takes a microsecond more)
+    int entry_v = -1, entry_k = -1, entry_next = p.joined && n > 0 ? lookup(tile0) : -1;
+    const long long u0 = p.joined ? blockIdx.x / p.joined % heads : 0;
     for (int i = 0; i < 2 * n && ok; ++i) {
       // K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1)
       const bool is_v = i > 0 && ((i & 1) == 0 || i == 2 * n - 1);
       const int g = i == 0 ? 0 : is_v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2;
       const int at = g % kRing, slot = i % kSlots;
-      if (!is_v) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);
+      if (is_v == (p.joined != 0)) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);   // (joined: for the arrival below alone)
       if (ok && i >= kSlots) ok = warp_wait(&sm.empty[slot], (i / kSlots - 1) & 1, &sm.abort);
       if (!ok) break;
-      const TileJob& job = sm.job[at];
-      if (!is_v && job.first) {
-        const int buf = job.unit & 1;
-        if (job.unit >= 2) ok = warp_wait(&sm.q_empty[buf], ((job.unit >> 1) - 1) & 1, &sm.abort);
+      int entry, key0, h;
+      if (p.joined) {
+        if (!is_v) {
+          entry_v = entry_k;
+          entry_k = entry_next;
+          if (g + 1 < n) entry_next = lookup(tile0 + g + 1);
+        }
+        entry = is_v && i < 2 * n - 1 ? entry_v : entry_k;
+        key0 = (tile0 + g) * kBN;
+        h = static_cast<int>(u0 / p.n_groups);
+      } else {
+        const TileJob& job = sm.job[at];
+        entry = job.page[lane % kMaxTilePages], key0 = job.key0, h = job.h;
+      }
+      if (!is_v && (p.joined ? i == 0 : sm.job[at].first != 0)) {
+        const int unit = p.joined ? 0 : sm.job[at].unit, buf = unit & 1;
+        const int q_row = p.joined ? static_cast<int>((static_cast<long long>(b0) * p.Hq + h * p.G) * p.Lq + (u0 % p.n_groups) * kN) : sm.job[at].q_row;
+        if (unit >= 2) ok = warp_wait(&sm.q_empty[buf], ((unit >> 1) - 1) & 1, &sm.abort);
         if (!ok) break;
         if (lane == 0) {
           mbar_arrive_expect_tx(&sm.q_full[buf], kN * kD * 2);
-          for (int h = 0; h < 2; ++h) tma_load_4d(sm.q[buf] + h * kN * 128, &tm_q, &sm.q_full[buf], 64 * h, job.q_row, 0, 0);
+          for (int half = 0; half < 2; ++half) tma_load_4d(sm.q[buf] + half * kN * 128, &tm_q, &sm.q_full[buf], 64 * half, q_row, 0, 0);
         }
-        q_issued = job.unit + 1;
+        q_issued = unit + 1;
       }
       if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], kTileBytes);
       __syncwarp();
-      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], job.key0, job.page[lane % kMaxTilePages], job.h, p.Hkv, p.page_log2, lane);
+      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], key0, entry, h, p.Hkv, p.page_log2, lane);
       __syncwarp();
       if (is_v && lane == 0) mbar_arrive(&sm.job_empty[at]);
       issued = i + 1;
@@ -770,14 +804,19 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 
       // ---------------- the rows' results ----------------
       tc_fence_after_sync();
+      // sums over the warp: each step adds up and hands on half of the rows, until a lane has one. (The code of a unit's end is kept short: in a call
+      // of a few tiles it runs once, out of a cold instruction cache. Unrolled over all rows it took 1.9 us.)
 #pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        if (i >= n_rows) break;
-        float x = l[i];
+      for (int d = 16, left = kN; left > 1; d >>= 1, left >>= 1) {
+        const bool upper = (lane & d) != 0;
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if (lane == (i & 31)) sm.red[stream][w4][i] = x;
+        for (int i = 0; i < left / 2; ++i) {
+          const float mine = upper ? l[i + left / 2] : l[i], other = upper ? l[i] : l[i + left / 2];
+          l[i] = mine + __shfl_xor_sync(0xffffffffu, other, d);
+        }
       }
+      if (kN == 16) l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
+      sm.red[stream][w4][kN == 16 ? lane >> 1 : lane] = l[0];
       sync_of<256>(1);
       // a stream without a tile here has seen nothing
       if (tid < n_rows) {
@@ -798,25 +837,25 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         else if (p.lse != nullptr) p.lse[orow0 + tid] = (top + lg2_approx(sum)) * 0.6931471805599453f;
       }
       sync_of<256>(1);
-      // thread = output column; the streams' warps take 16 rows in turn
-      for (int c0 = 16 * stream; c0 < n_rows; c0 += 32) {
-        uint32_t o[2][16];
-        tmem_ld16(quad + 2 * kN + c0, o[0]);
-        tmem_ld16(quad + 3 * kN + c0, o[1]);
-        tmem_ld_wait16(o[0]);
-        tmem_ld_wait16(o[1]);
+      // thread = output column; the streams' warps take four rows in turn
+#pragma unroll 1
+      for (int c0 = 4 * stream; c0 < n_rows; c0 += 8) {
+        uint32_t o[2][4];
+        tmem_ld4(quad + 2 * kN + c0, o[0]);
+        tmem_ld4(quad + 3 * kN + c0, o[1]);
+        tmem_ld_wait4(o[0]);
+        tmem_ld_wait4(o[1]);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 4; ++e) {
           const int i = c0 + e;
-          if (i < n_rows) {
-            const float4 f = sm.fin[i];
-            float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
-            if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
-            if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
-            if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
-            else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
-            else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
-          }
+          if (i >= n_rows) break;
+          const float4 f = sm.fin[i];
+          float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
+          if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
+          if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
+          if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
+          else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
+          else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
         }
         __syncwarp();
       }
