@@ -357,11 +357,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const long long u = blockIdx.x / p.joined;
     const int rank = static_cast<int>(blockIdx.x % p.joined);
     b0 = static_cast<int>(u / heads);
-    if (warp == kRowsCopyWarp) {   // the table is on its way while the length is
-      for (int i = lane * 32; i < min(p.M, 1024); i += 1024)
-        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.table + static_cast<size_t>(b0) * p.M + i));
-    }
+    int line = 0;
+    if (warp == kRowsCopyWarp && lane * 32 < p.M)   // the table's first lines are on their way to L1 while the length is
+      asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(line) : "l"(p.table + static_cast<size_t>(b0) * p.M + lane * 32));
     const int2 tiles = tiles_of<false>(p, b0);
+    asm volatile("" ::"r"(line));
     const int share = tiles.x / p.joined, more = tiles.x % p.joined, j = rank * share + min(rank, more);
     t0 = (u % heads) * tiles.x + j;
     t1 = t0 + share + (rank < more ? 1 : 0);
@@ -700,7 +700,6 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const int at = g % kRing;
         ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort) && warp_wait(&sm.s_full[stream], (g >> 1) & 1, &sm.abort);
         const bool partial = ok && sm.job[at].partial != 0;
-        if (partial) ok = warp_wait(&sm.v_clean[at], (g / kRing) & 1, &sm.abort);
         float t[kN];        // scores less the references, in log2 units
         bool over = !ok;    // a warp whose wait gave up votes all the same: the stream's barriers take 128 threads
         if (ok) {
@@ -719,11 +718,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           if (partial) {
             const int pos = sm.job[at].key0 + key;
             const bool held = ((sm.job[at].valid >> (key >> page_rows)) & 1u) != 0;
-            const bool nan = ((reinterpret_cast<const uint32_t*>(&sm.nan_keys[at])[key >> 5] >> (key & 31)) & 1u) != 0;
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
               const int4 row = sm.row[buf][i];
-              if (nan) t[i] = kNan;
               if (!held || pos < row.x || pos >= row.y || pos == row.z) t[i] = -INFINITY;
             }
           }
@@ -794,6 +791,21 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         fence_proxy_async_smem();
         tc_fence_before_sync();
         mbar_arrive(&sm.p_full[stream]);
+        if (partial) {
+          // V has been looked through by now: the rows that see a row of it that is not finite have a sum of NaN
+          ok = warp_wait(&sm.v_clean[at], (g / kRing) & 1, &sm.abort);
+          if (ok && ((reinterpret_cast<const uint32_t*>(&sm.nan_keys[at])[key >> 5] >> (key & 31)) & 1u) != 0) {
+            const int pos = sm.job[at].key0 + key;
+            const bool held = ((sm.job[at].valid >> (key >> page_rows)) & 1u) != 0;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+              const int4 row = sm.row[buf][i];
+              if (held && pos >= row.x && pos < row.y && pos != row.z) l[i] = kNan;
+            }
+          }
+          __syncwarp();
+          if (!ok && lane == 0) sm.abort = 1;   // (the next wait ends the loop, at a vote)
+        }
         if (lane == 0) mbar_arrive(&sm.job_empty[at]);
       }
       if (ok) ok = warp_wait(&sm.o_full, unit & 1, &sm.abort);
