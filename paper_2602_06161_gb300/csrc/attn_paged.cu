@@ -347,30 +347,29 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 
   // ---------------- the CTA's share of all tiles ----------------
   const int n_packed = p.G * p.Lq;
-  const long long heads = static_cast<long long>(p.Hkv) * p.n_groups;   // units of a sequence
+  const int heads = p.Hkv * p.n_groups;   // units of a sequence (at most B Hq Lq)
   long long t0, t1, all = 0, n_ctas = 0, c = blockIdx.x;
   int b0;
   long long before0 = 0;   // tiles before sequence b0's
   int tile0 = 0;           // joined: the CTA's first tile of the sequence's
   if (p.joined) {
     // tiles counted from the sequence's first: a part of those of the cluster's unit
-    const long long u = blockIdx.x / p.joined;
-    const int rank = static_cast<int>(blockIdx.x % p.joined);
-    b0 = static_cast<int>(u / heads);
+    const int u = static_cast<int>(blockIdx.x) / p.joined, rank = static_cast<int>(blockIdx.x) % p.joined;
+    b0 = u / heads;
     int line = 0;
     if (warp == kRowsCopyWarp && lane * 32 < p.M)   // the table's first lines are on their way to L1 while the length is
       asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(line) : "l"(p.table + static_cast<size_t>(b0) * p.M + lane * 32));
     const int2 tiles = tiles_of<false>(p, b0);
     asm volatile("" ::"r"(line));
     const int share = tiles.x / p.joined, more = tiles.x % p.joined, j = rank * share + min(rank, more);
-    t0 = (u % heads) * tiles.x + j;
+    t0 = static_cast<long long>(u % heads) * tiles.x + j;
     t1 = t0 + share + (rank < more ? 1 : 0);
     tile0 = tiles.y + j;
   } else {
     const int each = (p.B + kRowsThreads - 1) / kRowsThreads;           // sequences of a thread
     const int b_lo = min(tid * each, p.B), b_hi = min(b_lo + each, p.B);
     long long mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += tiles_of<true>(p, b).x * heads;
+    for (int b = b_lo; b < b_hi; ++b) mine += static_cast<long long>(tiles_of<true>(p, b).x) * heads;
     long long incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -389,7 +388,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     before += incl - mine;
     if (t0 < t1 && t0 >= before && t0 < before + mine) {
       int b = b_lo;
-      for (long long x; before + (x = tiles_of<true>(p, b).x * heads) <= t0; ++b) before += x;
+      for (long long x; before + (x = static_cast<long long>(tiles_of<true>(p, b).x) * heads) <= t0; ++b) before += x;
       sm.b0 = b;
       sm.before = before;
     }
@@ -408,8 +407,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     if (!p.joined && n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
     bool joined = false;
     for (long long t = t0; t < t1 && ok; ++unit) {
-      while (t >= first + tiles.x * heads) first += tiles.x * heads, tiles = tiles_of<false>(p, ++b);
-      const int u = static_cast<int>((t - first) / tiles.x), j = static_cast<int>((t - first) % tiles.x);
+      for (long long all_of; t >= first + (all_of = static_cast<long long>(tiles.x) * heads); ) first += all_of, tiles = tiles_of<false>(p, ++b);
+      int u, j;
+      if (t - first <= 0x7fffffffLL) u = static_cast<int>(t - first) / tiles.x, j = static_cast<int>(t - first) % tiles.x;
+      else u = static_cast<int>((t - first) / tiles.x), j = static_cast<int>((t - first) % tiles.x);
       const int nt = static_cast<int>(min(static_cast<long long>(tiles.x - j), t1 - t));
       const int h = u / p.n_groups, p0 = (u % p.n_groups) * kN, n_rows = min(kN, n_packed - p0);
       const long long rowbase = (static_cast<long long>(b) * p.Hq + h * p.G) * p.Lq;
@@ -503,7 +504,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const auto lookup = [&](int tile) { return lane < kBN >> rows_log2 ? page_of(p, b0, tile * kBN + (lane << rows_log2)) : -1; };
     // joined: the pages of the CTA's tiles, looked up here and a tile ahead (a job from the planning warp takes a microsecond more)
     int entry_v = -1, entry_k = -1, entry_next = p.joined && n > 0 ? lookup(tile0) : -1;
-    const long long u0 = p.joined ? blockIdx.x / p.joined % heads : 0;
+    const int u0 = p.joined ? static_cast<int>(blockIdx.x) / p.joined % heads : 0;
     for (int i = 0; i < 2 * n && ok; ++i) {
       // K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1)
       const bool is_v = i > 0 && ((i & 1) == 0 || i == 2 * n - 1);
@@ -521,7 +522,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         entry = is_v && i < 2 * n - 1 ? entry_v : entry_k;
         key0 = (tile0 + g) * kBN;
-        h = static_cast<int>(u0 / p.n_groups);
+        h = u0 / p.n_groups;
       } else {
         const TileJob& job = sm.job[at];
         entry = job.page[lane % kMaxTilePages], key0 = job.key0, h = job.h;
@@ -882,8 +883,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     }
     tc_fence_before_sync();
     if (p.joined) {
-      const long long u = blockIdx.x / p.joined % heads;
-      const int p0 = static_cast<int>(u % p.n_groups) * kN;
+      const int u = static_cast<int>(blockIdx.x) / p.joined % heads, p0 = u % p.n_groups * kN;
       __syncwarp();
       cluster_sync();   // every CTA's rows are staged
       join_rows<8>(p, staged, smem_u32(sm.ml), min(kN, n_packed - p0),
@@ -954,7 +954,7 @@ struct PairSmem {
   float red[2][2][kBM];                 // per Q tile and half of the columns
   int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
   int lo, hi;                           // keys that some row sees
-  int all_lo[2], all_hi[2];             // keys that every row of a Q tile sees that sees any
+  int all_lo, all_hi;                   // keys that every row sees that sees any
   int own_lo, own_hi;                   // seed rows' positions
   uint32_t tmem_base;
   int abort;
@@ -1131,9 +1131,9 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         mbar_init(&sm.v_clean[i], 1);
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], 256);
-        sm.all_lo[i] = 0;
-        sm.all_hi[i] = 0x7fffffff;
       }
+      sm.all_lo = 0;
+      sm.all_hi = 0x7fffffff;
       mbar_init(&sm.o_full, 1);
       mbar_init(&sm.drain, 1);
       sm.abort = 0;
@@ -1163,58 +1163,75 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   const bool softmax = warp < kPairSoftmaxWarps;
   const bool valid = softmax && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
+  int line = 0;
+  if (warp == kPairCopyWarp && lane * 32 < p.M)   // the table's first lines are on their way to L1 while the length is
+    asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(line) : "l"(p.table + static_cast<size_t>(b) * p.M + lane * 32));
   const int len = length_of(p, b);
+  asm volatile("" ::"r"(line));
   int row_lo = 0, row_hi = 0;
   if (valid) {
     const int2 keys = keys_of(p, static_cast<long long>(b) * p.Lq + r, len);
     row_lo = keys.x, row_hi = keys.y;
   }
-  if (p.n_seeds > 0) {
-    // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
-    const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
-    const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
-    const long long first = __ldg(p.q0 + b);
-    for (int s = tid; s < p.n_seeds; s += kPairsThreads) {
-      const long long at = __ldg(seeds + s) - first;
-      if (at < 0 || at >= p.Lq) continue;
-      const long long i = at >= r0 ? at - r0 : at - r0 + p.Lq;
-      if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
+  const bool some_keys = row_lo < row_hi;
+  int lo_key = 0, hi_key = len;   // keys that some row sees
+  if (p.key_lo != nullptr || p.key_hi != nullptr) {
+    if (softmax) {
+      const int lo = __reduce_min_sync(0xffffffffu, some_keys ? row_lo : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, row_hi);
+      if (lane == 0 && hi > 0) {
+        atomicMin(&sm.lo, lo);
+        atomicMax(&sm.hi, hi);
+      }
     }
     __syncthreads();
+    lo_key = sm.lo, hi_key = sm.hi;
   }
-  int slot = kNoSlot, pos = -1;   // of a seed row that sees its position
-  if (valid && p.n_seeds > 0) {
-    const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
-    const int s = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
-    if (s != kNoSlot && at >= row_lo && at < row_hi && page_of(p, b, at) >= 0) slot = s, pos = at;
-  }
-  const bool is_seed = slot != kNoSlot;
-  if (softmax) {
-    const bool some = row_lo < row_hi;
-    const int lo = __reduce_min_sync(0xffffffffu, some ? row_lo : 0x7fffffff), hi = __reduce_max_sync(0xffffffffu, row_hi);
-    const int all_lo = __reduce_max_sync(0xffffffffu, row_lo), all_hi = __reduce_min_sync(0xffffffffu, some ? row_hi : 0x7fffffff);
-    const int own_lo = __reduce_min_sync(0xffffffffu, is_seed ? pos : 0x7fffffff), own_hi = __reduce_max_sync(0xffffffffu, pos);
-    if (lane == 0 && hi > 0) {
-      atomicMin(&sm.lo, lo);
-      atomicMax(&sm.hi, hi);
-      atomicMax(&sm.all_lo[tile], all_lo);
-      atomicMin(&sm.all_hi[tile], all_hi);
-      if (own_hi >= 0) atomicMin(&sm.own_lo, own_lo), atomicMax(&sm.own_hi, own_hi);
-    }
-  }
-  __syncthreads();
-  const int2 part = part_of(sm.lo, sm.hi, ks, p.nsplit);
+  const int2 part = part_of(lo_key, hi_key, ks, p.nsplit);
   const int j0 = part.x, nt = part.y;
   const int page_rows = min(p.page_log2, 7), pages = kBN >> page_rows;   // of a KV tile
-  bool hole = false;   // some page with keys that rows see is not there
-  for (int i = tid; i < nt * pages; i += kPairsThreads) {
-    const int key = j0 * kBN + (i << page_rows);
-    if (key < sm.hi && sm.lo - key < 1 << page_rows) hole |= page_of(p, b, key) < 0;
-  }
-  const bool holes = __syncthreads_or(hole) != 0;
   const bool two_tiles = p0 + kBM < n_packed;   // the second Q tile has rows
-  // whether some row does not see some key of KV tile j of the part
-  const int all_lo = max(sm.all_lo[0], sm.all_lo[1]), all_hi = min(sm.all_hi[0], sm.all_hi[1]), own_lo = sm.own_lo, own_hi = sm.own_hi;
+  // What the softmax warps and the one that looks V through have to know besides; copies and products do not wait for it.
+  constexpr int kKnowing = 32 * (kPairSoftmaxWarps + 1);
+  int slot = kNoSlot, pos = -1;   // of a seed row that sees its position
+  bool holes = false;             // some page with keys that rows see is not there
+  if (softmax || warp == kPairScreenWarp) {
+    const int me = softmax ? tid : 32 * kPairSoftmaxWarps + lane;
+    if (p.n_seeds > 0) {
+      // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
+      const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
+      const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
+      const long long first = __ldg(p.q0 + b);
+      for (int s = me; s < p.n_seeds; s += kKnowing) {
+        const long long at = __ldg(seeds + s) - first;
+        if (at < 0 || at >= p.Lq) continue;
+        const long long i = at >= r0 ? at - r0 : at - r0 + p.Lq;
+        if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
+      }
+      sync_of<kKnowing>(1);
+      if (valid) {
+        const int s = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
+        if (s != kNoSlot && at >= row_lo && at < row_hi && page_of(p, b, at) >= 0) slot = s, pos = at;
+      }
+    }
+    if (softmax) {
+      const int all_lo = __reduce_max_sync(0xffffffffu, row_lo), all_hi = __reduce_min_sync(0xffffffffu, some_keys ? row_hi : 0x7fffffff);
+      const int own_lo = __reduce_min_sync(0xffffffffu, slot != kNoSlot ? pos : 0x7fffffff), own_hi = __reduce_max_sync(0xffffffffu, pos);
+      if (lane == 0) {
+        atomicMax(&sm.all_lo, all_lo);
+        atomicMin(&sm.all_hi, all_hi);
+        if (own_hi >= 0) atomicMin(&sm.own_lo, own_lo), atomicMax(&sm.own_hi, own_hi);
+      }
+    }
+    bool hole = false;
+    for (int i = me; i < nt * pages; i += kKnowing) {
+      const int key = j0 * kBN + (i << page_rows);
+      if (key < hi_key && lo_key - key < 1 << page_rows) hole |= page_of(p, b, key) < 0;
+    }
+    holes = any_of<kKnowing>(1, hole);
+  }
+  const bool is_seed = slot != kNoSlot;
+  // whether some row that sees a key does not see some key of KV tile j of the part
+  const int all_lo = sm.all_lo, all_hi = sm.all_hi, own_lo = sm.own_lo, own_hi = sm.own_hi;
   const auto partial = [&](int j) {
     const int key0 = (j0 + j) * kBN;
     return holes || key0 < all_lo || all_hi - key0 < kBN || (own_hi >= key0 && own_lo - key0 < kBN);
