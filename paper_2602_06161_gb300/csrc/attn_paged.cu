@@ -1580,21 +1580,48 @@ struct Plan {
   int joined;   // CTAs of a cluster that share a unit, or 0
 };
 
+// Clusters of 1 .. 8 CTAs, one CTA an SM, that are resident at once on every GPU measured.
+constexpr int kClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
+
+// The kernel and how the keys are shared, from the sizes and the table's width (the lengths are not known to the host: where they are shorter,
+// an even share of all tiles is better than predicted).
+//
+// Predicted microseconds, fitted to calls back to back on GB300, measured / predicted: rows of 16 joined, one token over 777 keys (28 / 4
+// heads, 7 CTAs a unit) 7.5 / 7.7, over 4096 (32 / 8, 8) 11.9 / 11.8, 16 sequences of 500 (1) 12.8 / 13.3; in even shares 11.0 / 13.5, 15.6 / 15.0, 18.7 / 16.4, 64
+// sequences of up to 8191 keys 192 / 251 (all of that length: 305). Rows of 32 joined 12.6 / 12.6 (32 rows over 2048, 32 / 8), in even shares 2 us a
+// tile. Pairs joined: 8 rows over 2048 (32 / 8, 8 CTAs a unit) 10.2 / 10.4, 32 over 1024 (28 / 4) 11.2 / 10.4, four sequences of 64 rows over 2048
+// (4) 19.8 / 16.1; by a second kernel 14.4 / 15.6 (32 over 1024 in 8 parts); 1216 rows over 8192 in one wave 118 / 111.
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
   const long long nkv = (static_cast<long long>(M) * page + kBN - 1) / kBN;   // KV tiles of a sequence at most
-  if (packed <= 32) {
-    const long long most = std::min<long long>(static_cast<long long>(B) * Hkv, kSms) * std::min<long long>(nkv, kSms);
-    return Plan{packed <= 16 ? kRows16 : kRows32, 1, 1, static_cast<int>(std::min<long long>(kSms, most)), 0};
-  }
-  Plan best{kPairs, static_cast<int>((packed + 2 * kBM - 1) / (2 * kBM)), 0, 0, 0};
   const double rows = static_cast<double>(B) * Hq * Lq;
-  const long long units = static_cast<long long>(best.n_groups) * Hkv * B;
+  Plan best{};
   double best_us = 0.0;
+  const auto consider = [&](const Plan& plan, double us) {
+    if (best.n_groups == 0 || us < best_us) best = plan, best_us = us;
+  };
+  if (packed <= 32) {
+    const bool few = packed <= 16;
+    const Mode mode = few ? kRows16 : kRows32;
+    const long long units = static_cast<long long>(B) * Hkv;
+    const double tile = few ? 1.48 : 1.95, fill = B > 1 ? 0.75 : 1.0;
+    const int ctas = static_cast<int>(std::min<long long>(kSms, std::min<long long>(units, kSms) * std::min<long long>(nkv, kSms)));
+    consider(Plan{mode, 1, 1, ctas, 0}, (few ? 12.0 : 15.0) + tile * std::ceil(fill * static_cast<double>(units) * nkv / kSms));
+    for (int c = 1; c <= kMaxJoined && c <= nkv; ++c) {
+      const double waves = std::ceil(static_cast<double>(units) / kClusters[c - 1]);
+      consider(Plan{mode, 1, 1, 0, c}, (few ? 6.3 : 9.8) + (units * c > kSms / 2 ? 1.5 : 0.0) + 3.0 * (waves - 1) + 1.38 * waves * std::ceil(static_cast<double>(nkv) / c));
+    }
+    if (few) return best;
+  }
+  const int groups = static_cast<int>((packed + 2 * kBM - 1) / (2 * kBM));
+  const long long units = static_cast<long long>(groups) * Hkv * B;
   for (int ns = 1; ns <= nkv && ns <= 64; ++ns) {
-    const long long waves = (units * ns + kSms - 1) / kSms, tiles = (nkv + ns - 1) / ns;
-    const double us = 5.0 + waves * (3.5 + 1.6 * tiles) + (ns > 1 ? 2.4 + 0.15 * ns + 1.9e-4 * rows * ns : 0.0);
-    if (best.nsplit == 0 || us < best_us) best.nsplit = ns, best_us = us;
+    const double waves = std::ceil(static_cast<double>(units * ns) / kSms), tiles = std::ceil(static_cast<double>(nkv) / ns);
+    consider(Plan{kPairs, groups, ns, 0, 0}, 5.0 + waves * (3.5 + 1.6 * tiles) + (ns > 1 ? 2.4 + 0.15 * ns + 1.9e-4 * rows * ns : 0.0));
+    if (ns > 1 && ns <= kMaxJoined) {
+      const double turns = std::ceil(static_cast<double>(units) / kClusters[ns - 1]);
+      consider(Plan{kPairs, groups, ns, 0, ns}, 7.2 + (units * ns > kSms / 2 ? 2.5 : 0.0) + 3.5 * (turns - 1) + 1.6 * turns * tiles);
+    }
     if (units * ns > 8 * kSms) break;
   }
   return best;
