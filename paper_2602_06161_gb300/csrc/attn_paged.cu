@@ -96,9 +96,9 @@ __device__ __forceinline__ int page_of(const Params& p, int b, int key) {
   const int e = i < p.M ? __ldg(p.table + static_cast<size_t>(b) * p.M + i) : -1;
   return e >= 0 && e < p.n_pages ? e : -1;
 }
-// Position of query row r of sequence b, or -1 where it is none that a key can have.
-__device__ __forceinline__ int position_of(const Params& p, int b, int r) {
-  const long long at = static_cast<long long>(__ldg(p.q0 + b)) + r;
+// Position of query row r of a sequence whose first is at q0, or -1 where it is none that a key can have.
+__device__ __forceinline__ int position_of(int q0, int r) {
+  const long long at = static_cast<long long>(q0) + r;
   return at >= 0 && at <= 0x7fffffffLL ? static_cast<int>(at) : -1;
 }
 
@@ -416,7 +416,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       const long long rowbase = (static_cast<long long>(b) * p.Hq + h * p.G) * p.Lq;
       const int len = length_of(p, b), buf = unit % kUnits;
       const int pages = kBN >> min(p.page_log2, 7);
-      // (looked up before the rows, whose keys and seeds take loads of their own)
+      // (loads that depend on nothing else first)
+      int first_pos = 0, first_seed = 0;
+      if (p.n_seeds > 0) {
+        first_pos = __ldg(p.q0 + b);
+        if (lane < p.n_seeds) first_seed = __ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + lane);
+      }
       int entry = lane < pages ? page_of(p, b, (tiles.y + j) * kBN + (lane << min(p.page_log2, 7))) : -1;
       if (unit >= kUnits) ok = warp_wait(&sm.unit_empty[buf], (unit / kUnits - 1) & 1, &sm.abort);
       if (!ok) break;
@@ -426,7 +431,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         if (lane < kN) sm.slot[lane] = kNoSlot;
         __syncwarp();
         for (int s = lane; s < p.n_seeds; s += 32) {
-          const long long at = static_cast<long long>(__ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + s)) - __ldg(p.q0 + b);
+          const int seed = s == lane ? first_seed : __ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + s);
+          const long long at = static_cast<long long>(seed) - first_pos;
           if (at < 0 || at >= p.Lq) continue;
           const int i = static_cast<int>(at >= r0 ? at - r0 : at - r0 + p.Lq);
           if (i < kN) atomicMin(&sm.slot[i], s);
@@ -441,7 +447,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           const int2 k = keys_of(p, static_cast<long long>(b) * p.Lq + r, len);
           row.x = k.x, row.y = k.y;
           if (p.n_seeds > 0) {
-            const int slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
+            const int slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(first_pos, r);
             if (slot != kNoSlot && at >= k.x && at < k.y && page_of(p, b, at) >= 0) {
               row.z = at, row.w = slot;
               own_lo = own_hi = at;
@@ -1067,23 +1073,24 @@ __device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const
   return store_weights(s, p_addr, u, c0);
 }
 
-// A seed row's own score in log2 units: q row `row` of [B Hq Lq], masked-input key row `self`.
-template <bool kCap>
-__device__ __forceinline__ float self_score(const Params& p, long long row, size_t self) {
-  const uint4* qr = reinterpret_cast<const uint4*>(p.q + row * kD);
-  const uint4* kr = reinterpret_cast<const uint4*>(p.k_seedmask + self * kD);
+// 64 columns' share of a seed row's own product: q from its half of a swizzled Q tile (row R), the masked-input key from global memory.
+__device__ __forceinline__ float self_product(const uint8_t* q_half, int R, const __nv_bfloat16* k) {
+  const uint32_t q = smem_u32(q_half) + R * 128;
+  uint4 c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = __ldg(reinterpret_cast<const uint4*>(k) + i);
   float d0 = 0.0f, d1 = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i < kD / 8; ++i) {
-    const uint4 a = __ldg(qr + i), c = __ldg(kr + i);
-    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 a = lds128(q + ((i ^ (R & 7)) << 4));
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       d0 = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), d0);
       d1 = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), d1);
     }
   }
-  return kCap ? capped(d0 + d1, p.cap_in, p.cap_log2) : (d0 + d1) * p.scale_log2;
+  return d0 + d1;
 }
 
 // o += w v for 32 columns of a masked-input value.
@@ -1163,6 +1170,14 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   const bool softmax = warp < kPairSoftmaxWarps;
   const bool valid = softmax && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
+  constexpr int kKnowing = 32 * (kPairSoftmaxWarps + 1);   // threads of the softmax warps and of the one that looks V through
+  const int me = softmax ? tid : 32 * kPairSoftmaxWarps + lane;
+  // loads that depend on nothing first: the sequence's first position and a seed, the table, the length
+  int first_pos = 0, first_seed = 0;
+  if (p.n_seeds > 0) {
+    first_pos = __ldg(p.q0 + b);
+    if (me < p.n_seeds) first_seed = __ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + me);
+  }
   int line = 0;
   if (warp == kPairCopyWarp && lane * 32 < p.M)   // the table's first lines are on their way to L1 while the length is
     asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(line) : "l"(p.table + static_cast<size_t>(b) * p.M + lane * 32));
@@ -1191,26 +1206,26 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   const int page_rows = min(p.page_log2, 7), pages = kBN >> page_rows;   // of a KV tile
   const bool two_tiles = p0 + kBM < n_packed;   // the second Q tile has rows
   // What the softmax warps and the one that looks V through have to know besides; copies and products do not wait for it.
-  constexpr int kKnowing = 32 * (kPairSoftmaxWarps + 1);
   int slot = kNoSlot, pos = -1;   // of a seed row that sees its position
   bool holes = false;             // some page with keys that rows see is not there
   if (softmax || warp == kPairScreenWarp) {
-    const int me = softmax ? tid : 32 * kPairSoftmaxWarps + lane;
     if (p.n_seeds > 0) {
       // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
       const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
       const int32_t* seeds = p.seed_idx + static_cast<size_t>(b) * p.n_seeds;
-      const long long first = __ldg(p.q0 + b);
+      const int own_at = position_of(first_pos, r);
+      const bool own = valid && own_at >= row_lo && own_at < row_hi;   // the row sees its position, if it has a page
+      const int own_page = own ? page_of(p, b, own_at) : -1;
       for (int s = me; s < p.n_seeds; s += kKnowing) {
-        const long long at = __ldg(seeds + s) - first;
+        const long long at = static_cast<long long>(s == me ? first_seed : __ldg(seeds + s)) - first_pos;
         if (at < 0 || at >= p.Lq) continue;
         const long long i = at >= r0 ? at - r0 : at - r0 + p.Lq;
         if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
       }
       sync_of<kKnowing>(1);
-      if (valid) {
-        const int s = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq], at = position_of(p, b, r);
-        if (s != kNoSlot && at >= row_lo && at < row_hi && page_of(p, b, at) >= 0) slot = s, pos = at;
+      if (own_page >= 0) {
+        slot = sm.slot[r >= r0 ? r - r0 : r - r0 + p.Lq];
+        if (slot != kNoSlot) pos = own_at;
       }
     }
     if (softmax) {
@@ -1373,15 +1388,31 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   } else {
     // ---------------- softmax ----------------
     const size_t self = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds + (is_seed ? slot : 0);
-    // the seed rows' own scores (log2 units), in the first part alone
-    const float s_self = ks == 0 && is_seed ? self_score<kCap>(p, rowbase + P, self) : -INFINITY;
+    // the seed rows' own scores (log2 units), in the first part of the keys that is not empty alone: Q is there, and each of a row's threads takes half
+    // of the columns
+    float s_self = -INFINITY;
+    bool ok = true;
+    if (own_hi >= 0 && ks == 0) {
+      ok = nt == 0 || warp_wait(&sm.q_full, 0, &sm.abort);
+      float product = 0.0f;
+      if (ok && nt > 0 && is_seed) {
+        product = self_product(sm.q[tile] + half * kBoxBytes, R, p.k_seedmask + self * kD + half * kHalf);
+        prefetch_l2(p.v_seedmask + self * kD + half * kHalf);
+      }
+      sm.red[tile][half][R] = product;
+      sync_of<256>(2 + tile);
+      if (is_seed) {
+        const float s = sm.red[tile][0][R] + sm.red[tile][1][R];
+        s_self = kCap ? capped(s, p.cap_in, p.cap_log2) : s * p.scale_log2;
+      }
+      sync_of<256>(2 + tile);
+    }
     const bool warp_live = __any_sync(0xffffffffu, valid);
     const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = quad + tile * kBN + half * kHalf;
     const uint32_t o_addr = quad + 2 * kBN + tile * kD + half * kHalf;
     const bool fixed = kCap && p.cap_ref >= 0.0f;
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
-    bool ok = true;
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
     for (int j = 0; j < jend; ++j) {
       ok = warp_wait(&sm.s_full[tile], j & 1, &sm.abort);
