@@ -133,6 +133,33 @@ __device__ __forceinline__ bool screen_row(uint32_t tile, int key) {
   return bad;
 }
 
+// The same for eight keys, by a warp: 2 KB in order, of which lane l reads 16 bytes of keys l / 8 and 4 + l / 8, of either half. Writes a byte
+// of what was found.
+__device__ __forceinline__ void screen_group(uint32_t group, uint8_t* found, int lane) {
+  uint32_t hit[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 c = lds128(group + 512 * i + 16 * lane);
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hit[i & 1] |= (w[e] & 0x7fff7fffu) + 0x00800080u;
+  }
+  uint32_t bad = 0;
+  if (__any_sync(0xffffffffu, ((hit[0] | hit[1]) & 0x80008000u) != 0)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t lanes = __ballot_sync(0xffffffffu, (hit[h] & 0x80008000u) != 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) bad |= ((lanes >> (8 * k)) & 0xffu) != 0 ? 1u << (4 * h + k) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((bad >> (4 * (i & 1) + (lane >> 3))) & 1u) sts128(group + 512 * i + 16 * lane, 0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (lane == 0) *found = static_cast<uint8_t>(bad);
+}
+
 // Four columns of tensor memory.
 __device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&r)[4]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
@@ -946,8 +973,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_paged_join_rows_kernel(c
 // 19 looks V tiles through.
 // Shared memory: Q (2 x 32 KB) | two tiles of K, two of V. Tensor memory: S0 | S1 (the P of a half overwrites the first 32 columns of that
 // half's scores, behind its loads) | O0 | O1, 128 columns each.
-constexpr int kPairsThreads = 640;
-constexpr int kPairSoftmaxWarps = 16, kPairMmaWarp = 16, kPairCopyWarp = 17, kPairScreenWarp = 19;
+constexpr int kPairsThreads = 608;
+constexpr int kPairSoftmaxWarps = 16, kPairMmaWarp = 16, kPairCopyWarp = 17;
 
 struct PairSmem {
   uint8_t q[2][kTileBytes];
@@ -973,35 +1000,32 @@ __device__ __forceinline__ int2 part_of(int lo, int hi, int ks, int nsplit) {
   return make_int2(t0 + ks * each + min(ks, more), each + (ks < more ? 1 : 0));
 }
 
-// What a row does not see of 64 columns of a KV tile: columns outside [lo, hi), its own one if it is a seed row (own, or -1), those without
-// a page (bit i of holes: keys i * 2^page_rows on of these 64); whether anything of it holds for some row of the warp.
-struct Unseen {
-  int lo, hi, own;
-  uint32_t holes;
-  int page_rows;
-  bool any;
+// What a row sees of 64 columns of a KV tile, a bit each, and whether some row of the warp does not see some
+// column of the first or the second 32.
+struct Seen {
+  uint32_t first, second;
+  bool some_first, some_second;
 };
 
-// Masks the scores of 32 columns from column c0 on.
-__device__ __forceinline__ void mask_scores(float (&s)[32], const Unseen& u, int c0) {
-  if (u.any) {
-    const int lo = u.lo - c0, hi = u.hi - c0, own = u.own - c0;
+// Bits lo <= c < hi of 32.
+__device__ __forceinline__ uint32_t bits_of(int lo, int hi) {
+  const uint32_t below = hi >= 32 ? 0xffffffffu : hi <= 0 ? 0u : (1u << hi) - 1u;
+  return lo <= 0 ? below : lo >= 32 ? 0u : below & ~((1u << lo) - 1u);
+}
+
+// Masks the scores of 32 columns: a bit a column (compared with a row's range and its own position one by one, in both passes over the
+// scores, the columns took a KV tile from 1.6 to 3.6 us).
+__device__ __forceinline__ void mask_scores(float (&s)[32], const Seen& u, int c0) {
+  if (c0 == 0 ? u.some_first : u.some_second) {
+    const uint32_t seen = c0 == 0 ? u.first : u.second;
 #pragma unroll
     for (int c = 0; c < 32; ++c)
-      if (c < lo || c >= hi || c == own) s[c] = -INFINITY;
-    if (u.holes != 0) {
-#pragma unroll
-      for (int c = 0; c < 32; c += 16)
-        if ((u.holes >> ((c0 + c) >> u.page_rows)) & 1u) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[c + e] = -INFINITY;
-        }
-    }
+      if (!((seen >> c) & 1u)) s[c] = -INFINITY;
   }
 }
 
 // The largest of 32 columns' scores, neither scaled nor capped yet.
-__device__ __forceinline__ float chunk_max(uint32_t addr, const Unseen& u, int c0) {
+__device__ __forceinline__ float chunk_max(uint32_t addr, const Seen& u, int c0) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
@@ -1012,7 +1036,7 @@ __device__ __forceinline__ float chunk_max(uint32_t addr, const Unseen& u, int c
 
 // The weights of 32 columns whose scores less the reference, in log2 units, are s: in bf16 to tensor memory (V's operands are, so P's have to be: a
 // weight is off by at most 2^-8 of itself). Returns their sum before rounding.
-__device__ __forceinline__ float store_weights(float (&s)[32], uint32_t p_addr, const Unseen& u, int c0) {
+__device__ __forceinline__ float store_weights(float (&s)[32], uint32_t p_addr, const Seen& u, int c0) {
   mask_scores(s, u, c0);
   uint64_t acc2[2] = {0, 0};
   uint32_t packed[16];
@@ -1030,7 +1054,7 @@ __device__ __forceinline__ float store_weights(float (&s)[32], uint32_t p_addr, 
 }
 
 // chunk_exp where some score is beyond the polynomial's range (kept out of the loop's code).
-__device__ __noinline__ float chunk_exp_far(uint32_t addr, uint32_t p_addr, float cap_in, float cap_log2, const Unseen u, int c0, float m) {
+__device__ __noinline__ float chunk_exp_far(uint32_t addr, uint32_t p_addr, float cap_in, float cap_log2, const Seen u, int c0, float m) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
@@ -1044,7 +1068,7 @@ __device__ __noinline__ float chunk_exp_far(uint32_t addr, uint32_t p_addr, floa
 // polynomial's range take it, x P(x^2) with the scale's powers in its coefficients, and no special function (with three of them a score a KV
 // tile took 3.2 us).
 template <bool kCap>
-__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Unseen& u, int c0, float m, bool valid) {
+__device__ __forceinline__ float chunk_exp(uint32_t addr, uint32_t p_addr, const Params& p, const Seen& u, int c0, float m, bool valid) {
   uint32_t raw[32];
   tmem_ld32(addr, raw);
   tmem_ld_wait(raw);
@@ -1135,7 +1159,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         mbar_init(&sm.k_empty[i], 1);
         mbar_init(&sm.v_full[i], 1);
         mbar_init(&sm.v_empty[i], 1);
-        mbar_init(&sm.v_clean[i], 1);
+        mbar_init(&sm.v_clean[i], p0 + kBM < n_packed ? kPairSoftmaxWarps : kPairSoftmaxWarps / 2);
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], 256);
       }
@@ -1170,13 +1194,12 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   const bool softmax = warp < kPairSoftmaxWarps;
   const bool valid = softmax && P < n_packed;
   const int r = valid ? P % p.Lq : 0;
-  constexpr int kKnowing = 32 * (kPairSoftmaxWarps + 1);   // threads of the softmax warps and of the one that looks V through
-  const int me = softmax ? tid : 32 * kPairSoftmaxWarps + lane;
+  constexpr int kKnowing = 32 * kPairSoftmaxWarps;   // the softmax warps' threads
   // loads that depend on nothing first: the sequence's first position and a seed, the table, the length
   int first_pos = 0, first_seed = 0;
   if (p.n_seeds > 0) {
     first_pos = __ldg(p.q0 + b);
-    if (me < p.n_seeds) first_seed = __ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + me);
+    if (tid < p.n_seeds) first_seed = __ldg(p.seed_idx + static_cast<size_t>(b) * p.n_seeds + tid);
   }
   int line = 0;
   if (warp == kPairCopyWarp && lane * 32 < p.M)   // the table's first lines are on their way to L1 while the length is
@@ -1205,10 +1228,10 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   const int j0 = part.x, nt = part.y;
   const int page_rows = min(p.page_log2, 7), pages = kBN >> page_rows;   // of a KV tile
   const bool two_tiles = p0 + kBM < n_packed;   // the second Q tile has rows
-  // What the softmax warps and the one that looks V through have to know besides; copies and products do not wait for it.
+  // What the softmax warps have to know besides; copies and products do not wait for it.
   int slot = kNoSlot, pos = -1;   // of a seed row that sees its position
   bool holes = false;             // some page with keys that rows see is not there
-  if (softmax || warp == kPairScreenWarp) {
+  if (softmax) {
     if (p.n_seeds > 0) {
       // the CTA's rows stand at up to 256 positions: r itself, or r - r0 around Lq
       const int r0 = p.Lq <= 2 * kBM ? 0 : p0 % p.Lq;
@@ -1216,8 +1239,8 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       const int own_at = position_of(first_pos, r);
       const bool own = valid && own_at >= row_lo && own_at < row_hi;   // the row sees its position, if it has a page
       const int own_page = own ? page_of(p, b, own_at) : -1;
-      for (int s = me; s < p.n_seeds; s += kKnowing) {
-        const long long at = static_cast<long long>(s == me ? first_seed : __ldg(seeds + s)) - first_pos;
+      for (int s = tid; s < p.n_seeds; s += kKnowing) {
+        const long long at = static_cast<long long>(s == tid ? first_seed : __ldg(seeds + s)) - first_pos;
         if (at < 0 || at >= p.Lq) continue;
         const long long i = at >= r0 ? at - r0 : at - r0 + p.Lq;
         if (i < 2 * kBM) atomicMin(&sm.slot[i], s);
@@ -1228,17 +1251,15 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         if (slot != kNoSlot) pos = own_at;
       }
     }
-    if (softmax) {
-      const int all_lo = __reduce_max_sync(0xffffffffu, row_lo), all_hi = __reduce_min_sync(0xffffffffu, some_keys ? row_hi : 0x7fffffff);
-      const int own_lo = __reduce_min_sync(0xffffffffu, slot != kNoSlot ? pos : 0x7fffffff), own_hi = __reduce_max_sync(0xffffffffu, pos);
-      if (lane == 0) {
-        atomicMax(&sm.all_lo, all_lo);
-        atomicMin(&sm.all_hi, all_hi);
-        if (own_hi >= 0) atomicMin(&sm.own_lo, own_lo), atomicMax(&sm.own_hi, own_hi);
-      }
+    const int all_lo = __reduce_max_sync(0xffffffffu, row_lo), all_hi = __reduce_min_sync(0xffffffffu, some_keys ? row_hi : 0x7fffffff);
+    const int own_lo = __reduce_min_sync(0xffffffffu, slot != kNoSlot ? pos : 0x7fffffff), own_hi = __reduce_max_sync(0xffffffffu, pos);
+    if (lane == 0) {
+      atomicMax(&sm.all_lo, all_lo);
+      atomicMin(&sm.all_hi, all_hi);
+      if (own_hi >= 0) atomicMin(&sm.own_lo, own_lo), atomicMax(&sm.own_hi, own_hi);
     }
     bool hole = false;
-    for (int i = me; i < nt * pages; i += kKnowing) {
+    for (int i = tid; i < nt * pages; i += kKnowing) {
       const int key = j0 * kBN + (i << page_rows);
       if (key < hi_key && lo_key - key < 1 << page_rows) hole |= page_of(p, b, key) < 0;
     }
@@ -1358,31 +1379,6 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         if (which == 0) mbar_wait(&sm.q_full, 0, nullptr);
         for (int f = max(0, j - 2); f < j; ++f) mbar_wait(&full[f & 1], (f >> 1) & 1, nullptr);
       }
-    } else if (warp == kPairScreenWarp) {
-      // ---------------- V rows that are not finite (a lane four keys) ----------------
-      bool ok = true;
-      for (int j = 0; j < nt; ++j) {
-        const int st = j & 1;
-        if (j >= 2) ok = warp_wait(&sm.v_empty[st], ((j >> 1) - 1) & 1, &sm.abort);   // no tile ahead of the copies
-        if (ok && partial(j)) {
-          ok = warp_wait(&sm.v_full[st], (j >> 1) & 1, &sm.abort);
-          if (ok) {
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t hit = __ballot_sync(0xffffffffu, screen_row(smem_u32(sm.v[st]), 32 * i + lane));
-              if (lane == i) reinterpret_cast<uint32_t*>(&sm.nan_keys[j & 3])[i] = hit;
-            }
-            fence_proxy_async_smem();
-          }
-        }
-        if (!ok) break;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.v_clean[st]);
-      }
-      if (!ok && lane == 0) {
-        if (!sm.abort) report_status(p.status, kStatusTimeout, 87);
-        sm.abort = 1;
-      }
     }
     __syncwarp();
   } else {
@@ -1414,20 +1410,61 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const bool fixed = kCap && p.cap_ref >= 0.0f;
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
-    for (int j = 0; j < jend; ++j) {
-      ok = warp_wait(&sm.s_full[tile], j & 1, &sm.abort);
-      tc_fence_after_sync();   // zeros are stored over S too, where no row sees a key
-      const int key0 = (j0 + j) * kBN + half * kHalf;
-      const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch of this half are seen
-      // (a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything)
-      const bool some = __any_sync(0xffffffffu, valid && max(cl, 0) < min(ch, kHalf));
-      Unseen u{cl, ch, is_seed ? pos - key0 : -1, 0u, page_rows, false};
-      u.any = __any_sync(0xffffffffu, valid && (cl > 0 || ch < kHalf || (u.own >= 0 && u.own < kHalf)));
-      if (holes) {
-        const int i = lane << page_rows;   // the half's pages, a lane each (pages of 128 and 256: one)
-        u.holes = __ballot_sync(0xffffffffu, (lane == 0 || i < kHalf) && page_of(p, b, key0 + i) < 0);
-        u.any |= u.holes != 0;
+    // Where some row does not see some key, V is looked through for rows that are not finite while the scores are waited for: a warp eight
+    // keys, or sixteen (a warp for all of it took a tile 1.5 us). What was found is read a tile later, when V's products are through.
+    const auto found = [&](int j) {
+      if (!partial(j)) return;
+      if (!warp_wait(&sm.v_clean[j & 1], (j >> 1) & 1, &sm.abort)) {
+        ok = false;
+        return;
       }
+      // a row that sees one of these keys has a sum of NaN (both threads of it look, for all 128)
+      const uint4 nan = sm.nan_keys[j & 3];
+      if ((nan.x | nan.y | nan.z | nan.w) == 0) return;
+#pragma unroll 1
+      for (int w = 0; w < 4; ++w) {
+        for (uint32_t bits = w == 0 ? nan.x : w == 1 ? nan.y : w == 2 ? nan.z : nan.w; bits != 0; bits &= bits - 1) {
+          const int at = (j0 + j) * kBN + 32 * w + __ffs(bits) - 1;
+          if (at >= row_lo && at < row_hi && !(is_seed && at == pos)) l_run = kNan;
+        }
+      }
+    };
+    const bool keyless = __any_sync(0xffffffffu, valid && !some_keys);   // a row of the warp sees no key at all
+    for (int j = 0; j < jend; ++j) {
+      const int key0 = (j0 + j) * kBN + half * kHalf;
+      const bool masked = partial(j);
+      Seen u{0xffffffffu, 0xffffffffu, false, false};
+      bool some = warp_live;   // a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything
+      if (masked) {
+        ok = warp_wait(&sm.v_full[j & 1], (j >> 1) & 1, &sm.abort);   // (its copy waits for the products of tile j - 2 alone)
+        if (ok)
+          for (int g = warp; g < kBN / 8; g += two_tiles ? kPairSoftmaxWarps : kPairSoftmaxWarps / 2)
+            screen_group(smem_u32(sm.v[j & 1]) + g * kGroupBytes, reinterpret_cast<uint8_t*>(&sm.nan_keys[j & 3]) + g, lane);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.v_clean[j & 1]);
+      if (masked || keyless) {
+        const int cl = row_lo - key0, ch = row_hi - key0;   // columns cl <= c < ch of this half are seen
+        u.first = bits_of(cl, ch);
+        u.second = bits_of(cl - 32, ch - 32);
+        if (is_seed && pos - key0 >= 0 && pos - key0 < kHalf) {
+          const uint32_t own = ~(1u << (pos & 31));
+          if (pos - key0 < 32) u.first &= own;
+          else u.second &= own;
+        }
+        if (holes) {
+          const uint32_t there = __ballot_sync(0xffffffffu, page_of(p, b, key0 + 2 * lane) >= 0);   // two keys a lane
+          // pages are of 16 keys at least: eight lanes'
+          u.first &= ((there & 0xffu) != 0 ? 0xffffu : 0u) | ((there & 0xff00u) != 0 ? 0xffff0000u : 0u);
+          u.second &= ((there & 0xff0000u) != 0 ? 0xffffu : 0u) | ((there & 0xff000000u) != 0 ? 0xffff0000u : 0u);
+        }
+        u.some_first = __any_sync(0xffffffffu, valid && u.first != 0xffffffffu);
+        u.some_second = __any_sync(0xffffffffu, valid && u.second != 0xffffffffu);
+        some = __any_sync(0xffffffffu, valid && (u.first | u.second) != 0);
+      }
+      ok = warp_wait(&sm.s_full[tile], j & 1, &sm.abort) && ok;
+      if (ok && j > 0) found(j - 1);
+      tc_fence_after_sync();   // zeros are stored over S too, where no row sees a key
       if (fixed) {
         if (!ok) break;
       } else {
@@ -1477,26 +1514,12 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         tmem_st16(s_addr, zeros);
         tmem_st16(s_addr + 16, zeros);
       }
-      if (partial(j)) {
-        // V was looked through: a row that sees one of these keys has a sum of NaN (both threads of it look, for all 128)
-        ok = warp_wait(&sm.v_clean[j & 1], (j >> 1) & 1, &sm.abort);
-        if (!ok && lane == 0) sm.abort = 1;   // (the next wait ends the loop, at a vote)
-        if (ok) {
-          const uint32_t* nan = reinterpret_cast<const uint32_t*>(&sm.nan_keys[j & 3]);
-#pragma unroll 1
-          for (int w = 0; w < 4; ++w) {
-            for (uint32_t bits = nan[w]; bits != 0; bits &= bits - 1) {
-              const int at = (j0 + j) * kBN + 32 * w + __ffs(bits) - 1;
-              if (at >= row_lo && at < row_hi && !(is_seed && at == pos)) l_run = kNan;
-            }
-          }
-        }
-      }
       tmem_st_wait();
       tc_fence_before_sync();
       mbar_arrive(&sm.p_full[tile]);
     }
     if (ok && nt > 0) ok = warp_wait(&sm.o_full, 0, &sm.abort);
+    if (ok && jend > 0) found(jend - 1);
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 88);
       sm.abort = 1;
@@ -1522,6 +1545,18 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const bool split = p.nsplit > 1;
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);   // 1 / l, once a row; zero where no key was seen
     const uint32_t staged = smem_u32(sm.q[0]);   // joined: every product is complete, Q and K are not read any more
+    // A warp's 32 rows of 128 bytes are turned in shared memory, where Q was, so that it stores whole lines (each thread its own row, 16 bytes
+    // at a time: 3.6 us a CTA).
+    const uint32_t turned = staged + warp * 4096 + lane * 128;
+    const auto store_turned = [&](uint8_t* dst, int row_bytes) {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = 4 * i + (lane >> 3), at = P - lane + row;
+        const uint4 x = lds128(staged + warp * 4096 + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+        if (at < n_packed) *reinterpret_cast<uint4*>(dst + static_cast<long long>(at) * row_bytes + 16 * (lane & 7)) = x;
+      }
+    };
     if (ok && warp_live) {
 #pragma unroll 1
       for (int c = 0; c < 2; ++c) {
@@ -1540,16 +1575,19 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
           for (int e = 0; e < 8; ++e)
             sts128(staged + staged_at(tile * kBM + R, col / 4 + e), __float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
                    __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
-        } else if (valid && split) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(ks) * p.rows + orow) * kD + col);
+        } else if (split) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-        } else if (valid) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kD + col);
+          for (int e = 0; e < 8; ++e)
+            sts128(turned + ((e ^ (lane & 7)) << 4), __float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]), __float_as_uint(o[4 * e + 2]),
+                   __float_as_uint(o[4 * e + 3]));
+          store_turned(reinterpret_cast<uint8_t*>(p.part_o + (static_cast<size_t>(ks) * p.rows + rowbase) * kD + col), kD * 4);
+        } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+            sts128(turned + (((4 * c + e) ^ (lane & 7)) << 4), pack_bf16x2(o[8 * e] * inv, o[8 * e + 1] * inv),
+                   pack_bf16x2(o[8 * e + 2] * inv, o[8 * e + 3] * inv), pack_bf16x2(o[8 * e + 4] * inv, o[8 * e + 5] * inv),
+                   pack_bf16x2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+          if (c == 1) store_turned(reinterpret_cast<uint8_t*>(p.out + rowbase * kD + half * kHalf), kD * 2);
         }
         __syncwarp();   // the next chunk is loaded by the whole warp
       }
