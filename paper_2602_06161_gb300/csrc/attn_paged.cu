@@ -250,7 +250,8 @@ __device__ __forceinline__ void join_pass() {
 // The products are turned over, S^T = K Q^T (128 keys x kN rows), O^T += V^T P^T (128 columns x kN rows): a Q tile of 128 rows
 // would cost the tensor cores and the softmax the same for one row as for 128. A softmax thread is a key. The rows' largest
 // scores are only looked for when some score is above its row's reference by more than the threshold (one vote a tile); sums stay with
-// the threads until the keys of a unit are through. Two streams take alternate KV tiles, with sums and an accumulator of their own.
+// the threads until the keys of a unit are through. Two streams take alternate KV tiles, with sums and an accumulator of their own; where
+// units are of one tile, a stream takes a unit (256 sequences of 100 keys, 32 / 8 heads: 64 us by one stream after the other, 48 so).
 //
 // One CTA an SM, and the KV tiles of all units (sequence, KV head, group of rows) are one row of tiles of which every CTA takes an even
 // share, whatever the lengths: a batch of sequences of 1 to 1000 tiles keeps all SMs reading until the end. Where a
@@ -265,7 +266,7 @@ __device__ __forceinline__ void join_pass() {
 // Tensor memory: S0 | S1 | O0 | O1, kN columns each.
 constexpr int kRowsThreads = 512;
 constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsCopyWarp = 13, kRowsPlanWarp = 14;
-constexpr int kSlots = 5, kRing = 8, kUnits = 4;
+constexpr int kSlots = 5, kRing = 8, kUnits = 8;
 
 struct TileJob {
   int page[kMaxTilePages];   // entries of its pages, -1 for none
@@ -277,25 +278,28 @@ struct TileJob {
 };
 
 template <int kN>
+constexpr int kQueries = 2;   // units whose Q is in shared memory
+
+template <int kN>
 struct RowsSmem {
   uint8_t kv[kSlots][kTileBytes];
-  uint8_t q[2][kN * kD * 2];
+  uint8_t q[kQueries<kN>][kN * kD * 2];
   uint8_t pt[2][kBN * 128];
   uint64_t full[kSlots], empty[kSlots];
-  uint64_t q_full[2], q_empty[2];
+  uint64_t q_full[kQueries<kN>], q_empty[kQueries<kN>];
   uint64_t job_full[kRing], job_empty[kRing], v_clean[kRing];
   uint64_t unit_full[kUnits], unit_empty[kUnits];
-  uint64_t s_full[2], p_full[2], o_full, drain;
+  uint64_t s_full[2], p_full[2], o_full[2], drain;
   TileJob job[kRing];
   uint4 nan_keys[kRing];
   int4 row[kUnits][kN];      // per unit: keys lo, hi, position of a seed row or -1, its slot
   int4 unit[kUnits];         // tiles here, rows, first row of [B Hq Lq], part's place: -1 whole, -2 joined, else its number
   int2 unit_mask[kUnits];    // masked-input rows of the KV head, whether the unit's first tile is here
-  float4 fin[kN];            // weights of the two accumulators and of the masked-input value, 1 / l
+  float4 fin[2][kN];         // weights of the two accumulators and of the masked-input value, 1 / l
   float m[2][kN], step[2][kN], factor[2][kN];
   int unseen[2][kN], any_unseen[2];
   float red[2][4][kN];
-  float s_self[kN];
+  float s_self[2][kN];
   int slot[kN];
   float2 ml[kN];             // joined in a cluster: the rows' references and sums
   long long scan[kRowsThreads / 32];
@@ -327,7 +331,7 @@ __device__ __forceinline__ int2 tiles_of(const Params& p, int b) {
   return make_int2((hi - 1) / kBN + 1 - first, first);
 }
 
-template <int kN, bool kCap>
+template <int kN, bool kCap, bool kJoined>
 __global__ void __launch_bounds__(kRowsThreads, 1)
     attn_paged_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ Params p) {
@@ -335,6 +339,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   using Sm = RowsSmem<kN>;
   Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr uint32_t kTmem = 4 * kN;
+  constexpr int kQ = kQueries<kN>;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (warp == kRowsMmaWarp) {
@@ -345,14 +350,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         mbar_init(&sm.job_empty[i], 10);   // copies, products, four warps that look V through, four of a stream
         mbar_init(&sm.v_clean[i], 128);
       }
+      for (int i = 0; i < kQ; ++i) mbar_init(&sm.q_full[i], 1), mbar_init(&sm.q_empty[i], 1);
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&sm.q_full[i], 1);
-        mbar_init(&sm.q_empty[i], 1);
         mbar_init(&sm.s_full[i], 1);
         mbar_init(&sm.p_full[i], 128);
       }
       for (int i = 0; i < kUnits; ++i) mbar_init(&sm.unit_full[i], 1), mbar_init(&sm.unit_empty[i], 8);
-      mbar_init(&sm.o_full, 1);
+      mbar_init(&sm.o_full[0], 1), mbar_init(&sm.o_full[1], 1);
       mbar_init(&sm.drain, 1);
       sm.abort = 0;
       sm.b0 = 0;
@@ -379,7 +383,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
   int b0;
   long long before0 = 0;   // tiles before sequence b0's
   int tile0 = 0;           // joined: the CTA's first tile of the sequence's
-  if (p.joined) {
+  if (kJoined) {
     // tiles counted from the sequence's first: a part of those of the cluster's unit
     const int u = static_cast<int>(blockIdx.x) / p.joined, rank = static_cast<int>(blockIdx.x) % p.joined;
     b0 = u / heads;
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     int b = b0, g = 0, unit = 0;
     long long first = before0;   // of the sequence's tiles
     int2 tiles = n > 0 ? tiles_of<false>(p, b) : make_int2(1, 0);
-    if (!p.joined && n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!kJoined && n == 0 && lane == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
     bool joined = false;
     for (long long t = t0; t < t1 && ok; ++unit) {
       for (long long all_of; t >= first + (all_of = static_cast<long long>(tiles.x) * heads); ) first += all_of, tiles = tiles_of<false>(p, ++b);
@@ -490,10 +494,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       __syncwarp();
       if (lane == 0) {
         // a part that begins its unit comes last in its CTA, any other first
-        const int place = p.joined ? -2 : whole ? -1 : static_cast<int>(2 * c) + (j == 0 ? 1 : 0);
+        const int place = kJoined ? -2 : whole ? -1 : static_cast<int>(2 * c) + (j == 0 ? 1 : 0);
         sm.unit[buf] = make_int4(nt, n_rows, static_cast<int>(rowbase + p0), place);
         sm.unit_mask[buf] = make_int2(static_cast<int>((static_cast<long long>(b) * p.Hkv + h)), j == 0 ? 1 : 0);
-        if (j == 0 && !whole && !p.joined) {
+        if (j == 0 && !whole && !kJoined) {
           // the unit's last tile is of CTA ((tile + 1) n - 1) / T
           const long long last = first + static_cast<long long>(u + 1) * tiles.x - 1;
           p.joins[blockIdx.x] = make_int4(static_cast<int>(((last + 1) * n_ctas - 1) / all - c) + 1, n_rows, static_cast<int>(rowbase + p0), 0);
@@ -524,7 +528,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       }
       t += nt;
     }
-    if (lane == 0 && n > 0 && !joined && !p.joined) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (lane == 0 && n > 0 && !joined && !kJoined) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 80);
       sm.abort = 1;
@@ -536,18 +540,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const int rows_log2 = min(p.page_log2, 7);
     const auto lookup = [&](int tile) { return lane < kBN >> rows_log2 ? page_of(p, b0, tile * kBN + (lane << rows_log2)) : -1; };
     // joined: the pages of the CTA's tiles, looked up here and a tile ahead (a job from the planning warp takes a microsecond more)
-    int entry_v = -1, entry_k = -1, entry_next = p.joined && n > 0 ? lookup(tile0) : -1;
-    const int u0 = p.joined ? static_cast<int>(blockIdx.x) / p.joined % heads : 0;
+    int entry_v = -1, entry_k = -1, entry_next = kJoined && n > 0 ? lookup(tile0) : -1;
+    const int u0 = kJoined ? static_cast<int>(blockIdx.x) / p.joined % heads : 0;
     for (int i = 0; i < 2 * n && ok; ++i) {
       // K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1)
       const bool is_v = i > 0 && ((i & 1) == 0 || i == 2 * n - 1);
       const int g = i == 0 ? 0 : is_v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2;
       const int at = g % kRing, slot = i % kSlots;
-      if (is_v == (p.joined != 0)) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);   // (joined: for the arrival below alone)
+      if (is_v == kJoined) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);   // (joined: for the arrival below alone)
       if (ok && i >= kSlots) ok = warp_wait(&sm.empty[slot], (i / kSlots - 1) & 1, &sm.abort);
       if (!ok) break;
       int entry, key0, h;
-      if (p.joined) {
+      if (kJoined) {
         if (!is_v) {
           entry_v = entry_k;
           entry_k = entry_next;
@@ -560,10 +564,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         const TileJob& job = sm.job[at];
         entry = job.page[lane % kMaxTilePages], key0 = job.key0, h = job.h;
       }
-      if (!is_v && (p.joined ? i == 0 : sm.job[at].first != 0)) {
-        const int unit = p.joined ? 0 : sm.job[at].unit, buf = unit & 1;
-        const int q_row = p.joined ? static_cast<int>((static_cast<long long>(b0) * p.Hq + h * p.G) * p.Lq + (u0 % p.n_groups) * kN) : sm.job[at].q_row;
-        if (unit >= 2) ok = warp_wait(&sm.q_empty[buf], ((unit >> 1) - 1) & 1, &sm.abort);
+      if (!is_v && (kJoined ? i == 0 : sm.job[at].first != 0)) {
+        const int unit = kJoined ? 0 : sm.job[at].unit, buf = unit % kQ;
+        const int q_row = kJoined ? static_cast<int>((static_cast<long long>(b0) * p.Hq + h * p.G) * p.Lq + (u0 % p.n_groups) * kN) : sm.job[at].q_row;
+        if (unit >= kQ) ok = warp_wait(&sm.q_empty[buf], (unit / kQ - 1) & 1, &sm.abort);
         if (!ok) break;
         if (lane == 0) {
           mbar_arrive_expect_tx(&sm.q_full[buf], kN * kD * 2);
@@ -585,7 +589,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     // every copy lands before the CTA's shared memory is released, whatever the other roles did
     if (lane == 0) {
       for (int f = max(0, issued - kSlots); f < issued; ++f) mbar_wait(&sm.full[f % kSlots], (f / kSlots) & 1, nullptr);
-      for (int f = max(0, q_issued - 2); f < q_issued; ++f) mbar_wait(&sm.q_full[f & 1], (f >> 1) & 1, nullptr);
+      for (int f = max(0, q_issued - kQ); f < q_issued; ++f) mbar_wait(&sm.q_full[f % kQ], (f / kQ) & 1, nullptr);
     }
   } else if (warp == kRowsMmaWarp) {
     if (lane == 0 && n > 0) {
@@ -613,17 +617,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         if (!ok) return;
         if (sm.job[at].first) {
           ++unit;
-          ok = wait(&sm.q_full[unit & 1], unit >> 1);
+          ok = wait(&sm.q_full[unit % kQ], unit / kQ);
           if (!ok) return;
         }
-        const uint32_t k = k_lo + ((slot * kTileBytes) >> 4), q = q_lo + (((unit & 1) * kN * kD * 2) >> 4);
+        const uint32_t k = k_lo + ((slot * kTileBytes) >> 4), q = q_lo + (((unit % kQ) * kN * kD * 2) >> 4);
 #pragma unroll
         for (int kk = 0; kk < kD / 16; ++kk)
           umma_ss(tbase + (g & 1) * kN, desc(k + (((kk >> 2) * kGroupHalf + (kk & 3) * 32) >> 4), kv_hi),
                   desc(q + (((kk >> 2) * kN * 128 + (kk & 3) * 32) >> 4), hi), id_s, kk > 0 ? 1u : 0u);
         umma_commit(&sm.s_full[g & 1]);
         umma_commit(&sm.empty[slot]);
-        if (sm.job[at].last) umma_commit(&sm.q_empty[unit & 1]);
+        if (sm.job[at].last) umma_commit(&sm.q_empty[unit % kQ]);
       };
       for (int g = 0; g < 2 && g < n && ok; ++g) issue_s(g);
       int in_unit = 0;   // the tile's number in its unit
@@ -640,7 +644,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           umma_ss(tbase + (2 + s) * kN, desc(v + ((kk * 2 * kGroupBytes) >> 4), kv_hi), desc(pt + ((kk * 2048) >> 4), hi), id_o,
                   (in_unit > 1 || kk > 0) ? 1u : 0u);
         umma_commit(&sm.empty[slot]);
-        if (last) umma_commit(&sm.o_full);
+        if (last && (in_unit > 0 || kJoined || s == 0)) umma_commit(&sm.o_full[0]);
+        if (last && (in_unit > 0 || kJoined || s == 1)) umma_commit(&sm.o_full[1]);   // (a unit of one tile is its stream's alone)
         mbar_arrive(&sm.job_empty[at]);
         if (g + 2 < n) issue_s(g + 2);
       }
@@ -690,29 +695,45 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     bool ok = true;
     int g = 0;
     if (n == 0 && tid < kN) sm.ml[tid] = make_float2(-INFINITY, 0.0f);
-    for (int unit = 0; g < n; ++unit) {
-      const int buf = unit % kUnits;
-      ok = warp_wait(&sm.unit_full[buf], (unit / kUnits) & 1, &sm.abort);
+    for (int first_unit = 0, o_waits = 0; g < n;) {
+      // Units of one tile, two in turn, are done by a stream each at the same time.
+      ok = warp_wait(&sm.unit_full[first_unit % kUnits], (first_unit / kUnits) & 1, &sm.abort);
+      const bool alone = ok && sm.unit[first_unit % kUnits].x == 1 && !kJoined;
+      bool two = alone && g + 1 < n;
+      if (two) {
+        ok = warp_wait(&sm.unit_full[(first_unit + 1) % kUnits], ((first_unit + 1) / kUnits) & 1, &sm.abort);
+        two = ok && sm.unit[(first_unit + 1) % kUnits].x == 1;
+      }
       if (any_of<256>(1, !ok)) {
         ok = false;
         break;
       }
+      const bool second = alone && (g & 1) != stream;   // the stream has the next unit, if that is one of a tile
+      const bool idle = second && !two;
+      const int unit = first_unit + (second && two ? 1 : 0), buf = unit % kUnits;
       const int4 info = sm.unit[buf];
-      const int nt = info.x, n_rows = info.y;
+      const int nt = alone ? (two ? 2 : 1) : info.x, n_rows = idle ? 0 : info.y;   // tiles of this turn
       const long long orow0 = info.z;
       const int place = info.w;
       const bool own_rows = sm.unit_mask[buf].y != 0 && p.n_seeds > 0;   // the masked-input pairs are added where the unit begins
       const size_t masked0 = static_cast<size_t>(sm.unit_mask[buf].x) * p.n_seeds;
+      float* const s_self_of = sm.s_self[alone ? stream : 0];
+      float4* const fin = sm.fin[alone ? stream : 0];
+      const bool leads = alone || stream == 0;   // of the unit's streams
+      const auto sync_unit = [&] {
+        if (alone) sync_of<128>(2 + stream);
+        else sync_of<256>(1);
+      };
       if (key < kN) {
         sm.m[stream][key] = 0.0f;
         sm.unseen[stream][key] = key < n_rows ? 1 : 0;
         if (key == 0) sm.any_unseen[stream] = 1;
-        if (stream == 0) sm.s_self[key] = -INFINITY;
+        if (leads) s_self_of[key] = -INFINITY;
       }
-      sync_of<256>(1);
+      sync_unit();
       if (own_rows) {
         // the seed rows' own scores (log2 units): a warp a row, four columns a lane
-        for (int i = warp; i < n_rows; i += 8) {
+        for (int i = alone ? w4 : warp; i < n_rows; i += alone ? 4 : 8) {
           const int4 row = sm.row[buf][i];
           if (row.z < 0) continue;
           const uint2 a = __ldg(reinterpret_cast<const uint2*>(p.q + (orow0 + i) * kD) + lane);
@@ -722,7 +743,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           dot = fmaf(__uint_as_float(a.y << 16), __uint_as_float(b.y << 16), dot);
           dot = fmaf(__uint_as_float(a.y & 0xffff0000u), __uint_as_float(b.y & 0xffff0000u), dot);
           for (int d = 16; d >= 1; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-          if (lane == 0) sm.s_self[i] = kCap ? capped(dot, p.cap_in, p.cap_log2) : dot * p.scale_log2;
+          if (lane == 0) s_self_of[i] = kCap ? capped(dot, p.cap_in, p.cap_log2) : dot * p.scale_log2;
         }
       }
       float l[kN];
@@ -745,6 +766,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             tmem_ld_wait16(x);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
+              if (kCap && e % 4 == 0 && c0 + e >= n_rows) break;   // (a cap is not worked out for rows that are none)
               const float f = __uint_as_float(x[e]);
               t[c0 + e] = kCap ? capped(f, p.cap_in, p.cap_log2) - m[c0 + e] : fmaf(f, p.scale_log2, -m[c0 + e]);
             }
@@ -754,6 +776,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const bool held = ((sm.job[at].valid >> (key >> page_rows)) & 1u) != 0;
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
+              if (i >= n_rows) break;
               const int4 row = sm.row[buf][i];
               if (!held || pos < row.x || pos >= row.y || pos == row.z) t[i] = -INFINITY;
             }
@@ -771,6 +794,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           // new references: the rows' maxima where they are above the old ones by more than the threshold
 #pragma unroll
           for (int i = 0; i < kN; ++i) {
+            if (i >= n_rows) break;   // (references of rows that are none are anything)
             const int top = __reduce_max_sync(0xffffffffu, ordered(t[i] == t[i] ? t[i] : -INFINITY));
             if (lane == (i & 31)) sm.red[stream][w4][i] = from_ordered(top);
           }
@@ -842,80 +866,88 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         if (lane == 0) mbar_arrive(&sm.job_empty[at]);
       }
-      if (ok) ok = warp_wait(&sm.o_full, unit & 1, &sm.abort);
+      if (ok && !idle) ok = warp_wait(&sm.o_full[stream], o_waits++ & 1, &sm.abort);
+      if (alone ? any_of<128>(2 + stream, !ok) : any_of<256>(1, !ok)) ok = false;   // (of a unit's threads all or none go on)
+
+      // ---------------- the rows' results ----------------
+      if (ok) {
+        tc_fence_after_sync();
+        // sums over the warp: each step adds up and hands on half of the rows, until a lane has one. (The code of a unit's end is kept short: in a call
+        // of a few tiles it runs once, out of a cold instruction cache. Unrolled over all rows it took 1.9 us.)
+#pragma unroll
+        for (int d = 16, left = kN; left > 1; d >>= 1, left >>= 1) {
+          const bool upper = (lane & d) != 0;
+#pragma unroll
+          for (int i = 0; i < left / 2; ++i) {
+            const float mine = upper ? l[i + left / 2] : l[i], other = upper ? l[i] : l[i + left / 2];
+            l[i] = mine + __shfl_xor_sync(0xffffffffu, other, d);
+          }
+        }
+        if (kN == 16) l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
+        sm.red[stream][w4][kN == 16 ? lane >> 1 : lane] = l[0];
+        sync_unit();
+        // a stream without a tile here has seen nothing
+        if (leads && key < n_rows) {
+          const float s_self = s_self_of[key];
+          float l2[2], m2[2];
+          for (int s = 0; s < 2; ++s) {
+            const bool seen = (!alone || s == stream) && !sm.unseen[s][key];
+            l2[s] = !alone || s == stream ? (sm.red[s][0][key] + sm.red[s][1][key]) + (sm.red[s][2][key] + sm.red[s][3][key]) : 0.0f;
+            m2[s] = seen ? sm.m[s][key] : -INFINITY;
+          }
+          const float m0 = m2[0], m1 = m2[1];
+          const float top = fmaxf(fmaxf(m0, m1), s_self);
+          const float f0 = m0 == -INFINITY ? 0.0f : ex2_approx(m0 - top), f1 = m1 == -INFINITY ? 0.0f : ex2_approx(m1 - top);
+          const float p_self = s_self == -INFINITY ? 0.0f : ex2_approx(s_self - top);
+          // (NaN scores leave the references alone: they are in the sums)
+          float sum = fmaf(f0, l2[0], fmaf(f1, l2[1], p_self));
+          if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
+          if (s_self != s_self) sum = s_self;
+          fin[key] = make_float4(f0, f1, p_self, place != -1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+          if (place == -2) sm.ml[key] = make_float2(top, sum);
+          else if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + key] = make_float2(top, sum);
+          else if (p.lse != nullptr) p.lse[orow0 + key] = (top + lg2_approx(sum)) * 0.6931471805599453f;
+        }
+        sync_unit();
+        // thread = output column; the streams' warps take four rows in turn
+#pragma unroll 1
+        for (int c0 = alone ? 0 : 4 * stream; c0 < n_rows; c0 += alone ? 4 : 8) {
+          uint32_t o[2][4];
+          tmem_ld4(quad + 2 * kN + c0, o[0]);
+          tmem_ld4(quad + 3 * kN + c0, o[1]);
+          tmem_ld_wait4(o[0]);
+          tmem_ld_wait4(o[1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = c0 + e;
+            if (i >= n_rows) break;
+            const float4 f = fin[i];
+            float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
+            if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
+            if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
+            if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
+            else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
+            else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
+          }
+          __syncwarp();
+        }
+      }
+      tc_fence_before_sync();
+      // both accumulators have been read before a stream lets the next unit's products begin
       if (any_of<256>(1, !ok)) {
         ok = false;
         break;
       }
-
-      // ---------------- the rows' results ----------------
-      tc_fence_after_sync();
-      // sums over the warp: each step adds up and hands on half of the rows, until a lane has one. (The code of a unit's end is kept short: in a call
-      // of a few tiles it runs once, out of a cold instruction cache. Unrolled over all rows it took 1.9 us.)
-#pragma unroll
-      for (int d = 16, left = kN; left > 1; d >>= 1, left >>= 1) {
-        const bool upper = (lane & d) != 0;
-#pragma unroll
-        for (int i = 0; i < left / 2; ++i) {
-          const float mine = upper ? l[i + left / 2] : l[i], other = upper ? l[i] : l[i + left / 2];
-          l[i] = mine + __shfl_xor_sync(0xffffffffu, other, d);
-        }
-      }
-      if (kN == 16) l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
-      sm.red[stream][w4][kN == 16 ? lane >> 1 : lane] = l[0];
-      sync_of<256>(1);
-      // a stream without a tile here has seen nothing
-      if (tid < n_rows) {
-        const float s_self = sm.s_self[tid];
-        float l2[2];
-        for (int s = 0; s < 2; ++s) l2[s] = (sm.red[s][0][tid] + sm.red[s][1][tid]) + (sm.red[s][2][tid] + sm.red[s][3][tid]);
-        const float m0 = sm.unseen[0][tid] ? -INFINITY : sm.m[0][tid], m1 = sm.unseen[1][tid] ? -INFINITY : sm.m[1][tid];
-        const float top = fmaxf(fmaxf(m0, m1), s_self);
-        const float f0 = m0 == -INFINITY ? 0.0f : ex2_approx(m0 - top), f1 = m1 == -INFINITY ? 0.0f : ex2_approx(m1 - top);
-        const float p_self = s_self == -INFINITY ? 0.0f : ex2_approx(s_self - top);
-        // (NaN scores leave the references alone: they are in the sums)
-        float sum = fmaf(f0, l2[0], fmaf(f1, l2[1], p_self));
-        if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
-        if (s_self != s_self) sum = s_self;
-        sm.fin[tid] = make_float4(f0, f1, p_self, place != -1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
-        if (place == -2) sm.ml[tid] = make_float2(top, sum);
-        else if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + tid] = make_float2(top, sum);
-        else if (p.lse != nullptr) p.lse[orow0 + tid] = (top + lg2_approx(sum)) * 0.6931471805599453f;
-      }
-      sync_of<256>(1);
-      // thread = output column; the streams' warps take four rows in turn
-#pragma unroll 1
-      for (int c0 = 4 * stream; c0 < n_rows; c0 += 8) {
-        uint32_t o[2][4];
-        tmem_ld4(quad + 2 * kN + c0, o[0]);
-        tmem_ld4(quad + 3 * kN + c0, o[1]);
-        tmem_ld_wait4(o[0]);
-        tmem_ld_wait4(o[1]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = c0 + e;
-          if (i >= n_rows) break;
-          const float4 f = sm.fin[i];
-          float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
-          if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
-          if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
-          if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
-          else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
-          else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
-        }
-        __syncwarp();
-      }
-      tc_fence_before_sync();
-      // both accumulators have been read before a stream lets the next unit's products begin
-      sync_of<256>(1);
-      if (lane == 0) mbar_arrive(&sm.unit_empty[buf]);
+      if (lane == 0) mbar_arrive(&sm.unit_empty[first_unit % kUnits]);
+      if (lane == 0 && two) mbar_arrive(&sm.unit_empty[(first_unit + 1) % kUnits]);
+      first_unit += two ? 2 : 1;
     }
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 84);
       sm.abort = 1;
     }
     tc_fence_before_sync();
-    if (p.joined) {
+    if (kJoined) {
       const int u = static_cast<int>(blockIdx.x) / p.joined % heads, p0 = u % p.n_groups * kN;
       __syncwarp();
       cluster_sync();   // every CTA's rows are staged
@@ -925,7 +957,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       cluster_sync();   // no CTA leaves while its rows are read
     }
   }
-  if (p.joined && warp >= kScreenWarp) join_pass();
+  if (kJoined && warp >= kScreenWarp) join_pass();
   __syncthreads();
   if (warp == kRowsMmaWarp) {
     tc_fence_after_sync();
@@ -1655,11 +1687,11 @@ constexpr int kClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
 // The kernel and how the keys are shared, from the sizes and the table's width (the lengths are not known to the host: where they are shorter,
 // an even share of all tiles is better than predicted).
 //
-// Predicted microseconds, fitted to calls back to back on GB300, measured / predicted: rows of 16 joined, one token over 777 keys (28 / 4
-// heads, 7 CTAs a unit) 7.5 / 7.7, over 4096 (32 / 8, 8) 11.9 / 11.8, 16 sequences of 500 (1) 12.8 / 13.3; in even shares 11.0 / 13.5, 15.6 / 15.0, 18.7 / 16.4, 64
-// sequences of up to 8191 keys 192 / 251 (all of that length: 305). Rows of 32 joined 12.6 / 12.6 (32 rows over 2048, 32 / 8), in even shares 2 us a
-// tile. Pairs joined: 8 rows over 2048 (32 / 8, 8 CTAs a unit) 10.2 / 10.4, 32 over 1024 (28 / 4) 11.2 / 10.4, four sequences of 64 rows over 2048
-// (4) 19.8 / 16.1; by a second kernel 14.4 / 15.6 (32 over 1024 in 8 parts); 1216 rows over 8192 in one wave 118 / 111.
+// Predicted microseconds, fitted to calls back to back on GB300, measured / predicted. Rows of 16 joined: one token over 777 keys (28 / 4 heads,
+// 7 CTAs a unit) 7.6 / 7.7, over 4096 (32 / 8, 8) 12.0 / 11.8, 16 sequences of 500 (1) 12.8 / 13.3, 29 of 51 (1) 16.1 / 16.8. In even shares
+// 11.5 / 13.0, 15.6 / 14.5, 18.8 / 17.0, 12.7 / 16.4; 128 sequences of 120 29.3 / 30.6, 256 of 100 48.2 / 49.7, 64 of 512 39.5 / 32.2. Rows of 32
+// joined 12.6 / 13.0 (32 rows over 2048, 32 / 8), in even shares 8 sequences of 32 over 4000 44.6 / 38.7. Pairs joined: 8 rows over 2048 (32 / 8, 8 CTAs a unit) 10.2 / 10.9,
+// 8 sequences of 8 rows over 1000 (2) 15.6 / 16.6, 5 of 75 over 699 (16 / 2, 3) 15.3 / 16.9; by a second kernel 16.0 / 18.0; in one wave 18.5 / 18.1.
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
   const long long nkv = (static_cast<long long>(M) * page + kBN - 1) / kBN;   // KV tiles of a sequence at most
@@ -1673,12 +1705,13 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
     const bool few = packed <= 16;
     const Mode mode = few ? kRows16 : kRows32;
     const long long units = static_cast<long long>(B) * Hkv;
-    const double tile = few ? 1.48 : 1.95, fill = B > 1 ? 0.75 : 1.0;
+    const double tile = few ? 1.48 : 2.2, fill = B > 1 && nkv > 1 ? 0.75 : 1.0;
     const int ctas = static_cast<int>(std::min<long long>(kSms, std::min<long long>(units, kSms) * std::min<long long>(nkv, kSms)));
-    consider(Plan{mode, 1, 1, ctas, 0}, (few ? 12.0 : 15.0) + tile * std::ceil(fill * static_cast<double>(units) * nkv / kSms));
+    consider(Plan{mode, 1, 1, ctas, 0}, (few ? 11.5 : 14.0) + tile * std::ceil(fill * static_cast<double>(units) * nkv / kSms) + 1.3 * static_cast<double>(units) / kSms);
     for (int c = 1; c <= kMaxJoined && c <= nkv; ++c) {
       const double waves = std::ceil(static_cast<double>(units) / kClusters[c - 1]);
-      consider(Plan{mode, 1, 1, 0, c}, (few ? 6.3 : 9.8) + (units * c > kSms / 2 ? 1.5 : 0.0) + 3.0 * (waves - 1) + 1.38 * waves * std::ceil(static_cast<double>(nkv) / c));
+      consider(Plan{mode, 1, 1, 0, c}, (few ? 6.3 : 9.8) + (units * c > kSms / 2 ? 1.5 : 0.0) + 6.2 * (waves - 1) +
+                                           (few ? 1.38 : 1.6) * waves * std::ceil(static_cast<double>(nkv) / c));
     }
     if (few) return best;
   }
@@ -1689,7 +1722,9 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
     consider(Plan{kPairs, groups, ns, 0, 0}, 5.0 + waves * (3.5 + 1.6 * tiles) + (ns > 1 ? 2.4 + 0.15 * ns + 1.9e-4 * rows * ns : 0.0));
     if (ns > 1 && ns <= kMaxJoined) {
       const double turns = std::ceil(static_cast<double>(units) / kClusters[ns - 1]);
-      consider(Plan{kPairs, groups, ns, 0, ns}, 7.2 + (units * ns > kSms / 2 ? 2.5 : 0.0) + 3.5 * (turns - 1) + 1.6 * turns * tiles);
+      const double join = 4.0 * std::min<long long>(packed, 2 * kBM) / (2 * kBM);   // of a unit's rows
+      consider(Plan{kPairs, groups, ns, 0, ns},
+               7.2 + (units * ns > kSms / 2 ? 2.5 : 0.0) + 3.5 * (turns - 1) + turns * (1.6 * tiles + join));
     }
     if (units * ns > 8 * kSms) break;
   }
@@ -1698,11 +1733,12 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
 
 constexpr size_t kRowsSmemBytes[2] = {sizeof(RowsSmem<16>) + 1024, sizeof(RowsSmem<32>) + 1024};
 constexpr size_t kPairSmemBytes = sizeof(PairSmem) + 1024;
-static_assert(kRowsSmemBytes[1] <= 227 * 1024 && kPairSmemBytes <= 227 * 1024, "shared memory of a CTA");
+static_assert(kRowsSmemBytes[0] <= 227 * 1024 && kRowsSmemBytes[1] <= 227 * 1024 && kPairSmemBytes <= 227 * 1024, "shared memory of a CTA");
 
 using Kernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params);
-constexpr Kernel kRowsKernels[2][2] = {{attn_paged_rows_kernel<16, false>, attn_paged_rows_kernel<16, true>},
-                                       {attn_paged_rows_kernel<32, false>, attn_paged_rows_kernel<32, true>}};
+template <int kN>
+constexpr Kernel kRowsOf[2][2] = {{attn_paged_rows_kernel<kN, false, false>, attn_paged_rows_kernel<kN, false, true>},
+                                  {attn_paged_rows_kernel<kN, true, false>, attn_paged_rows_kernel<kN, true, true>}};
 constexpr Kernel kPairKernels[2] = {attn_paged_pairs_kernel<false>, attn_paged_pairs_kernel<true>};
 
 // rows of all parts
@@ -1749,8 +1785,8 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
       return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
     };
     for (int c = 0; c < 2; ++c) {
-      for (int m = 0; m < 2; ++m)
-        if (!limit(kRowsKernels[m][c], kRowsSmemBytes[m])) return -3;
+      for (int j = 0; j < 2; ++j)
+        if (!limit(kRowsOf<16>[c][j], kRowsSmemBytes[0]) || !limit(kRowsOf<32>[c][j], kRowsSmemBytes[1])) return -3;
       if (!limit(kPairKernels[c], kPairSmemBytes)) return -3;
     }
     return 0;
@@ -1817,7 +1853,9 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
     cfg.attrs = attr;
     cfg.numAttrs = 2;
   }
-  cudaError_t e = cudaLaunchKernelEx(&cfg, few ? kRowsKernels[m][cap ? 1 : 0] : kPairKernels[cap ? 1 : 0], tq, tk, tv, p);
+  const int joined = plan.joined > 0 ? 1 : 0, capped = cap ? 1 : 0;
+  const Kernel kernel = !few ? kPairKernels[capped] : m == 0 ? kRowsOf<16>[capped][joined] : kRowsOf<32>[capped][joined];
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tq, tk, tv, p);
   if (e == cudaSuccess && parts > 0) {
     const dim3 join_grid = few ? dim3(width / kJoinWarps, plan.ctas) : dim3(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps));
     cfg = pdl_config(join_grid, dim3(kJoinWarps * 32), 0, stream, pdl);
