@@ -16,12 +16,12 @@
 // by more than kSlack. Logits far below it, -inf among them, are raised to where their weight still is 0 (0 * -inf would be NaN).
 // References beyond 2^20, where that correction is no small one, and infinities are left to a second, careful walk.
 //
-// The K best. A thread keeps the best of its vectors (every 192nd) as (largest element, vector), and the largest element of the others.
-// The K-th best of the threads' pairs is a bound: every one of the K best elements lies in a vector whose pair is not behind it,
-// and those are among the K threads in front. Their vectors are read again, the best one alone where the others' largest element is
-// behind the bound, and the elements that are not behind it are ranked by counting. What passes the bound is little more than K, whatever
-// ties there are (a row of equal logits: the first K vectors). A row whose K best crowd in a few threads may pass more than
-// kMaxFound: then the K best are taken one after the other, a walk over the row each.
+// The K best. A thread keeps the best of its vectors (every 192nd) as (largest element, vector), of many the second best too, and the
+// largest element of the others. The K-th best of the threads' best ones is a bound: every one of the K best elements lies in a vector whose
+// pair is not behind it, and those are among the K threads in front. Their vectors are read again, the kept ones alone where the others'
+// largest element is behind the bound, and the elements that are not behind it are ranked by counting. What passes the bound is little
+// more than K, whatever ties there are (a row of equal logits: the first K vectors). A row whose K best crowd in a few threads may
+// pass more than kMaxFound: then the K best are taken one after the other, a walk over the row each.
 //
 // Bound by memory, and not far from it by the special-function units (an exponential an element: 56 us of the 76 that reading 2048 x
 // 126464 bf16 takes). A CTA's warps have parts: six add up; one keeps a ring of three 12 KB pieces of the row's whole vectors filled by
@@ -36,6 +36,7 @@
 #include <type_traits>
 
 #include "cluster.cuh"
+#include "context.cuh"
 #include "kernels.cuh"
 #include "ptx.cuh"
 
@@ -244,22 +245,29 @@ __device__ __noinline__ Sums careful_sums(const Row<T>& row, int w0, int w1, boo
   return a;
 }
 
+// Alternatives asked for: none, up to kFewBest, or more. For few the threads' best vectors are enough, and the K best of the threads are taken
+// one after the other. For more, threads with two or three of the best ones are no exception and taking is slow: a thread keeps two vectors
+// and the bound is found by halving. Measured the first / second way, 2048 rows of 126464 bf16: 1 alternative 88 / 97 us, 5 89 / 98, 20 101 / 99,
+// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 10.8, 29 / 17.
+enum Best { kNone, kFew, kMany };
+constexpr int kFewBest = 16;
+
 // A row's sums and pairs, from the adding warps to the finishing one.
-template <bool kTop>
+template <Best kBest>
 struct Handover {
   Sums sums[kAddWarps];
-  unsigned long long pairs[kTop ? kAdders : 1];
-  float others[kTop ? kAdders : 1];   // the largest element of a thread's other vectors
+  unsigned long long pairs[kBest == kMany ? 2 : 1][kBest != kNone ? kAdders : 1];   // a thread's best vector, or its two best
+  float others[kBest != kNone ? kAdders : 1];                                       // the largest element of its other vectors
 };
 
-template <bool kTop>
+template <Best kBest>
 struct FwdShared {
   uint64_t full[kStages], empty[kStages], done[2], taken[2];
-  Handover<kTop> row[2];
+  Handover<kBest> row[2];
   Sums part;                          // the finishing warp's, read by the cluster's first CTA
-  unsigned long long best[kTop ? kMaxTopLogprob : 1];
-  unsigned long long found[kTop ? kMaxFound : 1];
-  int who[kTop ? kMaxTopLogprob : 1];
+  unsigned long long best[kBest != kNone ? kMaxTopLogprob : 1];
+  unsigned long long found[kBest != kNone ? kMaxFound : 1];
+  int who[kBest != kNone ? 2 * kMaxTopLogprob : 1], more[kBest != kNone ? kMaxTopLogprob : 1];
   int n_found, abort;
 };
 
@@ -278,12 +286,71 @@ __device__ __forceinline__ unsigned long long merge_best(int K, Next&& next, Tak
   return last;
 }
 
-template <typename T, bool kTop>
+// A bound that K of a warp's keys, kLists a lane, are not below, found by halving, the values first (the upper kBits of a key), then the indices
+// of the keys of the value that is cut; 0 where there are fewer than K keys.
+template <int kBits, int kLists>
+__device__ __forceinline__ unsigned long long bound_of(const unsigned long long (&keys)[kLists], int K) {
+  uint32_t hi = 0, lo = 0xffffffffu;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    const uint32_t u = static_cast<uint32_t>(keys[i] >> (64 - kBits));
+    if (keys[i] == 0) continue;
+    hi = max(hi, u), lo = min(lo, u), ++n;
+  }
+  if (__reduce_add_sync(0xffffffffu, n) < K) return 0;
+  hi = __reduce_max_sync(0xffffffffu, hi), lo = __reduce_min_sync(0xffffffffu, lo);
+  const auto halve = [&](uint32_t& from, uint32_t to, int want, auto&& is) {   // the lowest start of `want` of them, or of more
+    while (from < to) {
+      const uint32_t mid = from + (to - from + 1) / 2;
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) c += is(keys[i], mid) ? 1 : 0;
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (c >= want) from = mid;
+      else to = mid - 1;
+      if (c == want) return true;
+    }
+    return false;
+  };
+  const auto upper = [](unsigned long long key) { return static_cast<uint32_t>(key >> (64 - kBits)); };
+  if (halve(lo, hi, K, [&](unsigned long long key, uint32_t mid) { return upper(key) >= mid; }))
+    return static_cast<unsigned long long>(lo) << (64 - kBits);
+  // keys of value lo: all of them are too many, or just enough
+  int above = 0;
+  uint32_t first = 0xffffffffu, last = 0, word = 0;
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    above += upper(keys[i]) > lo ? 1 : 0;
+    if (keys[i] == 0 || upper(keys[i]) != lo) continue;
+    const uint32_t low = static_cast<uint32_t>(keys[i]);
+    first = min(first, low), last = max(last, low), word = static_cast<uint32_t>(keys[i] >> 32);
+  }
+  above = __reduce_add_sync(0xffffffffu, above);
+  first = __reduce_min_sync(0xffffffffu, first), last = __reduce_max_sync(0xffffffffu, last), word = __reduce_max_sync(0xffffffffu, word);
+  halve(first, last, K - above, [&](unsigned long long key, uint32_t mid) {
+    return upper(key) == lo && key != 0 && static_cast<uint32_t>(key) >= mid;
+  });
+  return (static_cast<unsigned long long>(word) << 32) | first;
+}
+
+// Puts the n keys of `from` in order, the K best of them into `to`: a key's place is the number of those in front of it.
+__device__ __forceinline__ void rank_keys(const unsigned long long* from, int n, int K, unsigned long long* to, int lane) {
+  for (int c = lane; c < n; c += 32) {
+    const unsigned long long key = from[c];
+    int rank = 0;
+    for (int o = 0; o < n; ++o) rank += from[o] > key ? 1 : 0;
+    if (rank < K) to[rank] = key;
+  }
+}
+
+template <typename T, Best kBest>
 __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __grid_constant__ FwdParams p) {
   using V16 = Vec16<T>;
   constexpr int N = V16::kN;
   extern __shared__ uint4 ring[];   // [kStages][kPiece]
-  __shared__ FwdShared<kTop> sm;
+  constexpr bool kTop = kBest != kNone;
+  __shared__ FwdShared<kBest> sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int part = p.parts > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   if (tid == 0) {
@@ -344,8 +411,8 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
       float c = -INFINITY;
       uint32_t floor = 0;
       uint64_t s2[2] = {0, 0}, w2[2] = {0, 0};
-      float best = -INFINITY, others = -INFINITY;
-      int best_vec = w.x + tid;
+      float best[2] = {-INFINITY, -INFINITY}, others = -INFINITY;
+      int best_vec[2] = {w.x + tid, 0};
       const auto take = [&](const auto& raw, auto count, int i0) {
         constexpr int n = decltype(count)::value;
         float top = -INFINITY, t[n];
@@ -354,17 +421,36 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
           t[k] = V16::top(raw[k]);
           top = fmaxf(top, t[k]);
         }
-        if (kTop) {
-          if (top > best) {
-            others = fmaxf(others, best);
-            best = top;
+        if constexpr (kBest == kFew) {
+          if (top > best[0]) {
+            others = fmaxf(others, best[0]);
+            best[0] = top;
             bool found = false;
 #pragma unroll
             for (int k = 0; k < n; ++k) {
               const bool this_one = !found && t[k] == top;
-              if (this_one) best_vec = i0 + k * kAdders;
+              if (this_one) best_vec[0] = i0 + k * kAdders;
               else others = fmaxf(others, t[k]);
               found |= this_one;
+            }
+          } else {
+            others = fmaxf(others, top);
+          }
+        } else if constexpr (kBest == kMany) {
+          if (top > best[1]) {
+#pragma unroll
+            for (int k = 0; k < n; ++k) {
+              const int vec = i0 + k * kAdders;
+              if (t[k] > best[0]) {
+                others = fmaxf(others, best[1]);
+                best[1] = best[0], best_vec[1] = best_vec[0];
+                best[0] = t[k], best_vec[0] = vec;
+              } else if (t[k] > best[1]) {
+                others = fmaxf(others, best[1]);
+                best[1] = t[k], best_vec[1] = vec;
+              } else {
+                others = fmaxf(others, t[k]);
+              }
             }
           } else {
             others = fmaxf(others, top);
@@ -436,7 +522,9 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
       if (ok && n_row >= 2) ok = warp_wait_all(&sm.taken[buf], ((n_row >> 1) - 1) & 1, &sm.abort);
       if (!ok) break;
       if constexpr (kTop) {
-        sm.row[buf].pairs[tid] = w.x + tid < w.y ? key_of(best, static_cast<uint32_t>(best_vec)) : 0ull;
+        sm.row[buf].pairs[0][tid] = w.x + tid < w.y ? key_of(best[0], static_cast<uint32_t>(best_vec[0])) : 0ull;
+        // (a second of -inf alone is left to the walk over the others, which are no less)
+        if constexpr (kBest == kMany) sm.row[buf].pairs[1][tid] = best[1] > -INFINITY ? key_of(best[1], static_cast<uint32_t>(best_vec[1])) : 0ull;
         sm.row[buf].others[tid] = others;
       }
       // the row's ends are no thread's pairs (they are looked at anyway)
@@ -513,35 +601,65 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
       for (int i = 1; i < kAddWarps; ++i) all = merge(all, sm.row[buf].sums[i]);
       if constexpr (kTop) {
         constexpr int kLists = kAdders / 32;
-        // the K best pairs: a lane's, in order
+        // the K best pairs
         unsigned long long mine[kLists];
 #pragma unroll
-        for (int i = 0; i < kLists; ++i) mine[i] = sm.row[buf].pairs[32 * i + lane];
-#pragma unroll
-        for (int i = 1; i < kLists; ++i)
-#pragma unroll
-          for (int j = i; j > 0; --j) {
-            const unsigned long long hi = max(mine[j - 1], mine[j]), lo = min(mine[j - 1], mine[j]);
-            mine[j - 1] = hi, mine[j] = lo;
-          }
-        const auto next = [&](int i) {
-          unsigned long long key = 0;
-#pragma unroll
-          for (int k = 0; k < kLists; ++k)
-            if (i == k) key = mine[k];
-          return key;
-        };
+        for (int i = 0; i < kLists; ++i) mine[i] = sm.row[buf].pairs[0][32 * i + lane];
         if (lane == 0) sm.n_found = 0;
         for (int k = lane; k < kMaxTopLogprob; k += 32) sm.best[k] = 0;   // (NaN may leave places empty)
         // (where fewer threads than K have vectors the bound is 0, and all their elements are looked at)
-        const unsigned long long bound =
-            merge_best(K, next, [&](int k, unsigned long long key) {
-              if (lane == 0) sm.who[k] = key != 0 ? static_cast<int>(index_of(key)) : -1;
-            });
-        const float bound_value = from_ordered(static_cast<uint32_t>(bound >> 32));
+        unsigned long long bound;
+        float bound_value;
+        int n_who = 0, n_more = 0;
+        const uint32_t before = (1u << lane) - 1u;
+        if constexpr (kBest == kFew) {
+          // a lane's, in order
+#pragma unroll
+          for (int i = 1; i < kLists; ++i)
+#pragma unroll
+            for (int j = i; j > 0; --j) {
+              const unsigned long long hi = max(mine[j - 1], mine[j]), lo = min(mine[j - 1], mine[j]);
+              mine[j - 1] = hi, mine[j] = lo;
+            }
+          const auto next = [&](int i) {
+            unsigned long long key = 0;
+#pragma unroll
+            for (int k = 0; k < kLists; ++k)
+              if (i == k) key = mine[k];
+            return key;
+          };
+          bound = merge_best(K, next, [&](int k, unsigned long long key) {
+            if (lane == 0 && key != 0) sm.who[k] = static_cast<int>(index_of(key));
+            if (key != 0) n_who = k + 1;
+          });
+          bound_value = from_ordered(static_cast<uint32_t>(bound >> 32));
+          __syncwarp();
+          static_assert(kFewBest <= 32, "a thread's vector a lane");
+          const int t = lane < n_who ? (sm.who[lane] - w.x) % kAdders : 0;
+          const bool more = lane < n_who && (bound == 0 || !(sm.row[buf].others[t] < bound_value));
+          const uint32_t walk = __ballot_sync(0xffffffffu, more);
+          if (more) sm.more[__popc(walk & before)] = t;
+          n_more = __popc(walk);
+        } else {
+          bound = bound_of<8 * sizeof(T)>(mine, K);
+          bound_value = from_ordered(static_cast<uint32_t>(bound >> 32));
+#pragma unroll
+          for (int i = 0; i < kLists; ++i) {
+            const unsigned long long second = sm.row[buf].pairs[1][32 * i + lane];
+            const bool in = mine[i] != 0 && mine[i] >= bound, in2 = in && second != 0 && second >= bound;
+            const bool more = in && (bound == 0 || !(sm.row[buf].others[32 * i + lane] < bound_value));
+            const uint32_t lanes = __ballot_sync(0xffffffffu, in), lanes2 = __ballot_sync(0xffffffffu, in2), walk = __ballot_sync(0xffffffffu, more);
+            if (in) sm.who[n_who + __popc(lanes & before)] = static_cast<int>(index_of(mine[i]));
+            n_who += __popc(lanes);
+            if (in2) sm.who[n_who + __popc(lanes2 & before)] = static_cast<int>(index_of(second));
+            n_who += __popc(lanes2);
+            if (more) sm.more[n_more + __popc(walk & before)] = 32 * i + lane;
+            n_more += __popc(walk);
+          }
+        }
         __syncwarp();
         const auto look = [&](const uint4& raw, int i) {
-          if (key_of(V16::top(raw), static_cast<uint32_t>(i)) < bound) return;
+          if (bound != 0 && V16::top(raw) < bound_value) return;
           float x[N];
           V16::unpack(raw, x);
 #pragma unroll
@@ -553,20 +671,33 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
             }
           }
         };
-        for (int k0 = 0; k0 < K; k0 += 32) {
-          const int vec = k0 + lane < K ? sm.who[k0 + lane] : -1;
-          bool more = false;
-          if (vec >= 0) {
-            look(__ldg(row.base + vec), vec);
-            const float others = sm.row[buf].others[(vec - w.x) % kAdders];
-            more = bound == 0 || !(others < bound_value);
+        for (int k = lane; k < n_who; k += 32) look(__ldg(row.base + sm.who[k]), sm.who[k]);
+        // threads whose other vectors may hold some too: these are dealt out to the lanes, kLooked loads at a time (a thread after the other
+        // 64 alternatives of 128k logits took 20 us)
+        constexpr int kLooked = 4;
+        const int each = (w.y - w.x + kAdders - 1) / kAdders, todo = n_more * each;
+        int m = lane / max(each, 1), step = lane - m * each;   // a lane's place: the thread's in the list, the vector's among its
+        for (int i0 = lane; i0 < todo; i0 += 32 * kLooked) {
+          uint4 raw[kLooked];
+          int at[kLooked];
+#pragma unroll
+          for (int u = 0; u < kLooked; ++u) {
+            at[u] = -1;
+            if (i0 + 32 * u < todo) {
+              const int t = sm.more[m], x = w.x + t + step * kAdders;
+              const bool seen = x == static_cast<int>(index_of(sm.row[buf].pairs[0][t])) ||
+                                (kBest == kMany && sm.row[buf].pairs[kBest == kMany ? 1 : 0][t] != 0 &&
+                                 x == static_cast<int>(index_of(sm.row[buf].pairs[kBest == kMany ? 1 : 0][t])));
+              if (x < w.y && !seen) {
+                at[u] = x;
+                raw[u] = __ldg(row.base + x);
+              }
+            }
+            for (step += 32; step >= each; step -= each) ++m;
           }
-          // threads whose other vectors may hold some too: all lanes look at them
-          for (uint32_t rest = __ballot_sync(0xffffffffu, more); rest != 0; rest &= rest - 1) {
-            const int v = __shfl_sync(0xffffffffu, vec, __ffs(rest) - 1), t = (v - w.x) % kAdders;
-            for (int i = w.x + t + lane * kAdders; i < w.y; i += 32 * kAdders)
-              if (i != v) look(__ldg(row.base + i), i);
-          }
+#pragma unroll
+          for (int u = 0; u < kLooked; ++u)
+            if (at[u] >= 0) look(raw[u], at[u]);
         }
         if (lane < 2) {
           const int end = lane == 0 ? 0 : row.n_vecs - 1;
@@ -575,12 +706,7 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
         __syncwarp();
         const int n = sm.n_found;
         if (n <= kMaxFound) {
-          for (int c = lane; c < n; c += 32) {
-            const unsigned long long key = sm.found[c];
-            int rank = 0;
-            for (int o = 0; o < n; ++o) rank += sm.found[o] > key ? 1 : 0;
-            if (rank < K) sm.best[rank] = key;
-          }
+          rank_keys(sm.found, n, K, sm.best, lane);
         } else {
           unsigned long long last = ~0ull;
           for (int k = 0; k < K; ++k) {
@@ -622,14 +748,36 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
       if (part == 0 && ok) {
         for (int c = 1; c < p.parts; ++c) all = merge(all, *cluster_ptr(&sm.part, c));
         if constexpr (kTop) {
-          // the parts' lists, which are in order: brought here, then merged, one a lane
           static_assert(kMaxParts * kMaxTopLogprob <= kMaxFound, "the parts' best");
-          for (int i = lane; i < p.parts * K; i += 32) sm.found[i] = cluster_ptr(sm.best, i / K)[i % K];
-          __syncwarp();
-          merge_best(K, [&](int i) { return lane < p.parts && i < K ? sm.found[lane * K + i] : 0ull; },
-                     [&](int k, unsigned long long key) {
-                       if (lane == 0) sm.best[k] = key;
-                     });
+          if constexpr (kBest == kFew) {
+            // the parts' lists, which are in order: brought here, then merged, one a lane
+            for (int i = lane; i < p.parts * K; i += 32) sm.found[i] = cluster_ptr(sm.best, i / K)[i % K];
+            __syncwarp();
+            merge_best(K, [&](int i) { return lane < p.parts && i < K ? sm.found[lane * K + i] : 0ull; },
+                       [&](int k, unsigned long long key) {
+                         if (lane == 0) sm.best[k] = key;
+                       });
+          } else {
+            // the parts' lists: K of their keys, ranked
+            unsigned long long theirs[kMaxParts * kMaxTopLogprob / 32];
+#pragma unroll
+            for (int i = 0; i < kMaxParts * kMaxTopLogprob / 32; ++i) {
+              const int at = 32 * i + lane;
+              theirs[i] = at < p.parts * K ? cluster_ptr(sm.best, at / K)[at % K] : 0ull;
+            }
+            const unsigned long long bound = bound_of<8 * sizeof(T)>(theirs, K);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kMaxParts * kMaxTopLogprob / 32; ++i) {
+              const bool in = theirs[i] != 0 && theirs[i] >= bound;
+              const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+              if (in) sm.found[n + __popc(lanes & ((1u << lane) - 1u))] = theirs[i];
+              n += __popc(lanes);
+            }
+            __syncwarp();
+            for (int k = n + lane; k < K; k += 32) sm.best[k] = 0;
+            rank_keys(sm.found, n, K, sm.best, lane);
+          }
           __syncwarp();
         }
         write(first_row);
@@ -646,8 +794,7 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
   }
 }
 
-// Parts of a row: as many as keep rows * parts at or below `times` CTAs an SM and leave a part `least` vectors. Rows alone do
-// from 1216 on:
+// Parts of a row: as many, a power of two, as keep rows * parts at or below `times` CTAs an SM and leave a part `least` vectors.
 int parts_of(int N, long long vecs, int times, long long least) {
   int parts = 1;
   while (parts < kMaxParts && 2LL * N * parts <= 152LL * times && vecs / (2 * parts) >= least) parts *= 2;
@@ -752,13 +899,14 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const __grid_c
 }  // namespace
 
 int launch_logprob_fwd(const LogprobArgs& a, int* status, cudaStream_t stream) {
+  constexpr int kRingBytes = kStages * kPiece * 16;
   const long long vecs = (static_cast<long long>(a.V) * a.elem_bytes + 15) / 16;
   const int parts = parts_of(a.N, vecs, 4, 512);
   FwdParams p{a.logits, a.tok, a.logp, a.entropy, a.lse, a.top_idx, a.top_logp, status, a.N, a.V, a.topk, parts};
   // rows that are not split: as many CTAs as the GPU holds at once, one row after the other each
   const int ctas = parts > 1 ? a.N * parts : std::min(a.N, 4 * 152);
   cudaLaunchAttribute pdl[1], attr[2];
-  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(ctas)), dim3(kFwdThreads), kStages * kPiece * 16, stream, pdl);
+  cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(ctas)), dim3(kFwdThreads), kRingBytes, stream, pdl);
   if (parts > 1) {
     attr[0] = pdl[0];
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -768,8 +916,21 @@ int launch_logprob_fwd(const LogprobArgs& a, int* status, cudaStream_t stream) {
     cfg.numAttrs = 2;
   }
   using bf16 = __nv_bfloat16;
-  const auto fn = a.elem_bytes == 2 ? (a.topk > 0 ? logprob_fwd_kernel<bf16, true> : logprob_fwd_kernel<bf16, false>)
-                                    : (a.topk > 0 ? logprob_fwd_kernel<float, true> : logprob_fwd_kernel<float, false>);
+  static ContextCache<int> setup;   // with the static part of a kernel with alternatives the ring is more than 48 KB
+  int unused = 0;
+  const int rc = setup.get(&unused, [](int&) {
+    const auto allow = [](auto fn) { return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes) == cudaSuccess; };
+    return allow(logprob_fwd_kernel<bf16, kFew>) && allow(logprob_fwd_kernel<bf16, kMany>) && allow(logprob_fwd_kernel<float, kFew>) &&
+                   allow(logprob_fwd_kernel<float, kMany>)
+               ? 0
+               : -3;
+  });
+  if (rc != 0) return rc;
+  const auto of = [&](auto zero) {
+    using T = decltype(zero);
+    return a.topk == 0 ? logprob_fwd_kernel<T, kNone> : a.topk <= kFewBest ? logprob_fwd_kernel<T, kFew> : logprob_fwd_kernel<T, kMany>;
+  };
+  const auto fn = a.elem_bytes == 2 ? of(bf16{}) : of(0.0f);
   const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, p);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
