@@ -5,9 +5,12 @@
 // lowest is taken; what has no page (a position outside the table, an entry outside the pool) is left out. k, and q beside
 // it, turn by their positions first (the formulas and the angles of rope_kernel.cu), in fp32, and are rounded once.
 //
-// Bound by memory: every row is read and written once. Work is dealt out as in rope_kernel.cu: a thread holds one 16-byte vector column (two,
-// R / 2 apart, in the layout of halves) of one token and walks over up to eight heads of q, k or v, so that its sines and
-// cosines, and its token's place, serve all of them.
+// Bound by memory: every row is read and written once. A thread holds two 16-byte vector columns (R / 2 apart in the layout of halves; one of
+// neighbouring pairs) of one token and walks over up to sixteen heads of q, k or v, so that its sines and cosines, and its token's place,
+// serve all of them. Four heads are on their way at a time, into places of shared memory that are the thread's own: held in registers it
+// was one head, and too few bytes were in flight. Threads are in the order (block of tokens, chunk of heads, token, column), so that a
+// warp's threads walk over equally many heads.
+// 4 x up to 8191 tokens, 32 + 8 + 8 heads of 128, bf16 (744 MB): 119 us, 6.2 TB/s; 150 us in registers, 127 with the chunks inside of a token.
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -21,7 +24,19 @@ namespace cover {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kDepth = 4;   // heads of a thread in flight
+constexpr int kMaxBlock = 8;   // tokens of a block
+constexpr int kStageBytes = kDepth * 2 * kThreads * 16;
 using bf16 = __nv_bfloat16;
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
 
 struct AppendTensor {
   const uint8_t* in;
@@ -41,25 +56,29 @@ struct AppendParams {
   const int32_t* rope_pos;  // [B, n] or null: the row's position in the memory
   int n, D, R, M, n_pages, page_log2, Hkv;
   int units, turn_units;    // a row's work items; of them, those that turn
+  bool rest_pairs;          // the others take two vectors
+  int block;                // tokens of a block
   int chunks;
-  long long items;
+  long long tokens, items;
   float mscale;
 };
 
 // T: element of the rows; N: elements of a thread's vector (16 bytes, or one element); kInter: pairs of neighbours.
 template <typename T, int N, bool kInter>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) paged_append_kernel(const __grid_constant__ AppendParams p) {
-  constexpr int kHeadsInFlight = sizeof(T) == 2 ? (kInter ? 2 : 1) : 4;
-  extern __shared__ uint64_t turns[];   // [R / 2]
-  __shared__ uint8_t s_named[kThreads + 1];   // per token of the CTA: a lower row names its position
+__global__ void __launch_bounds__(kThreads, 4) paged_append_kernel(const __grid_constant__ AppendParams p) {
+  extern __shared__ __align__(16) uint8_t smem[];   // wide rows: [kDepth][2][kThreads] vectors; turns [R / 2]
+  constexpr bool kStaged = N > 1;
+  uint64_t* const turns = reinterpret_cast<uint64_t*>(smem + (kStaged ? kStageBytes : 0));
+  __shared__ uint8_t s_named[kThreads + 2 * kMaxBlock];   // per token of the CTA's blocks: a lower row names its position
   const long long item0 = static_cast<long long>(blockIdx.x) * kThreads, item = item0 + threadIdx.x;
   const bool live = item < p.items;
-  const int per_token = p.units * p.chunks;
-  const long long i = live ? item : 0;
-  const long long token = i / per_token;
-  const int rest = static_cast<int>(i - token * per_token);
-  int c = rest / p.units;
-  const int u = rest - c * p.units;
+  const long long i = live ? item : 0, per_block = static_cast<long long>(p.units) * p.chunks * p.block;
+  const long long block = i / per_block;
+  const int in_block = static_cast<int>(i - block * per_block), per_chunk = p.units * static_cast<int>(min(static_cast<long long>(p.block), p.tokens - block * p.block));
+  int c = in_block / per_chunk;
+  const int in_chunk = in_block - c * per_chunk;
+  const long long token = block * p.block + in_chunk / p.units;
+  const int u = in_chunk % p.units;
   const int b = static_cast<int>(token / p.n), s = static_cast<int>(token - static_cast<long long>(b) * p.n);
   int which = 0;
   while (c >= p.t[which].chunks) c -= p.t[which++].chunks;
@@ -69,33 +88,53 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) paged_append
   constexpr int kHalf = kInter ? (N >= 2 ? N / 2 : 1) : N;   // pairs of a work item
   constexpr int kVecs = kInter && N >= 2 ? 1 : 2;            // vectors of a turning work item
   int col0, col1 = 0;
+  bool two = kVecs == 2;                                     // vectors of this one
   if (turn_unit) {
     col0 = kInter ? u * (N >= 2 ? N : 2) : u * N;
     col1 = kInter ? col0 + 1 : col0 + p.R / 2;
   } else {
     col0 = p.R + (u - p.turn_units) * N;
+    col1 = col0 + (p.D - p.R) / 2;
+    two = p.rest_pairs;
   }
   // heads c, c + step, ...: the chunks' threads, neighbours in a warp, take neighbouring heads
   const int step = t.chunks;
   int n = live ? (t.heads - c + step - 1) / step : 0;
   const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + s * t.in_l;
   using V = Vec<T, N>;
-  V x[kHeadsInFlight][2];
-  const auto load = [&](int i0) {
-#pragma unroll
-    for (int j = 0; j < kHeadsInFlight; ++j) {
-      if (i0 + j >= n) break;
-      const T* row = in + (c + (i0 + j) * step) * t.in_h;
-      x[j][0] = *reinterpret_cast<const V*>(row + col0);
-      if (kVecs == 2 && turn_unit) x[j][1] = *reinterpret_cast<const V*>(row + col1);
+  // a thread's places, in no other thread's way
+  const auto slot_of = [&](int k, int w) { return smem + (((k % kDepth) * 2 + w) * kThreads + threadIdx.x) * 16; };
+  // the k-th head's vectors, on their way to the thread's places
+  const auto fetch = [&](int k) {
+    if (k < n) {
+      const T* row = in + (c + k * step) * t.in_h;
+      copy_async16(smem_u32(slot_of(k, 0)), row + col0);
+      if (two) copy_async16(smem_u32(slot_of(k, 1)), row + col1);
     }
+    copy_async_commit();
   };
   griddep_wait();
   griddep_launch_dependents();
   // the first rows are on their way while the frequencies and the places are made ready
   const bool counted = p.count == nullptr || s < __ldg(p.count + b);
   if (!counted && t.pages != nullptr && t.out == nullptr) n = 0;   // padding
-  load(0);
+  if (kStaged) {
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k) fetch(k);
+  }
+  const long long token0 = item0 / per_block * p.block;
+  if (p.pos != nullptr) {
+    // a warp looks through the lists for a token of the CTA's blocks at a time
+    const long long last = (min(item0 + kThreads, p.items) - 1) / per_block;
+    for (long long k = token0 + (threadIdx.x >> 5); k < min((last + 1) * p.block, p.tokens); k += kThreads / 32) {
+      const long long row0 = k / p.n * p.n;
+      const int mine = __ldg(p.pos + k);
+      bool hit = false;
+      for (long long o = row0 + (threadIdx.x & 31); o < k; o += 32) hit |= __ldg(p.pos + o) == mine;
+      hit = __any_sync(0xffffffffu, hit);
+      if ((threadIdx.x & 31) == 0) s_named[k - token0] = hit ? 1 : 0;
+    }
+  }
   int64_t at = p.pos != nullptr ? __ldg(p.pos + token) : static_cast<int64_t>(__ldg(p.start + b)) + s;
   const int64_t angle_at = p.rope_pos != nullptr && turn ? __ldg(p.rope_pos + token) : at;
   int64_t place = -1;   // row of the pages, of head 0
@@ -109,19 +148,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) paged_append
     const double radians = p.inv_freq[k];
     turns[k] = rope_turns(radians);
     bad |= not_finite(radians);
-  }
-  const long long token0 = item0 / per_token;
-  if (p.pos != nullptr) {
-    // a warp looks through the list for a token of the CTA at a time
-    const long long last = min(item0 + kThreads, p.items) - 1;
-    for (long long k = token0 + (threadIdx.x >> 5); k <= last / per_token; k += kThreads / 32) {
-      const long long row0 = k / p.n * p.n;
-      const int mine = __ldg(p.pos + k);
-      bool hit = false;
-      for (long long o = row0 + (threadIdx.x & 31); o < k; o += 32) hit |= __ldg(p.pos + o) == mine;
-      hit = __any_sync(0xffffffffu, hit);
-      if ((threadIdx.x & 31) == 0) s_named[k - token0] = hit ? 1 : 0;
-    }
   }
   bad = __syncthreads_or(bad);
   if (p.pos != nullptr && live && s_named[token - token0] != 0) place = -1;
@@ -141,59 +167,46 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 3) paged_append
     }
   }
   T* const out = t.out == nullptr ? nullptr : reinterpret_cast<T*>(t.out) + (static_cast<size_t>(b) * t.heads * p.n + s) * p.D;
-  for (int i0 = 0; i0 < n; i0 += kHeadsInFlight) {
-    if (i0 > 0) load(i0);
+  for (int k = 0; k < n; ++k) {
+    const int h = c + k * step;
+    V x[2];
+    if constexpr (kStaged) {
+      copy_async_wait<kDepth - 1>();
+      x[0] = *reinterpret_cast<const V*>(slot_of(k, 0));
+      if (two) x[1] = *reinterpret_cast<const V*>(slot_of(k, 1));
+    } else {
+      const T* row = in + h * t.in_h;
+      x[0] = *reinterpret_cast<const V*>(row + col0);
+      if (two) x[1] = *reinterpret_cast<const V*>(row + col1);
+    }
+    if (turn) {
 #pragma unroll
-    for (int j = 0; j < kHeadsInFlight; ++j) {
-      if (i0 + j >= n) break;
-      const int h = c + (i0 + j) * step;
-      if constexpr (sizeof(T) == 2) {
-        // pages and outputs are of one type: a vector is turned where it is
-        if (turn) {
+      for (int e = 0; e < kHalf; ++e) {
+        T& xa = kVecs == 1 ? x[0].v[(2 * e) % N] : x[0].v[e % N];
+        T& xb = kVecs == 1 ? x[0].v[(2 * e + 1) % N] : x[1].v[e % N];
+        const float a = to_f(xa), d = to_f(xb);
+        xa = from_f<T>(a * cs[e] - d * sn[e]);
+        xb = from_f<T>(a * sn[e] + d * cs[e]);
+      }
+    }
 #pragma unroll
-          for (int k = 0; k < kHalf; ++k) {
-            T& xa = kVecs == 1 ? x[j][0].v[(2 * k) % N] : x[j][0].v[k % N];
-            T& xb = kVecs == 1 ? x[j][0].v[(2 * k + 1) % N] : x[j][1].v[k % N];
-            const float a = to_f(xa), d = to_f(xb);
-            xa = from_f<T>(a * cs[k] - d * sn[k]);
-            xb = from_f<T>(a * sn[k] + d * cs[k]);
-          }
-        }
-        if (out != nullptr) {
-          T* row = out + static_cast<size_t>(h) * p.n * p.D;
-          *reinterpret_cast<V*>(row + col0) = x[j][0];
-          if (kVecs == 2 && turn_unit) *reinterpret_cast<V*>(row + col1) = x[j][1];
-        }
-        if (place >= 0) {
-          T* row = reinterpret_cast<T*>(t.pages) + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D;
-          *reinterpret_cast<V*>(row + col0) = x[j][0];
-          if (kVecs == 2 && turn_unit) *reinterpret_cast<V*>(row + col1) = x[j][1];
-        }
-      } else {
-        if (turn) {
+    for (int w = 0; w < 2; ++w) {
+      if (w == 1 && !two) break;
+      const int col = w ? col1 : col0;
+      if (out != nullptr) *reinterpret_cast<V*>(out + static_cast<size_t>(h) * p.n * p.D + col) = x[w];
+      if (place >= 0) {
+        bf16* row = t.pages + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D + col;
+        if constexpr (sizeof(T) == 2) {   // pages and rows are of one type
+          *reinterpret_cast<V*>(row) = x[w];
+        } else {
+          Vec<bf16, N> r;
 #pragma unroll
-          for (int k = 0; k < kHalf; ++k) {
-            T& xa = kVecs == 1 ? x[j][0].v[(2 * k) % N] : x[j][0].v[k % N];
-            T& xb = kVecs == 1 ? x[j][0].v[(2 * k + 1) % N] : x[j][1].v[k % N];
-            const float a = to_f(xa), d = to_f(xb);
-            xa = from_f<T>(a * cs[k] - d * sn[k]);
-            xb = from_f<T>(a * sn[k] + d * cs[k]);
-          }
-        }
-#pragma unroll
-        for (int w = 0; w < kVecs; ++w) {
-          if (w == 1 && !turn_unit) break;
-          const int col = w ? col1 : col0;
-          if (out != nullptr) *reinterpret_cast<V*>(out + static_cast<size_t>(h) * p.n * p.D + col) = x[j][w];
-          if (place >= 0) {
-            Vec<bf16, N> r;
-#pragma unroll
-            for (int e = 0; e < N; ++e) r.v[e] = from_f<bf16>(to_f(x[j][w].v[e]));
-            *reinterpret_cast<Vec<bf16, N>*>(t.pages + (place + (static_cast<int64_t>(h) << p.page_log2)) * p.D + col) = r;
-          }
+          for (int e = 0; e < N; ++e) r.v[e] = from_f<bf16>(to_f(x[w].v[e]));
+          *reinterpret_cast<Vec<bf16, N>*>(row) = r;
         }
       }
     }
+    if (kStaged) fetch(k + kDepth);   // (what was in its places has been stored)
   }
 }
 
@@ -233,21 +246,27 @@ int launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream) {
   if (!wide) n = 1;
   const int per_unit = a.interleaved ? (n >= 2 ? n / 2 : 1) : n;   // pairs of a work item
   p.turn_units = a.R / 2 / per_unit;
-  p.units = p.turn_units + (a.D - a.R) / n;
-  // Heads a thread walks over: see rope_kernel.cu.
+  const int rest = (a.D - a.R) / n;   // vectors that do not turn
+  p.rest_pairs = rest % 2 == 0;
+  p.units = p.turn_units + (p.rest_pairs ? rest / 2 : rest);
+  // Heads a thread walks over: as many, up to 16, as leave 512 threads an SM (10 x 1253 tokens, 32 + 32 + 32 heads of 64: 54 us with up to 8, 48 so).
   const long long tokens = static_cast<long long>(a.B) * a.n;
   const long long all = tokens * p.units * (a.Hq + 2LL * a.Hkv);
-  const int chunk = static_cast<int>(std::min<long long>(8, std::max<long long>(1, all / (152 * 512))));
+  const int chunk = static_cast<int>(std::min<long long>(16, std::max<long long>(1, all / (152 * 512))));
   for (AppendTensor& t : p.t) {
     t.chunks = (t.heads + chunk - 1) / chunk;
     p.chunks += t.chunks;
   }
-  if (static_cast<long long>(p.chunks) * p.units > 0x7fffffffLL) return -2;
+  if (static_cast<long long>(p.chunks) * p.units > 0x7fffffffLL / kMaxBlock) return -2;
+  // A CTA looks through a list for each of its blocks' tokens, so blocks are small where there is one (8 x 63 listed tokens, 64 heads of 64,
+  // fp32: blocks of 8 5.1 us, of 2 4.4; 34 x 988 tokens in a run, 20 heads: 41 and 56).
+  p.block = a.pos != nullptr ? 2 : kMaxBlock;
+  p.tokens = tokens;
   p.items = tokens * p.chunks * p.units;
   const long long grid = (p.items + kThreads - 1) / kThreads;
   if (grid > 0x7fffffffLL) return -2;
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), static_cast<size_t>(a.R / 2) * 8, stream, attr);
+  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), (wide ? kStageBytes : 0) + static_cast<size_t>(a.R / 2) * 8, stream, attr);
   cudaError_t r;
   if (e == 2)
     r = wide ? (a.interleaved ? cudaLaunchKernelEx(&cfg, paged_append_kernel<bf16, 8, true>, p)
