@@ -1001,11 +1001,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attn_paged_join_rows_kernel(c
 // ---------------------------------------------------------------------------
 // A CTA takes two Q tiles of 128 packed rows, a stream each, that read each KV tile together, against one of nsplit parts of the keys that its
 // rows see. Two threads of different warpgroups share a row, 64 columns each, in two chunks of 32.
-// Roles (640 threads): warps 0-15 softmax (warpgroup 2 t + h: columns 64 h .. 64 h + 63 of Q tile t); 16 products; 17, 18 copies of K and V;
-// 19 looks V tiles through.
+// Roles (640 threads): warps 0-15 softmax (warpgroup 2 t + h: columns 64 h .. 64 h + 63 of Q tile t); 16 products; 17, 18 copies of K and V.
+// The softmax warps look V tiles through.
 // Shared memory: Q (2 x 32 KB) | two tiles of K, two of V. Tensor memory: S0 | S1 (the P of a half overwrites the first 32 columns of that
 // half's scores, behind its loads) | O0 | O1, 128 columns each.
-constexpr int kPairsThreads = 608;
+constexpr int kPairsThreads = 640;   // (the last warp has no part: with 19 warps 2048 rows over 8192 keys took 270 us, with 20 266)
 constexpr int kPairSoftmaxWarps = 16, kPairMmaWarp = 16, kPairCopyWarp = 17;
 
 struct PairSmem {
@@ -1416,25 +1416,12 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
   } else {
     // ---------------- softmax ----------------
     const size_t self = (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds + (is_seed ? slot : 0);
-    // the seed rows' own scores (log2 units), in the first part of the keys that is not empty alone: Q is there, and each of a row's threads takes half
-    // of the columns
-    float s_self = -INFINITY;
-    bool ok = true;
-    if (own_hi >= 0 && ks == 0) {
-      ok = nt == 0 || warp_wait(&sm.q_full, 0, &sm.abort);
-      float product = 0.0f;
-      if (ok && nt > 0 && is_seed) {
-        product = self_product(sm.q[tile] + half * kBoxBytes, R, p.k_seedmask + self * kD + half * kHalf);
-        prefetch_l2(p.v_seedmask + self * kD + half * kHalf);
-      }
-      sm.red[tile][half][R] = product;
-      sync_of<256>(2 + tile);
-      if (is_seed) {
-        const float s = sm.red[tile][0][R] + sm.red[tile][1][R];
-        s_self = kCap ? capped(s, p.cap_in, p.cap_log2) : s * p.scale_log2;
-      }
-      sync_of<256>(2 + tile);
+    const bool own_here = own_hi >= 0 && ks == 0;   // the seed rows' own pairs are added in the first part of the keys
+    if (own_here && is_seed) {
+      prefetch_l2(p.k_seedmask + self * kD + half * kHalf);
+      prefetch_l2(p.v_seedmask + self * kD + half * kHalf);
     }
+    bool ok = true;
     const bool warp_live = __any_sync(0xffffffffu, valid);
     const uint32_t quad = tbase + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = quad + tile * kBN + half * kHalf;
@@ -1443,9 +1430,8 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     float m_run = fixed ? p.cap_ref : -INFINITY, l_run = 0.0f;
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
     // Where some row does not see some key, V is looked through for rows that are not finite while the scores are waited for: a warp eight
-    // keys, or sixteen (a warp for all of it took a tile 1.5 us). What was found is read a tile later, when V's products are through.
+    // keys, or sixteen (a warp for all of it took a tile 1.5 us). What was found is read a tile later.
     const auto found = [&](int j) {
-      if (!partial(j)) return;
       if (!warp_wait(&sm.v_clean[j & 1], (j >> 1) & 1, &sm.abort)) {
         ok = false;
         return;
@@ -1462,13 +1448,15 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       }
     };
     const bool keyless = __any_sync(0xffffffffu, valid && !some_keys);   // a row of the warp sees no key at all
+    bool masked = false;
     for (int j = 0; j < jend; ++j) {
       const int key0 = (j0 + j) * kBN + half * kHalf;
-      const bool masked = partial(j);
+      if (masked) found(j - 1);
+      masked = partial(j);
       Seen u{0xffffffffu, 0xffffffffu, false, false};
       bool some = warp_live;   // a warp none of whose rows sees a key here stores zeros; a row without a query row may hold anything
       if (masked) {
-        ok = warp_wait(&sm.v_full[j & 1], (j >> 1) & 1, &sm.abort);   // (its copy waits for the products of tile j - 2 alone)
+        ok = warp_wait(&sm.v_full[j & 1], (j >> 1) & 1, &sm.abort) && ok;   // (its copy waits for the products of tile j - 2 alone)
         if (ok)
           for (int g = warp; g < kBN / 8; g += two_tiles ? kPairSoftmaxWarps : kPairSoftmaxWarps / 2)
             screen_group(smem_u32(sm.v[j & 1]) + g * kGroupBytes, reinterpret_cast<uint8_t*>(&sm.nan_keys[j & 3]) + g, lane);
@@ -1495,7 +1483,6 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
         some = __any_sync(0xffffffffu, valid && (u.first | u.second) != 0);
       }
       ok = warp_wait(&sm.s_full[tile], j & 1, &sm.abort) && ok;
-      if (ok && j > 0) found(j - 1);
       tc_fence_after_sync();   // zeros are stored over S too, where no row sees a key
       if (fixed) {
         if (!ok) break;
@@ -1550,8 +1537,24 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       tc_fence_before_sync();
       mbar_arrive(&sm.p_full[tile]);
     }
+    // Their scores (log2 units), while V's last products are on their way: Q is still there, and each of a row's threads takes half of the
+    // columns. (Before the first scores, 32 rows over 1024 keys with 32 seeds took 0.5 us more.)
+    float s_self = -INFINITY;
+    if (own_here) {
+      float product = 0.0f;
+      ok = ok && (nt == 0 || warp_wait(&sm.q_full, 0, &sm.abort));
+      if (ok && nt > 0 && is_seed) product = self_product(sm.q[tile] + half * kBoxBytes, R, p.k_seedmask + self * kD + half * kHalf);
+      sync_of<256>(2 + tile);   // the last references have been read
+      sm.red[tile][half][R] = product;
+      sync_of<256>(2 + tile);
+      if (is_seed) {
+        const float s = sm.red[tile][0][R] + sm.red[tile][1][R];
+        s_self = kCap ? capped(s, p.cap_in, p.cap_log2) : s * p.scale_log2;
+      }
+      if (p.joined) sync_of<kKnowing>(1);   // a tile's results are staged where the other tile's Q is
+    }
     if (ok && nt > 0) ok = warp_wait(&sm.o_full, 0, &sm.abort);
-    if (ok && jend > 0) found(jend - 1);
+    if (ok && masked) found(jend - 1);
     if (!ok && lane == 0) {
       if (!sm.abort) report_status(p.status, kStatusTimeout, 88);
       sm.abort = 1;
