@@ -764,11 +764,25 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             uint32_t x[16];
             tmem_ld16(s_addr + c0, x);
             tmem_ld_wait16(x);
+            float far = 0.0f;
+            if (kCap) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              if (kCap && e % 4 == 0 && c0 + e >= n_rows) break;   // (a cap is not worked out for rows that are none)
-              const float f = __uint_as_float(x[e]);
-              t[c0 + e] = kCap ? capped(f, p.cap_in, p.cap_log2) - m[c0 + e] : fmaf(f, p.scale_log2, -m[c0 + e]);
+              for (int e = 0; e < 16; e += 2) far = fmax3(far, fabsf(__uint_as_float(x[e])), fabsf(__uint_as_float(x[e + 1])));
+            }
+            if (kCap && __any_sync(0xffffffffu, !(far <= p.cap_near))) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                if (e % 4 == 0 && c0 + e >= n_rows) break;   // (a cap is not worked out for rows that are none)
+                t[c0 + e] = capped(__uint_as_float(x[e]), p.cap_in, p.cap_log2) - m[c0 + e];
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float f = __uint_as_float(x[e]), z = f * f;
+                // (the pairs kernel's polynomial of a cap)
+                if (kCap) t[c0 + e] = fmaf(f, fmaf(z, fmaf(z, fmaf(z, p.cap_poly[3], p.cap_poly[2]), p.cap_poly[1]), p.cap_poly[0]), -m[c0 + e]);
+                else t[c0 + e] = fmaf(f, p.scale_log2, -m[c0 + e]);
+              }
             }
           }
           if (partial) {
