@@ -189,15 +189,28 @@ __device__ __forceinline__ void sync_of(int barrier) {
 
 // Parts that a cluster's CTAs add up themselves: each stages its rows' accumulators [row][128] fp32 and (m, l) in its own
 // shared memory, and CTA `rank` finishes the rows rank, rank + parts, .., a warp a row, reading all CTAs'. Rows' 16-byte
-// pieces are swizzled, for threads that write a row each.
+// pieces are swizzled, for threads that write a row each. A seed row's own pair is one part more, where the rows' slots are given: its score
+// is in CTA 0's shared memory.
 constexpr int kMaxJoined = 8;   // a cluster's portable size
 __device__ __forceinline__ uint32_t staged_at(int row, int c4) { return row * (kD * 4) + ((c4 ^ (row & 31)) << 4); }
 
 template <int kWarps>
-__device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint32_t ml, int n_rows, long long orow0, int rank, int parts) {
+__device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint32_t ml, int n_rows, long long orow0, int rank, int parts,
+                                          const int* slots = nullptr, uint32_t scores = 0, const __nv_bfloat16* values = nullptr) {
   const int lane = threadIdx.x & 31;
   for (int row = rank + parts * static_cast<int>(threadIdx.x >> 5); row < n_rows; row += parts * kWarps) {
     float2 mine = make_float2(-INFINITY, 0.0f);
+    const int slot = slots != nullptr ? slots[row] : kNoSlot;
+    float4 own = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (slot != kNoSlot) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(values + static_cast<size_t>(slot) * kD) + lane);
+      own = make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+      if (lane == kMaxJoined) {
+        const uint32_t at = cluster_map(scores + 4 * row, 0);
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(mine.x) : "r"(at) : "memory");
+        mine.y = mine.x == -INFINITY ? 0.0f : 1.0f;
+      }
+    }
     if (lane < parts) {
       const uint32_t at = cluster_map(ml + 8 * row, lane);
       asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(mine.x), "=f"(mine.y) : "r"(at) : "memory");
@@ -214,16 +227,18 @@ __device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint
                      : "memory");
       }
     }
-    float m = mine.x;
+    float m = mine.x;   // (lanes up to kMaxJoined hold one)
 #pragma unroll
-    for (int d = kMaxJoined / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int d = kMaxJoined; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     m = __shfl_sync(0xffffffffu, m, 0);
     const float w = mine.x == -INFINITY ? 0.0f : ex2_approx(mine.x - m);
     float l = mine.x == -INFINITY ? mine.y : w * mine.y;   // (a sum of NaN is taken along)
 #pragma unroll
-    for (int d = kMaxJoined / 2; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    for (int d = kMaxJoined; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     l = __shfl_sync(0xffffffffu, l, 0);
+    const float w_own = __shfl_sync(0xffffffffu, w, kMaxJoined);
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (w_own != 0.0f) acc = make_float4(w_own * own.x, w_own * own.y, w_own * own.z, w_own * own.w);
 #pragma unroll
     for (int k = 0; k < kMaxJoined; ++k) {
       const float wk = __shfl_sync(0xffffffffu, w, k);
@@ -1030,6 +1045,8 @@ struct PairSmem {
   uint64_t s_full[2], p_full[2], o_full, drain;
   uint4 nan_keys[4];                    // per KV tile in turn: keys whose V row is not finite
   float2 ml[2 * kBM];                   // joined in a cluster: the rows' references and sums
+  float s_self[2 * kBM];                // and their own pairs' scores and slots
+  int own_slot[2 * kBM];
   float red[2][2][kBM];                 // per Q tile and half of the columns
   int slot[2 * kBM];                    // seed slot of a row's position, or kNoSlot
   int lo, hi;                           // keys that some row sees
@@ -1581,7 +1598,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     sync_of<256>(2 + tile);
     float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
     if (l == 0.0f) m = -INFINITY, w = 0.0f;     // no key was seen
-    if (s_self != -INFINITY) {
+    if (s_self != -INFINITY && !p.joined) {
       const float m_all = fmaxf(m, s_self);
       const float f = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
       p_self = ex2_approx(s_self - m_all);
@@ -1589,7 +1606,8 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
       w = f;
       m = m_all;
     }
-    if (s_self != s_self) l = s_self;           // NaN in the masked-input pair
+    if (s_self != s_self && !p.joined) l = s_self;   // NaN in the masked-input pair
+    if (p.joined && half == 0) sm.s_self[tile * kBM + R] = s_self, sm.own_slot[tile * kBM + R] = slot;
     const long long orow = rowbase + P;
     const bool split = p.nsplit > 1;
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);   // 1 / l, once a row; zero where no key was seen
@@ -1650,7 +1668,10 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     if (p.joined) {
       __syncwarp();
       cluster_sync();   // every CTA's rows are staged
-      join_rows<kPairSoftmaxWarps>(p, staged, smem_u32(sm.ml), min(2 * kBM, n_packed - p0), rowbase + p0, ks, p.nsplit);
+      // the seed rows' own pairs are added with the parts (by the first CTA alone they held the others up for 1.1 us)
+      join_rows<kPairSoftmaxWarps>(p, staged, smem_u32(sm.ml), min(2 * kBM, n_packed - p0), rowbase + p0, ks, p.nsplit,
+                                   p.n_seeds > 0 ? sm.own_slot : nullptr, smem_u32(sm.s_self),
+                                   p.v_seedmask + (static_cast<size_t>(b) * p.Hkv + hkv) * p.n_seeds * kD);
       __syncwarp();
       cluster_sync();   // no CTA leaves while its rows are read
     }
