@@ -248,7 +248,7 @@ __device__ __noinline__ Sums careful_sums(const Row<T>& row, int w0, int w1, boo
 // Alternatives asked for: none, up to kFewBest, or more. For few the threads' best vectors are enough, and the K best of the threads are taken
 // one after the other. For more, threads with two or three of the best ones are no exception and taking is slow: a thread keeps two vectors
 // and the bound is found by halving. Measured the first / second way, 2048 rows of 126464 bf16: 1 alternative 88 / 97 us, 5 89 / 98, 20 101 / 99,
-// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 10.8, 29 / 17.
+// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 10.0, 29 / 17.
 enum Best { kNone, kFew, kMany };
 constexpr int kFewBest = 16;
 
@@ -286,52 +286,59 @@ __device__ __forceinline__ unsigned long long merge_best(int K, Next&& next, Tak
   return last;
 }
 
-// A bound that K of a warp's keys, kLists a lane, are not below, found by halving, the values first (the upper kBits of a key), then the indices
-// of the keys of the value that is cut; 0 where there are fewer than K keys.
+// A bound that K to K + K / 4 of a warp's keys, and at most kMaxTopLogprob, are not below (kLists keys a lane), found by halving, the values
+// first (the upper kBits of a key), then the indices of the keys of the value that is cut; 0 where there are fewer than K keys. (Exactly K: the 20
+// best of one row of 32000 10.8 us, 10.0 so; more to look at costs 2048 rows of 126464 1 %.)
 template <int kBits, int kLists>
 __device__ __forceinline__ unsigned long long bound_of(const unsigned long long (&keys)[kLists], int K) {
+  const int most = min(K + K / 4, kMaxTopLogprob);
+  const auto upper = [](unsigned long long key) { return static_cast<uint32_t>(key >> (64 - kBits)); };
+  // the lowest key of a value (the lower half of the word of a bf16 is zeros, or ones where it is negative)
+  const auto of_value = [](uint32_t u) {
+    const uint32_t word = kBits == 32 ? u : (u << 16) | ((u & 0x8000u) != 0 ? 0u : 0xffffu);
+    return static_cast<unsigned long long>(word) << 32;
+  };
   uint32_t hi = 0, lo = 0xffffffffu;
   int n = 0;
 #pragma unroll
   for (int i = 0; i < kLists; ++i) {
-    const uint32_t u = static_cast<uint32_t>(keys[i] >> (64 - kBits));
     if (keys[i] == 0) continue;
-    hi = max(hi, u), lo = min(lo, u), ++n;
+    hi = max(hi, upper(keys[i])), lo = min(lo, upper(keys[i])), ++n;
   }
-  if (__reduce_add_sync(0xffffffffu, n) < K) return 0;
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (n < K) return 0;
   hi = __reduce_max_sync(0xffffffffu, hi), lo = __reduce_min_sync(0xffffffffu, lo);
-  const auto halve = [&](uint32_t& from, uint32_t to, int want, auto&& is) {   // the lowest start of `want` of them, or of more
-    while (from < to) {
+  // moves `from` up to the last start of `least` or more; n: how many that is
+  const auto halve = [&](uint32_t& from, uint32_t to, int least, int enough, auto&& is) {
+    while (from < to && n > enough) {
       const uint32_t mid = from + (to - from + 1) / 2;
       int c = 0;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) c += is(keys[i], mid) ? 1 : 0;
       c = __reduce_add_sync(0xffffffffu, c);
-      if (c >= want) from = mid;
+      if (c >= least) from = mid, n = c;
       else to = mid - 1;
-      if (c == want) return true;
     }
-    return false;
   };
-  const auto upper = [](unsigned long long key) { return static_cast<uint32_t>(key >> (64 - kBits)); };
-  if (halve(lo, hi, K, [&](unsigned long long key, uint32_t mid) { return upper(key) >= mid; }))
-    return static_cast<unsigned long long>(lo) << (64 - kBits);
-  // keys of value lo: all of them are too many, or just enough
-  int above = 0;
-  uint32_t first = 0xffffffffu, last = 0, word = 0;
+  halve(lo, hi, K, most, [&](unsigned long long key, uint32_t mid) { return upper(key) >= mid; });
+  const unsigned long long value = of_value(lo);
+  if (n <= most) return value;
+  // too many are of value lo
+  int above = 0, ties = 0;
+  uint32_t first = 0xffffffffu, last = 0;
 #pragma unroll
   for (int i = 0; i < kLists; ++i) {
     above += upper(keys[i]) > lo ? 1 : 0;
     if (keys[i] == 0 || upper(keys[i]) != lo) continue;
     const uint32_t low = static_cast<uint32_t>(keys[i]);
-    first = min(first, low), last = max(last, low), word = static_cast<uint32_t>(keys[i] >> 32);
+    first = min(first, low), last = max(last, low), ++ties;
   }
-  above = __reduce_add_sync(0xffffffffu, above);
-  first = __reduce_min_sync(0xffffffffu, first), last = __reduce_max_sync(0xffffffffu, last), word = __reduce_max_sync(0xffffffffu, word);
-  halve(first, last, K - above, [&](unsigned long long key, uint32_t mid) {
+  above = __reduce_add_sync(0xffffffffu, above), n = __reduce_add_sync(0xffffffffu, ties);
+  first = __reduce_min_sync(0xffffffffu, first), last = __reduce_max_sync(0xffffffffu, last);
+  halve(first, last, K - above, most - above, [&](unsigned long long key, uint32_t mid) {
     return upper(key) == lo && key != 0 && static_cast<uint32_t>(key) >= mid;
   });
-  return (static_cast<unsigned long long>(word) << 32) | first;
+  return value | first;
 }
 
 // Puts the n keys of `from` in order, the K best of them into `to`: a key's place is the number of those in front of it.
