@@ -47,8 +47,9 @@ constexpr int kGroupBytes = 2048, kGroupHalf = 1024;   // of K and V: eight rows
 constexpr int kHalf = kBN / 2;
 constexpr int kMaxTilePages = kBN / 16;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
-// Capped scores lie in [-C, C], C = cap log2(e). Up to C = kFixedCap (caps up to 55) the pairs kernel takes the same reference for every row, C - kFixedRange or 0,
-// and looks for no maxima: weights lie in [2^(kFixedRange - 2 C), 2^kFixedRange], at least 2^-100, and sums over L keys hold values up to 2^66 / L.
+// Capped scores lie in [-C, C], C = cap log2(e). Up to C = kFixedCap (caps up to 55) the pairs kernel takes the same reference
+// for every row, C - kFixedRange or 0, and looks for no maxima: weights lie in [2^(kFixedRange - 2 C), 2^kFixedRange], at least 2^-100, and sums
+// over L keys hold values up to 2^66 / L.
 constexpr float kFixedCap = 80.0f, kFixedRange = 60.0f;
 constexpr int kSms = 152;                  // of this GPU
 constexpr float kNan = __builtin_nanf("");
@@ -204,7 +205,8 @@ __device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint
     float4 own = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (slot != kNoSlot) {
       const uint2 v = __ldg(reinterpret_cast<const uint2*>(values + static_cast<size_t>(slot) * kD) + lane);
-      own = make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+      own = make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                        __uint_as_float(v.y & 0xffff0000u));
       if (lane == kMaxJoined) {
         const uint32_t at = cluster_map(scores + 4 * row, 0);
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(mine.x) : "r"(at) : "memory");
@@ -581,7 +583,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       }
       if (!is_v && (kJoined ? i == 0 : sm.job[at].first != 0)) {
         const int unit = kJoined ? 0 : sm.job[at].unit, buf = unit % kQ;
-        const int q_row = kJoined ? static_cast<int>((static_cast<long long>(b0) * p.Hq + h * p.G) * p.Lq + (u0 % p.n_groups) * kN) : sm.job[at].q_row;
+        const int q_row = kJoined ? static_cast<int>((static_cast<long long>(b0) * p.Hq + h * p.G) * p.Lq + (u0 % p.n_groups) * kN)
+                                  : sm.job[at].q_row;
         if (unit >= kQ) ok = warp_wait(&sm.q_empty[buf], (unit / kQ - 1) & 1, &sm.abort);
         if (!ok) break;
         if (lane == 0) {
@@ -901,8 +904,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       // ---------------- the rows' results ----------------
       if (ok) {
         tc_fence_after_sync();
-        // sums over the warp: each step adds up and hands on half of the rows, until a lane has one. (The code of a unit's end is kept short: in a call
-        // of a few tiles it runs once, out of a cold instruction cache. Unrolled over all rows it took 1.9 us.)
+        // sums over the warp: each step adds up and hands on half of the rows, until a lane has one. (The code of a unit's end is kept short: in
+        // a call of a few tiles it runs once, out of a cold instruction cache. Unrolled over all rows it took 1.9 us.)
 #pragma unroll
         for (int d = 16, left = kN; left > 1; d >>= 1, left >>= 1) {
           const bool upper = (lane & d) != 0;
@@ -1728,8 +1731,9 @@ constexpr int kClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
 // Predicted microseconds, fitted to calls back to back on GB300, measured / predicted. Rows of 16 joined: one token over 777 keys (28 / 4 heads,
 // 7 CTAs a unit) 7.6 / 7.7, over 4096 (32 / 8, 8) 12.0 / 11.8, 16 sequences of 500 (1) 12.8 / 13.3, 29 of 51 (1) 16.1 / 16.8. In even shares
 // 11.5 / 13.0, 15.6 / 14.5, 18.8 / 17.0, 12.7 / 16.4; 128 sequences of 120 29.3 / 30.6, 256 of 100 48.2 / 49.7, 64 of 512 39.5 / 32.2. Rows of 32
-// joined 12.6 / 13.0 (32 rows over 2048, 32 / 8), in even shares 8 sequences of 32 over 4000 44.6 / 38.7. Pairs joined: 8 rows over 2048 (32 / 8, 8 CTAs a unit) 10.2 / 10.9,
-// 8 sequences of 8 rows over 1000 (2) 15.6 / 16.6, 5 of 75 over 699 (16 / 2, 3) 15.3 / 16.9; by a second kernel 16.0 / 18.0; in one wave 18.5 / 18.1.
+// joined 12.6 / 13.0 (32 rows over 2048, 32 / 8), in even shares 8 sequences of 32 over 4000 44.6 / 38.7. Pairs joined: 8 rows over 2048
+// (32 / 8, 8 CTAs a unit) 10.2 / 10.9, 8 sequences of 8 rows over 1000 (2) 15.6 / 16.6, 5 of 75 over 699 (16 / 2, 3) 15.3 / 16.9; by a second
+// kernel 16.0 / 18.0; in one wave 18.5 / 18.1.
 Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
   const long long packed = static_cast<long long>(Hq / Hkv) * Lq;
   const long long nkv = (static_cast<long long>(M) * page + kBN - 1) / kBN;   // KV tiles of a sequence at most
@@ -1745,7 +1749,8 @@ Plan plan_of(int B, int Hq, int Hkv, int Lq, int M, int page) {
     const long long units = static_cast<long long>(B) * Hkv;
     const double tile = few ? 1.48 : 2.2, fill = B > 1 && nkv > 1 ? 0.75 : 1.0;
     const int ctas = static_cast<int>(std::min<long long>(kSms, std::min<long long>(units, kSms) * std::min<long long>(nkv, kSms)));
-    consider(Plan{mode, 1, 1, ctas, 0}, (few ? 11.5 : 14.0) + tile * std::ceil(fill * static_cast<double>(units) * nkv / kSms) + 1.3 * static_cast<double>(units) / kSms);
+    const double each = static_cast<double>(units) / kSms;
+    consider(Plan{mode, 1, 1, ctas, 0}, (few ? 11.5 : 14.0) + tile * std::ceil(fill * each * nkv) + 1.3 * each);
     for (int c = 1; c <= kMaxJoined && c <= nkv; ++c) {
       const double waves = std::ceil(static_cast<double>(units) / kClusters[c - 1]);
       consider(Plan{mode, 1, 1, 0, c}, (few ? 6.3 : 9.8) + (units * c > kSms / 2 ? 1.5 : 0.0) + 6.2 * (waves - 1) +
@@ -1897,7 +1902,8 @@ int launch_attn_paged(const AttnPagedArgs& a, int* status, cudaStream_t stream) 
   if (e == cudaSuccess && parts > 0) {
     const dim3 join_grid = few ? dim3(width / kJoinWarps, plan.ctas) : dim3(static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps));
     cfg = pdl_config(join_grid, dim3(kJoinWarps * 32), 0, stream, pdl);
-    e = cudaLaunchKernelEx(&cfg, few ? (m == 0 ? attn_paged_join_rows_kernel<16> : attn_paged_join_rows_kernel<32>) : attn_paged_join_pairs_kernel, p);
+    const auto join = !few ? attn_paged_join_pairs_kernel : m == 0 ? attn_paged_join_rows_kernel<16> : attn_paged_join_rows_kernel<32>;
+    e = cudaLaunchKernelEx(&cfg, join, p);
   }
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? 0 : -3;
 }

@@ -74,7 +74,8 @@ __global__ void __launch_bounds__(kThreads, 4) paged_append_kernel(const __grid_
   const bool live = item < p.items;
   const long long i = live ? item : 0, per_block = static_cast<long long>(p.units) * p.chunks * p.block;
   const long long block = i / per_block;
-  const int in_block = static_cast<int>(i - block * per_block), per_chunk = p.units * static_cast<int>(min(static_cast<long long>(p.block), p.tokens - block * p.block));
+  const int in_block = static_cast<int>(i - block * per_block);
+  const int per_chunk = p.units * static_cast<int>(min(static_cast<long long>(p.block), p.tokens - block * p.block));
   int c = in_block / per_chunk;
   const int in_chunk = in_block - c * per_chunk;
   const long long token = block * p.block + in_chunk / p.units;
@@ -223,7 +224,8 @@ int launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream) {
   AppendParams p{};
   const int64_t* st = a.strides;   // of k, v, q
   p.t[0] = AppendTensor{static_cast<const uint8_t*>(a.q), static_cast<uint8_t*>(a.q_out), nullptr, st[6], st[7], st[8], a.Hq, 0};
-  p.t[1] = AppendTensor{static_cast<const uint8_t*>(a.k), static_cast<uint8_t*>(a.k_out), static_cast<bf16*>(a.k_pages), st[0], st[1], st[2], a.Hkv, 0};
+  p.t[1] = AppendTensor{static_cast<const uint8_t*>(a.k), static_cast<uint8_t*>(a.k_out), static_cast<bf16*>(a.k_pages),
+                        st[0], st[1], st[2], a.Hkv, 0};
   p.t[2] = AppendTensor{static_cast<const uint8_t*>(a.v), nullptr, static_cast<bf16*>(a.v_pages), st[3], st[4], st[5], a.Hkv, 0};
   p.inv_freq = a.inv_freq;
   p.table = a.table;
@@ -266,7 +268,8 @@ int launch_paged_append(const PagedAppendArgs& a, cudaStream_t stream) {
   const long long grid = (p.items + kThreads - 1) / kThreads;
   if (grid > 0x7fffffffLL) return -2;
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), (wide ? kStageBytes : 0) + static_cast<size_t>(a.R / 2) * 8, stream, attr);
+  const size_t smem = (wide ? kStageBytes : 0) + static_cast<size_t>(a.R / 2) * 8;
+  const cudaLaunchConfig_t cfg = pdl_config(dim3(static_cast<unsigned>(grid)), dim3(kThreads), smem, stream, attr);
   cudaError_t r;
   if (e == 2)
     r = wide ? (a.interleaved ? cudaLaunchKernelEx(&cfg, paged_append_kernel<bf16, 8, true>, p)
