@@ -248,7 +248,7 @@ __device__ __noinline__ Sums careful_sums(const Row<T>& row, int w0, int w1, boo
 // Alternatives asked for: none, up to kFewBest, or more. For few the threads' best vectors are enough, and the K best of the threads are taken
 // one after the other. For more, threads with two or three of the best ones are no exception and taking is slow: a thread keeps two vectors
 // and the bound is found by halving. Measured the first / second way, 2048 rows of 126464 bf16: 1 alternative 88 / 97 us, 5 89 / 98, 20 101 / 99,
-// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 10.0, 29 / 17.
+// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 8.9, 29 / 17.
 enum Best { kNone, kFew, kMany };
 constexpr int kFewBest = 16;
 
@@ -288,7 +288,7 @@ __device__ __forceinline__ unsigned long long merge_best(int K, Next&& next, Tak
 
 // A bound that K to K + K / 4 of a warp's keys, and at most kMaxTopLogprob, are not below (kLists keys a lane), found by halving, the values
 // first (the upper kBits of a key), then the indices of the keys of the value that is cut; 0 where there are fewer than K keys. (Exactly K: the 20
-// best of one row of 32000 10.8 us, 10.0 so; more to look at costs 2048 rows of 126464 1 %.)
+// best of one row of 32000 took 0.8 us more; what is looked at besides costs 2048 rows of 126464 1 %.)
 template <int kBits, int kLists>
 __device__ __forceinline__ unsigned long long bound_of(const unsigned long long (&keys)[kLists], int K) {
   const int most = min(K + K / 4, kMaxTopLogprob);
@@ -765,22 +765,28 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
                          if (lane == 0) sm.best[k] = key;
                        });
           } else {
-            // the parts' lists: K of their keys, ranked
-            unsigned long long theirs[kMaxParts * kMaxTopLogprob / 32];
-#pragma unroll
-            for (int i = 0; i < kMaxParts * kMaxTopLogprob / 32; ++i) {
-              const int at = 32 * i + lane;
-              theirs[i] = at < p.parts * K ? cluster_ptr(sm.best, at / K)[at % K] : 0ull;
-            }
-            const unsigned long long bound = bound_of<8 * sizeof(T)>(theirs, K);
+            // the parts' lists: K of their keys or little more, ranked (held in six keys a lane where that is enough: with sixteen, mostly
+            // none, the 20 best of one row of 152064 took 11.7 us, so 10.7)
             int n = 0;
+            const auto pick = [&](auto lists) {
+              constexpr int kLists = decltype(lists)::value;
+              unsigned long long theirs[kLists];
 #pragma unroll
-            for (int i = 0; i < kMaxParts * kMaxTopLogprob / 32; ++i) {
-              const bool in = theirs[i] != 0 && theirs[i] >= bound;
-              const uint32_t lanes = __ballot_sync(0xffffffffu, in);
-              if (in) sm.found[n + __popc(lanes & ((1u << lane) - 1u))] = theirs[i];
-              n += __popc(lanes);
-            }
+              for (int i = 0; i < kLists; ++i) {
+                const int at = 32 * i + lane;
+                theirs[i] = at < p.parts * K ? cluster_ptr(sm.best, at / K)[at % K] : 0ull;
+              }
+              const unsigned long long bound = bound_of<8 * sizeof(T)>(theirs, K);
+#pragma unroll
+              for (int i = 0; i < kLists; ++i) {
+                const bool in = theirs[i] != 0 && theirs[i] >= bound;
+                const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+                if (in) sm.found[n + __popc(lanes & ((1u << lane) - 1u))] = theirs[i];
+                n += __popc(lanes);
+              }
+            };
+            if (p.parts * K <= 6 * 32) pick(std::integral_constant<int, 6>{});
+            else pick(std::integral_constant<int, kMaxParts * kMaxTopLogprob / 32>{});
             __syncwarp();
             for (int k = n + lane; k < K; k += 32) sm.best[k] = 0;
             rank_keys(sm.found, n, K, sm.best, lane);
