@@ -31,6 +31,7 @@
 #include "cluster.cuh"
 #include "context.cuh"
 #include "kernels.cuh"
+#include "paged_ring.cuh"
 #include "ptx.cuh"
 #include "route.cuh"
 #include "tmap.cuh"
@@ -283,7 +284,7 @@ __device__ __forceinline__ void join_pass() {
 // Tensor memory: S0 | S1 | O0 | O1, kN columns each.
 constexpr int kRowsThreads = 512;
 constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsCopyWarp = 13, kRowsPlanWarp = 14;
-constexpr int kSlots = 5, kRing = 8, kUnits = 8;
+constexpr int kSlots = paged_ring::kSlots, kRing = 8, kUnits = 8;
 
 struct TileJob {
   int page[kMaxTilePages];   // entries of its pages, -1 for none
@@ -302,7 +303,7 @@ struct RowsSmem {
   uint8_t kv[kSlots][kTileBytes];
   uint8_t q[kQueries<kN>][kN * kD * 2];
   uint8_t pt[2][kBN * 128];
-  uint64_t full[kSlots], empty[kSlots];
+  uint64_t k_full[paged_ring::kBarriers], v_full[paged_ring::kBarriers], empty[kSlots];
   uint64_t q_full[kQueries<kN>], q_empty[kQueries<kN>];
   uint64_t job_full[kRing], job_empty[kRing], v_clean[kRing];
   uint64_t unit_full[kUnits], unit_empty[kUnits];
@@ -361,7 +362,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 
   if (warp == kRowsMmaWarp) {
     if (lane == 0) {
-      for (int i = 0; i < kSlots; ++i) mbar_init(&sm.full[i], 1), mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < kSlots; ++i) mbar_init(&sm.empty[i], 1);
+      for (int i = 0; i < paged_ring::kBarriers; ++i) mbar_init(&sm.k_full[i], 1), mbar_init(&sm.v_full[i], 1);
       for (int i = 0; i < kRing; ++i) {
         mbar_init(&sm.job_full[i], 1);
         mbar_init(&sm.job_empty[i], 10);   // copies, products, four warps that look V through, four of a stream
@@ -560,10 +562,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     int entry_v = -1, entry_k = -1, entry_next = kJoined && n > 0 ? lookup(tile0) : -1;
     const int u0 = kJoined ? static_cast<int>(blockIdx.x) / p.joined % heads : 0;
     for (int i = 0; i < 2 * n && ok; ++i) {
-      // K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1)
-      const bool is_v = i > 0 && ((i & 1) == 0 || i == 2 * n - 1);
-      const int g = i == 0 ? 0 : is_v ? (i == 2 * n - 1 ? n - 1 : i / 2 - 1) : (i + 1) / 2;
-      const int at = g % kRing, slot = i % kSlots;
+      const paged_ring::Copy copy = paged_ring::copy_at(i, n);
+      const bool is_v = copy.is_v;
+      const int g = copy.tile, at = g % kRing, slot = paged_ring::slot_of(i);
+      uint64_t* const full = (is_v ? sm.v_full : sm.k_full) + paged_ring::barrier_of(g);
       if (is_v == kJoined) ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);   // (joined: for the arrival below alone)
       if (ok && i >= kSlots) ok = warp_wait(&sm.empty[slot], (i / kSlots - 1) & 1, &sm.abort);
       if (!ok) break;
@@ -593,9 +595,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
         q_issued = unit + 1;
       }
-      if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], kTileBytes);
+      if (lane == 0) mbar_arrive_expect_tx(full, kTileBytes);
       __syncwarp();
-      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], &sm.full[slot], key0, entry, h, p.Hkv, p.page_log2, lane);
+      copy_tile(is_v ? &tm_v : &tm_k, sm.kv[slot], full, key0, entry, h, p.Hkv, p.page_log2, lane);
       __syncwarp();
       if (is_v && lane == 0) mbar_arrive(&sm.job_empty[at]);
       issued = i + 1;
@@ -606,7 +608,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     }
     // every copy lands before the CTA's shared memory is released, whatever the other roles did
     if (lane == 0) {
-      for (int f = max(0, issued - kSlots); f < issued; ++f) mbar_wait(&sm.full[f % kSlots], (f / kSlots) & 1, nullptr);
+      for (int f = max(0, issued - kSlots); f < issued; ++f) {
+        const paged_ring::Copy copy = paged_ring::copy_at(f, n);
+        mbar_wait((copy.is_v ? sm.v_full : sm.k_full) + paged_ring::barrier_of(copy.tile), paged_ring::phase_of(copy.tile) & 1, nullptr);
+      }
       for (int f = max(0, q_issued - kQ); f < q_issued; ++f) mbar_wait(&sm.q_full[f % kQ], (f / kQ) & 1, nullptr);
     }
   } else if (warp == kRowsMmaWarp) {
@@ -625,13 +630,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         if (done) tc_fence_after_sync();
         return done;
       };
-      const auto k_load = [](int g) { return g == 0 ? 0 : 2 * g - 1; };   // number of a tile's copy
       bool ok = true;
       int unit = -1;   // of the last S
       // S^T[g & 1] = K(tile g) . Q^T
       const auto issue_s = [&](int g) {
-        const int at = g % kRing, i = k_load(g), slot = i % kSlots;
-        ok = wait(&sm.job_full[at], g / kRing) && wait(&sm.full[slot], i / kSlots);
+        const int at = g % kRing, slot = paged_ring::slot_of(paged_ring::copy_of_k(g));
+        ok = wait(&sm.job_full[at], g / kRing) && wait(&sm.k_full[paged_ring::barrier_of(g)], paged_ring::phase_of(g));
         if (!ok) return;
         if (sm.job[at].first) {
           ++unit;
@@ -650,8 +654,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       for (int g = 0; g < 2 && g < n && ok; ++g) issue_s(g);
       int in_unit = 0;   // the tile's number in its unit
       for (int g = 0; g < n && ok; ++g, ++in_unit) {
-        const int at = g % kRing, i = g == n - 1 ? 2 * n - 1 : 2 * g + 2, slot = i % kSlots, s = g & 1;
-        ok = wait(&sm.full[slot], i / kSlots) && wait(&sm.v_clean[at], g / kRing) && wait(&sm.p_full[s], g >> 1);
+        const int at = g % kRing, slot = paged_ring::slot_of(paged_ring::copy_of_v(g, n)), s = g & 1;
+        ok = wait(&sm.v_full[paged_ring::barrier_of(g)], paged_ring::phase_of(g)) && wait(&sm.v_clean[at], g / kRing) && wait(&sm.p_full[s], g >> 1);
         if (!ok) break;
         if (sm.job[at].first) in_unit = 0;
         const bool last = sm.job[at].last != 0;
@@ -680,11 +684,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     // ---------------- V rows that are not finite (thread = key) ----------------
     const int key = tid - kScreenWarp * 32;
     bool ok = true;
-    int waited = 0;   // every copy is waited for, in their order: a slot's barrier tells a copy from the one before it alone
     for (int g = 0; g < n; ++g) {
-      const int at = g % kRing, i = g == n - 1 ? 2 * n - 1 : 2 * g + 2, slot = i % kSlots;
-      ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort);
-      for (; waited <= i && ok; ++waited) ok = warp_wait(&sm.full[waited % kSlots], (waited / kSlots) & 1, &sm.abort);
+      const int at = g % kRing, slot = paged_ring::slot_of(paged_ring::copy_of_v(g, n));
+      ok = warp_wait(&sm.job_full[at], (g / kRing) & 1, &sm.abort) &&
+           warp_wait(&sm.v_full[paged_ring::barrier_of(g)], paged_ring::phase_of(g) & 1, &sm.abort);
       if (!ok) break;
       uint32_t bad = 0;
       if (sm.job[at].partial) {
