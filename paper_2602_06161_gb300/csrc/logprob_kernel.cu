@@ -21,7 +21,7 @@
 // pair is not behind it, and those are among the K threads in front. Their vectors are read again, the kept ones alone where the others'
 // largest element is behind the bound, and the elements that are not behind it are ranked by counting. What passes the bound is little
 // more than K, whatever ties there are (a row of equal logits: the first K vectors). A row whose K best crowd in a few threads may
-// pass more than kMaxFound: then the K best are taken one after the other, a walk over the row each.
+// pass more than kMaxFound: then its vectors are all looked at again, once, and the bound rises with what is found.
 //
 // Bound by memory, and not far from it by the special-function units (an exponential an element: 56 us of the 76 that reading 2048 x
 // 126464 bf16 takes). A CTA's warps have parts: six add up; one keeps a ring of three 12 KB pieces of the row's whole vectors filled by
@@ -93,6 +93,10 @@ struct Vec16<__nv_bfloat16> {
     const uint32_t u = __float_as_uint(x), h = (x < 0.0f ? u + 0xffffu : u) >> 16;
     return h | (h << 16);
   }
+  static __device__ __forceinline__ float at(const uint4& r, int e) {
+    const uint32_t w = e < 4 ? (e < 2 ? r.x : r.y) : (e < 6 ? r.z : r.w);
+    return __uint_as_float((e & 1) != 0 ? w & 0xffff0000u : w << 16);
+  }
   static __device__ __forceinline__ float value(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __forceinline__ __nv_bfloat16 from(float v) { return __float2bfloat16_rn(v); }
 };
@@ -117,6 +121,7 @@ struct Vec16<float> {
     return fmax3(__uint_as_float(r.x), __uint_as_float(r.y), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
   }
   static __device__ __forceinline__ uint32_t floor_of(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ float at(const uint4& r, int e) { return __uint_as_float(e < 2 ? (e < 1 ? r.x : r.y) : (e < 3 ? r.z : r.w)); }
   static __device__ __forceinline__ float value(float v) { return v; }
   static __device__ __forceinline__ float from(float v) { return v; }
 };
@@ -349,6 +354,83 @@ __device__ __forceinline__ void rank_keys(const unsigned long long* from, int n,
     for (int o = 0; o < n; ++o) rank += from[o] > key ? 1 : 0;
     if (rank < K) to[rank] = key;
   }
+}
+
+// The K best of a part's elements, where more of them than are ranked at once are not below `least` (-inf: any may be). One walk over the part's
+// vectors, by a warp: what is not behind the bound is kept, and where there may be no room for the next vectors' the bound rises to one
+// that K of the kept, or little more, are not behind. However the logits lie, that is one look at each and at most one rise for 192 kept. (A walk for
+// each alternative takes K times as long, and in rows of several million logits longer than the other warps wait.) Returns how many are in `found`.
+constexpr int kKept = 512;
+static_assert(kKept <= kMaxFound && kKept >= kMaxTopLogprob + 256, "room for a vector a lane behind those that stay");
+template <typename T>
+__device__ __forceinline__ int find_crowded(const Row<T>& row, int part, int parts, int K, float least, unsigned long long* found) {
+  using V16 = Vec16<T>;
+  constexpr int N = V16::kN;
+  const int2 w = row.part(part, parts);
+  const int lane = threadIdx.x & 31, most = min(K + K / 4, kMaxTopLogprob);
+  const uint32_t before = (1u << lane) - 1u;
+  unsigned long long bound = least == -INFINITY ? 0 : static_cast<unsigned long long>(ordered(least)) << 32;
+  int n = 0;
+  const auto rise = [&] {
+    __syncwarp();
+    // the bound is one of the keys (no two are the same), tried in turn: from one that the middle of the lanes holds between those that let
+    // too many through and those that let too few
+    unsigned long long above = ~0ull, key = found[n / 2];
+    for (int here = n; here > most;) {
+      int c = 0;
+      unsigned long long low = 0, high = 0;
+#pragma unroll 1
+      for (int k = lane; k < n; k += 32) {
+        const unsigned long long x = found[k];
+        c += x >= key ? 1 : 0;
+        if (x > key && x < above) high = x;
+        if (x < key && x > bound) low = x;
+      }
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (c >= K) bound = key, here = c;
+      else above = key;
+      const unsigned long long mine = c >= K ? high : low;
+      const uint32_t lanes = __ballot_sync(0xffffffffu, mine != 0);
+      const uint32_t middle = __ballot_sync(0xffffffffu, mine != 0 && __popc(lanes & before) == __popc(lanes) / 2);
+      key = __shfl_sync(0xffffffffu, mine, __ffs(middle) - 1);
+    }
+    least = from_ordered(static_cast<uint32_t>(bound >> 32));
+    const int all = n;
+    n = 0;
+    for (int k = 0; k < all; k += 32) {
+      const unsigned long long key = k + lane < all ? found[k + lane] : 0;
+      const bool in = key >= bound && key != 0;
+      const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+      if (in) found[n + __popc(lanes & before)] = key;   // (a place that has been read)
+      n += __popc(lanes);
+      __syncwarp();
+    }
+  };
+  const auto keep = [&](bool there, const uint4& raw, int i) {   // a vector a lane
+    const bool some = there && !(V16::top(raw) < least);
+    if (!__any_sync(0xffffffffu, some)) return;
+    if (n > kKept - 32 * N) rise();
+#pragma unroll 1
+    for (int e = 0; e < N; ++e) {
+      const uint32_t j = static_cast<uint32_t>(i) * N + e - row.skip;   // (above V where it is another row's)
+      const unsigned long long key = key_of(V16::at(raw, e), j);
+      const bool in = some && key >= bound && j < static_cast<uint32_t>(row.V);
+      const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+      if (in) found[n + __popc(lanes & before)] = key;
+      n += __popc(lanes);
+    }
+  };
+  const int end = lane == 0 ? 0 : row.n_vecs - 1;
+  const bool is_end = lane < 2 && row.is_end(end, lane, part, parts);
+#pragma unroll 1
+  for (int i0 = w.x;; i0 += 32) {
+    const bool ends = i0 >= w.y, there = ends ? is_end : i0 + lane < w.y;
+    const int i = ends ? end : i0 + lane;
+    keep(there, there ? row.load(i) : make_uint4(0, 0, 0, 0), i);
+    if (ends) break;
+  }
+  __syncwarp();
+  return n;
 }
 
 template <typename T, Best kBest>
@@ -711,33 +793,17 @@ __global__ void __launch_bounds__(kFwdThreads, 4) logprob_fwd_kernel(const __gri
           if (row.is_end(end, lane, part, p.parts)) look(row.load_end(end), end);
         }
         __syncwarp();
-        const int n = sm.n_found;
-        if (n <= kMaxFound) {
-          rank_keys(sm.found, n, K, sm.best, lane);
-        } else {
-          unsigned long long last = ~0ull;
-          for (int k = 0; k < K; ++k) {
-            unsigned long long top = 0;
-            const auto see = [&](const uint4& raw, int i) {
-              float x[N];
-              V16::unpack(raw, x);
-#pragma unroll
-              for (int e = 0; e < N; ++e) {
-                const unsigned long long key = key_of(x[e], static_cast<uint32_t>(i * static_cast<long long>(N) + e - row.skip));
-                if (row.has(i, e) && key < last && key > top) top = key;
-              }
-            };
-            for (int i = w.x + lane; i < w.y; i += 32) see(__ldg(row.base + i), i);
-            if (lane < 2) {
-              const int end = lane == 0 ? 0 : row.n_vecs - 1;
-              if (row.is_end(end, lane, part, p.parts)) see(row.load_end(end), end);
-            }
-            const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(top >> 32));
-            const uint32_t low = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(top >> 32) == hi ? static_cast<uint32_t>(top) : 0u);
-            last = (static_cast<unsigned long long>(hi) << 32) | low;
-            if (lane == 0) sm.best[k] = last;
-          }
+        int n = sm.n_found;
+        if (__builtin_expect(n > kMaxFound, 0)) {
+          // (the row is put together anew from numbers that the compiler does not know again: kept over this walk, it spilled registers where every
+          // row passes, and 2048 rows of 126464 with 8 alternatives took 92 us, not 90)
+          long long again = r;
+          int V = p.V;
+          asm volatile("" : "+l"(again), "+r"(V));
+          const Row<T> same(static_cast<const T*>(p.logits), again, V);
+          n = find_crowded(same, part, p.parts, K, bound == 0 ? -INFINITY : bound_value, sm.found);
         }
+        rank_keys(sm.found, n, K, sm.best, lane);
       }
       __syncwarp();
       if (p.parts == 1) write(r);
