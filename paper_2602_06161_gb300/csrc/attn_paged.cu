@@ -239,15 +239,13 @@ __device__ __forceinline__ void join_rows(const Params& p, uint32_t staged, uint
 #pragma unroll
     for (int d = kMaxJoined; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     l = __shfl_sync(0xffffffffu, l, 0);
+    // (every part counts, those of weight zero too: a value that is not finite makes its column NaN there)
     const float w_own = __shfl_sync(0xffffffffu, w, kMaxJoined);
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (w_own != 0.0f) acc = make_float4(w_own * own.x, w_own * own.y, w_own * own.z, w_own * own.w);
+    float4 acc = make_float4(w_own * own.x, w_own * own.y, w_own * own.z, w_own * own.w);
 #pragma unroll
     for (int k = 0; k < kMaxJoined; ++k) {
       const float wk = __shfl_sync(0xffffffffu, w, k);
-      if (wk != 0.0f) {   // (a part that saw no key holds anything)
-        acc.x = fmaf(wk, x[k].x, acc.x), acc.y = fmaf(wk, x[k].y, acc.y), acc.z = fmaf(wk, x[k].z, acc.z), acc.w = fmaf(wk, x[k].w, acc.w);
-      }
+      acc.x = fmaf(wk, x[k].x, acc.x), acc.y = fmaf(wk, x[k].y, acc.y), acc.z = fmaf(wk, x[k].z, acc.z), acc.w = fmaf(wk, x[k].w, acc.w);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     reinterpret_cast<uint2*>(p.out + (orow0 + row) * kD)[lane] =
@@ -715,7 +713,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const uint32_t staged = smem_u32(sm.kv[0]);   // joined: every copy and product is complete by then
     bool ok = true;
     int g = 0;
-    if (n == 0 && tid < kN) sm.ml[tid] = make_float2(-INFINITY, 0.0f);
+    if (n == 0) {   // joined: a part without keys
+      if (tid < kN) sm.ml[tid] = make_float2(-INFINITY, 0.0f);
+      if (kJoined)
+        for (int i = tid; i < kN * kD / 4; i += 2 * kBN) sts128(staged + 16 * i, 0, 0, 0, 0);
+    }
     for (int first_unit = 0, o_waits = 0; g < n;) {
       // Units of one tile, two in turn, are done by a stream each at the same time.
       ok = warp_wait(&sm.unit_full[first_unit % kUnits], (first_unit / kUnits) & 1, &sm.abort);
@@ -944,7 +946,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           else if (p.lse != nullptr) p.lse[orow0 + key] = (top + lg2_approx(sum)) * 0.6931471805599453f;
         }
         sync_unit();
-        // thread = output column; the streams' warps take four rows in turn
+        // thread = output column; the streams' warps take four rows in turn. Whose accumulators hold products of this unit: with two tiles and more
+        // both streams', else the tile's (g is the one behind it).
+        const bool has0 = alone ? stream == 0 : nt > 1 || (g & 1) == 1, has1 = alone ? stream == 1 : nt > 1 || (g & 1) == 0;
 #pragma unroll 1
         for (int c0 = alone ? 0 : 4 * stream; c0 < n_rows; c0 += alone ? 4 : 8) {
           uint32_t o[2][4];
@@ -957,9 +961,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             const int i = c0 + e;
             if (i >= n_rows) break;
             const float4 f = fin[i];
-            float x = f.x == 0.0f ? 0.0f : __uint_as_float(o[0][e]) * f.x;
-            if (f.y != 0.0f) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
-            if (f.z != 0.0f) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + sm.row[buf][i].w) * kD + key]), x);
+            // (a weight of zero counts too: a value that is not finite makes its column NaN there)
+            float x = has0 ? __uint_as_float(o[0][e]) * f.x : 0.0f;
+            if (has1) x = fmaf(__uint_as_float(o[1][e]), f.y, x);
+            if (own_rows) {
+              const int4 row = sm.row[buf][i];
+              if (row.z >= 0) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + row.w) * kD + key]), x);
+            }
             if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
             else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
             else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
@@ -1603,7 +1611,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     sm.red[tile][half][R] = l_run;
     sync_of<256>(2 + tile);
     float m = m_run, l = sm.red[tile][0][R] + sm.red[tile][1][R], w = 1.0f, p_self = 0.0f;
-    if (l == 0.0f) m = -INFINITY, w = 0.0f;     // no key was seen
+    if (l == 0.0f) m = -INFINITY;               // no key was seen
     if (s_self != -INFINITY && !p.joined) {
       const float m_all = fmaxf(m, s_self);
       const float f = m == -INFINITY ? 0.0f : ex2_approx(m - m_all);
@@ -1639,10 +1647,10 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
           tmem_ld32(o_addr + 32 * c, x);
           tmem_ld_wait(x);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = w == 0.0f ? 0.0f : __uint_as_float(x[e]) * w;
+          for (int e = 0; e < 32; ++e) o[e] = some_keys ? __uint_as_float(x[e]) * w : 0.0f;   // (what a row without keys has here may be NaN)
         }
         const int col = half * kHalf + 32 * c;
-        if (p_self != 0.0f) add_self(o, p_self, p.v_seedmask + self * kD + col);
+        if (own_here && is_seed && !p.joined) add_self(o, p_self, p.v_seedmask + self * kD + col);
         if (p.joined) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
