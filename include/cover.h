@@ -397,8 +397,8 @@ int cover_paged_append(const void* k, const void* v, const void* q, void* q_out,
  *   softcap 0, or c > 0: every score s = q . k / sqrt(D), a seed's own too, becomes c tanh(s / c) (c above 2^60 counts as
  *     2^60, c below 2^-30 as 2^-30).
  * What a row does not see does not reach it, NaN included: rows of a page behind a sequence's length may hold anything.
- * A row that sees an element of V that is not finite has no finite number in that column at least. Scores and sums are fp32: they hold
- * where the values seen are at most 2^100 in magnitude, and 2^66 / Lk with a cap.
+ * A row that sees an element of V that is not finite has no finite number in that column at least, be its weight 0 in fp32, and its lse is
+ * as without it. Scores and sums are fp32: they hold where the values seen are at most 2^100 in magnitude, and 2^66 / Lk with a cap.
  * workspace: cover_attn_paged_workspace_bytes bytes, 16-byte aligned, no initialisation needed (NULL if that is 0): scratch of the
  * call alone; calls that share one must not run concurrently on the GPU. The inputs must not alias out, lse or workspace.
  * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hq, Hkv, Lq, M or n_pages < 1, Hq % Hkv != 0, n_seeds < 0, a

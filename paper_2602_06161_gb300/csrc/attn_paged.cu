@@ -18,8 +18,9 @@
 //
 // What no row sees must not reach the sums: scores are taken out by selection, but a weight of zero times a value that is not finite
 // is NaN. KV tiles of which some row does not see some key (the last one of a sequence, diagonals, windows, seeds' own
-// columns) are looked through: a V row with an element that is not finite is set to zeros and reported, and the sums of the rows that see
-// it are made NaN instead. Tiles that all rows see whole are not (there the products give what they give).
+// columns) are looked through: a V row with an element that is not finite is set to zeros and reported, and the outputs of the rows that see
+// it are made NaN instead. Tiles that all rows see whole are not (there the products give what they give). Sums and lse, which are of Q and K
+// alone, stay what they are.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -314,6 +315,7 @@ struct RowsSmem {
   float4 fin[2][kN];         // weights of the two accumulators and of the masked-input value, 1 / l
   float m[2][kN], step[2][kN], factor[2][kN];
   int unseen[2][kN], any_unseen[2];
+  int bad[2][kN];            // whether the row sees a V row that was set to zeros
   float red[2][4][kN];
   float s_self[2][kN];
   int slot[kN];
@@ -750,6 +752,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (key < kN) {
         sm.m[stream][key] = 0.0f;
         sm.unseen[stream][key] = key < n_rows ? 1 : 0;
+        sm.bad[stream][key] = 0;
         if (key == 0) sm.any_unseen[stream] = 1;
         if (leads) s_self_of[key] = -INFINITY;
       }
@@ -887,7 +890,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         tc_fence_before_sync();
         mbar_arrive(&sm.p_full[stream]);
         if (partial) {
-          // V has been looked through by now: the rows that see a row of it that is not finite have a sum of NaN
+          // V has been looked through by now: the rows that see a row of it that is not finite are NaN
           ok = warp_wait(&sm.v_clean[at], (g / kRing) & 1, &sm.abort);
           if (ok && ((reinterpret_cast<const uint32_t*>(&sm.nan_keys[at])[key >> 5] >> (key & 31)) & 1u) != 0) {
             const int pos = sm.job[at].key0 + key;
@@ -895,7 +898,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
               const int4 row = sm.row[buf][i];
-              if (held && pos >= row.x && pos < row.y && pos != row.z) l[i] = kNan;
+              if (held && pos >= row.x && pos < row.y && pos != row.z) sm.bad[stream][i] = 1;
             }
           }
           __syncwarp();
@@ -940,7 +943,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           float sum = fmaf(f0, l2[0], fmaf(f1, l2[1], p_self));
           if (l2[0] != l2[0] || l2[1] != l2[1]) sum = l2[0] + l2[1];
           if (s_self != s_self) sum = s_self;
-          fin[key] = make_float4(f0, f1, p_self, place != -1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
+          const bool bad = alone ? sm.bad[stream][key] != 0 : (sm.bad[0][key] | sm.bad[1][key]) != 0;
+          fin[key] = make_float4(f0, f1, p_self, bad ? kNan : place != -1 ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum);
           if (place == -2) sm.ml[key] = make_float2(top, sum);
           else if (place >= 0) p.part_ml[static_cast<size_t>(place) * kN + key] = make_float2(top, sum);
           else if (p.lse != nullptr) p.lse[orow0 + key] = (top + lg2_approx(sum)) * 0.6931471805599453f;
@@ -968,9 +972,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
               const int4 row = sm.row[buf][i];
               if (row.z >= 0) x = fmaf(f.z, __bfloat162float(p.v_seedmask[(masked0 + row.w) * kD + key]), x);
             }
+            x *= f.w;
             if (place == -2) sts32(staged + staged_at(i, key >> 2) + 4 * (key & 3), __float_as_uint(x));
             else if (place >= 0) p.part_o[(static_cast<size_t>(place) * kN + i) * kD + key] = x;
-            else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x * f.w);
+            else p.out[(orow0 + i) * kD + key] = __float2bfloat16_rn(x);
           }
           __syncwarp();
         }
@@ -1476,19 +1481,20 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const int jend = tile == 1 && !two_tiles ? 0 : nt;
     // Where some row does not see some key, V is looked through for rows that are not finite while the scores are waited for: a warp eight
     // keys, or sixteen (a warp for all of it took a tile 1.5 us). What was found is read a tile later.
+    bool bad = false;   // the row sees a V row that was set to zeros
     const auto found = [&](int j) {
       if (!warp_wait(&sm.v_clean[j & 1], (j >> 1) & 1, &sm.abort)) {
         ok = false;
         return;
       }
-      // a row that sees one of these keys has a sum of NaN (both threads of it look, for all 128)
+      // a row that sees one of these keys is NaN (both threads of it look, for all 128)
       const uint4 nan = sm.nan_keys[j & 3];
       if ((nan.x | nan.y | nan.z | nan.w) == 0) return;
 #pragma unroll 1
       for (int w = 0; w < 4; ++w) {
         for (uint32_t bits = w == 0 ? nan.x : w == 1 ? nan.y : w == 2 ? nan.z : nan.w; bits != 0; bits &= bits - 1) {
           const int at = (j0 + j) * kBN + 32 * w + __ffs(bits) - 1;
-          if (at >= row_lo && at < row_hi && !(is_seed && at == pos)) l_run = kNan;
+          bad |= at >= row_lo && at < row_hi && !(is_seed && at == pos);
         }
       }
     };
@@ -1625,6 +1631,7 @@ __global__ void __launch_bounds__(kPairsThreads, 1)
     const long long orow = rowbase + P;
     const bool split = p.nsplit > 1;
     const float inv = split ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);   // 1 / l, once a row; zero where no key was seen
+    if (bad) w = kNan;
     const uint32_t staged = smem_u32(sm.q[0]);   // joined: every product is complete, Q and K are not read any more
     // A warp's 32 rows of 128 bytes are turned in shared memory, where Q was, so that it stores whole lines (each thread its own row, 16 bytes
     // at a time: 3.6 us a CTA).

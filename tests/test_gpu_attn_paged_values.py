@@ -96,3 +96,21 @@ def test_the_call_itself():
         out, lse = _run(d)
         rest = [c for c in range(128) if c != COLUMN]
         assert not out[..., COLUMN].isfinite().any() and torch.equal(out[..., rest], ref[..., rest]) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("mode,parts", WAYS)
+@pytest.mark.parametrize("Lq,cap", [(1, 0.0), (5, 0.0), (5, 30.0), (40, 0.0)])
+def test_lse_is_of_queries_and_keys_alone(mode, parts, Lq, cap):
+    """Values that are not finite in KV tiles which some row does not see whole, beside which others are seen: lse stays what it is."""
+    d = _inputs([700, 300], 4, 2, Lq, 3, 32, junk=False)
+    hi = _ints([[650 - 3 * r for r in range(Lq)], [290 - r if r % 2 == 0 else 60 for r in range(Lq)]])
+    ref, ref_lse = _forced(d, mode, parts, key_hi=hi, softcap=cap)
+    assert ref_lse.isfinite().all()
+    for value in (math.nan, math.inf, -math.inf):
+        for b, key in ((0, 520), (0, 3), (1, 257)):
+            d["vp"][int(d["table"][b, key // 32]), :, key % 32, COLUMN] = value
+        out, lse = _forced(d, mode, parts, key_hi=hi, softcap=cap)
+        assert torch.equal(lse, ref_lse)
+        sees = torch.stack([hi[0] > 3, hi[1] > 257])
+        assert not out.transpose(1, 2)[sees][..., COLUMN].isfinite().any()
+        assert torch.equal(out.transpose(1, 2)[~sees], ref.transpose(1, 2)[~sees])
