@@ -373,7 +373,8 @@ int cover_attn_fwd_prefix8(const void* q, const void* k8, const void* v8,
  *     k_out where the program needs the rows besides (the seeds' masked-input rows)
  *   inv_freq [R / 2], interleaved, mscale: as in cover_rope_fwd (R = 0: nothing turns); k and q turn by rope_pos[b, s] (int32
  *     [B, n]), or by the row's position in the memory where it is NULL. Rows are turned in fp32 and rounded once.
- * k, v and q must overlap neither the pages nor the outputs. n = 0 is a no-op.
+ * k, v and q must overlap neither the pages nor the outputs, and k_pages not v_pages (the Python call refuses what overlaps the
+ * pages). n = 0 is a no-op.
  * Errors: COVER_ERR_INVALID_ARG for a NULL required pointer, B, Hkv, D, M or n_pages < 1, Hq or n < 0, R odd, negative or above
  * D, elem_bytes not 2 or 4, neither or both of start and pos, count with pos, a pointer that is not aligned to its elements (the pages:
  * to 16 bytes); COVER_ERR_UNSUPPORTED for D other than 64 and 128, another page, M * page >= 2^31; COVER_ERR_CUDA for a

@@ -735,6 +735,14 @@ def _pages_need(k_pages, v_pages, table):
     _same_device(k_pages.device, v_pages=v_pages, table=table)
 
 
+def _pages_apart(k_pages, v_pages, **inputs):
+    """Refuses pages that are written where another of the tensors lies."""
+    for name, pages, others in (("k_pages", k_pages, {"v_pages": v_pages, **inputs}), ("v_pages", v_pages, inputs)):
+        for other, t in others.items():
+            if t is not None and _overlap(pages, t):
+                raise ValueError(f"{name} must not overlap {other}")
+
+
 def _ints_need(shape, device, **tensors):
     for name, t in tensors.items():
         if t is not None:
@@ -752,7 +760,7 @@ def cover_paged_append(k, v, k_pages, v_pages, table, *, start=None, count=None,
 
     Row s of sequence b goes to position start[b] + s where s < count[b] (int32 [B]; all rows where count is None), or to pos[b, s]
     (int32 [B, n]; of rows that name one position the lowest is taken). table: int32 [B, M], the sequences' pages; a position without
-    one is left out. inv_freq: fp64 [R / 2] (rope_frequencies; None: nothing turns), with ``interleaved`` and ``mscale`` as in
+    one is left out. None of the tensors may share a byte with the pages, nor k_pages with v_pages. inv_freq: fp64 [R / 2] (rope_frequencies; None: nothing turns), with ``interleaved`` and ``mscale`` as in
     cover_rope_fwd. rope_pos: int32 [B, n], positions to turn by where they are not those in the memory.
     """
     if stream is None and type(mscale) is float:
@@ -785,6 +793,7 @@ def cover_paged_append(k, v, k_pages, v_pages, table, *, start=None, count=None,
         R = 2 * inv_freq.shape[0]
         if R > D:
             raise ValueError("inv_freq must have at most D / 2 entries")
+    _pages_apart(k_pages, v_pages, table=table, k=k, v=v, q=q, start=start, count=count, pos=pos, rope_pos=rope_pos, inv_freq=inv_freq)
     make = _maker(stream, dev)
     q_out = None if q is None else make(q.shape, q.dtype)
     k_out = make(k.shape, k.dtype) if want_k else None

@@ -614,6 +614,18 @@ struct Pages {
   }
 };
 
+// The bytes from a tensor's first element to its last.
+struct Span {
+  uintptr_t from, to;
+  explicit Span(const Tensor& t) : from(reinterpret_cast<uintptr_t>(t.data_ptr())), to(from) {
+    if (t.numel() == 0) return;
+    int64_t last = 0;
+    for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
+    to += static_cast<uintptr_t>(last + 1) * t.element_size();
+  }
+  bool apart(const Span& o) const { return to <= o.from || o.to <= from; }
+};
+
 // An optional int32 [B] or [B, n] (n < 0: the former), a float [N] with dtype.
 const int32_t* ints(Args& in, PyObject* o, int B, int n = -1) {
   if (none(o)) return nullptr;
@@ -658,6 +670,15 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int inter = in.truth(a[11]) ? 1 : 0;
     const float mscale = static_cast<float>(in.real(a[12]));
     const bool want_k = in.truth(a[13]);
+    if (!in.ok) return nullptr;
+    // pages that may lie where another tensor does: the caller looks closer
+    const Span kp(THPVariable_Unpack(a[2])), vp(THPVariable_Unpack(a[3]));
+    in.need(kp.apart(vp));
+    for (const int i : {0, 1, 4, 5, 6, 7, 8, 9, 10}) {
+      if (none(a[i])) continue;
+      const Span s(THPVariable_Unpack(a[i]));
+      in.need(s.apart(kp) && s.apart(vp));
+    }
     if (!in.ok) return nullptr;
     int64_t st[9];
     strides_of(k, st);
