@@ -812,20 +812,8 @@ def cover_attn_paged_workspace_bytes(B: int, Hq: int, Hkv: int, Lq: int, M: int,
     return int(_lib.load().cover_attn_paged_workspace_bytes(*sizes))
 
 
-def cover_attn_fwd_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0=None, key_lo=None,
-                         key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True, workspace=None, stream=None):
-    """cover_attn_fwd_prefix over a memory in pages. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
-
-    table: int32 [B, M], the sequences' pages; lens: int32 [B], their keys. q0: int32 [B], the position of each sequence's
-    first query row (needed with seeds). key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees of its
-    sequence's (all where None; none: out 0, lse -inf). softcap c > 0: scores become c tanh(score / c). workspace: uint8, at
-    least cover_attn_paged_workspace_bytes, scratch of the call; allocated where None.
-    """
-    if stream is None and type(softcap) is float:
-        r = (_nat or _native()).attn_paged(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
-                                           softcap, out, lse, want_lse, workspace)
-        if r is not None:
-            return _done("cover_attn_fwd_paged", r)
+def _paged_need(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi):
+    """Checks the inputs; returns the number of seeds."""
     _need(q, "q", torch.bfloat16, 4)
     _pages_need(k_pages, v_pages, table)
     B, Hq, Lq, D = q.shape
@@ -849,6 +837,28 @@ def cover_attn_fwd_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_se
         raise TypeError("lens must be a torch.Tensor")
     _ints_need((B,), dev, lens=lens, q0=q0)
     _ints_need((B, Lq), dev, key_lo=key_lo, key_hi=key_hi)
+    _same_device(dev, k_pages=k_pages)
+    return S
+
+
+def cover_attn_fwd_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_seedmask=None, seed_idx=None, *, q0=None, key_lo=None,
+                         key_hi=None, softcap: float = 0.0, out=None, lse=None, want_lse=True, workspace=None, stream=None):
+    """cover_attn_fwd_prefix over a memory in pages. Returns (out [B,Hq,Lq,D] bf16, lse [B,Hq,Lq] f32 or None).
+
+    table: int32 [B, M], the sequences' pages; lens: int32 [B], their keys. q0: int32 [B], the position of each sequence's
+    first query row (needed with seeds). key_lo, key_hi: int32 [B, Lq], the keys [lo, hi) that each row sees of its
+    sequence's (all where None; none: out 0, lse -inf). softcap c > 0: scores become c tanh(score / c). workspace: uint8, at
+    least cover_attn_paged_workspace_bytes, scratch of the call; allocated where None.
+    """
+    if stream is None and type(softcap) is float:
+        r = (_nat or _native()).attn_paged(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi,
+                                           softcap, out, lse, want_lse, workspace)
+        if r is not None:
+            return _done("cover_attn_fwd_paged", r)
+    S = _paged_need(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi)
+    B, Hq, Lq, D = q.shape
+    n_pages, Hkv, page, _ = k_pages.shape
+    dev = q.device
     make = _maker(stream, dev)
     if out is None:
         out = make(q.shape, q.dtype)
@@ -870,7 +880,7 @@ def cover_attn_fwd_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_se
             raise ValueError(f"workspace must have at least {nbytes} bytes")
     elif nbytes:
         workspace = make(nbytes, torch.uint8)
-    _same_device(dev, k_pages=k_pages, out=out, lse=lse, workspace=workspace)
+    _same_device(dev, out=out, lse=lse, workspace=workspace)
     _launch("cover_attn_fwd_paged", dev, stream,
             (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), n_pages, M, page, _ptr(lens), _ptr(k_seedmask) if S else None,
              _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, _ptr(q0), B, Hq, Hkv, Lq, D,
@@ -1174,13 +1184,15 @@ def cover_debug_attn_paged(q, k_pages, v_pages, table, lens, k_seedmask=None, v_
                            parts: int = 1, key_lo=None, key_hi=None, softcap: float = 0.0, workspace=None):
     """cover_attn_fwd_paged on the kernel ``mode`` with the keys in ``parts`` parts (mode 2), or on that many CTAs (negative: on clusters of
     -parts CTAs a unit). Returns (out, lse)."""
+    S = _paged_need(q, k_pages, v_pages, table, lens, k_seedmask, v_seedmask, seed_idx, q0, key_lo, key_hi)
     B, Hq, Lq, D = q.shape
     n_pages, Hkv, page, _ = k_pages.shape
-    S = 0 if seed_idx is None else int(seed_idx.shape[1])
     out, lse = torch.empty_like(q), torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
     if workspace is None:
         n = B * Hq * Lq * parts * 520 if mode == 2 else parts * (2 * (16 << mode) * 520 + 16)
         workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+    _need(workspace, "workspace", torch.uint8, 1)
+    _same_device(q.device, workspace=workspace)
     _launch("cover_debug_attn_paged", q.device, None,
             (_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), n_pages, table.shape[1], page, _ptr(lens), _ptr(k_seedmask) if S else None,
              _ptr(v_seedmask) if S else None, _ptr(seed_idx) if S else None, S, _ptr(q0), B, Hq, Hkv, Lq, D,

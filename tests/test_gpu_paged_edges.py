@@ -30,3 +30,21 @@ def test_rows_in_the_pages_are_refused(mscale):
     yq, _ = api.cover_paged_append(rows, rows, *mine, table, start=start, q=q, inv_freq=f, mscale=mscale)
     zq, _ = api.cover_paged_append(k, k, kp, vp, table, start=start, q=q, inv_freq=f, mscale=mscale)
     assert torch.equal(yq, zq) and torch.equal(mine[0], kp) and torch.equal(mine[1], vp) and torch.equal(rows, k)
+
+
+def test_the_debug_attention_call_checks_its_tensors():
+    kp, vp = api.paged_memory(5, 2, 16)
+    q, table, lens = torch.zeros((1, 4, 8, 128), device="cuda", dtype=BF), _ints([[0, 1]]), _ints([20])
+    pair, seeds, q0 = torch.zeros((1, 2, 2, 128), device="cuda", dtype=BF), _ints([[3, 4]]), _ints([2])
+    call = lambda *a, mode=0, **kw: api.cover_debug_attn_paged(*a, mode=mode, **kw)  # noqa: E731
+    for args, kw, what in (((q, kp, vp, table, lens), dict(key_hi=torch.zeros((1, 8), device="cuda", dtype=torch.int64)), "key_hi"),
+                           ((q, kp, vp, table, lens), dict(key_lo=_ints([[0] * 7])), "key_lo"), ((q, kp, vp, table, lens), dict(q0=_ints([0, 0])), "q0"),
+                           ((q, kp, vp, table.expand(2, 2).contiguous(), lens), {}, "table"), ((q, kp, vp, table, _ints([20, 3])), {}, "lens"),
+                           ((q, kp, vp[1:], table, lens), {}, "v_pages"), ((q[..., :64].contiguous(), kp, vp, table, lens), {}, "pages"),
+                           ((q, kp, vp, table, lens, pair[:, :1].contiguous(), pair, seeds), dict(q0=q0), "k_seedmask"),
+                           ((q, kp, vp, table, lens, pair, pair, seeds.expand(2, 2).contiguous()), dict(q0=q0), "seed_idx"),
+                           ((q, kp, vp, table, lens, pair, pair, seeds), {}, "q0"),
+                           ((q, kp, vp, table, lens), dict(workspace=torch.zeros(4096, device="cuda")), "workspace")):
+        for mode in (0, 1, 2):
+            with pytest.raises((TypeError, ValueError), match=what):
+                call(*args, mode=mode, **kw)

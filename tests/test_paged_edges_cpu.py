@@ -21,3 +21,12 @@ def test_pages_that_are_written_lie_apart_from_everything():
                         ((kp, vp, dict(q=flat[2 * 8192 - 1:][:128 * 8].view(1, 2, 8, 64))), "v_pages must not overlap q")):
         with pytest.raises(ValueError, match=match):
             api._pages_apart(*args[:2], **args[2])
+
+
+def test_the_debug_attention_call_checks_its_tensors():
+    kp, vp = api.paged_memory(3, 2, 16, device="cpu")
+    q, i = torch.zeros(1, 4, 2, 128, dtype=BF), lambda *s: torch.zeros(s, dtype=torch.int32)
+    with pytest.raises(ValueError, match="q must be a CUDA tensor"):
+        api.cover_debug_attn_paged(q, kp, vp, i(1, 2), i(1), mode=0)
+    with pytest.raises(TypeError, match="q must be"):
+        api.cover_debug_attn_paged(q.float(), kp, vp, i(1, 2), i(1), mode=0)
