@@ -279,7 +279,8 @@ __device__ __forceinline__ void join_pass() {
 //
 // Roles (512 threads): warps 0-3, 4-7 softmax of the streams; 8-11 look V tiles through; 12 products; 13 copies; 14 lays out what
 // is to be done, tile by tile: pages, masks and rows, up to 8 tiles ahead.
-// Shared memory: five tiles of K or V in the order K0 K1 V0 K2 V1 .., Q of two units, P^T of two streams (rows of 128 bytes).
+// Shared memory: five tiles of K or V in the order K0 K1 V0 K2 V1 .. (paged_ring.cuh), Q of two units, P^T of two streams (rows of 128 bytes).
+// With 32 rows a thread's 32 scores and 32 sums do not fit into its 128 registers beside the rest: 104 to 216 bytes are spilled.
 // Tensor memory: S0 | S1 | O0 | O1, kN columns each.
 constexpr int kRowsThreads = 512;
 constexpr int kScreenWarp = 8, kRowsMmaWarp = 12, kRowsCopyWarp = 13, kRowsPlanWarp = 14;
@@ -1743,8 +1744,10 @@ struct Plan {
 // Clusters of 1 .. 8 CTAs, one CTA an SM, that are resident at once on every GPU measured.
 constexpr int kClusters[kMaxJoined] = {152, 76, 46, 36, 24, 20, 14, 14};
 
-// The kernel and how the keys are shared, from the sizes and the table's width (the lengths are not known to the host: where they are shorter,
-// an even share of all tiles is better than predicted).
+// The kernel and how the keys are shared, from the sizes and the table's width. The lengths are not known to the host, so the plan is that of
+// sequences as long as the table is wide. Shorter ones are right by it, but another plan may be faster: with tables of 131072 positions one
+// token over 777 keys takes 12.3 us (8.5 with a table of its length), 32 rows over 1024 with 32 seeds 24.4 (13.6), 2048 rows over 8192
+// 304 (261) and 136 MB of workspace for four parts (none); a token of 64 sequences of up to 8191 keys 187 (186).
 //
 // Predicted microseconds, fitted to calls back to back on GB300, measured / predicted. Rows of 16 joined: one token over 777 keys (28 / 4 heads,
 // 7 CTAs a unit) 7.6 / 7.7, over 4096 (32 / 8, 8) 12.0 / 11.8, 16 sequences of 500 (1) 12.8 / 13.3, 29 of 51 (1) 16.1 / 16.8. In even shares

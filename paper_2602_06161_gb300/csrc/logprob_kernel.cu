@@ -252,8 +252,9 @@ __device__ __noinline__ Sums careful_sums(const Row<T>& row, int w0, int w1, boo
 
 // Alternatives asked for: none, up to kFewBest, or more. For few the threads' best vectors are enough, and the K best of the threads are taken
 // one after the other. For more, threads with two or three of the best ones are no exception and taking is slow: a thread keeps two vectors
-// and the bound is found by halving. Measured the first / second way, 2048 rows of 126464 bf16: 1 alternative 88 / 97 us, 5 89 / 98, 20 101 / 99,
-// 64 251 / 127; 972 of 25063: 19 / 22, 22 / 23, 27 / 25, 58 / 35; one of 32000: 6.4 / 8.6, 7.5 / 9.5, 11.7 / 8.9, 29 / 17.
+// and the bound is found by halving. Measured the first / second way, 2048 rows of 126464 bf16: 1 alternative 87 / 100 us, 5 88 / 100, 16 94 / 100,
+// 20 102 / 101, 64 251 / 126; 972 of 25063: 19 / 22, 21 / 23, 24 / 24, 26 / 24, 58 / 34; one of 32000: 6.4 / 7.8, 7.5 / 8.3, 10.9 / 8.9, 11.9 / 9.1,
+// 29 / 17. (Single rows would change ways at 8 alternatives, batches do at 20.)
 enum Best { kNone, kFew, kMany };
 constexpr int kFewBest = 16;
 

@@ -10,7 +10,8 @@
 // serve all of them. Four heads are on their way at a time, into places of shared memory that are the thread's own: held in registers it
 // was one head, and too few bytes were in flight. Threads are in the order (block of tokens, chunk of heads, token, column), so that a
 // warp's threads walk over equally many heads.
-// 4 x up to 8191 tokens, 32 + 8 + 8 heads of 128, bf16 (744 MB): 119 us, 6.2 TB/s; 150 us in registers, 127 with the chunks inside of a token.
+// 4 x up to 8191 tokens, 32 + 8 + 8 heads of 128 (744 MB in bf16): 114 us, 6.5 TB/s; pairs of neighbours 124; fp32 rows 209, 6.6 TB/s. With a head
+// held in registers 153, 176 and 232 us; 8 x 63 listed rows gain 0.1 of 4.2 us by that, 64 x 400 lose 16 of 51, so there is one form.
 #include <cuda_bf16.h>
 #include <stdint.h>
 
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 4) paged_append_kernel(const __grid_
     col1 = col0 + (p.D - p.R) / 2;
     two = p.rest_pairs;
   }
-  // heads c, c + step, ...: the chunks' threads, neighbours in a warp, take neighbouring heads
+  // heads c, c + step, ...: at the same turn the chunks of a block of tokens, which lie behind one another, take neighbouring heads
   const int step = t.chunks;
   int n = live ? (t.heads - c + step - 1) / step : 0;
   const T* in = reinterpret_cast<const T*>(t.in) + b * t.in_b + s * t.in_l;
